@@ -308,6 +308,81 @@ bitnet_a48_status bitnet_a48_attention_prefill(const float* q_dev, const float* 
                                                void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Low-bit attention over a paged cache (Section 3, low-bit attention paragraph, for serving: sequences of any length
+ * share a pool of pages, key/value heads may be shared by several query heads, a batch mixes prompts and single tokens).
+ * The layer between the q/k/v BitLinears and the output BitLinear is then: bitnet_a48_paged_write (rotates q and k,
+ * quantises k and v into the pages) and bitnet_a48_attention_paged.
+ *
+ * The cache.  bits 8, 4 or 3; with 3 the heads at position 0 of a sequence keep 4 bits (the bos token).  A head vector x
+ * is stored as Eq. 3 with `bits` in place of 8: gamma = max|x|, L = 2^(bits-1) - 1, q = RoundClip(L/(gamma+eps)*x, -(L+1),
+ * L), and stands for (gamma/L)*q, gamma/L kept as fp32.  head_dim: a multiple of 4, at most 128; page_size: 16, 32, 64 or
+ * 128 positions.  The pool is bitnet_a48_paged_cache_bytes(cache) bytes of device memory, [n_pages][n_kv_heads] chunks of
+ *   key codes [page_size][row] | value codes [page_size][row] | key scales fp32 [page_size] | value scales fp32 [page_size]
+ *   | with 3 bits only: the 4-bit codes of key and value at position 0, 2 x P/2 bytes
+ * with P = head_dim padded to a multiple of 32, row = P*bits/8, an entry stored as the unsigned q + L + 1 (padding as 0's
+ * code): 8 bits one byte per entry; 4 bits entry 2i in the low half of byte i; 3 bits 32 entries in three little-endian
+ * words, entries 5j..5j+4 in bits 0..14 of the low half of word j, entry 15 in the three top bits of the low halves, entries
+ * 16..31 the same way in the high halves.  Pages carry no other state: a pool may be copied, and a page may serve several
+ * sequences (a shared prefix) as long as no call writes to it twice.
+ *
+ * The batch.  Sequence b has the new tokens q_start[b] .. q_start[b+1]-1 of the call's packed token rows (q_start ascending,
+ * n_seqs + 1 values; a sequence may have none) and kv_len[b] positions with them: token i of sequence b is at position
+ * kv_len[b] - (q_start[b+1] - q_start[b]) + i, and position p sits in slot p % page_size of page pages[b][p / page_size].
+ * The three arrays are device memory (4-byte aligned), read when the call runs: a captured graph may be replayed with other
+ * contents.  n_tokens: rows of the token arrays, rows outside q_start[0] .. q_start[n_seqs]-1 are neither read nor written.
+ * max_q, max_kv: upper bounds of the new tokens and of the positions of one sequence; they size the launch.  More than
+ * max_q new tokens of a sequence: those past max_q get no attention output.  A position without a page (negative, past the
+ * table, or an entry outside 0 .. n_pages-1) is not stored, reads as zero, and is not attended to; nothing faults.
+ *
+ * Alignment: the pool, read outputs and the workspace 16 bytes; q, k, v and out four elements (a slice of a fused
+ * projection's output will do).  Strides are elements from one token row to the next, a multiple of 4; the heads of a
+ * row are contiguous.  All calls are asynchronous on `stream`, allocate nothing and can be captured; two calls that may
+ * overlap must not write the same pages or share a workspace.
+ */
+typedef struct {
+    int bits, n_kv_heads, head_dim, page_size, n_pages;
+} bitnet_a48_paged_cache;
+typedef struct {
+    int n_seqs, n_tokens, max_q, max_kv, max_pages;
+    const int32_t* q_start_dev; /* [n_seqs + 1] */
+    const int32_t* kv_len_dev;  /* [n_seqs] */
+    const int32_t* pages_dev;   /* [n_seqs][max_pages] */
+} bitnet_a48_paged_batch;
+
+/* Bytes of the pool; 0 for a cache that is not supported. */
+size_t bitnet_a48_paged_cache_bytes(const bitnet_a48_paged_cache* cache);
+
+/* Stores the new tokens of the batch: k_dev, v_dev [n_tokens][n_kv_heads*head_dim] (fp32, or bf16 with x_bf16 != 0), the
+ * keys rotated first (RoPE on the pairs (i, i + head_dim/2), angle position*rope_base^(-2i/head_dim)) unless rope_base is 0.
+ * q_dev, q_out_dev: both NULL, or the queries [n_tokens][n_heads*head_dim] of k's type and where their rotated values go as
+ * bf16 (q_out_dev may be q_dev with the same stride when x_bf16 != 0).  The codes are those of float64 arithmetic. */
+bitnet_a48_status bitnet_a48_paged_write(const bitnet_a48_paged_cache* cache, void* pool_dev, const bitnet_a48_paged_batch* batch,
+                                         int n_heads, const void* q_dev, long long q_stride, const void* k_dev,
+                                         long long k_stride, const void* v_dev, long long v_stride, int x_bf16,
+                                         float rope_base, float eps, uint16_t* q_out_dev, long long q_out_stride,
+                                         void* stream);
+
+/* Dequantises the positions of the batch's tokens into k_out_dev, v_out_dev [n_tokens][n_kv_heads][head_dim], fp32 or
+ * (y_bf16 != 0) bf16.  With q_start the running sum of kv_len that is every position of every sequence. */
+bitnet_a48_status bitnet_a48_paged_read(const bitnet_a48_paged_cache* cache, const void* pool_dev,
+                                        const bitnet_a48_paged_batch* batch, void* k_out_dev, void* v_out_dev, int y_bf16,
+                                        void* stream);
+
+/* Causal attention of the batch's new tokens over the cache (which already holds them): a token at position p sees the
+ * positions j <= p and, with window > 0, of those the last `window` (j > p - window) and the first `sinks` (j < sinks).
+ *   q_dev, out_dev  bf16 [n_tokens][n_heads*head_dim]; query head h reads key/value head h / (n_heads / n_kv_heads)
+ *   scale           factor of the scores; 0 means 1/sqrt(head_dim)
+ * A token that sees nothing gets zeros.  Scores, softmax and sums are fp32, probabilities are rounded to fp16 in the second
+ * product.  workspace_dev: bitnet_a48_attention_paged_workspace_bytes bytes (NULL when 0), no need to clear it. */
+size_t bitnet_a48_attention_paged_workspace_bytes(const bitnet_a48_paged_cache* cache, const bitnet_a48_paged_batch* batch,
+                                                  int n_heads, int window, int sinks);
+bitnet_a48_status bitnet_a48_attention_paged(const bitnet_a48_paged_cache* cache, const void* pool_dev,
+                                             const bitnet_a48_paged_batch* batch, int n_heads, const uint16_t* q_dev,
+                                             long long q_stride, float scale, int window, int sinks, uint16_t* out_dev,
+                                             long long out_stride, void* workspace_dev, size_t workspace_bytes,
+                                             void* stream);
+
+/* ---------------------------------------------------------------------------
  * Feed-forward sub-layer for M <= 8 tokens with the gate projection first (Section 2.1, paragraph after Eq. 5;
  * Section 3 "Sparsity"): INT4 input (Eq. 7) -> gate BitLinear (Eq. 6) -> up BitLinear only for the output channels n
  * with ReLU²(gate[m, n]) != 0 for some token m (the other rows of W_up are not read) -> Eq. 5 -> top-k + INT8

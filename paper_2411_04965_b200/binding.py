@@ -37,6 +37,8 @@ EXPORTS = [
     "bitnet_a48_ffn_dense", "bitnet_a48_kv_cache_bytes", "bitnet_a48_weight_layout_bytes",
     "bitnet_a48_quant_int4_bf16", "bitnet_a48_topk_quant_int8_bf16", "bitnet_a48_linear_bf16",
     "bitnet_a48_attention_prefill", "bitnet_a48_attention_prefill_workspace_bytes",
+    "bitnet_a48_paged_cache_bytes", "bitnet_a48_paged_write", "bitnet_a48_paged_read",
+    "bitnet_a48_attention_paged", "bitnet_a48_attention_paged_workspace_bytes",
 ]
 
 
@@ -50,6 +52,15 @@ class BlockConfig(ctypes.Structure):
     _fields_ = [("hidden", c_int), ("n_heads", c_int), ("ffn", c_int), ("k_o", c_int), ("k_down", c_int),
                 ("ctx_cap", c_int), ("norm_eps", c_float), ("quant_eps", c_float), ("rope_base", c_float),
                 ("act_fp4", c_int), ("q_bits", c_int), ("kv_bits", c_int)]
+
+
+class PagedCacheConfig(ctypes.Structure):
+    _fields_ = [("bits", c_int), ("n_kv_heads", c_int), ("head_dim", c_int), ("page_size", c_int), ("n_pages", c_int)]
+
+
+class PagedBatchView(ctypes.Structure):
+    _fields_ = [("n_seqs", c_int), ("n_tokens", c_int), ("max_q", c_int), ("max_kv", c_int), ("max_pages", c_int),
+                ("q_start_dev", c_void_p), ("kv_len_dev", c_void_p), ("pages_dev", c_void_p)]
 
 
 _lib = None
@@ -119,6 +130,16 @@ def lib() -> ctypes.CDLL:
                                            c_size_t, c_void_p]
         L.bitnet_a48_ffn_gate_first_workspace_bytes.restype = c_size_t
         L.bitnet_a48_ffn_gate_first_workspace_bytes.argtypes = [c_void_p, c_void_p, c_void_p, c_int]
+        cache_p, batch_p, c_ll = POINTER(PagedCacheConfig), POINTER(PagedBatchView), ctypes.c_longlong
+        L.bitnet_a48_paged_cache_bytes.restype = c_size_t
+        L.bitnet_a48_paged_cache_bytes.argtypes = [cache_p]
+        L.bitnet_a48_paged_write.argtypes = [cache_p, c_void_p, batch_p, c_int, c_void_p, c_ll, c_void_p, c_ll, c_void_p, c_ll,
+                                             c_int, c_float, c_float, c_void_p, c_ll, c_void_p]
+        L.bitnet_a48_paged_read.argtypes = [cache_p, c_void_p, batch_p, c_void_p, c_void_p, c_int, c_void_p]
+        L.bitnet_a48_attention_paged_workspace_bytes.restype = c_size_t
+        L.bitnet_a48_attention_paged_workspace_bytes.argtypes = [cache_p, batch_p, c_int, c_int, c_int]
+        L.bitnet_a48_attention_paged.argtypes = [cache_p, c_void_p, batch_p, c_int, c_void_p, c_ll, c_float, c_int, c_int,
+                                                 c_void_p, c_ll, c_void_p, c_size_t, c_void_p]
         _lib = L
     return _lib
 
@@ -447,6 +468,118 @@ def attention_prefill(q: torch.Tensor, kcache: torch.Tensor, vcache: torch.Tenso
         workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
     _check(lib().bitnet_a48_attention_prefill(_ptr(q), _ptr(kcache), _ptr(vcache), B, T, n_heads, hd, pos0, cap, _ptr(out),
                                               _ptr(workspace), workspace.numel(), _stream(stream)), "attention_prefill")
+    return out
+
+
+class PagedCache:
+    """A pool of pages of a low-bit key/value cache (one layer), zero-filled, or over the caller's pool of bytes."""
+
+    def __init__(self, bits: int, n_kv_heads: int, head_dim: int, page_size: int, n_pages: int, pool=None, device="cuda"):
+        self.cfg = PagedCacheConfig(bits, n_kv_heads, head_dim, page_size, n_pages)
+        self.cfg_ref = byref(self.cfg)
+        self.nbytes = int(lib().bitnet_a48_paged_cache_bytes(self.cfg_ref))
+        if not self.nbytes:
+            raise A48Error(2, "PagedCache")
+        if pool is None:
+            pool = torch.zeros(self.nbytes, dtype=torch.uint8, device=device)
+        assert pool.is_cuda and pool.is_contiguous() and pool.numel() * pool.element_size() >= self.nbytes
+        self.pool = pool
+        self.bits, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages = bits, n_kv_heads, head_dim, page_size, n_pages
+
+
+class PagedBatch:
+    """The new tokens and page tables of a batch (see ``bitnet_a48_paged_batch``); int32 tensors on the cache's device."""
+
+    def __init__(self, q_start: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor, n_tokens: int, max_q: int, max_kv: int):
+        for t in (q_start, kv_len, pages):
+            assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()
+        assert pages.dim() == 2 and kv_len.numel() == pages.shape[0] and q_start.numel() == pages.shape[0] + 1
+        self.q_start, self.kv_len, self.pages, self.n_tokens = q_start, kv_len, pages, n_tokens
+        self.view = PagedBatchView(pages.shape[0], n_tokens, max_q, max_kv, pages.shape[1], q_start.data_ptr(), kv_len.data_ptr(),
+                                   pages.data_ptr())
+        self.view_ref = byref(self.view)
+
+
+class _On:
+    """Makes the tensors' device and the call's stream current, so that what a call allocates belongs to that stream."""
+
+    def __init__(self, t: torch.Tensor, stream):
+        self.stream = stream if stream is not None else torch.cuda.current_stream(t.device)
+        self.same = stream is None and t.device.index == torch.cuda.current_device()
+        self.guard = None if self.same else torch.cuda.stream(self.stream)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return c_void_p(self.stream.cuda_stream)
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _rows(t: torch.Tensor, n_tokens: int, width: int, dtype) -> int:
+    """Stride of token rows [n_tokens, width] whose columns are contiguous."""
+    assert t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape[0] == n_tokens and t.shape[1] == width
+    assert t.stride(1) == 1 or width == 1
+    return t.stride(0) if n_tokens > 1 else max(t.stride(0), width)
+
+
+def paged_write(cache: PagedCache, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor, q=None, rope_base: float = 10000.0,
+                eps: float = 1e-5, q_out=None, stream=None):
+    """Rotates (rope_base 0: does not), quantises and stores k, v [n_tokens, n_kv_heads*head_dim] (fp32 or bf16, rows may be
+    strided); rotates q [n_tokens, n_heads*head_dim] into q_out (bf16, made here unless given).  Returns q_out."""
+    n, width = batch.n_tokens, cache.n_kv_heads * cache.head_dim
+    bf16 = k.dtype == torch.bfloat16
+    dtype = torch.bfloat16 if bf16 else torch.float32
+    ks, vs, qs, os_, heads = _rows(k, n, width, dtype), _rows(v, n, width, dtype), 0, 0, 0
+    assert q_out is None or q is not None
+    with _On(k, stream) as st:
+        if q is not None:
+            heads = q.shape[1] // cache.head_dim
+            qs = _rows(q, n, heads * cache.head_dim, dtype)
+            if q_out is None:
+                q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+            os_ = _rows(q_out, n, q.shape[1], torch.bfloat16)
+        _check(lib().bitnet_a48_paged_write(cache.cfg_ref, cache.pool.data_ptr(), batch.view_ref, heads,
+                                            q.data_ptr() if q is not None else None, qs, k.data_ptr(), ks, v.data_ptr(), vs, int(bf16),
+                                            rope_base, eps, q_out.data_ptr() if q is not None else None, os_, st), "paged_write")
+    return q_out
+
+
+def paged_read(cache: PagedCache, batch: PagedBatch, dtype=torch.bfloat16, k_out=None, v_out=None, stream=None):
+    """The keys and values at the positions of the batch's tokens, [n_tokens, n_kv_heads, head_dim] each, fp32 or bf16."""
+    assert dtype in (torch.bfloat16, torch.float32)
+    shape = (batch.n_tokens, cache.n_kv_heads, cache.head_dim)
+    with _On(cache.pool, stream) as st:
+        k_out = k_out if k_out is not None else torch.empty(shape, dtype=dtype, device=cache.pool.device)
+        v_out = v_out if v_out is not None else torch.empty(shape, dtype=dtype, device=cache.pool.device)
+        for t in (k_out, v_out):
+            assert t.is_cuda and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == shape
+        _check(lib().bitnet_a48_paged_read(cache.cfg_ref, cache.pool.data_ptr(), batch.view_ref, k_out.data_ptr(), v_out.data_ptr(),
+                                           int(dtype == torch.bfloat16), st), "paged_read")
+    return k_out, v_out
+
+
+def attention_paged_workspace_bytes(cache: PagedCache, batch: PagedBatch, n_heads: int, window: int = 0, sinks: int = 0) -> int:
+    return int(lib().bitnet_a48_attention_paged_workspace_bytes(cache.cfg_ref, batch.view_ref, n_heads, window, sinks))
+
+
+def attention_paged(cache: PagedCache, batch: PagedBatch, q: torch.Tensor, scale: float = 0.0, window: int = 0, sinks: int = 0,
+                    out=None, workspace=None, stream=None) -> torch.Tensor:
+    """Causal attention of q bf16 [n_tokens, n_heads*head_dim] over the cache; rows may be strided.  Returns bf16."""
+    heads = q.shape[1] // cache.head_dim
+    qs = _rows(q, batch.n_tokens, heads * cache.head_dim, torch.bfloat16)
+    with _On(q, stream) as st:
+        if out is None:
+            out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+        os_ = _rows(out, batch.n_tokens, q.shape[1], torch.bfloat16)
+        need = attention_paged_workspace_bytes(cache, batch, heads, window, sinks)
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        given = workspace.numel() * workspace.element_size() if workspace is not None else 0
+        _check(lib().bitnet_a48_attention_paged(cache.cfg_ref, cache.pool.data_ptr(), batch.view_ref, heads, q.data_ptr(), qs, scale,
+                                                window, sinks, out.data_ptr(), os_, _ptr(workspace), given, st), "attention_paged")
     return out
 
 

@@ -10,7 +10,9 @@ namespace {
 
 constexpr int kMaxFeatures = 1 << 20;
 
-bool have_device() {
+}  // namespace
+
+bool a48_have_device() {
     static int cached = -1;  // the answer cannot change within a process
     if (cached < 0) {
         int n = 0;
@@ -19,6 +21,10 @@ bool have_device() {
     }
     return cached == 1;
 }
+
+namespace {
+
+bool have_device() { return a48_have_device(); }
 
 void free_weight_buffers(bitnet_a48_weight* w) {
     cudaFree(w->alpha_dev);

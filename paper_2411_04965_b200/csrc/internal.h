@@ -55,6 +55,7 @@ __device__ __forceinline__ void a48_store_y(float* base, size_t index, float y, 
 }
 #endif
 
+bool a48_have_device();  // api.cu
 static inline bool a48_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 static inline int a48_round_up(int x, int m) { return (x + m - 1) / m * m; }
 

@@ -1,0 +1,401 @@
+"""Paged low-bit cache and the attention over it on the GPU against the float64 oracle: codes exact, values to fp32
+rounding, attention within a bound made of its roundings (`attention_bound`)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged
+
+pytestmark = pytest.mark.gpu
+
+EPS32 = float(np.float32(1e-5))
+HALF_BF16, HALF_F16, HALF_F32 = 2.0 ** -8, 2.0 ** -11, 2.0 ** -24
+
+
+class Setup:
+    """A cache, a batch with a shuffled page table, and the oracle's copy of both."""
+
+    def __init__(self, a48, dev, bits, kvh, hd, page, q_lens, kv_lens, seed=0, spare=2, tail=0, width=None, garbage=False):
+        rng = np.random.default_rng(seed)
+        counts = [(max(n, 0) + page - 1) // page for n in kv_lens]
+        n_pages = sum(counts) + spare
+        order = rng.permutation(n_pages)
+        self.table = np.full((len(kv_lens), width or max(max(counts), 1)), -1, np.int32)
+        at = 0
+        for b, c in enumerate(counts):
+            c = min(c, self.table.shape[1])
+            self.table[b, :c] = order[at:at + c]
+            at += c
+        self.q_start = np.concatenate([[0], np.cumsum(q_lens)]).astype(np.int32)
+        self.kv_len = np.array(kv_lens, np.int32)
+        self.n_tokens = int(self.q_start[-1]) + tail
+        self.dev, self.a48, self.bits, self.kvh, self.hd, self.page = dev, a48, bits, kvh, hd, page
+        self.cache = a48.PagedCache(bits, kvh, hd, page, n_pages, device=dev)
+        if garbage:  # what a recycled page may hold: bits that are no numbers
+            self.cache.pool.fill_(255)
+        self.oracle = paged.Cache(bits, kvh, hd, page, n_pages)
+        self.batch = self.view(self.q_start, self.kv_len, self.n_tokens)
+
+    def view(self, q_start, kv_len, n_tokens, max_q=None, max_kv=None):
+        q_lens = np.diff(q_start)
+        return self.a48.PagedBatch(torch.tensor(q_start, dtype=torch.int32, device=self.dev), torch.tensor(kv_len, dtype=torch.int32, device=self.dev),
+                                   torch.tensor(self.table, device=self.dev), n_tokens, max_q or max(1, int(q_lens.max())),
+                                   max_kv or max(1, int(np.max(kv_len))))
+
+    def fill(self, rng, spread=1.0, dtype=torch.bfloat16):
+        """All positions of every sequence written in one call (keys rotated), on both sides."""
+        starts = np.concatenate([[0], np.cumsum(np.maximum(self.kv_len, 0))]).astype(np.int32)
+        n = int(starts[-1])
+        if n == 0:
+            return
+        k, v = (torch.tensor(rng.standard_normal((n, self.kvh * self.hd)) * spread, dtype=torch.float32).to(dtype) for _ in range(2))
+        self.a48.paged_write(self.cache, self.view(starts, np.maximum(self.kv_len, 0), n), k.to(self.dev), v.to(self.dev))
+        self.oracle.write(starts, np.maximum(self.kv_len, 0), self.table, k.double().numpy(), v.double().numpy(), 10000.0, EPS32)
+
+
+def attention_bound(out, mag, top, hd, vmax):
+    """Half a bf16 step of the result; half an fp16 step of every probability (times its value: `mag`); the fp32 scores, whose
+    error (a product and a sum per entry, each rounded by 2^-23 at most on the tensor cores, and six more roundings: scales,
+    softmax factor, difference, exponential of two units) acts on every probability and on the sum; probabilities that fall
+    below fp16's range, 2^-30 of the largest value."""
+    score = (hd + 6) * 2.0 ** -23 * top[..., None] + 8 * 2.0 ** -23
+    return HALF_BF16 * np.abs(out) + (HALF_F16 + 2 * score) * mag * (1 + HALF_BF16) + 2.0 ** -30 * vmax + 1e-30
+
+
+def check_attention(s, q, n_heads, window=0, sinks=0, scale=0.0, batch=None, **kw):
+    got = s.a48.attention_paged(s.cache, batch or s.batch, q.to(s.dev), scale=scale, window=window, sinks=sinks, **kw)
+    out, mag, top = s.oracle.attend(s.q_start, s.kv_len, s.table, q.double().numpy(), n_heads, scale, window, sinks)
+    got = got.double().cpu().numpy().reshape(out.shape)
+    rows = slice(int(s.q_start[0]), int(s.q_start[-1]))
+    vmax = np.abs(s.oracle.scales[1]).max() * 128
+    err, tol = np.abs(got - out)[rows], attention_bound(out, mag, top, s.hd, vmax)[rows]
+    assert np.isfinite(got[rows]).all()
+    worst = float((err / tol).max()) if err.size else 0.0
+    assert worst <= 1.0, worst
+    assert s.a48.kernel_status()[0] == 0
+    return got
+
+
+# ------------------------------------------------------------------------------------------------ write and read
+@pytest.mark.parametrize("bits", [8, 4, 3])
+@pytest.mark.parametrize("hd,kvh,heads,page", [(128, 2, 4, 16), (100, 1, 1, 32), (96, 3, 3, 64), (64, 2, 8, 128), (4, 1, 2, 16), (36, 5, 5, 16)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_write_codes_and_read_back(a48, cuda_dev, bits, hd, kvh, heads, page, dtype):
+    rng = np.random.default_rng(hd + bits)
+    q_lens, kv_lens = [3, 0, 1, 40, 17], [3, 5, 1, 77, 17 + page]
+    s = Setup(a48, cuda_dev, bits, kvh, hd, page, q_lens, kv_lens, seed=hd, garbage=True)
+    n = s.n_tokens
+    k, v, q = (torch.tensor(rng.standard_normal((n, m * hd)) * rng.choice([1.0, 30.0], (1, m * hd)), dtype=torch.float32).to(dtype)
+               for m in (kvh, kvh, heads))
+    v[2] = 0  # a head of zeros
+    before = s.cache.pool.cpu().numpy().copy()
+    q_out = a48.paged_write(s.cache, s.batch, k.to(cuda_dev), v.to(cuda_dev), q=q.to(cuda_dev), rope_base=10000.0)
+    s.oracle.write(s.q_start, s.kv_len, s.table, k.double().numpy(), v.double().numpy(), 10000.0, EPS32)
+    raw = s.cache.pool.cpu().numpy()
+    codes, scales, bos = paged.unpack_pool(raw, bits, kvh, hd, page, s.cache.n_pages)
+    for _, b, _, pos in paged.tokens(s.q_start, s.kv_len):
+        p, slot = paged.place(s.table, b, pos, page, s.cache.n_pages)
+        first = bits == 3 and pos == 0
+        got = bos[:, p] if first else codes[:, p, :, slot]
+        want = s.oracle.bos[:, p] if first else s.oracle.codes[:, p, :, slot]
+        assert np.array_equal(got[..., :hd], want)
+        assert (got[..., hd:] == 0).all()  # padding is the code of zero
+        ref = s.oracle.scales[:, p, :, slot]
+        assert np.all(np.abs(scales[:, p, :, slot] - ref) <= HALF_F32 * ref * (1 + 1e-6))
+    # slots that no token maps to are as they were (a slot's code rows and scales: compare the decoded views)
+    old = paged.unpack_pool(before, bits, kvh, hd, page, s.cache.n_pages)
+    touched = np.zeros((s.cache.n_pages, page), bool)
+    for _, b, _, pos in paged.tokens(s.q_start, s.kv_len):
+        touched[paged.place(s.table, b, pos, page, s.cache.n_pages)] = True
+    for a, o in zip((codes, scales), old):
+        moved = np.moveaxis(a, 3, 2)[:, ~touched], np.moveaxis(o, 3, 2)[:, ~touched]
+        assert np.array_equal(*(np.ascontiguousarray(x).view(np.uint8) for x in moved))
+    # the rotated queries: fp32 products (three roundings each) rounded to bf16
+    qn = q.double().numpy().reshape(n, heads, hd)
+    for row, _, _, pos in paged.tokens(s.q_start, s.kv_len):
+        want = paged.rotate(qn[row], pos, 10000.0)
+        part = np.abs(np.concatenate([qn[row][..., hd // 2:], qn[row][..., :hd // 2]], -1)) + np.abs(qn[row])
+        err = np.abs(q_out[row].double().cpu().numpy().reshape(heads, hd) - want)
+        assert (err <= HALF_BF16 * np.abs(want) + 4 * HALF_F32 * part * (1 + HALF_BF16)).all()
+    # reading back: fp32 is the scale times the code, one rounding of the scale and one of the product; bf16 one more
+    ref = s.oracle.read(s.q_start, s.kv_len, s.table, n)
+    for out_dtype, tol in ((torch.float32, 2 * HALF_F32), (torch.bfloat16, HALF_BF16 + 2 * HALF_F32)):
+        kv = a48.paged_read(s.cache, s.batch, dtype=out_dtype)
+        for got, want in zip(kv, ref):
+            assert (np.abs(got.double().cpu().numpy() - want) <= tol * np.abs(want) * (1 + 1e-6)).all()
+
+
+def test_write_ties_and_far_positions(a48, cuda_dev):
+    """Entries on rounding ties (exact in the input type: gamma = L makes the multiplier 1 with eps 0) round to even, and
+    the angle of a position past 2^20 is that of float64."""
+    hd, bits = 64, 4
+    s = Setup(a48, cuda_dev, bits, 1, hd, 128, [2], [2], seed=5)
+    x = torch.zeros(2, hd)
+    x[0, 0], x[1, 0] = 7.0, -7.0
+    x[:, 1:15] = torch.arange(14) - 6.5  # -6.5 .. 6.5
+    a48.paged_write(s.cache, s.batch, x.to(cuda_dev), x.to(cuda_dev), rope_base=0.0, eps=0.0)
+    k, v = a48.paged_read(s.cache, s.batch, dtype=torch.float32)
+    assert torch.equal(k.cpu()[:, 0], torch.round(x)) and torch.equal(v.cpu(), k.cpu())
+    n = (1 << 20) + 37  # one page table entry far out; the others have no page
+    far = Setup(a48, cuda_dev, 8, 2, hd, 128, [3], [3], seed=6, width=(n + 127) // 128)
+    far.kv_len = np.array([n], np.int32)
+    far.table[:] = -1
+    far.table[0, -1] = 1
+    far.batch = far.view(far.q_start, far.kv_len, 3)
+    rng = np.random.default_rng(3)
+    k, v, q = (torch.tensor(rng.standard_normal((3, 2 * hd)), dtype=torch.float32) for _ in range(3))
+    q_out = a48.paged_write(far.cache, far.batch, k.to(cuda_dev), v.to(cuda_dev), q=q.to(cuda_dev))
+    far.oracle.write(far.q_start, far.kv_len, far.table, k.numpy(), v.numpy(), 10000.0, EPS32)
+    got = a48.paged_read(far.cache, far.batch, dtype=torch.float32)
+    ref = far.oracle.read(far.q_start, far.kv_len, far.table, 3)
+    for a, b in zip(got, ref):
+        assert (np.abs(a.cpu().double().numpy() - b) <= 2 * HALF_F32 * np.abs(b) * (1 + 1e-6)).all()
+    want = paged.rotate(q.double().numpy().reshape(3, 2, hd)[2], n - 1, 10000.0).reshape(-1)
+    assert np.abs(q_out[2].cpu().double().numpy() - want).max() <= HALF_BF16 * np.abs(want).max() + 1e-6
+
+
+def test_strided_and_in_place_write(a48, cuda_dev):
+    """q, k and v as slices of one projection, the rotated queries written over the queries; tokens outside the plan's
+    rows and positions without a page are left alone."""
+    rng = np.random.default_rng(8)
+    hd, kvh, heads = 100, 1, 2  # slices that start on 8-byte boundaries only
+    s = Setup(a48, cuda_dev, 4, kvh, hd, 16, [5, 2], [5, 40], seed=9, tail=3)
+    s.table[1, 2] = 10 ** 6  # sequence 1's tokens sit on a page that does not exist
+    s.batch = s.view(s.q_start, s.kv_len, s.n_tokens)
+    qkv = torch.tensor(rng.standard_normal((s.n_tokens, (heads + 2 * kvh) * hd)), dtype=torch.float32).to(torch.bfloat16)
+    x = qkv.to(cuda_dev)
+    q, k, v = x.split([heads * hd, kvh * hd, kvh * hd], 1)
+    out = a48.paged_write(s.cache, s.batch, k, v, q=q, q_out=q)
+    assert out.data_ptr() == x.data_ptr()
+    s.oracle.write(s.q_start, s.kv_len, s.table, k.double().cpu().numpy(), v.double().cpu().numpy(), 10000.0, EPS32)
+    got = a48.paged_read(s.cache, s.batch, dtype=torch.float32)
+    ref = s.oracle.read(s.q_start, s.kv_len, s.table, s.n_tokens)
+    for g, r in zip(got, ref):
+        assert (np.abs(g.double().cpu().numpy() - r)[:7] <= 2 * HALF_F32 * np.abs(r[:7]) * (1 + 1e-6)).all()
+        assert (g[5:7] == 0).all()  # no page: read as zero
+    assert torch.equal(x[7:].cpu(), qkv[7:])  # rows behind the last sequence
+    qn = qkv[:, :heads * hd].double().numpy().reshape(-1, heads, hd)
+    for row, _, _, pos in paged.tokens(s.q_start, s.kv_len):
+        want = paged.rotate(qn[row], pos, 10000.0).reshape(-1)
+        assert np.abs(out[row].double().cpu().numpy() - want).max() <= HALF_BF16 * np.abs(want).max() + 1e-5
+
+
+# ------------------------------------------------------------------------------------------------ attention
+SHAPES = [(128, 2, 8, 64), (128, 2, 2, 16), (100, 2, 4, 32), (96, 1, 3, 128), (64, 2, 14, 64), (36, 1, 1, 16), (4, 1, 16, 16)]
+
+
+@pytest.mark.parametrize("bits", [8, 4, 3])
+@pytest.mark.parametrize("hd,kvh,heads,page", SHAPES)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (50, 4), (1, 0), (17, 40)])
+def test_decode(a48, cuda_dev, bits, hd, kvh, heads, page, window, sinks):
+    """One new token per sequence at lengths around page ends, from one position on."""
+    rng = np.random.default_rng(bits * 1000 + hd)
+    kv_lens = [1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 300]
+    s = Setup(a48, cuda_dev, bits, kvh, hd, page, [1] * len(kv_lens), kv_lens, seed=hd, garbage=True)
+    s.fill(rng)
+    q = torch.tensor(rng.standard_normal((s.n_tokens, heads * hd)) * 2, dtype=torch.float32).to(torch.bfloat16)
+    check_attention(s, q, heads, window, sinks)
+
+
+@pytest.mark.parametrize("bits", [8, 4, 3])
+@pytest.mark.parametrize("hd,kvh,heads,page", SHAPES)
+@pytest.mark.parametrize("window,sinks", [(0, 0), (40, 3)])
+def test_chunks(a48, cuda_dev, bits, hd, kvh, heads, page, window, sinks):
+    """Ragged chunks in one call: empty sequences, single tokens, whole prompts and chunks behind a cached part."""
+    rng = np.random.default_rng(bits * 100 + hd)
+    q_lens, kv_lens = [1, 0, 7, 70, 130, 2], [200, 9, 7, 70, 333, 131]
+    s = Setup(a48, cuda_dev, bits, kvh, hd, page, q_lens, kv_lens, seed=hd, garbage=True, tail=2)
+    s.fill(rng)
+    q = torch.tensor(rng.standard_normal((s.n_tokens, heads * hd)) * 2, dtype=torch.float32).to(torch.bfloat16)
+    out = torch.full((s.n_tokens, heads * hd), 7.0, dtype=torch.bfloat16, device=cuda_dev)
+    check_attention(s, q, heads, window, sinks, out=out)
+    assert (out[-2:] == 7).all()  # rows behind the last sequence
+
+
+@pytest.mark.parametrize("bits,hd,kvh,heads", [(4, 128, 1, 4), (3, 64, 1, 1), (8, 128, 2, 2)])
+@pytest.mark.parametrize("q_len,kv_len,window,sinks", [(1, 5000, 0, 0), (1, 5000, 700, 4), (3, 4097, 0, 0), (260, 3000, 0, 0), (300, 3000, 500, 2)])
+def test_long_contexts(a48, cuda_dev, bits, hd, kvh, heads, q_len, kv_len, window, sinks):
+    """One sequence over thousands of positions: the axis that is split."""
+    rng = np.random.default_rng(kv_len + bits)
+    s = Setup(a48, cuda_dev, bits, kvh, hd, 64, [q_len], [kv_len], seed=1)
+    s.fill(rng)
+    q = torch.tensor(rng.standard_normal((q_len, heads * hd)), dtype=torch.float32).to(torch.bfloat16)
+    check_attention(s, q, heads, window, sinks)
+
+
+@pytest.mark.parametrize("q_len", [1, 90])
+def test_rows_that_see_nothing(a48, cuda_dev, q_len):
+    """More new tokens than positions, positions without pages, lengths past the table: zeros where nothing is seen."""
+    rng = np.random.default_rng(4)
+    kv_lens = [0, max(1, q_len - 30), 64, 208]  # the last fills its pages
+    s = Setup(a48, cuda_dev, 4, 2, 64, 16, [q_len] * 4, kv_lens, seed=2, garbage=True)
+    s.fill(rng)
+    s.table[2, :] = -1          # none of sequence 2's positions has a page
+    s.table[3, 1:3] = [-7, 1 << 30]  # nor do some of sequence 3's
+    s.kv_len = np.array([0, kv_lens[1], 64, 208], np.int32)
+    s.batch = s.view(s.q_start, s.kv_len, s.n_tokens)
+    q = torch.tensor(rng.standard_normal((s.n_tokens, 4 * 64)), dtype=torch.float32).to(torch.bfloat16)
+    got = check_attention(s, q, 4)
+    assert (got[:q_len] == 0).all() and (got[2 * q_len:3 * q_len] == 0).all()
+    if q_len > 1:
+        assert (got[q_len:q_len + 29] == 0).all()
+    # a length past what the table holds: the positions past it have no page
+    s.kv_len = np.array([0, kv_lens[1], 64, 10 ** 9], np.int32)
+    s.batch = s.view(s.q_start, s.kv_len, s.n_tokens, max_kv=256)
+    check_attention(s, q, 4)
+
+
+@pytest.mark.parametrize("q_len", [1, 4, 100])
+def test_scores_far_apart_and_unlike_scales(a48, cuda_dev, q_len):
+    """Scores that leave one position all the weight, keys and values whose scales differ by many octaves, large and small
+    queries; and numbers that are no numbers where nothing is seen."""
+    rng = np.random.default_rng(6)
+    hd, kv = 128, 400
+    s = Setup(a48, cuda_dev, 4, 1, hd, 32, [q_len], [kv], seed=3)
+    k = rng.standard_normal((kv, hd)) * np.exp2(rng.integers(-6, 7, (kv, 1)))
+    v = rng.standard_normal((kv, hd)) * np.exp2(rng.integers(-9, 10, (kv, 1)))
+    starts = np.array([0, kv], np.int32)
+    kt, vt = (torch.tensor(x, dtype=torch.float32) for x in (k, v))
+    a48.paged_write(s.cache, s.view(starts, [kv], kv), kt.to(cuda_dev), vt.to(cuda_dev), rope_base=0.0)
+    s.oracle.write(starts, [kv], s.table, kt.double().numpy(), vt.double().numpy(), 0.0, EPS32)
+    for size in (1.0, 300.0, 1e-20, 0.0):
+        q = torch.tensor(rng.standard_normal((q_len, 2 * hd)) * size, dtype=torch.float32).to(torch.bfloat16)
+        check_attention(s, q, 2, scale=0.05)
+    # positions that nothing sees (outside the window) hold scales that are infinite or no numbers
+    bad = vt.clone()
+    bad[:kv - q_len - 64] = float("nan")
+    bad[5] = float("inf")
+    kb = kt.clone()
+    kb[:kv - q_len - 64] = float("inf")
+    a48.paged_write(s.cache, s.view(starts, [kv], kv), kb.to(cuda_dev), bad.to(cuda_dev), rope_base=0.0)
+    q = torch.tensor(rng.standard_normal((q_len, 2 * hd)), dtype=torch.float32).to(torch.bfloat16)
+    check_attention(s, q, 2, window=64, scale=0.05)
+
+
+@pytest.mark.parametrize("q_len", [1, 33, 200])
+def test_strided_rows(a48, cuda_dev, q_len):
+    rng = np.random.default_rng(7)
+    hd, heads = 100, 4
+    s = Setup(a48, cuda_dev, 4, 2, hd, 64, [q_len, q_len], [q_len + 70, q_len + 3], seed=4)
+    s.fill(rng)
+    q = torch.tensor(rng.standard_normal((s.n_tokens, heads * hd)), dtype=torch.float32).to(torch.bfloat16)
+    plain = check_attention(s, q, heads)
+    wide = torch.full((s.n_tokens, heads * hd + 108), float("nan"), dtype=torch.bfloat16, device=cuda_dev)
+    wide[:, 4:4 + heads * hd] = q.to(cuda_dev)
+    dst = torch.full((s.n_tokens, heads * hd + 12), 3.0, dtype=torch.bfloat16, device=cuda_dev)
+    a48.attention_paged(s.cache, s.batch, wide[:, 4:4 + heads * hd], out=dst[:, 4:4 + heads * hd])
+    assert np.array_equal(dst[:, 4:4 + heads * hd].double().cpu().numpy().reshape(plain.shape), plain)
+    assert (dst[:, :4] == 3).all() and (dst[:, 4 + heads * hd:] == 3).all()
+
+
+def test_results_do_not_depend_on_the_rest_of_the_batch_or_repeat(a48, cuda_dev):
+    """The same call twice gives the same bits."""
+    rng = np.random.default_rng(11)
+    s = Setup(a48, cuda_dev, 4, 2, 128, 64, [1, 200, 1, 5], [3000, 1200, 17, 900], seed=5)
+    s.fill(rng)
+    q = torch.tensor(rng.standard_normal((s.n_tokens, 8 * 128)), dtype=torch.float32).to(torch.bfloat16).to(cuda_dev)
+    first = a48.attention_paged(s.cache, s.batch, q).clone()
+    for _ in range(3):
+        assert torch.equal(a48.attention_paged(s.cache, s.batch, q), first)
+
+
+def test_captured_step_replayed_with_other_lengths(a48, cuda_dev):
+    """Write and attention captured once; replayed as the sequences grow, with the plan's contents changed in place."""
+    rng = np.random.default_rng(12)
+    hd, kvh, heads, page, B, top = 64, 2, 4, 16, 3, 120
+    s = Setup(a48, cuda_dev, 4, kvh, hd, page, [1] * B, [top] * B, seed=6)
+    batch = s.view(s.q_start, [1] * B, B, max_q=1, max_kv=top)
+    k, v = (torch.zeros(B, kvh * hd, device=cuda_dev) for _ in range(2))
+    q = torch.zeros(B, heads * hd, device=cuda_dev)
+    qr = torch.empty(B, heads * hd, dtype=torch.bfloat16, device=cuda_dev)
+    out = torch.empty_like(qr)
+    ws = torch.empty(max(16, a48.attention_paged_workspace_bytes(s.cache, batch, heads)), dtype=torch.uint8, device=cuda_dev)
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):  # warm up outside the capture
+        a48.paged_write(s.cache, batch, k, v, q=q, q_out=qr)
+        a48.attention_paged(s.cache, batch, qr, out=out, workspace=ws)
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        a48.paged_write(s.cache, batch, k, v, q=q, q_out=qr)
+        a48.attention_paged(s.cache, batch, qr, out=out, workspace=ws)
+    s.cache.pool.zero_()
+    for step in range(1, top + 1):
+        lens = np.array([step, max(1, step - 7), max(1, step // 2)], np.int32)
+        kn, vn, qn = (rng.standard_normal((B, m * hd)).astype(np.float32) for m in (kvh, kvh, heads))
+        for dst, src in ((k, kn), (v, vn), (q, qn)):
+            dst.copy_(torch.tensor(src))
+        batch.kv_len.copy_(torch.tensor(lens))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        s.oracle.write(s.q_start, lens, s.table, kn, vn, 10000.0, EPS32)
+        if step in (1, 2, 16, 17, 60, 119, 120):
+            ref, mag, top_ = s.oracle.attend(s.q_start, lens, s.table, qr.double().cpu().numpy(), heads)
+            got = out.double().cpu().numpy().reshape(ref.shape)
+            assert (np.abs(got - ref) <= attention_bound(ref, mag, top_, hd, np.abs(s.oracle.scales[1]).max() * 128)).all()
+
+
+def test_other_stream_and_two_calls_at_once(a48, cuda_dev):
+    """Calls on streams of their own, each with its own workspace and output, overlap without touching one another."""
+    rng = np.random.default_rng(13)
+    s = Setup(a48, cuda_dev, 3, 2, 128, 64, [1, 1, 150], [2500, 700, 1500], seed=7)
+    s.fill(rng)
+    q = torch.tensor(rng.standard_normal((s.n_tokens, 4 * 128)), dtype=torch.float32).to(torch.bfloat16)
+    want = check_attention(s, q, 4)
+    x = q.to(cuda_dev)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    outs = [[a48.attention_paged(s.cache, s.batch, x, stream=st) for _ in range(4)] for st in streams]
+    torch.cuda.synchronize()
+    for o in outs:
+        for y in o:
+            assert np.array_equal(y.double().cpu().numpy().reshape(want.shape), want)
+
+
+def test_offsets_past_32_bits(a48, cuda_dev):
+    """A pool of more than 4 GB, the sequence on its last pages."""
+    hd, kvh, page = 128, 8, 128
+    n_pages = (1 << 32) // (kvh * (2 * page * hd + 8 * page)) + 40
+    cache = a48.PagedCache(8, kvh, hd, page, n_pages, device=cuda_dev)
+    assert cache.nbytes > 1 << 32
+    small = paged.Cache(8, kvh, hd, page, 3)
+    rng = np.random.default_rng(14)
+    kv, q_len = 300, 70
+    table_small = np.array([[2, 0, 1]], np.int32)
+    table = torch.tensor(n_pages - 3 + table_small, dtype=torch.int32, device=cuda_dev)
+    k, v = (torch.tensor(rng.standard_normal((kv, kvh * hd)), dtype=torch.float32) for _ in range(2))
+    one = lambda n, t: a48.PagedBatch(torch.tensor([0, t], dtype=torch.int32, device=cuda_dev), torch.tensor([n], dtype=torch.int32, device=cuda_dev), table, t, t, n)  # noqa: E731
+    a48.paged_write(cache, one(kv, kv), k.to(cuda_dev), v.to(cuda_dev))
+    small.write([0, kv], [kv], table_small, k.numpy(), v.numpy(), 10000.0, EPS32)
+    got = a48.paged_read(cache, one(kv, kv), dtype=torch.float32)
+    for g, r in zip(got, small.read([0, kv], [kv], table_small, kv)):
+        assert (np.abs(g.double().cpu().numpy() - r) <= 2 * HALF_F32 * np.abs(r) * (1 + 1e-6)).all()
+    for t in (1, q_len):
+        q = torch.tensor(rng.standard_normal((t, 8 * hd)), dtype=torch.float32).to(torch.bfloat16)
+        got = a48.attention_paged(cache, one(kv, t), q.to(cuda_dev)).double().cpu().numpy().reshape(t, 8, hd)
+        ref, mag, top = small.attend([0, t], [kv], table_small, q.double().numpy(), 8)
+        assert (np.abs(got - ref) <= attention_bound(ref, mag, top, hd, np.abs(small.scales[1]).max() * 128)).all()
+
+
+def test_shared_prefix_and_many_sequences(a48, cuda_dev):
+    """Hundreds of sequences (the plan is searched in several steps), all on the same first pages."""
+    rng = np.random.default_rng(15)
+    hd, kvh, heads, page, B = 32, 1, 2, 16, 300
+    s = Setup(a48, cuda_dev, 4, kvh, hd, page, [64], [64], seed=8, spare=B)
+    s.fill(rng)
+    base = s.table[0].copy()
+    free = [p for p in range(s.cache.n_pages) if p not in set(base.tolist())]
+    s.table = np.array([list(base[:3]) + [free[b]] for b in range(B)], np.int32)
+    q_lens = [b % 3 for b in range(B)]
+    s.q_start = np.concatenate([[0], np.cumsum(q_lens)]).astype(np.int32)
+    s.kv_len = np.array([48 + max(1, n) + b % 9 for b, n in enumerate(q_lens)], np.int32)
+    starts = np.concatenate([[0], np.cumsum(s.kv_len - 48)]).astype(np.int32)
+    n = int(starts[-1])
+    k, v = (torch.tensor(rng.standard_normal((n, kvh * hd)), dtype=torch.float32) for _ in range(2))
+    a48.paged_write(s.cache, s.view(starts, s.kv_len, n), k.to(cuda_dev), v.to(cuda_dev))
+    s.oracle.write(starts, s.kv_len, s.table, k.numpy(), v.numpy(), 10000.0, EPS32)
+    s.n_tokens = int(s.q_start[-1])
+    s.batch = s.view(s.q_start, s.kv_len, s.n_tokens)
+    q = torch.tensor(rng.standard_normal((s.n_tokens, heads * hd)), dtype=torch.float32).to(torch.bfloat16)
+    check_attention(s, q, heads)

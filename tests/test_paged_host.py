@@ -1,0 +1,126 @@
+"""Paged low-bit cache without a GPU: the oracle against the definitions it restates, and what the calls refuse."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from oracle import paged
+
+
+def test_oracle_quantiser_is_the_head_quantiser(oracle):
+    x = np.random.default_rng(0).standard_normal((40, 96)).astype(np.float32)
+    for bits in (3, 4, 8):
+        q, d = paged.quantise(x, bits, np.float64(np.float32(1e-5)))
+        q2, d2 = oracle.quant_heads(x, bits, eps=float(np.float32(1e-5)))
+        assert np.array_equal(q, q2) and np.allclose(d, d2, rtol=1e-15, atol=0)
+
+
+def test_oracle_attention_reduces_to_the_block_s(oracle):
+    """One length, every position on a page, no window: the causal attention of the block on the dequantised heads."""
+    rng = np.random.default_rng(1)
+    B, T, nh, hd, page = 2, 21, 3, 12, 16
+    table = np.array([[3, 1], [0, 4]])
+    c = paged.Cache(8, nh, hd, page, 5)
+    q_start, kv_len = [0, T, 2 * T], [T, T]
+    k, v, q = (rng.standard_normal((B * T, nh * hd)) for _ in range(3))
+    c.write(q_start, kv_len, table, k, v, rope_base=100.0)
+    kv = c.read(q_start, kv_len, table, B * T).reshape(2, B, T, nh, hd).transpose(0, 1, 3, 2, 4)
+    out, _, _ = c.attend(q_start, kv_len, table, q, nh)
+    ref = oracle.attention_causal(q, kv[0], kv[1], B=B, T=T, n_heads=nh)
+    assert np.abs(out.reshape(B * T, -1) - ref).max() < 1e-12
+    # the window as its definition, position by position
+    win, _, _ = c.attend(q_start, kv_len, table, q, nh, window=5, sinks=2)
+    for b in range(B):
+        for t in range(T):
+            seen = [j for j in range(t + 1) if j > t - 5 or j < 2]
+            for h in range(nh):
+                s = np.array([kv[0, b, h, j] @ q[b * T + t, h * hd:(h + 1) * hd] for j in seen]) / np.sqrt(hd)
+                p = np.exp(s - s.max())
+                want = (p / p.sum()) @ kv[1, b, h, seen]
+                assert np.abs(win[b * T + t, h] - want).max() < 1e-12
+
+
+def test_rotation_keeps_lengths_and_angles_are_positions():
+    x = np.random.default_rng(2).standard_normal(8)
+    assert np.allclose(paged.rotate(x, 0, 10000.0), x)
+    far = paged.rotate(x, 1000003, 10000.0)
+    assert abs(np.linalg.norm(far) - np.linalg.norm(x)) < 1e-12
+    twice = paged.rotate(paged.rotate(x, 5, 7.0), 6, 7.0)
+    assert np.abs(twice - paged.rotate(x, 11, 7.0)).max() < 1e-12
+
+
+def make(a48, bits=4, heads=2, hd=64, page=16, n_pages=4):
+    return a48.PagedCacheConfig(bits, heads, hd, page, n_pages)
+
+
+def batch(a48, **kw):
+    d = dict(n_seqs=1, n_tokens=2, max_q=2, max_kv=2, max_pages=1, q_start_dev=4096, kv_len_dev=4096, pages_dev=4096)
+    d.update(kw)
+    return a48.PagedBatchView(*d.values())
+
+
+@pytest.mark.parametrize("bits,row", [(8, 128), (4, 64), (3, 48)])
+def test_pool_size(a48, bits, row):
+    lib = a48.lib()
+    for page in (16, 32, 64, 128):
+        for hd in (100, 128):
+            cfg = make(a48, bits, 3, hd, page, 7)
+            assert lib.bitnet_a48_paged_cache_bytes(ctypes.byref(cfg)) == 7 * 3 * (2 * page * row + 8 * page + (128 if bits == 3 else 0))
+    big = make(a48, bits, 8, 128, 64, 1 << 20)  # past 32 bits
+    assert lib.bitnet_a48_paged_cache_bytes(ctypes.byref(big)) > 1 << 32
+
+
+@pytest.mark.parametrize("kw", [dict(bits=5), dict(bits=16), dict(heads=0), dict(hd=0), dict(hd=2), dict(hd=132), dict(hd=66),
+                                dict(page=8), dict(page=48), dict(page=256), dict(n_pages=0)])
+def test_refused_caches(a48, kw):
+    cfg = make(a48, **kw)
+    assert a48.lib().bitnet_a48_paged_cache_bytes(ctypes.byref(cfg)) == 0
+
+
+def test_refusals_of_the_calls(a48):
+    lib = a48.lib()
+    INVALID, SHAPE, ALIGN, LIMIT = 1, 2, 3, 8
+    p, null = ctypes.c_void_p(4096), ctypes.c_void_p(0)
+    good = make(a48)
+    width = 2 * 64
+
+    def write(cfg=good, pool=p, b=None, heads=4, q=p, qs=4 * 64, k=p, ks=width, v=p, vs=width, bf16=1, base=1e4, eps=1e-5, qo=p, qos=4 * 64):
+        return lib.bitnet_a48_paged_write(ctypes.byref(cfg), pool, ctypes.byref(b or batch(a48)), heads, q, qs, k, ks, v, vs, bf16, base,
+                                          eps, qo, qos, null)
+
+    def read(cfg=good, pool=p, b=None, k=p, v=p):
+        return lib.bitnet_a48_paged_read(ctypes.byref(cfg), pool, ctypes.byref(b or batch(a48)), k, v, 1, null)
+
+    def attend(cfg=good, pool=p, b=None, heads=4, q=p, qs=4 * 64, scale=0.0, window=0, sinks=0, out=p, os=4 * 64, ws=p, nbytes=1 << 40):
+        return lib.bitnet_a48_attention_paged(ctypes.byref(cfg), pool, ctypes.byref(b or batch(a48)), heads, q, qs, scale, window, sinks,
+                                              out, os, ws, nbytes, null)
+
+    for call in (write, read, attend):
+        assert call(pool=null) == INVALID
+        assert call(pool=ctypes.c_void_p(4104)) == ALIGN
+        assert call(cfg=make(a48, bits=2)) == SHAPE
+        assert call(b=batch(a48, n_seqs=0)) == SHAPE
+        assert call(b=batch(a48, n_seqs=65536)) == LIMIT
+        assert call(b=batch(a48, n_tokens=0)) == SHAPE
+        assert call(b=batch(a48, max_q=0)) == SHAPE
+        assert call(b=batch(a48, max_kv=-1)) == SHAPE
+        assert call(b=batch(a48, max_pages=0)) == SHAPE
+        for field in ("q_start_dev", "kv_len_dev", "pages_dev"):
+            assert call(b=batch(a48, **{field: None})) == INVALID
+            assert call(b=batch(a48, **{field: 4098})) == ALIGN
+    assert write(k=null) == INVALID and write(v=null) == INVALID
+    assert write(q=null) == INVALID and write(qo=null) == INVALID  # both or neither
+    assert write(ks=width - 4) == SHAPE and write(vs=width + 2) == SHAPE and write(qs=0) == SHAPE and write(qos=4) == SHAPE
+    assert write(k=ctypes.c_void_p(4100)) == ALIGN and write(k=ctypes.c_void_p(4104), bf16=0) == ALIGN
+    assert write(heads=0) == SHAPE and write(eps=-1.0) == INVALID and write(base=-2.0) == INVALID and write(base=float("nan")) == INVALID
+    assert read(k=null) == INVALID and read(v=ctypes.c_void_p(4104)) == ALIGN
+    assert attend(q=null) == INVALID and attend(out=null) == INVALID
+    assert attend(heads=3) == SHAPE and attend(heads=0) == SHAPE and attend(heads=65536) == LIMIT
+    assert attend(qs=4 * 64 - 4) == SHAPE and attend(os=4 * 64 + 1) == SHAPE
+    assert attend(q=ctypes.c_void_p(4100)) == ALIGN and attend(out=ctypes.c_void_p(4098)) == ALIGN and attend(ws=ctypes.c_void_p(8)) == ALIGN
+    assert attend(window=-1) == INVALID and attend(sinks=-1) == INVALID and attend(scale=-1.0) == INVALID and attend(scale=float("inf")) == INVALID
+
+
+def test_binding_refuses(a48):
+    with pytest.raises(a48.A48Error):
+        a48.PagedCache(5, 2, 64, 16, 4)
