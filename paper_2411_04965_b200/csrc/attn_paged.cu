@@ -3,13 +3,24 @@
 //
 //   out[i] = sum_j softmax_j(scale q[i] . k[j]) v[j]   over j <= p, and with a window w: j > p - w or j < sinks
 //
-// p the position of token i.  k[j] = sk[j] c[j] with integer codes c, so the score is (q . c[j]) sk[j] scale, and the
-// value's scale goes to the probability.
-#include "paged.cuh"
+// p the position of token i.  k[j] = sk[j] c[j] and v[j] = sv[j] d[j] with integer codes c, d, so that
+//   score = (q . c[j]) sk[j] scale,   out = (sum_j p[j] sv[j] d[j]) / sum_j p[j]:
+// both contractions run on the codes, which fp16 holds exactly, and the scales meet the scores and the probabilities in
+// fp32.  A query row is brought into fp16 by a power of two of its own (its bf16 numbers keep all their bits down to
+// 2^-29 of the largest), the weights p sv by a power of two that follows the largest value scale; what is rounded is the
+// weight, to fp16's 11 bits (bf16's 8 would cost as much as the rounding of the output).
+//
+// The rows of one key/value head (token i, query head of the group) are taken together.  Sequences with few rows
+// (decoding, drafted tokens) go to attn_paged_rows_kernel, which splits the positions and is bound by memory; those
+// with more to attn_paged_simple_kernel.
+#include <climits>
+
+#include "paged_codes.cuh"
 
 namespace {
 
 using a48p::Batch;
+using a48p::exp2_approx;
 using a48p::Layout;
 
 struct AttnArgs {
@@ -21,16 +32,460 @@ struct AttnArgs {
     long long q_stride, out_stride;
     int heads, group, window, sinks;
     float scale;
+    // sequences with at most this many rows (new tokens x group) are the rows kernel's
+    int few_rows;
+    // rows kernel: tiles of rows per sequence, splits of the positions, 16-position blocks per split
+    int tiles, tile_rows, splits, per_split;
+    float* part_o;   // [split][token * heads + head][128]: sums of p sv d, relative to 2^part_m
+    float2* part_ml;  // [split][token * heads + head]: exponent of the reference, sum of p
 };
 
+// What a tile of rows sees of its sequence: blocks of 16 positions, [0, n_sink) and [first, first + count - n_sink).
+struct Span {
+    int n_sink, first, count;
+};
+__device__ __forceinline__ Span span_of(const AttnArgs& a, int pos_lo, int pos_hi) {
+    const long long reach = (long long)a.b.max_pages << a.l.page_shift;  // positions the table can place
+    const int end = (int)min((long long)pos_hi + 1, reach);
+    Span s{0, 0, 0};
+    if (end <= 0) return s;
+    const int behind = a.window > 0 ? max(0, pos_lo - a.window + 1) : 0;
+    s.first = behind >> 4;
+    s.n_sink = min((min(a.sinks, end) + 15) >> 4, s.first);
+    s.count = s.n_sink + max(0, ((end + 15) >> 4) - s.first);
+    return s;
+}
+
+// ---------------------------------------------------------------------------------------------------- few rows
+// A CTA of four warps takes a tile of 8 NT rows of one head and one split of the positions; a warp takes 16 positions at a
+// time, straight from memory into the registers that hold the operands of its MMAs, the next 16 under way meanwhile.
+//
+// The positions are the M side of both contractions (m16n8k16, fp16, fp32 accumulators), the rows the N side: S^T = C Q^T
+// and O^T = D^T P^T.  Eight rows are then no padding, and the codes, whose conversion is what a position costs, are
+// converted once for all rows.  Entries are dealt to lanes so that every lane converts what it loaded: lane 4g+t holds
+// for S^T the t-th quarter of the key rows of positions g and g + 8 (the order of the entries inside the contraction is
+// free: the query fragments are taken in the same order), for O^T the g-th eighth of the value rows of positions 2t, 2t+1,
+// 2t+8, 2t+9, whose words are first merged into halves of the same entry of two positions.  S^T's accumulators become
+// P^T's operand by one 8x8 transpose each.
+//
+// The running maximum is one reference per row that moves only when a score exceeds it by 2^8: then nothing is reduced
+// across lanes in the steady state, and weights stay below 2^14.
+constexpr int ROW_WARPS = 4;
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
+}
+
+// Words of a lane's share of a code row: of the keys a quarter, of the values an eighth (3 bits: the granule it is in).
+template <int BITS, int PD>
+struct Share {
+    static constexpr int K = BITS == 3 ? 3 : PD * BITS / 128, V = BITS == 3 ? 3 : PD * BITS / 256;
+};
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[N]) {
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4*>(p) + i);
+            w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+        }
+    } else if constexpr (N == 2) {
+        const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
+        w[0] = v.x, w[1] = v.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = __ldg(reinterpret_cast<const unsigned*>(p) + i);
+    }
+}
+
+// Entry of a key row that is half h of converted word i of quarter t (the order convert_k gives).
+template <int BITS, int PD>
+__device__ __forceinline__ int k_entry(int t, int i, int h) {
+    if (BITS == 3) return 32 * t + 16 * h + i;
+    if (BITS == 4) return PD / 4 * t + 8 * (i / 4) + i % 4 + 4 * h;
+    return PD / 4 * t + 4 * (i / 2) + i % 2 + 2 * h;
+}
+template <int BITS, int PD>
+__device__ __forceinline__ void convert_k(const uint32_t (&w)[Share<BITS, PD>::K], uint32_t (&out)[PD / 8]) {
+    if constexpr (BITS == 3) a48p::triples(w[0], w[1], w[2], out);
+    else if constexpr (BITS == 4) {
+#pragma unroll
+        for (int i = 0; i < PD / 32; ++i) a48p::nibbles(w[i], out + 4 * i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < PD / 16; ++i) a48p::bytes(w[i], out + 2 * i);
+    }
+}
+// The PD / 8 entries of an eighth, in order, of two positions a and b.
+template <int BITS, int PD>
+__device__ __forceinline__ void convert_v(const uint32_t (&a)[Share<BITS, PD>::V], const uint32_t (&b)[Share<BITS, PD>::V], uint32_t halves,
+                                          uint32_t (&out)[PD / 8]) {
+    if constexpr (BITS == 3) {
+        a48p::triples(__byte_perm(a[0], b[0], halves), __byte_perm(a[1], b[1], halves), __byte_perm(a[2], b[2], halves), out);
+    } else if constexpr (BITS == 4) {
+#pragma unroll
+        for (int i = 0; i < PD / 64; ++i) {
+            a48p::nibbles(__byte_perm(a[i], b[i], 0x5410), out + 8 * i);
+            a48p::nibbles(__byte_perm(a[i], b[i], 0x7632), out + 8 * i + 4);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PD / 32; ++i) {
+            a48p::bytes(__byte_perm(a[i], b[i], 0x5410), out + 4 * i);
+            a48p::bytes(__byte_perm(a[i], b[i], 0x7632), out + 4 * i + 2);
+        }
+    }
+}
+
+template <int BITS, int PD>
+struct Loaded {  // a lane's part of 16 positions
+    uint32_t k[2][Share<BITS, PD>::K], v[4][Share<BITS, PD>::V];
+    float sk[2], sv[2];
+};
+
+template <int BITS, int PD, int NT>
+__global__ void __launch_bounds__(32 * ROW_WARPS) attn_paged_rows_kernel(const __grid_constant__ AttnArgs a) {
+    constexpr int ROWS = 8 * NT, NK = PD / 8, LD = PD + 4;
+    __shared__ alignas(16) __half q_rows[ROWS][PD + 8];
+    __shared__ float row_mul[ROWS];
+    __shared__ float o_part[ROW_WARPS][ROWS][LD];
+    __shared__ float m_part[ROW_WARPS][ROWS], l_part[ROW_WARPS][ROWS];
+    a48_pdl_prologue();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int kvh = blockIdx.x % a.l.kv_heads, seq = blockIdx.x / a.l.kv_heads / a.tiles;
+    const int r0 = (blockIdx.x / a.l.kv_heads % a.tiles) * ROWS;
+    const int start = __ldg(a.b.q_start + seq), q_len = __ldg(a.b.q_start + seq + 1) - start;
+    const long long all_rows = (long long)q_len * a.group;
+    if (all_rows > a.few_rows || r0 >= all_rows || start < 0 || start + q_len > a.b.n_tokens) return;
+    const int rows = min(ROWS, (int)all_rows - r0);
+    const int pos0 = __ldg(a.b.kv_len + seq) - q_len;
+    const int pos_lo = pos0 + r0 / a.group, pos_hi = pos0 + (r0 + rows - 1) / a.group;
+    const Span span = span_of(a, pos_lo, pos_hi);
+    const int v_begin = blockIdx.y * a.per_split;
+    const int v_end = blockIdx.y + 1 == gridDim.y ? span.count : min(span.count, v_begin + a.per_split);
+
+    auto row_id = [&](int r) { return (size_t)(start + (r0 + r) / a.group) * a.heads + kvh * a.group + (r0 + r) % a.group; };
+    if (v_begin >= v_end && a.splits > 1) {  // nothing in this split
+        if (threadIdx.x < rows) a.part_ml[(size_t)blockIdx.y * a.b.n_tokens * a.heads + row_id(threadIdx.x)] = make_float2(0.f, 0.f);
+        return;
+    }
+
+    // ---- the query rows: a warp brings one at a time to fp16
+    for (int r = warp; r < ROWS; r += ROW_WARPS) {
+        float x[4] = {};
+        if (r < rows && 4 * lane < a.l.hd) {
+            const size_t id = row_id(r);
+            const uint2 u = __ldg(reinterpret_cast<const uint2*>(a.q + id / a.heads * a.q_stride + id % a.heads * a.l.hd) + lane);
+            x[0] = __uint_as_float(u.x << 16), x[1] = __uint_as_float(u.x & 0xffff0000u);
+            x[2] = __uint_as_float(u.y << 16), x[3] = __uint_as_float(u.y & 0xffff0000u);
+        }
+        float mx = fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        const int e = mx > 0.f && mx <= 3.4e38f ? 14 - ilogbf(mx) : 0;  // the largest goes to [2^14, 2^15)
+        if (4 * lane < PD) {
+            const __half2 lo = __floats2half2_rn(scalbnf(x[0], e), scalbnf(x[1], e)), hi = __floats2half2_rn(scalbnf(x[2], e), scalbnf(x[3], e));
+            *reinterpret_cast<uint2*>(&q_rows[r][4 * lane]) =
+                make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        }
+        if (lane == 0) row_mul[r] = scalbnf(a.scale * 1.4426950408889634f, -e);
+    }
+    __syncthreads();
+    uint32_t qf[NT][NK];
+    float mul[NT][2];
+    int lim[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int i = 0; i < NK; ++i) {
+            const __half2 h = __halves2half2(q_rows[8 * n + g][k_entry<BITS, PD>(t, i, 0)], q_rows[8 * n + g][k_entry<BITS, PD>(t, i, 1)]);
+            qf[n][i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = 8 * n + 2 * t + i;
+            mul[n][i] = row_mul[r];
+            lim[n][i] = r < rows ? pos0 + (r0 + r) / a.group : INT_MIN;  // the last position the row sees
+        }
+    }
+
+    float o[NT][PD / 16][4], m[NT][2], l[NT][2];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int i = 0; i < PD / 16; ++i)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) o[n][i][c] = 0.f;
+        m[n][0] = m[n][1] = -1e30f;
+        l[n][0] = l[n][1] = 0.f;
+    }
+    float v_unit = 0.f;  // 2^6 / (a power of two not below the largest value scale so far)
+
+    const int k_at = BITS == 3 ? 12 * t : PD * BITS / 32 * t, v_at = BITS == 3 ? 12 * (g >> 1) : PD * BITS / 64 * g;
+    const bool k_there = k_at < a.l.row, v_there = v_at < a.l.row;
+    const uint32_t halves = (g & 1) ? 0x7632u : 0x5410u;
+
+    auto block_of = [&](int v) { return v < span.n_sink ? v : v - span.n_sink + span.first; };
+    auto page_at = [&](int v) { return v < v_end ? a48p::page_of(a.l, a.b, seq, block_of(v) << 4) : -1; };
+    auto load = [&](int v, int page, Loaded<BITS, PD>& x) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int j = 0; j < Share<BITS, PD>::K; ++j) x.k[i][j] = 0;
+            x.sk[i] = x.sv[i] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < Share<BITS, PD>::V; ++j) x.v[i][j] = 0;
+        if (page < 0) return;
+        const uint8_t* chunk = a.pool + a48p::chunk_at(a.l, page, kvh);
+        const int slot = (block_of(v) << 4) & (a.l.page - 1);
+        const uint8_t* kr = chunk + slot * a.l.row + k_at;
+        const uint8_t* vr = chunk + a.l.v_codes + slot * a.l.row + v_at;
+        if (k_there) {
+            load_words(kr + g * a.l.row, x.k[0]);
+            load_words(kr + (g + 8) * a.l.row, x.k[1]);
+        }
+        if (v_there) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load_words(vr + (2 * t + (i & 1) + 8 * (i >> 1)) * a.l.row, x.v[i]);
+        }
+        const float* sk = reinterpret_cast<const float*>(chunk + a.l.k_scales) + slot;
+        const float* sv = reinterpret_cast<const float*>(chunk + a.l.v_scales) + slot;
+        x.sk[0] = __ldg(sk + g), x.sk[1] = __ldg(sk + g + 8);
+        x.sv[0] = __ldg(sv + g), x.sv[1] = __ldg(sv + g + 8);
+    };
+    // 16 positions from `first` on, `page` >= 0
+    auto take = [&](int first, int page, Loaded<BITS, PD>& x) {
+        float s[NT][4] = {};
+        uint32_t ka[NK], kb[NK];
+        convert_k<BITS, PD>(x.k[0], ka);
+        convert_k<BITS, PD>(x.k[1], kb);
+        if (BITS == 3 && first == 0) {  // the bos heads: 4-bit codes of their own, in convert_k's order
+            const uint8_t* bos = a.pool + a48p::chunk_at(a.l, page, kvh) + a.l.bos;
+            if (g == 0 && k_there) {
+#pragma unroll
+                for (int i = 0; i < NK; ++i) {
+                    const int e0 = k_entry<BITS, PD>(t, i, 0), e1 = k_entry<BITS, PD>(t, i, 1);
+                    const __half2 h = __floats2half2_rn((float)((bos[e0 / 2] >> (4 * (e0 & 1))) & 15) - 8.f,
+                                                        (float)((bos[e1 / 2] >> (4 * (e1 & 1))) & 15) - 8.f);
+                    ka[i] = *reinterpret_cast<const uint32_t*>(&h);
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < NK / 2; ++i) mma_f16(s[n], ka[2 * i], kb[2 * i], ka[2 * i + 1], kb[2 * i + 1], qf[n][2 * i], qf[n][2 * i + 1]);
+        // scores in units of log2 e; what a row does not see is -inf
+        const bool whole = first + 15 <= pos_lo && (a.window == 0 || first > pos_hi - a.window || first + 15 < a.sinks);
+        bool high = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[n][c] *= x.sk[c >> 1] * mul[n][c & 1];
+        if (!whole || rows < ROWS) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int j = first + g + 8 * (c >> 1), last = lim[n][c & 1];
+                    // (last - window cannot wrap: INT_MIN rows fail the first test)
+                    const bool seen = j <= last && (a.window == 0 || j > last - a.window || j < a.sinks);
+                    s[n][c] = seen ? s[n][c] : -INFINITY;
+                }
+        }
+        // a value scale counts if it is finite and some row may see its position
+        float f[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int j = first + g + 8 * i;
+            const bool may = j <= pos_hi && (a.window == 0 || j > pos_lo - a.window || j < a.sinks);
+            f[i] = may ? x.sv[i] : 0.f;
+            high |= f[i] * v_unit > 64.f && f[i] <= 3.4e38f;
+            high |= v_unit == 0.f && f[i] > 0.f;
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) high |= s[n][c] - m[n][c & 1] > 8.f;
+        if (__any_sync(0xffffffffu, high)) {  // rarely: move the references up
+            float top = fmaxf(f[0] <= 3.4e38f ? f[0] : 0.f, f[1] <= 3.4e38f ? f[1] : 0.f);
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            float ratio = 1.f;
+            if (top > 0.f && (v_unit == 0.f || top * v_unit > 64.f)) {
+                // two octaves of room, so that scales of one size do not come back here; within fp32's exponents
+                const int e = min(max(5 - (ilogbf(top) + 2), -120), 120);
+                const float unit = scalbnf(1.f, e);
+                ratio = v_unit == 0.f ? 0.f : unit / v_unit;
+                v_unit = unit;
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float mx = fmaxf(s[n][i], s[n][i + 2]);
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+                    const float m_new = fmaxf(m[n][i], mx), corr = exp2_approx(m[n][i] - m_new);
+                    m[n][i] = m_new;
+                    l[n][i] *= corr;
+#pragma unroll
+                    for (int k = 0; k < PD / 16; ++k) o[n][k][i] *= corr * ratio, o[n][k][i + 2] *= corr * ratio;
+                }
+        }
+        uint32_t pb[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {  // positions g, g + 8
+                const float p0 = exp2_approx(s[n][2 * i] - m[n][0]), p1 = exp2_approx(s[n][2 * i + 1] - m[n][1]);
+                l[n][0] += p0;
+                l[n][1] += p1;
+                // (a weight of zero stays zero whatever the scale: the position may not be seen by this row)
+                const float w0 = p0 > 0.f ? p0 * (f[i] * v_unit) : 0.f, w1 = p1 > 0.f ? p1 * (f[i] * v_unit) : 0.f;
+                const __half2 h = __floats2half2_rn(w0, w1);
+                pb[n][i] = transpose8(*reinterpret_cast<const uint32_t*>(&h));
+            }
+        }
+        uint32_t va[NK], vb[NK];  // positions (2t, 2t+1) and (2t+8, 2t+9)
+        convert_v<BITS, PD>(x.v[0], x.v[1], halves, va);
+        convert_v<BITS, PD>(x.v[2], x.v[3], halves, vb);
+        if (BITS == 3 && first == 0) {
+            const uint8_t* bos = a.pool + a48p::chunk_at(a.l, page, kvh) + a.l.bos + a.l.padded / 2;
+            if (t == 0 && v_there) {
+#pragma unroll
+                for (int i = 0; i < NK; ++i) {
+                    const int e = NK * g + i;
+                    const __half h = __float2half((float)((bos[e / 2] >> (4 * (e & 1))) & 15) - 8.f);
+                    va[i] = (va[i] & 0xffff0000u) | __half_as_ushort(h);
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int k = 0; k < PD / 16; ++k) mma_f16(o[n][k], va[2 * k], va[2 * k + 1], vb[2 * k], vb[2 * k + 1], pb[n][0], pb[n][1]);
+    };
+
+    {
+        int v = v_begin + warp;
+        int page = page_at(v), page_next = page_at(v + ROW_WARPS);
+        Loaded<BITS, PD> x;
+        load(v, page, x);
+        while (v < v_end) {
+            Loaded<BITS, PD> y;
+            load(v + ROW_WARPS, page_next, y);
+            const int page_after = page_at(v + 2 * ROW_WARPS);
+            if (page >= 0) take(block_of(v) << 4, page, x);
+            x = y;
+            v += ROW_WARPS;
+            page = page_next, page_next = page_after;
+        }
+    }
+
+    // ---- the warps' parts meet in shared memory
+    const float unit = v_unit == 0.f ? 0.f : 1.f / v_unit;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], d);
+            const int r = 8 * n + 2 * t + i;
+            if (g == 0) m_part[warp][r] = m[n][i], l_part[warp][r] = l[n][i];
+#pragma unroll
+            for (int k = 0; k < PD / 16; ++k) {
+                float* dst = &o_part[warp][r][NK * g + 2 * k];
+                dst[0] = o[n][k][i] * unit;
+                dst[1] = o[n][k][i + 2] * unit;
+            }
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * (PD / 4); i += 32 * ROW_WARPS) {
+        const int r = i / (PD / 4), c = 4 * (i % (PD / 4));
+        if (c >= a.l.hd) continue;
+        float top = m_part[0][r], sum = 0.f, acc[4] = {};
+#pragma unroll
+        for (int w = 1; w < ROW_WARPS; ++w) top = fmaxf(top, m_part[w][r]);
+#pragma unroll
+        for (int w = 0; w < ROW_WARPS; ++w) {
+            const float corr = exp2_approx(m_part[w][r] - top);
+            const float4 x = *reinterpret_cast<const float4*>(&o_part[w][r][c]);
+            sum += corr * l_part[w][r];
+            acc[0] += corr * x.x, acc[1] += corr * x.y, acc[2] += corr * x.z, acc[3] += corr * x.w;
+        }
+        const size_t id = row_id(r);
+        if (a.splits > 1) {
+            const size_t at = (size_t)blockIdx.y * a.b.n_tokens * a.heads + id;
+            reinterpret_cast<float4*>(a.part_o + at * 128)[c / 4] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+            if (c == 0) a.part_ml[at] = make_float2(top, sum);
+        } else {
+            const float inv = sum > 0.f ? 1.f / sum : 0.f;
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(acc[0] * inv, acc[1] * inv), hi = __floats2bfloat162_rn(acc[2] * inv, acc[3] * inv);
+            *reinterpret_cast<uint2*>(a.out + id / a.heads * a.out_stride + id % a.heads * a.l.hd + c) =
+                make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        }
+    }
+}
+
+// The splits' parts of a row, in order.  One warp per (token, query head), four head dims per lane.
+__global__ void __launch_bounds__(256) attn_paged_join_kernel(const __grid_constant__ AttnArgs a) {
+    a48_pdl_prologue();
+    const int lane = threadIdx.x & 31;
+    const long long id = (long long)blockIdx.x * 8 + (threadIdx.x >> 5), all = (long long)a.b.n_tokens * a.heads;
+    if (id >= all) return;
+    const int token = (int)(id / a.heads), head = (int)(id % a.heads);
+    const int s = a48p::sequence_of(a.b, token, lane);
+    if (s < 0) return;
+    const int start = __ldg(a.b.q_start + s), end = __ldg(a.b.q_start + s + 1);
+    if ((long long)(end - start) * a.group > a.few_rows || end > a.b.n_tokens) return;
+    if (((long long)(token - start) * a.group + head % a.group) / a.tile_rows >= a.tiles) return;  // past max_q
+    float top = -1e30f;
+    for (int i = 0; i < a.splits; ++i) {
+        const float2 ml = __ldg(a.part_ml + i * all + id);
+        if (ml.y > 0.f) top = fmaxf(top, ml.x);
+    }
+    float sum = 0.f, acc[4] = {};
+    for (int i = 0; i < a.splits; ++i) {
+        const float2 ml = __ldg(a.part_ml + i * all + id);
+        if (!(ml.y != 0.f)) continue;  // (a sum that is no number is passed on)
+        const float corr = exp2_approx(ml.x - top);
+        sum += corr * ml.y;
+        if (4 * lane < a.l.hd) {
+            const float4 x = __ldg(reinterpret_cast<const float4*>(a.part_o + (i * all + id) * 128) + lane);
+            acc[0] += corr * x.x, acc[1] += corr * x.y, acc[2] += corr * x.z, acc[3] += corr * x.w;
+        }
+    }
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    if (4 * lane < a.l.hd) {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(acc[0] * inv, acc[1] * inv), hi = __floats2bfloat162_rn(acc[2] * inv, acc[3] * inv);
+        *reinterpret_cast<uint2*>(a.out + token * a.out_stride + (size_t)head * a.l.hd + 4 * lane) =
+            make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------- any rows
 // One warp per (token, query head), lane l owning entries 4l .. 4l+3 of the head: any shape, one key at a time.
-__global__ void __launch_bounds__(256) attn_paged_simple_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(256) attn_paged_simple_kernel(const __grid_constant__ AttnArgs a) {
     a48_pdl_prologue();
     const int lane = threadIdx.x & 31, token = blockIdx.x, h = blockIdx.y * 8 + (threadIdx.x >> 5);
     if (h >= a.heads) return;
     const int s = a48p::sequence_of(a.b, token, lane);
     if (s < 0) return;
     const int first = __ldg(a.b.q_start + s), end = __ldg(a.b.q_start + s + 1);
+    if ((long long)(end - first) * a.group <= a.few_rows) return;  // the rows kernel's
     const int pos = __ldg(a.b.kv_len + s) - (end - first) + (token - first);
     const int e = 4 * lane, kvh = h / a.group;
     const bool mine = e < a.l.hd;
@@ -75,14 +530,66 @@ __global__ void __launch_bounds__(256) attn_paged_simple_kernel(const AttnArgs a
     }
 }
 
+// ---------------------------------------------------------------------------------------------------- host
+constexpr int FEW_ROWS = 64;
+constexpr int kFar = 1 << 30;  // tokens of a call, and what a window is cut to: position differences stay in 32 bits
+
+// How a call is cut up; from its bounds alone, so that the workspace can be asked for ahead.
+struct Plan {
+    bool few, many;  // which kernels run
+    int nt, tiles, splits, per_split;
+    size_t part_o, bytes;  // offset of the partial sums (exponents and sums of p come first), workspace
+};
+
+Plan plan_of(const bitnet_a48_paged_cache& c, const bitnet_a48_paged_batch& b, int heads, int window, int sinks) {
+    Plan p;
+    const long long group = heads / c.n_kv_heads, rows = (long long)b.max_q * group;
+    p.few = true;
+    p.many = rows > FEW_ROWS;
+    const int few = (int)(rows < FEW_ROWS ? rows : FEW_ROWS);
+    p.nt = few > 8 ? 2 : 1;
+    p.tiles = (few + 8 * p.nt - 1) / (8 * p.nt);
+    long long reach = (long long)b.max_pages * c.page_size;
+    if (b.max_kv < reach) reach = b.max_kv;
+    if (window > 0 && (long long)window + sinks + 64 < reach) reach = (long long)window + sinks + 64;
+    const long long blocks = (reach + 15) / 16, ctas = (long long)b.n_seqs * c.n_kv_heads * p.tiles;
+    // One wave of CTAs (four to an SM), as long as every warp of a split has two blocks.
+    long long splits = (4 * 148 + ctas - 1) / ctas, most = (blocks + 2 * ROW_WARPS - 1) / (2 * ROW_WARPS);
+    if (splits > most) splits = most;
+    if (splits > 64) splits = 64;
+    if (splits < 1) splits = 1;
+    p.per_split = (int)((blocks + splits - 1) / splits);
+    p.splits = (int)((blocks + p.per_split - 1) / p.per_split);
+    const size_t ids = (size_t)b.n_tokens * heads * p.splits;
+    p.part_o = (ids * sizeof(float2) + 255) / 256 * 256;
+    p.bytes = p.splits > 1 ? p.part_o + ids * 128 * sizeof(float) : 0;
+    return p;
+}
+
+template <int BITS, int PD>
+cudaError_t launch_rows(const AttnArgs& a, int nt, cudaStream_t st) {
+    const dim3 grid(a.l.kv_heads * a.b.n_seqs * a.tiles, a.splits), block(32 * ROW_WARPS);
+    return nt == 1 ? a48_launch_pdl(attn_paged_rows_kernel<BITS, PD, 1>, grid, block, 0, st, a)
+                   : a48_launch_pdl(attn_paged_rows_kernel<BITS, PD, 2>, grid, block, 0, st, a);
+}
+
+// (the caches and batches that reach this have been checked)
+bitnet_a48_status check_attention(const bitnet_a48_paged_cache* cache, const bitnet_a48_paged_batch* batch, int n_heads, int window, int sinks) {
+    if (n_heads <= 0 || n_heads % cache->n_kv_heads != 0) return BITNET_A48_ERR_SHAPE;
+    if (n_heads > 65535 || batch->n_tokens > kFar || (long long)cache->n_kv_heads * batch->n_seqs * (FEW_ROWS / 8) > INT_MAX) return BITNET_A48_ERR_LIMIT;
+    return window < 0 || sinks < 0 ? BITNET_A48_ERR_INVALID_ARG : BITNET_A48_OK;
+}
+
 }  // namespace
 
 extern "C" {
 
 size_t bitnet_a48_attention_paged_workspace_bytes(const bitnet_a48_paged_cache* cache, const bitnet_a48_paged_batch* batch, int n_heads,
                                                   int window, int sinks) {
-    (void)cache, (void)batch, (void)n_heads, (void)window, (void)sinks;
-    return 0;
+    if (!batch || !bitnet_a48_paged_cache_bytes(cache) || batch->n_seqs <= 0 || batch->n_tokens <= 0 || batch->max_q <= 0 ||
+        batch->max_kv <= 0 || batch->max_pages <= 0 || check_attention(cache, batch, n_heads, window, sinks) != BITNET_A48_OK)
+        return 0;
+    return plan_of(*cache, *batch, n_heads, window, sinks).bytes;
 }
 
 bitnet_a48_status bitnet_a48_attention_paged(const bitnet_a48_paged_cache* cache, const void* pool_dev,
@@ -91,16 +598,16 @@ bitnet_a48_status bitnet_a48_attention_paged(const bitnet_a48_paged_cache* cache
                                              long long out_stride, void* workspace_dev, size_t workspace_bytes, void* stream) {
     bitnet_a48_status st = a48p::check(cache, pool_dev, batch);
     if (st != BITNET_A48_OK) return st;
-    if (n_heads <= 0 || n_heads % cache->n_kv_heads != 0) return BITNET_A48_ERR_SHAPE;
-    if (n_heads > 65535) return BITNET_A48_ERR_LIMIT;
-    if (window < 0 || sinks < 0 || !(scale >= 0.f) || scale > 3e38f) return BITNET_A48_ERR_INVALID_ARG;
+    if ((st = check_attention(cache, batch, n_heads, window, sinks)) != BITNET_A48_OK) return st;
+    if (!(scale >= 0.f) || scale > 3e38f) return BITNET_A48_ERR_INVALID_ARG;
     const long long width = (long long)n_heads * cache->head_dim;
     if ((st = a48p::check_rows(q_dev, q_stride, width, 2)) != BITNET_A48_OK) return st;
     if ((st = a48p::check_rows(out_dev, out_stride, width, 2)) != BITNET_A48_OK) return st;
-    const size_t need = bitnet_a48_attention_paged_workspace_bytes(cache, batch, n_heads, window, sinks);
-    if (need && (!workspace_dev || workspace_bytes < need)) return BITNET_A48_ERR_NOMEM;
+    const Plan p = plan_of(*cache, *batch, n_heads, window, sinks);
     if (!a48_aligned16(workspace_dev)) return BITNET_A48_ERR_ALIGNMENT;
+    if (p.bytes && (!workspace_dev || workspace_bytes < p.bytes)) return BITNET_A48_ERR_NOMEM;
     if (!a48_have_device()) return BITNET_A48_ERR_CUDA;
+    const cudaStream_t cu = (cudaStream_t)stream;
     AttnArgs a;
     a.l = a48p::layout_of(*cache);
     a.b = a48p::batch_of(*batch);
@@ -109,10 +616,28 @@ bitnet_a48_status bitnet_a48_attention_paged(const bitnet_a48_paged_cache* cache
     a.out = reinterpret_cast<__nv_bfloat16*>(out_dev);
     a.q_stride = q_stride, a.out_stride = out_stride;
     a.heads = n_heads, a.group = n_heads / cache->n_kv_heads;
-    a.window = window, a.sinks = window > 0 ? sinks : 0;
+    a.window = window < kFar ? window : kFar, a.sinks = window > 0 ? sinks : 0;
     a.scale = scale > 0.f ? scale : 1.f / sqrtf((float)cache->head_dim);
-    const dim3 grid(batch->n_tokens, (n_heads + 7) / 8);
-    A48_CUDA_TRY(a48_launch_pdl(attn_paged_simple_kernel, grid, dim3(256), 0, (cudaStream_t)stream, a));
+    a.few_rows = p.many ? FEW_ROWS : INT_MAX;
+    a.tiles = p.tiles, a.tile_rows = 8 * p.nt, a.splits = p.splits, a.per_split = p.per_split;
+    a.part_ml = static_cast<float2*>(workspace_dev);
+    a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + p.part_o);
+    if (p.many) {
+        const dim3 grid(batch->n_tokens, (n_heads + 7) / 8);
+        A48_CUDA_TRY(a48_launch_pdl(attn_paged_simple_kernel, grid, dim3(256), 0, cu, a));
+    }
+    if (p.few) {
+        cudaError_t e;
+        const bool wide = a.l.padded > 64;
+        if (a.l.bits == 3) e = launch_rows<3, 128>(a, p.nt, cu);
+        else if (a.l.bits == 4) e = wide ? launch_rows<4, 128>(a, p.nt, cu) : launch_rows<4, 64>(a, p.nt, cu);
+        else e = wide ? launch_rows<8, 128>(a, p.nt, cu) : launch_rows<8, 64>(a, p.nt, cu);
+        A48_CUDA_TRY(e);
+        if (p.splits > 1) {
+            const long long ids = (long long)batch->n_tokens * n_heads;
+            A48_CUDA_TRY(a48_launch_pdl(attn_paged_join_kernel, dim3((unsigned)((ids + 7) / 8)), dim3(256), 0, cu, a));
+        }
+    }
     return BITNET_A48_OK;
 }
 
