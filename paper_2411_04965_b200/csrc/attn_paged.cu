@@ -11,50 +11,19 @@
 // weight, to fp16's 11 bits (bf16's 8 would cost as much as the rounding of the output).
 //
 // The rows of one key/value head (token i, query head of the group) are taken together.  Sequences with few rows
-// (decoding, drafted tokens) go to attn_paged_rows_kernel, which splits the positions and is bound by memory; those
-// with more to attn_paged_simple_kernel.
+// (decoding, drafted tokens) go to attn_paged_rows_kernel below, those with more to the tile kernel of attn_paged_tc.cu.
 #include <climits>
 
-#include "paged_codes.cuh"
+#include "attn_paged.cuh"
 
 namespace {
 
-using a48p::Batch;
 using a48p::exp2_approx;
 using a48p::Layout;
 
-struct AttnArgs {
-    Layout l;
-    Batch b;
-    const uint8_t* pool;
-    const __nv_bfloat16* q;
-    __nv_bfloat16* out;
-    long long q_stride, out_stride;
-    int heads, group, window, sinks;
-    float scale;
-    // sequences with at most this many rows (new tokens x group) are the rows kernel's
-    int few_rows;
-    // rows kernel: tiles of rows per sequence, splits of the positions, 16-position blocks per split
-    int tiles, tile_rows, splits, per_split;
-    float* part_o;   // [split][token * heads + head][128]: sums of p sv d, relative to 2^part_m
-    float2* part_ml;  // [split][token * heads + head]: exponent of the reference, sum of p
-};
-
-// What a tile of rows sees of its sequence: blocks of 16 positions, [0, n_sink) and [first, first + count - n_sink).
-struct Span {
-    int n_sink, first, count;
-};
-__device__ __forceinline__ Span span_of(const AttnArgs& a, int pos_lo, int pos_hi) {
-    const long long reach = (long long)a.b.max_pages << a.l.page_shift;  // positions the table can place
-    const int end = (int)min((long long)pos_hi + 1, reach);
-    Span s{0, 0, 0};
-    if (end <= 0) return s;
-    const int behind = a.window > 0 ? max(0, pos_lo - a.window + 1) : 0;
-    s.first = behind >> 4;
-    s.n_sink = min((min(a.sinks, end) + 15) >> 4, s.first);
-    s.count = s.n_sink + max(0, ((end + 15) >> 4) - s.first);
-    return s;
-}
+using a48p::AttnArgs;
+using a48p::Span;
+using a48p::span_of;
 
 // ---------------------------------------------------------------------------------------------------- few rows
 // A CTA of four warps takes a tile of 8 NT rows of one head and one split of the positions; a warp takes 16 positions at a
@@ -168,7 +137,7 @@ __global__ void __launch_bounds__(32 * ROW_WARPS) attn_paged_rows_kernel(const _
     const int rows = min(ROWS, (int)all_rows - r0);
     const int pos0 = __ldg(a.b.kv_len + seq) - q_len;
     const int pos_lo = pos0 + r0 / a.group, pos_hi = pos0 + (r0 + rows - 1) / a.group;
-    const Span span = span_of(a, pos_lo, pos_hi);
+    const Span span = span_of<4>(a, pos_lo, pos_hi);
     const int v_begin = blockIdx.y * a.per_split;
     const int v_end = blockIdx.y + 1 == gridDim.y ? span.count : min(span.count, v_begin + a.per_split);
 
@@ -233,8 +202,7 @@ __global__ void __launch_bounds__(32 * ROW_WARPS) attn_paged_rows_kernel(const _
     const bool k_there = k_at < a.l.row, v_there = v_at < a.l.row;
     const uint32_t halves = (g & 1) ? 0x7632u : 0x5410u;
 
-    auto block_of = [&](int v) { return v < span.n_sink ? v : v - span.n_sink + span.first; };
-    auto page_at = [&](int v) { return v < v_end ? a48p::page_of(a.l, a.b, seq, block_of(v) << 4) : -1; };
+    auto page_at = [&](int v) { return v < v_end ? a48p::page_of(a.l, a.b, seq, span.block(v) << 4) : -1; };
     auto load = [&](int v, int page, Loaded<BITS, PD>& x) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -248,7 +216,7 @@ __global__ void __launch_bounds__(32 * ROW_WARPS) attn_paged_rows_kernel(const _
             for (int j = 0; j < Share<BITS, PD>::V; ++j) x.v[i][j] = 0;
         if (page < 0) return;
         const uint8_t* chunk = a.pool + a48p::chunk_at(a.l, page, kvh);
-        const int slot = (block_of(v) << 4) & (a.l.page - 1);
+        const int slot = (span.block(v) << 4) & (a.l.page - 1);
         const uint8_t* kr = chunk + slot * a.l.row + k_at;
         const uint8_t* vr = chunk + a.l.v_codes + slot * a.l.row + v_at;
         if (k_there) {
@@ -387,7 +355,7 @@ __global__ void __launch_bounds__(32 * ROW_WARPS) attn_paged_rows_kernel(const _
             Loaded<BITS, PD> y;
             load(v + ROW_WARPS, page_next, y);
             const int page_after = page_at(v + 2 * ROW_WARPS);
-            if (page >= 0) take(block_of(v) << 4, page, x);
+            if (page >= 0) take(span.block(v) << 4, page, x);
             x = y;
             v += ROW_WARPS;
             page = page_next, page_next = page_after;
@@ -450,15 +418,18 @@ __global__ void __launch_bounds__(256) attn_paged_join_kernel(const __grid_const
     const int s = a48p::sequence_of(a.b, token, lane);
     if (s < 0) return;
     const int start = __ldg(a.b.q_start + s), end = __ldg(a.b.q_start + s + 1);
-    if ((long long)(end - start) * a.group > a.few_rows || end > a.b.n_tokens) return;
-    if (((long long)(token - start) * a.group + head % a.group) / a.tile_rows >= a.tiles) return;  // past max_q
+    const bool many = (long long)(end - start) * a.group > a.few_rows;
+    const int splits = many ? a.tc_splits : a.splits, tiles = many ? a.tc_tiles : a.tiles;
+    if (splits == 1 || end > a.b.n_tokens) return;
+    const long long tile = ((long long)(token - start) * a.group + head % a.group) / (many ? a48p::TILE_ROWS : a.tile_rows);
+    if (tiles > 0 && tile >= tiles) return;  // past max_q
     float top = -1e30f;
-    for (int i = 0; i < a.splits; ++i) {
+    for (int i = 0; i < splits; ++i) {
         const float2 ml = __ldg(a.part_ml + i * all + id);
         if (ml.y > 0.f) top = fmaxf(top, ml.x);
     }
     float sum = 0.f, acc[4] = {};
-    for (int i = 0; i < a.splits; ++i) {
+    for (int i = 0; i < splits; ++i) {
         const float2 ml = __ldg(a.part_ml + i * all + id);
         if (!(ml.y != 0.f)) continue;  // (a sum that is no number is passed on)
         const float corr = exp2_approx(ml.x - top);
@@ -476,93 +447,54 @@ __global__ void __launch_bounds__(256) attn_paged_join_kernel(const __grid_const
     }
 }
 
-// ---------------------------------------------------------------------------------------------------- any rows
-// One warp per (token, query head), lane l owning entries 4l .. 4l+3 of the head: any shape, one key at a time.
-__global__ void __launch_bounds__(256) attn_paged_simple_kernel(const __grid_constant__ AttnArgs a) {
-    a48_pdl_prologue();
-    const int lane = threadIdx.x & 31, token = blockIdx.x, h = blockIdx.y * 8 + (threadIdx.x >> 5);
-    if (h >= a.heads) return;
-    const int s = a48p::sequence_of(a.b, token, lane);
-    if (s < 0) return;
-    const int first = __ldg(a.b.q_start + s), end = __ldg(a.b.q_start + s + 1);
-    if ((long long)(end - first) * a.group <= a.few_rows) return;  // the rows kernel's
-    const int pos = __ldg(a.b.kv_len + s) - (end - first) + (token - first);
-    const int e = 4 * lane, kvh = h / a.group;
-    const bool mine = e < a.l.hd;
-    float q[4] = {}, o[4] = {};
-    if (mine)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = __bfloat162float(a.q[(size_t)token * a.q_stride + (size_t)h * a.l.hd + e + i]);
-    float m = -INFINITY, sum = 0.f;
-    const int last = (int)min((long long)pos, ((long long)a.b.max_pages << a.l.page_shift) - 1);  // the table's reach
-    const int behind = a.window > 0 ? max(0, pos - a.window + 1) : 0;  // first position inside the window
-    for (int j = min(a.sinks, behind) > 0 ? 0 : behind; j <= last; ++j) {
-        if (j >= a.sinks && j < behind) j = behind;
-        const int page = a48p::page_of(a.l, a.b, s, j);
-        if (page < 0) continue;
-        const int slot = j & (a.l.page - 1);
-        const uint8_t* chunk = a.pool + a48p::chunk_at(a.l, page, kvh);
-        const bool bos = a.l.bits == 3 && j == 0;
-        float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
-        if (mine) {
-            k = bos ? a48p::four_entries(chunk + a.l.bos, e, 4) : a48p::four_entries(chunk + slot * a.l.row, e, a.l.bits);
-            v = bos ? a48p::four_entries(chunk + a.l.bos + a.l.padded / 2, e, 4)
-                    : a48p::four_entries(chunk + a.l.v_codes + slot * a.l.row, e, a.l.bits);
-        }
-        float dot = q[0] * k.x + q[1] * k.y + q[2] * k.z + q[3] * k.w;
-#pragma unroll
-        for (int x = 16; x > 0; x >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, x);
-        const float score = dot * (__ldg(reinterpret_cast<const float*>(chunk + a.l.k_scales) + slot) * a.scale);
-        const float m_new = fmaxf(m, score), corr = expf(m - m_new), p = expf(score - m_new);
-        const float pv = p * __ldg(reinterpret_cast<const float*>(chunk + a.l.v_scales) + slot);
-        m = m_new;
-        sum = sum * corr + p;
-        o[0] = o[0] * corr + pv * v.x;
-        o[1] = o[1] * corr + pv * v.y;
-        o[2] = o[2] * corr + pv * v.z;
-        o[3] = o[3] * corr + pv * v.w;
-    }
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    if (mine) {
-        __nv_bfloat162* out = reinterpret_cast<__nv_bfloat162*>(a.out + (size_t)token * a.out_stride + (size_t)h * a.l.hd + e);
-        out[0] = __floats2bfloat162_rn(o[0] * inv, o[1] * inv);
-        out[1] = __floats2bfloat162_rn(o[2] * inv, o[3] * inv);
-    }
-}
-
 // ---------------------------------------------------------------------------------------------------- host
-constexpr int FEW_ROWS = 64;
-constexpr int kFar = 1 << 30;  // tokens of a call, and what a window is cut to: position differences stay in 32 bits
+constexpr int FEW_ROWS = 64, SMS = 148;
+constexpr int kFar = 1 << 30;  // what a window is cut to: position differences stay in 32 bits
 
 // How a call is cut up; from its bounds alone, so that the workspace can be asked for ahead.
 struct Plan {
-    bool few, many;  // which kernels run
-    int nt, tiles, splits, per_split;
+    bool many;  // some sequence may be the tile kernel's
+    int nt, tiles, splits, per_split, tc_tiles, tc_splits, tc_per_split;
     size_t part_o, bytes;  // offset of the partial sums (exponents and sums of p come first), workspace
 };
+
+// `positions` in steps of `step`, in at most `splits` parts of at least `least` steps
+void cut(long long positions, int step, long long splits, int least, int& n, int& per) {
+    const long long steps = (positions + step - 1) / step, most = (steps + least - 1) / least;
+    if (splits > most) splits = most;
+    if (splits > 64) splits = 64;
+    if (splits < 1) splits = 1;
+    per = (int)((steps + splits - 1) / splits);
+    n = (int)((steps + per - 1) / per);
+}
 
 Plan plan_of(const bitnet_a48_paged_cache& c, const bitnet_a48_paged_batch& b, int heads, int window, int sinks) {
     Plan p;
     const long long group = heads / c.n_kv_heads, rows = (long long)b.max_q * group;
-    p.few = true;
     p.many = rows > FEW_ROWS;
     const int few = (int)(rows < FEW_ROWS ? rows : FEW_ROWS);
     p.nt = few > 8 ? 2 : 1;
     p.tiles = (few + 8 * p.nt - 1) / (8 * p.nt);
     long long reach = (long long)b.max_pages * c.page_size;
     if (b.max_kv < reach) reach = b.max_kv;
-    if (window > 0 && (long long)window + sinks + 64 < reach) reach = (long long)window + sinks + 64;
-    const long long blocks = (reach + 15) / 16, ctas = (long long)b.n_seqs * c.n_kv_heads * p.tiles;
-    // One wave of CTAs (four to an SM), as long as every warp of a split has two blocks.
-    long long splits = (4 * 148 + ctas - 1) / ctas, most = (blocks + 2 * ROW_WARPS - 1) / (2 * ROW_WARPS);
-    if (splits > most) splits = most;
-    if (splits > 64) splits = 64;
-    if (splits < 1) splits = 1;
-    p.per_split = (int)((blocks + splits - 1) / splits);
-    p.splits = (int)((blocks + p.per_split - 1) / p.per_split);
-    const size_t ids = (size_t)b.n_tokens * heads * p.splits;
+    // positions a tile of `span` tokens may see
+    auto seen = [&](long long span) { return window > 0 && window + sinks + span < reach ? window + sinks + span : reach; };
+    // Few rows: one wave of CTAs (four to an SM), as long as every warp of a split has two blocks.
+    const long long ctas = (long long)b.n_seqs * c.n_kv_heads * p.tiles;
+    cut(seen(64), 16, (4 * SMS + ctas - 1) / ctas, 2 * ROW_WARPS, p.splits, p.per_split);
+    // Many: one CTA per SM; split while the tiles do not fill the SMs, into parts of two tiles or more.
+    p.tc_tiles = 0, p.tc_splits = 1, p.tc_per_split = INT_MAX;
+    if (p.many) {
+        const long long direct = (rows + a48p::TILE_ROWS - 1) / a48p::TILE_ROWS;
+        const long long found = (long long)b.n_tokens * group / a48p::TILE_ROWS;
+        if (direct * b.n_seqs <= found + b.n_seqs) p.tc_tiles = (int)direct;
+        const long long real = (p.tc_tiles ? direct * b.n_seqs : found + 1) * c.n_kv_heads;
+        cut(seen(a48p::TILE_ROWS / group + 2 * a48p::TILE_POSITIONS), a48p::TILE_POSITIONS, SMS / real, 2, p.tc_splits, p.tc_per_split);
+    }
+    const int parts = p.splits > p.tc_splits ? p.splits : p.tc_splits;
+    const size_t ids = (size_t)b.n_tokens * heads * parts;
     p.part_o = (ids * sizeof(float2) + 255) / 256 * 256;
-    p.bytes = p.splits > 1 ? p.part_o + ids * 128 * sizeof(float) : 0;
+    p.bytes = parts > 1 ? p.part_o + ids * 128 * sizeof(float) : 0;
     return p;
 }
 
@@ -576,7 +508,8 @@ cudaError_t launch_rows(const AttnArgs& a, int nt, cudaStream_t st) {
 // (the caches and batches that reach this have been checked)
 bitnet_a48_status check_attention(const bitnet_a48_paged_cache* cache, const bitnet_a48_paged_batch* batch, int n_heads, int window, int sinks) {
     if (n_heads <= 0 || n_heads % cache->n_kv_heads != 0) return BITNET_A48_ERR_SHAPE;
-    if (n_heads > 65535 || batch->n_tokens > kFar || (long long)cache->n_kv_heads * batch->n_seqs * (FEW_ROWS / 8) > INT_MAX) return BITNET_A48_ERR_LIMIT;
+    if (n_heads > 65535 || (long long)batch->n_tokens * n_heads > INT_MAX ||
+        (long long)cache->n_kv_heads * batch->n_seqs * (FEW_ROWS / 8) > INT_MAX) return BITNET_A48_ERR_LIMIT;
     return window < 0 || sinks < 0 ? BITNET_A48_ERR_INVALID_ARG : BITNET_A48_OK;
 }
 
@@ -620,23 +553,19 @@ bitnet_a48_status bitnet_a48_attention_paged(const bitnet_a48_paged_cache* cache
     a.scale = scale > 0.f ? scale : 1.f / sqrtf((float)cache->head_dim);
     a.few_rows = p.many ? FEW_ROWS : INT_MAX;
     a.tiles = p.tiles, a.tile_rows = 8 * p.nt, a.splits = p.splits, a.per_split = p.per_split;
+    a.tc_tiles = p.tc_tiles, a.tc_splits = p.tc_splits, a.tc_per_split = p.tc_per_split;
     a.part_ml = static_cast<float2*>(workspace_dev);
     a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + p.part_o);
-    if (p.many) {
-        const dim3 grid(batch->n_tokens, (n_heads + 7) / 8);
-        A48_CUDA_TRY(a48_launch_pdl(attn_paged_simple_kernel, grid, dim3(256), 0, cu, a));
-    }
-    if (p.few) {
-        cudaError_t e;
-        const bool wide = a.l.padded > 64;
-        if (a.l.bits == 3) e = launch_rows<3, 128>(a, p.nt, cu);
-        else if (a.l.bits == 4) e = wide ? launch_rows<4, 128>(a, p.nt, cu) : launch_rows<4, 64>(a, p.nt, cu);
-        else e = wide ? launch_rows<8, 128>(a, p.nt, cu) : launch_rows<8, 64>(a, p.nt, cu);
-        A48_CUDA_TRY(e);
-        if (p.splits > 1) {
-            const long long ids = (long long)batch->n_tokens * n_heads;
-            A48_CUDA_TRY(a48_launch_pdl(attn_paged_join_kernel, dim3((unsigned)((ids + 7) / 8)), dim3(256), 0, cu, a));
-        }
+    if (p.many && (st = a48p::launch_tiles(a, cu)) != BITNET_A48_OK) return st;
+    const bool wide = a.l.padded > 64;
+    cudaError_t e;
+    if (a.l.bits == 3) e = launch_rows<3, 128>(a, p.nt, cu);
+    else if (a.l.bits == 4) e = wide ? launch_rows<4, 128>(a, p.nt, cu) : launch_rows<4, 64>(a, p.nt, cu);
+    else e = wide ? launch_rows<8, 128>(a, p.nt, cu) : launch_rows<8, 64>(a, p.nt, cu);
+    A48_CUDA_TRY(e);
+    if (p.bytes) {
+        const long long ids = (long long)batch->n_tokens * n_heads;
+        A48_CUDA_TRY(a48_launch_pdl(attn_paged_join_kernel, dim3((unsigned)((ids + 7) / 8)), dim3(256), 0, cu, a));
     }
     return BITNET_A48_OK;
 }

@@ -183,6 +183,9 @@ bitnet_a48_status a48_launch_attn_tc(const float* q, const float* kcache, const 
                                      int pos0, int cap, float* out, void* ws, cudaStream_t st);
 bitnet_a48_status a48_read_attn_status(unsigned int words_host[4]);
 
+// ---- attn_paged_tc.cu
+bitnet_a48_status a48_read_attn_paged_status(unsigned int words_host[4]);
+
 // ---- block.cu
 size_t a48_block_workspace_bytes(const bitnet_a48_block* blk, int B, int T);
 bitnet_a48_status a48_block_forward(const bitnet_a48_block* blk, const float* X, int B, int T, int pos0,

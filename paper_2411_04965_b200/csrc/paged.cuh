@@ -61,23 +61,26 @@ __device__ __forceinline__ size_t chunk_at(const Layout& l, int page, int head) 
     return ((size_t)page * l.kv_heads + head) * l.chunk;
 }
 
-// The sequence whose new tokens include row `row` of the packed tokens (the last b with q_start[b] <= row), or -1.  The
-// whole warp searches, 32 starts at a time.
-__device__ __forceinline__ int sequence_of(const Batch& b, int row, int lane) {
-    int lo = 0, n = b.n_seqs;  // the answer is in [lo - 1, lo + n)
+// The last i in [0, n) with key(i) <= x (key ascending), or -1.  The whole warp searches, 32 keys at a time.
+template <typename Key>
+__device__ __forceinline__ int last_at_most(int n, long long x, int lane, Key key) {
+    int lo = 0;  // the answer is in [lo - 1, lo + n)
     while (n > 0) {
         const int step = (n + 31) / 32;
-        const int at = lo + lane * step;
-        const bool below = lane * step < n && __ldg(b.q_start + at) <= row;
+        const bool below = lane * step < n && key(lo + lane * step) <= x;
         const int hits = __popc(__ballot_sync(0xffffffffu, below));
         if (hits == 0) break;
         const int end = lo + n;
-        lo = lo + (hits - 1) * step + 1;  // starts up to lo - 1 are known to be <= row
+        lo += (hits - 1) * step + 1;  // keys up to lo - 1 are known to be <= x
         n = min(step - 1, end - lo);
     }
-    const int s = lo - 1;
-    if (s < 0 || row >= __ldg(b.q_start + s + 1)) return -1;
-    return s;
+    return lo - 1;
+}
+
+// The sequence whose new tokens include row `row` of the packed tokens, or -1.
+__device__ __forceinline__ int sequence_of(const Batch& b, int row, int lane) {
+    const int s = last_at_most(b.n_seqs, row, lane, [&](int i) { return (long long)__ldg(b.q_start + i); });
+    return s < 0 || row >= __ldg(b.q_start + s + 1) ? -1 : s;
 }
 
 // Page and slot of position `pos` of sequence s; page -1 where the table has none (negative or past the table's or the
@@ -127,7 +130,8 @@ inline bitnet_a48_status check(const bitnet_a48_paged_cache* c, const void* pool
     if (!c || !pool || !b || !b->q_start_dev || !b->kv_len_dev || !b->pages_dev) return BITNET_A48_ERR_INVALID_ARG;
     if (!bitnet_a48_paged_cache_bytes(c)) return BITNET_A48_ERR_SHAPE;
     if (b->n_seqs <= 0 || b->n_tokens <= 0 || b->max_q <= 0 || b->max_kv <= 0 || b->max_pages <= 0) return BITNET_A48_ERR_SHAPE;
-    if (b->n_seqs > 65535) return BITNET_A48_ERR_LIMIT;
+    // rows and positions of a call stay in 32 bits
+    if (b->n_seqs > 65535 || b->n_tokens > (1 << 30) || (long long)b->max_pages * c->page_size > (1 << 30)) return BITNET_A48_ERR_LIMIT;
     const uintptr_t plan = reinterpret_cast<uintptr_t>(b->q_start_dev) | reinterpret_cast<uintptr_t>(b->kv_len_dev) |
                            reinterpret_cast<uintptr_t>(b->pages_dev);
     if (!a48_aligned16(pool) || (plan & 3)) return BITNET_A48_ERR_ALIGNMENT;
