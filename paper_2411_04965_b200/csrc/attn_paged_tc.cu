@@ -2,27 +2,32 @@
 // cores.  A CTA takes 256 rows (token, query head of the group) of one key/value head as two tiles of 128, and walks the
 // positions they see 128 at a time.
 //
-// Both contractions run on the codes (attn_paged.cu has the formulas): S = Q C^T with Q brought to fp16 by a power of two
-// per row, O += P D with P = 2^(score - reference) times the value scale in fp16, fp32 accumulators in tensor memory.  The
+// Both contractions run on the codes (attn_paged.cu has the formulas): S = Q C^T, O += P D with P = 2^(score - reference)
+// times the value scale in fp16, fp32 accumulators in tensor memory.  Q is brought to fp16 by one power of two for the
+// CTA's rows (a row 2^20 below the largest still has all its bits, one 2^29 below it the upper ten); that power, the factor
+// of the scores and log2 e go into the key scales, so that an exponent is one fused multiply-add of an accumulator.  The
 // codes of 128 positions are converted to fp16 once for the 256 rows, into shared memory in the 128-byte swizzle, one row
 // per position for keys and values alike: the keys are then a K-major operand and the values an MN-major one, and nothing is
 // transposed.  The entries of a row keep the order in which the conversion gives them; the query rows are stored in the
 // same order, and the output columns are put right when they are stored.
 //
-//   warps 0-3, 4-7   one thread per row of tile 0, 1: scores from tensor memory, times key scale and row factor, 2^x, the
-//                    weights back over the scores.  One pass: the reference moves only when a score exceeds it by 2^8
-//                    (or a value scale its unit by 2^6), then the tile is taken again and O rescaled; in the steady state
-//                    no pass for the maximum and no rescaling.  Products and sums are two at a time (f32x2).  One thread
-//                    of each tile then issues the MMAs O(t) and, behind it on the pipe, S(t+1): while one tile's weights
-//                    are taken, the pipe has the other's two products.  (A warp of its own for the MMAs would be the
-//                    thirteenth, and leave every thread 128 registers instead of 168.)
-//   warps 8-11       one thread per position: codes and scales from memory (the next position's under way while these are
-//                    converted), fp16 entries into a ring of four buffers K(t) V(t) K(t+1) V(t+1).
+//   warps 0-3, 4-7   the rows of tile 0, 1: scores from tensor memory, 2^(score - reference), the weights back over the
+//                    scores.  One pass: the reference moves only when the weights of a row (a thread's 16 of 64 columns) sum
+//                    to more than 2^9, or a value scale exceeds its unit by 2^6; then the columns' maximum is found, O
+//                    rescaled and the columns taken again.  The sum bounds each weight, so there is no maximum to keep in the steady
+//                    state: per two entries a multiply-add, two exponentials, a sum, the value scale and the conversion
+//                    (f32x2 where there is such a form).  A thread has four rows and a quarter of the columns (the
+//                    16x256b form of the loads), so that it reads a quarter of the scales.  One thread of each tile then
+//                    issues the MMAs O(t) and, behind it on the pipe, S(t+1): while one tile's weights are taken, the
+//                    pipe has the other's two products.  (A warp of its own for the MMAs would be the thirteenth, and
+//                    leave every thread 128 registers instead of 168.)
+//   warps 8-11       codes to fp16: two lanes per row, 32 entries each, so that both the loads and the swizzled stores are
+//                    free of conflicts; the next tile's codes and the page numbers of the one after it under way
+//                    meanwhile.  A ring of four buffers, K(t) V(t) K(t+1) V(t+1).
 // Tensor memory: two score tiles (128 columns, P over the first 64) and two output tiles (up to 128 columns).
 // Every wait is bounded; one that gives up records itself (bitnet_a48_kernel_status), and every later wait of the CTA then
 // falls through, so that the kernel ends by itself.
 #include <climits>
-#include <type_traits>
 
 #include "attn_paged.cuh"
 
@@ -123,17 +128,35 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
         : "r"(taddr)
         : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+// 16 lanes x 16 columns; thread 4g+t has columns 8i + 2t, 8i + 2t + 1 of lane g in r[4i], r[4i+1], of lane g + 8 in the next two
+__device__ __forceinline__ void tmem_ld_16x16(uint32_t taddr, uint32_t* r) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_st_16x16(uint32_t taddr, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.16x256b.x2.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+                 "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+// 16 lanes x 32 columns; thread 4g+t has column 4i + t of lane g in r[2i], of lane g + 8 in r[2i+1]
+__device__ __forceinline__ void tmem_st_16x32(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        "tcgen05.st.sync.aligned.16x128b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
         ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
-          "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
-          "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// the same, for loads into these registers: nothing that reads them is moved ahead of the wait
+__device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[2][8]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0][0]), "+r"(r[0][1]), "+r"(r[0][2]), "+r"(r[0][3]), "+r"(r[0][4]), "+r"(r[0][5]), "+r"(r[0][6]), "+r"(r[0][7]),
+                   "+r"(r[1][0]), "+r"(r[1][1]), "+r"(r[1][2]), "+r"(r[1][3]), "+r"(r[1][4]), "+r"(r[1][5]), "+r"(r[1][6]), "+r"(r[1][7])
+                 :
+                 : "memory");
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // two floats as one operand
@@ -161,6 +184,7 @@ __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
 }
 
 __device__ __forceinline__ void tile_sync(int half) { asm volatile("bar.sync %0, 128;" ::"r"(2 + half) : "memory"); }
+__device__ __forceinline__ void queries_sync() { asm volatile("bar.sync 4, %0;" ::"n"(THREADS) : "memory"); }
 __device__ __forceinline__ void convert_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 __device__ __forceinline__ bool convert_any(bool x) {
     uint32_t r;
@@ -176,7 +200,7 @@ __device__ __forceinline__ bool convert_any(bool x) {
 
 // Scales of the 128 positions of a tile.
 struct TileScales {
-    float key[TK], value[TK];  // value scales times `unit`
+    float scale[TK / 2][4];    // of two positions: key scales times the factors of a score, value scales times `unit`
     uint32_t dead[TK / 32];    // positions without a page
     float unit;                // 2^6 over a power of two not below the largest value scale so far; 0 while all are zero
     float pad[3];
@@ -193,10 +217,17 @@ __host__ __device__ constexpr int entry_of(int i) {  // the entry at place i
 template <int PD>
 struct Cfg {
     static constexpr int BUF = TK * PD * 2;  // one tile of keys, values or query rows
-    static constexpr int Q_AT = RING * BUF, CTRL_AT = Q_AT + 2 * BUF, SCALES_AT = CTRL_AT + 256;
+    static constexpr int Q_AT = RING * BUF, CTRL_AT = Q_AT + 2 * BUF, ROWS_AT = CTRL_AT + 256,
+                         SCALES_AT = ROWS_AT + 2 * TQ * 8;
     static constexpr int SMEM = SCALES_AT + SCALES * (int)sizeof(TileScales) + 1024 /*alignment slack*/;
     static_assert(SMEM <= 227 * 1024, "shared memory budget");
 };
+
+// the power of two that brings the largest query entry to [2^14, 2^15)
+__device__ __forceinline__ int query_exponent(uint32_t top) {
+    const float x = __uint_as_float(top);
+    return x > 0.f ? 14 - ilogbf(x) : 0;
+}
 
 // what a wait that gave up was for
 enum { WAIT_FULL = 41, WAIT_EMPTY = 42, WAIT_S = 43, WAIT_O = 45 };
@@ -207,11 +238,14 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
     constexpr int PANELS = PD / 64, PANEL = TK * 128;
     constexpr int WORDS = PD * BITS / 32;  // of a code row
     extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    // (an offset, not an aligned integer: the compiler then knows these as shared-memory addresses)
+    uint8_t* smem = smem_raw + (-smem_u32(smem_raw) & 1023u);
     uint8_t* ctrl = smem + C::CTRL_AT;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl + 192);
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(ctrl + 196);
-    float* top_part = reinterpret_cast<float*>(ctrl + 208);  // largest value scale per converting warp
+    uint32_t* q_top = reinterpret_cast<uint32_t*>(ctrl + 200);  // the largest query entry, as bits
+    float* top_part = reinterpret_cast<float*>(ctrl + 208);     // largest value scale per converting warp
+    float2* row_info = reinterpret_cast<float2*>(smem + C::ROWS_AT);  // last position seen; at the end reference and sum
     TileScales* scales = reinterpret_cast<TileScales*>(smem + C::SCALES_AT);
     const uint32_t ring = smem_u32(smem), sq = ring + C::Q_AT;
     // barriers: full[4] | empty[4] | s[2] | o[2]
@@ -251,6 +285,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             mbar_init(bar_o + 8 * i, 1);
         }
         *abort_flag = 0;
+        *q_top = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == CONVERT_WARP) {
@@ -265,137 +300,187 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
 
     if (warp >= CONVERT_WARP) {
         // ------------------------------------------------------------------------------------------ codes to fp16
-        const int r = threadIdx.x - 32 * CONVERT_WARP;
-        uint32_t kw[WORDS], vw[WORDS];
-        float sk = 0.f, sv = 0.f;
-        const uint8_t* chunk = nullptr;
-        int pos = 0, slot = 0;
-        float unit = 0.f;
-        // the position of this thread in tile t, its page and scales
-        auto locate = [&](int t) {
-            pos = span.block(v0 + t) * TK + r;
-            slot = pos & (a.l.page - 1);
-            const int page = pos <= pos_hi ? a48p::page_of(a.l, a.b, seq, pos) : -1;
-            chunk = page >= 0 ? a.pool + a48p::chunk_at(a.l, page, kvh) : nullptr;
-        };
-        auto load_row = [&](uint32_t (&w)[WORDS], int part) {
-            const uint32_t* src = chunk ? reinterpret_cast<const uint32_t*>(chunk + part * a.l.v_codes + slot * a.l.row) : nullptr;
-            constexpr int STEP = BITS;  // words of 32 entries
+        const int w = warp - CONVERT_WARP, r = 32 * w + lane;  // r: the position whose scales are this thread's
+        const int sub = lane >> 1, odd = lane & 1;
+        // Codes: block b (16 positions) of the warp's two, entries 64p + 32 odd .. + 31 of the row at position sub.
+        typedef uint32_t Codes[2][PANELS][BITS];
+        float sk = 0.f, sv = 0.f, unit = 0.f;
+        int page[2] = {-1, -1}, next[2] = {-1, -1};  // pages of the blocks, of this tile and of the next
+        int base = 0;                                // first position of the warp in the tile
+        const uint8_t* chunk[2] = {nullptr, nullptr};
+        int slot[2] = {0, 0};
+        auto look_up = [&](int t) {
 #pragma unroll
-            for (int c = 0; c < WORDS; c += STEP) {
-                const bool there = src && 4 * c < a.l.row;
-                if constexpr (BITS == 3) {
-#pragma unroll
-                    for (int i = 0; i < 3; ++i) w[c + i] = there ? __ldg(src + c + i) : 0u;
-                } else {
-#pragma unroll
-                    for (int i = 0; i < STEP; i += 4) {
-                        const uint4 x = there ? __ldg(reinterpret_cast<const uint4*>(src + c + i)) : make_uint4(0, 0, 0, 0);
-                        w[c + i] = x.x, w[c + i + 1] = x.y, w[c + i + 2] = x.z, w[c + i + 3] = x.w;
-                    }
-                }
+            for (int b = 0; b < 2; ++b) {
+                const int p = t < n_tiles ? span.block(v0 + t) * TK + 32 * w + 16 * b : INT_MAX;
+                next[b] = p <= pos_hi ? a48p::page_of(a.l, a.b, seq, p) : -1;
             }
         };
-        auto load_scales = [&]() {
-            sk = chunk ? __ldg(reinterpret_cast<const float*>(chunk + a.l.k_scales) + slot) : 0.f;
-            sv = chunk ? __ldg(reinterpret_cast<const float*>(chunk + a.l.v_scales) + slot) : 0.f;
+        auto locate = [&](int t) {
+            base = span.block(v0 + t) * TK + 32 * w;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                page[b] = next[b];
+                chunk[b] = a.pool + a48p::chunk_at(a.l, max(page[b], 0), kvh);
+                slot[b] = (base + 16 * b) & (a.l.page - 1);
+            }
         };
-        // a row of fp16 entries to row r of a buffer, 32 entries (four 16-byte pieces) at a time
-        auto store_row = [&](uint8_t* buf, const uint32_t (&w)[WORDS], const uint8_t* bos) {
+        auto load_codes = [&](Codes& x, int part) {
 #pragma unroll
-            for (int c = 0; c < PD / 32; ++c) {
-                uint32_t h[16];
-                if constexpr (BITS == 3) {
-                    a48p::triples(w[3 * c], w[3 * c + 1], w[3 * c + 2], h);
-                    if (bos) {  // position 0: 4-bit codes of its own
+            for (int b = 0; b < 2; ++b)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int e = 32 * c + i;
-                            float x = 0.f, y = 0.f;
-                            if (32 * c < a.l.padded) {
-                                x = (float)((bos[e / 2] >> (4 * (e & 1))) & 15) - 8.f;
-                                y = (float)((bos[e / 2 + 8] >> (4 * (e & 1))) & 15) - 8.f;
-                            }
-                            const __half2 p = __floats2half2_rn(x, y);
-                            h[i] = *reinterpret_cast<const uint32_t*>(&p);
+                for (int p = 0; p < PANELS; ++p) {
+                    const int at = (2 * p + odd) * 4 * BITS;
+                    const bool there = page[b] >= 0 && at < a.l.row;
+                    const uint8_t* src = chunk[b] + part * a.l.v_codes + (slot[b] + sub) * a.l.row + at;
+                    if constexpr (BITS == 3) {
+#pragma unroll
+                        for (int i = 0; i < 3; ++i) x[b][p][i] = there ? __ldg(reinterpret_cast<const uint32_t*>(src) + i) : 0u;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < BITS; i += 4) {
+                            const uint4 v = there ? __ldg(reinterpret_cast<const uint4*>(src + 4 * i)) : make_uint4(0, 0, 0, 0);
+                            x[b][p][i] = v.x, x[b][p][i + 1] = v.y, x[b][p][i + 2] = v.z, x[b][p][i + 3] = v.w;
                         }
                     }
-                } else if constexpr (BITS == 4) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) a48p::nibbles(w[4 * c + i], h + 4 * i);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) a48p::bytes(w[8 * c + i], h + 2 * i);
                 }
+        };
+        auto load_scales = [&]() {
+            const int b = lane >> 4;
+            const bool there = page[b] >= 0;
+            const uint8_t* from = b ? chunk[1] : chunk[0];
+            const int at = (b ? slot[1] : slot[0]) + (lane & 15);
+            sk = there ? __ldg(reinterpret_cast<const float*>(from + a.l.k_scales) + at) : 0.f;
+            sv = there ? __ldg(reinterpret_cast<const float*>(from + a.l.v_scales) + at) : 0.f;
+        };
+        auto store_codes = [&](uint8_t* buf, const Codes& x, const uint8_t* bos) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    *reinterpret_cast<uint4*>(buf + c / 2 * PANEL + r * 128 + (((c % 2 * 4 + i) ^ (r & 7)) << 4)) =
-                        make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
+            for (int b = 0; b < 2; ++b) {
+                const int row = 32 * w + 16 * b + sub;
+#pragma unroll
+                for (int p = 0; p < PANELS; ++p) {
+                    uint32_t h[16];
+                    const uint32_t(&c)[BITS] = x[b][p];
+                    if constexpr (BITS == 3) {
+                        a48p::triples(c[0], c[1], c[2], h);
+                        if (bos && row == 0) {  // position 0: 4-bit codes of its own
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const int e = 64 * p + 32 * odd + i;
+                                float lo = 0.f, hi = 0.f;
+                                if (64 * p + 32 * odd < a.l.padded) {
+                                    lo = (float)((bos[e / 2] >> (4 * (e & 1))) & 15) - 8.f;
+                                    hi = (float)((bos[e / 2 + 8] >> (4 * (e & 1))) & 15) - 8.f;
+                                }
+                                const __half2 pair = __floats2half2_rn(lo, hi);
+                                h[i] = *reinterpret_cast<const uint32_t*>(&pair);
+                            }
+                        }
+                    } else if constexpr (BITS == 4) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) a48p::nibbles(c[i], h + 4 * i);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) a48p::bytes(c[i], h + 2 * i);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<uint4*>(buf + p * PANEL + row * 128 + (((4 * odd + i) ^ (row & 7)) << 4)) =
+                            make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]);
+                }
             }
         };
-        auto publish = [&](int n) {
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            mbar_arrive(bar_full + 8 * (n % RING));
-        };
+        // The parts K(0) V(0) K(1) ... one after the other, the next two's codes under way.  (One piece of code for keys and
+        // values: the loops of a CTA have to fit in the instruction cache together.)
+        Codes now, next_codes;
+        look_up(0);
         if (n_tiles > 0) {
             locate(0);
-            load_row(kw, 0);
-            load_row(vw, 1);
             load_scales();
+            load_codes(now, 0);
+            load_codes(next_codes, 1);
+            look_up(1);
         }
-        for (int t = 0; t < n_tiles; ++t) {
-            const int kn = 2 * t, vn = 2 * t + 1;
-            const bool first = BITS == 3 && pos == 0 && chunk;
-            const uint8_t* bos = first ? chunk + a.l.bos : nullptr;
-            const bool dead = !chunk && pos <= pos_hi;
-            // ---- scales; one counts for the unit if it is finite and some row may see its position
-            const bool may = a.window == 0 || pos > pos_lo - a.window || pos < a.sinks;
-            const float f = may ? sv : 0.f;
-            const bool finite = f <= 3.4e38f;
-            if (convert_any(finite && (unit == 0.f ? f > 0.f : f * unit > 64.f))) {
-                float top = finite ? f : 0.f;
+        queries_sync();
+        const float factor = scalbnf(a.scale * 1.4426950408889634f, -query_exponent(*q_top));
+        const uint8_t* bos = nullptr;  // position 0's codes, in the tile that has it
+#pragma unroll 1
+        for (int n = 0; n < 2 * n_tiles; ++n) {
+            const int t = n >> 1, part = n & 1;
+            uint32_t sick = 0;
+            float key = 0.f, f = 0.f;
+            bool dead = false;
+            if (part == 0) {
+                const int pos = base + lane;
+                bos = BITS == 3 && base == 0 && page[0] >= 0 ? chunk[0] + a.l.bos : nullptr;
+                dead = (lane < 16 ? page[0] : page[1]) < 0 && pos <= pos_hi;
+                // ---- scales; one counts if it is finite and some row may see its position
+                const bool may = pos <= pos_hi && (a.window == 0 || pos > pos_lo - a.window || pos < a.sinks);
+                const bool finite = sk <= 3.4e38f && sv <= 3.4e38f;
+                // The scores of a row that does not see a position are set to -inf ahead of these factors, so they have to be
+                // positive and finite; where the scales are not, the rows that do see the position get no numbers from its key.
+                key = finite && may ? fminf(fmaxf(sk * factor, 1e-37f), 3e38f) : 1.f;
+                f = finite && may ? sv : 0.f;
+                sick = __ballot_sync(0xffffffffu, may && !finite);
+                if (convert_any(unit == 0.f ? f > 0.f : f * unit > 64.f)) {
+                    float top = f;
 #pragma unroll
-                for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                if (lane == 0) top_part[warp - CONVERT_WARP] = top;
-                convert_sync();
-                top = fmaxf(fmaxf(top_part[0], top_part[1]), fmaxf(top_part[2], top_part[3]));
-                // two octaves of room, so that scales of one size do not come back here; within fp32's exponents
-                unit = scalbnf(1.f, min(max(5 - (ilogbf(top) + 2), -120), 120));
+                    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    if (lane == 0) top_part[w] = top;
+                    convert_sync();
+                    top = fmaxf(fmaxf(top_part[0], top_part[1]), fmaxf(top_part[2], top_part[3]));
+                    // two octaves of room, so that scales of one size do not come back here; within fp32's exponents
+                    unit = scalbnf(1.f, min(max(5 - (ilogbf(top) + 2), -120), 120));
+                }
             }
-            // ---- keys.  (The ring is what keeps the scales of four tiles apart: K(t) can be written once the scores of
-            // t - 2 are done, and the weights of t - 3 were taken before the scores of t - 2 were issued.)
-            if (kn >= RING) mbar_wait(bar_empty + 8 * (kn % RING), (kn / RING & 1) ^ 1, abort_flag, WAIT_EMPTY, kn);
-            TileScales& ts = scales[t % SCALES];
-            ts.key[r] = sk;
-            ts.value[r] = f * unit;
-            const uint32_t gone = __ballot_sync(0xffffffffu, dead);
-            if (lane == 0) ts.dead[warp - CONVERT_WARP] = gone;
-            if (r == 0) ts.unit = unit;
-            store_row(smem + kn % RING * C::BUF, kw, bos);
-            publish(kn);
-            // ---- the next tile's keys under way, then the values of this one
-            const uint8_t* v_bos = first ? bos + a.l.padded / 2 : nullptr;
-            if (t + 1 < n_tiles) {
-                locate(t + 1);
-                load_row(kw, 0);
-                load_scales();
+            // (The ring is what keeps the scales of four tiles apart: K(t) can be written once the scores of t - 2 are done,
+            // and the weights of t - 3 were taken before the scores of t - 2 were issued.)
+            if (n >= RING) mbar_wait(bar_empty + 8 * (n % RING), (n / RING & 1) ^ 1, abort_flag, WAIT_EMPTY, n);
+            uint8_t* buf = smem + n % RING * C::BUF;
+            store_codes(buf, now, bos ? bos + part * (a.l.padded / 2) : nullptr);
+            if (part == 0) {
+                TileScales& ts = scales[t % SCALES];
+                ts.scale[r >> 1][r & 1] = key;
+                ts.scale[r >> 1][2 + (r & 1)] = f * unit;
+                const uint32_t gone = __ballot_sync(0xffffffffu, dead);
+                if (lane == 0) ts.dead[w] = gone;
+                if (r == 0) ts.unit = unit;
+                if (sick) {
+                    __syncwarp();
+                    for (int i = 0; i < PD / 8; ++i)
+                        if ((sick >> lane) & 1)
+                            *reinterpret_cast<uint4*>(buf + i / 8 * PANEL + r * 128 + i % 8 * 16) =
+                                make_uint4(0x7e007e00u, 0x7e007e00u, 0x7e007e00u, 0x7e007e00u);
+                }
             }
-            if (vn >= RING) mbar_wait(bar_empty + 8 * (vn % RING), (vn / RING & 1) ^ 1, abort_flag, WAIT_EMPTY, vn);
-            store_row(smem + vn % RING * C::BUF, vw, v_bos);
-            publish(vn);
-            if (t + 1 < n_tiles) load_row(vw, 1);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            mbar_arrive(bar_full + 8 * (n % RING));
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int p = 0; p < PANELS; ++p)
+#pragma unroll
+                    for (int i = 0; i < BITS; ++i) now[b][p][i] = next_codes[b][p][i];
+            if (n + 2 < 2 * n_tiles) {  // the same part of the next tile
+                if (part == 0) {
+                    locate(t + 1);
+                    load_scales();
+                } else {
+                    look_up(t + 2);
+                }
+                load_codes(next_codes, part);
+            }
         }
     } else {
         // ------------------------------------------------------------------------------------------ rows
         const int half = warp >> 2, row = (warp & 3) * 32 + lane, r = half * TQ + row;
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t s_at = lanes + COL_S + TK * half, o_at = lanes + COL_O + 128 * half;
+        // this thread's row while queries are loaded and outputs stored
         const bool mine = r < rows;
         const long long in_seq = r0 + (mine ? r : rows - 1);
         const int token = start + (int)(in_seq / a.group), head = kvh * a.group + (int)(in_seq % a.group);
-        const int lim = pos0 + (int)(in_seq / a.group);  // the last position the row sees
-        float mul;
-        // ---- the query row to fp16 by a power of two, in the order of the converted codes
+        // ---- the query rows to fp16 by a power of two, in the order of the converted codes
         {
             uint2 x[PD / 4];
             const uint2* src = reinterpret_cast<const uint2*>(a.q + (size_t)token * a.q_stride + (size_t)head * a.l.hd);
@@ -406,8 +491,11 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                 mx = fmaxf(mx, fmaxf(fmaxf(fabsf(__uint_as_float(x[i].x << 16)), fabsf(__uint_as_float(x[i].x & 0xffff0000u))),
                                      fmaxf(fabsf(__uint_as_float(x[i].y << 16)), fabsf(__uint_as_float(x[i].y & 0xffff0000u)))));
             }
-            const int e = mx > 0.f && mx <= 3.4e38f ? 14 - ilogbf(mx) : 0;  // the largest goes to [2^14, 2^15)
-            mul = scalbnf(a.scale * 1.4426950408889634f, -e);
+            const uint32_t top = __reduce_max_sync(0xffffffffu, mx <= 3.4e38f ? __float_as_uint(mx) : 0u);
+            if (lane == 0) atomicMax(q_top, top);
+            row_info[r].x = __int_as_float(pos0 + (int)(in_seq / a.group));
+            queries_sync();
+            const int e = query_exponent(*q_top);
             const float up0 = scalbnf(1.f, e / 2), up1 = scalbnf(1.f, e - e / 2);  // (2^e may be past fp32)
             auto value = [&](int n) {
                 const uint32_t w = n & 2 ? x[n / 4].y : x[n / 4].x;
@@ -434,30 +522,42 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             tc_fence_after();
             return ring + n % RING * C::BUF;
         };
+        const uint64_t q_desc = smem_desc(sq + half * C::BUF);
         auto issue_s = [&](int t) {
-            const uint32_t keys = wait_full(2 * t);
+            const uint64_t k_desc = smem_desc(wait_full(2 * t));
 #pragma unroll
-            for (int ks = 0; ks < PD / 16; ++ks)
-                mma_ss(t_s, smem_desc(sq + half * C::BUF + ks / 4 * PANEL) + 2 * (ks % 4), smem_desc(keys + ks / 4 * PANEL) + 2 * (ks % 4), idesc_s, ks != 0);
+            for (int ks = 0; ks < PD / 16; ++ks) {
+                constexpr int STEP = PANEL / 16;  // of a descriptor's address, per 64 entries
+                mma_ss(t_s, q_desc + ks / 4 * STEP + 2 * (ks % 4), k_desc + ks / 4 * STEP + 2 * (ks % 4), idesc_s, ks != 0);
+            }
             tc_commit(bar_s + 8 * half);
             tc_commit(bar_empty + 8 * (2 * t % RING));
         };
         auto issue_o = [&](int t, bool last) {
-            const uint32_t values = wait_full(2 * t + 1);
+            const uint64_t v_desc = smem_desc(wait_full(2 * t + 1));
+            mma_ts(t_o, t_s, v_desc, idesc_o, t != 0);
 #pragma unroll
-            for (int j = 0; j < TK / 16; ++j) mma_ts(t_o, t_s + 8 * j, smem_desc(values + 2048 * j), idesc_o, (t | j) != 0);
+            for (int j = 1; j < TK / 16; ++j) mma_ts(t_o, t_s + 8 * j, v_desc + 2048 / 16 * j, idesc_o, 1);
             tc_commit(bar_o + 8 * half);
             // (not on the last tile: nothing waits for it, and the CTA must not end before it has arrived)
             if (!last) tc_commit(bar_empty + 8 * ((2 * t + 1) % RING));
         };
         const bool issuer = (threadIdx.x & (TQ - 1)) == 0;
-        float m = -1e30f, unit = 0.f;
-        float l = 0.f;
         const int used = half < halves ? n_tiles : 0;
         tile_sync(half);
         if (issuer && used > 0) issue_s(0);
         __syncwarp();
-        const int lim_lo = __reduce_min_sync(0xffffffffu, lim), lim_hi = __reduce_max_sync(0xffffffffu, lim);
+        // the four rows of this thread between loads and stores: lanes g, g + 8, g + 16, g + 24 of the warp
+        const int g = lane >> 2, c0 = 2 * (lane & 3);
+        float m[4], l[4], unit = 0.f;
+        int lim[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            lim[i] = __float_as_int(row_info[half * TQ + (warp & 3) * 32 + 8 * i + g].x);
+            m[i] = -1e30f, l[i] = 0.f;
+        }
+        const int lim_lo = __reduce_min_sync(0xffffffffu, min(min(lim[0], lim[1]), min(lim[2], lim[3])));
+        const int lim_hi = __reduce_max_sync(0xffffffffu, max(max(lim[0], lim[1]), max(lim[2], lim[3])));
         for (int t = 0; t < used; ++t) {
             mbar_wait(bar_s + 8 * half, t & 1, abort_flag, WAIT_S, t);
             tc_fence_after();
@@ -466,88 +566,135 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             const uint4 dead = *reinterpret_cast<const uint4*>(ts.dead);
             const bool whole = base + TK - 1 <= lim_lo && (a.window == 0 || base > lim_hi - a.window || base + TK - 1 < a.sinks) &&
                                (dead.x | dead.y | dead.z | dead.w) == 0;
-            uint32_t p[TK / 2];  // weights, two to a word
-            float mx, sum;
-            // weights of the tile for reference m; largest product of accumulator and key scale, sum of 2^(score - m)
-            auto pass = [&](auto masked) {
-                constexpr bool MASKED = decltype(masked)::value;
-                const f2 mul_2 = pack2(mul, mul), m_2 = pack2(-m, -m);
-                f2 sum2 = pack2(0.f, 0.f);
-                mx = -INFINITY;
-                const int to = lim - base, from = a.window > 0 ? lim - a.window + 1 - base : INT_MIN, sunk = a.sinks - base;
+            if (!whole) {  // the scores that a row does not see become -inf
+#pragma unroll 1
+                for (int c = 0; c < TK / 16; ++c) {
+                    uint32_t acc[2][8];
+                    tmem_ld_16x16(s_at + 16 * c, acc[0]);
+                    tmem_ld_16x16(s_at + (16u << 16) + 16 * c, acc[1]);
+                    tmem_wait_ld(acc);
+                    const uint32_t gone = ts.dead[c >> 1] >> (16 * (c & 1) + c0);
 #pragma unroll
-                for (int c = 0; c < TK / 32; ++c) {
-                    uint32_t acc[32];
-                    tmem_ld32(s_at + 32 * c, acc);
-                    tmem_wait_ld();
-                    const uint32_t gone = c == 0 ? dead.x : c == 1 ? dead.y : c == 2 ? dead.z : dead.w;
+                    for (int i = 0; i < 16; ++i) {
+                        const int n = 16 * c + 8 * ((i >> 2) & 1) + c0 + (i & 1), to = lim[(i >> 3) * 2 + ((i >> 1) & 1)] - base;
+                        const bool seen = n <= to && (a.window == 0 || n > to - a.window || n < a.sinks - base) && !((gone >> (8 * ((i >> 2) & 1) + (i & 1))) & 1);
+                        if (!seen) acc[i >> 3][i & 7] = 0xff800000u;
+                    }
+                    tmem_st_16x16(s_at + 16 * c, acc[0]);
+                    tmem_st_16x16(s_at + (16u << 16) + 16 * c, acc[1]);
+                }
+                tmem_wait_st();
+            }
+            // ---- 64 columns, then the other 64
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                uint32_t p[2][16];  // weights, two columns to a word
+                float sum[4];
+                for (bool settled = false;; settled = true) {
+                    // weights and sums of 2^(score - m), 16 columns at a time, the next 16 under way meanwhile
+                    f2 m_2[4], sum_2[4];
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        const ulonglong2 ks = *reinterpret_cast<const ulonglong2*>(ts.key + 32 * c + i);
-                        const ulonglong2 vs = *reinterpret_cast<const ulonglong2*>(ts.value + 32 * c + i);
+                    for (int i = 0; i < 4; ++i) m_2[i] = pack2(-m[i], -m[i]), sum_2[i] = pack2(0.f, 0.f);
+                    uint32_t acc[2][2][8];
+                    tmem_ld_16x16(s_at + 64 * h, acc[0][0]);
+                    tmem_ld_16x16(s_at + (16u << 16) + 64 * h, acc[0][1]);
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        tmem_wait_ld(acc[c & 1]);
+                        if (c < 3) {
+                            tmem_ld_16x16(s_at + 64 * h + 16 * (c + 1), acc[(c + 1) & 1][0]);
+                            tmem_ld_16x16(s_at + (16u << 16) + 64 * h + 16 * (c + 1), acc[(c + 1) & 1][1]);
+                        }
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {
-                            const int n = i + 2 * k;  // of the 32
-                            f2 x = mul2(pack2(__uint_as_float(acc[n]), __uint_as_float(acc[n + 1])), k ? ks.y : ks.x);
-                            float x0, x1, y0, y1, w0, w1;
-                            unpack2(x, x0, x1);
-                            bool seen0 = true, seen1 = true;
-                            if (MASKED) {
-                                const int j = 32 * c + n;
-                                seen0 = j <= to && (j >= from || j < sunk) && !((gone >> n) & 1);
-                                seen1 = j + 1 <= to && (j + 1 >= from || j + 1 < sunk) && !((gone >> (n + 1)) & 1);
-                                x0 = seen0 ? x0 : -INFINITY;
-                                x1 = seen1 ? x1 : -INFINITY;
-                                x = pack2(x0, x1);
+                            const ulonglong2 scale = *reinterpret_cast<const ulonglong2*>(ts.scale[32 * h + 8 * c + 4 * k + c0 / 2]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t* from = acc[c & 1][i >> 1] + 4 * k + 2 * (i & 1);
+                                float y0, y1, w0, w1;
+                                unpack2(fma2(pack2(__uint_as_float(from[0]), __uint_as_float(from[1])), scale.x, m_2[i]), y0, y1);
+                                const f2 e = pack2(exp2_approx(y0), exp2_approx(y1));
+                                sum_2[i] = add2(sum_2[i], e);
+                                unpack2(mul2(e, scale.y), w0, w1);
+                                const __half2 w = __floats2half2_rn(w0, w1);
+                                p[i >> 1][2 * (2 * c + k) + (i & 1)] = *reinterpret_cast<const uint32_t*>(&w);
                             }
-                            mx = fmaxf(mx, fmaxf(x0, x1));
-                            unpack2(fma2(x, mul_2, m_2), y0, y1);
-                            if (MASKED) {  // (a row factor of zero times -inf is no number)
-                                y0 = seen0 ? y0 : -INFINITY;
-                                y1 = seen1 ? y1 : -INFINITY;
-                            }
-                            const f2 e = pack2(exp2_approx(y0), exp2_approx(y1));
-                            sum2 = add2(sum2, e);
-                            unpack2(mul2(e, k ? vs.y : vs.x), w0, w1);
-                            if (MASKED) {
-                                w0 = seen0 ? w0 : 0.f;
-                                w1 = seen1 ? w1 : 0.f;
-                            }
-                            const __half2 h = __floats2half2_rn(w0, w1);
-                            p[(32 * c + n) / 2] = *reinterpret_cast<const uint32_t*>(&h);
                         }
                     }
-                }
-                float s0, s1;
-                unpack2(sum2, s0, s1);
-                sum = s0 + s1;
-            };
-            for (bool settled = false;; settled = true) {
-                if (whole) pass(std::false_type{});
-                else pass(std::true_type{});
-                const float u = ts.unit, score = mx == -INFINITY ? -INFINITY : mx * mul;
-                if (settled || !__any_sync(0xffffffffu, score > m + 8.f || u != unit)) break;
-                const float m_new = score > m + 8.f ? score : m;
-                const float corr = exp2_approx(m - m_new), o_corr = unit == 0.f ? 0.f : corr * (u / unit);
-                m = m_new;
-                unit = u;
-                l *= corr;
-                if (t == 0) continue;
-                mbar_wait(bar_o + 8 * half, (t - 1) & 1, abort_flag, WAIT_O, t);
-                tc_fence_after();
 #pragma unroll
-                for (int c = 0; c < PD / 32; ++c) {
-                    uint32_t acc[32];
-                    tmem_ld32(o_at + 32 * c, acc);
-                    tmem_wait_ld();
+                    for (int i = 0; i < 4; ++i) {
+                        float s0, s1;
+                        unpack2(sum_2[i], s0, s1);
+                        sum[i] = s0 + s1;
+                    }
+                    const float u = ts.unit;
+                    const bool high = u != unit || fmaxf(fmaxf(sum[0], sum[1]), fmaxf(sum[2], sum[3])) > 512.f;
+                    if (settled || !__any_sync(0xffffffffu, high)) break;
+                    // ---- rarely: references to the largest scores of these columns where those are higher (rounded up to
+                    // whole numbers: what moves along then moves by powers of two), and with them O, and the first columns'
+                    // weights while the second's are taken
+                    float corr[4];
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) acc[i] = __float_as_uint(__uint_as_float(acc[i]) * o_corr);
-                    tmem_st32(o_at + 32 * c, acc);
+                    for (int i = 0; i < 4; ++i) corr[i] = -INFINITY;
+#pragma unroll 1
+                    for (int c = 0; c < 4; ++c) {
+                        tmem_ld_16x16(s_at + 64 * h + 16 * c, acc[0][0]);
+                        tmem_ld_16x16(s_at + (16u << 16) + 64 * h + 16 * c, acc[0][1]);
+                        tmem_wait_ld(acc[0]);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int row = (i >> 3) * 2 + ((i >> 1) & 1);
+                            corr[row] = fmaxf(corr[row], __uint_as_float(acc[0][i >> 3][i & 7]) *
+                                                             ts.scale[32 * h + 8 * c + 4 * ((i >> 2) & 1) + c0 / 2][i & 1]);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        corr[i] = fmaxf(corr[i], __shfl_xor_sync(0xffffffffu, corr[i], 1));
+                        corr[i] = fmaxf(corr[i], __shfl_xor_sync(0xffffffffu, corr[i], 2));
+                        const float m_new = fmaxf(m[i], ceilf(corr[i]));
+                        corr[i] = exp2_approx(m[i] - m_new);
+                        m[i] = m_new;
+                        l[i] *= corr[i];
+                    }
+                    if (h > 0) {
+#pragma unroll 1
+                        for (int c = 0; c < 2; ++c) {  // (16 words are 32 weights)
+                            tmem_ld_16x16(s_at + 16 * c, acc[0][0]);
+                            tmem_ld_16x16(s_at + (16u << 16) + 16 * c, acc[0][1]);
+                            tmem_wait_ld(acc[0]);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                uint32_t& w = acc[0][i >> 3][i & 7];
+                                const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(corr[(i >> 3) * 2 + ((i >> 1) & 1)]));
+                                w = *reinterpret_cast<const uint32_t*>(&x);
+                            }
+                            tmem_st_16x16(s_at + 16 * c, acc[0][0]);
+                            tmem_st_16x16(s_at + (16u << 16) + 16 * c, acc[0][1]);
+                        }
+                    }
+                    const float ratio = unit == 0.f ? 0.f : u / unit;  // (the unit moves between tiles only)
+                    unit = u;
+                    if (t == 0) continue;
+                    mbar_wait(bar_o + 8 * half, (t - 1) & 1, abort_flag, WAIT_O, t);
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c = 0; c < PD / 16; ++c) {
+                        tmem_ld_16x16(o_at + 16 * c, acc[0][0]);
+                        tmem_ld_16x16(o_at + (16u << 16) + 16 * c, acc[0][1]);
+                        tmem_wait_ld(acc[0]);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            acc[0][i >> 3][i & 7] = __float_as_uint(__uint_as_float(acc[0][i >> 3][i & 7]) * (corr[(i >> 3) * 2 + ((i >> 1) & 1)] * ratio));
+                        tmem_st_16x16(o_at + 16 * c, acc[0][0]);
+                        tmem_st_16x16(o_at + (16u << 16) + 16 * c, acc[0][1]);
+                    }
                 }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) l[i] += sum[i];
+                tmem_st_16x32(s_at + 32 * h, p[0]);  // (over scores that have been taken)
+                tmem_st_16x32(s_at + (16u << 16) + 32 * h, p[1]);
             }
-            l += sum;
-            tmem_st32(s_at, p);
-            tmem_st32(s_at + 32, p + 32);
             tmem_wait_st();
             tc_fence_before();
             tile_sync(half);
@@ -558,15 +705,23 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             }
             __syncwarp();
         }
-        // ---- out = O / (unit l)
+        // ---- out = O / (unit l), one row per thread again
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+            if (c0 == 0) row_info[half * TQ + (warp & 3) * 32 + 8 * i + g] = make_float2(m[i], l[i]);
+        }
+        __syncwarp();
+        const float2 ml = row_info[r];
         if (used > 0) {
             mbar_wait(bar_o + 8 * half, (used - 1) & 1, abort_flag, WAIT_O, used);
             tc_fence_after();
         }
         const size_t id = (size_t)token * a.heads + head, part = (size_t)blockIdx.y * a.b.n_tokens * a.heads + id;
         const bool split = a.tc_splits > 1;
-        const float inv = unit == 0.f ? 0.f : split ? 1.f / unit : l > 0.f ? 1.f / (unit * l) : 0.f;
-        if (split && mine) a.part_ml[part] = make_float2(m, l);
+        const float inv = unit == 0.f ? 0.f : split ? 1.f / unit : ml.y != 0.f ? 1.f / ml.y / unit : 0.f;
+        if (split && mine) a.part_ml[part] = ml;
         __nv_bfloat16* out = a.out + (size_t)token * a.out_stride + (size_t)head * a.l.hd;
 #pragma unroll
         for (int c = 0; c < PD / 32; ++c) {
