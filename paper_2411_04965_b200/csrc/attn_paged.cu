@@ -563,7 +563,7 @@ bitnet_a48_status bitnet_a48_attention_paged(const bitnet_a48_paged_cache* cache
     else if (a.l.bits == 4) e = wide ? launch_rows<4, 128>(a, p.nt, cu) : launch_rows<4, 64>(a, p.nt, cu);
     else e = wide ? launch_rows<8, 128>(a, p.nt, cu) : launch_rows<8, 64>(a, p.nt, cu);
     A48_CUDA_TRY(e);
-    if (p.bytes) {
+    if (p.bytes) {  // (some kernel's parts: the join leaves rows that were not split alone)
         const long long ids = (long long)batch->n_tokens * n_heads;
         A48_CUDA_TRY(a48_launch_pdl(attn_paged_join_kernel, dim3((unsigned)((ids + 7) / 8)), dim3(256), 0, cu, a));
     }

@@ -106,6 +106,11 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b_desc, 
         ::"r"(d), "r"(a), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+__device__ __forceinline__ bool elect() {
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one) : : "memory");
+    return one != 0;
+}
 // Descriptor of an operand whose rows of 128 bytes (64 fp16) lie in the 128-byte swizzle, groups of eight rows 1024 bytes
 // apart.  K-major (rows along M or N): 16 elements further along K is 32 bytes.  MN-major (rows along K): 16 rows further
 // along K is 2048 bytes, and the next 64 columns are one panel of TK rows further on.
@@ -159,6 +164,13 @@ __device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[2][8]) {
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Keeps a kernel argument in a register: read in a loop it would come from the constant bank again and again, which the
+// loop's own code keeps pushing out of the cache (measured: 0.5k clocks a tile).
+__device__ __forceinline__ int in_register(int x) {
+    asm volatile("" : "+r"(x));
+    return x;
+}
+
 // two floats as one operand
 typedef unsigned long long f2;
 __device__ __forceinline__ f2 pack2(float x, float y) {
@@ -184,6 +196,9 @@ __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) {
 }
 
 __device__ __forceinline__ void tile_sync(int half) { asm volatile("bar.sync %0, 128;" ::"r"(2 + half) : "memory"); }
+// The two tiles take their weights in turn: one waits until the other is through, which then has the tensor pipe working.
+__device__ __forceinline__ void turn_wait(int half) { asm volatile("bar.sync %0, 256;" ::"r"(5 + half) : "memory"); }
+__device__ __forceinline__ void turn_pass(int half) { asm volatile("bar.arrive %0, 256;" ::"r"(6 - half) : "memory"); }
 __device__ __forceinline__ void queries_sync() { asm volatile("bar.sync 4, %0;" ::"n"(THREADS) : "memory"); }
 __device__ __forceinline__ void convert_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
 __device__ __forceinline__ bool convert_any(bool x) {
@@ -236,7 +251,6 @@ template <int BITS, int PD>
 __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_constant__ AttnArgs a) {
     using C = Cfg<PD>;
     constexpr int PANELS = PD / 64, PANEL = TK * 128;
-    constexpr int WORDS = PD * BITS / 32;  // of a code row
     extern __shared__ uint8_t smem_raw[];
     // (an offset, not an aligned integer: the compiler then knows these as shared-memory addresses)
     uint8_t* smem = smem_raw + (-smem_u32(smem_raw) & 1023u);
@@ -250,7 +264,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
     const uint32_t ring = smem_u32(smem), sq = ring + C::Q_AT;
     // barriers: full[4] | empty[4] | s[2] | o[2]
     const uint32_t bar_full = smem_u32(ctrl), bar_empty = bar_full + 32, bar_s = bar_full + 64, bar_o = bar_full + 80;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // (known to be the same in a warp)
     a48_pdl_prologue();
 
     // ---- which rows: the tiles with the most positions first
@@ -304,6 +318,8 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
         const int sub = lane >> 1, odd = lane & 1;
         // Codes: block b (16 positions) of the warp's two, entries 64p + 32 odd .. + 31 of the row at position sub.
         typedef uint32_t Codes[2][PANELS][BITS];
+        const int window = in_register(a.window), sinks = in_register(a.sinks), row_bytes = in_register(a.l.row), v_codes = in_register(a.l.v_codes),
+                  k_scales = in_register(a.l.k_scales), v_scales = in_register(a.l.v_scales), slots = in_register(a.l.page - 1);
         float sk = 0.f, sv = 0.f, unit = 0.f;
         int page[2] = {-1, -1}, next[2] = {-1, -1};  // pages of the blocks, of this tile and of the next
         int base = 0;                                // first position of the warp in the tile
@@ -322,7 +338,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             for (int b = 0; b < 2; ++b) {
                 page[b] = next[b];
                 chunk[b] = a.pool + a48p::chunk_at(a.l, max(page[b], 0), kvh);
-                slot[b] = (base + 16 * b) & (a.l.page - 1);
+                slot[b] = (base + 16 * b) & slots;
             }
         };
         auto load_codes = [&](Codes& x, int part) {
@@ -331,8 +347,8 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
 #pragma unroll
                 for (int p = 0; p < PANELS; ++p) {
                     const int at = (2 * p + odd) * 4 * BITS;
-                    const bool there = page[b] >= 0 && at < a.l.row;
-                    const uint8_t* src = chunk[b] + part * a.l.v_codes + (slot[b] + sub) * a.l.row + at;
+                    const bool there = page[b] >= 0 && at < row_bytes;
+                    const uint8_t* src = chunk[b] + part * v_codes + (slot[b] + sub) * row_bytes + at;
                     if constexpr (BITS == 3) {
 #pragma unroll
                         for (int i = 0; i < 3; ++i) x[b][p][i] = there ? __ldg(reinterpret_cast<const uint32_t*>(src) + i) : 0u;
@@ -350,8 +366,8 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             const bool there = page[b] >= 0;
             const uint8_t* from = b ? chunk[1] : chunk[0];
             const int at = (b ? slot[1] : slot[0]) + (lane & 15);
-            sk = there ? __ldg(reinterpret_cast<const float*>(from + a.l.k_scales) + at) : 0.f;
-            sv = there ? __ldg(reinterpret_cast<const float*>(from + a.l.v_scales) + at) : 0.f;
+            sk = there ? __ldg(reinterpret_cast<const float*>(from + k_scales) + at) : 0.f;
+            sv = there ? __ldg(reinterpret_cast<const float*>(from + v_scales) + at) : 0.f;
         };
         auto store_codes = [&](uint8_t* buf, const Codes& x, const uint8_t* bos) {
 #pragma unroll
@@ -390,85 +406,75 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                 }
             }
         };
-        // The parts K(0) V(0) K(1) ... one after the other, the next two's codes under way.  (One piece of code for keys and
-        // values: the loops of a CTA have to fit in the instruction cache together.)
-        Codes now, next_codes;
+        Codes keys, values;
         look_up(0);
         if (n_tiles > 0) {
             locate(0);
             load_scales();
-            load_codes(now, 0);
-            load_codes(next_codes, 1);
+            load_codes(keys, 0);
+            load_codes(values, 1);
             look_up(1);
         }
         queries_sync();
         const float factor = scalbnf(a.scale * 1.4426950408889634f, -query_exponent(*q_top));
-        const uint8_t* bos = nullptr;  // position 0's codes, in the tile that has it
-#pragma unroll 1
-        for (int n = 0; n < 2 * n_tiles; ++n) {
-            const int t = n >> 1, part = n & 1;
-            uint32_t sick = 0;
-            float key = 0.f, f = 0.f;
-            bool dead = false;
-            if (part == 0) {
-                const int pos = base + lane;
-                bos = BITS == 3 && base == 0 && page[0] >= 0 ? chunk[0] + a.l.bos : nullptr;
-                dead = (lane < 16 ? page[0] : page[1]) < 0 && pos <= pos_hi;
-                // ---- scales; one counts if it is finite and some row may see its position
-                const bool may = pos <= pos_hi && (a.window == 0 || pos > pos_lo - a.window || pos < a.sinks);
-                const bool finite = sk <= 3.4e38f && sv <= 3.4e38f;
-                // The scores of a row that does not see a position are set to -inf ahead of these factors, so they have to be
-                // positive and finite; where the scales are not, the rows that do see the position get no numbers from its key.
-                key = finite && may ? fminf(fmaxf(sk * factor, 1e-37f), 3e38f) : 1.f;
-                f = finite && may ? sv : 0.f;
-                sick = __ballot_sync(0xffffffffu, may && !finite);
-                if (convert_any(unit == 0.f ? f > 0.f : f * unit > 64.f)) {
-                    float top = f;
-#pragma unroll
-                    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                    if (lane == 0) top_part[w] = top;
-                    convert_sync();
-                    top = fmaxf(fmaxf(top_part[0], top_part[1]), fmaxf(top_part[2], top_part[3]));
-                    // two octaves of room, so that scales of one size do not come back here; within fp32's exponents
-                    unit = scalbnf(1.f, min(max(5 - (ilogbf(top) + 2), -120), 120));
-                }
-            }
-            // (The ring is what keeps the scales of four tiles apart: K(t) can be written once the scores of t - 2 are done,
-            // and the weights of t - 3 were taken before the scores of t - 2 were issued.)
+        auto wait_empty = [&](int n) {
             if (n >= RING) mbar_wait(bar_empty + 8 * (n % RING), (n / RING & 1) ^ 1, abort_flag, WAIT_EMPTY, n);
-            uint8_t* buf = smem + n % RING * C::BUF;
-            store_codes(buf, now, bos ? bos + part * (a.l.padded / 2) : nullptr);
-            if (part == 0) {
-                TileScales& ts = scales[t % SCALES];
-                ts.scale[r >> 1][r & 1] = key;
-                ts.scale[r >> 1][2 + (r & 1)] = f * unit;
-                const uint32_t gone = __ballot_sync(0xffffffffu, dead);
-                if (lane == 0) ts.dead[w] = gone;
-                if (r == 0) ts.unit = unit;
-                if (sick) {
-                    __syncwarp();
-                    for (int i = 0; i < PD / 8; ++i)
-                        if ((sick >> lane) & 1)
-                            *reinterpret_cast<uint4*>(buf + i / 8 * PANEL + r * 128 + i % 8 * 16) =
-                                make_uint4(0x7e007e00u, 0x7e007e00u, 0x7e007e00u, 0x7e007e00u);
-                }
-            }
+            return smem + n % RING * C::BUF;
+        };
+        auto publish = [&](int n) {
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             mbar_arrive(bar_full + 8 * (n % RING));
+        };
+#pragma unroll 1
+        for (int t = 0; t < n_tiles; ++t) {
+            const int pos = base + lane;
+            const uint8_t* bos = BITS == 3 && base == 0 && page[0] >= 0 ? chunk[0] + a.l.bos : nullptr;  // position 0's codes
+            const bool dead = (lane < 16 ? page[0] : page[1]) < 0 && pos <= pos_hi;
+            // ---- scales; one counts if it is finite and some row may see its position
+            const bool may = pos <= pos_hi && (window == 0 || pos > pos_lo - window || pos < sinks);
+            const bool finite = sk <= 3.4e38f && sv <= 3.4e38f;
+            // The scores of a row that does not see a position are set to -inf ahead of these factors, so they have to be
+            // positive and finite; where the scales are not, the rows that do see the position get no numbers from its key.
+            const float key = finite && may ? fminf(fmaxf(sk * factor, 1e-37f), 3e38f) : 1.f, f = finite && may ? sv : 0.f;
+            const uint32_t sick = __ballot_sync(0xffffffffu, may && !finite), gone = __ballot_sync(0xffffffffu, dead);
+            if (convert_any(unit == 0.f ? f > 0.f : f * unit > 64.f)) {
+                float top = f;
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-                for (int p = 0; p < PANELS; ++p)
-#pragma unroll
-                    for (int i = 0; i < BITS; ++i) now[b][p][i] = next_codes[b][p][i];
-            if (n + 2 < 2 * n_tiles) {  // the same part of the next tile
-                if (part == 0) {
-                    locate(t + 1);
-                    load_scales();
-                } else {
-                    look_up(t + 2);
-                }
-                load_codes(next_codes, part);
+                for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                if (lane == 0) top_part[w] = top;
+                convert_sync();
+                top = fmaxf(fmaxf(top_part[0], top_part[1]), fmaxf(top_part[2], top_part[3]));
+                // two octaves of room, so that scales of one size do not come back here; within fp32's exponents
+                unit = scalbnf(1.f, min(max(5 - (ilogbf(top) + 2), -120), 120));
+            }
+            // ---- keys.  (The ring is what keeps the scales of four tiles apart: K(t) can be written once the scores of
+            // t - 2 are done, and the weights of t - 3 were taken before the scores of t - 2 were issued.)
+            uint8_t* buf = wait_empty(2 * t);
+            store_codes(buf, keys, bos);
+            TileScales& ts = scales[t % SCALES];
+            ts.scale[r >> 1][r & 1] = key;
+            ts.scale[r >> 1][2 + (r & 1)] = f * unit;
+            if (lane == 0) ts.dead[w] = gone;
+            if (r == 0) ts.unit = unit;
+            if (sick) {
+                __syncwarp();
+                for (int i = 0; i < PD / 8; ++i)
+                    if ((sick >> lane) & 1)
+                        *reinterpret_cast<uint4*>(buf + i / 8 * PANEL + r * 128 + i % 8 * 16) =
+                            make_uint4(0x7e007e00u, 0x7e007e00u, 0x7e007e00u, 0x7e007e00u);
+            }
+            publish(2 * t);
+            // ---- the next tile's keys under way, then the values of this one
+            if (t + 1 < n_tiles) {
+                locate(t + 1);
+                load_scales();
+                load_codes(keys, 0);
+            }
+            store_codes(wait_empty(2 * t + 1), values, bos ? bos + a.l.padded / 2 : nullptr);
+            publish(2 * t + 1);
+            if (t + 1 < n_tiles) {
+                load_codes(values, 1);
+                look_up(t + 2);
             }
         }
     } else {
@@ -525,28 +531,34 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
         const uint64_t q_desc = smem_desc(sq + half * C::BUF);
         auto issue_s = [&](int t) {
             const uint64_t k_desc = smem_desc(wait_full(2 * t));
+            if (elect()) {
 #pragma unroll
-            for (int ks = 0; ks < PD / 16; ++ks) {
-                constexpr int STEP = PANEL / 16;  // of a descriptor's address, per 64 entries
-                mma_ss(t_s, q_desc + ks / 4 * STEP + 2 * (ks % 4), k_desc + ks / 4 * STEP + 2 * (ks % 4), idesc_s, ks != 0);
+                for (int ks = 0; ks < PD / 16; ++ks) {
+                    constexpr int STEP = PANEL / 16;  // of a descriptor's address, per 64 entries
+                    mma_ss(t_s, q_desc + ks / 4 * STEP + 2 * (ks % 4), k_desc + ks / 4 * STEP + 2 * (ks % 4), idesc_s, ks != 0);
+                }
+                tc_commit(bar_s + 8 * half);
+                tc_commit(bar_empty + 8 * (2 * t % RING));
             }
-            tc_commit(bar_s + 8 * half);
-            tc_commit(bar_empty + 8 * (2 * t % RING));
+            __syncwarp();
         };
         auto issue_o = [&](int t, bool last) {
             const uint64_t v_desc = smem_desc(wait_full(2 * t + 1));
-            mma_ts(t_o, t_s, v_desc, idesc_o, t != 0);
+            if (elect()) {
+                mma_ts(t_o, t_s, v_desc, idesc_o, t != 0);
 #pragma unroll
-            for (int j = 1; j < TK / 16; ++j) mma_ts(t_o, t_s + 8 * j, v_desc + 2048 / 16 * j, idesc_o, 1);
-            tc_commit(bar_o + 8 * half);
-            // (not on the last tile: nothing waits for it, and the CTA must not end before it has arrived)
-            if (!last) tc_commit(bar_empty + 8 * ((2 * t + 1) % RING));
+                for (int j = 1; j < TK / 16; ++j) mma_ts(t_o, t_s + 8 * j, v_desc + 2048 / 16 * j, idesc_o, 1);
+                tc_commit(bar_o + 8 * half);
+                // (not on the last tile: nothing waits for it, and the CTA must not end before it has arrived)
+                if (!last) tc_commit(bar_empty + 8 * ((2 * t + 1) % RING));
+            }
+            __syncwarp();
         };
-        const bool issuer = (threadIdx.x & (TQ - 1)) == 0;
+        const bool issuer = (warp & 3) == 0;
         const int used = half < halves ? n_tiles : 0;
+        const int window = in_register(a.window), sinks = in_register(a.sinks);
         tile_sync(half);
         if (issuer && used > 0) issue_s(0);
-        __syncwarp();
         // the four rows of this thread between loads and stores: lanes g, g + 8, g + 16, g + 24 of the warp
         const int g = lane >> 2, c0 = 2 * (lane & 3);
         float m[4], l[4], unit = 0.f;
@@ -558,13 +570,14 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
         }
         const int lim_lo = __reduce_min_sync(0xffffffffu, min(min(lim[0], lim[1]), min(lim[2], lim[3])));
         const int lim_hi = __reduce_max_sync(0xffffffffu, max(max(lim[0], lim[1]), max(lim[2], lim[3])));
+        if (halves == 2 && half == 1 && used > 0) turn_pass(1);
         for (int t = 0; t < used; ++t) {
             mbar_wait(bar_s + 8 * half, t & 1, abort_flag, WAIT_S, t);
             tc_fence_after();
             const TileScales& ts = scales[t % SCALES];
             const int base = span.block(v0 + t) * TK;
             const uint4 dead = *reinterpret_cast<const uint4*>(ts.dead);
-            const bool whole = base + TK - 1 <= lim_lo && (a.window == 0 || base > lim_hi - a.window || base + TK - 1 < a.sinks) &&
+            const bool whole = base + TK - 1 <= lim_lo && (window == 0 || base > lim_hi - window || base + TK - 1 < sinks) &&
                                (dead.x | dead.y | dead.z | dead.w) == 0;
             if (!whole) {  // the scores that a row does not see become -inf
 #pragma unroll 1
@@ -577,7 +590,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
                         const int n = 16 * c + 8 * ((i >> 2) & 1) + c0 + (i & 1), to = lim[(i >> 3) * 2 + ((i >> 1) & 1)] - base;
-                        const bool seen = n <= to && (a.window == 0 || n > to - a.window || n < a.sinks - base) && !((gone >> (8 * ((i >> 2) & 1) + (i & 1))) & 1);
+                        const bool seen = n <= to && (window == 0 || n > to - window || n < sinks - base) && !((gone >> (8 * ((i >> 2) & 1) + (i & 1))) & 1);
                         if (!seen) acc[i >> 3][i & 7] = 0xff800000u;
                     }
                     tmem_st_16x16(s_at + 16 * c, acc[0]);
@@ -585,6 +598,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                 }
                 tmem_wait_st();
             }
+            if (halves == 2) turn_wait(half);
             // ---- 64 columns, then the other 64
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {
@@ -598,6 +612,9 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                     uint32_t acc[2][2][8];
                     tmem_ld_16x16(s_at + 64 * h, acc[0][0]);
                     tmem_ld_16x16(s_at + (16u << 16) + 64 * h, acc[0][1]);
+                    ulonglong2 scale[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) scale[k] = *reinterpret_cast<const ulonglong2*>(ts.scale[32 * h + 4 * k + c0 / 2]);
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         tmem_wait_ld(acc[c & 1]);
@@ -607,15 +624,14 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                         }
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {
-                            const ulonglong2 scale = *reinterpret_cast<const ulonglong2*>(ts.scale[32 * h + 8 * c + 4 * k + c0 / 2]);
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 const uint32_t* from = acc[c & 1][i >> 1] + 4 * k + 2 * (i & 1);
                                 float y0, y1, w0, w1;
-                                unpack2(fma2(pack2(__uint_as_float(from[0]), __uint_as_float(from[1])), scale.x, m_2[i]), y0, y1);
+                                unpack2(fma2(pack2(__uint_as_float(from[0]), __uint_as_float(from[1])), scale[2 * c + k].x, m_2[i]), y0, y1);
                                 const f2 e = pack2(exp2_approx(y0), exp2_approx(y1));
                                 sum_2[i] = add2(sum_2[i], e);
-                                unpack2(mul2(e, scale.y), w0, w1);
+                                unpack2(mul2(e, scale[2 * c + k].y), w0, w1);
                                 const __half2 w = __floats2half2_rn(w0, w1);
                                 p[i >> 1][2 * (2 * c + k) + (i & 1)] = *reinterpret_cast<const uint32_t*>(&w);
                             }
@@ -694,6 +710,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                 for (int i = 0; i < 4; ++i) l[i] += sum[i];
                 tmem_st_16x32(s_at + 32 * h, p[0]);  // (over scores that have been taken)
                 tmem_st_16x32(s_at + (16u << 16) + 32 * h, p[1]);
+                if (h == 0 && halves == 2 && (half == 0 || t + 1 < used)) turn_pass(half);
             }
             tmem_wait_st();
             tc_fence_before();
@@ -703,7 +720,6 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                 issue_o(t, t + 1 == used);
                 if (t + 1 < used) issue_s(t + 1);  // behind O(t) on the pipe: P(t) is read before scores go over it
             }
-            __syncwarp();
         }
         // ---- out = O / (unit l), one row per thread again
 #pragma unroll
