@@ -26,7 +26,7 @@ using a48p::Span;
 using a48p::span_of;
 
 // ---------------------------------------------------------------------------------------------------- few rows
-// A CTA of four warps takes a tile of 8 NT rows of one head and one split of the positions; a warp takes 16 positions at a
+// A CTA of four warps takes a tile of 8 NT rows of one head and one part of the positions; a warp takes 16 positions at a
 // time, straight from memory into the registers that hold the operands of its MMAs, the next 16 under way meanwhile.
 //
 // The positions are the M side of both contractions (m16n8k16, fp16, fp32 accumulators), the rows the N side: S^T = C Q^T
@@ -39,7 +39,7 @@ using a48p::span_of;
 //
 // The running maximum is one reference per row that moves only when a score exceeds it by 2^8: then nothing is reduced
 // across lanes in the steady state, and weights stay below 2^14.
-constexpr int ROW_WARPS = 4;
+constexpr int ROW_WARPS = 4, MAX_RANKS = 8;
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile(
@@ -121,32 +121,55 @@ struct Loaded {  // a lane's part of 16 positions
 };
 
 template <int BITS, int PD, int NT>
-__global__ void __launch_bounds__(32 * ROW_WARPS) attn_paged_rows_kernel(const __grid_constant__ AttnArgs a) {
-    constexpr int ROWS = 8 * NT, NK = PD / 8, LD = PD + 4;
-    __shared__ alignas(16) __half q_rows[ROWS][PD + 8];
-    __shared__ float row_mul[ROWS];
-    __shared__ float o_part[ROW_WARPS][ROWS][LD];
-    __shared__ float m_part[ROW_WARPS][ROWS], l_part[ROW_WARPS][ROWS];
-    a48_pdl_prologue();
+struct RowsShared {
+    static constexpr int ROWS = 8 * NT;
+    alignas(16) __half q[ROWS][PD + 8];
+    float mul[ROWS];
+    alignas(16) float o[ROW_WARPS][ROWS][PD + 4];  // the warps' sums; the first then holds the CTA's
+    float m[ROW_WARPS][ROWS], l[ROW_WARPS][ROWS];
+    float cta_m[ROWS], cta_l[ROWS];
+};
+
+__device__ __forceinline__ void cluster_sync_all() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t of_rank(const void* p, int rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float ld_rank(uint32_t at) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ld_rank4(uint32_t at) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
+    return v;
+}
+
+template <int BITS, int PD, int NT>
+__device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, PD, NT>& sm) {
+    constexpr int ROWS = 8 * NT, NK = PD / 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int kvh = blockIdx.x % a.l.kv_heads, seq = blockIdx.x / a.l.kv_heads / a.tiles;
     const int r0 = (blockIdx.x / a.l.kv_heads % a.tiles) * ROWS;
     const int start = __ldg(a.b.q_start + seq), q_len = __ldg(a.b.q_start + seq + 1) - start;
     const long long all_rows = (long long)q_len * a.group;
-    if (all_rows > a.few_rows || r0 >= all_rows || start < 0 || start + q_len > a.b.n_tokens) return;
-    const int rows = min(ROWS, (int)all_rows - r0);
+    // (the same for all CTAs of a cluster)
+    if (all_rows > a.few_rows || r0 >= all_rows || start < 0 || q_len > a.b.n_tokens - start) return;
+    const int rows = min(ROWS, (int)min(all_rows - r0, (long long)ROWS));
     const int pos0 = __ldg(a.b.kv_len + seq) - q_len;
     const int pos_lo = pos0 + r0 / a.group, pos_hi = pos0 + (r0 + rows - 1) / a.group;
     const Span span = span_of<4>(a, pos_lo, pos_hi);
-    const int v_begin = blockIdx.y * a.per_split;
-    const int v_end = blockIdx.y + 1 == gridDim.y ? span.count : min(span.count, v_begin + a.per_split);
+    // positions are dealt out evenly, two blocks for every warp of a part at least
+    const int rank = blockIdx.y % a.ranks, cluster = blockIdx.y / a.ranks, parts = gridDim.y;
+    const int per = max(2 * ROW_WARPS, (span.count + parts - 1) / parts);
+    const int v_begin = blockIdx.y * per, v_end = min(span.count, v_begin + per);
 
     auto row_id = [&](int r) { return (size_t)(start + (r0 + r) / a.group) * a.heads + kvh * a.group + (r0 + r) % a.group; };
-    if (v_begin >= v_end && a.splits > 1) {  // nothing in this split
-        if (threadIdx.x < rows) a.part_ml[(size_t)blockIdx.y * a.b.n_tokens * a.heads + row_id(threadIdx.x)] = make_float2(0.f, 0.f);
-        return;
-    }
-
     // ---- the query rows: a warp brings one at a time to fp16
     for (int r = warp; r < ROWS; r += ROW_WARPS) {
         float x[4] = {};
@@ -162,10 +185,10 @@ __global__ void __launch_bounds__(32 * ROW_WARPS) attn_paged_rows_kernel(const _
         const int e = mx > 0.f && mx <= 3.4e38f ? 14 - ilogbf(mx) : 0;  // the largest goes to [2^14, 2^15)
         if (4 * lane < PD) {
             const __half2 lo = __floats2half2_rn(scalbnf(x[0], e), scalbnf(x[1], e)), hi = __floats2half2_rn(scalbnf(x[2], e), scalbnf(x[3], e));
-            *reinterpret_cast<uint2*>(&q_rows[r][4 * lane]) =
+            *reinterpret_cast<uint2*>(&sm.q[r][4 * lane]) =
                 make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
         }
-        if (lane == 0) row_mul[r] = scalbnf(a.scale * 1.4426950408889634f, -e);
+        if (lane == 0) sm.mul[r] = scalbnf(a.scale * 1.4426950408889634f, -e);
     }
     __syncthreads();
     uint32_t qf[NT][NK];
@@ -175,13 +198,13 @@ __global__ void __launch_bounds__(32 * ROW_WARPS) attn_paged_rows_kernel(const _
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
-            const __half2 h = __halves2half2(q_rows[8 * n + g][k_entry<BITS, PD>(t, i, 0)], q_rows[8 * n + g][k_entry<BITS, PD>(t, i, 1)]);
+            const __half2 h = __halves2half2(sm.q[8 * n + g][k_entry<BITS, PD>(t, i, 0)], sm.q[8 * n + g][k_entry<BITS, PD>(t, i, 1)]);
             qf[n][i] = *reinterpret_cast<const uint32_t*>(&h);
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int r = 8 * n + 2 * t + i;
-            mul[n][i] = row_mul[r];
+            mul[n][i] = sm.mul[r];
             lim[n][i] = r < rows ? pos0 + (r0 + r) / a.group : INT_MIN;  // the last position the row sees
         }
     }
@@ -362,7 +385,7 @@ __global__ void __launch_bounds__(32 * ROW_WARPS) attn_paged_rows_kernel(const _
         }
     }
 
-    // ---- the warps' parts meet in shared memory
+    // ---- the warps' sums meet in shared memory
     const float unit = v_unit == 0.f ? 0.f : 1.f / v_unit;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -371,44 +394,93 @@ __global__ void __launch_bounds__(32 * ROW_WARPS) attn_paged_rows_kernel(const _
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], d);
             const int r = 8 * n + 2 * t + i;
-            if (g == 0) m_part[warp][r] = m[n][i], l_part[warp][r] = l[n][i];
+            if (g == 0) sm.m[warp][r] = m[n][i], sm.l[warp][r] = l[n][i];
 #pragma unroll
-            for (int k = 0; k < PD / 16; ++k) {
-                float* dst = &o_part[warp][r][NK * g + 2 * k];
-                dst[0] = o[n][k][i] * unit;
-                dst[1] = o[n][k][i + 2] * unit;
-            }
+            for (int k = 0; k < PD / 16; ++k)
+                *reinterpret_cast<float2*>(&sm.o[warp][r][NK * g + 2 * k]) = make_float2(o[n][k][i] * unit, o[n][k][i + 2] * unit);
         }
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < rows * (PD / 4); i += 32 * ROW_WARPS) {
-        const int r = i / (PD / 4), c = 4 * (i % (PD / 4));
-        if (c >= a.l.hd) continue;
-        float top = m_part[0][r], sum = 0.f, acc[4] = {};
-#pragma unroll
-        for (int w = 1; w < ROW_WARPS; ++w) top = fmaxf(top, m_part[w][r]);
-#pragma unroll
-        for (int w = 0; w < ROW_WARPS; ++w) {
-            const float corr = exp2_approx(m_part[w][r] - top);
-            const float4 x = *reinterpret_cast<const float4*>(&o_part[w][r][c]);
-            sum += corr * l_part[w][r];
-            acc[0] += corr * x.x, acc[1] += corr * x.y, acc[2] += corr * x.z, acc[3] += corr * x.w;
-        }
+    auto finish = [&](int r, int c, float top, float sum, const float (&acc)[4]) {
         const size_t id = row_id(r);
-        if (a.splits > 1) {
-            const size_t at = (size_t)blockIdx.y * a.b.n_tokens * a.heads + id;
+        if (a.clusters > 1) {
+            const size_t at = (size_t)cluster * a.b.n_tokens * a.heads + id;
             reinterpret_cast<float4*>(a.part_o + at * 128)[c / 4] = make_float4(acc[0], acc[1], acc[2], acc[3]);
             if (c == 0) a.part_ml[at] = make_float2(top, sum);
         } else {
-            const float inv = sum > 0.f ? 1.f / sum : 0.f;
+            const float inv = sum != 0.f ? 1.f / sum : 0.f;
             const __nv_bfloat162 lo = __floats2bfloat162_rn(acc[0] * inv, acc[1] * inv), hi = __floats2bfloat162_rn(acc[2] * inv, acc[3] * inv);
             *reinterpret_cast<uint2*>(a.out + id / a.heads * a.out_stride + id % a.heads * a.l.hd + c) =
                 make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
         }
+    };
+    for (int i = threadIdx.x; i < rows * (PD / 4); i += 32 * ROW_WARPS) {
+        const int r = i / (PD / 4), c = 4 * (i % (PD / 4));
+        if (c >= a.l.hd) continue;
+        float top = sm.m[0][r], sum = 0.f, acc[4] = {};
+#pragma unroll
+        for (int w = 1; w < ROW_WARPS; ++w) top = fmaxf(top, sm.m[w][r]);
+#pragma unroll
+        for (int w = 0; w < ROW_WARPS; ++w) {
+            const float corr = exp2_approx(sm.m[w][r] - top);
+            const float4 x = *reinterpret_cast<const float4*>(&sm.o[w][r][c]);
+            sum += corr * sm.l[w][r];
+            acc[0] += corr * x.x, acc[1] += corr * x.y, acc[2] += corr * x.z, acc[3] += corr * x.w;
+        }
+        if (a.ranks == 1) {
+            finish(r, c, top, sum, acc);
+        } else {
+            *reinterpret_cast<float4*>(&sm.o[0][r][c]) = make_float4(acc[0], acc[1], acc[2], acc[3]);  // (read by this thread alone)
+            if (c == 0) sm.cta_m[r] = top, sm.cta_l[r] = sum;
+        }
+    }
+    if (a.ranks == 1) return;
+    // ---- and the CTAs' sums through distributed shared memory: every rank finishes a share of the columns
+    cluster_sync_all();
+    for (int i = threadIdx.x + 32 * ROW_WARPS * rank; i < rows * (PD / 4); i += 32 * ROW_WARPS * a.ranks) {
+        const int r = i / (PD / 4), c = 4 * (i % (PD / 4));
+        if (c >= a.l.hd) continue;
+        float ms[MAX_RANKS], ls[MAX_RANKS], top = -1e30f, sum = 0.f, acc[4] = {};
+        float4 x[MAX_RANKS];
+#pragma unroll
+        for (int k = 0; k < MAX_RANKS; ++k) {
+            if (k >= a.ranks) break;
+            ms[k] = ld_rank(of_rank(&sm.cta_m[r], k));
+            ls[k] = ld_rank(of_rank(&sm.cta_l[r], k));
+            x[k] = ld_rank4(of_rank(&sm.o[0][r][c], k));
+        }
+#pragma unroll
+        for (int k = 0; k < MAX_RANKS; ++k)
+            if (k < a.ranks) top = fmaxf(top, ms[k]);
+#pragma unroll
+        for (int k = 0; k < MAX_RANKS; ++k) {
+            if (k >= a.ranks) break;
+            const float corr = exp2_approx(ms[k] - top);
+            sum += corr * ls[k];
+            acc[0] += corr * x[k].x, acc[1] += corr * x[k].y, acc[2] += corr * x[k].z, acc[3] += corr * x[k].w;
+        }
+        finish(r, c, top, sum, acc);
+    }
+    cluster_sync_all();  // no CTA's shared memory goes before all have read it
+}
+
+// Registers are held to what lets four CTAs of eight rows (two of sixteen) share an SM: loads in flight are what hides
+// memory.
+template <int BITS, int PD, int NT>
+__global__ void __launch_bounds__(32 * ROW_WARPS, NT == 1 ? 4 : 2) attn_paged_rows_kernel(const __grid_constant__ AttnArgs a) {
+    __shared__ RowsShared<BITS, PD, NT> sm;
+    if (!a.beside) {
+        a48_pdl_prologue();
+        attend_rows<BITS, PD, NT>(a, sm);
+    } else {
+        // Launched behind the tile kernel, which lets it start once all that came before is done: the two write different
+        // rows.  The wait at the end keeps this kernel from completing ahead of the other.
+        attend_rows<BITS, PD, NT>(a, sm);
+        a48_pdl_prologue();
     }
 }
 
-// The splits' parts of a row, in order.  One warp per (token, query head), four head dims per lane.
+// The parts of a row, in order.  One warp per (token, query head), four head dims per lane.
 __global__ void __launch_bounds__(256) attn_paged_join_kernel(const __grid_constant__ AttnArgs a) {
     a48_pdl_prologue();
     const int lane = threadIdx.x & 31;
@@ -419,7 +491,7 @@ __global__ void __launch_bounds__(256) attn_paged_join_kernel(const __grid_const
     if (s < 0) return;
     const int start = __ldg(a.b.q_start + s), end = __ldg(a.b.q_start + s + 1);
     const bool many = (long long)(end - start) * a.group > a.few_rows;
-    const int splits = many ? a.tc_splits : a.splits, tiles = many ? a.tc_tiles : a.tiles;
+    const int splits = many ? a.tc_splits : a.clusters, tiles = many ? a.tc_tiles : a.tiles;
     if (splits == 1 || end > a.b.n_tokens) return;
     const long long tile = ((long long)(token - start) * a.group + head % a.group) / (many ? a48p::TILE_ROWS : a.tile_rows);
     if (tiles > 0 && tile >= tiles) return;  // past max_q
@@ -454,44 +526,41 @@ constexpr int kFar = 1 << 30;  // what a window is cut to: position differences 
 // How a call is cut up; from its bounds alone, so that the workspace can be asked for ahead.
 struct Plan {
     bool many;  // some sequence may be the tile kernel's
-    int nt, tiles, splits, per_split, tc_tiles, tc_splits, tc_per_split;
+    int nt, few_rows, tiles, ranks, clusters, tc_tiles, tc_splits;
     size_t part_o, bytes;  // offset of the partial sums (exponents and sums of p come first), workspace
 };
 
-// `positions` in steps of `step`, in at most `splits` parts of at least `least` steps
-void cut(long long positions, int step, long long splits, int least, int& n, int& per) {
-    const long long steps = (positions + step - 1) / step, most = (steps + least - 1) / least;
-    if (splits > most) splits = most;
-    if (splits > 64) splits = 64;
-    if (splits < 1) splits = 1;
-    per = (int)((steps + splits - 1) / splits);
-    n = (int)((steps + per - 1) / per);
-}
+long long up(long long x, long long y) { return (x + y - 1) / y; }
+int within(long long x, long long lo, long long hi) { return (int)(x < lo ? lo : x > hi ? hi : x); }
 
 Plan plan_of(const bitnet_a48_paged_cache& c, const bitnet_a48_paged_batch& b, int heads, int window, int sinks) {
     Plan p;
     const long long group = heads / c.n_kv_heads, rows = (long long)b.max_q * group;
     p.many = rows > FEW_ROWS;
-    const int few = (int)(rows < FEW_ROWS ? rows : FEW_ROWS);
+    // Rows kernel.  Where some sequences are the tile kernel's, the others are taken to be decoding: one tile of rows.
+    const int few = p.many ? (group <= 8 ? 8 : 16) : (int)rows;
     p.nt = few > 8 ? 2 : 1;
-    p.tiles = (few + 8 * p.nt - 1) / (8 * p.nt);
+    p.tiles = (int)up(few, 8 * p.nt);
+    p.few_rows = p.many ? few : INT_MAX;
     long long reach = (long long)b.max_pages * c.page_size;
     if (b.max_kv < reach) reach = b.max_kv;
     // positions a tile of `span` tokens may see
     auto seen = [&](long long span) { return window > 0 && window + sinks + span < reach ? window + sinks + span : reach; };
-    // Few rows: one wave of CTAs (four to an SM), as long as every warp of a split has two blocks.
-    const long long ctas = (long long)b.n_seqs * c.n_kv_heads * p.tiles;
-    cut(seen(64), 16, (4 * SMS + ctas - 1) / ctas, 2 * ROW_WARPS, p.splits, p.per_split);
-    // Many: one CTA per SM; split while the tiles do not fill the SMs, into parts of two tiles or more.
-    p.tc_tiles = 0, p.tc_splits = 1, p.tc_per_split = INT_MAX;
+    // Four waves of CTAs at four to an SM, which evens out sequences of unlike lengths, as long as every warp of a part has
+    // two blocks of 16 positions.  Up to eight parts join inside a cluster; more only where those leave SMs idle.
+    const long long base = (long long)b.n_seqs * c.n_kv_heads * p.tiles, most = up(seen(64), 16 * 2 * ROW_WARPS);
+    p.ranks = within(up(16 * SMS, base), 1, most < MAX_RANKS ? most : MAX_RANKS);
+    p.clusters = p.ranks < MAX_RANKS ? 1 : within(2 * SMS / (base * MAX_RANKS), 1, most / MAX_RANKS < 16 ? most / MAX_RANKS : 16);
+    // Tile kernel, one CTA per SM: split while the tiles do not fill the SMs, into parts of two tiles or more.
+    p.tc_tiles = 0, p.tc_splits = 1;
     if (p.many) {
-        const long long direct = (rows + a48p::TILE_ROWS - 1) / a48p::TILE_ROWS;
-        const long long found = (long long)b.n_tokens * group / a48p::TILE_ROWS;
+        const long long direct = up(rows, a48p::TILE_ROWS), found = (long long)b.n_tokens * group / a48p::TILE_ROWS;
         if (direct * b.n_seqs <= found + b.n_seqs) p.tc_tiles = (int)direct;
         const long long real = (p.tc_tiles ? direct * b.n_seqs : found + 1) * c.n_kv_heads;
-        cut(seen(a48p::TILE_ROWS / group + 2 * a48p::TILE_POSITIONS), a48p::TILE_POSITIONS, SMS / real, 2, p.tc_splits, p.tc_per_split);
+        const long long steps = up(seen(a48p::TILE_ROWS / group + 2 * a48p::TILE_POSITIONS), a48p::TILE_POSITIONS);
+        p.tc_splits = within(SMS / real, 1, up(steps, 2) < 64 ? up(steps, 2) : 64);
     }
-    const int parts = p.splits > p.tc_splits ? p.splits : p.tc_splits;
+    const int parts = p.clusters > p.tc_splits ? p.clusters : p.tc_splits;
     const size_t ids = (size_t)b.n_tokens * heads * parts;
     p.part_o = (ids * sizeof(float2) + 255) / 256 * 256;
     p.bytes = parts > 1 ? p.part_o + ids * 128 * sizeof(float) : 0;
@@ -500,9 +569,19 @@ Plan plan_of(const bitnet_a48_paged_cache& c, const bitnet_a48_paged_batch& b, i
 
 template <int BITS, int PD>
 cudaError_t launch_rows(const AttnArgs& a, int nt, cudaStream_t st) {
-    const dim3 grid(a.l.kv_heads * a.b.n_seqs * a.tiles, a.splits), block(32 * ROW_WARPS);
-    return nt == 1 ? a48_launch_pdl(attn_paged_rows_kernel<BITS, PD, 1>, grid, block, 0, st, a)
-                   : a48_launch_pdl(attn_paged_rows_kernel<BITS, PD, 2>, grid, block, 0, st, a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(a.l.kv_heads * a.b.n_seqs * a.tiles, a.ranks * a.clusters);
+    cfg.blockDim = dim3(32 * ROW_WARPS);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim = {1, (unsigned)a.ranks, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = a.ranks > 1 ? 2 : 1;
+    return nt == 1 ? cudaLaunchKernelEx(&cfg, attn_paged_rows_kernel<BITS, PD, 1>, a)
+                   : cudaLaunchKernelEx(&cfg, attn_paged_rows_kernel<BITS, PD, 2>, a);
 }
 
 // (the caches and batches that reach this have been checked)
@@ -551,9 +630,10 @@ bitnet_a48_status bitnet_a48_attention_paged(const bitnet_a48_paged_cache* cache
     a.heads = n_heads, a.group = n_heads / cache->n_kv_heads;
     a.window = window < kFar ? window : kFar, a.sinks = window > 0 ? sinks : 0;
     a.scale = scale > 0.f ? scale : 1.f / sqrtf((float)cache->head_dim);
-    a.few_rows = p.many ? FEW_ROWS : INT_MAX;
-    a.tiles = p.tiles, a.tile_rows = 8 * p.nt, a.splits = p.splits, a.per_split = p.per_split;
-    a.tc_tiles = p.tc_tiles, a.tc_splits = p.tc_splits, a.tc_per_split = p.tc_per_split;
+    a.few_rows = p.few_rows;
+    a.tiles = p.tiles, a.tile_rows = 8 * p.nt, a.ranks = p.ranks, a.clusters = p.clusters;
+    a.beside = p.many;
+    a.tc_tiles = p.tc_tiles, a.tc_splits = p.tc_splits;
     a.part_ml = static_cast<float2*>(workspace_dev);
     a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + p.part_o);
     if (p.many && (st = a48p::launch_tiles(a, cu)) != BITNET_A48_OK) return st;

@@ -16,12 +16,14 @@ struct AttnArgs {
     float scale;
     // sequences with at most this many rows (new tokens x group) are the rows kernel's
     int few_rows;
-    // rows kernel: tiles of rows per sequence, splits of the positions, 16-position blocks per split
-    int tiles, tile_rows, splits, per_split;
-    // tile kernel: tiles of 256 rows per sequence (0: found by search), splits, 128-position tiles per split
-    int tc_tiles, tc_splits, tc_per_split;
-    float* part_o;   // [split][token * heads + head][128]: sums of p sv d, relative to 2^part_m
-    float2* part_ml;  // [split][token * heads + head]: exponent of the reference, sum of p
+    // rows kernel: tiles of rows per sequence, rows of a tile, parts of the positions: `ranks` CTAs of a cluster that join
+    // their sums, `clusters` of them that leave their sums to the join kernel
+    int tiles, tile_rows, ranks, clusters;
+    bool beside;  // the rows kernel runs beside the tile kernel launched ahead of it
+    // tile kernel: tiles of 256 rows per sequence (0: found by search), parts of the positions
+    int tc_tiles, tc_splits;
+    float* part_o;   // [part][token * heads + head][128]: sums of p sv d, relative to 2^part_m
+    float2* part_ml;  // [part][token * heads + head]: exponent of the reference, sum of p
 };
 
 // What a tile of rows sees of its sequence: blocks of 2^SHIFT positions, [0, n_sink) and [first, first + count - n_sink).

@@ -265,7 +265,10 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
     // barriers: full[4] | empty[4] | s[2] | o[2]
     const uint32_t bar_full = smem_u32(ctrl), bar_empty = bar_full + 32, bar_s = bar_full + 64, bar_o = bar_full + 80;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // (known to be the same in a warp)
-    a48_pdl_prologue();
+    // (Dependents are let go only once what came before is done and seen: the rows kernel that follows may then start beside
+    // this one.)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // ---- which rows: the tiles with the most positions first
     const int kvh = blockIdx.x % a.l.kv_heads, at = gridDim.x / a.l.kv_heads - 1 - blockIdx.x / a.l.kv_heads;
@@ -286,8 +289,8 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
     const int pos0 = __ldg(a.b.kv_len + seq) - q_len;
     const int pos_lo = pos0 + (int)(r0 / a.group), pos_hi = pos0 + (int)((r0 + rows - 1) / a.group);
     const Span span = a48p::span_of<7>(a, pos_lo, pos_hi);
-    const int v0 = blockIdx.y * a.tc_per_split;
-    const int n_tiles = max(0, (blockIdx.y + 1 == gridDim.y ? span.count : min(span.count, v0 + a.tc_per_split)) - v0);
+    const int per = max(2, (span.count + (int)gridDim.y - 1) / (int)gridDim.y), v0 = blockIdx.y * per;
+    const int n_tiles = max(0, min(span.count, v0 + per) - v0);
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < RING; ++i) {
