@@ -37,8 +37,8 @@ using a48p::span_of;
 // 2t+8, 2t+9, whose words are first merged into halves of the same entry of two positions.  S^T's accumulators become
 // P^T's operand by one 8x8 transpose each.
 //
-// The running maximum is one reference per row that moves only when a score exceeds it by 2^8: then nothing is reduced
-// across lanes in the steady state, and weights stay below 2^14.
+// The running maximum is one reference per row that moves only when a weight would exceed 2^9 (or a value scale its unit by
+// 2^6): nothing is reduced across lanes in the steady state but one vote, and weights stay within fp16.
 constexpr int ROW_WARPS = 4, MAX_RANKS = 8;
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -123,31 +123,36 @@ struct Loaded {  // a lane's part of 16 positions
 template <int BITS, int PD, int NT>
 struct RowsShared {
     static constexpr int ROWS = 8 * NT;
-    alignas(16) __half q[ROWS][PD + 8];
-    float mul[ROWS];
-    alignas(16) float o[ROW_WARPS][ROWS][PD + 4];  // the warps' sums; the first then holds the CTA's
+    float top[ROW_WARPS], factor;
+    alignas(16) float o[ROW_WARPS][ROWS][PD + 4];  // the warps' sums
     float m[ROW_WARPS][ROWS], l[ROW_WARPS][ROWS];
-    float cta_m[ROWS], cta_l[ROWS];
+    int token[ROWS], head[ROWS];
+    // what the cluster's CTAs send: pieces of four head dims, with the exponent of their reference and their sum of p
+    alignas(16) float4 piece[ROWS * PD / 4 + MAX_RANKS];
+    union {
+        alignas(16) __half q[ROWS][PD + 8];
+        float2 piece_ml[ROWS * PD / 4 + MAX_RANKS];
+    };
 };
 
-__device__ __forceinline__ void cluster_sync_all() {
+__device__ __forceinline__ void cluster_arrive() {
     __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ uint32_t of_rank(const void* p, int rank) {
     uint32_t r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
     return r;
 }
-__device__ __forceinline__ float ld_rank(uint32_t at) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
-    return v;
+__device__ __forceinline__ void st_rank(uint32_t at, float4 v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(at), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
-__device__ __forceinline__ float4 ld_rank4(uint32_t at) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
-    return v;
+__device__ __forceinline__ void st_rank(uint32_t at, float2 v) {
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(at), "f"(v.x), "f"(v.y) : "memory");
 }
 
 template <int BITS, int PD, int NT>
@@ -169,30 +174,81 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
     const int per = max(2 * ROW_WARPS, (span.count + parts - 1) / parts);
     const int v_begin = blockIdx.y * per, v_end = min(span.count, v_begin + per);
 
-    auto row_id = [&](int r) { return (size_t)(start + (r0 + r) / a.group) * a.heads + kvh * a.group + (r0 + r) % a.group; };
-    // ---- the query rows: a warp brings one at a time to fp16
-    for (int r = warp; r < ROWS; r += ROW_WARPS) {
-        float x[4] = {};
-        if (r < rows && 4 * lane < a.l.hd) {
-            const size_t id = row_id(r);
-            const uint2 u = __ldg(reinterpret_cast<const uint2*>(a.q + id / a.heads * a.q_stride + id % a.heads * a.l.hd) + lane);
-            x[0] = __uint_as_float(u.x << 16), x[1] = __uint_as_float(u.x & 0xffff0000u);
-            x[2] = __uint_as_float(u.y << 16), x[3] = __uint_as_float(u.y & 0xffff0000u);
-        }
-        float mx = fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])));
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        const int e = mx > 0.f && mx <= 3.4e38f ? 14 - ilogbf(mx) : 0;  // the largest goes to [2^14, 2^15)
-        if (4 * lane < PD) {
-            const __half2 lo = __floats2half2_rn(scalbnf(x[0], e), scalbnf(x[1], e)), hi = __floats2half2_rn(scalbnf(x[2], e), scalbnf(x[3], e));
-            *reinterpret_cast<uint2*>(&sm.q[r][4 * lane]) =
-                make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-        }
-        if (lane == 0) sm.mul[r] = scalbnf(a.scale * 1.4426950408889634f, -e);
+    // ---- the first blocks' pages under way, and which token and head a row is
+    const size_t page_bytes = (size_t)a.l.kv_heads * a.l.chunk;
+    auto page_at = [&](int v) { return v < v_end ? a48p::page_of(a.l, a.b, seq, span.block(v) << 4) : -1; };
+    int v = v_begin + warp;
+    int page[2] = {page_at(v), page_at(v + ROW_WARPS)};
+    if (threadIdx.x < ROWS) {
+        const int in_seq = r0 + min((int)threadIdx.x, rows - 1), i = in_seq / a.group;
+        sm.token[threadIdx.x] = start + i;
+        sm.head[threadIdx.x] = kvh * a.group + in_seq - i * a.group;
     }
     __syncthreads();
+
+    // What a lane reads of 16 positions, as offsets from the block's first key row and first key scale.  (A lane whose
+    // entries lie past the padded head reads some that exist: they meet zeros of the query, or columns that are not stored.)
+    const int row = a.l.row;
+    const uint32_t k_first = BITS == 3 ? 12 * t : PD * BITS / 32 * t, v_first = BITS == 3 ? 12 * (g >> 1) : PD * BITS / 64 * g;
+    const bool k_there = k_first < row, v_there = v_first < row;
+    const uint32_t k_off = (k_there ? k_first : 0) + g * row, v_off = a.l.v_codes + (v_there ? v_first : 0) + 2 * t * row, row8 = 8 * row;
+    const uint32_t sv_off = a.l.v_scales - a.l.k_scales + 4 * g;
+    const uint32_t halves = (g & 1) ? 0x7632u : 0x5410u;
+    const uint8_t* head_chunks = a.pool + (size_t)kvh * a.l.chunk;
+
+    auto load = [&](int v, int page, Loaded<BITS, PD>& x) {
+        page = __shfl_sync(0xffffffffu, page, 0);  // the same for the warp: the addresses are formed once for it
+        const int slot = (span.block(v) << 4) & (a.l.page - 1);
+        const uint8_t* chunk = head_chunks + max(page, 0) * page_bytes;
+        const uint8_t* codes = chunk + slot * row;
+        const uint8_t* scales = chunk + a.l.k_scales + 4 * slot;
+        load_words(codes + k_off, x.k[0]);
+        load_words(codes + (k_off + row8), x.k[1]);
+        load_words(codes + v_off, x.v[0]);
+        load_words(codes + (v_off + row), x.v[1]);
+        load_words(codes + (v_off + row8), x.v[2]);
+        load_words(codes + (v_off + row8 + row), x.v[3]);
+        x.sk[0] = __ldg(reinterpret_cast<const float*>(scales + 4 * g)), x.sk[1] = __ldg(reinterpret_cast<const float*>(scales + (4 * g + 32)));
+        x.sv[0] = __ldg(reinterpret_cast<const float*>(scales + sv_off)), x.sv[1] = __ldg(reinterpret_cast<const float*>(scales + (sv_off + 32)));
+    };
+    Loaded<BITS, PD> x[2];
+    if (v < v_end) load(v, page[0], x[0]);
+
+    // ---- the query rows to fp16 by one power of two (the largest entry of the tile to [2^14, 2^15): a row 2^20 below it
+    // still has all its bits, one 2^29 below it the upper ten)
+    {
+        constexpr int PER = ROWS / ROW_WARPS;
+        float x[PER][4] = {};
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int r = warp + ROW_WARPS * k;
+            if (r < rows && 4 * lane < a.l.hd) {
+                const uint2 u = __ldg(reinterpret_cast<const uint2*>(a.q + sm.token[r] * a.q_stride + (size_t)sm.head[r] * a.l.hd) + lane);
+                x[k][0] = __uint_as_float(u.x << 16), x[k][1] = __uint_as_float(u.x & 0xffff0000u);
+                x[k][2] = __uint_as_float(u.y << 16), x[k][3] = __uint_as_float(u.y & 0xffff0000u);
+            }
+            const float mx = fmaxf(fmaxf(fabsf(x[k][0]), fabsf(x[k][1])), fmaxf(fabsf(x[k][2]), fabsf(x[k][3])));
+            if (mx <= 3.4e38f) top = max(top, __float_as_uint(mx));
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (lane == 0) sm.top[warp] = __uint_as_float(top);
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < ROW_WARPS; ++w) top = max(top, __float_as_uint(sm.top[w]));
+        const int e = top > 0 ? 14 - ilogbf(__uint_as_float(top)) : 0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int r = warp + ROW_WARPS * k;
+            const __half2 lo = __floats2half2_rn(scalbnf(x[k][0], e), scalbnf(x[k][1], e)), hi = __floats2half2_rn(scalbnf(x[k][2], e), scalbnf(x[k][3], e));
+            if (4 * lane < PD)
+                *reinterpret_cast<uint2*>(&sm.q[r][4 * lane]) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        }
+        if (threadIdx.x == 0) sm.factor = scalbnf(a.scale * 1.4426950408889634f, -e);
+    }
+    __syncthreads();
+    const float factor = sm.factor;  // of an accumulator times its key scale: the score in units of log2 e
     uint32_t qf[NT][NK];
-    float mul[NT][2];
     int lim[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -202,12 +258,10 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
             qf[n][i] = *reinterpret_cast<const uint32_t*>(&h);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int r = 8 * n + 2 * t + i;
-            mul[n][i] = sm.mul[r];
-            lim[n][i] = r < rows ? pos0 + (r0 + r) / a.group : INT_MIN;  // the last position the row sees
-        }
+        for (int i = 0; i < 2; ++i) lim[n][i] = pos0 + (r0 + min(8 * n + 2 * t + i, rows - 1)) / a.group;  // the last position the row sees
     }
+
+    if (a.ranks > 1) cluster_arrive();  // (waited for ahead of the first write to another CTA's shared memory, over the queries)
 
     float o[NT][PD / 16][4], m[NT][2], l[NT][2];
 #pragma unroll
@@ -219,113 +273,102 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
         m[n][0] = m[n][1] = -1e30f;
         l[n][0] = l[n][1] = 0.f;
     }
-    float v_unit = 0.f;  // 2^6 / (a power of two not below the largest value scale so far)
+    float v_unit = INFINITY;  // 2^6 over a power of two not below the largest value scale so far; infinite while that is 0
 
-    const int k_at = BITS == 3 ? 12 * t : PD * BITS / 32 * t, v_at = BITS == 3 ? 12 * (g >> 1) : PD * BITS / 64 * g;
-    const bool k_there = k_at < a.l.row, v_there = v_at < a.l.row;
-    const uint32_t halves = (g & 1) ? 0x7632u : 0x5410u;
-
-    auto page_at = [&](int v) { return v < v_end ? a48p::page_of(a.l, a.b, seq, span.block(v) << 4) : -1; };
-    auto load = [&](int v, int page, Loaded<BITS, PD>& x) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-#pragma unroll
-            for (int j = 0; j < Share<BITS, PD>::K; ++j) x.k[i][j] = 0;
-            x.sk[i] = x.sv[i] = 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < Share<BITS, PD>::V; ++j) x.v[i][j] = 0;
-        if (page < 0) return;
-        const uint8_t* chunk = a.pool + a48p::chunk_at(a.l, page, kvh);
-        const int slot = (span.block(v) << 4) & (a.l.page - 1);
-        const uint8_t* kr = chunk + slot * a.l.row + k_at;
-        const uint8_t* vr = chunk + a.l.v_codes + slot * a.l.row + v_at;
-        if (k_there) {
-            load_words(kr + g * a.l.row, x.k[0]);
-            load_words(kr + (g + 8) * a.l.row, x.k[1]);
-        }
-        if (v_there) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) load_words(vr + (2 * t + (i & 1) + 8 * (i >> 1)) * a.l.row, x.v[i]);
-        }
-        const float* sk = reinterpret_cast<const float*>(chunk + a.l.k_scales) + slot;
-        const float* sv = reinterpret_cast<const float*>(chunk + a.l.v_scales) + slot;
-        x.sk[0] = __ldg(sk + g), x.sk[1] = __ldg(sk + g + 8);
-        x.sv[0] = __ldg(sv + g), x.sv[1] = __ldg(sv + g + 8);
-    };
     // 16 positions from `first` on, `page` >= 0
     auto take = [&](int first, int page, Loaded<BITS, PD>& x) {
-        float s[NT][4] = {};
-        uint32_t ka[NK], kb[NK];
-        convert_k<BITS, PD>(x.k[0], ka);
-        convert_k<BITS, PD>(x.k[1], kb);
-        if (BITS == 3 && first == 0) {  // the bos heads: 4-bit codes of their own, in convert_k's order
-            const uint8_t* bos = a.pool + a48p::chunk_at(a.l, page, kvh) + a.l.bos;
-            if (g == 0 && k_there) {
+        float s[NT][4], y[NT][4];
 #pragma unroll
-                for (int i = 0; i < NK; ++i) {
-                    const int e0 = k_entry<BITS, PD>(t, i, 0), e1 = k_entry<BITS, PD>(t, i, 1);
-                    const __half2 h = __floats2half2_rn((float)((bos[e0 / 2] >> (4 * (e0 & 1))) & 15) - 8.f,
-                                                        (float)((bos[e1 / 2] >> (4 * (e1 & 1))) & 15) - 8.f);
-                    ka[i] = *reinterpret_cast<const uint32_t*>(&h);
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[n][c] = 0.f;
+        {
+            uint32_t ka[NK], kb[NK];
+            convert_k<BITS, PD>(x.k[0], ka);
+            convert_k<BITS, PD>(x.k[1], kb);
+            if (BITS == 3 && first == 0) {  // the bos heads: 4-bit codes of their own, in convert_k's order
+                const uint8_t* bos = a.pool + a48p::chunk_at(a.l, page, kvh) + a.l.bos;
+                if (g == 0 && k_there) {
+#pragma unroll
+                    for (int i = 0; i < NK; ++i) {
+                        const int e0 = k_entry<BITS, PD>(t, i, 0), e1 = k_entry<BITS, PD>(t, i, 1);
+                        const __half2 h = __floats2half2_rn((float)((bos[e0 / 2] >> (4 * (e0 & 1))) & 15) - 8.f,
+                                                            (float)((bos[e1 / 2] >> (4 * (e1 & 1))) & 15) - 8.f);
+                        ka[i] = *reinterpret_cast<const uint32_t*>(&h);
+                    }
                 }
             }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float s2[4] = {};  // (two chains of MMAs instead of one of twice the length)
+#pragma unroll
+                for (int i = 0; i < NK / 2; ++i)
+                    mma_f16(i & 1 ? s2 : s[n], ka[2 * i], kb[2 * i], ka[2 * i + 1], kb[2 * i + 1], qf[n][2 * i], qf[n][2 * i + 1]);
+#pragma unroll
+                for (int c = 0; c < 4; ++c) s[n][c] += s2[c];
+            }
         }
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < NK / 2; ++i) mma_f16(s[n], ka[2 * i], kb[2 * i], ka[2 * i + 1], kb[2 * i + 1], qf[n][2 * i], qf[n][2 * i + 1]);
-        // scores in units of log2 e; what a row does not see is -inf
         const bool whole = first + 15 <= pos_lo && (a.window == 0 || first > pos_hi - a.window || first + 15 < a.sinks);
-        bool high = false;
+        auto seen = [&](int n, int c) {  // by row 2t + c % 2, position g + 8 (c / 2)
+            const int j = first + g + 8 * (c >> 1), last = lim[n][c & 1];
+            return j <= last && (a.window == 0 || j > last - a.window || j < a.sinks);
+        };
+        const float ks[2] = {x.sk[0] * factor, x.sk[1] * factor};
+        float f[2] = {x.sv[0], x.sv[1]};
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) s[n][c] *= x.sk[c >> 1] * mul[n][c & 1];
-        if (!whole || rows < ROWS) {
+            for (int c = 0; c < 4; ++c) y[n][c] = fmaf(s[n][c], ks[c >> 1], -m[n][c & 1]);
+        if (!whole) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int j = first + g + 8 * (c >> 1), last = lim[n][c & 1];
-                    // (last - window cannot wrap: INT_MIN rows fail the first test)
-                    const bool seen = j <= last && (a.window == 0 || j > last - a.window || j < a.sinks);
-                    s[n][c] = seen ? s[n][c] : -INFINITY;
-                }
-        }
-        // a value scale counts if it is finite and some row may see its position
-        float f[2];
+                for (int c = 0; c < 4; ++c) y[n][c] = seen(n, c) ? y[n][c] : -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int j = first + g + 8 * i;
-            const bool may = j <= pos_hi && (a.window == 0 || j > pos_lo - a.window || j < a.sinks);
-            f[i] = may ? x.sv[i] : 0.f;
-            high |= f[i] * v_unit > 64.f && f[i] <= 3.4e38f;
-            high |= v_unit == 0.f && f[i] > 0.f;
+            for (int i = 0; i < 2; ++i) {  // what no row sees does not count
+                const int j = first + g + 8 * i;
+                if (!(j <= pos_hi && (a.window == 0 || j > pos_lo - a.window || j < a.sinks))) f[i] = 0.f;
+            }
         }
+        float w[2] = {f[0] * v_unit, f[1] * v_unit};
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) high |= s[n][c] - m[n][c & 1] > 8.f;
-        if (__any_sync(0xffffffffu, high)) {  // rarely: move the references up
-            float top = fmaxf(f[0] <= 3.4e38f ? f[0] : 0.f, f[1] <= 3.4e38f ? f[1] : 0.f);
+            for (int c = 0; c < 4; ++c) y[n][c] = exp2_approx(y[n][c]);
+        float most = y[0][0];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) most = fmaxf(most, y[n][c]);
+        if (__any_sync(0xffffffffu, !(w[0] <= 64.f) || !(w[1] <= 64.f) || most > 512.f)) {  // rarely: move the references up
+            bool number[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                number[i] = f[i] <= 3.4e38f;
+                f[i] = number[i] ? f[i] : 0.f;
+            }
+            float top = fmaxf(f[0], f[1]), ratio = 1.f;
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-            float ratio = 1.f;
-            if (top > 0.f && (v_unit == 0.f || top * v_unit > 64.f)) {
+            if (top * v_unit > 64.f) {
                 // two octaves of room, so that scales of one size do not come back here; within fp32's exponents
-                const int e = min(max(5 - (ilogbf(top) + 2), -120), 120);
-                const float unit = scalbnf(1.f, e);
-                ratio = v_unit == 0.f ? 0.f : unit / v_unit;
+                const float unit = scalbnf(1.f, min(max(5 - (ilogbf(top) + 2), -120), 120));
+                ratio = v_unit == INFINITY ? 0.f : unit / v_unit;
                 v_unit = unit;
             }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) w[i] = f[i] > 0.f ? f[i] * v_unit : 0.f;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    float mx = fmaxf(s[n][i], s[n][i + 2]);
+                    float z[2], mx = -INFINITY;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        z[k] = whole || seen(n, i + 2 * k) ? s[n][i + 2 * k] * ks[k] : -INFINITY;
+                        if (!number[k] && z[k] != -INFINITY) z[k] = NAN;  // a value that is none, for the rows that see it
+                        mx = fmaxf(mx, z[k]);
+                    }
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
                     const float m_new = fmaxf(m[n][i], mx), corr = exp2_approx(m[n][i] - m_new);
@@ -333,22 +376,20 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
                     l[n][i] *= corr;
 #pragma unroll
                     for (int k = 0; k < PD / 16; ++k) o[n][k][i] *= corr * ratio, o[n][k][i + 2] *= corr * ratio;
+                    y[n][i] = exp2_approx(z[0] - m_new);
+                    y[n][i + 2] = exp2_approx(z[1] - m_new);
                 }
         }
         uint32_t pb[NT][2];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {  // positions g, g + 8
-                const float p0 = exp2_approx(s[n][2 * i] - m[n][0]), p1 = exp2_approx(s[n][2 * i + 1] - m[n][1]);
-                l[n][0] += p0;
-                l[n][1] += p1;
-                // (a weight of zero stays zero whatever the scale: the position may not be seen by this row)
-                const float w0 = p0 > 0.f ? p0 * (f[i] * v_unit) : 0.f, w1 = p1 > 0.f ? p1 * (f[i] * v_unit) : 0.f;
-                const __half2 h = __floats2half2_rn(w0, w1);
+                l[n][0] += y[n][2 * i];
+                l[n][1] += y[n][2 * i + 1];
+                const __half2 h = __floats2half2_rn(y[n][2 * i] * w[i], y[n][2 * i + 1] * w[i]);
                 pb[n][i] = transpose8(*reinterpret_cast<const uint32_t*>(&h));
             }
-        }
         uint32_t va[NK], vb[NK];  // positions (2t, 2t+1) and (2t+8, 2t+9)
         convert_v<BITS, PD>(x.v[0], x.v[1], halves, va);
         convert_v<BITS, PD>(x.v[2], x.v[3], halves, vb);
@@ -369,24 +410,22 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
             for (int k = 0; k < PD / 16; ++k) mma_f16(o[n][k], va[2 * k], va[2 * k + 1], vb[2 * k], vb[2 * k + 1], pb[n][0], pb[n][1]);
     };
 
-    {
-        int v = v_begin + warp;
-        int page = page_at(v), page_next = page_at(v + ROW_WARPS);
-        Loaded<BITS, PD> x;
-        load(v, page, x);
-        while (v < v_end) {
-            Loaded<BITS, PD> y;
-            load(v + ROW_WARPS, page_next, y);
-            const int page_after = page_at(v + 2 * ROW_WARPS);
-            if (page >= 0) take(span.block(v) << 4, page, x);
-            x = y;
+#pragma unroll 1
+    while (v < v_end) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {  // (two steps, so that nothing moves between registers)
+            if (v < v_end) {
+                if (v + ROW_WARPS < v_end) load(v + ROW_WARPS, page[k ^ 1], x[k ^ 1]);
+                const int after = page_at(v + 2 * ROW_WARPS);
+                if (page[k] >= 0) take(span.block(v) << 4, page[k], x[k]);
+                page[k] = after;
+            }
             v += ROW_WARPS;
-            page = page_next, page_next = page_after;
         }
     }
 
     // ---- the warps' sums meet in shared memory
-    const float unit = v_unit == 0.f ? 0.f : 1.f / v_unit;
+    const float unit = v_unit == INFINITY ? 0.f : 1.f / v_unit;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -402,18 +441,19 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
     }
     __syncthreads();
     auto finish = [&](int r, int c, float top, float sum, const float (&acc)[4]) {
-        const size_t id = row_id(r);
+        const int token = sm.token[r], head = sm.head[r];
         if (a.clusters > 1) {
-            const size_t at = (size_t)cluster * a.b.n_tokens * a.heads + id;
+            const size_t at = ((size_t)cluster * a.b.n_tokens + token) * a.heads + head;
             reinterpret_cast<float4*>(a.part_o + at * 128)[c / 4] = make_float4(acc[0], acc[1], acc[2], acc[3]);
             if (c == 0) a.part_ml[at] = make_float2(top, sum);
         } else {
             const float inv = sum != 0.f ? 1.f / sum : 0.f;
             const __nv_bfloat162 lo = __floats2bfloat162_rn(acc[0] * inv, acc[1] * inv), hi = __floats2bfloat162_rn(acc[2] * inv, acc[3] * inv);
-            *reinterpret_cast<uint2*>(a.out + id / a.heads * a.out_stride + id % a.heads * a.l.hd + c) =
+            *reinterpret_cast<uint2*>(a.out + token * a.out_stride + (size_t)head * a.l.hd + c) =
                 make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
         }
     };
+    if (a.ranks > 1) cluster_wait();  // every CTA of the cluster runs: its shared memory may be written
     for (int i = threadIdx.x; i < rows * (PD / 4); i += 32 * ROW_WARPS) {
         const int r = i / (PD / 4), c = 4 * (i % (PD / 4));
         if (c >= a.l.hd) continue;
@@ -423,51 +463,42 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
 #pragma unroll
         for (int w = 0; w < ROW_WARPS; ++w) {
             const float corr = exp2_approx(sm.m[w][r] - top);
-            const float4 x = *reinterpret_cast<const float4*>(&sm.o[w][r][c]);
+            const float4 z = *reinterpret_cast<const float4*>(&sm.o[w][r][c]);
             sum += corr * sm.l[w][r];
-            acc[0] += corr * x.x, acc[1] += corr * x.y, acc[2] += corr * x.z, acc[3] += corr * x.w;
+            acc[0] += corr * z.x, acc[1] += corr * z.y, acc[2] += corr * z.z, acc[3] += corr * z.w;
         }
         if (a.ranks == 1) {
             finish(r, c, top, sum, acc);
-        } else {
-            *reinterpret_cast<float4*>(&sm.o[0][r][c]) = make_float4(acc[0], acc[1], acc[2], acc[3]);  // (read by this thread alone)
-            if (c == 0) sm.cta_m[r] = top, sm.cta_l[r] = sum;
+        } else {  // to the CTA that finishes this piece
+            const int to = i % a.ranks, at = i / a.ranks * a.ranks + rank;
+            st_rank(of_rank(&sm.piece[at], to), make_float4(acc[0], acc[1], acc[2], acc[3]));
+            st_rank(of_rank(&sm.piece_ml[at], to), make_float2(top, sum));
         }
     }
     if (a.ranks == 1) return;
-    // ---- and the CTAs' sums through distributed shared memory: every rank finishes a share of the columns
-    cluster_sync_all();
-    for (int i = threadIdx.x + 32 * ROW_WARPS * rank; i < rows * (PD / 4); i += 32 * ROW_WARPS * a.ranks) {
-        const int r = i / (PD / 4), c = 4 * (i % (PD / 4));
+    // ---- and the CTAs' sums: each has sent every other its part of a share of the pieces (piece i goes to rank i % ranks)
+    cluster_arrive();
+    cluster_wait();
+    for (int i = threadIdx.x * a.ranks + rank; i < rows * (PD / 4); i += 32 * ROW_WARPS * a.ranks) {
+        const int r = i / (PD / 4), c = 4 * (i % (PD / 4)), at = i - rank;
         if (c >= a.l.hd) continue;
-        float ms[MAX_RANKS], ls[MAX_RANKS], top = -1e30f, sum = 0.f, acc[4] = {};
-        float4 x[MAX_RANKS];
-#pragma unroll
-        for (int k = 0; k < MAX_RANKS; ++k) {
-            if (k >= a.ranks) break;
-            ms[k] = ld_rank(of_rank(&sm.cta_m[r], k));
-            ls[k] = ld_rank(of_rank(&sm.cta_l[r], k));
-            x[k] = ld_rank4(of_rank(&sm.o[0][r][c], k));
-        }
-#pragma unroll
-        for (int k = 0; k < MAX_RANKS; ++k)
-            if (k < a.ranks) top = fmaxf(top, ms[k]);
-#pragma unroll
-        for (int k = 0; k < MAX_RANKS; ++k) {
-            if (k >= a.ranks) break;
-            const float corr = exp2_approx(ms[k] - top);
-            sum += corr * ls[k];
-            acc[0] += corr * x[k].x, acc[1] += corr * x[k].y, acc[2] += corr * x[k].z, acc[3] += corr * x[k].w;
+        float top = -1e30f, sum = 0.f, acc[4] = {};
+        for (int k = 0; k < a.ranks; ++k) top = fmaxf(top, sm.piece_ml[at + k].x);
+        for (int k = 0; k < a.ranks; ++k) {
+            const float2 ml = sm.piece_ml[at + k];
+            const float4 z = sm.piece[at + k];
+            const float corr = exp2_approx(ml.x - top);
+            sum += corr * ml.y;
+            acc[0] += corr * z.x, acc[1] += corr * z.y, acc[2] += corr * z.z, acc[3] += corr * z.w;
         }
         finish(r, c, top, sum, acc);
     }
-    cluster_sync_all();  // no CTA's shared memory goes before all have read it
 }
 
 // Registers are held to what lets four CTAs of eight rows (two of sixteen) share an SM: loads in flight are what hides
 // memory.
 template <int BITS, int PD, int NT>
-__global__ void __launch_bounds__(32 * ROW_WARPS, NT == 1 ? 4 : 2) attn_paged_rows_kernel(const __grid_constant__ AttnArgs a) {
+__global__ void __launch_bounds__(32 * ROW_WARPS, NT == 2 ? 2 : BITS == 4 || PD == 64 ? 4 : 3) attn_paged_rows_kernel(const __grid_constant__ AttnArgs a) {
     __shared__ RowsShared<BITS, PD, NT> sm;
     if (!a.beside) {
         a48_pdl_prologue();
