@@ -26,12 +26,13 @@ using a48p::Span;
 using a48p::span_of;
 
 // ---------------------------------------------------------------------------------------------------- few rows
-// A CTA of four warps takes a tile of 8 NT rows of one head and one part of the positions; a warp takes 16 positions at a
-// time, straight from memory into the registers that hold the operands of its MMAs, the next 16 under way meanwhile.
+// A CTA of four warps takes a tile of 8 NT rows of one head and one part of the positions; a warp takes blocks of 16
+// positions, two at a time, out of a ring of four in shared memory that asynchronous copies fill (a block's codes are one run
+// of a page, so are its scales): what hides memory is bytes in flight, and registers hold too few.
 //
 // The positions are the M side of both contractions (m16n8k16, fp16, fp32 accumulators), the rows the N side: S^T = C Q^T
 // and O^T = D^T P^T.  Eight rows are then no padding, and the codes, whose conversion is what a position costs, are
-// converted once for all rows.  Entries are dealt to lanes so that every lane converts what it loaded: lane 4g+t holds
+// converted once for all rows.  Entries are dealt to lanes so that every lane converts what it read: lane 4g+t holds
 // for S^T the t-th quarter of the key rows of positions g and g + 8 (the order of the entries inside the contraction is
 // free: the query fragments are taken in the same order), for O^T the g-th eighth of the value rows of positions 2t, 2t+1,
 // 2t+8, 2t+9, whose words are first merged into halves of the same entry of two positions.  S^T's accumulators become
@@ -59,21 +60,34 @@ struct Share {
     static constexpr int K = BITS == 3 ? 3 : PD * BITS / 128, V = BITS == 3 ? 3 : PD * BITS / 256;
 };
 template <int N>
-__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[N]) {
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t (&w)[N]) {  // of shared memory
     if constexpr (N % 4 == 0) {
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) {
-            const uint4 v = __ldg(reinterpret_cast<const uint4*>(p) + i);
+            const uint4 v = reinterpret_cast<const uint4*>(p)[i];
             w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
         }
     } else if constexpr (N == 2) {
-        const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
         w[0] = v.x, w[1] = v.y;
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = __ldg(reinterpret_cast<const unsigned*>(p) + i);
+        for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const unsigned*>(p)[i];
     }
 }
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// A block of 16 positions in the ring: key rows, value rows, key scales, value scales.  Value rows are read two apart by
+// the lanes of a request (positions 2t): 4- and 8-bit rows lie 16 bytes past a multiple of 64 apart, so that those fall into
+// different banks (3-bit rows do so as they are).
+template <int BITS, int PD>
+struct Block {
+    static constexpr int PITCH = BITS == 3 ? 48 : BITS * PD / 8 <= 64 ? 80 : 144;
+    static constexpr int K = 0, V = 16 * PD * BITS / 8, SK = V + 16 * PITCH, SV = SK + 64, BYTES = SV + 64;
+};
+constexpr int STAGES = 4;
 
 // Entry of a key row that is half h of converted word i of quarter t (the order convert_k gives).
 template <int BITS, int PD>
@@ -114,17 +128,14 @@ __device__ __forceinline__ void convert_v(const uint32_t (&a)[Share<BITS, PD>::V
     }
 }
 
-template <int BITS, int PD>
-struct Loaded {  // a lane's part of 16 positions
-    uint32_t k[2][Share<BITS, PD>::K], v[4][Share<BITS, PD>::V];
-    float sk[2], sv[2];
-};
-
 template <int BITS, int PD, int NT>
 struct RowsShared {
     static constexpr int ROWS = 8 * NT;
+    union {
+        alignas(16) uint8_t ring[ROW_WARPS][STAGES][Block<BITS, PD>::BYTES];
+        alignas(16) float o[ROW_WARPS][ROWS][PD + 4];  // the warps' sums
+    };
     float top[ROW_WARPS], factor;
-    alignas(16) float o[ROW_WARPS][ROWS][PD + 4];  // the warps' sums
     float m[ROW_WARPS][ROWS], l[ROW_WARPS][ROWS];
     int token[ROWS], head[ROWS];
     // what the cluster's CTAs send: pieces of four head dims, with the exponent of their reference and their sum of p
@@ -174,11 +185,15 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
     const int per = max(2 * ROW_WARPS, (span.count + parts - 1) / parts);
     const int v_begin = blockIdx.y * per, v_end = min(span.count, v_begin + per);
 
-    // ---- the first blocks' pages under way, and which token and head a row is
-    const size_t page_bytes = (size_t)a.l.kv_heads * a.l.chunk;
-    auto page_at = [&](int v) { return v < v_end ? a48p::page_of(a.l, a.b, seq, span.block(v) << 4) : -1; };
-    int v = v_begin + warp;
-    int page[2] = {page_at(v), page_at(v + ROW_WARPS)};
+    // ---- the warp's blocks v_begin + warp + 4k: pages of the first ones under way
+    const int blocks = max(0, (v_end - v_begin - warp + ROW_WARPS - 1) / ROW_WARPS);
+    auto block_at = [&](int k) { return span.block(v_begin + warp + ROW_WARPS * k); };
+    auto page_at = [&](int k) { return k < blocks ? a48p::page_of(a.l, a.b, seq, block_at(k) << 4) : -1; };
+    int page[STAGES], next_page[2];  // of the blocks in the ring, of the next two
+#pragma unroll
+    for (int k = 0; k < STAGES; ++k) page[k] = page_at(k);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) next_page[k] = page_at(STAGES + k);
     if (threadIdx.x < ROWS) {
         const int in_seq = r0 + min((int)threadIdx.x, rows - 1), i = in_seq / a.group;
         sm.token[threadIdx.x] = start + i;
@@ -186,33 +201,46 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
     }
     __syncthreads();
 
-    // What a lane reads of 16 positions, as offsets from the block's first key row and first key scale.  (A lane whose
-    // entries lie past the padded head reads some that exist: they meet zeros of the query, or columns that are not stored.)
-    const int row = a.l.row;
+    // What a lane copies of a block: 16-byte pieces lane + 32i of the key rows and of the value rows, and (lanes 0..7) one of
+    // the scales.
+    using B = Block<BITS, PD>;
+    constexpr int PIECES = (PD * BITS / 8 + 31) / 32;
+    const int row = a.l.row, pitch = BITS == 3 ? row : B::PITCH;
+    uint8_t* ring = &sm.ring[warp][0][0];
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    uint32_t v_dst[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        const int at = 16 * (lane + 32 * i);
+        v_dst[i] = B::V + (BITS == 3 ? at : at / row * pitch + at % row);
+    }
+    const uint8_t* head_chunks = a.pool + (size_t)kvh * a.l.chunk;
+    const size_t page_bytes = (size_t)a.l.kv_heads * a.l.chunk;
+    auto load = [&](int k, int stage, int from) {
+        const int p = __shfl_sync(0xffffffffu, from, 0);  // the same for the warp: the addresses are formed once for it
+        if (p >= 0) {
+            const int slot = (block_at(k) << 4) & (a.l.page - 1);
+            const uint8_t* chunk = head_chunks + p * page_bytes;
+            const uint8_t* codes = chunk + slot * row + 16 * lane;
+            const uint32_t dst = ring_at + stage * B::BYTES;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+                if (lane + 32 * i < row) {
+                    copy16(dst + B::K + 16 * (lane + 32 * i), codes + 512 * i);
+                    copy16(dst + v_dst[i], codes + a.l.v_codes + 512 * i);
+                }
+            if (lane < 8) copy16(dst + B::SK + 16 * lane, chunk + (lane < 4 ? a.l.k_scales : a.l.v_scales) + 4 * slot + 16 * (lane & 3));
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int k = 0; k < STAGES; ++k) load(k, k, page[k]);
+    // What it reads.  (A lane whose entries lie past the padded head reads some that exist: they meet zeros of the query, or
+    // columns that are not stored.)
     const uint32_t k_first = BITS == 3 ? 12 * t : PD * BITS / 32 * t, v_first = BITS == 3 ? 12 * (g >> 1) : PD * BITS / 64 * g;
     const bool k_there = k_first < row, v_there = v_first < row;
-    const uint32_t k_off = (k_there ? k_first : 0) + g * row, v_off = a.l.v_codes + (v_there ? v_first : 0) + 2 * t * row, row8 = 8 * row;
-    const uint32_t sv_off = a.l.v_scales - a.l.k_scales + 4 * g;
+    const uint32_t k_off = B::K + (k_there ? k_first : 0) + g * row, v_off = B::V + (v_there ? v_first : 0) + 2 * t * pitch;
     const uint32_t halves = (g & 1) ? 0x7632u : 0x5410u;
-    const uint8_t* head_chunks = a.pool + (size_t)kvh * a.l.chunk;
-
-    auto load = [&](int v, int page, Loaded<BITS, PD>& x) {
-        page = __shfl_sync(0xffffffffu, page, 0);  // the same for the warp: the addresses are formed once for it
-        const int slot = (span.block(v) << 4) & (a.l.page - 1);
-        const uint8_t* chunk = head_chunks + max(page, 0) * page_bytes;
-        const uint8_t* codes = chunk + slot * row;
-        const uint8_t* scales = chunk + a.l.k_scales + 4 * slot;
-        load_words(codes + k_off, x.k[0]);
-        load_words(codes + (k_off + row8), x.k[1]);
-        load_words(codes + v_off, x.v[0]);
-        load_words(codes + (v_off + row), x.v[1]);
-        load_words(codes + (v_off + row8), x.v[2]);
-        load_words(codes + (v_off + row8 + row), x.v[3]);
-        x.sk[0] = __ldg(reinterpret_cast<const float*>(scales + 4 * g)), x.sk[1] = __ldg(reinterpret_cast<const float*>(scales + (4 * g + 32)));
-        x.sv[0] = __ldg(reinterpret_cast<const float*>(scales + sv_off)), x.sv[1] = __ldg(reinterpret_cast<const float*>(scales + (sv_off + 32)));
-    };
-    Loaded<BITS, PD> x[2];
-    if (v < v_end) load(v, page[0], x[0]);
 
     // ---- the query rows to fp16 by one power of two (the largest entry of the tile to [2^14, 2^15): a row 2^20 below it
     // still has all its bits, one 2^29 below it the upper ten)
@@ -275,19 +303,27 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
     }
     float v_unit = INFINITY;  // 2^6 over a power of two not below the largest value scale so far; infinite while that is 0
 
-    // 16 positions from `first` on, `page` >= 0
-    auto take = [&](int first, int page, Loaded<BITS, PD>& x) {
-        float s[NT][4], y[NT][4];
+    // Two blocks, in stages `stage` and `stage` + 1 of the ring; first[b]: their first positions, NOWHERE for one that is not
+    // there (past the warp's last, or without a page).
+    constexpr int NOWHERE = 0x7fffff00;
+    auto take = [&](int stage, const int (&first)[2], const int (&from)[2]) {
+        float s[2][NT][4], y[2][NT][4], ks[2][2], f[2][2], w[2][2];
+        bool whole[2];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int b = 0; b < 2; ++b) {
+            const uint8_t* block = ring + (stage + b) * B::BYTES;
+            uint32_t k0[Share<BITS, PD>::K], k1[Share<BITS, PD>::K], ka[NK], kb[NK];
+            load_words(block + k_off, k0);
+            load_words(block + k_off + 8 * row, k1);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) s[n][c] = 0.f;
-        {
-            uint32_t ka[NK], kb[NK];
-            convert_k<BITS, PD>(x.k[0], ka);
-            convert_k<BITS, PD>(x.k[1], kb);
-            if (BITS == 3 && first == 0) {  // the bos heads: 4-bit codes of their own, in convert_k's order
-                const uint8_t* bos = a.pool + a48p::chunk_at(a.l, page, kvh) + a.l.bos;
+            for (int i = 0; i < 2; ++i) {
+                ks[b][i] = reinterpret_cast<const float*>(block + B::SK)[g + 8 * i] * factor;
+                f[b][i] = reinterpret_cast<const float*>(block + B::SV)[g + 8 * i];
+            }
+            convert_k<BITS, PD>(k0, ka);
+            convert_k<BITS, PD>(k1, kb);
+            if (BITS == 3 && first[b] == 0) {  // the bos heads: 4-bit codes of their own, in convert_k's order
+                const uint8_t* bos = a.pool + a48p::chunk_at(a.l, from[b], kvh) + a.l.bos;
                 if (g == 0 && k_there) {
 #pragma unroll
                     for (int i = 0; i < NK; ++i) {
@@ -302,52 +338,67 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
             for (int n = 0; n < NT; ++n) {
                 float s2[4] = {};  // (two chains of MMAs instead of one of twice the length)
 #pragma unroll
+                for (int c = 0; c < 4; ++c) s[b][n][c] = 0.f;
+#pragma unroll
                 for (int i = 0; i < NK / 2; ++i)
-                    mma_f16(i & 1 ? s2 : s[n], ka[2 * i], kb[2 * i], ka[2 * i + 1], kb[2 * i + 1], qf[n][2 * i], qf[n][2 * i + 1]);
+                    mma_f16(i & 1 ? s2 : s[b][n], ka[2 * i], kb[2 * i], ka[2 * i + 1], kb[2 * i + 1], qf[n][2 * i], qf[n][2 * i + 1]);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) s[n][c] += s2[c];
+                for (int c = 0; c < 4; ++c) s[b][n][c] += s2[c];
             }
+            whole[b] = first[b] != NOWHERE && first[b] + 15 <= pos_lo && (a.window == 0 || first[b] > pos_hi - a.window || first[b] + 15 < a.sinks);
         }
-        const bool whole = first + 15 <= pos_lo && (a.window == 0 || first > pos_hi - a.window || first + 15 < a.sinks);
-        auto seen = [&](int n, int c) {  // by row 2t + c % 2, position g + 8 (c / 2)
-            const int j = first + g + 8 * (c >> 1), last = lim[n][c & 1];
-            return j <= last && (a.window == 0 || j > last - a.window || j < a.sinks);
+        auto seen = [&](int b, int n, int c) {  // by row 2t + c % 2, position g + 8 (c / 2)
+            const int j = first[b] + g + 8 * (c >> 1), last = lim[n][c & 1];
+            return first[b] != NOWHERE && j <= last && (a.window == 0 || j > last - a.window || j < a.sinks);
         };
-        const float ks[2] = {x.sk[0] * factor, x.sk[1] * factor};
-        float f[2] = {x.sv[0], x.sv[1]};
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) y[n][c] = fmaf(s[n][c], ks[c >> 1], -m[n][c & 1]);
-        if (!whole) {
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) y[n][c] = seen(n, c) ? y[n][c] : -INFINITY;
+                for (int c = 0; c < 4; ++c) y[b][n][c] = fmaf(s[b][n][c], ks[b][c >> 1], -m[n][c & 1]);
+        if (!(whole[0] && whole[1])) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {  // what no row sees does not count
-                const int j = first + g + 8 * i;
-                if (!(j <= pos_hi && (a.window == 0 || j > pos_lo - a.window || j < a.sinks))) f[i] = 0.f;
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) y[b][n][c] = seen(b, n, c) ? y[b][n][c] : -INFINITY;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {  // what no row sees does not count
+                    const int j = first[b] + g + 8 * i;
+                    if (first[b] == NOWHERE || !(j <= pos_hi && (a.window == 0 || j > pos_lo - a.window || j < a.sinks))) f[b][i] = 0.f;
+                }
             }
         }
-        float w[2] = {f[0] * v_unit, f[1] * v_unit};
+        float most = -INFINITY;
+        bool high = false;
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) y[n][c] = exp2_approx(y[n][c]);
-        float most = y[0][0];
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) most = fmaxf(most, y[n][c]);
-        if (__any_sync(0xffffffffu, !(w[0] <= 64.f) || !(w[1] <= 64.f) || most > 512.f)) {  // rarely: move the references up
-            bool number[2];
+        for (int b = 0; b < 2; ++b) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                number[i] = f[i] <= 3.4e38f;
-                f[i] = number[i] ? f[i] : 0.f;
+                w[b][i] = f[b][i] * v_unit;
+                high |= !(w[b][i] <= 64.f);
             }
-            float top = fmaxf(f[0], f[1]), ratio = 1.f;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    y[b][n][c] = exp2_approx(y[b][n][c]);
+                    most = fmaxf(most, y[b][n][c]);
+                }
+        }
+        if (__any_sync(0xffffffffu, high || most > 512.f)) {  // rarely: move the references up
+            bool number[2][2];
+            float top = 0.f, ratio = 1.f;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    number[b][i] = f[b][i] <= 3.4e38f;
+                    f[b][i] = number[b][i] ? f[b][i] : 0.f;
+                    top = fmaxf(top, f[b][i]);
+                }
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
             if (top * v_unit > 64.f) {
@@ -357,18 +408,22 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
                 v_unit = unit;
             }
 #pragma unroll
-            for (int i = 0; i < 2; ++i) w[i] = f[i] > 0.f ? f[i] * v_unit : 0.f;
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) w[b][i] = f[b][i] > 0.f ? f[b][i] * v_unit : 0.f;
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    float z[2], mx = -INFINITY;
+                    float z[2][2], mx = -INFINITY;
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        z[k] = whole || seen(n, i + 2 * k) ? s[n][i + 2 * k] * ks[k] : -INFINITY;
-                        if (!number[k] && z[k] != -INFINITY) z[k] = NAN;  // a value that is none, for the rows that see it
-                        mx = fmaxf(mx, z[k]);
-                    }
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            z[b][k] = whole[b] || seen(b, n, i + 2 * k) ? s[b][n][i + 2 * k] * ks[b][k] : -INFINITY;
+                            if (!number[b][k] && z[b][k] != -INFINITY) z[b][k] = NAN;  // a value that is none, for the rows that see it
+                            mx = fmaxf(mx, z[b][k]);
+                        }
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
                     const float m_new = fmaxf(m[n][i], mx), corr = exp2_approx(m[n][i] - m_new);
@@ -376,53 +431,65 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
                     l[n][i] *= corr;
 #pragma unroll
                     for (int k = 0; k < PD / 16; ++k) o[n][k][i] *= corr * ratio, o[n][k][i + 2] *= corr * ratio;
-                    y[n][i] = exp2_approx(z[0] - m_new);
-                    y[n][i + 2] = exp2_approx(z[1] - m_new);
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) y[b][n][i + 2 * k] = exp2_approx(z[b][k] - m_new);
                 }
         }
-        uint32_t pb[NT][2];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int b = 0; b < 2; ++b) {
+            const uint8_t* block = ring + (stage + b) * B::BYTES;
+            uint32_t pb[NT][2];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {  // positions g, g + 8
-                l[n][0] += y[n][2 * i];
-                l[n][1] += y[n][2 * i + 1];
-                const __half2 h = __floats2half2_rn(y[n][2 * i] * w[i], y[n][2 * i + 1] * w[i]);
-                pb[n][i] = transpose8(*reinterpret_cast<const uint32_t*>(&h));
-            }
-        uint32_t va[NK], vb[NK];  // positions (2t, 2t+1) and (2t+8, 2t+9)
-        convert_v<BITS, PD>(x.v[0], x.v[1], halves, va);
-        convert_v<BITS, PD>(x.v[2], x.v[3], halves, vb);
-        if (BITS == 3 && first == 0) {
-            const uint8_t* bos = a.pool + a48p::chunk_at(a.l, page, kvh) + a.l.bos + a.l.padded / 2;
-            if (t == 0 && v_there) {
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int i = 0; i < NK; ++i) {
-                    const int e = NK * g + i;
-                    const __half h = __float2half((float)((bos[e / 2] >> (4 * (e & 1))) & 15) - 8.f);
-                    va[i] = (va[i] & 0xffff0000u) | __half_as_ushort(h);
+                for (int i = 0; i < 2; ++i) {  // positions g, g + 8
+                    l[n][0] += y[b][n][2 * i];
+                    l[n][1] += y[b][n][2 * i + 1];
+                    const __half2 h = __floats2half2_rn(y[b][n][2 * i] * w[b][i], y[b][n][2 * i + 1] * w[b][i]);
+                    pb[n][i] = transpose8(*reinterpret_cast<const uint32_t*>(&h));
+                }
+            uint32_t v0[4][Share<BITS, PD>::V], va[NK], vb[NK];  // positions (2t, 2t+1) and (2t+8, 2t+9)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) load_words(block + v_off + ((i & 1) + 8 * (i >> 1)) * pitch, v0[i]);
+            convert_v<BITS, PD>(v0[0], v0[1], halves, va);
+            convert_v<BITS, PD>(v0[2], v0[3], halves, vb);
+            if (BITS == 3 && first[b] == 0) {
+                const uint8_t* bos = a.pool + a48p::chunk_at(a.l, from[b], kvh) + a.l.bos + a.l.padded / 2;
+                if (t == 0 && v_there) {
+#pragma unroll
+                    for (int i = 0; i < NK; ++i) {
+                        const int e = NK * g + i;
+                        const __half h = __float2half((float)((bos[e / 2] >> (4 * (e & 1))) & 15) - 8.f);
+                        va[i] = (va[i] & 0xffff0000u) | __half_as_ushort(h);
+                    }
                 }
             }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int k = 0; k < PD / 16; ++k) mma_f16(o[n][k], va[2 * k], va[2 * k + 1], vb[2 * k], vb[2 * k + 1], pb[n][0], pb[n][1]);
         }
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int k = 0; k < PD / 16; ++k) mma_f16(o[n][k], va[2 * k], va[2 * k + 1], vb[2 * k], vb[2 * k + 1], pb[n][0], pb[n][1]);
     };
-
 #pragma unroll 1
-    while (v < v_end) {
+    for (int k = 0; k < blocks; k += 2) {
+        const int stage = k & 2;
+        asm volatile("cp.async.wait_group 2;" ::: "memory");  // all but the next two blocks
+        __syncwarp();
+        const int from[2] = {stage ? page[2] : page[0], stage ? page[3] : page[1]};
+        const int first[2] = {from[0] >= 0 ? block_at(k) << 4 : NOWHERE, from[1] >= 0 ? block_at(k + 1) << 4 : NOWHERE};
+        take(stage, first, from);
+        __syncwarp();  // every lane has read the two stages
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {  // (two steps, so that nothing moves between registers)
-            if (v < v_end) {
-                if (v + ROW_WARPS < v_end) load(v + ROW_WARPS, page[k ^ 1], x[k ^ 1]);
-                const int after = page_at(v + 2 * ROW_WARPS);
-                if (page[k] >= 0) take(span.block(v) << 4, page[k], x[k]);
-                page[k] = after;
-            }
-            v += ROW_WARPS;
+        for (int b = 0; b < 2; ++b) {
+            load(k + STAGES + b, stage + b, next_page[b]);
+            (stage ? page[2 + b] : page[b]) = next_page[b];
+            next_page[b] = page_at(k + STAGES + 2 + b);
         }
     }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();  // the ring's memory is the sums' now
 
     // ---- the warps' sums meet in shared memory
     const float unit = v_unit == INFINITY ? 0.f : 1.f / v_unit;
@@ -499,7 +566,8 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
 // memory.
 template <int BITS, int PD, int NT>
 __global__ void __launch_bounds__(32 * ROW_WARPS, NT == 2 ? 2 : BITS == 4 || PD == 64 ? 4 : 3) attn_paged_rows_kernel(const __grid_constant__ AttnArgs a) {
-    __shared__ RowsShared<BITS, PD, NT> sm;
+    extern __shared__ __align__(16) uint8_t smem[];
+    RowsShared<BITS, PD, NT>& sm = *reinterpret_cast<RowsShared<BITS, PD, NT>*>(smem);
     if (!a.beside) {
         a48_pdl_prologue();
         attend_rows<BITS, PD, NT>(a, sm);
@@ -598,11 +666,15 @@ Plan plan_of(const bitnet_a48_paged_cache& c, const bitnet_a48_paged_batch& b, i
     return p;
 }
 
-template <int BITS, int PD>
-cudaError_t launch_rows(const AttnArgs& a, int nt, cudaStream_t st) {
+template <int BITS, int PD, int NT>
+cudaError_t launch_rows(const AttnArgs& a, cudaStream_t st) {
+    constexpr size_t SMEM = sizeof(RowsShared<BITS, PD, NT>);
+    const cudaError_t e = cudaFuncSetAttribute(attn_paged_rows_kernel<BITS, PD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM);
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(a.l.kv_heads * a.b.n_seqs * a.tiles, a.ranks * a.clusters);
     cfg.blockDim = dim3(32 * ROW_WARPS);
+    cfg.dynamicSmemBytes = SMEM;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -611,8 +683,11 @@ cudaError_t launch_rows(const AttnArgs& a, int nt, cudaStream_t st) {
     attr[1].val.clusterDim = {1, (unsigned)a.ranks, 1};
     cfg.attrs = attr;
     cfg.numAttrs = a.ranks > 1 ? 2 : 1;
-    return nt == 1 ? cudaLaunchKernelEx(&cfg, attn_paged_rows_kernel<BITS, PD, 1>, a)
-                   : cudaLaunchKernelEx(&cfg, attn_paged_rows_kernel<BITS, PD, 2>, a);
+    return cudaLaunchKernelEx(&cfg, attn_paged_rows_kernel<BITS, PD, NT>, a);
+}
+template <int BITS, int PD>
+cudaError_t launch_rows(const AttnArgs& a, int nt, cudaStream_t st) {
+    return nt == 1 ? launch_rows<BITS, PD, 1>(a, st) : launch_rows<BITS, PD, 2>(a, st);
 }
 
 // (the caches and batches that reach this have been checked)
