@@ -19,6 +19,7 @@
 namespace {
 
 using a48p::exp2_approx;
+using a48p::in_register;
 using a48p::Layout;
 
 using a48p::AttnArgs;
@@ -26,9 +27,9 @@ using a48p::Span;
 using a48p::span_of;
 
 // ---------------------------------------------------------------------------------------------------- few rows
-// A CTA of four warps takes a tile of 8 NT rows of one head and one part of the positions; a warp takes blocks of 16
-// positions, two at a time, out of a ring of four in shared memory that asynchronous copies fill (a block's codes are one run
-// of a page, so are its scales): what hides memory is bytes in flight, and registers hold too few.
+// A CTA of four warps takes a tile of 8 NT rows of one head and one part of the positions; a warp takes pairs of blocks of 16
+// positions out of two stages in shared memory that asynchronous copies fill (a block's codes are one run of a page, so
+// are its scales): what hides memory is bytes in flight, and registers hold too few.
 //
 // The positions are the M side of both contractions (m16n8k16, fp16, fp32 accumulators), the rows the N side: S^T = C Q^T
 // and O^T = D^T P^T.  Eight rows are then no padding, and the codes, whose conversion is what a position costs, are
@@ -47,6 +48,13 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// the first of a chain: onto zero
+__device__ __forceinline__ void mma_f16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     uint32_t r;
@@ -79,7 +87,7 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// A block of 16 positions in the ring: key rows, value rows, key scales, value scales.  Value rows are read two apart by
+// A block of 16 positions in a stage: key rows, value rows, key scales, value scales.  Value rows are read two apart by
 // the lanes of a request (positions 2t): 4- and 8-bit rows lie 16 bytes past a multiple of 64 apart, so that those fall into
 // different banks (3-bit rows do so as they are).
 template <int BITS, int PD>
@@ -87,7 +95,7 @@ struct Block {
     static constexpr int PITCH = BITS == 3 ? 48 : BITS * PD / 8 <= 64 ? 80 : 144;
     static constexpr int K = 0, V = 16 * PD * BITS / 8, SK = V + 16 * PITCH, SV = SK + 64, BYTES = SV + 64;
 };
-constexpr int STAGES = 4;
+constexpr int STAGES = 2;
 
 // Entry of a key row that is half h of converted word i of quarter t (the order convert_k gives).
 template <int BITS, int PD>
@@ -132,7 +140,7 @@ template <int BITS, int PD, int NT>
 struct RowsShared {
     static constexpr int ROWS = 8 * NT;
     union {
-        alignas(16) uint8_t ring[ROW_WARPS][STAGES][Block<BITS, PD>::BYTES];
+        alignas(16) uint8_t ring[ROW_WARPS][STAGES][2][Block<BITS, PD>::BYTES];
         alignas(16) float o[ROW_WARPS][ROWS][PD + 4];  // the warps' sums
     };
     float top[ROW_WARPS], factor;
@@ -179,21 +187,24 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
     const int rows = min(ROWS, (int)min(all_rows - r0, (long long)ROWS));
     const int pos0 = __ldg(a.b.kv_len + seq) - q_len;
     const int pos_lo = pos0 + r0 / a.group, pos_hi = pos0 + (r0 + rows - 1) / a.group;
-    const Span span = span_of<4>(a, pos_lo, pos_hi);
-    // positions are dealt out evenly, two blocks for every warp of a part at least
-    const int rank = blockIdx.y % a.ranks, cluster = blockIdx.y / a.ranks, parts = gridDim.y;
-    const int per = max(2 * ROW_WARPS, (span.count + parts - 1) / parts);
+    const Span span = span_of<5>(a, pos_lo, pos_hi);
+    // positions are dealt out evenly, a pair of blocks for every warp of a part at least
+    const int rank = blockIdx.y & (a.ranks - 1), cluster = blockIdx.y / a.ranks, parts = gridDim.y;
+    const int per = max(ROW_WARPS, (span.count + parts - 1) / parts);
     const int v_begin = blockIdx.y * per, v_end = min(span.count, v_begin + per);
 
-    // ---- the warp's blocks v_begin + warp + 4k: pages of the first ones under way
-    const int blocks = max(0, (v_end - v_begin - warp + ROW_WARPS - 1) / ROW_WARPS);
-    auto block_at = [&](int k) { return span.block(v_begin + warp + ROW_WARPS * k); };
-    auto page_at = [&](int k) { return k < blocks ? a48p::page_of(a.l, a.b, seq, block_at(k) << 4) : -1; };
-    int page[STAGES], next_page[2];  // of the blocks in the ring, of the next two
+    // ---- the warp's pairs of blocks v_begin + warp + 4k: pages of the first ones under way
+    const int window = in_register(a.window), sinks = in_register(a.sinks);
+    const int pairs = max(0, (v_end - v_begin - warp + ROW_WARPS - 1) / ROW_WARPS);
+    auto first_of = [&](int k) { return span.block(v_begin + warp + ROW_WARPS * k) << 5; };
+    auto page_at = [&](int k, int b) {  // of block b of pair k; the second block has the first's page if that is large enough
+        return k < pairs && (b == 0 || a.l.page_shift == 4) ? a48p::page_of(a.l, a.b, seq, first_of(k) + 16 * b) : -1;
+    };
+    int page[STAGES + 1][2];  // of the pairs in the stages and of the next
 #pragma unroll
-    for (int k = 0; k < STAGES; ++k) page[k] = page_at(k);
+    for (int k = 0; k <= STAGES; ++k)
 #pragma unroll
-    for (int k = 0; k < 2; ++k) next_page[k] = page_at(STAGES + k);
+        for (int b = 0; b < 2; ++b) page[k][b] = page_at(k, b);
     if (threadIdx.x < ROWS) {
         const int in_seq = r0 + min((int)threadIdx.x, rows - 1), i = in_seq / a.group;
         sm.token[threadIdx.x] = start + i;
@@ -206,7 +217,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
     using B = Block<BITS, PD>;
     constexpr int PIECES = (PD * BITS / 8 + 31) / 32;
     const int row = a.l.row, pitch = BITS == 3 ? row : B::PITCH;
-    uint8_t* ring = &sm.ring[warp][0][0];
+    uint8_t* ring = &sm.ring[warp][0][0][0];
     const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
     uint32_t v_dst[PIECES];
 #pragma unroll
@@ -216,20 +227,27 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
     }
     const uint8_t* head_chunks = a.pool + (size_t)kvh * a.l.chunk;
     const size_t page_bytes = (size_t)a.l.kv_heads * a.l.chunk;
-    auto load = [&](int k, int stage, int from) {
-        const int p = __shfl_sync(0xffffffffu, from, 0);  // the same for the warp: the addresses are formed once for it
-        if (p >= 0) {
-            const int slot = (block_at(k) << 4) & (a.l.page - 1);
-            const uint8_t* chunk = head_chunks + p * page_bytes;
-            const uint8_t* codes = chunk + slot * row + 16 * lane;
-            const uint32_t dst = ring_at + stage * B::BYTES;
+    const int slots = in_register(a.l.page - 1), v_codes = in_register(a.l.v_codes);
+    const int scales = lane < 4 ? a.l.k_scales + 16 * lane : a.l.v_scales + 16 * (lane - 4);
+    // pair k into a stage; returns its pages (the same for the warp: addresses are formed once for it)
+    auto load = [&](int k, int stage, int (&from)[2]) {
+        from[0] = __shfl_sync(0xffffffffu, from[0], 0);
+        from[1] = a.l.page_shift == 4 ? __shfl_sync(0xffffffffu, from[1], 0) : from[0];
+        const int slot = first_of(k) & slots;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            if (from[b] < 0) continue;
+            const int at = (slot + 16 * b) & slots;
+            const uint8_t* chunk = head_chunks + from[b] * page_bytes;
+            const uint8_t* codes = chunk + at * row + 16 * lane;
+            const uint32_t dst = ring_at + (2 * stage + b) * B::BYTES;
 #pragma unroll
             for (int i = 0; i < PIECES; ++i)
                 if (lane + 32 * i < row) {
                     copy16(dst + B::K + 16 * (lane + 32 * i), codes + 512 * i);
-                    copy16(dst + v_dst[i], codes + a.l.v_codes + 512 * i);
+                    copy16(dst + v_dst[i], codes + (v_codes + 512 * i));
                 }
-            if (lane < 8) copy16(dst + B::SK + 16 * lane, chunk + (lane < 4 ? a.l.k_scales : a.l.v_scales) + 4 * slot + 16 * (lane & 3));
+            if (lane < 8) copy16(dst + B::SK + 16 * lane, chunk + scales + 4 * at);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -264,15 +282,17 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
         __syncthreads();
 #pragma unroll
         for (int w = 0; w < ROW_WARPS; ++w) top = max(top, __float_as_uint(sm.top[w]));
-        const int e = top > 0 ? 14 - ilogbf(__uint_as_float(top)) : 0;
+        const int e = a48p::query_exponent(top);
+        const float up0 = a48p::power_of_two(e / 2), up1 = a48p::power_of_two(e - e / 2);
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
             const int r = warp + ROW_WARPS * k;
-            const __half2 lo = __floats2half2_rn(scalbnf(x[k][0], e), scalbnf(x[k][1], e)), hi = __floats2half2_rn(scalbnf(x[k][2], e), scalbnf(x[k][3], e));
+            const __half2 lo = __floats2half2_rn(x[k][0] * up0 * up1, x[k][1] * up0 * up1),
+                          hi = __floats2half2_rn(x[k][2] * up0 * up1, x[k][3] * up0 * up1);
             if (4 * lane < PD)
                 *reinterpret_cast<uint2*>(&sm.q[r][4 * lane]) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
         }
-        if (threadIdx.x == 0) sm.factor = scalbnf(a.scale * 1.4426950408889634f, -e);
+        if (threadIdx.x == 0) sm.factor = a.scale * 1.4426950408889634f * a48p::power_of_two(-e / 2) * a48p::power_of_two(-(e - e / 2));
     }
     __syncthreads();
     const float factor = sm.factor;  // of an accumulator times its key scale: the score in units of log2 e
@@ -303,15 +323,12 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
     }
     float v_unit = INFINITY;  // 2^6 over a power of two not below the largest value scale so far; infinite while that is 0
 
-    // Two blocks, in stages `stage` and `stage` + 1 of the ring; first[b]: their first positions, NOWHERE for one that is not
-    // there (past the warp's last, or without a page).
-    constexpr int NOWHERE = 0x7fffff00;
-    auto take = [&](int stage, const int (&first)[2], const int (&from)[2]) {
+    // The pair of blocks in a stage, at positions from `first` on; from[b] < 0: block b is not there.
+    auto take = [&](int stage, int first, const int (&from)[2]) {
         float s[2][NT][4], y[2][NT][4], ks[2][2], f[2][2], w[2][2];
-        bool whole[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const uint8_t* block = ring + (stage + b) * B::BYTES;
+            const uint8_t* block = ring + (2 * stage + b) * B::BYTES;
             uint32_t k0[Share<BITS, PD>::K], k1[Share<BITS, PD>::K], ka[NK], kb[NK];
             load_words(block + k_off, k0);
             load_words(block + k_off + 8 * row, k1);
@@ -322,7 +339,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
             }
             convert_k<BITS, PD>(k0, ka);
             convert_k<BITS, PD>(k1, kb);
-            if (BITS == 3 && first[b] == 0) {  // the bos heads: 4-bit codes of their own, in convert_k's order
+            if (BITS == 3 && b == 0 && first == 0 && from[0] >= 0) {  // the bos heads: 4-bit codes of their own, in convert_k's order
                 const uint8_t* bos = a.pool + a48p::chunk_at(a.l, from[b], kvh) + a.l.bos;
                 if (g == 0 && k_there) {
 #pragma unroll
@@ -336,20 +353,15 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                float s2[4] = {};  // (two chains of MMAs instead of one of twice the length)
+                mma_f16_first(s[b][n], ka[0], kb[0], ka[1], kb[1], qf[n][0], qf[n][1]);
 #pragma unroll
-                for (int c = 0; c < 4; ++c) s[b][n][c] = 0.f;
-#pragma unroll
-                for (int i = 0; i < NK / 2; ++i)
-                    mma_f16(i & 1 ? s2 : s[b][n], ka[2 * i], kb[2 * i], ka[2 * i + 1], kb[2 * i + 1], qf[n][2 * i], qf[n][2 * i + 1]);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) s[b][n][c] += s2[c];
+                for (int i = 1; i < NK / 2; ++i) mma_f16(s[b][n], ka[2 * i], kb[2 * i], ka[2 * i + 1], kb[2 * i + 1], qf[n][2 * i], qf[n][2 * i + 1]);
             }
-            whole[b] = first[b] != NOWHERE && first[b] + 15 <= pos_lo && (a.window == 0 || first[b] > pos_hi - a.window || first[b] + 15 < a.sinks);
         }
-        auto seen = [&](int b, int n, int c) {  // by row 2t + c % 2, position g + 8 (c / 2)
-            const int j = first[b] + g + 8 * (c >> 1), last = lim[n][c & 1];
-            return first[b] != NOWHERE && j <= last && (a.window == 0 || j > last - a.window || j < a.sinks);
+        const bool whole = first + 31 <= pos_lo && (window == 0 || first > pos_hi - window || first + 31 < sinks) && (from[0] | from[1]) >= 0;
+        auto seen = [&](int b, int n, int c) {  // by row 2t + c % 2, position g + 8 (c / 2) of the block
+            const int j = first + 16 * b + g + 8 * (c >> 1), last = lim[n][c & 1];
+            return from[b] >= 0 && j <= last && (window == 0 || j > last - window || j < sinks);
         };
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -357,7 +369,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) y[b][n][c] = fmaf(s[b][n][c], ks[b][c >> 1], -m[n][c & 1]);
-        if (!(whole[0] && whole[1])) {
+        if (!whole) {
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
 #pragma unroll
@@ -366,8 +378,8 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
                     for (int c = 0; c < 4; ++c) y[b][n][c] = seen(b, n, c) ? y[b][n][c] : -INFINITY;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {  // what no row sees does not count
-                    const int j = first[b] + g + 8 * i;
-                    if (first[b] == NOWHERE || !(j <= pos_hi && (a.window == 0 || j > pos_lo - a.window || j < a.sinks))) f[b][i] = 0.f;
+                    const int j = first + 16 * b + g + 8 * i;
+                    if (!(from[b] >= 0 && j <= pos_hi && (window == 0 || j > pos_lo - window || j < sinks))) f[b][i] = 0.f;
                 }
             }
         }
@@ -420,7 +432,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
                     for (int b = 0; b < 2; ++b)
 #pragma unroll
                         for (int k = 0; k < 2; ++k) {
-                            z[b][k] = whole[b] || seen(b, n, i + 2 * k) ? s[b][n][i + 2 * k] * ks[b][k] : -INFINITY;
+                            z[b][k] = whole || seen(b, n, i + 2 * k) ? s[b][n][i + 2 * k] * ks[b][k] : -INFINITY;
                             if (!number[b][k] && z[b][k] != -INFINITY) z[b][k] = NAN;  // a value that is none, for the rows that see it
                             mx = fmaxf(mx, z[b][k]);
                         }
@@ -439,7 +451,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
         }
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-            const uint8_t* block = ring + (stage + b) * B::BYTES;
+            const uint8_t* block = ring + (2 * stage + b) * B::BYTES;
             uint32_t pb[NT][2];
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -455,7 +467,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
             for (int i = 0; i < 4; ++i) load_words(block + v_off + ((i & 1) + 8 * (i >> 1)) * pitch, v0[i]);
             convert_v<BITS, PD>(v0[0], v0[1], halves, va);
             convert_v<BITS, PD>(v0[2], v0[3], halves, vb);
-            if (BITS == 3 && first[b] == 0) {
+            if (BITS == 3 && b == 0 && first == 0 && from[0] >= 0) {
                 const uint8_t* bos = a.pool + a48p::chunk_at(a.l, from[b], kvh) + a.l.bos + a.l.padded / 2;
                 if (t == 0 && v_there) {
 #pragma unroll
@@ -473,20 +485,14 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
         }
     };
 #pragma unroll 1
-    for (int k = 0; k < blocks; k += 2) {
-        const int stage = k & 2;
-        asm volatile("cp.async.wait_group 2;" ::: "memory");  // all but the next two blocks
+    for (int k = 0; k < pairs; ++k) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
         __syncwarp();
-        const int from[2] = {stage ? page[2] : page[0], stage ? page[3] : page[1]};
-        const int first[2] = {from[0] >= 0 ? block_at(k) << 4 : NOWHERE, from[1] >= 0 ? block_at(k + 1) << 4 : NOWHERE};
-        take(stage, first, from);
-        __syncwarp();  // every lane has read the two stages
+        take(k & 1, first_of(k), page[0]);
+        __syncwarp();  // every lane has read the stage
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-            load(k + STAGES + b, stage + b, next_page[b]);
-            (stage ? page[2 + b] : page[b]) = next_page[b];
-            next_page[b] = page_at(k + STAGES + 2 + b);
-        }
+        for (int b = 0; b < 2; ++b) page[0][b] = page[1][b], page[1][b] = page[2][b], page[2][b] = page_at(k + STAGES + 1, b);
+        load(k + STAGES, k & 1, page[1]);
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();  // the ring's memory is the sums' now
@@ -537,7 +543,7 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
         if (a.ranks == 1) {
             finish(r, c, top, sum, acc);
         } else {  // to the CTA that finishes this piece
-            const int to = i % a.ranks, at = i / a.ranks * a.ranks + rank;
+            const int to = i & (a.ranks - 1), at = (i & -a.ranks) + rank;
             st_rank(of_rank(&sm.piece[at], to), make_float4(acc[0], acc[1], acc[2], acc[3]));
             st_rank(of_rank(&sm.piece_ml[at], to), make_float2(top, sum));
         }
@@ -645,10 +651,11 @@ Plan plan_of(const bitnet_a48_paged_cache& c, const bitnet_a48_paged_batch& b, i
     if (b.max_kv < reach) reach = b.max_kv;
     // positions a tile of `span` tokens may see
     auto seen = [&](long long span) { return window > 0 && window + sinks + span < reach ? window + sinks + span : reach; };
-    // Four waves of CTAs at four to an SM, which evens out sequences of unlike lengths, as long as every warp of a part has
-    // two blocks of 16 positions.  Up to eight parts join inside a cluster; more only where those leave SMs idle.
-    const long long base = (long long)b.n_seqs * c.n_kv_heads * p.tiles, most = up(seen(64), 16 * 2 * ROW_WARPS);
-    p.ranks = within(up(16 * SMS, base), 1, most < MAX_RANKS ? most : MAX_RANKS);
+    // One wave of CTAs at four to an SM, as long as every warp of a part has
+    // a pair of blocks.  Up to eight parts join inside a cluster; more only where those leave SMs idle.
+    const long long base = (long long)b.n_seqs * c.n_kv_heads * p.tiles, most = up(seen(64), 32 * ROW_WARPS);
+    p.ranks = 1;  // a power of two
+    while (p.ranks < MAX_RANKS && base * p.ranks < 4 * SMS && 2 * p.ranks <= most) p.ranks *= 2;
     p.clusters = p.ranks < MAX_RANKS ? 1 : within(2 * SMS / (base * MAX_RANKS), 1, most / MAX_RANKS < 16 ? most / MAX_RANKS : 16);
     // Tile kernel, one CTA per SM: split while the tiles do not fill the SMs, into parts of two tiles or more.
     p.tc_tiles = 0, p.tc_splits = 1;

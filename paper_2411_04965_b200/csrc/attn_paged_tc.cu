@@ -35,6 +35,9 @@ namespace {
 
 using a48p::AttnArgs;
 using a48p::exp2_approx;
+using a48p::in_register;
+using a48p::power_of_two;
+using a48p::query_exponent;
 using a48p::Span;
 
 constexpr int TQ = 128, TK = a48p::TILE_POSITIONS, RING = 4, SCALES = 4;
@@ -164,13 +167,6 @@ __device__ __forceinline__ void tmem_wait_ld(uint32_t (&r)[2][8]) {
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Keeps a kernel argument in a register: read in a loop it would come from the constant bank again and again, which the
-// loop's own code keeps pushing out of the cache (measured: 0.5k clocks a tile).
-__device__ __forceinline__ int in_register(int x) {
-    asm volatile("" : "+r"(x));
-    return x;
-}
-
 // two floats as one operand
 typedef unsigned long long f2;
 __device__ __forceinline__ f2 pack2(float x, float y) {
@@ -237,12 +233,6 @@ struct Cfg {
     static constexpr int SMEM = SCALES_AT + SCALES * (int)sizeof(TileScales) + 1024 /*alignment slack*/;
     static_assert(SMEM <= 227 * 1024, "shared memory budget");
 };
-
-// the power of two that brings the largest query entry to [2^14, 2^15)
-__device__ __forceinline__ int query_exponent(uint32_t top) {
-    const float x = __uint_as_float(top);
-    return x > 0.f ? 14 - ilogbf(x) : 0;
-}
 
 // what a wait that gave up was for
 enum { WAIT_FULL = 41, WAIT_EMPTY = 42, WAIT_S = 43, WAIT_O = 45 };
@@ -419,7 +409,8 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             look_up(1);
         }
         queries_sync();
-        const float factor = scalbnf(a.scale * 1.4426950408889634f, -query_exponent(*q_top));
+        const int e = query_exponent(*q_top);
+        const float factor = a.scale * 1.4426950408889634f * power_of_two(-e / 2) * power_of_two(-(e - e / 2));
         auto wait_empty = [&](int n) {
             if (n >= RING) mbar_wait(bar_empty + 8 * (n % RING), (n / RING & 1) ^ 1, abort_flag, WAIT_EMPTY, n);
             return smem + n % RING * C::BUF;
@@ -505,7 +496,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             row_info[r].x = __int_as_float(pos0 + (int)(in_seq / a.group));
             queries_sync();
             const int e = query_exponent(*q_top);
-            const float up0 = scalbnf(1.f, e / 2), up1 = scalbnf(1.f, e - e / 2);  // (2^e may be past fp32)
+            const float up0 = power_of_two(e / 2), up1 = power_of_two(e - e / 2);  // (2^e may be past fp32)
             auto value = [&](int n) {
                 const uint32_t w = n & 2 ? x[n / 4].y : x[n / 4].x;
                 return __uint_as_float(n & 1 ? w & 0xffff0000u : w << 16) * up0 * up1;

@@ -52,6 +52,18 @@ __device__ __forceinline__ void triples(uint32_t w0, uint32_t w1, uint32_t w2, u
     out[15] = fields<0>(top, 0x00070007u, 4);
 }
 
+// 2^e for -126 <= e <= 127
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }
+// The e that brings the largest of some query entries (finite, as bits) to [2^14, 2^15), fp16's top; entries below fp32's
+// normal numbers go as far as they go (their scores are nothing).
+__device__ __forceinline__ int query_exponent(uint32_t top) { return top ? 14 + 127 - (int)(top >> 23) : 0; }
+// A kernel argument kept in a register: read in a loop it would come from the constant bank again and again, which the
+// loop's own code keeps pushing out of the cache (measured: 0.5k clocks a tile of the tile kernel).
+__device__ __forceinline__ int in_register(int x) {
+    asm volatile("" : "+r"(x));
+    return x;
+}
+
 // 2^x, two units in the last place at most; 2^-inf = 0
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
