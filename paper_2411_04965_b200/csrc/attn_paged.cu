@@ -6,9 +6,9 @@
 // p the position of token i.  k[j] = sk[j] c[j] and v[j] = sv[j] d[j] with integer codes c, d, so that
 //   score = (q . c[j]) sk[j] scale,   out = (sum_j p[j] sv[j] d[j]) / sum_j p[j]:
 // both contractions run on the codes, which fp16 holds exactly, and the scales meet the scores and the probabilities in
-// fp32.  A query row is brought into fp16 by a power of two of its own (its bf16 numbers keep all their bits down to
-// 2^-29 of the largest), the weights p sv by a power of two that follows the largest value scale; what is rounded is the
-// weight, to fp16's 11 bits (bf16's 8 would cost as much as the rounding of the output).
+// fp32.  Query rows are brought into fp16 by a power of two (their bf16 numbers fit its 11 bits), the weights p sv by a
+// power of two that follows the largest value scale; what is rounded is the weight, to fp16's 11 bits (bf16's 8 would
+// cost as much as the rounding of the output).
 //
 // The rows of one key/value head (token i, query head of the group) are taken together.  Sequences with few rows
 // (decoding, drafted tokens) go to attn_paged_rows_kernel below, those with more to the tile kernel of attn_paged_tc.cu.
@@ -49,12 +49,13 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// the first of a chain: onto zero
-__device__ __forceinline__ void mma_f16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+// the first of a chain: onto `start`, by the column's parity
+__device__ __forceinline__ void mma_f16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1,
+                                              const float (&start)[2]) {
     asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
         : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(start[0]), "f"(start[1]), "f"(start[0]), "f"(start[1]));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     uint32_t r;
@@ -104,15 +105,18 @@ __device__ __forceinline__ int k_entry(int t, int i, int h) {
     if (BITS == 4) return PD / 4 * t + 8 * (i / 4) + i % 4 + 4 * h;
     return PD / 4 * t + 4 * (i / 2) + i % 2 + 2 * h;
 }
+// (as raw fields: the query fragments carry 2^-s, the factor of the scores 2^24, and the accumulators start at the offset's
+// share, -2^(bits-1) times the sum of the query's entries.  Not so for the values: their sums run over thousands of
+// positions, and would grow with the offset where those of signed codes do not.)
 template <int BITS, int PD>
 __device__ __forceinline__ void convert_k(const uint32_t (&w)[Share<BITS, PD>::K], uint32_t (&out)[PD / 8]) {
-    if constexpr (BITS == 3) a48p::triples(w[0], w[1], w[2], out);
+    if constexpr (BITS == 3) a48p::raw_triples(w[0], w[1], w[2], out);
     else if constexpr (BITS == 4) {
 #pragma unroll
-        for (int i = 0; i < PD / 32; ++i) a48p::nibbles(w[i], out + 4 * i);
+        for (int i = 0; i < PD / 32; ++i) a48p::raw_nibbles(w[i], out + 4 * i);
     } else {
 #pragma unroll
-        for (int i = 0; i < PD / 16; ++i) a48p::bytes(w[i], out + 2 * i);
+        for (int i = 0; i < PD / 16; ++i) a48p::raw_bytes(w[i], out + 2 * i);
     }
 }
 // The PD / 8 entries of an eighth, in order, of two positions a and b.
@@ -143,7 +147,7 @@ struct RowsShared {
         alignas(16) uint8_t ring[ROW_WARPS][STAGES][2][Block<BITS, PD>::BYTES];
         alignas(16) float o[ROW_WARPS][ROWS][PD + 4];  // the warps' sums
     };
-    float top[ROW_WARPS], factor;
+    float top[ROW_WARPS], start[ROWS], factor;  // start: of a row's accumulators
     float m[ROW_WARPS][ROWS], l[ROW_WARPS][ROWS];
     int token[ROWS], head[ROWS];
     // what the cluster's CTAs send: pieces of four head dims, with the exponent of their reference and their sum of p
@@ -260,8 +264,8 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
     const uint32_t k_off = B::K + (k_there ? k_first : 0) + g * row, v_off = B::V + (v_there ? v_first : 0) + 2 * t * pitch;
     const uint32_t halves = (g & 1) ? 0x7632u : 0x5410u;
 
-    // ---- the query rows to fp16 by one power of two (the largest entry of the tile to [2^14, 2^15): a row 2^20 below it
-    // still has all its bits, one 2^29 below it the upper ten)
+    // ---- the query rows to fp16 by one power of two (the largest entry of the tile to [2^14, 2^15): a row 2^14 below it
+    // still has all its bits, one 2^23 below it the upper ten)
     {
         constexpr int PER = ROWS / ROW_WARPS;
         float x[PER][4] = {};
@@ -289,24 +293,34 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
             const int r = warp + ROW_WARPS * k;
             const __half2 lo = __floats2half2_rn(x[k][0] * up0 * up1, x[k][1] * up0 * up1),
                           hi = __floats2half2_rn(x[k][2] * up0 * up1, x[k][3] * up0 * up1);
+            // (of the numbers as they are rounded)
+            float sum = __low2float(lo) + __high2float(lo) + __low2float(hi) + __high2float(hi);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (lane == 0) sm.start[r] = -sum * (float)(1 << (BITS - 1)) * 0x1p-24f;
             if (4 * lane < PD)
                 *reinterpret_cast<uint2*>(&sm.q[r][4 * lane]) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
         }
-        if (threadIdx.x == 0) sm.factor = a.scale * 1.4426950408889634f * a48p::power_of_two(-e / 2) * a48p::power_of_two(-(e - e / 2));
+        if (threadIdx.x == 0) sm.factor = a.scale * 1.4426950408889634f * a48p::power_of_two(24 - e / 2) * a48p::power_of_two(-(e - e / 2));
     }
     __syncthreads();
     const float factor = sm.factor;  // of an accumulator times its key scale: the score in units of log2 e
     uint32_t qf[NT][NK];
     int lim[NT][2];
+    float begin[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
         for (int i = 0; i < NK; ++i) {
-            const __half2 h = __halves2half2(sm.q[8 * n + g][k_entry<BITS, PD>(t, i, 0)], sm.q[8 * n + g][k_entry<BITS, PD>(t, i, 1)]);
+            const __half2 h = __hmul2(__halves2half2(sm.q[8 * n + g][k_entry<BITS, PD>(t, i, 0)], sm.q[8 * n + g][k_entry<BITS, PD>(t, i, 1)]),
+                                      __float2half2_rn(1.f / (1 << a48p::raw_shift<BITS>(i))));
             qf[n][i] = *reinterpret_cast<const uint32_t*>(&h);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) lim[n][i] = pos0 + (r0 + min(8 * n + 2 * t + i, rows - 1)) / a.group;  // the last position the row sees
+        for (int i = 0; i < 2; ++i) {
+            lim[n][i] = pos0 + (r0 + min(8 * n + 2 * t + i, rows - 1)) / a.group;  // the last position the row sees
+            begin[n][i] = sm.start[8 * n + 2 * t + i];
+        }
     }
 
     if (a.ranks > 1) cluster_arrive();  // (waited for ahead of the first write to another CTA's shared memory, over the queries)
@@ -345,15 +359,16 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
 #pragma unroll
                     for (int i = 0; i < NK; ++i) {
                         const int e0 = k_entry<BITS, PD>(t, i, 0), e1 = k_entry<BITS, PD>(t, i, 1);
-                        const __half2 h = __floats2half2_rn((float)((bos[e0 / 2] >> (4 * (e0 & 1))) & 15) - 8.f,
-                                                            (float)((bos[e1 / 2] >> (4 * (e1 & 1))) & 15) - 8.f);
+                        const float unit = (float)(1 << a48p::raw_shift<3>(i)) * 0x1p-24f;  // (codes less 8 on top of an offset of 4)
+                        const __half2 h = __floats2half2_rn(((float)((bos[e0 / 2] >> (4 * (e0 & 1))) & 15) - 4.f) * unit,
+                                                            ((float)((bos[e1 / 2] >> (4 * (e1 & 1))) & 15) - 4.f) * unit);
                         ka[i] = *reinterpret_cast<const uint32_t*>(&h);
                     }
                 }
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                mma_f16_first(s[b][n], ka[0], kb[0], ka[1], kb[1], qf[n][0], qf[n][1]);
+                mma_f16_first(s[b][n], ka[0], kb[0], ka[1], kb[1], qf[n][0], qf[n][1], begin[n]);
 #pragma unroll
                 for (int i = 1; i < NK / 2; ++i) mma_f16(s[b][n], ka[2 * i], kb[2 * i], ka[2 * i + 1], kb[2 * i + 1], qf[n][2 * i], qf[n][2 * i + 1]);
             }

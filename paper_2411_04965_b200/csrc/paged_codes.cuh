@@ -52,6 +52,38 @@ __device__ __forceinline__ void triples(uint32_t w0, uint32_t w1, uint32_t w2, u
     out[15] = fields<0>(top, 0x00070007u, 4);
 }
 
+// The same fields as they are: u 2^s in the mantissa of a subnormal fp16 number, u 2^(s-24).  One mask per pair; the offset and
+// the 2^(s-24) are the other operand's.
+__device__ __forceinline__ void raw_nibbles(uint32_t w, uint32_t* out) {
+    out[0] = w & 0x000f000fu;
+    out[1] = w & 0x00f000f0u;
+    w >>= 8;
+    out[2] = w & 0x000f000fu;
+    out[3] = w & 0x00f000f0u;
+}
+__device__ __forceinline__ void raw_bytes(uint32_t w, uint32_t* out) {
+    out[0] = w & 0x00ff00ffu;
+    out[1] = (w >> 8) & 0x00ff00ffu;
+}
+__device__ __forceinline__ void raw_triples(uint32_t w0, uint32_t w1, uint32_t w2, uint32_t* out) {
+    const uint32_t w[3] = {w0, w1, w2};
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+        out[5 * j] = w[j] & 0x00070007u;
+        out[5 * j + 1] = w[j] & 0x00380038u;
+        out[5 * j + 2] = w[j] & 0x01c001c0u;
+        const uint32_t up = w[j] >> 9;
+        out[5 * j + 3] = up & 0x00070007u;
+        out[5 * j + 4] = up & 0x00380038u;
+    }
+    out[15] = ((w0 >> 15) & 0x00010001u) | ((w1 >> 14) & 0x00020002u) | ((w2 >> 13) & 0x00040004u);
+}
+// s of the i-th word that they give
+template <int BITS>
+__device__ __forceinline__ constexpr int raw_shift(int i) {
+    return BITS == 8 ? 0 : BITS == 4 ? 4 * (i & 1) : i == 15 ? 0 : i % 5 < 3 ? 3 * (i % 5) : 3 * (i % 5 - 3);
+}
+
 // 2^e for -126 <= e <= 127
 __device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }
 // The e that brings the largest of some query entries (finite, as bits) to [2^14, 2^15), fp16's top; entries below fp32's
