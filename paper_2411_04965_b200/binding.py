@@ -483,7 +483,7 @@ class PagedCache:
         if pool is None:
             pool = torch.zeros(self.nbytes, dtype=torch.uint8, device=device)
         assert pool.is_cuda and pool.is_contiguous() and pool.numel() * pool.element_size() >= self.nbytes
-        self.pool = pool
+        self.pool, self.pool_ptr = pool, pool.data_ptr()
         self.bits, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages = bits, n_kv_heads, head_dim, page_size, n_pages
 
 
@@ -493,93 +493,104 @@ class PagedBatch:
     def __init__(self, q_start: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor, n_tokens: int, max_q: int, max_kv: int):
         for t in (q_start, kv_len, pages):
             assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()
-        assert pages.dim() == 2 and kv_len.numel() == pages.shape[0] and q_start.numel() == pages.shape[0] + 1
+        n_seqs, max_pages = pages.shape
+        assert kv_len.shape == (n_seqs,) and q_start.shape == (n_seqs + 1,)
         self.q_start, self.kv_len, self.pages, self.n_tokens = q_start, kv_len, pages, n_tokens
-        self.view = PagedBatchView(pages.shape[0], n_tokens, max_q, max_kv, pages.shape[1], q_start.data_ptr(), kv_len.data_ptr(),
-                                   pages.data_ptr())
+        self.view = PagedBatchView(n_seqs, n_tokens, max_q, max_kv, max_pages, q_start.data_ptr(), kv_len.data_ptr(), pages.data_ptr())
         self.view_ref = byref(self.view)
 
 
-class _On:
-    """Makes the tensors' device and the call's stream current, so that what a call allocates belongs to that stream."""
+def _on_stream(t: torch.Tensor, stream):
+    """The raw handle of the current stream where the call may go on as it is; None where the tensor's device or the call's
+    stream has to be made current first (what a call allocates then belongs to that stream)."""
+    index = t.device.index
+    if stream is None and index == torch._C._cuda_getDevice():
+        return torch._C._cuda_getCurrentRawStream(index)
+    return None
 
-    def __init__(self, t: torch.Tensor, stream):
-        self.stream = stream if stream is not None else torch.cuda.current_stream(t.device)
-        self.same = stream is None and t.device.index == torch.cuda.current_device()
-        self.guard = None if self.same else torch.cuda.stream(self.stream)
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return c_void_p(self.stream.cuda_stream)
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _made_current(t: torch.Tensor, stream):
+    return torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(t.device))
 
 
 def _rows(t: torch.Tensor, n_tokens: int, width: int, dtype) -> int:
     """Stride of token rows [n_tokens, width] whose columns are contiguous."""
-    assert t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape[0] == n_tokens and t.shape[1] == width
-    assert t.stride(1) == 1 or width == 1
-    return t.stride(0) if n_tokens > 1 else max(t.stride(0), width)
+    assert t.is_cuda and t.dtype == dtype and t.shape == (n_tokens, width)
+    stride, one = t.stride()
+    assert one == 1 or width == 1
+    return stride if n_tokens > 1 else max(stride, width)
 
 
 def paged_write(cache: PagedCache, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor, q=None, rope_base: float = 10000.0,
                 eps: float = 1e-5, q_out=None, stream=None):
     """Rotates (rope_base 0: does not), quantises and stores k, v [n_tokens, n_kv_heads*head_dim] (fp32 or bf16, rows may be
     strided); rotates q [n_tokens, n_heads*head_dim] into q_out (bf16, made here unless given).  Returns q_out."""
-    n, width = batch.n_tokens, cache.n_kv_heads * cache.head_dim
-    bf16 = k.dtype == torch.bfloat16
-    dtype = torch.bfloat16 if bf16 else torch.float32
-    ks, vs, qs, os_, heads = _rows(k, n, width, dtype), _rows(v, n, width, dtype), 0, 0, 0
-    assert q_out is None or q is not None
-    with _On(k, stream) as st:
-        if q is not None:
-            heads = q.shape[1] // cache.head_dim
-            qs = _rows(q, n, heads * cache.head_dim, dtype)
-            if q_out is None:
-                q_out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-            os_ = _rows(q_out, n, q.shape[1], torch.bfloat16)
-        _check(lib().bitnet_a48_paged_write(cache.cfg_ref, cache.pool.data_ptr(), batch.view_ref, heads,
-                                            q.data_ptr() if q is not None else None, qs, k.data_ptr(), ks, v.data_ptr(), vs, int(bf16),
-                                            rope_base, eps, q_out.data_ptr() if q is not None else None, os_, st), "paged_write")
+    st = _on_stream(k, stream)
+    if st is None:
+        with _made_current(k, stream):
+            return paged_write(cache, batch, k, v, q, rope_base, eps, q_out)
+    n, width, dtype = batch.n_tokens, cache.n_kv_heads * cache.head_dim, k.dtype
+    bf16 = dtype == torch.bfloat16
+    assert bf16 or dtype == torch.float32
+    ks, vs = _rows(k, n, width, dtype), _rows(v, n, width, dtype)
+    if q is None:
+        assert q_out is None
+        qp, qs, op, os_, heads = None, 0, None, 0, 0
+    else:
+        heads = q.shape[1] // cache.head_dim
+        qs = _rows(q, n, heads * cache.head_dim, dtype)
+        if q_out is None:
+            q_out = torch.empty(n, heads * cache.head_dim, dtype=torch.bfloat16, device=q.device)
+        qp, op, os_ = q.data_ptr(), q_out.data_ptr(), _rows(q_out, n, heads * cache.head_dim, torch.bfloat16)
+    _check(_lib.bitnet_a48_paged_write(cache.cfg_ref, cache.pool_ptr, batch.view_ref, heads, qp, qs, k.data_ptr(), ks, v.data_ptr(), vs,
+                                       bf16, rope_base, eps, op, os_, st), "paged_write")
     return q_out
 
 
 def paged_read(cache: PagedCache, batch: PagedBatch, dtype=torch.bfloat16, k_out=None, v_out=None, stream=None):
     """The keys and values at the positions of the batch's tokens, [n_tokens, n_kv_heads, head_dim] each, fp32 or bf16."""
+    st = _on_stream(cache.pool, stream)
+    if st is None:
+        with _made_current(cache.pool, stream):
+            return paged_read(cache, batch, dtype, k_out, v_out)
     assert dtype in (torch.bfloat16, torch.float32)
     shape = (batch.n_tokens, cache.n_kv_heads, cache.head_dim)
-    with _On(cache.pool, stream) as st:
-        k_out = k_out if k_out is not None else torch.empty(shape, dtype=dtype, device=cache.pool.device)
-        v_out = v_out if v_out is not None else torch.empty(shape, dtype=dtype, device=cache.pool.device)
-        for t in (k_out, v_out):
-            assert t.is_cuda and t.dtype == dtype and t.is_contiguous() and tuple(t.shape) == shape
-        _check(lib().bitnet_a48_paged_read(cache.cfg_ref, cache.pool.data_ptr(), batch.view_ref, k_out.data_ptr(), v_out.data_ptr(),
-                                           int(dtype == torch.bfloat16), st), "paged_read")
+    k_out = k_out if k_out is not None else torch.empty(shape, dtype=dtype, device=cache.pool.device)
+    v_out = v_out if v_out is not None else torch.empty(shape, dtype=dtype, device=cache.pool.device)
+    for t in (k_out, v_out):
+        assert t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.shape == shape
+    _check(_lib.bitnet_a48_paged_read(cache.cfg_ref, cache.pool_ptr, batch.view_ref, k_out.data_ptr(), v_out.data_ptr(),
+                                      dtype == torch.bfloat16, st), "paged_read")
     return k_out, v_out
 
 
 def attention_paged_workspace_bytes(cache: PagedCache, batch: PagedBatch, n_heads: int, window: int = 0, sinks: int = 0) -> int:
-    return int(lib().bitnet_a48_attention_paged_workspace_bytes(cache.cfg_ref, batch.view_ref, n_heads, window, sinks))
+    return _lib.bitnet_a48_attention_paged_workspace_bytes(cache.cfg_ref, batch.view_ref, n_heads, window, sinks)
 
 
 def attention_paged(cache: PagedCache, batch: PagedBatch, q: torch.Tensor, scale: float = 0.0, window: int = 0, sinks: int = 0,
                     out=None, workspace=None, stream=None) -> torch.Tensor:
     """Causal attention of q bf16 [n_tokens, n_heads*head_dim] over the cache; rows may be strided.  Returns bf16."""
+    st = _on_stream(q, stream)
+    if st is None:
+        with _made_current(q, stream):
+            return attention_paged(cache, batch, q, scale, window, sinks, out, workspace)
     heads = q.shape[1] // cache.head_dim
-    qs = _rows(q, batch.n_tokens, heads * cache.head_dim, torch.bfloat16)
-    with _On(q, stream) as st:
-        if out is None:
-            out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-        os_ = _rows(out, batch.n_tokens, q.shape[1], torch.bfloat16)
-        need = attention_paged_workspace_bytes(cache, batch, heads, window, sinks)
-        if workspace is None and need:
+    width = heads * cache.head_dim
+    qs = _rows(q, batch.n_tokens, width, torch.bfloat16)
+    if out is None:
+        out = torch.empty(batch.n_tokens, width, dtype=torch.bfloat16, device=q.device)
+    os_ = _rows(out, batch.n_tokens, width, torch.bfloat16)
+    wp, given = None, 0
+    if workspace is not None:
+        wp, given = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    else:
+        need = _lib.bitnet_a48_attention_paged_workspace_bytes(cache.cfg_ref, batch.view_ref, heads, window, sinks)
+        if need:
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-        given = workspace.numel() * workspace.element_size() if workspace is not None else 0
-        _check(lib().bitnet_a48_attention_paged(cache.cfg_ref, cache.pool.data_ptr(), batch.view_ref, heads, q.data_ptr(), qs, scale,
-                                                window, sinks, out.data_ptr(), os_, _ptr(workspace), given, st), "attention_paged")
+            wp, given = workspace.data_ptr(), need
+    _check(_lib.bitnet_a48_attention_paged(cache.cfg_ref, cache.pool_ptr, batch.view_ref, heads, q.data_ptr(), qs, scale, window, sinks,
+                                           out.data_ptr(), os_, wp, given, st), "attention_paged")
     return out
 
 

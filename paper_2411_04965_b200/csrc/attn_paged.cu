@@ -691,7 +691,8 @@ Plan plan_of(const bitnet_a48_paged_cache& c, const bitnet_a48_paged_batch& b, i
 template <int BITS, int PD, int NT>
 cudaError_t launch_rows(const AttnArgs& a, cudaStream_t st) {
     constexpr size_t SMEM = sizeof(RowsShared<BITS, PD, NT>);
-    const cudaError_t e = cudaFuncSetAttribute(attn_paged_rows_kernel<BITS, PD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM);
+    static bool allowed[64];
+    const cudaError_t e = a48_allow_smem(attn_paged_rows_kernel<BITS, PD, NT>, SMEM, allowed);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(a.l.kv_heads * a.b.n_seqs * a.tiles, a.ranks * a.clusters);

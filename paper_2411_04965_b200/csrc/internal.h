@@ -38,6 +38,19 @@ static inline cudaError_t a48_launch_pdl(void (*kernel)(KArgs...), dim3 grid, di
 }
 #endif
 
+#ifdef __CUDACC__
+// Allows a kernel its dynamic shared memory on the current device; asked of the runtime once per device.
+template <typename... KArgs>
+static inline cudaError_t a48_allow_smem(void (*kernel)(KArgs...), size_t bytes, bool (&done)[64]) {
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess || (device < 64 && done[device])) return e;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess && device < 64) done[device] = true;
+    return e;
+}
+#endif
+
 // Output element type of the contraction kernels for the call in flight on this host thread: 0 = fp32, 1 = bf16
 // (round to nearest even of the fp32 result).  Set by bitnet_a48_linear_bf16 around its dispatch, read by the
 // launchers, which pass it to their kernels as a parameter.
