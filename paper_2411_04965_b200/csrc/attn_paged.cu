@@ -666,11 +666,16 @@ Plan plan_of(const bitnet_a48_paged_cache& c, const bitnet_a48_paged_batch& b, i
     if (b.max_kv < reach) reach = b.max_kv;
     // positions a tile of `span` tokens may see
     auto seen = [&](long long span) { return window > 0 && window + sinks + span < reach ? window + sinks + span : reach; };
-    // One wave of CTAs at four to an SM, as long as every warp of a part has
-    // a pair of blocks.  Up to eight parts join inside a cluster; more only where those leave SMs idle.
+    // Parts of the positions, a power of two, each with a pair of blocks for every warp at least.  As many as fit the SMs at
+    // once (a second wave costs its start again: 8 sequences of 4 tokens, 27.8 us with 512 CTAs on 296 places, 18 with 256);
+    // two where that would be one, which evens out sequences of unlike lengths (64 of 130 .. 8192 positions: 121 us with
+    // one part, 94 with two, 96 with four).  Up to eight join inside a cluster; more only where those leave SMs idle.
     const long long base = (long long)b.n_seqs * c.n_kv_heads * p.tiles, most = up(seen(64), 32 * ROW_WARPS);
-    p.ranks = 1;  // a power of two
-    while (p.ranks < MAX_RANKS && base * p.ranks < 4 * SMS && 2 * p.ranks <= most) p.ranks *= 2;
+    const bool narrow = (c.head_dim + 31) / 32 * 32 <= 64 && c.bits != 3;
+    const long long places = (long long)SMS * (p.nt == 2 ? 2 : c.bits == 4 || narrow ? 4 : 3);
+    p.ranks = 1;
+    while (p.ranks < MAX_RANKS && 2 * p.ranks * base <= places && 2 * p.ranks <= most) p.ranks *= 2;
+    if (p.ranks == 1 && base <= places && most >= 2) p.ranks = 2;
     p.clusters = p.ranks < MAX_RANKS ? 1 : within(2 * SMS / (base * MAX_RANKS), 1, most / MAX_RANKS < 16 ? most / MAX_RANKS : 16);
     // Tile kernel, one CTA per SM: split while the tiles do not fill the SMs, into parts of two tiles or more.
     p.tc_tiles = 0, p.tc_splits = 1;
