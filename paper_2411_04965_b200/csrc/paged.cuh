@@ -91,32 +91,6 @@ __device__ __forceinline__ int page_of(const Layout& l, const Batch& b, int s, i
     const int page = __ldg(b.pages + (size_t)s * b.max_pages + index);
     return page >= 0 && page < l.n_pages ? page : -1;
 }
-
-// Entries e .. e+3 (e a multiple of 4) of a code row, as codes minus their offset.
-__device__ __forceinline__ float4 four_entries(const uint8_t* __restrict__ row, int e, int bits) {
-    unsigned u[4];
-    if (bits == 8) {
-        const unsigned w = __ldg(reinterpret_cast<const unsigned*>(row + e));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = (w >> (8 * i)) & 255u;
-    } else if (bits == 4) {
-        const unsigned w = __ldg(reinterpret_cast<const unsigned short*>(row + e / 2));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = (w >> (4 * i)) & 15u;
-    } else {
-        // the three halves of these 16 entries side by side: entry n at bits 3n
-        const unsigned short* h = reinterpret_cast<const unsigned short*>(row + (e >> 5) * 12) + ((e >> 4) & 1);
-        const unsigned a = __ldg(h), b = __ldg(h + 2), c = __ldg(h + 4);
-        const unsigned long long w = (unsigned long long)(a & 0x7fffu) | ((unsigned long long)(b & 0x7fffu) << 15) |
-                                     ((unsigned long long)(c & 0x7fffu) << 30) |
-                                     ((unsigned long long)((a >> 15) | ((b >> 15) << 1) | ((c >> 15) << 2)) << 45);
-        const unsigned v = (unsigned)(w >> (3 * (e & 15)));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = (v >> (3 * i)) & 7u;
-    }
-    const float off = (float)(1 << (bits - 1));
-    return make_float4((float)u[0] - off, (float)u[1] - off, (float)u[2] - off, (float)u[3] - off);
-}
 #endif
 
 // Token rows of heads: the pointer to four elements, the stride at least the row and a multiple of four elements.

@@ -1,9 +1,9 @@
 // Writing the paged low-bit cache (rotation, quantisation and placement of new tokens in one pass) and reading it back.
 //
 // Both kernels move bytes and little else: the write reads q, k and v once and stores the rotated queries and the codes,
-// the read loads codes and scales and stores the values.  What has to be kept off their way is the float64 arithmetic
-// that makes the codes exact (angles, rotation of the keys, scale and rounding): the angles are taken once per token and
-// block, not per head, and the rotation of the queries, whose result is rounded to bf16, is done in fp32.
+// the read loads codes and scales and stores the values.  What has to be kept off their way is arithmetic: the float64 that
+// makes the codes exact (the angles are taken once per token and block, not per head, and entries in fp32 unless they lie
+// at a rounding border), and divisions by shapes that are not known when this is compiled.
 #include "paged.cuh"
 
 namespace {
@@ -11,63 +11,75 @@ namespace {
 using a48p::Batch;
 using a48p::Layout;
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 8, MAX_TOKENS = 4;
 
-// base^(-i / half) of the rotation pairs, evaluated on the host
+// base^(-i / half) / pi of the rotation pairs, evaluated on the host: half turns per position
 struct Rates {
     double f[64];
 };
 
-template <bool BF16>
-__device__ __forceinline__ float2 load2(const void* row, int e) {
-    if (BF16) {
-        const unsigned u = __ldg(reinterpret_cast<const unsigned*>(reinterpret_cast<const uint16_t*>(row) + e));
-        return make_float2(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+// W consecutive entries of a row
+template <bool BF16, int W>
+__device__ __forceinline__ void load_entries(const void* row, int e, float (&x)[W]) {
+    if constexpr (BF16) {
+        uint32_t u[W / 2];
+        if constexpr (W == 4) {
+            const uint2 v = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(row) + e));
+            u[0] = v.x, u[1] = v.y;
+        } else {
+            u[0] = __ldg(reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(row) + e));
+        }
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) x[2 * i] = __uint_as_float(u[i] << 16), x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    } else if constexpr (W == 4) {
+        const float4 v = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(row) + e));
+        x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+    } else {
+        const float2 v = __ldg(reinterpret_cast<const float2*>(static_cast<const float*>(row) + e));
+        x[0] = v.x, x[1] = v.y;
     }
-    return __ldg(reinterpret_cast<const float2*>(reinterpret_cast<const float*>(row) + e));
 }
 
-// One warp quantises one head vector, four entries per lane (zero past the head), with Eq. 3's arithmetic in float64:
-// gamma = max|x|, u = RoundClip(L / (gamma + eps) x, -(L+1), L) + L + 1.
-__device__ __forceinline__ void quantise(const double (&x)[4], int bits, double eps, int (&u)[4], float& scale) {
-    double gamma = fmax(fmax(fabs(x[0]), fabs(x[1])), fmax(fabs(x[2]), fabs(x[3])));
+// W entries from e on, to a row of bf16 or of codes (the low byte of each word; the rest of it may hold anything)
+template <int W>
+__device__ __forceinline__ void store_bf16(__nv_bfloat16* row, int e, const float (&x)[W]) {
+    uint32_t u[W / 2];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) gamma = fmax(gamma, __shfl_xor_sync(0xffffffffu, gamma, o));
-    const int L = (1 << (bits - 1)) - 1;
-    const double s = (double)L / (gamma + eps);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int q = __double2int_rn(s * x[i]);
-        u[i] = min(max(q, -(L + 1)), L) + L + 1;
+    for (int i = 0; i < W / 2; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+        u[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
-    scale = (float)(gamma / (double)L);
+    if constexpr (W == 4) *reinterpret_cast<uint2*>(row + e) = make_uint2(u[0], u[1]);
+    else *reinterpret_cast<uint32_t*>(row + e) = u[0];
 }
-
-// The entries of a row, one byte each in shared memory, packed into words by the lanes that have one.
-__device__ __forceinline__ void store_row(uint8_t* __restrict__ dst, const uint8_t* u, int padded, int bits, int lane) {
-    unsigned* out = reinterpret_cast<unsigned*>(dst);
+template <int W>
+__device__ __forceinline__ void store_codes(uint8_t* row, int e, int bits, const uint32_t (&u)[W]) {
+    uint32_t w = __byte_perm(u[0], u[1], 0x0040);  // entries in bytes 0, 1
+    if constexpr (W == 4) w = __byte_perm(w, __byte_perm(u[2], u[3], 0x0040), 0x5410);
     if (bits == 8) {
-        if (4 * lane < padded) out[lane] = reinterpret_cast<const unsigned*>(u)[lane];
-    } else if (bits == 4) {
-        if (8 * lane < padded) {
-            const uint2 b = reinterpret_cast<const uint2*>(u)[lane];  // byte i: entry i; fold the pairs of bytes
-            const unsigned lo = (b.x | (b.x >> 4)) & 0x00ff00ffu, hi = (b.y | (b.y >> 4)) & 0x00ff00ffu;
-            out[lane] = ((lo | (lo >> 8)) & 0xffffu) | ((hi | (hi >> 8)) << 16);
-        }
-    } else if (lane < 3 * padded / 32) {  // three words per 32 entries
-        const int granule = lane / 3, j = lane % 3;
-        const uint8_t* g = u + 32 * granule;
-        unsigned w = 0;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            unsigned v = 0;
-#pragma unroll
-            for (int e = 0; e < 5; ++e) v |= (unsigned)g[16 * half + 5 * j + e] << (3 * e);
-            v |= ((g[16 * half + 15] >> j) & 1u) << 15;
-            w |= v << (16 * half);
-        }
-        out[lane] = w;
+        if constexpr (W == 4) *reinterpret_cast<uint32_t*>(row + e) = w;
+        else *reinterpret_cast<uint16_t*>(row + e) = (uint16_t)w;
+    } else {  // fold the pairs of bytes
+        w = (w | (w >> 4)) & 0x00ff00ffu;
+        if constexpr (W == 4) *reinterpret_cast<uint16_t*>(row + e / 2) = (uint16_t)(w | (w >> 8));
+        else row[e / 2] = (uint8_t)w;
     }
+}
+
+// Word `at` of a 3-bit row from its entries, one byte each.
+__device__ __forceinline__ uint32_t word_of_triples(const uint8_t* u, int at) {
+    const int j = at % 3;
+    const uint8_t* g = u + 32 * (at / 3);
+    uint32_t w = 0;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        uint32_t v = 0;
+#pragma unroll
+        for (int e = 0; e < 5; ++e) v |= (uint32_t)g[16 * half + 5 * j + e] << (3 * e);
+        v |= ((g[16 * half + 15] >> j) & 1u) << 15;
+        w |= v << (16 * half);
+    }
+    return w;
 }
 
 struct WriteArgs {
@@ -77,98 +89,226 @@ struct WriteArgs {
     const void *q, *k, *v;
     long long q_stride, k_stride, v_stride, out_stride;
     __nv_bfloat16* q_out;
-    int q_heads, rotate;
+    int q_heads, rotate, tokens;  // tokens: of a block
     double eps;
     Rates rates;
 };
 
-// grid (token, slice of heads).  A warp takes one query head (rotate, round to bf16) or one key/value head (rotate the
-// key, quantise both, store) at a time.  Lane l owns entries 2l, 2l+1 and half + 2l, half + 2l + 1: rotation partners
-// meet in one lane.
-template <bool BF16>
-__global__ void __launch_bounds__(32 * kWarps) paged_write_kernel(const __grid_constant__ WriteArgs a) {
-    __shared__ double2 turn[64];  // cos, sin of the token's position
-    __shared__ alignas(8) uint8_t codes[kWarps][2][128];
+// grid (tokens / `tokens`, slice of heads).  A block's warps are dealt out to its tokens; a group of G lanes takes one head
+// vector at a time, of the queries (rotate, round to bf16), the keys (rotate, quantise) or the values (quantise); lane l of
+// it has entries W l .. W l + W - 1 and their rotation partners.
+//
+// The codes are those of float64 arithmetic without float64 for every entry: rotation and scale are taken in fp32, whose
+// errors move an entry's multiple of the step by less than L 2^-19 (of L: the rotation 6 2^-24 of gamma, the scale
+// 10 2^-24); only where that multiple lies so near a rounding border (one entry in 4000 at 8 bits, one in 70000 at 4) are
+// the lane's entries taken again in float64.  The scale itself comes from gamma in float64: of the lanes whose entries can be
+// the largest.
+template <bool BF16, int W, int G>
+__global__ void __launch_bounds__(32 * kWarps, 4) paged_write_kernel(const __grid_constant__ WriteArgs a) {
+    constexpr int PER = 32 / G;  // head vectors that a warp takes at a time
+    __shared__ double2 turn_of[MAX_TOKENS][64];  // cos, sin of the tokens' positions
+    __shared__ float2 turn_f_of[MAX_TOKENS][64];
+    __shared__ int positions[MAX_TOKENS];
+    __shared__ alignas(8) uint8_t row_codes[kWarps][32][8];  // for 3-bit rows; a group's lanes have room for its padded row
     a48_pdl_prologue();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, token = blockIdx.x;
-    const int s = a48p::sequence_of(a.b, token, lane);
-    if (s < 0) return;  // behind the last sequence
-    const int first = __ldg(a.b.q_start + s), end = __ldg(a.b.q_start + s + 1);
-    const int pos = __ldg(a.b.kv_len + s) - (end - first) + (token - first);
-    const int half = a.l.hd / 2;
+    const int lane = threadIdx.x & 31, warps = kWarps / a.tokens, of = (threadIdx.x >> 5) / warps, token = blockIdx.x * a.tokens + of;
+    const int s = token < a.b.n_tokens ? a48p::sequence_of(a.b, token, lane) : -1;  // (none behind the last sequence)
+    int pos = 0;
+    if (s >= 0) {
+        const int first = __ldg(a.b.q_start + s), end = __ldg(a.b.q_start + s + 1);
+        pos = __ldg(a.b.kv_len + s) - (end - first) + (token - first);
+    }
+    const int half = a.l.hd / 2, l = lane & (G - 1), e = W * l, row_bytes = a.l.hd * (BF16 ? 2 : 4);
+    const bool mine = e < half;
     if (a.rotate) {
-        for (int i = threadIdx.x; i < half; i += blockDim.x) {
+        if (lane == 0) positions[of] = pos;  // (the same from each of the token's warps)
+        __syncthreads();
+        for (int i = threadIdx.x; i < 64 * a.tokens; i += blockDim.x) {
+            if ((i & 63) >= half) continue;
             double sn, cn;
-            sincos((double)pos * a.rates.f[i], &sn, &cn);
-            turn[i] = make_double2(cn, sn);
+            sincospi((double)positions[i >> 6] * a.rates.f[i & 63], &sn, &cn);
+            turn_of[i >> 6][i & 63] = make_double2(cn, sn);
+            turn_f_of[i >> 6][i & 63] = make_float2((float)cn, (float)sn);
         }
         __syncthreads();
     }
-    const int page = a48p::page_of(a.l, a.b, s, pos), slot = pos & (a.l.page - 1);
-    const int e = 2 * lane;
-    const bool mine = e < half;
-    double2 t0 = make_double2(1.0, 0.0), t1 = t0;
-    if (a.rotate && mine) t0 = turn[e], t1 = turn[e + 1];
-    const int items = a.q_heads + a.l.kv_heads;
-    for (int item = blockIdx.y * kWarps + warp; item < items; item += gridDim.y * kWarps) {
-        if (item < a.q_heads) {
-            const size_t elem = BF16 ? 2 : 4;
-            const char* row = static_cast<const char*>(a.q) + ((size_t)token * a.q_stride + (size_t)item * a.l.hd) * elem;
-            float2 lo = make_float2(0.f, 0.f), hi = lo;
-            if (mine) lo = load2<BF16>(row, e), hi = load2<BF16>(row, half + e);
-            __syncwarp();  // q_out may be q: every lane has read before any lane writes
-            if (mine) {
-                const float c0 = (float)t0.x, s0 = (float)t0.y, c1 = (float)t1.x, s1 = (float)t1.y;
-                __nv_bfloat16* out = a.q_out + (size_t)token * a.out_stride + (size_t)item * a.l.hd;
-                *reinterpret_cast<__nv_bfloat162*>(out + e) = __floats2bfloat162_rn(lo.x * c0 - hi.x * s0, lo.y * c1 - hi.y * s1);
-                *reinterpret_cast<__nv_bfloat162*>(out + half + e) = __floats2bfloat162_rn(hi.x * c0 + lo.x * s0, hi.y * c1 + lo.y * s1);
-            }
-            continue;
-        }
-        if (page < 0) continue;  // no page for this position: nothing is stored
-        const int head = item - a.q_heads;
-        uint8_t* chunk = a.pool + a48p::chunk_at(a.l, page, head);
-        const size_t elem = BF16 ? 2 : 4;
-        const char* krow = static_cast<const char*>(a.k) + ((size_t)token * a.k_stride + (size_t)head * a.l.hd) * elem;
-        const char* vrow = static_cast<const char*>(a.v) + ((size_t)token * a.v_stride + (size_t)head * a.l.hd) * elem;
-        float2 f[2][2] = {};
-        if (mine) {
-            f[0][0] = load2<BF16>(krow, e), f[0][1] = load2<BF16>(krow, half + e);
-            f[1][0] = load2<BF16>(vrow, e), f[1][1] = load2<BF16>(vrow, half + e);
-        }
-        const bool bos = a.l.bits == 3 && pos == 0;  // the bos heads keep 4 bits
-        const int bits = bos ? 4 : a.l.bits;
+    if (s < 0) return;
+    const double2* turn = turn_of[of];
+    float c[W], sn[W];
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const double l0 = f[n][0].x, l1 = f[n][0].y, h0 = f[n][1].x, h1 = f[n][1].y;
-            double x[4] = {l0, l1, h0, h1};
-            if (n == 0 && a.rotate) {
-                x[0] = l0 * t0.x - h0 * t0.y;
-                x[1] = l1 * t1.x - h1 * t1.y;
-                x[2] = h0 * t0.x + l0 * t0.y;
-                x[3] = h1 * t1.x + l1 * t1.y;
+    for (int i = 0; i < W; ++i) {
+        const float2 t = a.rotate && mine ? turn_f_of[of][e + i] : make_float2(1.f, 0.f);
+        c[i] = t.x, sn[i] = t.y;
+    }
+    const int begin = (blockIdx.y * warps + (threadIdx.x >> 5) % warps) * PER + lane / G, stride = gridDim.y * warps * PER;
+    // ---- queries
+    {
+        const char* rows = static_cast<const char*>(a.q) + (size_t)token * a.q_stride * (BF16 ? 2 : 4);
+        __nv_bfloat16* out = a.q_out + (size_t)token * a.out_stride;
+#pragma unroll 2
+        for (int head = begin; head - lane / G < a.q_heads; head += stride) {  // (the same for the warp)
+            const bool there = mine && head < a.q_heads;
+            float lo[W] = {}, hi[W] = {};
+            if (there) {
+                load_entries<BF16, W>(rows + (size_t)head * row_bytes, e, lo);
+                load_entries<BF16, W>(rows + (size_t)head * row_bytes, half + e, hi);
             }
-            int u[4];
-            float scale;
-            quantise(x, bits, a.eps, u, scale);
-            uint8_t* buf = codes[warp][n];
-            if (mine) {
-                *reinterpret_cast<uchar2*>(buf + e) = make_uchar2(u[0], u[1]);
-                *reinterpret_cast<uchar2*>(buf + half + e) = make_uchar2(u[2], u[3]);
+            float x[2][W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) x[0][i] = lo[i] * c[i] - hi[i] * sn[i], x[1][i] = hi[i] * c[i] + lo[i] * sn[i];
+            __syncwarp();  // q_out may be q: every lane has read before any lane writes
+            if (there) {
+                store_bf16<W>(out + head * a.l.hd, e, x[0]);
+                store_bf16<W>(out + head * a.l.hd, half + e, x[1]);
             }
-            if (a.l.hd + lane < a.l.padded) buf[a.l.hd + lane] = (uint8_t)(1 << (bits - 1));
-            __syncwarp();
-            uint8_t* dst = bos ? chunk + a.l.bos + n * (a.l.padded / 2) : chunk + (n == 0 ? 0 : a.l.v_codes) + slot * a.l.row;
-            store_row(dst, buf, a.l.padded, bits, lane);
-            if (lane == 0) reinterpret_cast<float*>(chunk + (n == 0 ? a.l.k_scales : a.l.v_scales))[slot] = scale;
         }
-        __syncwarp();  // the row buffers are free again
+    }
+    // ---- keys and values: row r is head r / 2's key or value
+    const int page = a48p::page_of(a.l, a.b, s, pos), slot = pos & (a.l.page - 1);
+    if (page < 0) return;  // no page for this position: nothing is stored
+    const char* k_rows = static_cast<const char*>(a.k) + (size_t)token * a.k_stride * (BF16 ? 2 : 4);
+    const char* v_rows = static_cast<const char*>(a.v) + (size_t)token * a.v_stride * (BF16 ? 2 : 4);
+    uint8_t* chunks = a.pool + a48p::chunk_at(a.l, page, 0);
+    const bool bos = a.l.bits == 3 && pos == 0;  // the bos heads keep 4 bits
+    const int bits = bos ? 4 : a.l.bits, L = (1 << (bits - 1)) - 1;
+    const float eps = (float)a.eps, border = 0.5f - (float)L * 0x1p-19f;
+    // x step + magic: the nearest multiple's code (q + L + 1) in the low byte of the sum, ties to even
+    const float magic = 12582912.f + (float)(L + 1);
+    for (int r = begin; r - lane / G < 2 * a.l.kv_heads; r += stride) {
+        const int which = r & 1, head = r >> 1;
+        const bool there = mine && head < a.l.kv_heads, turned = a.rotate && !which;
+        float lo[W] = {}, hi[W] = {}, x[2][W];
+        if (there) {
+            const char* row = (which ? v_rows : k_rows) + (size_t)head * row_bytes;
+            load_entries<BF16, W>(row, e, lo);
+            load_entries<BF16, W>(row, half + e, hi);
+        }
+        // an entry in float64
+        auto exact = [&](int h, int i) {
+            if (!turned) return (double)(h ? hi[i] : lo[i]);
+            const double2 t = turn[e + i];
+            return h == 0 ? (double)lo[i] * t.x - (double)hi[i] * t.y : (double)hi[i] * t.x + (double)lo[i] * t.y;
+        };
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            x[0][i] = turned ? lo[i] * c[i] - hi[i] * sn[i] : lo[i];
+            x[1][i] = turned ? hi[i] * c[i] + lo[i] * sn[i] : hi[i];
+            top = fmaxf(top, fmaxf(fabsf(x[0][i]), fabsf(x[1][i])));
+        }
+        float gamma_f = top;
+#pragma unroll
+        for (int o = G / 2; o > 0; o >>= 1) gamma_f = fmaxf(gamma_f, __shfl_xor_sync(0xffffffffu, gamma_f, o));
+        double gamma = turned ? 0.0 : (double)gamma_f;
+        if (turned && there && top >= gamma_f * (1.f - 0x1p-20f)) {
+#pragma unroll
+            for (int i = 0; i < W; ++i) gamma = fmax(gamma, fmax(fabs(exact(0, i)), fabs(exact(1, i))));
+        }
+#pragma unroll
+        for (int o = G / 2; o > 0; o >>= 1) gamma = fmax(gamma, __shfl_xor_sync(0xffffffffu, gamma, o));
+        const float step = __fdividef((float)L, gamma_f + eps);
+        uint32_t u[2][W];
+        float worst = 0.f;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                const float sum = fmaf(x[h][i], step, magic);
+                worst = fmaxf(worst, fabsf(fmaf(x[h][i], step, magic - sum)));
+                u[h][i] = __float_as_uint(sum);
+            }
+        // (out of the bounds' reach: numbers so small or so large, or none)
+        if (there && (worst > border || !(gamma_f > 0x1p-100f && gamma_f < 0x1p100f))) {
+            const double multiple = (double)L / (gamma + a.eps);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < W; ++i) u[h][i] = (uint32_t)(min(max(__double2int_rn(multiple * exact(h, i)), -(L + 1)), L) + L + 1);
+        }
+        uint8_t* chunk = chunks + (size_t)min(head, a.l.kv_heads - 1) * a.l.chunk;
+        uint8_t* dst = bos ? chunk + a.l.bos + which * (a.l.padded / 2) : chunk + which * a.l.v_codes + slot * a.l.row;
+        const uint32_t zero = 1u << (bits - 1);
+        const int pad = head < a.l.kv_heads ? a.l.padded - a.l.hd : 0;  // entries past the head hold the code of 0
+        if (bits != 3) {
+            if (there) {
+                store_codes<W>(dst, e, bits, u[0]);
+                store_codes<W>(dst, half + e, bits, u[1]);
+            }
+            uint32_t z[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) z[i] = zero;
+            for (int i = W * l; i < pad; i += W * G) store_codes<W>(dst, a.l.hd + i, bits, z);
+        } else {
+            uint8_t* buf = &row_codes[threadIdx.x >> 5][lane & ~(G - 1)][0];
+            if (there) {
+#pragma unroll
+                for (int i = 0; i < W; i += 2) {
+                    *reinterpret_cast<uint16_t*>(buf + e + i) = (uint16_t)__byte_perm(u[0][i], u[0][i + 1], 0x0040);
+                    *reinterpret_cast<uint16_t*>(buf + half + e + i) = (uint16_t)__byte_perm(u[1][i], u[1][i + 1], 0x0040);
+                }
+            }
+            for (int i = l; i < pad; i += G) buf[a.l.hd + i] = (uint8_t)zero;
+            __syncwarp();
+            if (head < a.l.kv_heads)
+                for (int i = l; i < 3 * a.l.padded / 32; i += G) reinterpret_cast<uint32_t*>(dst)[i] = word_of_triples(buf, i);
+            __syncwarp();  // the bytes are free again
+        }
+        if (l == 0 && head < a.l.kv_heads) {
+            const float scale = turned ? (float)(gamma * (1.0 / L)) : __fdiv_rn(gamma_f, (float)L);
+            reinterpret_cast<float*>(chunk + (which ? a.l.v_scales : a.l.k_scales))[slot] = scale;
+        }
     }
 }
 
-// One warp per (token, slice of its keys and values), four entries per thread and step: the stores of a warp are one run
-// of the output row.  A position without a page reads as zero.
 template <bool BF16>
+cudaError_t launch_write(WriteArgs& a, cudaStream_t st) {
+    const int half = a.l.hd / 2, wide = a.l.hd % 8 == 0 ? 4 : 2;
+    const int group = wide == 4 ? (half <= 32 ? 8 : 16) : (half <= 32 ? 16 : 32);  // (four lanes at least have room for 32 entries)
+    // Few tokens: their heads are spread over blocks; many: a block takes four tokens, whose angles take as long as one's.
+    a.tokens = a.b.n_tokens >= 8 * 148 ? MAX_TOKENS : 1;
+    const int per = kWarps / a.tokens * (32 / group), most = a.q_heads > 2 * a.l.kv_heads ? a.q_heads : 2 * a.l.kv_heads;
+    const int rounds = (most + per - 1) / per, blocks = (a.b.n_tokens + a.tokens - 1) / a.tokens;
+    int slices = a.tokens > 1 ? 1 : (8 * 148 + blocks - 1) / blocks;
+    slices = slices < rounds ? slices : rounds;
+    auto kernel = wide == 4 ? (group == 8 ? paged_write_kernel<BF16, 4, 8> : paged_write_kernel<BF16, 4, 16>)
+                            : (group == 16 ? paged_write_kernel<BF16, 2, 16> : paged_write_kernel<BF16, 2, 32>);
+    return a48_launch_pdl(kernel, dim3(blocks, slices), dim3(32 * kWarps), 0, st, a);
+}
+
+// E entries from e on of a code row, as codes minus their offset.  (An integer below 2^23 or-ed into 2^23's pattern is the
+// float 2^23 plus it.)
+template <int E>
+__device__ __forceinline__ void read_codes(const uint8_t* __restrict__ row, int e, int bits, float (&x)[E]) {
+    const float off = 8388608.f + (float)(1 << (bits - 1));
+    auto entry = [&](uint32_t field) { return __uint_as_float(0x4b000000u | field) - off; };
+    if (bits == 8) {
+#pragma unroll
+        for (int i = 0; i < E; i += 4) {
+            const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(row + e + i));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[i + j] = __uint_as_float(__byte_perm(w, 0x4b000000u, 0x7440 + j)) - off;  // bytes w[j] 0 0 4b
+        }
+    } else if (bits == 4) {
+        const uint32_t w = E == 8 ? __ldg(reinterpret_cast<const uint32_t*>(row + e / 2)) : __ldg(reinterpret_cast<const unsigned short*>(row + e / 2));
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] = entry((w >> (4 * i)) & 15u);
+    } else {
+        // entry n of 16 at bits 3n of three halves side by side, 15 bits of each; the last one's bits on top of them
+        const unsigned short* h = reinterpret_cast<const unsigned short*>(row + (e >> 5) * 12) + ((e >> 4) & 1);
+        const uint32_t a = __ldg(h), b = __ldg(h + 2), c = __ldg(h + 4);
+        const uint32_t lo = (a & 0x7fffu) | (b << 15);                                                   // entries 0 .. 9
+        const uint32_t hi = (c & 0x7fffu) | ((a >> 15) << 15) | ((b >> 15) << 16) | ((c >> 15) << 17);  // 10 .. 15
+        const int n = e & 15;
+        const uint32_t v = n < 8 ? lo >> (3 * n) : n == 8 ? ((lo >> 24) & 63u) | (hi << 6) : hi >> 6;
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] = entry((v >> (3 * i)) & 7u);
+    }
+}
+
+// One warp per (token, slice of its heads); LANES lanes share a head vector, E entries each, so that a store is 16 bytes
+// (8 where the head dimension does not divide by 8).  Items are (head, keys or values); a position without a page reads as
+// zero.
+template <bool BF16, int E, int BITS, int LANES>
 __global__ void __launch_bounds__(32 * kWarps) paged_read_kernel(const Layout l, const Batch b, const uint8_t* __restrict__ pool,
                                                                  void* __restrict__ k_out, void* __restrict__ v_out) {
     a48_pdl_prologue();
@@ -179,30 +319,61 @@ __global__ void __launch_bounds__(32 * kWarps) paged_read_kernel(const Layout l,
     const int first = __ldg(b.q_start + s), end = __ldg(b.q_start + s + 1);
     const int pos = __ldg(b.kv_len + s) - (end - first) + (token - first);
     const int page = a48p::page_of(l, b, s, pos), slot = pos & (l.page - 1);
-    const int quads = l.hd / 4, per_row = l.kv_heads * quads;
-    const bool bos = l.bits == 3 && pos == 0;
+    constexpr int PER = 32 / LANES;  // head vectors that a warp takes at a time
+    const int e = E * (lane & (LANES - 1));
+    if (e >= l.hd) return;
+    const bool bos = BITS == 3 && pos == 0;
+    const uint8_t* chunks = pool + a48p::chunk_at(l, max(page, 0), 0);
+    const size_t out_row = (size_t)token * l.kv_heads * l.hd + e;
+    const int codes[2] = {bos ? l.bos : slot * l.row, bos ? l.bos + l.padded / 2 : l.v_codes + slot * l.row};
+    const int scales[2] = {l.k_scales + 4 * slot, l.v_scales + 4 * slot};
+    const int chunk_bytes = l.chunk, kv_heads = l.kv_heads, hd = l.hd;
 #pragma unroll 4
-    for (int i = blockIdx.y * 32 + lane; i < 2 * per_row; i += gridDim.y * 32) {
-        const int which = i >= per_row, at = which ? i - per_row : i;
-        const int head = at / quads, e = 4 * (at % quads);
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = blockIdx.y * PER + lane / LANES; i < 2 * kv_heads; i += gridDim.y * PER) {
+        const int head = i >> 1, which = i & 1;
+        float x[E];
+#pragma unroll
+        for (int j = 0; j < E; ++j) x[j] = 0.f;
         if (page >= 0) {
-            const uint8_t* chunk = pool + a48p::chunk_at(l, page, head);
-            const float scale = __ldg(reinterpret_cast<const float*>(chunk + (which ? l.v_scales : l.k_scales)) + slot);
-            x = bos ? a48p::four_entries(chunk + l.bos + which * (l.padded / 2), e, 4)
-                    : a48p::four_entries(chunk + (which ? l.v_codes : 0) + slot * l.row, e, l.bits);
-            x.x *= scale, x.y *= scale, x.z *= scale, x.w *= scale;
+            const uint8_t* chunk = chunks + (size_t)head * chunk_bytes;
+            const float scale = __ldg(reinterpret_cast<const float*>(chunk + (which ? scales[1] : scales[0])));
+            const uint8_t* row = chunk + (which ? codes[1] : codes[0]);
+            if (BITS == 3 && bos) read_codes<E>(row, e, 4, x);
+            else read_codes<E>(row, e, BITS, x);
+#pragma unroll
+            for (int j = 0; j < E; ++j) x[j] *= scale;
         }
-        const size_t o = (size_t)token * per_row + at;
         void* out = which ? v_out : k_out;
-        if (BF16) {
-            const __nv_bfloat162 lo = __floats2bfloat162_rn(x.x, x.y), hi = __floats2bfloat162_rn(x.z, x.w);
-            reinterpret_cast<uint2*>(out)[o] =
-                make_uint2(*reinterpret_cast<const unsigned*>(&lo), *reinterpret_cast<const unsigned*>(&hi));
+        const size_t at = out_row + (size_t)head * hd;
+        if constexpr (BF16) {
+            uint32_t w[E / 2];
+#pragma unroll
+            for (int j = 0; j < E / 2; ++j) {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
+                w[j] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            if constexpr (E == 8) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+            else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = make_uint2(w[0], w[1]);
         } else {
-            reinterpret_cast<float4*>(out)[o] = x;
+            *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(x[0], x[1], x[2], x[3]);
         }
     }
+}
+
+template <bool BF16, int E, int LANES>
+cudaError_t launch_read(const Layout& l, const Batch& b, const uint8_t* pool, void* k_out, void* v_out, cudaStream_t st) {
+    const int steps = (2 * l.kv_heads + 32 / LANES - 1) / (32 / LANES);  // of a warp over one token
+    int slices = (8192 + b.n_tokens - 1) / b.n_tokens;
+    slices = slices < steps ? slices : steps;
+    const dim3 grid((b.n_tokens + kWarps - 1) / kWarps, slices);
+    auto kernel = l.bits == 8 ? paged_read_kernel<BF16, E, 8, LANES> : l.bits == 4 ? paged_read_kernel<BF16, E, 4, LANES> : paged_read_kernel<BF16, E, 3, LANES>;
+    return a48_launch_pdl(kernel, grid, dim3(32 * kWarps), 0, st, l, b, pool, k_out, v_out);
+}
+template <bool BF16, int E>
+cudaError_t launch_read(const Layout& l, const Batch& b, const uint8_t* pool, void* k_out, void* v_out, cudaStream_t st) {
+    return l.hd <= 8 * E    ? launch_read<BF16, E, 8>(l, b, pool, k_out, v_out, st)
+           : l.hd <= 16 * E ? launch_read<BF16, E, 16>(l, b, pool, k_out, v_out, st)
+                            : launch_read<BF16, E, 32>(l, b, pool, k_out, v_out, st);
 }
 
 // Rotation rates for a base and head dimension; the last table of this host thread is kept, decode loops ask for one.
@@ -211,7 +382,7 @@ const Rates& rates_of(float base, int half) {
     thread_local float last_base = 0.f;
     thread_local int last_half = 0;
     if (base != last_base || half != last_half) {
-        for (int i = 0; i < half; ++i) r.f[i] = pow((double)base, -(double)i / (double)half);
+        for (int i = 0; i < half; ++i) r.f[i] = pow((double)base, -(double)i / (double)half) * 0.318309886183790671538;  // 1 / pi
         last_base = base;
         last_half = half;
     }
@@ -258,13 +429,7 @@ bitnet_a48_status bitnet_a48_paged_write(const bitnet_a48_paged_cache* cache, vo
     a.rotate = rope_base > 0.f;
     a.eps = (double)eps;
     if (a.rotate) a.rates = rates_of(rope_base, cache->head_dim / 2);
-    // Few tokens: their heads are spread over blocks, one head per warp; many: a block keeps its token's angles.
-    const int items = a.q_heads + a.l.kv_heads, rounds = (items + kWarps - 1) / kWarps;
-    int slices = (2048 + batch->n_tokens - 1) / batch->n_tokens;
-    slices = slices < rounds ? slices : rounds;
-    const dim3 grid(batch->n_tokens, slices);
-    auto kernel = x_bf16 ? paged_write_kernel<true> : paged_write_kernel<false>;
-    A48_CUDA_TRY(a48_launch_pdl(kernel, grid, dim3(32 * kWarps), 0, (cudaStream_t)stream, a));
+    A48_CUDA_TRY(x_bf16 ? launch_write<true>(a, (cudaStream_t)stream) : launch_write<false>(a, (cudaStream_t)stream));
     return BITNET_A48_OK;
 }
 
@@ -276,13 +441,13 @@ bitnet_a48_status bitnet_a48_paged_read(const bitnet_a48_paged_cache* cache, con
     if (!a48_aligned16(k_out_dev) || !a48_aligned16(v_out_dev)) return BITNET_A48_ERR_ALIGNMENT;
     if (!a48_have_device()) return BITNET_A48_ERR_CUDA;
     const Layout l = a48p::layout_of(*cache);
-    const int steps = (2 * l.kv_heads * (l.hd / 4) + 31) / 32;  // of a warp over one token
-    int slices = (8192 + batch->n_tokens - 1) / batch->n_tokens;
-    slices = slices < steps ? slices : steps;
-    const dim3 grid((batch->n_tokens + kWarps - 1) / kWarps, slices);
-    auto kernel = y_bf16 ? paged_read_kernel<true> : paged_read_kernel<false>;
-    A48_CUDA_TRY(a48_launch_pdl(kernel, grid, dim3(32 * kWarps), 0, (cudaStream_t)stream, l, a48p::batch_of(*batch),
-                                static_cast<const uint8_t*>(pool_dev), k_out_dev, v_out_dev));
+    const Batch b = a48p::batch_of(*batch);
+    const uint8_t* pool = static_cast<const uint8_t*>(pool_dev);
+    const cudaStream_t cu = (cudaStream_t)stream;
+    const cudaError_t e = !y_bf16 ? launch_read<false, 4>(l, b, pool, k_out_dev, v_out_dev, cu)
+                          : l.hd % 8 == 0 ? launch_read<true, 8>(l, b, pool, k_out_dev, v_out_dev, cu)
+                                          : launch_read<true, 4>(l, b, pool, k_out_dev, v_out_dev, cu);
+    A48_CUDA_TRY(e);
     return BITNET_A48_OK;
 }
 
