@@ -11,34 +11,38 @@ namespace {
 using a48p::Batch;
 using a48p::Layout;
 
-constexpr int kWarps = 8, MAX_TOKENS = 4;
+constexpr int kWarps = 8, MAX_TOKENS = 4, BATCH = 4, READ_TOKENS = 16;
 
 // base^(-i / half) / pi of the rotation pairs, evaluated on the host: half turns per position
 struct Rates {
     double f[64];
 };
 
-// W consecutive entries of a row
+// W consecutive entries of a row, as they lie in memory
 template <bool BF16, int W>
-__device__ __forceinline__ void load_entries(const void* row, int e, float (&x)[W]) {
-    if constexpr (BF16) {
-        uint32_t u[W / 2];
-        if constexpr (W == 4) {
-            const uint2 v = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(row) + e));
+struct Raw {
+    static constexpr int N = BF16 ? W / 2 : W;
+    uint32_t u[N];
+    __device__ void load(const void* row, int e) {
+        const uint32_t* p = reinterpret_cast<const uint32_t*>(static_cast<const char*>(row) + e * (BF16 ? 2 : 4));
+        if constexpr (N == 4) {
+            const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
+            u[0] = v.x, u[1] = v.y, u[2] = v.z, u[3] = v.w;
+        } else if constexpr (N == 2) {
+            const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
             u[0] = v.x, u[1] = v.y;
         } else {
-            u[0] = __ldg(reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(row) + e));
+            u[0] = __ldg(p);
         }
-#pragma unroll
-        for (int i = 0; i < W / 2; ++i) x[2 * i] = __uint_as_float(u[i] << 16), x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-    } else if constexpr (W == 4) {
-        const float4 v = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(row) + e));
-        x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
-    } else {
-        const float2 v = __ldg(reinterpret_cast<const float2*>(static_cast<const float*>(row) + e));
-        x[0] = v.x, x[1] = v.y;
     }
-}
+    __device__ void clear() {
+#pragma unroll
+        for (int i = 0; i < N; ++i) u[i] = 0;
+    }
+    __device__ float operator[](int i) const {
+        return __uint_as_float(!BF16 ? u[i] : i & 1 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
+    }
+};
 
 // W entries from e on, to a row of bf16 or of codes (the low byte of each word; the rest of it may hold anything)
 template <int W>
@@ -120,6 +124,21 @@ __global__ void __launch_bounds__(32 * kWarps, 4) paged_write_kernel(const __gri
     }
     const int half = a.l.hd / 2, l = lane & (G - 1), e = W * l, row_bytes = a.l.hd * (BF16 ? 2 : 4);
     const bool mine = e < half;
+    const int page = s >= 0 ? a48p::page_of(a.l, a.b, s, pos) : -1, slot = pos & (a.l.page - 1);
+    const int begin = (blockIdx.y * warps + (threadIdx.x >> 5) % warps) * PER + lane / G, stride = gridDim.y * warps * PER;
+    // ---- queries, BATCH of a warp's at a time: the first ones under way while the angles are taken
+    const char* q_rows = static_cast<const char*>(a.q) + (size_t)token * a.q_stride * (BF16 ? 2 : 4);
+    Raw<BF16, W> q[BATCH][2];
+    auto load_queries = [&](int head) {
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k)
+            if (s >= 0 && mine && head + k * stride < a.q_heads) {
+                const char* row = q_rows + (size_t)(head + k * stride) * row_bytes;
+                q[k][0].load(row, e);
+                q[k][1].load(row, half + e);
+            }
+    };
+    load_queries(begin);
     if (a.rotate) {
         if (lane == 0) positions[of] = pos;  // (the same from each of the token's warps)
         __syncthreads();
@@ -140,31 +159,24 @@ __global__ void __launch_bounds__(32 * kWarps, 4) paged_write_kernel(const __gri
         const float2 t = a.rotate && mine ? turn_f_of[of][e + i] : make_float2(1.f, 0.f);
         c[i] = t.x, sn[i] = t.y;
     }
-    const int begin = (blockIdx.y * warps + (threadIdx.x >> 5) % warps) * PER + lane / G, stride = gridDim.y * warps * PER;
-    // ---- queries
-    {
-        const char* rows = static_cast<const char*>(a.q) + (size_t)token * a.q_stride * (BF16 ? 2 : 4);
-        __nv_bfloat16* out = a.q_out + (size_t)token * a.out_stride;
-#pragma unroll 2
-        for (int head = begin; head - lane / G < a.q_heads; head += stride) {  // (the same for the warp)
-            const bool there = mine && head < a.q_heads;
-            float lo[W] = {}, hi[W] = {};
-            if (there) {
-                load_entries<BF16, W>(rows + (size_t)head * row_bytes, e, lo);
-                load_entries<BF16, W>(rows + (size_t)head * row_bytes, half + e, hi);
-            }
+    // (q_out may be q: a lane writes the entries that it has read)
+    __nv_bfloat16* out = a.q_out + (size_t)token * a.out_stride;
+    for (int head = begin; head < a.q_heads; head += BATCH * stride) {
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            if (!mine || head + k * stride >= a.q_heads) continue;
             float x[2][W];
 #pragma unroll
-            for (int i = 0; i < W; ++i) x[0][i] = lo[i] * c[i] - hi[i] * sn[i], x[1][i] = hi[i] * c[i] + lo[i] * sn[i];
-            __syncwarp();  // q_out may be q: every lane has read before any lane writes
-            if (there) {
-                store_bf16<W>(out + head * a.l.hd, e, x[0]);
-                store_bf16<W>(out + head * a.l.hd, half + e, x[1]);
+            for (int i = 0; i < W; ++i) {
+                x[0][i] = q[k][0][i] * c[i] - q[k][1][i] * sn[i];
+                x[1][i] = q[k][1][i] * c[i] + q[k][0][i] * sn[i];
             }
+            store_bf16<W>(out + (head + k * stride) * a.l.hd, e, x[0]);
+            store_bf16<W>(out + (head + k * stride) * a.l.hd, half + e, x[1]);
         }
+        load_queries(head + BATCH * stride);
     }
     // ---- keys and values: row r is head r / 2's key or value
-    const int page = a48p::page_of(a.l, a.b, s, pos), slot = pos & (a.l.page - 1);
     if (page < 0) return;  // no page for this position: nothing is stored
     const char* k_rows = static_cast<const char*>(a.k) + (size_t)token * a.k_stride * (BF16 ? 2 : 4);
     const char* v_rows = static_cast<const char*>(a.v) + (size_t)token * a.v_stride * (BF16 ? 2 : 4);
@@ -174,15 +186,22 @@ __global__ void __launch_bounds__(32 * kWarps, 4) paged_write_kernel(const __gri
     const float eps = (float)a.eps, border = 0.5f - (float)L * 0x1p-19f;
     // x step + magic: the nearest multiple's code (q + L + 1) in the low byte of the sum, ties to even
     const float magic = 12582912.f + (float)(L + 1);
-    for (int r = begin; r - lane / G < 2 * a.l.kv_heads; r += stride) {
+    Raw<BF16, W> next[2];  // of the next row
+    auto load_row = [&](int r) {
+        next[0].clear(), next[1].clear();
+        if (mine && r < 2 * a.l.kv_heads) {
+            const char* row = (r & 1 ? v_rows : k_rows) + (size_t)(r >> 1) * row_bytes;
+            next[0].load(row, e);
+            next[1].load(row, half + e);
+        }
+    };
+    load_row(begin);
+    for (int r = begin; r - lane / G < 2 * a.l.kv_heads; r += stride) {  // (the same for the warp)
         const int which = r & 1, head = r >> 1;
         const bool there = mine && head < a.l.kv_heads, turned = a.rotate && !which;
-        float lo[W] = {}, hi[W] = {}, x[2][W];
-        if (there) {
-            const char* row = (which ? v_rows : k_rows) + (size_t)head * row_bytes;
-            load_entries<BF16, W>(row, e, lo);
-            load_entries<BF16, W>(row, half + e, hi);
-        }
+        const Raw<BF16, W> lo = next[0], hi = next[1];
+        load_row(r + stride);
+        float x[2][W];
         // an entry in float64
         auto exact = [&](int h, int i) {
             if (!turned) return (double)(h ? hi[i] : lo[i]);
@@ -305,57 +324,75 @@ __device__ __forceinline__ void read_codes(const uint8_t* __restrict__ row, int 
     }
 }
 
-// One warp per (token, slice of its heads); LANES lanes share a head vector, E entries each, so that a store is 16 bytes
-// (8 where the head dimension does not divide by 8).  Items are (head, keys or values); a position without a page reads as
-// zero.
+// A block takes READ_TOKENS tokens (and a slice of their heads): where they lie is found once, a token per lane, and then
+// every load is independent of every other.  LANES lanes share a head vector, E entries each, so that a store is 16 bytes (8
+// where the head dimension does not divide by 8).  Items are (token, head, keys or values); a position without a page reads
+// as zero.
 template <bool BF16, int E, int BITS, int LANES>
 __global__ void __launch_bounds__(32 * kWarps) paged_read_kernel(const Layout l, const Batch b, const uint8_t* __restrict__ pool,
                                                                  void* __restrict__ k_out, void* __restrict__ v_out) {
-    a48_pdl_prologue();
-    const int lane = threadIdx.x & 31, token = blockIdx.x * kWarps + (threadIdx.x >> 5);
-    if (token >= b.n_tokens) return;
-    const int s = a48p::sequence_of(b, token, lane);
-    if (s < 0) return;
-    const int first = __ldg(b.q_start + s), end = __ldg(b.q_start + s + 1);
-    const int pos = __ldg(b.kv_len + s) - (end - first) + (token - first);
-    const int page = a48p::page_of(l, b, s, pos), slot = pos & (l.page - 1);
     constexpr int PER = 32 / LANES;  // head vectors that a warp takes at a time
-    const int e = E * (lane & (LANES - 1));
-    if (e >= l.hd) return;
-    const bool bos = BITS == 3 && pos == 0;
-    const uint8_t* chunks = pool + a48p::chunk_at(l, max(page, 0), 0);
-    const size_t out_row = (size_t)token * l.kv_heads * l.hd + e;
-    const int codes[2] = {bos ? l.bos : slot * l.row, bos ? l.bos + l.padded / 2 : l.v_codes + slot * l.row};
-    const int scales[2] = {l.k_scales + 4 * slot, l.v_scales + 4 * slot};
-    const int chunk_bytes = l.chunk, kv_heads = l.kv_heads, hd = l.hd;
-#pragma unroll 4
-    for (int i = blockIdx.y * PER + lane / LANES; i < 2 * kv_heads; i += gridDim.y * PER) {
-        const int head = i >> 1, which = i & 1;
-        float x[E];
-#pragma unroll
-        for (int j = 0; j < E; ++j) x[j] = 0.f;
-        if (page >= 0) {
-            const uint8_t* chunk = chunks + (size_t)head * chunk_bytes;
-            const float scale = __ldg(reinterpret_cast<const float*>(chunk + (which ? scales[1] : scales[0])));
-            const uint8_t* row = chunk + (which ? codes[1] : codes[0]);
-            if (BITS == 3 && bos) read_codes<E>(row, e, 4, x);
-            else read_codes<E>(row, e, BITS, x);
-#pragma unroll
-            for (int j = 0; j < E; ++j) x[j] *= scale;
+    __shared__ const uint8_t* chunks_of[READ_TOKENS];  // of the token's page, head 0; none: no page
+    __shared__ int pos_of[READ_TOKENS], there[READ_TOKENS];
+    a48_pdl_prologue();
+    const int lane = threadIdx.x & 31, first_token = blockIdx.x * READ_TOKENS;
+    if (threadIdx.x < 32) {
+        // the first token's sequence or the one behind which it lies, then on from there
+        int s = max(0, a48p::last_at_most(b.n_seqs, first_token, lane, [&](int i) { return (long long)__ldg(b.q_start + i); }));
+        const int token = first_token + lane;
+        if (lane < READ_TOKENS) {
+            int end = __ldg(b.q_start + s + 1);
+            while (token >= end && s + 1 < b.n_seqs) end = __ldg(b.q_start + ++s + 1);
+            const int first = __ldg(b.q_start + s);
+            const bool in = token >= first && token < end && token < b.n_tokens;
+            const int pos = __ldg(b.kv_len + s) - (end - first) + (token - first), page = in ? a48p::page_of(l, b, s, pos) : -1;
+            chunks_of[lane] = page >= 0 ? pool + a48p::chunk_at(l, page, 0) : nullptr;
+            pos_of[lane] = pos;
+            there[lane] = in;
         }
-        void* out = which ? v_out : k_out;
-        const size_t at = out_row + (size_t)head * hd;
-        if constexpr (BF16) {
-            uint32_t w[E / 2];
+    }
+    __syncthreads();
+    const int e = E * (lane & (LANES - 1)), slots = l.page - 1, chunk_bytes = l.chunk, hd = l.hd, rows = 2 * l.kv_heads;
+    if (e >= hd) return;
+    // a warp takes a token's rows of its slice, then the next token's
+    const int warp = threadIdx.x >> 5, begin = blockIdx.y * PER + lane / LANES;
+    for (int t = warp; t < READ_TOKENS; t += kWarps) {
+        if (!there[t]) continue;
+        const uint8_t* chunks = chunks_of[t];
+        const int pos = pos_of[t], slot = pos & slots;
+        const bool bos = BITS == 3 && pos == 0, page = chunks != nullptr;
+        const int codes[2] = {bos ? l.bos : slot * l.row, bos ? l.bos + l.padded / 2 : l.v_codes + slot * l.row};
+        const int scales[2] = {l.k_scales + 4 * slot, l.v_scales + 4 * slot};
+        const size_t out_row = (size_t)(first_token + t) * (rows / 2) * hd + e;
+#pragma unroll 4
+        for (int i = begin; i < rows; i += gridDim.y * PER) {
+            const int head = i >> 1, which = i & 1;
+            float x[E];
 #pragma unroll
-            for (int j = 0; j < E / 2; ++j) {
-                const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
-                w[j] = *reinterpret_cast<const uint32_t*>(&h);
+            for (int j = 0; j < E; ++j) x[j] = 0.f;
+            if (page) {
+                const uint8_t* chunk = chunks + (size_t)head * chunk_bytes;
+                const float scale = __ldg(reinterpret_cast<const float*>(chunk + (which ? scales[1] : scales[0])));
+                const uint8_t* row = chunk + (which ? codes[1] : codes[0]);
+                if (BITS == 3 && bos) read_codes<E>(row, e, 4, x);
+                else read_codes<E>(row, e, BITS, x);
+#pragma unroll
+                for (int j = 0; j < E; ++j) x[j] *= scale;
             }
-            if constexpr (E == 8) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at) = make_uint4(w[0], w[1], w[2], w[3]);
-            else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = make_uint2(w[0], w[1]);
-        } else {
-            *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(x[0], x[1], x[2], x[3]);
+            void* out = which ? v_out : k_out;
+            const size_t at = out_row + (size_t)head * hd;
+            if constexpr (BF16) {
+                uint32_t w[E / 2];
+#pragma unroll
+                for (int j = 0; j < E / 2; ++j) {
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
+                    w[j] = *reinterpret_cast<const uint32_t*>(&h);
+                }
+                if constexpr (E == 8) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at) = make_uint4(w[0], w[1], w[2], w[3]);
+                else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(out) + at) = make_uint2(w[0], w[1]);
+            } else {
+                *reinterpret_cast<float4*>(static_cast<float*>(out) + at) = make_float4(x[0], x[1], x[2], x[3]);
+            }
         }
     }
 }
@@ -363,9 +400,10 @@ __global__ void __launch_bounds__(32 * kWarps) paged_read_kernel(const Layout l,
 template <bool BF16, int E, int LANES>
 cudaError_t launch_read(const Layout& l, const Batch& b, const uint8_t* pool, void* k_out, void* v_out, cudaStream_t st) {
     const int steps = (2 * l.kv_heads + 32 / LANES - 1) / (32 / LANES);  // of a warp over one token
-    int slices = (8192 + b.n_tokens - 1) / b.n_tokens;
+    const int blocks = (b.n_tokens + READ_TOKENS - 1) / READ_TOKENS;
+    int slices = (8 * 148 + blocks - 1) / blocks;
     slices = slices < steps ? slices : steps;
-    const dim3 grid((b.n_tokens + kWarps - 1) / kWarps, slices);
+    const dim3 grid(blocks, slices);
     auto kernel = l.bits == 8 ? paged_read_kernel<BF16, E, 8, LANES> : l.bits == 4 ? paged_read_kernel<BF16, E, 4, LANES> : paged_read_kernel<BF16, E, 3, LANES>;
     return a48_launch_pdl(kernel, grid, dim3(32 * kWarps), 0, st, l, b, pool, k_out, v_out);
 }
