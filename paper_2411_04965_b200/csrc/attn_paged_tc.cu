@@ -482,12 +482,18 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
         const int token = start + (int)(in_seq / a.group), head = kvh * a.group + (int)(in_seq % a.group);
         // ---- the query rows to fp16 by a power of two, in the order of the converted codes
         {
-            uint2 x[PD / 4];
-            const uint2* src = reinterpret_cast<const uint2*>(a.q + (size_t)token * a.q_stride + (size_t)head * a.l.hd);
+            // (four entries to a lane, whole rows to an instruction: with a row to a thread, loads and stores of queries and
+            // outputs were a fifth of the time of a prompt)
+            constexpr int UNITS = PD / 4, AT_ONCE = 32 / UNITS;
+            const int u = lane % UNITS, sub = lane / UNITS;
+            const size_t from = (size_t)token * a.q_stride + (size_t)head * a.l.hd;
+            uint2 x[UNITS];
             float mx = 0.f;
 #pragma unroll
-            for (int i = 0; i < PD / 4; ++i) {
-                x[i] = mine && 4 * i < a.l.hd ? __ldg(src + i) : make_uint2(0, 0);
+            for (int i = 0; i < UNITS; ++i) {
+                const int j = AT_ONCE * i + sub;
+                const size_t at = __shfl_sync(0xffffffffu, (unsigned long long)from, j);
+                x[i] = r - lane + j < rows && 4 * u < a.l.hd ? __ldg(reinterpret_cast<const uint2*>(a.q + at) + u) : make_uint2(0, 0);
                 mx = fmaxf(mx, fmaxf(fmaxf(fabsf(__uint_as_float(x[i].x << 16)), fabsf(__uint_as_float(x[i].x & 0xffff0000u))),
                                      fmaxf(fabsf(__uint_as_float(x[i].y << 16)), fabsf(__uint_as_float(x[i].y & 0xffff0000u)))));
             }
@@ -497,20 +503,26 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             queries_sync();
             const int e = query_exponent(*q_top);
             const float up0 = power_of_two(e / 2), up1 = power_of_two(e - e / 2);  // (2^e may be past fp32)
-            auto value = [&](int n) {
-                const uint32_t w = n & 2 ? x[n / 4].y : x[n / 4].x;
-                return __uint_as_float(n & 1 ? w & 0xffff0000u : w << 16) * up0 * up1;
+            auto halves_of = [&](uint32_t w) {
+                const __half2 h = __floats2half2_rn(__uint_as_float(w << 16) * up0 * up1, __uint_as_float(w & 0xffff0000u) * up0 * up1);
+                return *reinterpret_cast<const uint32_t*>(&h);
             };
-            uint8_t* dst = smem + C::Q_AT + half * C::BUF + row * 128;
+            // Entries n and n + 16 (n + 4 at 4 bits) side by side: of two lanes that far apart, either gives two entries to the
+            // other.  At 8 bits the pairs (n, n + 2) are the lane's own.
+            constexpr int APART = BITS == 3 ? 4 : BITS == 4 ? 1 : 0;
+            const bool upper = (u & APART) != 0;
+            const int place = BITS == 3 ? (4 * u & ~31) + 8 * (u & 3) + (u & 4) : 4 * u;
+            uint8_t* dst = smem + C::Q_AT + half * C::BUF + place / 64 * PANEL + (place & 4) * 2;
 #pragma unroll
-            for (int c = 0; c < PD / 8; ++c) {
-                uint32_t h[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const __half2 p = __floats2half2_rn(value(entry_of<BITS>(8 * c + 2 * i)), value(entry_of<BITS>(8 * c + 2 * i + 1)));
-                    h[i] = *reinterpret_cast<const uint32_t*>(&p);
+            for (int i = 0; i < UNITS; ++i) {
+                const int at = (warp & 3) * 32 + AT_ONCE * i + sub;
+                uint32_t lo = halves_of(x[i].x), hi = halves_of(x[i].y);
+                if constexpr (APART > 0) {
+                    const uint32_t got = __shfl_xor_sync(0xffffffffu, upper ? lo : hi, APART);
+                    lo = upper ? got : lo, hi = upper ? hi : got;
                 }
-                *reinterpret_cast<uint4*>(dst + c / 8 * PANEL + (((c % 8) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+                *reinterpret_cast<uint2*>(dst + at * 128 + (((place / 8 % 8) ^ (at & 7)) << 4)) =
+                    make_uint2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
@@ -732,7 +744,26 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
         const bool split = a.tc_splits > 1;
         const float inv = unit == 0.f ? 0.f : split ? 1.f / unit : ml.y != 0.f ? 1.f / ml.y / unit : 0.f;
         if (split && mine) a.part_ml[part] = ml;
-        __nv_bfloat16* out = a.out + (size_t)token * a.out_stride + (size_t)head * a.l.hd;
+        // Through the place of the warp's query rows, which the last scores have been taken from: 16 bytes of its row at a time
+        // from a thread, eight of one to each lane to memory.
+        uint8_t* stage = smem + C::Q_AT + half * C::BUF + (warp & 3) * 64 * PD;
+        const size_t to = split ? part * 128 : (size_t)token * a.out_stride + (size_t)head * a.l.hd;
+        constexpr int UNITS = PD / 4, AT_ONCE = 32 / UNITS;
+        auto put = [&](int chunk, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+            *reinterpret_cast<uint4*>(stage + lane * 2 * PD + ((chunk ^ (lane & 7)) << 4)) = make_uint4(x, y, z, w);
+        };
+        auto store_rows = [&](uint8_t* base, int elem, int width) {  // elem: bytes of an entry; width: bytes of a row that there are
+            __syncwarp();
+            const int u = lane % UNITS, sub = lane / UNITS;
+#pragma unroll 8
+            for (int i = 0; i < UNITS; ++i) {
+                const int j = AT_ONCE * i + sub;
+                const size_t at = __shfl_sync(0xffffffffu, (unsigned long long)to, j);
+                const uint2 v = *reinterpret_cast<const uint2*>(stage + j * 2 * PD + (((u >> 1) ^ (j & 7)) << 4) + 8 * (u & 1));
+                if (r - lane + j < rows && 8 * u < width) *reinterpret_cast<uint2*>(base + at * elem + 8 * u) = v;
+            }
+            __syncwarp();
+        };
 #pragma unroll
         for (int c = 0; c < PD / 32; ++c) {
             uint32_t acc[32];
@@ -746,18 +777,26 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             }
 #pragma unroll
             for (int i = 0; i < 32; ++i) y[entry_of<BITS>(i)] = inv == 0.f ? 0.f : __uint_as_float(acc[i]) * inv;
+            if (split) {
+                constexpr int HALF = PD / 64;  // 32-column blocks that the place holds as fp32
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                if (!mine || 32 * c + i >= a.l.hd) continue;
-                if (split) {
-                    reinterpret_cast<float4*>(a.part_o + part * 128)[8 * c + i / 4] = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
-                } else {
-                    const __nv_bfloat162 lo = __floats2bfloat162_rn(y[i], y[i + 1]), hi = __floats2bfloat162_rn(y[i + 2], y[i + 3]);
-                    *reinterpret_cast<uint2*>(out + 32 * c + i) =
-                        make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+                for (int i = 0; i < 32; i += 4)
+                    put(8 * (c % HALF) + i / 4, __float_as_uint(y[i]), __float_as_uint(y[i + 1]), __float_as_uint(y[i + 2]), __float_as_uint(y[i + 3]));
+                if (c % HALF == HALF - 1) store_rows(reinterpret_cast<uint8_t*>(a.part_o) + 128 * (c - HALF + 1), 4, a.l.hd * 4 - 128 * (c - HALF + 1));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; i += 8) {
+                    uint32_t w[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const __nv_bfloat162 v = __floats2bfloat162_rn(y[i + 2 * k], y[i + 2 * k + 1]);
+                        w[k] = *reinterpret_cast<const uint32_t*>(&v);
+                    }
+                    put(4 * c + i / 8, w[0], w[1], w[2], w[3]);
                 }
             }
         }
+        if (!split) store_rows(reinterpret_cast<uint8_t*>(a.out), 2, a.l.hd * 2);
     }
     tc_fence_before();
     __syncthreads();
