@@ -75,7 +75,7 @@ __device__ __noinline__ void mbar_wait_slow(uint32_t bar, uint32_t parity, volat
                 *abort_flag = 1;
                 if (atomicCAS(&g_status[0], 0u, (unsigned)BITNET_A48_ERR_TIMEOUT) == 0u) {
                     g_status[1] = id;
-                    g_status[2] = blockIdx.x + gridDim.x * blockIdx.y;
+                    g_status[2] = blockIdx.x;
                     g_status[3] = iter;
                 }
                 return;
@@ -87,6 +87,18 @@ __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatil
     if (mbar_try(bar, parity)) return;
     if (*abort_flag) return;
     mbar_wait_slow(bar, parity, abort_flag, id, iter);
+}
+__device__ __noinline__ void mbar_wait_long(uint32_t bar, uint32_t parity, uint32_t iter) {
+    const unsigned long long t0 = clock64();
+    while (!mbar_try(bar, parity))
+        if (clock64() - t0 > 5 * kWaitClocks) {
+            if (atomicCAS(&g_status[0], 0u, (unsigned)BITNET_A48_ERR_TIMEOUT) == 0u) {
+                g_status[1] = 46;
+                g_status[2] = blockIdx.x;
+                g_status[3] = iter;
+            }
+            return;
+        }
 }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -229,13 +241,48 @@ template <int PD>
 struct Cfg {
     static constexpr int BUF = TK * PD * 2;  // one tile of keys, values or query rows
     static constexpr int Q_AT = RING * BUF, CTRL_AT = Q_AT + 2 * BUF, ROWS_AT = CTRL_AT + 256,
-                         SCALES_AT = ROWS_AT + 2 * TQ * 8;
-    static constexpr int SMEM = SCALES_AT + SCALES * (int)sizeof(TileScales) + 1024 /*alignment slack*/;
+                         SCALES_AT = ROWS_AT + 2 * TQ * 8, OUT_AT = SCALES_AT + SCALES * (int)sizeof(TileScales);
+    static constexpr int SMEM = OUT_AT + 2 * TQ * 64 + 1024 /*alignment slack*/;
     static_assert(SMEM <= 227 * 1024, "shared memory budget");
 };
 
 // what a wait that gave up was for
-enum { WAIT_FULL = 41, WAIT_EMPTY = 42, WAIT_S = 43, WAIT_O = 45 };
+enum { WAIT_FULL = 41, WAIT_EMPTY = 42, WAIT_S = 43, WAIT_ANSWER = 44, WAIT_O = 45 };
+
+// What a CTA takes at a time: up to 256 rows of a sequence with one key/value head, and the blocks of positions v0 ..
+// v0 + n_tiles - 1 of their span.  The tiles with the most positions come first.
+struct Item {
+    Span span;
+    long long r0;  // first row
+    int kvh, part, seq, start, rows, halves, pos0, pos_lo, pos_hi, v0, n_tiles;
+};
+__device__ __forceinline__ bool item_of(const AttnArgs& a, int index, int lane, Item& it) {  // false: no rows there
+    const int x = index / a.tc_splits, at = gridDim.x / a.tc_splits / a.l.kv_heads - 1 - x / a.l.kv_heads;
+    it.part = index % a.tc_splits, it.kvh = x % a.l.kv_heads;
+    int tile;
+    if (a.tc_tiles > 0) {
+        it.seq = at % a.b.n_seqs, tile = at / a.b.n_seqs;
+    } else {  // sequence b has the tiles from floor(q_start[b] group / 256) + b on, more than it needs
+        auto first_tile = [&](int b) { return (long long)__ldg(a.b.q_start + b) * a.group / a48p::TILE_ROWS + b; };
+        it.seq = a48p::last_at_most(a.b.n_seqs, at, lane, first_tile);
+        if (it.seq < 0) return false;
+        tile = at - (int)first_tile(it.seq);
+    }
+    it.start = __ldg(a.b.q_start + it.seq);
+    const int q_len = __ldg(a.b.q_start + it.seq + 1) - it.start;
+    const long long all_rows = (long long)q_len * a.group;
+    it.r0 = (long long)tile * a48p::TILE_ROWS;
+    if (all_rows <= a.few_rows || it.r0 >= all_rows || it.start < 0 || q_len > a.b.n_tokens - it.start) return false;
+    it.rows = (int)min((long long)a48p::TILE_ROWS, all_rows - it.r0);
+    it.halves = it.rows > TQ ? 2 : 1;
+    it.pos0 = __ldg(a.b.kv_len + it.seq) - q_len;
+    it.pos_lo = it.pos0 + (int)(it.r0 / a.group), it.pos_hi = it.pos0 + (int)((it.r0 + it.rows - 1) / a.group);
+    it.span = a48p::span_of<7>(a, it.pos_lo, it.pos_hi);
+    const int per = max(2, (it.span.count + a.tc_splits - 1) / a.tc_splits);
+    it.v0 = it.part * per;
+    it.n_tiles = max(0, min(it.span.count, it.v0 + per) - it.v0);
+    return true;
+}
 
 template <int BITS, int PD>
 __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_constant__ AttnArgs a) {
@@ -245,54 +292,40 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
     // (an offset, not an aligned integer: the compiler then knows these as shared-memory addresses)
     uint8_t* smem = smem_raw + (-smem_u32(smem_raw) & 1023u);
     uint8_t* ctrl = smem + C::CTRL_AT;
+    uint8_t* canceled = ctrl + 128;  // the answer about a CTA not yet started, 16 bytes
+    volatile int* next_item = reinterpret_cast<volatile int*>(ctrl + 144);
+    uint32_t* q_tops = reinterpret_cast<uint32_t*>(ctrl + 160);  // the largest query entry, as bits, of three items
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl + 192);
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(ctrl + 196);
-    uint32_t* q_top = reinterpret_cast<uint32_t*>(ctrl + 200);  // the largest query entry, as bits
     float* top_part = reinterpret_cast<float*>(ctrl + 208);     // largest value scale per converting warp
     float2* row_info = reinterpret_cast<float2*>(smem + C::ROWS_AT);  // last position seen; at the end reference and sum
     TileScales* scales = reinterpret_cast<TileScales*>(smem + C::SCALES_AT);
     const uint32_t ring = smem_u32(smem), sq = ring + C::Q_AT;
-    // barriers: full[4] | empty[4] | s[2] | o[2]
-    const uint32_t bar_full = smem_u32(ctrl), bar_empty = bar_full + 32, bar_s = bar_full + 64, bar_o = bar_full + 80;
+    // barriers: full[4] | empty[4] | s[2] | o[2] | answer | next item
+    const uint32_t bar_full = smem_u32(ctrl), bar_empty = bar_full + 32, bar_s = bar_full + 64, bar_o = bar_full + 80,
+                   bar_answer = bar_full + 96, bar_next = bar_full + 104;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // (known to be the same in a warp)
     // (Dependents are let go only once what came before is done and seen: the rows kernel that follows may then start beside
     // this one.)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    // ---- which rows: the tiles with the most positions first
-    const int kvh = blockIdx.x % a.l.kv_heads, at = gridDim.x / a.l.kv_heads - 1 - blockIdx.x / a.l.kv_heads;
-    int seq, tile;
-    if (a.tc_tiles > 0) {
-        seq = at % a.b.n_seqs, tile = at / a.b.n_seqs;
-    } else {  // sequence b has the tiles from floor(q_start[b] group / 256) + b on, more than it needs
-        auto first_tile = [&](int b) { return (long long)__ldg(a.b.q_start + b) * a.group / a48p::TILE_ROWS + b; };
-        seq = a48p::last_at_most(a.b.n_seqs, at, lane, first_tile);
-        if (seq < 0) return;
-        tile = at - (int)first_tile(seq);
-    }
-    const int start = __ldg(a.b.q_start + seq), q_len = __ldg(a.b.q_start + seq + 1) - start;
-    const long long all_rows = (long long)q_len * a.group, r0 = (long long)tile * a48p::TILE_ROWS;
-    if (all_rows <= a.few_rows || r0 >= all_rows || start < 0 || q_len > a.b.n_tokens - start) return;
-    const int rows = (int)min((long long)a48p::TILE_ROWS, all_rows - r0);
-    const int halves = rows > TQ ? 2 : 1;
-    const int pos0 = __ldg(a.b.kv_len + seq) - q_len;
-    const int pos_lo = pos0 + (int)(r0 / a.group), pos_hi = pos0 + (int)((r0 + rows - 1) / a.group);
-    const Span span = a48p::span_of<7>(a, pos_lo, pos_hi);
-    const int per = max(2, (span.count + (int)gridDim.y - 1) / (int)gridDim.y), v0 = blockIdx.y * per;
-    const int n_tiles = max(0, min(span.count, v0 + per) - v0);
-
+    Item it;
+    bool there = item_of(a, blockIdx.x, lane, it);
+    if (!there) return;
     if (threadIdx.x == 0) {
         for (int i = 0; i < RING; ++i) {
             mbar_init(bar_full + 8 * i, TQ);
-            mbar_init(bar_empty + 8 * i, halves);
+            mbar_init(bar_empty + 8 * i, 2);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(bar_s + 8 * i, 1);
             mbar_init(bar_o + 8 * i, 1);
         }
+        mbar_init(bar_answer, 1);
+        mbar_init(bar_next, 1);
         *abort_flag = 0;
-        *q_top = 0;
+        q_tops[0] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == CONVERT_WARP) {
@@ -305,6 +338,38 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
 
+    // Items: the CTA's own, then those of CTAs that have not started, which it cancels and takes over one at a time.  One
+    // thread asks while the last tile of positions of an item is converted, and hands the answer on; the others have
+    // read the one before by then (every item has a queries_sync of all warps).
+    auto ask = [&]() {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], 16;" ::"r"(bar_answer) : "memory");
+        asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                         smem_u32(canceled)),
+                     "r"(bar_answer)
+                     : "memory");
+    };
+    auto hand_on = [&](int k) {  // what was asked for ahead of item k
+        mbar_wait(bar_answer, (k - 1) & 1, abort_flag, WAIT_ANSWER, k);
+        uint32_t taken, index;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t.reg .b128 answer;\n\t"
+            "ld.shared.b128 answer, [%2];\n\t"
+            "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, answer;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\tmov.u32 %1, 0;\n\t"
+            "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, answer;\n\t}"
+            : "=r"(taken), "=r"(index)
+            : "r"(smem_u32(canceled))
+            : "memory");
+        *next_item = taken && !*abort_flag ? (int)index : -1;
+        mbar_arrive(bar_next);
+    };
+    // (This one wait must not be given up before that thread has come through its own: five times their limit.)
+    auto item_after = [&](int k) {
+        mbar_wait_long(bar_next, (k - 1) & 1, k);
+        return *next_item;
+    };
+    int n0 = 0;  // tiles of positions of the items before
     if (warp >= CONVERT_WARP) {
         // ------------------------------------------------------------------------------------------ codes to fp16
         const int w = warp - CONVERT_WARP, r = 32 * w + lane;  // r: the position whose scales are this thread's
@@ -321,16 +386,16 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
         auto look_up = [&](int t) {
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                const int p = t < n_tiles ? span.block(v0 + t) * TK + 32 * w + 16 * b : INT_MAX;
-                next[b] = p <= pos_hi ? a48p::page_of(a.l, a.b, seq, p) : -1;
+                const int p = t < it.n_tiles ? it.span.block(it.v0 + t) * TK + 32 * w + 16 * b : INT_MAX;
+                next[b] = p <= it.pos_hi ? a48p::page_of(a.l, a.b, it.seq, p) : -1;
             }
         };
         auto locate = [&](int t) {
-            base = span.block(v0 + t) * TK + 32 * w;
+            base = it.span.block(it.v0 + t) * TK + 32 * w;
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
                 page[b] = next[b];
-                chunk[b] = a.pool + a48p::chunk_at(a.l, max(page[b], 0), kvh);
+                chunk[b] = a.pool + a48p::chunk_at(a.l, max(page[b], 0), it.kvh);
                 slot[b] = (base + 16 * b) & slots;
             }
         };
@@ -400,17 +465,6 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             }
         };
         Codes keys, values;
-        look_up(0);
-        if (n_tiles > 0) {
-            locate(0);
-            load_scales();
-            load_codes(keys, 0);
-            load_codes(values, 1);
-            look_up(1);
-        }
-        queries_sync();
-        const int e = query_exponent(*q_top);
-        const float factor = a.scale * 1.4426950408889634f * power_of_two(-e / 2) * power_of_two(-(e - e / 2));
         auto wait_empty = [&](int n) {
             if (n >= RING) mbar_wait(bar_empty + 8 * (n % RING), (n / RING & 1) ^ 1, abort_flag, WAIT_EMPTY, n);
             return smem + n % RING * C::BUF;
@@ -419,384 +473,458 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             mbar_arrive(bar_full + 8 * (n % RING));
         };
+        int index = blockIdx.x;
 #pragma unroll 1
-        for (int t = 0; t < n_tiles; ++t) {
-            const int pos = base + lane;
-            const uint8_t* bos = BITS == 3 && base == 0 && page[0] >= 0 ? chunk[0] + a.l.bos : nullptr;  // position 0's codes
-            const bool dead = (lane < 16 ? page[0] : page[1]) < 0 && pos <= pos_hi;
-            // ---- scales; one counts if it is finite and some row may see its position
-            const bool may = pos <= pos_hi && (window == 0 || pos > pos_lo - window || pos < sinks);
-            const bool finite = sk <= 3.4e38f && sv <= 3.4e38f;
-            // The scores of a row that does not see a position are set to -inf ahead of these factors, so they have to be
-            // positive and finite; where the scales are not, the rows that do see the position get no numbers from its key.
-            const float key = finite && may ? fminf(fmaxf(sk * factor, 1e-37f), 3e38f) : 1.f, f = finite && may ? sv : 0.f;
-            const uint32_t sick = __ballot_sync(0xffffffffu, may && !finite), gone = __ballot_sync(0xffffffffu, dead);
-            if (convert_any(unit == 0.f ? f > 0.f : f * unit > 64.f)) {
-                float top = f;
-#pragma unroll
-                for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                if (lane == 0) top_part[w] = top;
-                convert_sync();
-                top = fmaxf(fmaxf(top_part[0], top_part[1]), fmaxf(top_part[2], top_part[3]));
-                // two octaves of room, so that scales of one size do not come back here; within fp32's exponents
-                unit = scalbnf(1.f, min(max(5 - (ilogbf(top) + 2), -120), 120));
-            }
-            // ---- keys.  (The ring is what keeps the scales of four tiles apart: K(t) can be written once the scores of
-            // t - 2 are done, and the weights of t - 3 were taken before the scores of t - 2 were issued.)
-            uint8_t* buf = wait_empty(2 * t);
-            store_codes(buf, keys, bos);
-            TileScales& ts = scales[t % SCALES];
-            ts.scale[r >> 1][r & 1] = key;
-            ts.scale[r >> 1][2 + (r & 1)] = f * unit;
-            if (lane == 0) ts.dead[w] = gone;
-            if (r == 0) ts.unit = unit;
-            if (sick) {
-                __syncwarp();
-                for (int i = 0; i < PD / 8; ++i)
-                    if ((sick >> lane) & 1)
-                        *reinterpret_cast<uint4*>(buf + i / 8 * PANEL + r * 128 + i % 8 * 16) =
-                            make_uint4(0x7e007e00u, 0x7e007e00u, 0x7e007e00u, 0x7e007e00u);
-            }
-            publish(2 * t);
-            // ---- the next tile's keys under way, then the values of this one
-            if (t + 1 < n_tiles) {
-                locate(t + 1);
+        for (int k = 0; index >= 0;) {
+            if (it.n_tiles > 0) {
+                unit = 0.f;
+                look_up(0);
+                locate(0);
                 load_scales();
                 load_codes(keys, 0);
-            }
-            store_codes(wait_empty(2 * t + 1), values, bos ? bos + a.l.padded / 2 : nullptr);
-            publish(2 * t + 1);
-            if (t + 1 < n_tiles) {
                 load_codes(values, 1);
-                look_up(t + 2);
+                look_up(1);
+            } else {
+                queries_sync();
+                if (threadIdx.x == 32 * CONVERT_WARP) ask();
             }
+            float factor = 0.f;
+#pragma unroll 1
+            for (int t = 0; t < it.n_tiles; ++t) {
+                const int pos = base + lane;
+                const uint8_t* bos = BITS == 3 && base == 0 && page[0] >= 0 ? chunk[0] + a.l.bos : nullptr;  // position 0's codes
+                const bool dead = (lane < 16 ? page[0] : page[1]) < 0 && pos <= it.pos_hi;
+                // ---- the codes of the keys.  (The ring is what keeps the scales of four tiles apart: K(t) can be written once
+                // the scores of t - 2 are done, and the weights of t - 3 were taken before the scores of t - 2 were issued.)
+                const int n = 2 * (n0 + t);
+                uint8_t* buf = wait_empty(n);
+                store_codes(buf, keys, bos);
+                if (t == 0) {
+                    queries_sync();
+                    const int e = query_exponent(q_tops[k % 3]);
+                    factor = a.scale * 1.4426950408889634f * power_of_two(-e / 2) * power_of_two(-(e - e / 2));
+                }
+                if (t + 1 == it.n_tiles && threadIdx.x == 32 * CONVERT_WARP) ask();
+                // ---- their scales; one counts if it is finite and some row may see its position
+                const bool may = pos <= it.pos_hi && (window == 0 || pos > it.pos_lo - window || pos < sinks);
+                const bool finite = sk <= 3.4e38f && sv <= 3.4e38f;
+                // The scores of a row that does not see a position are set to -inf ahead of these factors, so they have to be
+                // positive and finite; where the scales are not, the rows that do see the position get no numbers from its key.
+                const float key = finite && may ? fminf(fmaxf(sk * factor, 1e-37f), 3e38f) : 1.f, f = finite && may ? sv : 0.f;
+                const uint32_t sick = __ballot_sync(0xffffffffu, may && !finite), gone = __ballot_sync(0xffffffffu, dead);
+                if (convert_any(unit == 0.f ? f > 0.f : f * unit > 64.f)) {
+                    float top = f;
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                    if (lane == 0) top_part[w] = top;
+                    convert_sync();
+                    top = fmaxf(fmaxf(top_part[0], top_part[1]), fmaxf(top_part[2], top_part[3]));
+                    // two octaves of room, so that scales of one size do not come back here; within fp32's exponents
+                    unit = scalbnf(1.f, min(max(5 - (ilogbf(top) + 2), -120), 120));
+                }
+                TileScales& ts = scales[(n0 + t) % SCALES];
+                ts.scale[r >> 1][r & 1] = key;
+                ts.scale[r >> 1][2 + (r & 1)] = f * unit;
+                if (lane == 0) ts.dead[w] = gone;
+                if (r == 0) ts.unit = unit;
+                if (sick) {
+                    __syncwarp();
+                    for (int i = 0; i < PD / 8; ++i)
+                        if ((sick >> lane) & 1)
+                            *reinterpret_cast<uint4*>(buf + i / 8 * PANEL + r * 128 + i % 8 * 16) =
+                                make_uint4(0x7e007e00u, 0x7e007e00u, 0x7e007e00u, 0x7e007e00u);
+                }
+                publish(n);
+                // ---- the next tile's keys under way, then the values of this one
+                if (t + 1 < it.n_tiles) {
+                    locate(t + 1);
+                    load_scales();
+                    load_codes(keys, 0);
+                }
+                store_codes(wait_empty(n + 1), values, bos ? bos + a.l.padded / 2 : nullptr);
+                publish(n + 1);
+                if (t + 1 < it.n_tiles) {
+                    load_codes(values, 1);
+                    look_up(t + 2);
+                }
+            }
+            if (threadIdx.x == 32 * CONVERT_WARP) hand_on(k + 1);
+            n0 += it.n_tiles;
+            index = item_after(++k);
+            if (index >= 0 && !item_of(a, index, lane, it)) it.n_tiles = 0;
+        }
+        // the CTA must not end before the last arrivals on its barriers
+        for (int i = 0; i < RING; ++i) {
+            const int uses = (2 * n0 - i + RING - 1) / RING;
+            if (uses > 0) mbar_wait(bar_empty + 8 * i, (uses - 1) & 1, abort_flag, WAIT_EMPTY, n0);
         }
     } else {
         // ------------------------------------------------------------------------------------------ rows
         const int half = warp >> 2, row = (warp & 3) * 32 + lane, r = half * TQ + row;
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         const uint32_t s_at = lanes + COL_S + TK * half, o_at = lanes + COL_O + 128 * half;
-        // this thread's row while queries are loaded and outputs stored
-        const bool mine = r < rows;
-        const long long in_seq = r0 + (mine ? r : rows - 1);
-        const int token = start + (int)(in_seq / a.group), head = kvh * a.group + (int)(in_seq % a.group);
-        // ---- the query rows to fp16 by a power of two, in the order of the converted codes
-        {
-            // (four entries to a lane, whole rows to an instruction: with a row to a thread, loads and stores of queries and
-            // outputs were a fifth of the time of a prompt)
-            constexpr int UNITS = PD / 4, AT_ONCE = 32 / UNITS;
-            const int u = lane % UNITS, sub = lane / UNITS;
-            const size_t from = (size_t)token * a.q_stride + (size_t)head * a.l.hd;
-            uint2 x[UNITS];
-            float mx = 0.f;
-#pragma unroll
-            for (int i = 0; i < UNITS; ++i) {
-                const int j = AT_ONCE * i + sub;
-                const size_t at = __shfl_sync(0xffffffffu, (unsigned long long)from, j);
-                x[i] = r - lane + j < rows && 4 * u < a.l.hd ? __ldg(reinterpret_cast<const uint2*>(a.q + at) + u) : make_uint2(0, 0);
-                mx = fmaxf(mx, fmaxf(fmaxf(fabsf(__uint_as_float(x[i].x << 16)), fabsf(__uint_as_float(x[i].x & 0xffff0000u))),
-                                     fmaxf(fabsf(__uint_as_float(x[i].y << 16)), fabsf(__uint_as_float(x[i].y & 0xffff0000u)))));
-            }
-            const uint32_t top = __reduce_max_sync(0xffffffffu, mx <= 3.4e38f ? __float_as_uint(mx) : 0u);
-            if (lane == 0) atomicMax(q_top, top);
-            row_info[r].x = __int_as_float(pos0 + (int)(in_seq / a.group));
-            queries_sync();
-            const int e = query_exponent(*q_top);
-            const float up0 = power_of_two(e / 2), up1 = power_of_two(e - e / 2);  // (2^e may be past fp32)
-            auto halves_of = [&](uint32_t w) {
-                const __half2 h = __floats2half2_rn(__uint_as_float(w << 16) * up0 * up1, __uint_as_float(w & 0xffff0000u) * up0 * up1);
-                return *reinterpret_cast<const uint32_t*>(&h);
-            };
-            // Entries n and n + 16 (n + 4 at 4 bits) side by side: of two lanes that far apart, either gives two entries to the
-            // other.  At 8 bits the pairs (n, n + 2) are the lane's own.
-            constexpr int APART = BITS == 3 ? 4 : BITS == 4 ? 1 : 0;
-            const bool upper = (u & APART) != 0;
-            const int place = BITS == 3 ? (4 * u & ~31) + 8 * (u & 3) + (u & 4) : 4 * u;
-            uint8_t* dst = smem + C::Q_AT + half * C::BUF + place / 64 * PANEL + (place & 4) * 2;
-#pragma unroll
-            for (int i = 0; i < UNITS; ++i) {
-                const int at = (warp & 3) * 32 + AT_ONCE * i + sub;
-                uint32_t lo = halves_of(x[i].x), hi = halves_of(x[i].y);
-                if constexpr (APART > 0) {
-                    const uint32_t got = __shfl_xor_sync(0xffffffffu, upper ? lo : hi, APART);
-                    lo = upper ? got : lo, hi = upper ? hi : got;
-                }
-                *reinterpret_cast<uint2*>(dst + at * 128 + (((place / 8 % 8) ^ (at & 7)) << 4)) =
-                    make_uint2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        }
-        // ---- MMAs of this tile: by one thread, once all have done their part
-        constexpr uint32_t idesc_s = idesc_f16(TQ, TK, false), idesc_o = idesc_f16(TQ, PD, true);
-        const uint32_t t_s = tmem + COL_S + TK * half, t_o = tmem + COL_O + 128 * half;
-        auto wait_full = [&](int n) {
-            mbar_wait(bar_full + 8 * (n % RING), n / RING & 1, abort_flag, WAIT_FULL, n);
-            tc_fence_after();
-            return ring + n % RING * C::BUF;
-        };
-        const uint64_t q_desc = smem_desc(sq + half * C::BUF);
-        auto issue_s = [&](int t) {
-            const uint64_t k_desc = smem_desc(wait_full(2 * t));
-            if (elect()) {
-#pragma unroll
-                for (int ks = 0; ks < PD / 16; ++ks) {
-                    constexpr int STEP = PANEL / 16;  // of a descriptor's address, per 64 entries
-                    mma_ss(t_s, q_desc + ks / 4 * STEP + 2 * (ks % 4), k_desc + ks / 4 * STEP + 2 * (ks % 4), idesc_s, ks != 0);
-                }
-                tc_commit(bar_s + 8 * half);
-                tc_commit(bar_empty + 8 * (2 * t % RING));
-            }
-            __syncwarp();
-        };
-        auto issue_o = [&](int t, bool last) {
-            const uint64_t v_desc = smem_desc(wait_full(2 * t + 1));
-            if (elect()) {
-                mma_ts(t_o, t_s, v_desc, idesc_o, t != 0);
-#pragma unroll
-                for (int j = 1; j < TK / 16; ++j) mma_ts(t_o, t_s + 8 * j, v_desc + 2048 / 16 * j, idesc_o, 1);
-                tc_commit(bar_o + 8 * half);
-                // (not on the last tile: nothing waits for it, and the CTA must not end before it has arrived)
-                if (!last) tc_commit(bar_empty + 8 * ((2 * t + 1) % RING));
-            }
-            __syncwarp();
-        };
-        const bool issuer = (warp & 3) == 0;
-        const int used = half < halves ? n_tiles : 0;
         const int window = in_register(a.window), sinks = in_register(a.sinks);
-        tile_sync(half);
-        if (issuer && used > 0) issue_s(0);
-        // the four rows of this thread between loads and stores: lanes g, g + 8, g + 16, g + 24 of the warp
-        const int g = lane >> 2, c0 = 2 * (lane & 3);
-        float m[4], l[4], unit = 0.f;
-        int lim[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            lim[i] = __float_as_int(row_info[half * TQ + (warp & 3) * 32 + 8 * i + g].x);
-            m[i] = -1e30f, l[i] = 0.f;
-        }
-        const int lim_lo = __reduce_min_sync(0xffffffffu, min(min(lim[0], lim[1]), min(lim[2], lim[3])));
-        const int lim_hi = __reduce_max_sync(0xffffffffu, max(max(lim[0], lim[1]), max(lim[2], lim[3])));
-        if (halves == 2 && half == 1 && used > 0) turn_pass(1);
-        for (int t = 0; t < used; ++t) {
-            mbar_wait(bar_s + 8 * half, t & 1, abort_flag, WAIT_S, t);
-            tc_fence_after();
-            const TileScales& ts = scales[t % SCALES];
-            const int base = span.block(v0 + t) * TK;
-            const uint4 dead = *reinterpret_cast<const uint4*>(ts.dead);
-            const bool whole = base + TK - 1 <= lim_lo && (window == 0 || base > lim_hi - window || base + TK - 1 < sinks) &&
-                               (dead.x | dead.y | dead.z | dead.w) == 0;
-            if (!whole) {  // the scores that a row does not see become -inf
-#pragma unroll 1
-                for (int c = 0; c < TK / 16; ++c) {
-                    uint32_t acc[2][8];
-                    tmem_ld_16x16(s_at + 16 * c, acc[0]);
-                    tmem_ld_16x16(s_at + (16u << 16) + 16 * c, acc[1]);
-                    tmem_wait_ld(acc);
-                    const uint32_t gone = ts.dead[c >> 1] >> (16 * (c & 1) + c0);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int n = 16 * c + 8 * ((i >> 2) & 1) + c0 + (i & 1), to = lim[(i >> 3) * 2 + ((i >> 1) & 1)] - base;
-                        const bool seen = n <= to && (window == 0 || n > to - window || n < sinks - base) && !((gone >> (8 * ((i >> 2) & 1) + (i & 1))) & 1);
-                        if (!seen) acc[i >> 3][i & 7] = 0xff800000u;
-                    }
-                    tmem_st_16x16(s_at + 16 * c, acc[0]);
-                    tmem_st_16x16(s_at + (16u << 16) + 16 * c, acc[1]);
-                }
-                tmem_wait_st();
-            }
-            if (halves == 2) turn_wait(half);
-            // ---- 64 columns, then the other 64
-#pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-                uint32_t p[2][16];  // weights, two columns to a word
-                float sum[4];
-                for (bool settled = false;; settled = true) {
-                    // weights and sums of 2^(score - m), 16 columns at a time, the next 16 under way meanwhile
-                    f2 m_2[4], sum_2[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) m_2[i] = pack2(-m[i], -m[i]), sum_2[i] = pack2(0.f, 0.f);
-                    uint32_t acc[2][2][8];
-                    tmem_ld_16x16(s_at + 64 * h, acc[0][0]);
-                    tmem_ld_16x16(s_at + (16u << 16) + 64 * h, acc[0][1]);
-                    ulonglong2 scale[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) scale[k] = *reinterpret_cast<const ulonglong2*>(ts.scale[32 * h + 4 * k + c0 / 2]);
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        tmem_wait_ld(acc[c & 1]);
-                        if (c < 3) {
-                            tmem_ld_16x16(s_at + 64 * h + 16 * (c + 1), acc[(c + 1) & 1][0]);
-                            tmem_ld_16x16(s_at + (16u << 16) + 64 * h + 16 * (c + 1), acc[(c + 1) & 1][1]);
-                        }
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const uint32_t* from = acc[c & 1][i >> 1] + 4 * k + 2 * (i & 1);
-                                float y0, y1, w0, w1;
-                                unpack2(fma2(pack2(__uint_as_float(from[0]), __uint_as_float(from[1])), scale[2 * c + k].x, m_2[i]), y0, y1);
-                                const f2 e = pack2(exp2_approx(y0), exp2_approx(y1));
-                                sum_2[i] = add2(sum_2[i], e);
-                                unpack2(mul2(e, scale[2 * c + k].y), w0, w1);
-                                const __half2 w = __floats2half2_rn(w0, w1);
-                                p[i >> 1][2 * (2 * c + k) + (i & 1)] = *reinterpret_cast<const uint32_t*>(&w);
-                            }
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float s0, s1;
-                        unpack2(sum_2[i], s0, s1);
-                        sum[i] = s0 + s1;
-                    }
-                    const float u = ts.unit;
-                    const bool high = u != unit || fmaxf(fmaxf(sum[0], sum[1]), fmaxf(sum[2], sum[3])) > 512.f;
-                    if (settled || !__any_sync(0xffffffffu, high)) break;
-                    // ---- rarely: references to the largest scores of these columns where those are higher (rounded up to
-                    // whole numbers: what moves along then moves by powers of two), and with them O, and the first columns'
-                    // weights while the second's are taken
-                    float corr[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) corr[i] = -INFINITY;
-#pragma unroll 1
-                    for (int c = 0; c < 4; ++c) {
-                        tmem_ld_16x16(s_at + 64 * h + 16 * c, acc[0][0]);
-                        tmem_ld_16x16(s_at + (16u << 16) + 64 * h + 16 * c, acc[0][1]);
-                        tmem_wait_ld(acc[0]);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int row = (i >> 3) * 2 + ((i >> 1) & 1);
-                            corr[row] = fmaxf(corr[row], __uint_as_float(acc[0][i >> 3][i & 7]) *
-                                                             ts.scale[32 * h + 8 * c + 4 * ((i >> 2) & 1) + c0 / 2][i & 1]);
-                        }
-                    }
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        corr[i] = fmaxf(corr[i], __shfl_xor_sync(0xffffffffu, corr[i], 1));
-                        corr[i] = fmaxf(corr[i], __shfl_xor_sync(0xffffffffu, corr[i], 2));
-                        const float m_new = fmaxf(m[i], ceilf(corr[i]));
-                        corr[i] = exp2_approx(m[i] - m_new);
-                        m[i] = m_new;
-                        l[i] *= corr[i];
-                    }
-                    if (h > 0) {
-#pragma unroll 1
-                        for (int c = 0; c < 2; ++c) {  // (16 words are 32 weights)
-                            tmem_ld_16x16(s_at + 16 * c, acc[0][0]);
-                            tmem_ld_16x16(s_at + (16u << 16) + 16 * c, acc[0][1]);
-                            tmem_wait_ld(acc[0]);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                uint32_t& w = acc[0][i >> 3][i & 7];
-                                const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(corr[(i >> 3) * 2 + ((i >> 1) & 1)]));
-                                w = *reinterpret_cast<const uint32_t*>(&x);
-                            }
-                            tmem_st_16x16(s_at + 16 * c, acc[0][0]);
-                            tmem_st_16x16(s_at + (16u << 16) + 16 * c, acc[0][1]);
-                        }
-                    }
-                    const float ratio = unit == 0.f ? 0.f : u / unit;  // (the unit moves between tiles only)
-                    unit = u;
-                    if (t == 0) continue;
-                    mbar_wait(bar_o + 8 * half, (t - 1) & 1, abort_flag, WAIT_O, t);
-                    tc_fence_after();
-#pragma unroll 1
-                    for (int c = 0; c < PD / 16; ++c) {
-                        tmem_ld_16x16(o_at + 16 * c, acc[0][0]);
-                        tmem_ld_16x16(o_at + (16u << 16) + 16 * c, acc[0][1]);
-                        tmem_wait_ld(acc[0]);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            acc[0][i >> 3][i & 7] = __float_as_uint(__uint_as_float(acc[0][i >> 3][i & 7]) * (corr[(i >> 3) * 2 + ((i >> 1) & 1)] * ratio));
-                        tmem_st_16x16(o_at + 16 * c, acc[0][0]);
-                        tmem_st_16x16(o_at + (16u << 16) + 16 * c, acc[0][1]);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) l[i] += sum[i];
-                tmem_st_16x32(s_at + 32 * h, p[0]);  // (over scores that have been taken)
-                tmem_st_16x32(s_at + (16u << 16) + 32 * h, p[1]);
-                if (h == 0 && halves == 2 && (half == 0 || t + 1 < used)) turn_pass(half);
-            }
-            tmem_wait_st();
-            tc_fence_before();
-            tile_sync(half);
-            if (issuer) {
-                tc_fence_after();
-                issue_o(t, t + 1 == used);
-                if (t + 1 < used) issue_s(t + 1);  // behind O(t) on the pipe: P(t) is read before scores go over it
-            }
-        }
-        // ---- out = O / (unit l), one row per thread again
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-            if (c0 == 0) row_info[half * TQ + (warp & 3) * 32 + 8 * i + g] = make_float2(m[i], l[i]);
-        }
-        __syncwarp();
-        const float2 ml = row_info[r];
-        if (used > 0) {
-            mbar_wait(bar_o + 8 * half, (used - 1) & 1, abort_flag, WAIT_O, used);
-            tc_fence_after();
-        }
-        const size_t id = (size_t)token * a.heads + head, part = (size_t)blockIdx.y * a.b.n_tokens * a.heads + id;
         const bool split = a.tc_splits > 1;
-        const float inv = unit == 0.f ? 0.f : split ? 1.f / unit : ml.y != 0.f ? 1.f / ml.y / unit : 0.f;
-        if (split && mine) a.part_ml[part] = ml;
-        // Through the place of the warp's query rows, which the last scores have been taken from: 16 bytes of its row at a time
-        // from a thread, eight of one to each lane to memory.
-        uint8_t* stage = smem + C::Q_AT + half * C::BUF + (warp & 3) * 64 * PD;
-        const size_t to = split ? part * 128 : (size_t)token * a.out_stride + (size_t)head * a.l.hd;
+        // Query rows come through the place of their fp16 form, those of the next item while the last weights of this one are
+        // multiplied and its outputs stored.  Queries and outputs move four entries to a lane, whole rows to an instruction
+        // (with a row to a thread they were a fifth of the time of a prompt).
         constexpr int UNITS = PD / 4, AT_ONCE = 32 / UNITS;
-        auto put = [&](int chunk, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
-            *reinterpret_cast<uint4*>(stage + lane * 2 * PD + ((chunk ^ (lane & 7)) << 4)) = make_uint4(x, y, z, w);
+        const int u = lane % UNITS, sub = lane / UNITS;
+        uint8_t* queries = smem + C::Q_AT + half * C::BUF + (warp & 3) * 64 * PD;
+        int index = blockIdx.x, k = 0, u0 = 0;  // u0: tiles of positions that this tile of rows has taken
+        auto place_of = [&](int& token, int& head) {  // of this thread's row; without one, of the item's last
+            const uint32_t n = (uint32_t)it.r0 + min(r, it.rows - 1);  // (rows of a call are counted in 31 bits)
+            token = it.start + (int)(n / (uint32_t)a.group), head = it.kvh * a.group + (int)(n % (uint32_t)a.group);
         };
-        auto store_rows = [&](uint8_t* base, int elem, int width) {  // elem: bytes of an entry; width: bytes of a row that there are
-            __syncwarp();
-            const int u = lane % UNITS, sub = lane / UNITS;
+        auto fetch = [&]() {
+            int token, head;
+            place_of(token, head);
+            const size_t from = (size_t)token * a.q_stride + (size_t)head * a.l.hd;
 #pragma unroll 8
             for (int i = 0; i < UNITS; ++i) {
                 const int j = AT_ONCE * i + sub;
-                const size_t at = __shfl_sync(0xffffffffu, (unsigned long long)to, j);
-                const uint2 v = *reinterpret_cast<const uint2*>(stage + j * 2 * PD + (((u >> 1) ^ (j & 7)) << 4) + 8 * (u & 1));
-                if (r - lane + j < rows && 8 * u < width) *reinterpret_cast<uint2*>(base + at * elem + 8 * u) = v;
+                const size_t at = __shfl_sync(0xffffffffu, (unsigned long long)from, j);
+                const bool real = r - lane + j < it.rows && 4 * u < a.l.hd;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(smem_u32(queries) + j * 2 * PD + 8 * u), "l"(a.q + (real ? at + 4 * u : 0)),
+                             "r"(real ? 8 : 0)
+                             : "memory");
             }
-            __syncwarp();
         };
-#pragma unroll
-        for (int c = 0; c < PD / 32; ++c) {
-            uint32_t acc[32];
-            float y[32];
-            if (used > 0) {  // (the same for the whole warp)
-                tmem_ld32(o_at + 32 * c, acc);
-                tmem_wait_ld();
-            } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) acc[i] = 0u;
+        auto take = [&]() {  // the item `index`
+            there = index >= 0 && item_of(a, index, lane, it);
+            if (there) fetch();
+        };
+        fetch();
+#pragma unroll 1
+        while (index >= 0) {
+            if (threadIdx.x == 0) q_tops[(k + 1) % 3] = 0;  // (read for the last time before the queries_sync of k - 1)
+            if (!there) {
+                queries_sync();
+                index = item_after(++k);
+                take();
+                continue;
             }
+            uint32_t* q_top = q_tops + k % 3;
+            const int rows = it.rows, halves = it.halves;
+            // ---- the query rows to fp16 by a power of two, in the order of the converted codes
+            {
+                uint2 x[UNITS];
+                float mx = 0.f;
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) y[entry_of<BITS>(i)] = inv == 0.f ? 0.f : __uint_as_float(acc[i]) * inv;
-            if (split) {
-                constexpr int HALF = PD / 64;  // 32-column blocks that the place holds as fp32
+                for (int i = 0; i < UNITS; ++i) {
+                    x[i] = *reinterpret_cast<const uint2*>(queries + (AT_ONCE * i + sub) * 2 * PD + 8 * u);
+                    mx = fmaxf(mx, fmaxf(fmaxf(fabsf(__uint_as_float(x[i].x << 16)), fabsf(__uint_as_float(x[i].x & 0xffff0000u))),
+                                         fmaxf(fabsf(__uint_as_float(x[i].y << 16)), fabsf(__uint_as_float(x[i].y & 0xffff0000u)))));
+                }
+                const uint32_t top = __reduce_max_sync(0xffffffffu, mx <= 3.4e38f ? __float_as_uint(mx) : 0u);
+                if (lane == 0) atomicMax(q_top, top);
+                row_info[r].x = __int_as_float(it.pos0 + (int)(((uint32_t)it.r0 + min(r, rows - 1)) / (uint32_t)a.group));
+                queries_sync();
+                const int e = query_exponent(*q_top);
+                const float up0 = power_of_two(e / 2), up1 = power_of_two(e - e / 2);  // (2^e may be past fp32)
+                auto halves_of = [&](uint32_t w) {
+                    const __half2 h = __floats2half2_rn(__uint_as_float(w << 16) * up0 * up1, __uint_as_float(w & 0xffff0000u) * up0 * up1);
+                    return *reinterpret_cast<const uint32_t*>(&h);
+                };
+                // Entries n and n + 16 (n + 4 at 4 bits) side by side: of two lanes that far apart, either gives two entries to the
+                // other.  At 8 bits the pairs (n, n + 2) are the lane's own.
+                constexpr int APART = BITS == 3 ? 4 : BITS == 4 ? 1 : 0;
+                const bool upper = (u & APART) != 0;
+                const int place = BITS == 3 ? (4 * u & ~31) + 8 * (u & 3) + (u & 4) : 4 * u;
+                uint8_t* dst = smem + C::Q_AT + half * C::BUF + place / 64 * PANEL + (place & 4) * 2;
 #pragma unroll
-                for (int i = 0; i < 32; i += 4)
-                    put(8 * (c % HALF) + i / 4, __float_as_uint(y[i]), __float_as_uint(y[i + 1]), __float_as_uint(y[i + 2]), __float_as_uint(y[i + 3]));
-                if (c % HALF == HALF - 1) store_rows(reinterpret_cast<uint8_t*>(a.part_o) + 128 * (c - HALF + 1), 4, a.l.hd * 4 - 128 * (c - HALF + 1));
-            } else {
-#pragma unroll
-                for (int i = 0; i < 32; i += 8) {
-                    uint32_t w[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const __nv_bfloat162 v = __floats2bfloat162_rn(y[i + 2 * k], y[i + 2 * k + 1]);
-                        w[k] = *reinterpret_cast<const uint32_t*>(&v);
+                for (int i = 0; i < UNITS; ++i) {
+                    const int at = (warp & 3) * 32 + AT_ONCE * i + sub;
+                    uint32_t lo = halves_of(x[i].x), hi = halves_of(x[i].y);
+                    if constexpr (APART > 0) {
+                        const uint32_t got = __shfl_xor_sync(0xffffffffu, upper ? lo : hi, APART);
+                        lo = upper ? got : lo, hi = upper ? hi : got;
                     }
-                    put(4 * c + i / 8, w[0], w[1], w[2], w[3]);
+                    *reinterpret_cast<uint2*>(dst + at * 128 + (((place / 8 % 8) ^ (at & 7)) << 4)) =
+                        make_uint2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            }
+            // ---- MMAs of this tile: by one thread, once all have done their part
+            constexpr uint32_t idesc_s = idesc_f16(TQ, TK, false), idesc_o = idesc_f16(TQ, PD, true);
+            const uint32_t t_s = tmem + COL_S + TK * half, t_o = tmem + COL_O + 128 * half;
+            auto wait_full = [&](int n) {
+                mbar_wait(bar_full + 8 * (n % RING), n / RING & 1, abort_flag, WAIT_FULL, n);
+                tc_fence_after();
+                return ring + n % RING * C::BUF;
+            };
+            const uint64_t q_desc = smem_desc(sq + half * C::BUF);
+            auto issue_s = [&](int t) {
+                const uint64_t k_desc = smem_desc(wait_full(2 * (n0 + t)));
+                if (elect()) {
+#pragma unroll
+                    for (int ks = 0; ks < PD / 16; ++ks) {
+                        constexpr int STEP = PANEL / 16;  // of a descriptor's address, per 64 entries
+                        mma_ss(t_s, q_desc + ks / 4 * STEP + 2 * (ks % 4), k_desc + ks / 4 * STEP + 2 * (ks % 4), idesc_s, ks != 0);
+                    }
+                    tc_commit(bar_s + 8 * half);
+                    for (int i = halves; i < 3; ++i) tc_commit(bar_empty + 8 * (2 * (n0 + t) % RING));  // (for a second tile without rows too)
+                }
+                __syncwarp();
+            };
+            auto issue_o = [&](int t) {
+                const uint64_t v_desc = smem_desc(wait_full(2 * (n0 + t) + 1));
+                if (elect()) {
+                    mma_ts(t_o, t_s, v_desc, idesc_o, t != 0);
+#pragma unroll
+                    for (int j = 1; j < TK / 16; ++j) mma_ts(t_o, t_s + 8 * j, v_desc + 2048 / 16 * j, idesc_o, 1);
+                    tc_commit(bar_o + 8 * half);
+                    for (int i = halves; i < 3; ++i) tc_commit(bar_empty + 8 * ((2 * (n0 + t) + 1) % RING));
+                }
+                __syncwarp();
+            };
+            const bool issuer = (warp & 3) == 0;
+            const int used = half < halves ? it.n_tiles : 0;
+            tile_sync(half);  // the query rows are in place
+            if (issuer && used > 0) issue_s(0);
+            // the four rows of this thread between loads and stores: lanes g, g + 8, g + 16, g + 24 of the warp
+            const int g = lane >> 2, c0 = 2 * (lane & 3);
+            float m[4], l[4], unit = 0.f;
+            int lim[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                lim[i] = __float_as_int(row_info[half * TQ + (warp & 3) * 32 + 8 * i + g].x);
+                m[i] = -1e30f, l[i] = 0.f;
+            }
+            const int lim_lo = __reduce_min_sync(0xffffffffu, min(min(lim[0], lim[1]), min(lim[2], lim[3])));
+            const int lim_hi = __reduce_max_sync(0xffffffffu, max(max(lim[0], lim[1]), max(lim[2], lim[3])));
+            if (halves == 2 && half == 1 && used > 0) turn_pass(1);
+            for (int t = 0; t < used; ++t) {
+                mbar_wait(bar_s + 8 * half, (u0 + t) & 1, abort_flag, WAIT_S, t);
+                tc_fence_after();
+                const TileScales& ts = scales[(n0 + t) % SCALES];
+                const int base = it.span.block(it.v0 + t) * TK;
+                const uint4 dead = *reinterpret_cast<const uint4*>(ts.dead);
+                const bool whole = base + TK - 1 <= lim_lo && (window == 0 || base > lim_hi - window || base + TK - 1 < sinks) &&
+                                   (dead.x | dead.y | dead.z | dead.w) == 0;
+                if (!whole) {  // the scores that a row does not see become -inf
+#pragma unroll 1
+                    for (int c = 0; c < TK / 16; ++c) {
+                        uint32_t acc[2][8];
+                        tmem_ld_16x16(s_at + 16 * c, acc[0]);
+                        tmem_ld_16x16(s_at + (16u << 16) + 16 * c, acc[1]);
+                        tmem_wait_ld(acc);
+                        const uint32_t gone = ts.dead[c >> 1] >> (16 * (c & 1) + c0);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int n = 16 * c + 8 * ((i >> 2) & 1) + c0 + (i & 1), to = lim[(i >> 3) * 2 + ((i >> 1) & 1)] - base;
+                            const bool seen = n <= to && (window == 0 || n > to - window || n < sinks - base) && !((gone >> (8 * ((i >> 2) & 1) + (i & 1))) & 1);
+                            if (!seen) acc[i >> 3][i & 7] = 0xff800000u;
+                        }
+                        tmem_st_16x16(s_at + 16 * c, acc[0]);
+                        tmem_st_16x16(s_at + (16u << 16) + 16 * c, acc[1]);
+                    }
+                    tmem_wait_st();
+                }
+                if (halves == 2) turn_wait(half);
+                // ---- 64 columns, then the other 64
+#pragma unroll 1
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t p[2][16];  // weights, two columns to a word
+                    float sum[4];
+                    for (bool settled = false;; settled = true) {
+                        // weights and sums of 2^(score - m), 16 columns at a time, the next 16 under way meanwhile
+                        f2 m_2[4], sum_2[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) m_2[i] = pack2(-m[i], -m[i]), sum_2[i] = pack2(0.f, 0.f);
+                        uint32_t acc[2][2][8];
+                        tmem_ld_16x16(s_at + 64 * h, acc[0][0]);
+                        tmem_ld_16x16(s_at + (16u << 16) + 64 * h, acc[0][1]);
+                        ulonglong2 scale[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) scale[k] = *reinterpret_cast<const ulonglong2*>(ts.scale[32 * h + 4 * k + c0 / 2]);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            tmem_wait_ld(acc[c & 1]);
+                            if (c < 3) {
+                                tmem_ld_16x16(s_at + 64 * h + 16 * (c + 1), acc[(c + 1) & 1][0]);
+                                tmem_ld_16x16(s_at + (16u << 16) + 64 * h + 16 * (c + 1), acc[(c + 1) & 1][1]);
+                            }
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const uint32_t* from = acc[c & 1][i >> 1] + 4 * k + 2 * (i & 1);
+                                    float y0, y1, w0, w1;
+                                    unpack2(fma2(pack2(__uint_as_float(from[0]), __uint_as_float(from[1])), scale[2 * c + k].x, m_2[i]), y0, y1);
+                                    const f2 e = pack2(exp2_approx(y0), exp2_approx(y1));
+                                    sum_2[i] = add2(sum_2[i], e);
+                                    unpack2(mul2(e, scale[2 * c + k].y), w0, w1);
+                                    const __half2 w = __floats2half2_rn(w0, w1);
+                                    p[i >> 1][2 * (2 * c + k) + (i & 1)] = *reinterpret_cast<const uint32_t*>(&w);
+                                }
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float s0, s1;
+                            unpack2(sum_2[i], s0, s1);
+                            sum[i] = s0 + s1;
+                        }
+                        const float u = ts.unit;
+                        const bool high = u != unit || fmaxf(fmaxf(sum[0], sum[1]), fmaxf(sum[2], sum[3])) > 512.f;
+                        if (settled || !__any_sync(0xffffffffu, high)) break;
+                        // ---- rarely: references to the largest scores of these columns where those are higher (rounded up to
+                        // whole numbers: what moves along then moves by powers of two), and with them O, and the first columns'
+                        // weights while the second's are taken
+                        float corr[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) corr[i] = -INFINITY;
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            tmem_ld_16x16(s_at + 64 * h + 16 * c, acc[0][0]);
+                            tmem_ld_16x16(s_at + (16u << 16) + 64 * h + 16 * c, acc[0][1]);
+                            tmem_wait_ld(acc[0]);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const int row = (i >> 3) * 2 + ((i >> 1) & 1);
+                                corr[row] = fmaxf(corr[row], __uint_as_float(acc[0][i >> 3][i & 7]) *
+                                                                 ts.scale[32 * h + 8 * c + 4 * ((i >> 2) & 1) + c0 / 2][i & 1]);
+                            }
+                        }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            corr[i] = fmaxf(corr[i], __shfl_xor_sync(0xffffffffu, corr[i], 1));
+                            corr[i] = fmaxf(corr[i], __shfl_xor_sync(0xffffffffu, corr[i], 2));
+                            const float m_new = fmaxf(m[i], ceilf(corr[i]));
+                            corr[i] = exp2_approx(m[i] - m_new);
+                            m[i] = m_new;
+                            l[i] *= corr[i];
+                        }
+                        if (h > 0) {
+#pragma unroll 1
+                            for (int c = 0; c < 2; ++c) {  // (16 words are 32 weights)
+                                tmem_ld_16x16(s_at + 16 * c, acc[0][0]);
+                                tmem_ld_16x16(s_at + (16u << 16) + 16 * c, acc[0][1]);
+                                tmem_wait_ld(acc[0]);
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) {
+                                    uint32_t& w = acc[0][i >> 3][i & 7];
+                                    const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(corr[(i >> 3) * 2 + ((i >> 1) & 1)]));
+                                    w = *reinterpret_cast<const uint32_t*>(&x);
+                                }
+                                tmem_st_16x16(s_at + 16 * c, acc[0][0]);
+                                tmem_st_16x16(s_at + (16u << 16) + 16 * c, acc[0][1]);
+                            }
+                        }
+                        const float ratio = unit == 0.f ? 0.f : u / unit;  // (the unit moves between tiles only)
+                        unit = u;
+                        if (t == 0) continue;
+                        mbar_wait(bar_o + 8 * half, (u0 + t - 1) & 1, abort_flag, WAIT_O, t);
+                        tc_fence_after();
+#pragma unroll 1
+                        for (int c = 0; c < PD / 16; ++c) {
+                            tmem_ld_16x16(o_at + 16 * c, acc[0][0]);
+                            tmem_ld_16x16(o_at + (16u << 16) + 16 * c, acc[0][1]);
+                            tmem_wait_ld(acc[0]);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                acc[0][i >> 3][i & 7] = __float_as_uint(__uint_as_float(acc[0][i >> 3][i & 7]) * (corr[(i >> 3) * 2 + ((i >> 1) & 1)] * ratio));
+                            tmem_st_16x16(o_at + 16 * c, acc[0][0]);
+                            tmem_st_16x16(o_at + (16u << 16) + 16 * c, acc[0][1]);
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) l[i] += sum[i];
+                    tmem_st_16x32(s_at + 32 * h, p[0]);  // (over scores that have been taken)
+                    tmem_st_16x32(s_at + (16u << 16) + 32 * h, p[1]);
+                    if (h == 0 && halves == 2 && (half == 0 || t + 1 < used)) turn_pass(half);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                tile_sync(half);
+                if (issuer) {
+                    tc_fence_after();
+                    issue_o(t);
+                    if (t + 1 < used) issue_s(t + 1);  // behind O(t) on the pipe: P(t) is read before scores go over it
                 }
             }
+            // ---- out = O / (unit l), one row per thread again
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+                if (c0 == 0) row_info[half * TQ + (warp & 3) * 32 + 8 * i + g] = make_float2(m[i], l[i]);
+            }
+            __syncwarp();
+            const float2 ml = row_info[r];
+            int token, head;
+            place_of(token, head);
+            const size_t id = (size_t)token * a.heads + head, part = (size_t)it.part * a.b.n_tokens * a.heads + id;
+            const float inv = unit == 0.f ? 0.f : split ? 1.f / unit : ml.y != 0.f ? 1.f / ml.y / unit : 0.f;
+            if (split && r < rows) a.part_ml[part] = ml;
+            const size_t to = split ? part * 128 : (size_t)token * a.out_stride + (size_t)head * a.l.hd;
+            n0 += it.n_tiles;
+            index = item_after(++k);
+            take();
+            if (used > 0) {
+                mbar_wait(bar_o + 8 * half, (u0 + used - 1) & 1, abort_flag, WAIT_O, used);
+                tc_fence_after();
+            }
+            u0 += used;
+            // 64 bytes of each row at a time through shared memory: 16 of its row from a thread, eight of one to each lane to memory
+            uint8_t* stage = smem + C::OUT_AT + warp * 32 * 64;
+            auto put = [&](int chunk, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+                *reinterpret_cast<uint4*>(stage + lane * 64 + ((chunk ^ ((lane >> 1) & 3)) << 4)) = make_uint4(x, y, z, w);
+            };
+            auto store_rows = [&](uint8_t* base, int elem, int width) {  // elem: bytes of an entry; width: bytes of a row that there are
+                __syncwarp();
+                const int u = lane & 7;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int j = 4 * i + (lane >> 3);
+                    const size_t at = __shfl_sync(0xffffffffu, (unsigned long long)to, j);
+                    const uint2 v = *reinterpret_cast<const uint2*>(stage + j * 64 + (((u >> 1) ^ ((j >> 1) & 3)) << 4) + 8 * (u & 1));
+                    if (r - lane + j < rows && 8 * u < width) *reinterpret_cast<uint2*>(base + at * elem + 8 * u) = v;
+                }
+                __syncwarp();
+            };
+#pragma unroll
+            for (int c = 0; c < PD / 32; ++c) {
+                uint32_t acc[32];
+                float y[32];
+                if (used > 0) {  // (the same for the whole warp)
+                    tmem_ld32(o_at + 32 * c, acc);
+                    tmem_wait_ld();
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) acc[i] = 0u;
+                }
+#pragma unroll
+                for (int i = 0; i < 32; ++i) y[entry_of<BITS>(i)] = inv == 0.f ? 0.f : __uint_as_float(acc[i]) * inv;
+                if (split) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float* v = y + 16 * h + 4 * i;
+                            put(i, __float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+                        }
+                        store_rows(reinterpret_cast<uint8_t*>(a.part_o) + 128 * c + 64 * h, 4, a.l.hd * 4 - 128 * c - 64 * h);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) {
+                            const __nv_bfloat162 v = __floats2bfloat162_rn(y[8 * i + 2 * n], y[8 * i + 2 * n + 1]);
+                            w[n] = *reinterpret_cast<const uint32_t*>(&v);
+                        }
+                        put(i, w[0], w[1], w[2], w[3]);
+                    }
+                    store_rows(reinterpret_cast<uint8_t*>(a.out) + 64 * c, 2, a.l.hd * 2 - 64 * c);
+                }
+            }
+            tc_fence_before();
         }
-        if (!split) store_rows(reinterpret_cast<uint8_t*>(a.out), 2, a.l.hd * 2);
     }
     tc_fence_before();
     __syncthreads();
@@ -809,7 +937,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
 template <int BITS, int PD>
 cudaError_t launch(const AttnArgs& a, cudaStream_t st) {
     const long long tiles = a.tc_tiles > 0 ? (long long)a.tc_tiles * a.b.n_seqs : (long long)a.b.n_tokens * a.group / a48p::TILE_ROWS + a.b.n_seqs;
-    const dim3 grid((unsigned)(tiles * a.l.kv_heads), a.tc_splits);
+    const dim3 grid((unsigned)(tiles * a.l.kv_heads * a.tc_splits));
     static bool allowed[64];
     const cudaError_t e = a48_allow_smem(attn_paged_tc_kernel<BITS, PD>, Cfg<PD>::SMEM, allowed);
     return e != cudaSuccess ? e : a48_launch_pdl(attn_paged_tc_kernel<BITS, PD>, grid, dim3(THREADS), (size_t)Cfg<PD>::SMEM, st, a);
