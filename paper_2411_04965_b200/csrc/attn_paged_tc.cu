@@ -25,6 +25,16 @@
 //                    free of conflicts; the next tile's codes and the page numbers of the one after it under way
 //                    meanwhile.  A ring of four buffers, K(t) V(t) K(t+1) V(t+1).
 // Tensor memory: two score tiles (128 columns, P over the first 64) and two output tiles (up to 128 columns).
+//
+// A CTA that is through with its rows cancels one that has not started and takes its rows over, so that the codes and queries
+// of the next rows are under way while the last weights are multiplied and outputs stored: four prompts of 4096 tokens, 32
+// heads of 128, 3 bits, 821 us (669 TFLOP/s of the 4 x 128 operations per score), 854 with one CTA to each.  What bounds it:
+// 128 positions take a CTA about 4500 clocks, of which the products of both tiles occupy the tensor pipe for 2600.  A tile
+// needs 250 clocks from its scores to the first weights, 2400 for the weights (1400 for the 64 columns taken while the other
+// tile takes its last 64, 1000 for the others; their exponentials alone are 1024 clocks of the SFUs) and 1300 for O and the
+// next S; with no room for a second score tile in tensor memory these follow one another.  Without the exponentials it
+// would be 749 us, without the conversion to fp16 829.  Tiles of 64 positions, with two score tiles each, took 1015 us (against 917 then): the
+// products of 64 columns are bound by shared memory.  Without the two tiles' turns 866.
 // Every wait is bounded; one that gives up records itself (bitnet_a48_kernel_status), and every later wait of the CTA then
 // falls through, so that the kernel ends by itself.
 #include <climits>
