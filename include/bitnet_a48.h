@@ -331,7 +331,9 @@ bitnet_a48_status bitnet_a48_attention_prefill(const float* q_dev, const float* 
  * The three arrays are device memory (4-byte aligned), read when the call runs: a captured graph may be replayed with other
  * contents.  n_tokens: rows of the token arrays, rows outside q_start[0] .. q_start[n_seqs]-1 are neither read nor written.
  * max_q, max_kv: upper bounds of the new tokens and of the positions of one sequence; they size the launch.  More than
- * max_q new tokens of a sequence: those past max_q get no attention output.  A position without a page (negative, past the
+ * max_q new tokens of a sequence: those past max_q may get no attention output.  Limits (BITNET_A48_ERR_LIMIT past them):
+ * n_seqs and n_heads 65535, n_tokens and max_pages*page_size 2^30, n_tokens*n_heads 2^31 - 1, n_kv_heads*n_seqs
+ * (2^31 - 1) / 8.  A position without a page (negative, past the
  * table, or an entry outside 0 .. n_pages-1) is not stored, reads as zero, and is not attended to; nothing faults.
  *
  * Alignment: the pool, read outputs and the workspace 16 bytes; q, k, v and out four elements (a slice of a fused

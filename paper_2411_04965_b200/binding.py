@@ -483,7 +483,7 @@ class PagedCache:
         if pool is None:
             pool = torch.zeros(self.nbytes, dtype=torch.uint8, device=device)
         assert pool.is_cuda and pool.is_contiguous() and pool.numel() * pool.element_size() >= self.nbytes
-        self.pool, self.pool_ptr = pool, pool.data_ptr()
+        self.pool, self.pool_ptr, self.device_index = pool, pool.data_ptr(), pool.get_device()
         self.bits, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages = bits, n_kv_heads, head_dim, page_size, n_pages
 
 
@@ -492,10 +492,10 @@ class PagedBatch:
 
     def __init__(self, q_start: torch.Tensor, kv_len: torch.Tensor, pages: torch.Tensor, n_tokens: int, max_q: int, max_kv: int):
         for t in (q_start, kv_len, pages):
-            assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()
+            assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous() and t.get_device() == pages.get_device()
         n_seqs, max_pages = pages.shape
         assert kv_len.shape == (n_seqs,) and q_start.shape == (n_seqs + 1,)
-        self.q_start, self.kv_len, self.pages, self.n_tokens = q_start, kv_len, pages, n_tokens
+        self.q_start, self.kv_len, self.pages, self.n_tokens, self.device_index = q_start, kv_len, pages, n_tokens, pages.get_device()
         self.view = PagedBatchView(n_seqs, n_tokens, max_q, max_kv, max_pages, q_start.data_ptr(), kv_len.data_ptr(), pages.data_ptr())
         self.view_ref = byref(self.view)
 
@@ -510,12 +510,13 @@ def _on_stream(t: torch.Tensor, stream):
 
 
 def _made_current(t: torch.Tensor, stream):
+    assert t.is_cuda and (stream is None or stream.device == t.device)
     return torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(t.device))
 
 
-def _rows(t: torch.Tensor, n_tokens: int, width: int, dtype) -> int:
-    """Stride of token rows [n_tokens, width] whose columns are contiguous."""
-    assert t.is_cuda and t.dtype == dtype and t.shape == (n_tokens, width)
+def _rows(t: torch.Tensor, cache: "PagedCache", n_tokens: int, width: int, dtype) -> int:
+    """Stride of token rows [n_tokens, width] on the cache's device whose columns are contiguous."""
+    assert t.get_device() == cache.device_index and t.dtype == dtype and t.shape == (n_tokens, width)
     stride, one = t.stride()
     assert one == 1 or width == 1
     return stride if n_tokens > 1 else max(stride, width)
@@ -525,6 +526,7 @@ def paged_write(cache: PagedCache, batch: PagedBatch, k: torch.Tensor, v: torch.
                 eps: float = 1e-5, q_out=None, stream=None):
     """Rotates (rope_base 0: does not), quantises and stores k, v [n_tokens, n_kv_heads*head_dim] (fp32 or bf16, rows may be
     strided); rotates q [n_tokens, n_heads*head_dim] into q_out (bf16, made here unless given).  Returns q_out."""
+    assert cache.device_index == batch.device_index
     st = _on_stream(k, stream)
     if st is None:
         with _made_current(k, stream):
@@ -532,16 +534,16 @@ def paged_write(cache: PagedCache, batch: PagedBatch, k: torch.Tensor, v: torch.
     n, width, dtype = batch.n_tokens, cache.n_kv_heads * cache.head_dim, k.dtype
     bf16 = dtype == torch.bfloat16
     assert bf16 or dtype == torch.float32
-    ks, vs = _rows(k, n, width, dtype), _rows(v, n, width, dtype)
+    ks, vs = _rows(k, cache, n, width, dtype), _rows(v, cache, n, width, dtype)
     if q is None:
         assert q_out is None
         qp, qs, op, os_, heads = None, 0, None, 0, 0
     else:
         heads = q.shape[1] // cache.head_dim
-        qs = _rows(q, n, heads * cache.head_dim, dtype)
+        qs = _rows(q, cache, n, heads * cache.head_dim, dtype)
         if q_out is None:
             q_out = torch.empty(n, heads * cache.head_dim, dtype=torch.bfloat16, device=q.device)
-        qp, op, os_ = q.data_ptr(), q_out.data_ptr(), _rows(q_out, n, heads * cache.head_dim, torch.bfloat16)
+        qp, op, os_ = q.data_ptr(), q_out.data_ptr(), _rows(q_out, cache, n, heads * cache.head_dim, torch.bfloat16)
     _check(_lib.bitnet_a48_paged_write(cache.cfg_ref, cache.pool_ptr, batch.view_ref, heads, qp, qs, k.data_ptr(), ks, v.data_ptr(), vs,
                                        bf16, rope_base, eps, op, os_, st), "paged_write")
     return q_out
@@ -549,6 +551,7 @@ def paged_write(cache: PagedCache, batch: PagedBatch, k: torch.Tensor, v: torch.
 
 def paged_read(cache: PagedCache, batch: PagedBatch, dtype=torch.bfloat16, k_out=None, v_out=None, stream=None):
     """The keys and values at the positions of the batch's tokens, [n_tokens, n_kv_heads, head_dim] each, fp32 or bf16."""
+    assert cache.device_index == batch.device_index
     st = _on_stream(cache.pool, stream)
     if st is None:
         with _made_current(cache.pool, stream):
@@ -558,7 +561,7 @@ def paged_read(cache: PagedCache, batch: PagedBatch, dtype=torch.bfloat16, k_out
     k_out = k_out if k_out is not None else torch.empty(shape, dtype=dtype, device=cache.pool.device)
     v_out = v_out if v_out is not None else torch.empty(shape, dtype=dtype, device=cache.pool.device)
     for t in (k_out, v_out):
-        assert t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.shape == shape
+        assert t.get_device() == cache.device_index and t.dtype == dtype and t.is_contiguous() and t.shape == shape
     _check(_lib.bitnet_a48_paged_read(cache.cfg_ref, cache.pool_ptr, batch.view_ref, k_out.data_ptr(), v_out.data_ptr(),
                                       dtype == torch.bfloat16, st), "paged_read")
     return k_out, v_out
@@ -571,18 +574,20 @@ def attention_paged_workspace_bytes(cache: PagedCache, batch: PagedBatch, n_head
 def attention_paged(cache: PagedCache, batch: PagedBatch, q: torch.Tensor, scale: float = 0.0, window: int = 0, sinks: int = 0,
                     out=None, workspace=None, stream=None) -> torch.Tensor:
     """Causal attention of q bf16 [n_tokens, n_heads*head_dim] over the cache; rows may be strided.  Returns bf16."""
+    assert cache.device_index == batch.device_index
     st = _on_stream(q, stream)
     if st is None:
         with _made_current(q, stream):
             return attention_paged(cache, batch, q, scale, window, sinks, out, workspace)
     heads = q.shape[1] // cache.head_dim
     width = heads * cache.head_dim
-    qs = _rows(q, batch.n_tokens, width, torch.bfloat16)
+    qs = _rows(q, cache, batch.n_tokens, width, torch.bfloat16)
     if out is None:
         out = torch.empty(batch.n_tokens, width, dtype=torch.bfloat16, device=q.device)
-    os_ = _rows(out, batch.n_tokens, width, torch.bfloat16)
+    os_ = _rows(out, cache, batch.n_tokens, width, torch.bfloat16)
     wp, given = None, 0
     if workspace is not None:
+        assert workspace.get_device() == cache.device_index and workspace.is_contiguous()
         wp, given = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     else:
         need = _lib.bitnet_a48_attention_paged_workspace_bytes(cache.cfg_ref, batch.view_ref, heads, window, sinks)

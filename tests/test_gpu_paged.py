@@ -399,3 +399,179 @@ def test_shared_prefix_and_many_sequences(a48, cuda_dev):
     s.batch = s.view(s.q_start, s.kv_len, s.n_tokens)
     q = torch.tensor(rng.standard_normal((s.n_tokens, heads * hd)), dtype=torch.float32).to(torch.bfloat16)
     check_attention(s, q, heads)
+
+
+# ------------------------------------------------------------------------------------------------ as they are used
+def test_layer_over_the_cache(a48, cuda_dev):
+    """q/k/v BitLinears, write, attention, output BitLinear: prompts of unlike lengths, then tokens one at a time by a captured
+    graph.  The attention of every step is the oracle's over the rows that the projections gave."""
+    rng = np.random.default_rng(21)
+    H, heads, kvh, hd, page, B, k_o = 256, 4, 2, 64, 16, 3, 128
+    lens = np.array([90, 1, 37])
+    steps, eps = 4, 1e-5
+    total = lens + steps
+    w = {n: a48.pack_ternary(torch.tensor(rng.standard_normal((m, H if n != "o" else heads * hd)), dtype=torch.float32, device=cuda_dev))
+         for n, m in (("q", heads * hd), ("k", kvh * hd), ("v", kvh * hd), ("o", H))}
+    s = Setup(a48, cuda_dev, 3, kvh, hd, page, [0] * B, total, seed=9)
+
+    def layer(x, batch, bufs=None):
+        codes, scale = a48.quant_int4_bf16(x, eps)
+        q, k, v = (a48.linear_bf16(w[n], codes, scale) for n in "qkv")
+        qr = a48.paged_write(s.cache, batch, k, v, q=q)
+        y = a48.attention_paged(s.cache, batch, qr)
+        c8, s8 = a48.topk_quant_int8_bf16(y, k_o, eps)
+        return k, v, qr, y, a48.linear_bf16(w["o"], c8, s8, kind=a48.ACT_TOPK_INT8)
+
+    def check(q_start, kv_len, parts):
+        k, v, qr, y, out = (t.double().cpu().numpy() for t in parts)
+        s.oracle.write(q_start, kv_len, s.table, k, v, 10000.0, EPS32)
+        ref, mag, top = s.oracle.attend(q_start, kv_len, s.table, qr, heads)
+        vmax = np.abs(s.oracle.scales[1]).max() * 128
+        assert (np.abs(y.reshape(ref.shape) - ref) <= attention_bound(ref, mag, top, hd, vmax)).all()
+        assert np.isfinite(out).all() and (out != 0).any(axis=1).all()
+
+    x = torch.tensor(rng.standard_normal((int(lens.sum()), H)), dtype=torch.float32).to(torch.bfloat16).to(cuda_dev)
+    q_start = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    check(q_start, lens, layer(x, s.view(q_start, lens, int(lens.sum()))))
+
+    q_start = np.arange(B + 1, dtype=np.int32)
+    batch = s.view(q_start, lens + 1, B, max_q=1, max_kv=int(total.max()))
+    xs = torch.zeros(B, H, dtype=torch.bfloat16, device=cuda_dev)
+    pool = s.cache.pool.clone()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        layer(xs, batch)
+    stream.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        parts = layer(xs, batch)
+    s.cache.pool.copy_(pool)
+    for step in range(1, steps + 1):
+        xs.copy_(torch.tensor(rng.standard_normal((B, H))))
+        batch.kv_len.copy_(torch.tensor(lens + step, dtype=torch.int32))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        check(q_start, lens + step, parts)
+        eager = layer(xs, batch)  # (writes the same codes again)
+        assert all(torch.equal(a, b) for a, b in zip(parts, eager))
+    assert a48.kernel_status()[0] == 0
+
+
+@pytest.mark.parametrize("bits,hd,window,sinks", [(4, 64, 0, 0), (3, 128, 0, 0), (8, 36, 90, 5)])
+def test_more_tiles_of_rows_than_sms(a48, cuda_dev, bits, hd, window, sinks):
+    """CTAs of the tile kernel take over rows of others: unlike lengths, sequences with a few rows or none among them."""
+    rng = np.random.default_rng(22)
+    kvh, heads, page = 8, 32, 32
+    q_lens = [300, 1, 700, 0, 33, 64, 257, 5, 129, 480, 17, 90]
+    kv_lens = [n + int(rng.integers(0, 300)) for n in q_lens]
+    s = Setup(a48, cuda_dev, bits, kvh, hd, page, q_lens, kv_lens, seed=10, tail=3)
+    s.fill(rng)
+    assert sum((4 * n + 255) // 256 for n in q_lens if n > 8) * kvh > 148
+    q = torch.tensor(rng.standard_normal((s.n_tokens, heads * hd)), dtype=torch.float32).to(torch.bfloat16)
+    out = torch.full((s.n_tokens, heads * hd), 7.0, dtype=torch.bfloat16, device=cuda_dev)
+    first = check_attention(s, q, heads, window, sinks, out=out)
+    assert (out[int(s.q_start[-1]):] == 7).all()  # rows behind the last sequence
+    for _ in range(3):
+        again = a48.attention_paged(s.cache, s.batch, q.to(cuda_dev), window=window, sinks=sinks)
+        assert np.array_equal(again.double().cpu().numpy().reshape(first.shape)[:-3], first[:-3])
+
+
+def test_captured_prompts_replayed_with_other_lengths(a48, cuda_dev):
+    rng = np.random.default_rng(23)
+    hd, kvh, heads, page, B, top = 64, 4, 16, 64, 4, 600
+    s = Setup(a48, cuda_dev, 4, kvh, hd, page, [top] * B, [top] * B, seed=11)
+    s.fill(rng)
+    n = 1100
+    q = torch.tensor(rng.standard_normal((n, heads * hd)), dtype=torch.float32).to(torch.bfloat16)
+    x, out = q.to(cuda_dev), torch.zeros(n, heads * hd, dtype=torch.bfloat16, device=cuda_dev)
+    batch = s.view(np.array([0] * B + [top], np.int32), [top] * B, n, max_q=top, max_kv=top)
+    ws = torch.empty(max(16, a48.attention_paged_workspace_bytes(s.cache, batch, heads)), dtype=torch.uint8, device=cuda_dev)
+    a48.attention_paged(s.cache, batch, x, out=out, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a48.attention_paged(s.cache, batch, x, out=out, workspace=ws)
+    for q_lens, kv_lens in (([600, 500, 0, 0], [600, 500, 0, 9]), ([1, 2, 3, 600], [600, 600, 600, 600]), ([275] * 4, [275, 300, 599, 600]), ([0] * 4, [1] * 4)):
+        s.q_start = np.concatenate([[0], np.cumsum(q_lens)]).astype(np.int32)
+        s.kv_len = np.array(kv_lens, np.int32)
+        batch.q_start.copy_(torch.tensor(s.q_start))
+        batch.kv_len.copy_(torch.tensor(s.kv_len))
+        out.fill_(7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        ref, mag, best = s.oracle.attend(s.q_start, s.kv_len, s.table, q.double().numpy(), heads)
+        got, end = out.double().cpu().numpy().reshape(ref.shape), int(s.q_start[-1])
+        bound = attention_bound(ref, mag, best, hd, np.abs(s.oracle.scales[1]).max() * 128)
+        assert (np.abs(got - ref) <= bound)[:end].all() and (got[end:] == 7).all()
+
+
+def test_bounds_smaller_than_the_batch(a48, cuda_dev):
+    """max_q and max_kv size the launch only: tokens within max_q are right, the others right or left alone."""
+    rng = np.random.default_rng(24)
+    hd, kvh, heads, page = 64, 2, 8, 16
+    s = Setup(a48, cuda_dev, 4, kvh, hd, page, [150, 3, 40], [400, 3, 90], seed=12)
+    s.fill(rng)
+    q = torch.tensor(rng.standard_normal((s.n_tokens, heads * hd)), dtype=torch.float32).to(torch.bfloat16)
+    ref, mag, top = s.oracle.attend(s.q_start, s.kv_len, s.table, q.double().numpy(), heads)
+    bound = attention_bound(ref, mag, top, hd, np.abs(s.oracle.scales[1]).max() * 128)
+    for max_q, max_kv in ((1, 1), (2, 400), (20, 16), (100, 50), (150, 1)):
+        out = torch.full((s.n_tokens, heads * hd), 7.0, dtype=torch.bfloat16, device=cuda_dev)
+        a48.attention_paged(s.cache, s.view(s.q_start, s.kv_len, s.n_tokens, max_q=max_q, max_kv=max_kv), q.to(cuda_dev), out=out)
+        got = out.double().cpu().numpy().reshape(ref.shape)
+        right, alone = (np.abs(got - ref) <= bound).all(axis=(1, 2)), (got == 7).all(axis=(1, 2))
+        assert (right | alone).all()
+        for b in range(3):
+            within = int(s.q_start[b]) + min(max_q, int(s.q_start[b + 1] - s.q_start[b]))
+            assert right[int(s.q_start[b]):within].all()
+
+
+@pytest.mark.parametrize("q_lens,kv_lens", [([1, 2], [40, 2]), ([90, 0, 30], [200, 7, 30])])
+def test_rows_ahead_of_the_first_sequence(a48, cuda_dev, q_lens, kv_lens):
+    """q_start need not begin at 0: the rows ahead of it and behind the last are neither read nor written."""
+    rng = np.random.default_rng(25)
+    hd, kvh, heads, page, ahead, behind = 32, 2, 4, 16, 5, 4
+    s = Setup(a48, cuda_dev, 4, kvh, hd, page, q_lens, kv_lens, seed=13, tail=behind)
+    s.fill(rng)
+    s.q_start, s.n_tokens = s.q_start + ahead, s.n_tokens + ahead
+    s.batch = s.view(s.q_start, s.kv_len, s.n_tokens)
+    lo, hi = int(s.q_start[0]), int(s.q_start[-1])
+    k, v, q = (torch.tensor(rng.standard_normal((s.n_tokens, m * hd)), dtype=torch.float32) for m in (kvh, kvh, heads))
+    for t in (k, v, q):
+        t[:lo], t[hi:] = float("nan"), float("nan")
+    qr = torch.full((s.n_tokens, heads * hd), 7.0, dtype=torch.bfloat16, device=cuda_dev)
+    a48.paged_write(s.cache, s.batch, k.to(cuda_dev), v.to(cuda_dev), q=q.to(cuda_dev), q_out=qr)
+    s.oracle.write(s.q_start, s.kv_len, s.table, k.numpy(), v.numpy(), 10000.0, EPS32)
+    out = torch.full_like(qr, 7.0)
+    check_attention(s, qr.cpu(), heads, out=out)
+    ko, vo = (torch.full((s.n_tokens, kvh, hd), 7.0, device=cuda_dev) for _ in range(2))
+    a48.paged_read(s.cache, s.batch, dtype=torch.float32, k_out=ko, v_out=vo)
+    for t in (qr, out, ko, vo):
+        assert (t[:lo] == 7).all() and (t[hi:] == 7).all() and (t[lo:hi] != 7).any()
+    for g, r in zip((ko, vo), s.oracle.read(s.q_start, s.kv_len, s.table, s.n_tokens)):
+        assert (np.abs(g.double().cpu().numpy() - r) <= 2 * HALF_F32 * np.abs(r) * (1 + 1e-6))[lo:hi].all()
+
+
+@pytest.mark.parametrize("heads,kvh,hd,q_len,kv", [(300, 1, 32, 3, 70), (300, 1, 32, 1, 40), (40, 8, 64, 2, 300), (514, 2, 4, 2, 33)])
+def test_many_heads_to_a_key_head(a48, cuda_dev, heads, kvh, hd, q_len, kv):
+    """A token's query heads fill more than a tile, so that tiles begin and end inside a token."""
+    rng = np.random.default_rng(26)
+    s = Setup(a48, cuda_dev, 8, kvh, hd, 16, [q_len, 1, q_len], [kv, 1, q_len], seed=14)
+    s.fill(rng)
+    q = torch.tensor(rng.standard_normal((s.n_tokens, heads * hd)), dtype=torch.float32).to(torch.bfloat16)
+    check_attention(s, q, heads)
+
+
+def test_tensors_of_other_devices_are_refused(a48, cuda_dev):
+    s = Setup(a48, cuda_dev, 4, 1, 32, 16, [1], [1], seed=15)
+    x = torch.zeros(1, 32)
+    with pytest.raises(AssertionError):
+        a48.paged_write(s.cache, s.batch, x, x)
+    with pytest.raises(AssertionError):
+        a48.paged_write(s.cache, s.batch, x.to(cuda_dev), x)
+    with pytest.raises(AssertionError):
+        a48.attention_paged(s.cache, s.batch, x.to(torch.bfloat16))
+    with pytest.raises(AssertionError):
+        a48.attention_paged(s.cache, s.batch, x.to(cuda_dev, torch.bfloat16), workspace=torch.empty(64, dtype=torch.uint8))
