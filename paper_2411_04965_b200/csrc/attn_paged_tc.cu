@@ -251,7 +251,7 @@ template <int PD>
 struct Cfg {
     static constexpr int BUF = TK * PD * 2;  // one tile of keys, values or query rows
     static constexpr int Q_AT = RING * BUF, CTRL_AT = Q_AT + 2 * BUF, ROWS_AT = CTRL_AT + 256,
-                         SCALES_AT = ROWS_AT + 2 * TQ * 8, OUT_AT = SCALES_AT + SCALES * (int)sizeof(TileScales);
+                         SCALES_AT = ROWS_AT + 2 * TQ * 8, ITEM_AT = SCALES_AT + SCALES * (int)sizeof(TileScales), OUT_AT = ITEM_AT + 2 * 128;
     static constexpr int SMEM = OUT_AT + 2 * TQ * 64 + 1024 /*alignment slack*/;
     static_assert(SMEM <= 227 * 1024, "shared memory budget");
 };
@@ -263,10 +263,13 @@ enum { WAIT_FULL = 41, WAIT_EMPTY = 42, WAIT_S = 43, WAIT_ANSWER = 44, WAIT_O = 
 // v0 + n_tiles - 1 of their span.  The tiles with the most positions come first.
 struct Item {
     Span span;
-    long long r0;  // first row
-    int kvh, part, seq, start, rows, halves, pos0, pos_lo, pos_hi, v0, n_tiles;
+    int rows;     // 0: none there; -1: no more items
+    int r0;       // first row (rows of a call are counted in 31 bits)
+    int kvh, part, seq, start, pos0, pos_lo, pos_hi, v0, n_tiles;
+    int used0, used1;  // tiles of positions that a row of either tile may see: the first may not see the last one
 };
 __device__ __forceinline__ bool item_of(const AttnArgs& a, int index, int lane, Item& it) {  // false: no rows there
+    it.rows = it.n_tiles = 0;
     const int x = index / a.tc_splits, at = gridDim.x / a.tc_splits / a.l.kv_heads - 1 - x / a.l.kv_heads;
     it.part = index % a.tc_splits, it.kvh = x % a.l.kv_heads;
     int tile;
@@ -281,16 +284,19 @@ __device__ __forceinline__ bool item_of(const AttnArgs& a, int index, int lane, 
     it.start = __ldg(a.b.q_start + it.seq);
     const int q_len = __ldg(a.b.q_start + it.seq + 1) - it.start;
     const long long all_rows = (long long)q_len * a.group;
-    it.r0 = (long long)tile * a48p::TILE_ROWS;
-    if (all_rows <= a.few_rows || it.r0 >= all_rows || it.start < 0 || q_len > a.b.n_tokens - it.start) return false;
-    it.rows = (int)min((long long)a48p::TILE_ROWS, all_rows - it.r0);
-    it.halves = it.rows > TQ ? 2 : 1;
+    const long long r0 = (long long)tile * a48p::TILE_ROWS;
+    it.r0 = (int)r0;
+    if (all_rows <= a.few_rows || r0 >= all_rows || it.start < 0 || q_len > a.b.n_tokens - it.start) return false;
+    it.rows = (int)min((long long)a48p::TILE_ROWS, all_rows - r0);
     it.pos0 = __ldg(a.b.kv_len + it.seq) - q_len;
-    it.pos_lo = it.pos0 + (int)(it.r0 / a.group), it.pos_hi = it.pos0 + (int)((it.r0 + it.rows - 1) / a.group);
+    it.pos_lo = it.pos0 + it.r0 / a.group, it.pos_hi = it.pos0 + (it.r0 + it.rows - 1) / a.group;
     it.span = a48p::span_of<7>(a, it.pos_lo, it.pos_hi);
     const int per = max(2, (it.span.count + a.tc_splits - 1) / a.tc_splits);
     it.v0 = it.part * per;
     it.n_tiles = max(0, min(it.span.count, it.v0 + per) - it.v0);
+    const int hi = it.pos0 + (it.r0 + min(it.rows, TQ) - 1) / a.group;  // at most TQ = TK positions below pos_hi
+    it.used0 = it.n_tiles > 0 && it.span.block(it.v0 + it.n_tiles - 1) * TK > hi ? it.n_tiles - 1 : it.n_tiles;
+    it.used1 = it.rows > TQ ? it.n_tiles : 0;
     return true;
 }
 
@@ -303,12 +309,12 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
     uint8_t* smem = smem_raw + (-smem_u32(smem_raw) & 1023u);
     uint8_t* ctrl = smem + C::CTRL_AT;
     uint8_t* canceled = ctrl + 128;  // the answer about a CTA not yet started, 16 bytes
-    volatile int* next_item = reinterpret_cast<volatile int*>(ctrl + 144);
     uint32_t* q_tops = reinterpret_cast<uint32_t*>(ctrl + 160);  // the largest query entry, as bits, of three items
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl + 192);
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(ctrl + 196);
     float* top_part = reinterpret_cast<float*>(ctrl + 208);     // largest value scale per converting warp
     float2* row_info = reinterpret_cast<float2*>(smem + C::ROWS_AT);  // last position seen; at the end reference and sum
+    Item* items = reinterpret_cast<Item*>(smem + C::ITEM_AT);  // this one and the next, by the parity of their number
     TileScales* scales = reinterpret_cast<TileScales*>(smem + C::SCALES_AT);
     const uint32_t ring = smem_u32(smem), sq = ring + C::Q_AT;
     // barriers: full[4] | empty[4] | s[2] | o[2] | answer | next item
@@ -320,9 +326,8 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    Item it;
-    bool there = item_of(a, blockIdx.x, lane, it);
-    if (!there) return;
+    Item first;
+    if (!item_of(a, blockIdx.x, lane, first)) return;
     if (threadIdx.x == 0) {
         for (int i = 0; i < RING; ++i) {
             mbar_init(bar_full + 8 * i, TQ);
@@ -336,6 +341,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
         mbar_init(bar_next, 1);
         *abort_flag = 0;
         q_tops[0] = 0;
+        items[0] = first;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == CONVERT_WARP) {
@@ -359,25 +365,36 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                      "r"(bar_answer)
                      : "memory");
     };
-    auto hand_on = [&](int k) {  // what was asked for ahead of item k
-        mbar_wait(bar_answer, (k - 1) & 1, abort_flag, WAIT_ANSWER, k);
-        uint32_t taken, index;
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t.reg .b128 answer;\n\t"
-            "ld.shared.b128 answer, [%2];\n\t"
-            "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, answer;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\tmov.u32 %1, 0;\n\t"
-            "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, answer;\n\t}"
-            : "=r"(taken), "=r"(index)
-            : "r"(smem_u32(canceled))
-            : "memory");
-        *next_item = taken && !*abort_flag ? (int)index : -1;
-        mbar_arrive(bar_next);
+    auto hand_on = [&](int k) {  // what was asked for ahead of item k, by the thread's warp
+        uint32_t taken = 0, index = 0;
+        if (lane == 0) {
+            mbar_wait(bar_answer, (k - 1) & 1, abort_flag, WAIT_ANSWER, k);
+            asm volatile(
+                "{\n\t.reg .pred p;\n\t.reg .b128 answer;\n\t"
+                "ld.shared.b128 answer, [%2];\n\t"
+                "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, answer;\n\t"
+                "selp.u32 %0, 1, 0, p;\n\tmov.u32 %1, 0;\n\t"
+                "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, answer;\n\t}"
+                : "=r"(taken), "=r"(index)
+                : "r"(smem_u32(canceled))
+                : "memory");
+            if (*abort_flag) taken = 0;
+        }
+        taken = __shfl_sync(0xffffffffu, taken, 0), index = __shfl_sync(0xffffffffu, index, 0);
+        Item got;
+        if (taken) item_of(a, (int)index, lane, got);
+        else got.rows = -1, got.n_tiles = 0;
+        if (lane == 0) {
+            items[k & 1] = got;
+            mbar_arrive(bar_next);
+        }
+        __syncwarp();
     };
     // (This one wait must not be given up before that thread has come through its own: five times their limit.)
+    Item it = first;
     auto item_after = [&](int k) {
         mbar_wait_long(bar_next, (k - 1) & 1, k);
-        return *next_item;
+        it = items[k & 1];
     };
     int n0 = 0;  // tiles of positions of the items before
     if (warp >= CONVERT_WARP) {
@@ -483,9 +500,8 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             mbar_arrive(bar_full + 8 * (n % RING));
         };
-        int index = blockIdx.x;
 #pragma unroll 1
-        for (int k = 0; index >= 0;) {
+        for (int k = 0; it.rows >= 0;) {
             if (it.n_tiles > 0) {
                 unit = 0.f;
                 look_up(0);
@@ -558,10 +574,9 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                     look_up(t + 2);
                 }
             }
-            if (threadIdx.x == 32 * CONVERT_WARP) hand_on(k + 1);
+            if (w == 0) hand_on(k + 1);
             n0 += it.n_tiles;
-            index = item_after(++k);
-            if (index >= 0 && !item_of(a, index, lane, it)) it.n_tiles = 0;
+            item_after(++k);
         }
         // the CTA must not end before the last arrivals on its barriers
         for (int i = 0; i < RING; ++i) {
@@ -580,57 +595,55 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
         // (with a row to a thread they were a fifth of the time of a prompt).
         constexpr int UNITS = PD / 4, AT_ONCE = 32 / UNITS;
         const int u = lane % UNITS, sub = lane / UNITS;
-        uint8_t* queries = smem + C::Q_AT + half * C::BUF + (warp & 3) * 64 * PD;
-        int index = blockIdx.x, k = 0, u0 = 0;  // u0: tiles of positions that this tile of rows has taken
-        auto place_of = [&](int& token, int& head) {  // of this thread's row; without one, of the item's last
-            const uint32_t n = (uint32_t)it.r0 + min(r, it.rows - 1);  // (rows of a call are counted in 31 bits)
-            token = it.start + (int)(n / (uint32_t)a.group), head = it.kvh * a.group + (int)(n % (uint32_t)a.group);
+        uint8_t* queries = smem + C::Q_AT + half * C::BUF + (warp & 3) * 32 * 128;
+        int k = 0, u0 = 0;  // u0: tiles of positions that this tile of rows has taken
+        auto place_of = [&](const Item& i, int& token, int& head) {  // of this thread's row; without one, of the item's last
+            const uint32_t n = i.r0 + min(r, i.rows - 1);
+            token = i.start + (int)(n / (uint32_t)a.group), head = i.kvh * a.group + (int)(n % (uint32_t)a.group);
         };
+        // Raw, either half of a row lies where its fp16 form will: a warp's rows are its own.
+        auto at_unit = [&](int j, int unit) { return queries + j * 128 + unit / 16 * PANEL + unit % 16 * 8; };
         auto fetch = [&]() {
+            if (it.rows <= 0) return;
             int token, head;
-            place_of(token, head);
+            place_of(it, token, head);
             const size_t from = (size_t)token * a.q_stride + (size_t)head * a.l.hd;
-#pragma unroll 8
+#pragma unroll 4
             for (int i = 0; i < UNITS; ++i) {
                 const int j = AT_ONCE * i + sub;
                 const size_t at = __shfl_sync(0xffffffffu, (unsigned long long)from, j);
                 const bool real = r - lane + j < it.rows && 4 * u < a.l.hd;
-                asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(smem_u32(queries) + j * 2 * PD + 8 * u), "l"(a.q + (real ? at + 4 * u : 0)),
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(smem_u32(at_unit(j, u))), "l"(a.q + (real ? at + 4 * u : 0)),
                              "r"(real ? 8 : 0)
                              : "memory");
             }
         };
-        auto take = [&]() {  // the item `index`
-            there = index >= 0 && item_of(a, index, lane, it);
-            if (there) fetch();
-        };
         fetch();
 #pragma unroll 1
-        while (index >= 0) {
+        while (it.rows >= 0) {
             if (threadIdx.x == 0) q_tops[(k + 1) % 3] = 0;  // (read for the last time before the queries_sync of k - 1)
-            if (!there) {
+            if (it.rows == 0) {
                 queries_sync();
-                index = item_after(++k);
-                take();
+                item_after(++k);
+                fetch();
                 continue;
             }
             uint32_t* q_top = q_tops + k % 3;
-            const int rows = it.rows, halves = it.halves;
+            const int rows = it.rows;
             // ---- the query rows to fp16 by a power of two, in the order of the converted codes
             {
-                uint2 x[UNITS];
                 float mx = 0.f;
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 __syncwarp();
-#pragma unroll
+#pragma unroll 4
                 for (int i = 0; i < UNITS; ++i) {
-                    x[i] = *reinterpret_cast<const uint2*>(queries + (AT_ONCE * i + sub) * 2 * PD + 8 * u);
-                    mx = fmaxf(mx, fmaxf(fmaxf(fabsf(__uint_as_float(x[i].x << 16)), fabsf(__uint_as_float(x[i].x & 0xffff0000u))),
-                                         fmaxf(fabsf(__uint_as_float(x[i].y << 16)), fabsf(__uint_as_float(x[i].y & 0xffff0000u)))));
+                    const uint2 x = *reinterpret_cast<const uint2*>(at_unit(AT_ONCE * i + sub, u));
+                    mx = fmaxf(mx, fmaxf(fmaxf(fabsf(__uint_as_float(x.x << 16)), fabsf(__uint_as_float(x.x & 0xffff0000u))),
+                                         fmaxf(fabsf(__uint_as_float(x.y << 16)), fabsf(__uint_as_float(x.y & 0xffff0000u)))));
                 }
                 const uint32_t top = __reduce_max_sync(0xffffffffu, mx <= 3.4e38f ? __float_as_uint(mx) : 0u);
                 if (lane == 0) atomicMax(q_top, top);
-                row_info[r].x = __int_as_float(it.pos0 + (int)(((uint32_t)it.r0 + min(r, rows - 1)) / (uint32_t)a.group));
+                row_info[r].x = __int_as_float(it.pos0 + (it.r0 + min(r, rows - 1)) / a.group);
                 queries_sync();
                 const int e = query_exponent(*q_top);
                 const float up0 = power_of_two(e / 2), up1 = power_of_two(e - e / 2);  // (2^e may be past fp32)
@@ -643,16 +656,18 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                 constexpr int APART = BITS == 3 ? 4 : BITS == 4 ? 1 : 0;
                 const bool upper = (u & APART) != 0;
                 const int place = BITS == 3 ? (4 * u & ~31) + 8 * (u & 3) + (u & 4) : 4 * u;
-                uint8_t* dst = smem + C::Q_AT + half * C::BUF + place / 64 * PANEL + (place & 4) * 2;
-#pragma unroll
+                uint8_t* dst = queries + place / 64 * PANEL + (place & 4) * 2;
+#pragma unroll 4
                 for (int i = 0; i < UNITS; ++i) {
-                    const int at = (warp & 3) * 32 + AT_ONCE * i + sub;
-                    uint32_t lo = halves_of(x[i].x), hi = halves_of(x[i].y);
+                    const int j = AT_ONCE * i + sub;
+                    const uint2 x = *reinterpret_cast<const uint2*>(at_unit(j, u));
+                    uint32_t lo = halves_of(x.x), hi = halves_of(x.y);
                     if constexpr (APART > 0) {
                         const uint32_t got = __shfl_xor_sync(0xffffffffu, upper ? lo : hi, APART);
                         lo = upper ? got : lo, hi = upper ? hi : got;
                     }
-                    *reinterpret_cast<uint2*>(dst + at * 128 + (((place / 8 % 8) ^ (at & 7)) << 4)) =
+                    __syncwarp();  // (the whole row has been read)
+                    *reinterpret_cast<uint2*>(dst + j * 128 + (((place / 8 % 8) ^ (j & 7)) << 4)) =
                         make_uint2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -660,6 +675,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             // ---- MMAs of this tile: by one thread, once all have done their part
             constexpr uint32_t idesc_s = idesc_f16(TQ, TK, false), idesc_o = idesc_f16(TQ, PD, true);
             const uint32_t t_s = tmem + COL_S + TK * half, t_o = tmem + COL_O + 128 * half;
+            const int used = half ? it.used1 : it.used0, other = half ? it.used0 : it.used1, both = min(used, other);  // tiles of positions
             auto wait_full = [&](int n) {
                 mbar_wait(bar_full + 8 * (n % RING), n / RING & 1, abort_flag, WAIT_FULL, n);
                 tc_fence_after();
@@ -675,7 +691,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                         mma_ss(t_s, q_desc + ks / 4 * STEP + 2 * (ks % 4), k_desc + ks / 4 * STEP + 2 * (ks % 4), idesc_s, ks != 0);
                     }
                     tc_commit(bar_s + 8 * half);
-                    for (int i = halves; i < 3; ++i) tc_commit(bar_empty + 8 * (2 * (n0 + t) % RING));  // (for a second tile without rows too)
+                    for (int i = t < other; i < 2; ++i) tc_commit(bar_empty + 8 * (2 * (n0 + t) % RING));  // (for the other tile too if it is not used there)
                 }
                 __syncwarp();
             };
@@ -686,12 +702,11 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
 #pragma unroll
                     for (int j = 1; j < TK / 16; ++j) mma_ts(t_o, t_s + 8 * j, v_desc + 2048 / 16 * j, idesc_o, 1);
                     tc_commit(bar_o + 8 * half);
-                    for (int i = halves; i < 3; ++i) tc_commit(bar_empty + 8 * ((2 * (n0 + t) + 1) % RING));
+                    for (int i = t < other; i < 2; ++i) tc_commit(bar_empty + 8 * ((2 * (n0 + t) + 1) % RING));
                 }
                 __syncwarp();
             };
             const bool issuer = (warp & 3) == 0;
-            const int used = half < halves ? it.n_tiles : 0;
             tile_sync(half);  // the query rows are in place
             if (issuer && used > 0) issue_s(0);
             // the four rows of this thread between loads and stores: lanes g, g + 8, g + 16, g + 24 of the warp
@@ -705,7 +720,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             }
             const int lim_lo = __reduce_min_sync(0xffffffffu, min(min(lim[0], lim[1]), min(lim[2], lim[3])));
             const int lim_hi = __reduce_max_sync(0xffffffffu, max(max(lim[0], lim[1]), max(lim[2], lim[3])));
-            if (halves == 2 && half == 1 && used > 0) turn_pass(1);
+            if (half == 1 && both > 0) turn_pass(1);
             for (int t = 0; t < used; ++t) {
                 mbar_wait(bar_s + 8 * half, (u0 + t) & 1, abort_flag, WAIT_S, t);
                 tc_fence_after();
@@ -716,24 +731,37 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                                    (dead.x | dead.y | dead.z | dead.w) == 0;
                 if (!whole) {  // the scores that a row does not see become -inf
 #pragma unroll 1
-                    for (int c = 0; c < TK / 16; ++c) {
+                    for (int c = 0; c < TK / 16; ++c) {  // (most groups of 16 positions are seen by all of the warp's rows, or by none)
+                        const int from = base + 16 * c;
+                        const uint32_t gone = ts.dead[c >> 1] >> (16 * (c & 1)) & 0xffff;
+                        if (gone == 0 && from + 15 <= lim_lo && (window == 0 || from > lim_hi - window || from + 15 < sinks)) continue;
                         uint32_t acc[2][8];
-                        tmem_ld_16x16(s_at + 16 * c, acc[0]);
-                        tmem_ld_16x16(s_at + (16u << 16) + 16 * c, acc[1]);
-                        tmem_wait_ld(acc);
-                        const uint32_t gone = ts.dead[c >> 1] >> (16 * (c & 1) + c0);
+                        if (gone == 0xffff || from > lim_hi || (window > 0 && from + 15 <= lim_lo - window && from >= sinks)) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int n = 16 * c + 8 * ((i >> 2) & 1) + c0 + (i & 1), to = lim[(i >> 3) * 2 + ((i >> 1) & 1)] - base;
-                            const bool seen = n <= to && (window == 0 || n > to - window || n < sinks - base) && !((gone >> (8 * ((i >> 2) & 1) + (i & 1))) & 1);
-                            if (!seen) acc[i >> 3][i & 7] = 0xff800000u;
+                            for (int i = 0; i < 16; ++i) acc[i >> 3][i & 7] = 0xff800000u;
+                        } else {
+                            tmem_ld_16x16(s_at + 16 * c, acc[0]);
+                            tmem_ld_16x16(s_at + (16u << 16) + 16 * c, acc[1]);
+                            auto below = [](int n) { return (1u << min(max(n, 0), 16)) - 1; };  // bits of the first n of the 16
+                            uint32_t seen[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const int to = lim[i] - from;
+                                uint32_t s = below(to + 1);
+                                if (window > 0) s &= ~below(to + 1 - window) | below(sinks - from);
+                                seen[i] = (s & ~gone) >> c0;
+                            }
+                            tmem_wait_ld(acc);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                if (!((seen[(i >> 3) * 2 + ((i >> 1) & 1)] >> (8 * ((i >> 2) & 1) + (i & 1))) & 1)) acc[i >> 3][i & 7] = 0xff800000u;
                         }
                         tmem_st_16x16(s_at + 16 * c, acc[0]);
                         tmem_st_16x16(s_at + (16u << 16) + 16 * c, acc[1]);
                     }
                     tmem_wait_st();
                 }
-                if (halves == 2) turn_wait(half);
+                if (t < both) turn_wait(half);
                 // ---- 64 columns, then the other 64
 #pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
@@ -845,7 +873,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                     for (int i = 0; i < 4; ++i) l[i] += sum[i];
                     tmem_st_16x32(s_at + 32 * h, p[0]);  // (over scores that have been taken)
                     tmem_st_16x32(s_at + (16u << 16) + 32 * h, p[1]);
-                    if (h == 0 && halves == 2 && (half == 0 || t + 1 < used)) turn_pass(half);
+                    if (h == 0 && t + half < both) turn_pass(half);
                 }
                 tmem_wait_st();
                 tc_fence_before();
@@ -865,15 +893,16 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             }
             __syncwarp();
             const float2 ml = row_info[r];
+            const Item done = items[k & 1];  // (again: not kept in registers meanwhile)
             int token, head;
-            place_of(token, head);
-            const size_t id = (size_t)token * a.heads + head, part = (size_t)it.part * a.b.n_tokens * a.heads + id;
+            place_of(done, token, head);
+            const size_t id = (size_t)token * a.heads + head, part = (size_t)done.part * a.b.n_tokens * a.heads + id;
             const float inv = unit == 0.f ? 0.f : split ? 1.f / unit : ml.y != 0.f ? 1.f / ml.y / unit : 0.f;
-            if (split && r < rows) a.part_ml[part] = ml;
+            if (split && r < done.rows) a.part_ml[part] = ml;
             const size_t to = split ? part * 128 : (size_t)token * a.out_stride + (size_t)head * a.l.hd;
-            n0 += it.n_tiles;
-            index = item_after(++k);
-            take();
+            n0 += done.n_tiles;
+            item_after(++k);
+            fetch();
             if (used > 0) {
                 mbar_wait(bar_o + 8 * half, (u0 + used - 1) & 1, abort_flag, WAIT_O, used);
                 tc_fence_after();
@@ -892,11 +921,11 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                     const int j = 4 * i + (lane >> 3);
                     const size_t at = __shfl_sync(0xffffffffu, (unsigned long long)to, j);
                     const uint2 v = *reinterpret_cast<const uint2*>(stage + j * 64 + (((u >> 1) ^ ((j >> 1) & 3)) << 4) + 8 * (u & 1));
-                    if (r - lane + j < rows && 8 * u < width) *reinterpret_cast<uint2*>(base + at * elem + 8 * u) = v;
+                    if (r - lane + j < done.rows && 8 * u < width) *reinterpret_cast<uint2*>(base + at * elem + 8 * u) = v;
                 }
                 __syncwarp();
             };
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < PD / 32; ++c) {
                 uint32_t acc[32];
                 float y[32];
