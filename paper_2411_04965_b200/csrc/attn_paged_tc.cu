@@ -27,14 +27,18 @@
 // Tensor memory: two score tiles (128 columns, P over the first 64) and two output tiles (up to 128 columns).
 //
 // A CTA that is through with its rows cancels one that has not started and takes its rows over, so that the codes and queries
-// of the next rows are under way while the last weights are multiplied and outputs stored: four prompts of 4096 tokens, 32
-// heads of 128, 3 bits, 821 us (669 TFLOP/s of the 4 x 128 operations per score), 854 with one CTA to each.  What bounds it:
-// 128 positions take a CTA about 4500 clocks, of which the products of both tiles occupy the tensor pipe for 2600.  A tile
-// needs 250 clocks from its scores to the first weights, 2400 for the weights (1400 for the 64 columns taken while the other
-// tile takes its last 64, 1000 for the others; their exponentials alone are 1024 clocks of the SFUs) and 1300 for O and the
-// next S; with no room for a second score tile in tensor memory these follow one another.  Without the exponentials it
-// would be 749 us, without the conversion to fp16 829.  Tiles of 64 positions, with two score tiles each, took 1015 us (against 917 then): the
-// products of 64 columns are bound by shared memory.  Without the two tiles' turns 866.
+// of the next rows are under way while the last weights are multiplied and outputs stored.  Four prompts of 4096 tokens, 32
+// heads of 128, 3 bits: 669 us (822 TFLOP/s of the 4 x 128 operations per score); two chunks of up to 2048 tokens with a
+// window of 2048, 195 us.  On the way there, for the prompts: one CTA to each tile of rows 854 us, taking over 821, masks by
+// groups of 16 positions and no tiles that the first rows do not see 691, queries converted eight rows at a time 669.
+//
+// What bounds it: 128 positions take a CTA about 4250 clocks, of which the products of both tiles occupy the tensor pipe for
+// 2600.  A tile needs 250 clocks from its scores to the first weights, 2400 for the weights (1400 for the 64 columns taken
+// while the other tile takes its last 64, 1000 for the others; the exponentials alone are 1024 clocks of the SFUs) and 1300
+// for O and the next S; with no room for a second score tile in tensor memory these follow one another.  Without the
+// exponentials the 821 us were 749, without the conversion to fp16 829, without the turns that the tiles take 866.  Tiles of
+// 64 positions, with two score tiles each, were slower (1015 us against 917 then): products of 64 columns are bound by
+// shared memory.  Rows cost about 13000 clocks of their own, half of which the first tile waits for the second.
 // Every wait is bounded; one that gives up records itself (bitnet_a48_kernel_status), and every later wait of the CTA then
 // falls through, so that the kernel ends by itself.
 #include <climits>
@@ -608,7 +612,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             int token, head;
             place_of(it, token, head);
             const size_t from = (size_t)token * a.q_stride + (size_t)head * a.l.hd;
-#pragma unroll 4
+#pragma unroll 8
             for (int i = 0; i < UNITS; ++i) {
                 const int j = AT_ONCE * i + sub;
                 const size_t at = __shfl_sync(0xffffffffu, (unsigned long long)from, j);
@@ -635,7 +639,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                 float mx = 0.f;
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 __syncwarp();
-#pragma unroll 4
+#pragma unroll 8
                 for (int i = 0; i < UNITS; ++i) {
                     const uint2 x = *reinterpret_cast<const uint2*>(at_unit(AT_ONCE * i + sub, u));
                     mx = fmaxf(mx, fmaxf(fmaxf(fabsf(__uint_as_float(x.x << 16)), fabsf(__uint_as_float(x.x & 0xffff0000u))),
@@ -657,18 +661,26 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                 const bool upper = (u & APART) != 0;
                 const int place = BITS == 3 ? (4 * u & ~31) + 8 * (u & 3) + (u & 4) : 4 * u;
                 uint8_t* dst = queries + place / 64 * PANEL + (place & 4) * 2;
-#pragma unroll 4
-                for (int i = 0; i < UNITS; ++i) {
-                    const int j = AT_ONCE * i + sub;
-                    const uint2 x = *reinterpret_cast<const uint2*>(at_unit(j, u));
-                    uint32_t lo = halves_of(x.x), hi = halves_of(x.y);
-                    if constexpr (APART > 0) {
-                        const uint32_t got = __shfl_xor_sync(0xffffffffu, upper ? lo : hi, APART);
-                        lo = upper ? got : lo, hi = upper ? hi : got;
+#pragma unroll 1
+                for (int i = 0; i < UNITS; i += 8) {  // (eight loads, then eight stores: they cannot be told apart)
+                    uint2 x[8];
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) x[n] = *reinterpret_cast<const uint2*>(at_unit(AT_ONCE * (i + n) + sub, u));
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) {
+                        uint32_t lo = halves_of(x[n].x), hi = halves_of(x[n].y);
+                        if constexpr (APART > 0) {
+                            const uint32_t got = __shfl_xor_sync(0xffffffffu, upper ? lo : hi, APART);
+                            lo = upper ? got : lo, hi = upper ? hi : got;
+                        }
+                        x[n] = make_uint2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
                     }
-                    __syncwarp();  // (the whole row has been read)
-                    *reinterpret_cast<uint2*>(dst + j * 128 + (((place / 8 % 8) ^ (j & 7)) << 4)) =
-                        make_uint2(__byte_perm(lo, hi, 0x5410), __byte_perm(lo, hi, 0x7632));
+                    __syncwarp();  // (the rows have been read)
+#pragma unroll
+                    for (int n = 0; n < 8; ++n) {
+                        const int j = AT_ONCE * (i + n) + sub;
+                        *reinterpret_cast<uint2*>(dst + j * 128 + (((place / 8 % 8) ^ (j & 7)) << 4)) = x[n];
+                    }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             }
