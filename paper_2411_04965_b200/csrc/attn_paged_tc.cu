@@ -642,10 +642,15 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
 #pragma unroll 8
                 for (int i = 0; i < UNITS; ++i) {
                     const uint2 x = *reinterpret_cast<const uint2*>(at_unit(AT_ONCE * i + sub, u));
-                    mx = fmaxf(mx, fmaxf(fmaxf(fabsf(__uint_as_float(x.x << 16)), fabsf(__uint_as_float(x.x & 0xffff0000u))),
-                                         fmaxf(fabsf(__uint_as_float(x.y << 16)), fabsf(__uint_as_float(x.y & 0xffff0000u)))));
+                    // (numbers only: an infinity of one row must not hide the others' entries, which would overflow)
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) {
+                        const uint32_t w = n & 2 ? x.y : x.x;
+                        const float v = fabsf(__uint_as_float(n & 1 ? w & 0xffff0000u : w << 16));
+                        mx = v <= 3.4e38f ? fmaxf(mx, v) : mx;
+                    }
                 }
-                const uint32_t top = __reduce_max_sync(0xffffffffu, mx <= 3.4e38f ? __float_as_uint(mx) : 0u);
+                const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(mx));
                 if (lane == 0) atomicMax(q_top, top);
                 row_info[r].x = __int_as_float(it.pos0 + (it.r0 + min(r, rows - 1)) / a.group);
                 queries_sync();

@@ -575,3 +575,22 @@ def test_tensors_of_other_devices_are_refused(a48, cuda_dev):
         a48.attention_paged(s.cache, s.batch, x.to(torch.bfloat16))
     with pytest.raises(AssertionError):
         a48.attention_paged(s.cache, s.batch, x.to(cuda_dev, torch.bfloat16), workspace=torch.empty(64, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("q_len", [1, 6, 100])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_queries_that_are_no_numbers_stay_alone(a48, cuda_dev, q_len, bad):
+    """A query head with an infinity or NaN, where its other heads and the next two tokens have the largest entries of all."""
+    rng = np.random.default_rng(27)
+    hd, kvh, heads = 128, 1, 4
+    s = Setup(a48, cuda_dev, 4, kvh, hd, 16, [q_len, 2], [q_len + 60, 33], seed=16)
+    s.fill(rng)
+    x = rng.standard_normal((s.n_tokens, heads, hd)) * 2.0 ** -6
+    x[:3, :, 5] *= 2.0 ** 15
+    q = torch.tensor(x.reshape(s.n_tokens, -1), dtype=torch.float32).to(torch.bfloat16)
+    ref, mag, top = s.oracle.attend(s.q_start, s.kv_len, s.table, q.double().numpy(), heads)
+    q.view(s.n_tokens, heads, hd)[0, 1, 5] = bad
+    got = a48.attention_paged(s.cache, s.batch, q.to(cuda_dev)).double().cpu().numpy().reshape(ref.shape)
+    right = np.abs(got - ref) <= attention_bound(ref, mag, top, hd, np.abs(s.oracle.scales[1]).max() * 128)
+    right[0, 1] = True
+    assert right.all()
