@@ -28,8 +28,8 @@
 //
 // A CTA that is through with its rows cancels one that has not started and takes its rows over, so that the codes and queries
 // of the next rows are under way while the last weights are multiplied and outputs stored.  Four prompts of 4096 tokens, 32
-// heads of 128, 3 bits: 669 us (822 TFLOP/s of the 4 x 128 operations per score); two chunks of up to 2048 tokens with a
-// window of 2048, 195 us.  On the way there, for the prompts: one CTA to each tile of rows 854 us, taking over 821, masks by
+// heads of 128, 3 bits: 672 us (818 TFLOP/s of the 4 x 128 operations per score); two chunks of up to 2048 tokens with a
+// window of 2048, 196 us.  On the way there, for the prompts: one CTA to each tile of rows 854 us, taking over 821, masks by
 // groups of 16 positions and no tiles that the first rows do not see 691, queries converted eight rows at a time 669.
 //
 // What bounds it: 128 positions take a CTA about 4250 clocks, of which the products of both tiles occupy the tensor pipe for
@@ -38,7 +38,8 @@
 // for O and the next S; with no room for a second score tile in tensor memory these follow one another.  Without the
 // exponentials the 821 us were 749, without the conversion to fp16 829, without the turns that the tiles take 866.  Tiles of
 // 64 positions, with two score tiles each, were slower (1015 us against 917 then): products of 64 columns are bound by
-// shared memory.  Rows cost about 13000 clocks of their own, half of which the first tile waits for the second.
+// shared memory.  Rows cost about 13000 clocks of their own, half of which the first tile waits for the second; letting it
+// go on ahead, with the converting warps finding the largest query entry, was no faster (687 us).
 // Every wait is bounded; one that gives up records itself (bitnet_a48_kernel_status), and every later wait of the CTA then
 // falls through, so that the kernel ends by itself.
 #include <climits>
