@@ -594,3 +594,26 @@ def test_queries_that_are_no_numbers_stay_alone(a48, cuda_dev, q_len, bad):
     right = np.abs(got - ref) <= attention_bound(ref, mag, top, hd, np.abs(s.oracle.scales[1]).max() * 128)
     right[0, 1] = True
     assert right.all()
+
+
+@pytest.mark.parametrize("bits", [8, 4, 3])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_heads_of_zeros_and_of_tiny_numbers_without_eps(a48, cuda_dev, bits, dtype):
+    """eps 0: a head of zeros has no scale to divide by and reads as zeros; the smallest numbers keep their codes."""
+    rng = np.random.default_rng(28)
+    hd, kvh, n = 32, 2, 7
+    s = Setup(a48, cuda_dev, bits, kvh, hd, 16, [n], [n], seed=17)
+    k, v = (torch.tensor(rng.standard_normal((n, kvh * hd)), dtype=torch.float32) for _ in range(2))
+    k[2], v[1], v[0, :hd] = 0, 0, 0
+    k[3], v[3] = k[3] * 1e-30, v[3] * 1e-30
+    k, v = k.to(dtype), v.to(dtype)
+    a48.paged_write(s.cache, s.batch, k.to(cuda_dev), v.to(cuda_dev), rope_base=0.0, eps=0.0)
+    got = [t.double().cpu().numpy() for t in a48.paged_read(s.cache, s.batch, dtype=torch.float32)]
+    for g, x in zip(got, (k, v)):
+        x = x.double().numpy().reshape(n, kvh, hd)
+        gamma = np.abs(x).max(-1, keepdims=True)
+        assert (g[x == 0] == 0).all()
+        levels = np.where((np.arange(n) == 0) & (bits == 3), 7, 2 ** (bits - 1) - 1)[:, None, None]
+        assert (np.abs(g - x) <= 0.5 * gamma / levels * (1 + 1e-5)).all()  # half a step of the code
+    q = torch.tensor(rng.standard_normal((n, kvh * hd)), dtype=torch.float32).to(torch.bfloat16)
+    assert torch.isfinite(a48.attention_paged(s.cache, s.batch, q.to(cuda_dev)).float()).all()
