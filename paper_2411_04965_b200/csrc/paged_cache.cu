@@ -453,7 +453,8 @@ bitnet_a48_status bitnet_a48_paged_write(const bitnet_a48_paged_cache* cache, vo
     if ((st = a48p::check_rows(k_dev, k_stride, kv_width, elem)) != BITNET_A48_OK) return st;
     if ((st = a48p::check_rows(v_dev, v_stride, kv_width, elem)) != BITNET_A48_OK) return st;
     if (q_dev || q_out_dev) {
-        if (n_heads <= 0 || n_heads > 65535) return BITNET_A48_ERR_SHAPE;
+        if (n_heads <= 0) return BITNET_A48_ERR_SHAPE;
+        if (n_heads > 65535) return BITNET_A48_ERR_LIMIT;
         if ((st = a48p::check_rows(q_dev, q_stride, q_width, elem)) != BITNET_A48_OK) return st;
         if ((st = a48p::check_rows(q_out_dev, q_out_stride, q_width, 2)) != BITNET_A48_OK) return st;
     }

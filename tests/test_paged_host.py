@@ -121,6 +121,30 @@ def test_refusals_of_the_calls(a48):
     assert attend(window=-1) == INVALID and attend(sinks=-1) == INVALID and attend(scale=-1.0) == INVALID and attend(scale=float("inf")) == INVALID
 
 
+def test_limits_and_workspace(a48):
+    lib = a48.lib()
+    NOMEM, LIMIT = 7, 8
+    p, null = ctypes.c_void_p(4096), ctypes.c_void_p(0)
+    good = make(a48)
+
+    def attend(b, heads=4, ws=p, nbytes=1 << 40):
+        return lib.bitnet_a48_attention_paged(ctypes.byref(good), p, ctypes.byref(b), heads, p, heads * 64, 0.0, 0, 0, p, heads * 64, ws, nbytes, null)
+
+    def need(b, heads=4):
+        return lib.bitnet_a48_attention_paged_workspace_bytes(ctypes.byref(good), ctypes.byref(b), heads, 0, 0)
+
+    assert attend(batch(a48, n_tokens=(1 << 30) + 1)) == LIMIT
+    assert attend(batch(a48, max_pages=1 << 27)) == LIMIT  # times 16 positions
+    assert attend(batch(a48, n_tokens=1 << 30), heads=4) == LIMIT  # rows past 2^31 - 1
+    assert lib.bitnet_a48_paged_write(ctypes.byref(good), p, ctypes.byref(batch(a48)), 65536, p, 65536 * 64, p, 128, p, 128, 1, 1e4, 1e-5, p,
+                                      65536 * 64, null) == LIMIT
+    for b in (batch(a48, max_q=1, max_kv=1 << 20, max_pages=1 << 16), batch(a48, n_tokens=300, max_q=300, max_kv=1 << 16, max_pages=1 << 12)):
+        n = need(b)  # one long sequence: parts that are joined through the workspace
+        assert n > 0
+        assert attend(b, ws=null, nbytes=0) == NOMEM and attend(b, nbytes=n - 1) == NOMEM and attend(b, ws=null, nbytes=n) == NOMEM
+    assert need(batch(a48, n_seqs=0)) == 0 and need(batch(a48), heads=3) == 0
+
+
 def test_binding_refuses(a48):
     with pytest.raises(a48.A48Error):
         a48.PagedCache(5, 2, 64, 16, 4)
