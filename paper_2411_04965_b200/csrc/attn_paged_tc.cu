@@ -829,7 +829,9 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                         if (settled || !__any_sync(0xffffffffu, high)) break;
                         // ---- rarely: references to the largest scores of these columns where those are higher (rounded up to
                         // whole numbers: what moves along then moves by powers of two), and with them O, and the first columns'
-                        // weights while the second's are taken
+                        // weights while the second's are taken.  (Weights, and O of an earlier move, may still be on their way
+                        // into tensor memory: loads are ordered behind stores by this wait alone.)
+                        tmem_wait_st();
                         float corr[4];
 #pragma unroll
                         for (int i = 0; i < 4; ++i) corr[i] = -INFINITY;

@@ -617,3 +617,42 @@ def test_heads_of_zeros_and_of_tiny_numbers_without_eps(a48, cuda_dev, bits, dty
         assert (np.abs(g - x) <= 0.5 * gamma / levels * (1 + 1e-5)).all()  # half a step of the code
     q = torch.tensor(rng.standard_normal((n, kvh * hd)), dtype=torch.float32).to(torch.bfloat16)
     assert torch.isfinite(a48.attention_paged(s.cache, s.batch, q.to(cuda_dev)).float()).all()
+
+
+def weight_tail(n, vmax):
+    """What n weights below fp16's normal numbers lose at most: a weight times its value scale and unit is rounded by half a
+    subnormal step, 2^-25, and once more, by as much, if it is scaled down by 1/2 or less (so 1.5 2^-25 < 2^-24 in all); the unit
+    brings the largest value scale so far to 8 or more and codes are 128 at most, which makes it 2^-27 of the largest value
+    (`vmax` = 128 times the largest scale); the sum of the weights is 1/2 at least."""
+    return n * 2.0 ** -26 * vmax
+
+
+@pytest.mark.parametrize("bits", [8, 4, 3])
+@pytest.mark.parametrize("kv,tiles", [(128, 1), (512, 4)])
+def test_references_that_move_twice_within_a_tile(a48, cuda_dev, bits, kv, tiles):
+    """Every tile of 128 positions has a larger score than all before it in its first 64 positions and a larger one still in the
+    others: the second move finds the first's weights (and, behind the first tile, its outputs) just stored."""
+    rng = np.random.default_rng(29)
+    hd, q_len = 64, 128
+    s = Setup(a48, cuda_dev, bits, 1, hd, 32, [q_len, q_len], [kv + q_len] * 2, seed=18)
+    n = kv + q_len
+    direction = np.where(np.arange(hd) % 2, 1.0, -1.0)
+    k = 0.02 * rng.standard_normal((2 * n, hd))
+    size = 0.0
+    for t in range(tiles + 1):
+        for at in (128 * t + 5 + t, 128 * t + 70 + t):
+            size += 1.0
+            k[[at, n + at]] = size * direction
+    v = rng.standard_normal((2 * n, hd))
+    starts = np.array([0, n, 2 * n], np.int32)
+    kt, vt = (torch.tensor(x, dtype=torch.float32) for x in (k, v))
+    a48.paged_write(s.cache, s.view(starts, [n, n], 2 * n), kt.to(cuda_dev), vt.to(cuda_dev), rope_base=0.0)
+    s.oracle.write(starts, [n, n], s.table, kt.double().numpy(), vt.double().numpy(), 0.0, EPS32)
+    # the steps from one to the next are 1.5 .. 12 octaves times a row's factor: the new weights swallow the old ones or not
+    q = direction * rng.choice([0.25, 0.5, 1.0, 2.0], (2 * q_len, 2, 1)) + 0.01 * rng.standard_normal((2 * q_len, 2, hd))
+    q = torch.tensor(q.reshape(2 * q_len, -1), dtype=torch.float32).to(torch.bfloat16)
+    got = a48.attention_paged(s.cache, s.batch, q.to(cuda_dev), scale=0.125)
+    out, mag, top = s.oracle.attend(s.q_start, s.kv_len, s.table, q.double().numpy(), 2, 0.125)
+    vmax = np.abs(s.oracle.scales[1]).max() * 128
+    assert (np.abs(got.double().cpu().numpy().reshape(out.shape) - out) <= attention_bound(out, mag, top, hd, vmax) + weight_tail(n, vmax)).all()
+    assert a48.kernel_status()[0] == 0
