@@ -593,15 +593,8 @@ template <int BITS, int PD, int NT>
 __global__ void __launch_bounds__(32 * ROW_WARPS, NT == 2 ? 2 : BITS == 4 || PD == 64 ? 4 : 3) attn_paged_rows_kernel(const __grid_constant__ AttnArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
     RowsShared<BITS, PD, NT>& sm = *reinterpret_cast<RowsShared<BITS, PD, NT>*>(smem);
-    if (!a.beside) {
-        a48_pdl_prologue();
-        attend_rows<BITS, PD, NT>(a, sm);
-    } else {
-        // Launched behind the tile kernel, which lets it start once all that came before is done: the two write different
-        // rows.  The wait at the end keeps this kernel from completing ahead of the other.
-        attend_rows<BITS, PD, NT>(a, sm);
-        a48_pdl_prologue();
-    }
+    a48_pdl_prologue();
+    attend_rows<BITS, PD, NT>(a, sm);
 }
 
 // The parts of a row, in order.  One warp per (token, query head), four head dims per lane.
@@ -770,7 +763,6 @@ bitnet_a48_status bitnet_a48_attention_paged(const bitnet_a48_paged_cache* cache
     a.scale = scale > 0.f ? scale : 1.f / sqrtf((float)cache->head_dim);
     a.few_rows = p.few_rows;
     a.tiles = p.tiles, a.tile_rows = 8 * p.nt, a.ranks = p.ranks, a.clusters = p.clusters;
-    a.beside = p.many;
     a.tc_tiles = p.tc_tiles, a.tc_splits = p.tc_splits;
     a.part_ml = static_cast<float2*>(workspace_dev);
     a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + p.part_o);

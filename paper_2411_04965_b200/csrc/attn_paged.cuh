@@ -19,7 +19,6 @@ struct AttnArgs {
     // rows kernel: tiles of rows per sequence, rows of a tile, parts of the positions: `ranks` CTAs of a cluster that join
     // their sums, `clusters` of them that leave their sums to the join kernel
     int tiles, tile_rows, ranks, clusters;
-    bool beside;  // the rows kernel runs beside the tile kernel launched ahead of it
     // tile kernel: tiles of 256 rows per sequence (0: found by search), parts of the positions
     int tc_tiles, tc_splits;
     float* part_o;   // [part][token * heads + head][128]: sums of p sv d, relative to 2^part_m

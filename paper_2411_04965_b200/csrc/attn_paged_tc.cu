@@ -326,10 +326,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
     const uint32_t bar_full = smem_u32(ctrl), bar_empty = bar_full + 32, bar_s = bar_full + 64, bar_o = bar_full + 80,
                    bar_answer = bar_full + 96, bar_next = bar_full + 104;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;  // (known to be the same in a warp)
-    // (Dependents are let go only once what came before is done and seen: the rows kernel that follows may then start beside
-    // this one.)
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    a48_pdl_prologue();
 
     Item first;
     if (!item_of(a, blockIdx.x, lane, first)) return;

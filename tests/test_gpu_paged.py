@@ -656,3 +656,52 @@ def test_references_that_move_twice_within_a_tile(a48, cuda_dev, bits, kv, tiles
     vmax = np.abs(s.oracle.scales[1]).max() * 128
     assert (np.abs(got.double().cpu().numpy().reshape(out.shape) - out) <= attention_bound(out, mag, top, hd, vmax) + weight_tail(n, vmax)).all()
     assert a48.kernel_status()[0] == 0
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_plan_queries_and_cache_changed_right_ahead_of_each_mixed_call(a48, cuda_dev, captured):
+    """Prompts beside single tokens, step after step without a wait: the kernels of a call see the plan, the queries and the pages
+    that kernels just ahead of it wrote, and calls share one workspace in turn."""
+    rng = np.random.default_rng(30)
+    hd, kvh, heads, page, B, top = 64, 2, 8, 16, 6, 400
+    s = Setup(a48, cuda_dev, 4, kvh, hd, page, [0] * B, [top] * B, seed=19)
+    plans = [([150, 1, 0, 1, 2, 1], [300, 400, 9, 33, 2, 128]), ([1, 1, 200, 1, 0, 1], [301, 400, 200, 34, 2, 129]),
+             ([2, 90, 1, 1, 1, 80], [400, 400, 201, 35, 3, 209]), ([1, 1, 1, 1, 1, 1], [1, 1, 202, 36, 4, 210])]
+    n = max(sum(p[0]) for p in plans)
+    plan = [torch.tensor(np.concatenate([[0], np.cumsum(p[0]), p[1]]), dtype=torch.int32, device=cuda_dev) for p in plans]
+    k, v, q = ([torch.tensor(rng.standard_normal((n, m * hd)), dtype=torch.float32, device=cuda_dev) for _ in plans] for m in (kvh, kvh, heads))
+    batch = s.view(np.arange(B + 1, dtype=np.int32), [1] * B, n, max_q=200, max_kv=top)
+    now = [torch.zeros(n, m * hd, device=cuda_dev) for m in (kvh, kvh, heads)]
+    qr = [torch.zeros(n, heads * hd, dtype=torch.bfloat16, device=cuda_dev) for _ in plans]
+    out = [torch.zeros_like(x) for x in qr]
+    ws = torch.empty(max(16, a48.attention_paged_workspace_bytes(s.cache, batch, heads)), dtype=torch.uint8, device=cuda_dev)
+
+    def steps():
+        for i in range(len(plans)):
+            batch.q_start.copy_(plan[i][:B + 1])
+            batch.kv_len.copy_(plan[i][B + 1:])
+            for dst, src in zip(now, (k[i], v[i], q[i])):
+                dst.copy_(src)
+            a48.paged_write(s.cache, batch, now[0], now[1], q=now[2], q_out=qr[i])
+            a48.attention_paged(s.cache, batch, qr[i], out=out[i], workspace=ws)
+
+    steps()
+    torch.cuda.synchronize()
+    s.cache.pool.zero_()
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            steps()
+        s.cache.pool.zero_()
+        graph.replay()
+    else:
+        steps()
+    torch.cuda.synchronize()
+    for i, (q_lens, kv_lens) in enumerate(plans):
+        q_start = np.concatenate([[0], np.cumsum(q_lens)]).astype(np.int32)
+        s.oracle.write(q_start, kv_lens, s.table, k[i].double().cpu().numpy(), v[i].double().cpu().numpy(), 10000.0, EPS32)
+        ref, mag, best = s.oracle.attend(q_start, kv_lens, s.table, qr[i].double().cpu().numpy(), heads)
+        vmax, end = np.abs(s.oracle.scales[1]).max() * 128, int(q_start[-1])
+        bound = attention_bound(ref, mag, best, hd, vmax) + weight_tail(top, vmax)
+        assert (np.abs(out[i].double().cpu().numpy().reshape(ref.shape) - ref) <= bound)[:end].all()
+    assert a48.kernel_status()[0] == 0
