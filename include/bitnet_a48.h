@@ -357,7 +357,9 @@ size_t bitnet_a48_paged_cache_bytes(const bitnet_a48_paged_cache* cache);
 /* Stores the new tokens of the batch: k_dev, v_dev [n_tokens][n_kv_heads*head_dim] (fp32, or bf16 with x_bf16 != 0), the
  * keys rotated first (RoPE on the pairs (i, i + head_dim/2), angle position*rope_base^(-2i/head_dim)) unless rope_base is 0.
  * q_dev, q_out_dev: both NULL, or the queries [n_tokens][n_heads*head_dim] of k's type and where their rotated values go as
- * bf16 (q_out_dev may be q_dev with the same stride when x_bf16 != 0).  The codes are those of float64 arithmetic. */
+ * bf16 (q_out_dev may be q_dev with the same stride when x_bf16 != 0).  The codes are those of float64 arithmetic.  A key or
+ * value head with an entry that is no number gets NaN for a scale: it reads as NaN, what attends to it becomes NaN, and no
+ * other head is touched. */
 bitnet_a48_status bitnet_a48_paged_write(const bitnet_a48_paged_cache* cache, void* pool_dev, const bitnet_a48_paged_batch* batch,
                                          int n_heads, const void* q_dev, long long q_stride, const void* k_dev,
                                          long long k_stride, const void* v_dev, long long v_stride, int x_bf16,

@@ -72,6 +72,13 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int e, int bits, const
     }
 }
 
+// The larger of two numbers, NaN if either is none.
+__device__ __forceinline__ float max_or_nan(float x, float y) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
+    return r;
+}
+
 // Word `at` of a 3-bit row from its entries, one byte each.
 __device__ __forceinline__ uint32_t word_of_triples(const uint8_t* u, int at) {
     const int j = at % 3;
@@ -210,17 +217,18 @@ __global__ void __launch_bounds__(32 * kWarps, 4) paged_write_kernel(const __gri
             const double2 t = turn[e + i];
             return h == 0 ? (double)lo[i] * t.x - (double)hi[i] * t.y : (double)hi[i] * t.x + (double)lo[i] * t.y;
         };
+        // (a maximum that keeps what is no number: a head with a NaN has none for a scale, and reads as none)
         float top = 0.f;
 #pragma unroll
         for (int i = 0; i < W; ++i) {
             x[0][i] = turned ? lo[i] * c[i] - hi[i] * sn[i] : lo[i];
             x[1][i] = turned ? hi[i] * c[i] + lo[i] * sn[i] : hi[i];
-            top = fmaxf(top, fmaxf(fabsf(x[0][i]), fabsf(x[1][i])));
+            top = max_or_nan(top, max_or_nan(fabsf(x[0][i]), fabsf(x[1][i])));
         }
         float gamma_f = top;
 #pragma unroll
-        for (int o = G / 2; o > 0; o >>= 1) gamma_f = fmaxf(gamma_f, __shfl_xor_sync(0xffffffffu, gamma_f, o));
-        double gamma = turned ? 0.0 : (double)gamma_f;
+        for (int o = G / 2; o > 0; o >>= 1) gamma_f = max_or_nan(gamma_f, __shfl_xor_sync(0xffffffffu, gamma_f, o));
+        double gamma = turned && gamma_f == gamma_f ? 0.0 : (double)gamma_f;
         if (turned && there && top >= gamma_f * (1.f - 0x1p-20f)) {
 #pragma unroll
             for (int i = 0; i < W; ++i) gamma = fmax(gamma, fmax(fabs(exact(0, i)), fabs(exact(1, i))));
@@ -238,7 +246,7 @@ __global__ void __launch_bounds__(32 * kWarps, 4) paged_write_kernel(const __gri
                 worst = fmaxf(worst, fabsf(fmaf(x[h][i], step, magic - sum)));
                 u[h][i] = __float_as_uint(sum);
             }
-        // (out of the bounds' reach: numbers so small or so large, or none)
+        // (out of the bounds' reach: numbers so small or so large, or none, whose codes above may be more than `bits` wide)
         if (there && (worst > border || !(gamma_f > 0x1p-100f && gamma_f < 0x1p100f))) {
             const double multiple = (double)L / (gamma + a.eps);
 #pragma unroll

@@ -705,3 +705,47 @@ def test_plan_queries_and_cache_changed_right_ahead_of_each_mixed_call(a48, cuda
         bound = attention_bound(ref, mag, best, hd, vmax) + weight_tail(top, vmax)
         assert (np.abs(out[i].double().cpu().numpy().reshape(ref.shape) - ref) <= bound)[:end].all()
     assert a48.kernel_status()[0] == 0
+
+
+@pytest.mark.parametrize("bits", [8, 4, 3])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rope_base,hd", [(0.0, 64), (10000.0, 64), (10000.0, 36), (0.0, 100)])
+def test_heads_that_are_no_numbers_are_kept_as_such(a48, cuda_dev, bits, dtype, rope_base, hd):
+    """One NaN in a key or value head, and heads of nothing else: no scale is a number where the head is none, the codes and
+    scales of all other heads are the oracle's, and attention is NaN exactly for the rows and heads that see them."""
+    rng = np.random.default_rng(31)
+    kvh, heads, n, page = 3, 6, 150, 16
+    s = Setup(a48, cuda_dev, bits, kvh, hd, page, [n], [n], seed=20, garbage=True)
+    x = [torch.tensor(rng.standard_normal((n, kvh, hd)), dtype=torch.float32).to(dtype) for _ in range(2)]
+    bad = [(0, 0, 1, 3), (0, 17, 0, None), (1, 40, 1, hd - 1), (1, 40, 2, None), (0, 131, 2, hd // 2), (1, 149, 0, 0), (1, 0, 0, 5)]
+    sick = np.zeros((2, kvh, n), bool)
+    clean = [t.clone() for t in x]
+    for which, pos, head, entry in bad:
+        x[which][pos, head, slice(None) if entry is None else entry] = float("nan")
+        sick[which, head, pos] = True
+    a48.paged_write(s.cache, s.batch, *(t.view(n, -1).to(cuda_dev) for t in x), rope_base=rope_base)
+    s.oracle.write(s.q_start, s.kv_len, s.table, *(t.view(n, -1).double().numpy() for t in clean), rope_base, EPS32)
+    codes, scales, bos = paged.unpack_pool(s.cache.pool.cpu().numpy(), bits, kvh, hd, page, s.cache.n_pages)
+    for pos in range(n):
+        p, slot = paged.place(s.table, 0, pos, page, s.cache.n_pages)
+        first = bits == 3 and pos == 0
+        well = ~sick[:, :, pos]
+        assert np.array_equal((bos[:, p] if first else codes[:, p, :, slot])[well][:, :hd], (s.oracle.bos[:, p] if first else s.oracle.codes[:, p, :, slot])[well])
+        got, ref = scales[:, p, :, slot], s.oracle.scales[:, p, :, slot]
+        assert np.isnan(got[~well]).all() and (np.abs(got - ref)[well] <= HALF_F32 * ref[well] * (1 + 1e-6)).all()
+    read = [t.cpu().numpy() for t in a48.paged_read(s.cache, s.batch, dtype=torch.float32)]
+    for which in range(2):
+        assert np.array_equal(np.isnan(read[which]).all(-1), sick[which].T) and np.array_equal(np.isnan(read[which]).any(-1), sick[which].T)
+    q = torch.tensor(rng.standard_normal((n, heads * hd)), dtype=torch.float32).to(torch.bfloat16)
+    for q_len, window in ((n, 0), (n, 20), (8, 0), (8, 20), (1, 0)):  # tiles, and rows from the last ones on
+        q_start = np.array([0, q_len], np.int32)
+        got = a48.attention_paged(s.cache, s.view(q_start, s.kv_len, q_len), q[:q_len].to(cuda_dev), window=window)
+        got = got.double().cpu().numpy().reshape(q_len, heads, hd)
+        ref, mag, top = s.oracle.attend(q_start, s.kv_len, s.table, q[:q_len].double().numpy(), heads, 0.0, window, 0)
+        vmax = np.abs(s.oracle.scales[1]).max() * 128
+        right = (np.abs(got - ref) <= attention_bound(ref, mag, top, hd, vmax) + weight_tail(n, vmax)).all(-1)
+        for i in range(q_len):
+            last = n - q_len + i
+            sees = sick[:, :, max(0, last + 1 - window) if window else 0:last + 1].any((0, 2)).repeat(heads // kvh)
+            assert np.array_equal(np.isnan(got[i]).all(-1), sees) and right[i, ~sees].all(), (q_len, window, i)
+    assert a48.kernel_status()[0] == 0
