@@ -662,7 +662,10 @@ Plan plan_of(const bitnet_a48_paged_cache& c, const bitnet_a48_paged_batch& b, i
     long long reach = (long long)b.max_pages * c.page_size;
     if (b.max_kv < reach) reach = b.max_kv;
     // positions a tile of `span` tokens may see
-    auto seen = [&](long long span) { return window > 0 && window + sinks + span < reach ? window + sinks + span : reach; };
+    auto seen = [&](long long span) {
+        const long long most = (long long)window + sinks + span;
+        return window > 0 && most < reach ? most : reach;
+    };
     // Parts of the positions, a power of two, each with a pair of blocks for every warp at least.  As many as fit the SMs at
     // once (a second wave costs its start again: 8 sequences of 4 tokens, 27.8 us with 512 CTAs on 296 places, 18 with 256);
     // two where that would be one, which evens out sequences of unlike lengths (64 of 130 .. 8192 positions: 121 us with

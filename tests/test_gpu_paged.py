@@ -749,3 +749,17 @@ def test_heads_that_are_no_numbers_are_kept_as_such(a48, cuda_dev, bits, dtype, 
             sees = sick[:, :, max(0, last + 1 - window) if window else 0:last + 1].any((0, 2)).repeat(heads // kvh)
             assert np.array_equal(np.isnan(got[i]).all(-1), sees) and right[i, ~sees].all(), (q_len, window, i)
     assert a48.kernel_status()[0] == 0
+
+
+@pytest.mark.parametrize("q_lens,kv_lens", [([1, 1], [700, 33]), ([3, 2], [700, 33]), ([260, 1], [700, 33])])
+@pytest.mark.parametrize("window,sinks", [((1 << 31) - 1, 4), ((1 << 31) - 1, (1 << 31) - 1), (1 << 30, 1 << 30), (1, (1 << 31) - 1)])
+def test_windows_and_sinks_past_the_context(a48, cuda_dev, q_lens, kv_lens, window, sinks):
+    """Windows or sinks that reach over the whole context see what no window does, bit for bit."""
+    rng = np.random.default_rng(32)
+    hd, kvh, heads = 64, 2, 8
+    s = Setup(a48, cuda_dev, 4, kvh, hd, 32, q_lens, kv_lens, seed=21)
+    s.fill(rng)
+    q = torch.tensor(rng.standard_normal((s.n_tokens, heads * hd)), dtype=torch.float32).to(torch.bfloat16)
+    want = check_attention(s, q, heads)
+    got = a48.attention_paged(s.cache, s.batch, q.to(cuda_dev), window=window, sinks=sinks)
+    assert np.array_equal(got.double().cpu().numpy().reshape(want.shape), want)

@@ -148,3 +148,17 @@ def test_limits_and_workspace(a48):
 def test_binding_refuses(a48):
     with pytest.raises(a48.A48Error):
         a48.PagedCache(5, 2, 64, 16, 4)
+
+
+@pytest.mark.parametrize("kw,heads", [(dict(n_tokens=300, max_q=300), 4), (dict(max_q=1), 4), (dict(n_seqs=8, n_tokens=32, max_q=4), 2),
+                                      (dict(n_seqs=2, n_tokens=4096, max_q=2048), 4)])
+@pytest.mark.parametrize("big", [(1 << 30) - 1, 1 << 30, (1 << 31) - 1])
+def test_windows_and_sinks_of_any_size(a48, kw, heads, big):
+    """A window or sinks as long as the context cut a call up as no window does: the same workspace, however large they are."""
+    lib, good = a48.lib(), make(a48, heads=2, n_pages=1 << 12)
+    b = batch(a48, **dict(dict(max_kv=1 << 16, max_pages=1 << 12), **kw))
+    need = lambda window, sinks: lib.bitnet_a48_attention_paged_workspace_bytes(ctypes.byref(good), ctypes.byref(b), heads, window, sinks)  # noqa: E731
+    want = need(0, 0)
+    assert want > 0 or kw.get("n_seqs", 1) > 1
+    for window, sinks in ((big, 0), (big, 4), (big, big), (1 << 16, big), (1, big), (64, big)):
+        assert need(window, sinks) == want, (window, sinks)
