@@ -377,7 +377,8 @@ bitnet_a48_status bitnet_a48_paged_read(const bitnet_a48_paged_cache* cache, con
  *   q_dev, out_dev  bf16 [n_tokens][n_heads*head_dim]; query head h reads key/value head h / (n_heads / n_kv_heads)
  *   scale           factor of the scores; 0 means 1/sqrt(head_dim)
  * A token that sees nothing gets zeros.  Scores, softmax and sums are fp32, probabilities are rounded to fp16 in the second
- * product.  workspace_dev: bitnet_a48_attention_paged_workspace_bytes bytes (NULL when 0), no need to clear it. */
+ * product.  workspace_dev: bitnet_a48_attention_paged_workspace_bytes bytes (NULL when 0; at most 21 MB, whatever the sizes),
+ * no need to clear it. */
 size_t bitnet_a48_attention_paged_workspace_bytes(const bitnet_a48_paged_cache* cache, const bitnet_a48_paged_batch* batch,
                                                   int n_heads, int window, int sinks);
 bitnet_a48_status bitnet_a48_attention_paged(const bitnet_a48_paged_cache* cache, const void* pool_dev,

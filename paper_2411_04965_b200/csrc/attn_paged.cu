@@ -535,9 +535,10 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
     auto finish = [&](int r, int c, float top, float sum, const float (&acc)[4]) {
         const int token = sm.token[r], head = sm.head[r];
         if (a.clusters > 1) {
-            const size_t at = ((size_t)cluster * a.b.n_tokens + token) * a.heads + head;
-            reinterpret_cast<float4*>(a.part_o + at * 128)[c / 4] = make_float4(acc[0], acc[1], acc[2], acc[3]);
-            if (c == 0) a.part_ml[at] = make_float2(top, sum);
+            const a48p::Parts& to = a.row_parts;
+            const size_t at = (size_t)(cluster * to.rows + ((long long)seq * a.l.kv_heads + kvh) * to.per_head + r0 + r);
+            reinterpret_cast<float4*>(to.o + at * 128)[c / 4] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+            if (c == 0) to.ml[at] = make_float2(top, sum);
         } else {
             const float inv = sum != 0.f ? 1.f / sum : 0.f;
             const __nv_bfloat162 lo = __floats2bfloat162_rn(acc[0] * inv, acc[1] * inv), hi = __floats2bfloat162_rn(acc[2] * inv, acc[3] * inv);
@@ -597,34 +598,47 @@ __global__ void __launch_bounds__(32 * ROW_WARPS, NT == 2 ? 2 : BITS == 4 || PD 
     attend_rows<BITS, PD, NT>(a, sm);
 }
 
-// The parts of a row, in order.  One warp per (token, query head), four head dims per lane.
+// The parts of a row, in order.  One warp per place of a row, the rows kernel's ahead of the tile kernel's, four head dims per
+// lane.
 __global__ void __launch_bounds__(256) attn_paged_join_kernel(const __grid_constant__ AttnArgs a) {
     a48_pdl_prologue();
     const int lane = threadIdx.x & 31;
-    const long long id = (long long)blockIdx.x * 8 + (threadIdx.x >> 5), all = (long long)a.b.n_tokens * a.heads;
-    if (id >= all) return;
-    const int token = (int)(id / a.heads), head = (int)(id % a.heads);
-    const int s = a48p::sequence_of(a.b, token, lane);
-    if (s < 0) return;
-    const int start = __ldg(a.b.q_start + s), end = __ldg(a.b.q_start + s + 1);
-    const bool many = (long long)(end - start) * a.group > a.few_rows;
-    const int splits = many ? a.tc_splits : a.clusters, tiles = many ? a.tc_tiles : a.tiles;
-    if (splits == 1 || end > a.b.n_tokens) return;
-    const long long tile = ((long long)(token - start) * a.group + head % a.group) / (many ? a48p::TILE_ROWS : a.tile_rows);
-    if (tiles > 0 && tile >= tiles) return;  // past max_q
+    const long long ahead = a.row_parts.parts > 1 ? a.row_parts.rows : 0, place = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const bool many = place >= ahead;  // a row of the tile kernel
+    const a48p::Parts& from = many ? a.tile_parts : a.row_parts;
+    const long long id = many ? place - ahead : place;
+    if (from.parts == 1 || id >= from.rows) return;
+    int seq, token, head;
+    long long row;
+    if (from.per_head > 0) {
+        const long long of_head = id / from.per_head;
+        row = id - of_head * from.per_head;
+        seq = (int)(of_head / a.l.kv_heads);
+        head = (int)(of_head % a.l.kv_heads) * a.group + (int)(row % a.group);
+        token = __ldg(a.b.q_start + seq) + (int)(row / a.group);
+    } else {
+        token = (int)(id / a.heads), head = (int)(id % a.heads);
+        seq = a48p::sequence_of(a.b, token, lane);
+        if (seq < 0) return;
+        row = (long long)(token - __ldg(a.b.q_start + seq)) * a.group + head % a.group;
+    }
+    const int start = __ldg(a.b.q_start + seq), end = __ldg(a.b.q_start + seq + 1);
+    const long long all_rows = (long long)(end - start) * a.group;
+    if (row >= all_rows || all_rows > a.few_rows != many || start < 0 || end > a.b.n_tokens) return;
+    const int splits = from.parts;
     float top = -1e30f;
     for (int i = 0; i < splits; ++i) {
-        const float2 ml = __ldg(a.part_ml + i * all + id);
+        const float2 ml = __ldg(from.ml + i * from.rows + id);
         if (ml.y > 0.f) top = fmaxf(top, ml.x);
     }
     float sum = 0.f, acc[4] = {};
     for (int i = 0; i < splits; ++i) {
-        const float2 ml = __ldg(a.part_ml + i * all + id);
+        const float2 ml = __ldg(from.ml + i * from.rows + id);
         if (!(ml.y != 0.f)) continue;  // (a sum that is no number is passed on)
         const float corr = exp2_approx(ml.x - top);
         sum += corr * ml.y;
         if (4 * lane < a.l.hd) {
-            const float4 x = __ldg(reinterpret_cast<const float4*>(a.part_o + (i * all + id) * 128) + lane);
+            const float4 x = __ldg(reinterpret_cast<const float4*>(from.o + (i * from.rows + id) * 128) + lane);
             acc[0] += corr * x.x, acc[1] += corr * x.y, acc[2] += corr * x.z, acc[3] += corr * x.w;
         }
     }
@@ -644,7 +658,8 @@ constexpr int kFar = 1 << 30;  // what a window is cut to: position differences 
 struct Plan {
     bool many;  // some sequence may be the tile kernel's
     int nt, few_rows, tiles, ranks, clusters, tc_tiles, tc_splits;
-    size_t part_o, bytes;  // offset of the partial sums (exponents and sums of p come first), workspace
+    long long row_rows, row_per_head, tile_rows, tile_per_head;  // places of parts (a48p::Parts)
+    size_t row_o, tile_ml, tile_o, bytes;  // workspace: offsets of the parts (the rows kernel's exponents come first), and its size
 };
 
 long long up(long long x, long long y) { return (x + y - 1) / y; }
@@ -686,10 +701,19 @@ Plan plan_of(const bitnet_a48_paged_cache& c, const bitnet_a48_paged_batch& b, i
         const long long steps = up(seen(a48p::TILE_ROWS / group + 2 * a48p::TILE_POSITIONS), a48p::TILE_POSITIONS);
         p.tc_splits = within(SMS / real, 1, up(steps, 2) < 64 ? up(steps, 2) : 64);
     }
-    const int parts = p.clusters > p.tc_splits ? p.clusters : p.tc_splits;
-    const size_t ids = (size_t)b.n_tokens * heads * parts;
-    p.part_o = (ids * sizeof(float2) + 255) / 256 * 256;
-    p.bytes = parts > 1 ? p.part_o + ids * 128 * sizeof(float) : 0;
+    // Parts have places by the rows that can have them, so that a long prompt beside them, whose rows are not split, adds none:
+    // the rows kernel's are 37 x 16 at most (base * clusters is at most 2 SMS / MAX_RANKS where it leaves parts), the tile kernel's
+    // 148 x 256 (its tiles times parts fill the SMs once; by token where tiles are found by search, since n_tokens is what bounds
+    // those).
+    p.row_per_head = p.tiles * 8LL * p.nt, p.row_rows = (long long)b.n_seqs * c.n_kv_heads * p.row_per_head;
+    p.tile_per_head = (long long)p.tc_tiles * a48p::TILE_ROWS;
+    p.tile_rows = p.tc_tiles ? (long long)b.n_seqs * c.n_kv_heads * p.tile_per_head : (long long)b.n_tokens * heads;
+    const size_t row_places = p.clusters > 1 ? (size_t)p.row_rows * p.clusters : 0, tile_places = p.tc_splits > 1 ? (size_t)p.tile_rows * p.tc_splits : 0;
+    auto aligned = [](size_t n) { return (n + 255) / 256 * 256; };
+    p.row_o = aligned(row_places * sizeof(float2));
+    p.tile_ml = p.row_o + row_places * 128 * sizeof(float);
+    p.tile_o = p.tile_ml + aligned(tile_places * sizeof(float2));
+    p.bytes = p.tile_o + tile_places * 128 * sizeof(float);
     return p;
 }
 
@@ -767,8 +791,9 @@ bitnet_a48_status bitnet_a48_attention_paged(const bitnet_a48_paged_cache* cache
     a.few_rows = p.few_rows;
     a.tiles = p.tiles, a.tile_rows = 8 * p.nt, a.ranks = p.ranks, a.clusters = p.clusters;
     a.tc_tiles = p.tc_tiles, a.tc_splits = p.tc_splits;
-    a.part_ml = static_cast<float2*>(workspace_dev);
-    a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace_dev) + p.part_o);
+    char* const ws = static_cast<char*>(workspace_dev);
+    a.row_parts = {reinterpret_cast<float*>(ws + p.row_o), reinterpret_cast<float2*>(ws), p.row_rows, p.row_per_head, p.clusters};
+    a.tile_parts = {reinterpret_cast<float*>(ws + p.tile_o), reinterpret_cast<float2*>(ws + p.tile_ml), p.tile_rows, p.tile_per_head, p.tc_splits};
     if (p.many && (st = a48p::launch_tiles(a, cu)) != BITNET_A48_OK) return st;
     const bool wide = a.l.padded > 64;
     cudaError_t e;
@@ -776,9 +801,9 @@ bitnet_a48_status bitnet_a48_attention_paged(const bitnet_a48_paged_cache* cache
     else if (a.l.bits == 4) e = wide ? launch_rows<4, 128>(a, p.nt, cu) : launch_rows<4, 64>(a, p.nt, cu);
     else e = wide ? launch_rows<8, 128>(a, p.nt, cu) : launch_rows<8, 64>(a, p.nt, cu);
     A48_CUDA_TRY(e);
-    if (p.bytes) {  // (some kernel's parts: the join leaves rows that were not split alone)
-        const long long ids = (long long)batch->n_tokens * n_heads;
-        A48_CUDA_TRY(a48_launch_pdl(attn_paged_join_kernel, dim3((unsigned)((ids + 7) / 8)), dim3(256), 0, cu, a));
+    if (p.bytes) {
+        const long long places = (p.clusters > 1 ? p.row_rows : 0) + (p.tc_splits > 1 ? p.tile_rows : 0);
+        A48_CUDA_TRY(a48_launch_pdl(attn_paged_join_kernel, dim3((unsigned)((places + 7) / 8)), dim3(256), 0, cu, a));
     }
     return BITNET_A48_OK;
 }

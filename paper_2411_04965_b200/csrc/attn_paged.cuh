@@ -5,6 +5,16 @@
 
 namespace a48p {
 
+// Where a kernel leaves the sums of a part of the positions: `parts` times `rows` places, of a row each.  The places are those
+// of the rows that the kernel may have, not of the call's tokens: a row of a sequence is place (sequence * kv_heads + head) *
+// per_head + row, or (per_head 0) token * heads + head.
+struct Parts {
+    float* o;    // [part][row][128]: sums of p sv d, relative to 2^m
+    float2* ml;  // [part][row]: m, the exponent of the reference, and the sum of p
+    long long rows, per_head;
+    int parts;  // 1: none is left, the kernel has the whole sums
+};
+
 struct AttnArgs {
     Layout l;
     Batch b;
@@ -21,8 +31,7 @@ struct AttnArgs {
     int tiles, tile_rows, ranks, clusters;
     // tile kernel: tiles of 256 rows per sequence (0: found by search), parts of the positions
     int tc_tiles, tc_splits;
-    float* part_o;   // [part][token * heads + head][128]: sums of p sv d, relative to 2^part_m
-    float2* part_ml;  // [part][token * heads + head]: exponent of the reference, sum of p
+    Parts row_parts, tile_parts;
 };
 
 // What a tile of rows sees of its sequence: blocks of 2^SHIFT positions, [0, n_sink) and [first, first + count - n_sink).

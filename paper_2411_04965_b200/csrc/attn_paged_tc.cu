@@ -913,9 +913,15 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
             const Item done = items[k & 1];  // (again: not kept in registers meanwhile)
             int token, head;
             place_of(done, token, head);
-            const size_t id = (size_t)token * a.heads + head, part = (size_t)done.part * a.b.n_tokens * a.heads + id;
+            size_t part = 0;
+            if (split) {
+                const a48p::Parts& of = a.tile_parts;
+                const long long place = of.per_head > 0 ? ((long long)done.seq * a.l.kv_heads + done.kvh) * of.per_head + done.r0 + min(r, done.rows - 1)
+                                                        : (long long)token * a.heads + head;
+                part = (size_t)(done.part * of.rows + place);
+            }
             const float inv = unit == 0.f ? 0.f : split ? 1.f / unit : ml.y != 0.f ? 1.f / ml.y / unit : 0.f;
-            if (split && r < done.rows) a.part_ml[part] = ml;
+            if (split && r < done.rows) a.tile_parts.ml[part] = ml;
             const size_t to = split ? part * 128 : (size_t)token * a.out_stride + (size_t)head * a.l.hd;
             n0 += done.n_tiles;
             item_after(++k);
@@ -963,7 +969,7 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
                             const float* v = y + 16 * h + 4 * i;
                             put(i, __float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
                         }
-                        store_rows(reinterpret_cast<uint8_t*>(a.part_o) + 128 * c + 64 * h, 4, a.l.hd * 4 - 128 * c - 64 * h);
+                        store_rows(reinterpret_cast<uint8_t*>(a.tile_parts.o) + 128 * c + 64 * h, 4, a.l.hd * 4 - 128 * c - 64 * h);
                     }
                 } else {
 #pragma unroll

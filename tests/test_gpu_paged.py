@@ -763,3 +763,42 @@ def test_windows_and_sinks_past_the_context(a48, cuda_dev, q_lens, kv_lens, wind
     want = check_attention(s, q, heads)
     got = a48.attention_paged(s.cache, s.batch, q.to(cuda_dev), window=window, sinks=sinks)
     assert np.array_equal(got.double().cpu().numpy().reshape(want.shape), want)
+
+
+@pytest.mark.parametrize("q_lens,kv_lens,kvh,heads,tail,bounds", [
+    ([200, 1, 2, 0, 1], [300, 6000, 2500, 5, 1], 1, 4, 0, None),      # parts of decoding sequences beside a prompt
+    ([1, 2], [6000, 4001], 2, 8, 700, None),                          # decoding alone, token rows to spare
+    ([300, 1], [5000, 5000], 1, 2, 3000, None),                       # parts of both kernels, rows to spare
+    ([5, 90, 0, 40, 1], [3000, 2000, 0, 2100, 4000], 1, 4, 0, (2000, 4000)),  # tiles found by search, in parts
+    ([40, 40, 3], [2000, 2100, 2200], 1, 2, 5, (33, 3000)),           # sequences longer than max_q says
+])
+def test_workspace_between_guards(a48, cuda_dev, q_lens, kv_lens, kvh, heads, tail, bounds):
+    """A workspace of exactly the bytes asked for, full of what is no number, and the bytes around it left as they were."""
+    rng = np.random.default_rng(33)
+    hd = 64
+    s = Setup(a48, cuda_dev, 4, kvh, hd, 64, q_lens, kv_lens, seed=22, tail=tail)
+    s.fill(rng)
+    b = s.batch if bounds is None else s.view(s.q_start, s.kv_len, s.n_tokens, max_q=bounds[0], max_kv=bounds[1])
+    need = a48.attention_paged_workspace_bytes(s.cache, b, heads)
+    assert need > 0
+    room = torch.full((need + 8192,), 255, dtype=torch.uint8, device=cuda_dev)
+    ws = room[4096:4096 + need]
+    q = torch.tensor(rng.standard_normal((s.n_tokens, heads * hd)), dtype=torch.float32).to(torch.bfloat16)
+    out = torch.full((s.n_tokens, heads * hd), 7.0, dtype=torch.bfloat16, device=cuda_dev)
+    a48.attention_paged(s.cache, b, q.to(cuda_dev), out=out, workspace=ws)
+    ref, mag, top = s.oracle.attend(s.q_start, s.kv_len, s.table, q.double().numpy(), heads)
+    vmax, end = np.abs(s.oracle.scales[1]).max() * 128, int(s.q_start[-1])
+    got = out.double().cpu().numpy().reshape(ref.shape)
+    right = (np.abs(got - ref) <= attention_bound(ref, mag, top, hd, vmax) + weight_tail(max(kv_lens), vmax)).all((1, 2))
+    if bounds is None or bounds[0] >= max(q_lens):
+        assert right[:end].all()
+    else:
+        for i, n in enumerate(q_lens):
+            at = int(s.q_start[i])
+            assert right[at:at + min(n, bounds[0])].all()
+        assert (right | (got == 7).all((1, 2)))[:end].all()
+    assert (got[end:] == 7).all()
+    assert (room[:4096] == 255).all() and (room[4096 + need:] == 255).all()
+    with pytest.raises(a48.A48Error):
+        a48.attention_paged(s.cache, b, q.to(cuda_dev), workspace=ws[:need - 1])
+    assert a48.kernel_status()[0] == 0

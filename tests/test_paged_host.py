@@ -162,3 +162,27 @@ def test_windows_and_sinks_of_any_size(a48, kw, heads, big):
     assert want > 0 or kw.get("n_seqs", 1) > 1
     for window, sinks in ((big, 0), (big, 4), (big, big), (1 << 16, big), (1, big), (64, big)):
         assert need(window, sinks) == want, (window, sinks)
+
+
+@pytest.mark.parametrize("heads,kvh,hd,bits", [(32, 32, 128, 3), (32, 8, 128, 4), (32, 4, 64, 8), (32, 1, 128, 4), (16, 1, 96, 8), (1, 1, 4, 4), (300, 1, 32, 8)])
+def test_workspace_holds_only_what_is_split(a48, heads, kvh, hd, bits):
+    """Places of partial sums go by the rows that can be split, of which the SMs take 148 tiles of 256 at once and 37 of 16: long
+    prompts, many of them, token arrays with room to spare and bounds that are too large add none."""
+    lib, cfg = a48.lib(), make(a48, bits, kvh, hd, 64, 1 << 16)
+    bound = 520 * (148 * 256 + 37 * 16) + 4 * 256  # 128 sums, exponent and sum of a place; alignment
+    sizes = [1, 2, 3, 7, 8, 63, 64, 65, 200, 300, 2048, 16384, 32768, 1 << 20, 1 << 24]
+    worst = 0
+    for max_q in sizes:
+        for n_seqs in (1, 2, 5, 8, 64, 1000, 65535):
+            for n_tokens in {max_q, min(max_q * n_seqs, 1 << 24), 1 << 20}:
+                for max_kv, window in ((max_q, 0), (1 << 20, 0), (1 << 20, 2048), (1 << 20, 1)):
+                    b = batch(a48, n_seqs=n_seqs, n_tokens=n_tokens, max_q=max_q, max_kv=max_kv, max_pages=1 << 14)
+                    worst = max(worst, lib.bitnet_a48_attention_paged_workspace_bytes(ctypes.byref(cfg), ctypes.byref(b), heads, window, 4))
+    assert 0 < worst <= bound
+    prompt = batch(a48, n_tokens=1 << 14, max_q=1 << 14, max_kv=1 << 14, max_pages=1 << 8)
+    one = batch(a48, n_tokens=1, max_q=1, max_kv=1 << 14, max_pages=1 << 8)
+    need = [lib.bitnet_a48_attention_paged_workspace_bytes(ctypes.byref(cfg), ctypes.byref(b), heads, 0, 0) for b in (prompt, one)]
+    if heads > 16:  # the prompt alone fills the SMs: what is left is what one decoding sequence may have
+        assert need[0] <= 37 * 16 * 520 + 4 * 256
+    if heads // kvh <= 64:  # (more rows than that are the tile kernel's)
+        assert need[1] <= 37 * 16 * 520 + 4 * 256
