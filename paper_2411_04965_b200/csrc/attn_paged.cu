@@ -352,7 +352,8 @@ __device__ __forceinline__ void attend_rows(const AttnArgs& a, RowsShared<BITS, 
             load_words(block + k_off + 8 * row, k1);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                ks[b][i] = reinterpret_cast<const float*>(block + B::SK)[g + 8 * i] * factor;
+                const float scale = reinterpret_cast<const float*>(block + B::SK)[g + 8 * i];
+                ks[b][i] = fmaf(scale, 0.f, scale) * factor;  // (an infinite scale is none, not a score of -inf that would hide its key)
                 f[b][i] = reinterpret_cast<const float*>(block + B::SV)[g + 8 * i];
             }
             convert_k<BITS, PD>(k0, ka);

@@ -802,3 +802,41 @@ def test_workspace_between_guards(a48, cuda_dev, q_lens, kv_lens, kvh, heads, ta
     with pytest.raises(a48.A48Error):
         a48.attention_paged(s.cache, b, q.to(cuda_dev), workspace=ws[:need - 1])
     assert a48.kernel_status()[0] == 0
+
+
+@pytest.mark.parametrize("bits", [8, 4, 3])
+@pytest.mark.parametrize("hd,page", [(64, 16), (128, 64)])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_scales_that_are_no_numbers(a48, cuda_dev, bits, hd, page, bad):
+    """Key or value scales of single positions made infinite or no numbers in the pool itself: NaN for every row of the head that
+    sees one of them, and for no other; the rows kernel (few rows, parts joined in a cluster or by a kernel) and the tile kernel."""
+    rng = np.random.default_rng(34)
+    kvh, heads, n = 2, 4, 1000
+    s = Setup(a48, cuda_dev, bits, kvh, hd, page, [n], [n], seed=23)
+    s.fill(rng)
+    P = (hd + 31) // 32 * 32
+    row = P * bits // 8
+    chunk = 2 * page * row + 8 * page + (P if bits == 3 else 0)
+    pool = s.cache.pool.view(s.cache.n_pages, kvh, chunk)
+    sick = np.zeros((kvh, n), bool)
+    for which, pos, head in ((0, 0, 1), (1, 300, 0), (0, 555, 0), (1, 700, 1), (0, 997, 0), (1, 998, 1)):
+        p, slot = paged.place(s.table, 0, pos, page, s.cache.n_pages)
+        at = 2 * page * row + 4 * page * which + 4 * slot
+        pool[p, head, at:at + 4] = torch.tensor([bad], dtype=torch.float32).view(torch.uint8).to(cuda_dev)
+        sick[head, pos] = True
+    q = torch.tensor(rng.standard_normal((n, heads * hd)), dtype=torch.float32).to(torch.bfloat16)
+    for q_len, kv, window, sinks in ((n, n, 0, 0), (300, n, 40, 3), (300, n, 40, 0), (1, n, 0, 0), (1, 997, 200, 0), (4, n, 2, 0), (4, n, 2, 1), (9, 560, 3, 0),
+                                     (5, 280, 0, 0)):
+        q_start, kv_len = np.array([0, q_len], np.int32), np.array([kv], np.int32)
+        got = a48.attention_paged(s.cache, s.view(q_start, kv_len, q_len), q[:q_len].to(cuda_dev), window=window, sinks=sinks)
+        got = got.double().cpu().numpy().reshape(q_len, heads, hd)
+        ref, mag, top = s.oracle.attend(q_start, kv_len, s.table, q[:q_len].double().numpy(), heads, 0.0, window, sinks)
+        vmax = np.abs(s.oracle.scales[1]).max() * 128
+        right = (np.abs(got - ref) <= attention_bound(ref, mag, top, hd, vmax) + weight_tail(n, vmax)).all(-1)
+        j = np.arange(n)
+        for i in range(q_len):
+            p = kv - q_len + i
+            seen = (j <= p) & ((j > p - window) | (j < sinks) if window else True)
+            sees = (sick & seen).any(1).repeat(heads // kvh)
+            assert np.array_equal(np.isnan(got[i]).all(-1), sees) and right[i, ~sees].all(), (q_len, kv, window, i)
+    assert a48.kernel_status()[0] == 0
