@@ -515,11 +515,11 @@ def _made_current(t: torch.Tensor, stream):
 
 
 def _rows(t: torch.Tensor, cache: "PagedCache", n_tokens: int, width: int, dtype) -> int:
-    """Stride of token rows [n_tokens, width] on the cache's device whose columns are contiguous."""
+    """Stride of token rows [n_tokens, width] on the cache's device whose columns are contiguous; of one row any will do."""
     assert t.get_device() == cache.device_index and t.dtype == dtype and t.shape == (n_tokens, width)
     stride, one = t.stride()
     assert one == 1 or width == 1
-    return stride if n_tokens > 1 else max(stride, width)
+    return stride if n_tokens > 1 else width
 
 
 def paged_write(cache: PagedCache, batch: PagedBatch, k: torch.Tensor, v: torch.Tensor, q=None, rope_base: float = 10000.0,

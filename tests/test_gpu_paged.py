@@ -840,3 +840,22 @@ def test_scales_that_are_no_numbers(a48, cuda_dev, bits, hd, page, bad):
             sees = (sick & seen).any(1).repeat(heads // kvh)
             assert np.array_equal(np.isnan(got[i]).all(-1), sees) and right[i, ~sees].all(), (q_len, kv, window, i)
     assert a48.kernel_status()[0] == 0
+
+
+def test_one_token_out_of_rows_of_an_odd_length(a48, cuda_dev):
+    rng = np.random.default_rng(35)
+    hd, kvh, heads = 64, 1, 2
+    s = Setup(a48, cuda_dev, 4, kvh, hd, 16, [1], [40], seed=24)
+    s.fill(rng)
+    width = (heads + 2 * kvh) * hd
+    rows = torch.zeros(3, width + 9, device=cuda_dev)  # an odd stride, and row 0 on a 16-byte boundary
+    rows[0, :width] = torch.tensor(rng.standard_normal(width), dtype=torch.float32)
+    q, k, v = rows[:1, :width].split([heads * hd, kvh * hd, kvh * hd], 1)
+    qr = torch.zeros(3, heads * hd + 9, dtype=torch.bfloat16, device=cuda_dev)[:1, :heads * hd]
+    assert a48.paged_write(s.cache, s.batch, k, v, q=q, q_out=qr) is qr
+    s.oracle.write(s.q_start, s.kv_len, s.table, k.double().cpu().numpy(), v.double().cpu().numpy(), 10000.0, EPS32)
+    out = torch.zeros(3, heads * hd + 9, dtype=torch.bfloat16, device=cuda_dev)
+    a48.attention_paged(s.cache, s.batch, qr, out=out[:1, :heads * hd])
+    want = check_attention(s, qr.cpu(), heads)
+    assert np.array_equal(out[:1, :heads * hd].double().cpu().numpy().reshape(want.shape), want)
+    assert (out[1:] == 0).all() and (out[0, heads * hd:] == 0).all()

@@ -186,3 +186,18 @@ def test_workspace_holds_only_what_is_split(a48, heads, kvh, hd, bits):
         assert need[0] <= 37 * 16 * 520 + 4 * 256
     if heads // kvh <= 64:  # (more rows than that are the tile kernel's)
         assert need[1] <= 37 * 16 * 520 + 4 * 256
+
+
+def test_stride_of_a_single_row_does_not_matter(a48):
+    """A token's row out of rows of any length: its stride is never used, so none is refused."""
+    torch = pytest.importorskip("torch")
+
+    class OnTheHost:
+        device_index = -1
+
+    rows = torch.zeros(6, 131)
+    assert a48._rows(rows[3:4, 4:132], OnTheHost, 1, 127, torch.float32) == 127
+    assert a48._rows(rows[3:4, 4:68], OnTheHost, 1, 64, torch.float32) == 64
+    assert a48._rows(rows[2:4, 4:68], OnTheHost, 2, 64, torch.float32) == 131
+    with pytest.raises(AssertionError):  # columns apart
+        a48._rows(torch.zeros(64, 6).t()[1:2], OnTheHost, 1, 64, torch.float32)
