@@ -721,7 +721,7 @@ Plan plan_of(const bitnet_a48_paged_cache& c, const bitnet_a48_paged_batch& b, i
 template <int BITS, int PD, int NT>
 cudaError_t launch_rows(const AttnArgs& a, cudaStream_t st) {
     constexpr size_t SMEM = sizeof(RowsShared<BITS, PD, NT>);
-    static bool allowed[64];
+    static std::atomic<bool> allowed[64];
     const cudaError_t e = a48_allow_smem(attn_paged_rows_kernel<BITS, PD, NT>, SMEM, allowed);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};

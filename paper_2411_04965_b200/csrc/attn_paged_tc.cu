@@ -1000,7 +1000,7 @@ template <int BITS, int PD>
 cudaError_t launch(const AttnArgs& a, cudaStream_t st) {
     const long long tiles = a.tc_tiles > 0 ? (long long)a.tc_tiles * a.b.n_seqs : (long long)a.b.n_tokens * a.group / a48p::TILE_ROWS + a.b.n_seqs;
     const dim3 grid((unsigned)(tiles * a.l.kv_heads * a.tc_splits));
-    static bool allowed[64];
+    static std::atomic<bool> allowed[64];
     const cudaError_t e = a48_allow_smem(attn_paged_tc_kernel<BITS, PD>, Cfg<PD>::SMEM, allowed);
     return e != cudaSuccess ? e : a48_launch_pdl(attn_paged_tc_kernel<BITS, PD>, grid, dim3(THREADS), (size_t)Cfg<PD>::SMEM, st, a);
 }

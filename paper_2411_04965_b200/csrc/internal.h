@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "bitnet_a48.h"
 
 #define A48_CUDA_TRY(expr)                                  \
@@ -39,14 +41,15 @@ static inline cudaError_t a48_launch_pdl(void (*kernel)(KArgs...), dim3 grid, di
 #endif
 
 #ifdef __CUDACC__
-// Allows a kernel its dynamic shared memory on the current device; asked of the runtime once per device.
+// Allows a kernel its dynamic shared memory on the current device; asked of the runtime once per device (or more often, by
+// threads that make their first call at once).
 template <typename... KArgs>
-static inline cudaError_t a48_allow_smem(void (*kernel)(KArgs...), size_t bytes, bool (&done)[64]) {
+static inline cudaError_t a48_allow_smem(void (*kernel)(KArgs...), size_t bytes, std::atomic<bool> (&done)[64]) {
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
-    if (e != cudaSuccess || (device < 64 && done[device])) return e;
+    if (e != cudaSuccess || (device < 64 && done[device].load(std::memory_order_acquire))) return e;
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e == cudaSuccess && device < 64) done[device] = true;
+    if (e == cudaSuccess && device < 64) done[device].store(true, std::memory_order_release);
     return e;
 }
 #endif

@@ -859,3 +859,36 @@ def test_one_token_out_of_rows_of_an_odd_length(a48, cuda_dev):
     want = check_attention(s, qr.cpu(), heads)
     assert np.array_equal(out[:1, :heads * hd].double().cpu().numpy().reshape(want.shape), want)
     assert (out[1:] == 0).all() and (out[0, heads * hd:] == 0).all()
+
+
+def test_two_host_threads_at_once(a48, cuda_dev):
+    """First calls and later ones from threads of their own, each on its stream with a cache of its own and kernels that the
+    other launches too."""
+    import threading
+
+    rng = np.random.default_rng(36)
+    work = []
+    for i in range(2):
+        s = Setup(a48, cuda_dev, (4, 3)[i], 2, 128, 32, [150, 1, 3], [400, 900, 70], seed=25 + i)
+        s.fill(rng)
+        q = torch.tensor(rng.standard_normal((s.n_tokens, 8 * 128)), dtype=torch.float32).to(torch.bfloat16)
+        work.append((s, q.to(cuda_dev), check_attention(s, q, 8), torch.cuda.Stream(), []))
+    torch.cuda.synchronize()
+    start = threading.Barrier(2)
+
+    def run(s, q, want, stream, got):
+        start.wait()
+        with torch.cuda.stream(stream):
+            for other in work + work:
+                got.append((other[2], a48.attention_paged(other[0].cache, other[0].batch, other[1])))
+            stream.synchronize()
+
+    threads = [threading.Thread(target=run, args=w) for w in work]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for w in work:
+        assert len(w[4]) == 4
+        for want, y in w[4]:
+            assert np.array_equal(y.double().cpu().numpy().reshape(want.shape), want)
