@@ -892,3 +892,76 @@ def test_two_host_threads_at_once(a48, cuda_dev):
         assert len(w[4]) == 4
         for want, y in w[4]:
             assert np.array_equal(y.double().cpu().numpy().reshape(want.shape), want)
+
+
+@pytest.mark.parametrize("bits", [8, 4, 3])
+@pytest.mark.parametrize("hd,kvh,heads,dtype", [(128, 2, 3, torch.bfloat16), (100, 1, 2, torch.float32), (64, 3, 3, torch.float32), (36, 1, 1, torch.bfloat16)])
+def test_codes_of_long_prompts_one_by_one(a48, cuda_dev, bits, hd, kvh, heads, dtype):
+    """Enough tokens for the form that takes four to a block, a count that four does not divide, sequences that begin and end
+    inside a block: every code and scale, and the rotated queries, against float64."""
+    rng = np.random.default_rng(37)
+    page, q_lens = 32, [1, 601, 0, 2, 593, 90]
+    kv_lens = [1, 601, 4, 2, 700, 91]
+    s = Setup(a48, cuda_dev, bits, kvh, hd, page, q_lens, kv_lens, seed=27, garbage=True, tail=2)
+    n, real = s.n_tokens, int(s.q_start[-1])
+    assert n >= 1184 and n % 4
+    k, v, q = (torch.tensor(rng.standard_normal((n, m * hd)) * np.exp2(rng.integers(-8, 9, (n, 1))), dtype=torch.float32).to(dtype) for m in (kvh, kvh, heads))
+    qr = torch.full((n, heads * hd), 7.0, dtype=torch.bfloat16, device=cuda_dev)
+    a48.paged_write(s.cache, s.batch, k.to(cuda_dev), v.to(cuda_dev), q=q.to(cuda_dev), q_out=qr)
+    # the definition over all tokens at once, in 64 bits
+    where = np.array([(b, pos) for _, b, _, pos in paged.tokens(s.q_start, s.kv_len)])
+    pos = where[:, 1]
+    angle = pos[:, None] * 10000.0 ** (-2.0 * np.arange(hd // 2) / hd)
+    c, sn = np.cos(angle)[:, None], np.sin(angle)[:, None]
+
+    def turned(x):
+        lo, hi = x[..., :hd // 2], x[..., hd // 2:]
+        return np.concatenate([lo * c - hi * sn, hi * c + lo * sn], -1)
+
+    kn, vn, qn = (t.double().numpy()[:real].reshape(real, -1, hd) for t in (k, v, q))
+    codes, scales, bos = paged.unpack_pool(s.cache.pool.cpu().numpy(), bits, kvh, hd, page, s.cache.n_pages)
+    at = np.array([paged.place(s.table, b, p, page, s.cache.n_pages) for b, p in where])
+    for which, x in enumerate((turned(kn), vn)):
+        got = codes[which][at[:, 0], :, at[:, 1]][..., :hd]
+        first = pos == 0
+        if bits == 3:
+            got[first] = bos[which][at[first, 0]][..., :hd]
+        for rows, b in ((first, 4 if bits == 3 else bits), (~first, bits)):
+            want, scale = paged.quantise(x[rows], b, EPS32)
+            assert np.array_equal(got[rows], want)
+            held = scales[which][at[rows, 0], :, at[rows, 1]]
+            assert (np.abs(held - scale) <= HALF_F32 * scale * (1 + 1e-6)).all()
+    want = turned(qn)
+    part = np.abs(qn) + np.abs(np.concatenate([qn[..., hd // 2:], qn[..., :hd // 2]], -1))
+    out = qr.double().cpu().numpy().reshape(n, heads, hd)
+    assert (np.abs(out[:real] - want) <= HALF_BF16 * np.abs(want) + 4 * HALF_F32 * part * (1 + HALF_BF16)).all()
+    assert (out[real:] == 7).all()
+
+
+@pytest.mark.parametrize("q_len,kv_len", [(1, 900), (3, 77), (120, 500)])
+def test_a_sequence_among_others(a48, cuda_dev, q_len, kv_len):
+    """One sequence alone, beside prompts, beside many single tokens and behind longer bounds: the cut into parts is another each
+    time, and each result lies within the bound of the oracle's."""
+    rng = np.random.default_rng(38)
+    hd, kvh, heads, page = 64, 2, 8, 32
+    others = {"alone": ([], []), "prompts": ([300, 90], [300, 1200]), "tokens": ([1] * 40, list(rng.integers(1, 600, 40))), "few": ([2, 5], [33, 64])}
+    seen = []
+    for name, (q_lens, kv_lens) in others.items():
+        s = Setup(a48, cuda_dev, 4, kvh, hd, page, [q_len] + q_lens, [kv_len] + [int(n) for n in kv_lens], seed=28)
+        s.fill(np.random.default_rng(39))
+        first = a48.PagedBatch(torch.tensor([0, kv_len], dtype=torch.int32, device=cuda_dev), s.batch.kv_len[:1], s.batch.pages[:1], kv_len, kv_len, kv_len)
+        x = np.random.default_rng(40)
+        k, v = (torch.tensor(x.standard_normal((kv_len, kvh * hd)), dtype=torch.float32) for _ in range(2))
+        a48.paged_write(s.cache, first, k.to(cuda_dev), v.to(cuda_dev))
+        s.oracle.write([0, kv_len], [kv_len], s.table[:1], k.numpy(), v.numpy(), 10000.0, EPS32)
+        q = torch.tensor(np.concatenate([np.random.default_rng(41).standard_normal((q_len, heads * hd)),
+                                         rng.standard_normal((sum(q_lens), heads * hd))]), dtype=torch.float32).to(torch.bfloat16)
+        for batch in (s.batch, s.view(s.q_start, s.kv_len, s.n_tokens, max_q=700, max_kv=20000)):
+            got = a48.attention_paged(s.cache, batch, q.to(cuda_dev)).double().cpu().numpy().reshape(-1, heads, hd)
+            ref, mag, top = s.oracle.attend(s.q_start, s.kv_len, s.table, q.double().numpy(), heads)
+            vmax = np.abs(s.oracle.scales[1]).max() * 128
+            assert (np.abs(got - ref) <= attention_bound(ref, mag, top, hd, vmax) + weight_tail(max(kv_len, 1200), vmax)).all(), name
+            seen.append((got[:q_len], ref[:q_len], (attention_bound(ref, mag, top, hd, vmax) + weight_tail(max(kv_len, 1200), vmax))[:q_len]))
+    for got, ref, bound in seen[1:]:
+        assert np.allclose(ref, seen[0][1], rtol=1e-12, atol=1e-14)  # the same sequence each time
+        assert (np.abs(got - seen[0][0]) <= bound + seen[0][2]).all()
