@@ -965,3 +965,24 @@ def test_a_sequence_among_others(a48, cuda_dev, q_len, kv_len):
     for got, ref, bound in seen[1:]:
         assert np.allclose(ref, seen[0][1], rtol=1e-12, atol=1e-14)  # the same sequence each time
         assert (np.abs(got - seen[0][0]) <= bound + seen[0][2]).all()
+
+
+@pytest.mark.parametrize("bits,hd,heads,page", [(4, 64, 4, 16), (3, 128, 2, 64), (8, 100, 3, 32)])
+def test_beside_the_attention_of_a_contiguous_cache(a48, cuda_dev, bits, hd, heads, page):
+    """The keys and values read back from the pages through the framework's attention over a contiguous fp32 cache: the same
+    outputs, within the bound of the paged one and the other's fp32 rounding."""
+    rng = np.random.default_rng(42)
+    B, T, cached = 3, 70, 61
+    s = Setup(a48, cuda_dev, bits, heads, hd, page, [T] * B, [T + cached] * B, seed=29)
+    s.fill(rng)
+    n = T + cached
+    every = s.view(np.arange(B + 1, dtype=np.int32) * n, s.kv_len, B * n)
+    k, v = (t.view(B, n, heads, hd).transpose(1, 2).contiguous() for t in a48.paged_read(s.cache, every, dtype=torch.float32))
+    q = torch.tensor(rng.standard_normal((B * T, heads * hd)), dtype=torch.float32).to(torch.bfloat16)
+    want = a48.attention_prefill(q.float().to(cuda_dev), k, v, B, T, pos0=cached).double().cpu().numpy().reshape(B * T, heads, hd)
+    got = check_attention(s, q, heads)
+    out, mag, top = s.oracle.attend(s.q_start, s.kv_len, s.table, q.double().numpy(), heads)
+    vmax = np.abs(s.oracle.scales[1]).max() * 128
+    # the other call: 4e-8 |score| relative to the row's largest output, and a rounding of the read value
+    other = (4e-8 * top[..., None] + 4 * HALF_F32) * np.abs(out).max(-1, keepdims=True) + 2 * HALF_F32 * (1 + 2 * top[..., None]) * mag
+    assert (np.abs(got - want) <= attention_bound(out, mag, top, hd, vmax) + weight_tail(n, vmax) + other).all()
