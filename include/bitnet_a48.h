@@ -331,8 +331,9 @@ bitnet_a48_status bitnet_a48_attention_prefill(const float* q_dev, const float* 
  * The three arrays are device memory (4-byte aligned), read when the call runs: a captured graph may be replayed with other
  * contents.  n_tokens: rows of the token arrays, rows outside q_start[0] .. q_start[n_seqs]-1 are neither read nor written.
  * max_q, max_kv: upper bounds of the new tokens and of the positions of one sequence; they size the launch.  More than
- * max_q new tokens of a sequence: those past max_q may get no attention output.  Limits (BITNET_A48_ERR_LIMIT past them):
- * n_seqs and n_heads 65535, n_tokens and max_pages*page_size 2^30, n_tokens*n_heads 2^31 - 1, n_kv_heads*n_seqs
+ * max_q new tokens of a sequence: those past max_q may get no attention output.  A call without tokens or sequences is refused
+ * (BITNET_A48_ERR_SHAPE), sequences without new tokens are not.  Limits (BITNET_A48_ERR_LIMIT past them):
+ * n_seqs and n_heads 65535, n_tokens and max_pages*page_size 2^30 (kv_len too, unchecked), n_tokens*n_heads 2^31 - 1, n_kv_heads*n_seqs
  * (2^31 - 1) / 8.  A position without a page (negative, past the
  * table, or an entry outside 0 .. n_pages-1) is not stored, reads as zero, and is not attended to; nothing faults.
  *
@@ -376,9 +377,13 @@ bitnet_a48_status bitnet_a48_paged_read(const bitnet_a48_paged_cache* cache, con
  * positions j <= p and, with window > 0, of those the last `window` (j > p - window) and the first `sinks` (j < sinks).
  *   q_dev, out_dev  bf16 [n_tokens][n_heads*head_dim]; query head h reads key/value head h / (n_heads / n_kv_heads)
  *   scale           factor of the scores; 0 means 1/sqrt(head_dim)
- * A token that sees nothing gets zeros.  Scores, softmax and sums are fp32, probabilities are rounded to fp16 in the second
- * product.  workspace_dev: bitnet_a48_attention_paged_workspace_bytes bytes (NULL when 0; at most 21 MB, whatever the sizes),
- * no need to clear it. */
+ * A token that sees nothing gets zeros.  A window, or sinks, past the context count as the context.
+ * Scores, softmax and sums are fp32; probabilities times the value scales are rounded to fp16 for the second product.  Both
+ * products run on fp16 numbers scaled by powers of two that rows share: where query rows of a call differ by more than 2^14 in
+ * size, the smaller may lose bits, and each position adds an error of up to 2^-26 of the largest value that the new tokens of
+ * its sequence see.
+ *   workspace_dev   bitnet_a48_attention_paged_workspace_bytes bytes (NULL when 0; at most 21 MB, whatever the sizes), no
+ *                   need to clear it */
 size_t bitnet_a48_attention_paged_workspace_bytes(const bitnet_a48_paged_cache* cache, const bitnet_a48_paged_batch* batch,
                                                   int n_heads, int window, int sinks);
 bitnet_a48_status bitnet_a48_attention_paged(const bitnet_a48_paged_cache* cache, const void* pool_dev,

@@ -29,7 +29,7 @@
 // A CTA that is through with its rows cancels one that has not started and takes its rows over, so that the codes and queries
 // of the next rows are under way while the last weights are multiplied and outputs stored.  Four prompts of 4096 tokens, 32
 // heads of 128, 3 bits: 672 us (818 TFLOP/s of the 4 x 128 operations per score); two chunks of up to 2048 tokens with a
-// window of 2048, 196 us.  On the way there, for the prompts: one CTA to each tile of rows 854 us, taking over 821, masks by
+// window of 2048, 181 us.  On the way there, for the prompts: one CTA to each tile of rows 854 us, taking over 821, masks by
 // groups of 16 positions and no tiles that the first rows do not see 691, queries converted eight rows at a time 669.
 //
 // What bounds it: 128 positions take a CTA about 4250 clocks, of which the products of both tiles occupy the tensor pipe for

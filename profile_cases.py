@@ -5,12 +5,16 @@
     python profile_cases.py decode --M 1 --N 11008 --K 4096 --kind topk --copies 32 --reps 3
     python profile_cases.py block  --B 1 --T 2048 --hidden 4096 --ffn 11008 --heads 32 --reps 3
     python profile_cases.py block  --B 1 --T 1 --ctx 2048 --reps 4          # one decode step against a cached context
+    python profile_cases.py paged_write  --B 4 --T 2048 --kv-heads 8 --bits 4          # prompts of bf16 q, k, v
+    python profile_cases.py paged_read   --B 16 --T 2048 --kv-heads 8 --bits 4         # every position, as bf16
+    python profile_cases.py paged_attend --B 64 --T 1 --ctx 4095 --kv-heads 8 --bits 4 # T new tokens behind ctx positions
 
 Each case builds seeded synthetic inputs (the same recipes the benchmark uses),
 runs the kernel `reps` times after one warm-up call and prints the mean time
 from CUDA events on the launching stream.  `decode` cycles over `copies`
 distinct weight matrices so that the weight bytes come from HBM, not L2.  `block` is one transformer block on a
-prefill of B sequences of T tokens (quantisers, the seven BitLinears, RoPE, the tensor-core attention).
+prefill of B sequences of T tokens (quantisers, the seven BitLinears, RoPE, the tensor-core attention).  The `paged`
+cases run one operator of the paged cache over B sequences of one length, pages in shuffled order.
 (The sweep over the token count is a leg of the benchmark: `python bench.py --legs sweep`.)
 """
 from __future__ import annotations
@@ -49,9 +53,48 @@ def _acts(kind, M, K, dev, k_frac=0.5):
     return x, codes, scale, a48.ACT_TOPK_INT8
 
 
+def _paged(args, dev, stream):
+    B, T, n, hd, kvh = args.B, args.T, args.ctx + args.T, args.head_dim, args.kv_heads
+    per = (n + args.page - 1) // args.page
+    cache = a48.PagedCache(args.bits, kvh, hd, args.page, B * per, device=dev)
+    gen = torch.Generator(device=dev).manual_seed(21)
+    pages = torch.randperm(B * per, generator=gen, device=dev).to(torch.int32).view(B, per)
+
+    def batch(new):
+        i32 = dict(dtype=torch.int32, device=dev)
+        return a48.PagedBatch(torch.arange(B + 1, **i32) * new, torch.full((B,), n, **i32), pages, B * new, new, n)
+
+    def heads(rows, count):
+        return torch.randn(rows, count * hd, generator=gen, device=dev, dtype=torch.bfloat16)
+
+    k, v = heads(B * n, kvh), heads(B * n, kvh)
+    a48.paged_write(cache, batch(n), k, v)
+    q, new = heads(B * T, args.heads), batch(T)
+    row = (hd + 31) // 32 * 32 * args.bits // 8 + 4
+    if args.case == "paged_write":
+        k, v, qr = k[:B * T].contiguous(), v[:B * T].contiguous(), torch.empty_like(q)
+        ms = _time(lambda: a48.paged_write(cache, new, k, v, q=q, q_out=qr), args.reps, stream)
+        moved = B * T * (4 * args.heads * hd + 2 * kvh * (2 * hd + row))
+    elif args.case == "paged_read":
+        del k, v
+        ko, vo = a48.paged_read(cache, new)
+        ms = _time(lambda: a48.paged_read(cache, new, k_out=ko, v_out=vo), args.reps, stream)
+        moved = B * T * 2 * kvh * (row + 2 * hd)
+    else:
+        del k, v
+        y = torch.empty_like(q)
+        need = a48.attention_paged_workspace_bytes(cache, new, args.heads, args.window, args.sinks)
+        wsp = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+        ms = _time(lambda: a48.attention_paged(cache, new, q, window=args.window, sinks=args.sinks, out=y, workspace=wsp), args.reps, stream)
+        seen = n if args.window == 0 else min(n, args.window + T - 1 + args.sinks)
+        moved = B * (T * args.heads * hd * 4 + seen * 2 * kvh * row)
+    return {"case": args.case, "B": B, "T": T, "ctx": args.ctx, "heads": args.heads, "kv_heads": kvh, "head_dim": hd, "bits": args.bits,
+            "page": args.page, "ms": ms, "bytes": moved, "gbs": moved / ms / 1e6}
+
+
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("case", choices=["gemm", "quant", "decode", "block"])
+    ap.add_argument("case", choices=["gemm", "quant", "decode", "block", "paged_write", "paged_read", "paged_attend"])
     ap.add_argument("--M", type=int, default=8192)
     ap.add_argument("--N", type=int, default=11008)
     ap.add_argument("--K", type=int, default=4096)
@@ -64,7 +107,13 @@ def main():
     ap.add_argument("--hidden", type=int, default=4096)
     ap.add_argument("--ffn", type=int, default=11008)
     ap.add_argument("--heads", type=int, default=32)
-    ap.add_argument("--ctx", type=int, default=0, help="block: cached positions in front of the call (fp32 cache), e.g. a decode step")
+    ap.add_argument("--ctx", type=int, default=0, help="block, paged: cached positions in front of the call, e.g. of a decode step")
+    ap.add_argument("--kv-heads", type=int, default=8)
+    ap.add_argument("--head-dim", type=int, default=128)
+    ap.add_argument("--bits", type=int, default=4)
+    ap.add_argument("--page", type=int, default=64)
+    ap.add_argument("--window", type=int, default=0)
+    ap.add_argument("--sinks", type=int, default=0)
     args = ap.parse_args()
     a48_build.build()
     dev = torch.device("cuda:0")
@@ -91,6 +140,8 @@ def main():
         hd = Hs // args.heads
         out = {"case": "block", "B": B, "T": T, "hidden": Hs, "ffn": Fs, "heads": args.heads, "ms": ms,
                "tokens_per_s": B * T / (ms * 1e-3), "attention_gflop": 4.0 * B * args.heads * (T * T / 2.0) * hd / 1e9}
+    elif args.case.startswith("paged"):
+        out = _paged(args, dev, stream)
     elif args.case == "quant":
         x = (synth.student_t3 if args.kind == "topk" else synth.gaussian_outlier_activations)(M, K, 11, device=dev)
         codes = torch.empty(M, K, dtype=torch.int8, device=dev)
