@@ -9,11 +9,13 @@ is `passes_per_step` such passes, chosen so that the timed region lasts at
 least a second whatever --steps says (the GPU then runs at the clock its power
 cap leaves, not at a cold burst).  The headline value is dense-equivalent TOPS
 (2*M*N*K summed over the seven projections, divided by the time of a pass,
-quantisers included).  The same JSON line also carries the roofline of every
-rated kernel, the end-to-end figure with host buffers, the CPU oracle timed on
-a bounded sample, and one leg per remaining benchmark configuration: the decode
-chains of the 7B and 3B shapes at 1/8/32/64 tokens, the 700M-shape prefill, the
-M = 1..16384 sweep of the isolated BitLinear, and block tokens/s.
+quantisers included).  The JSON line on stdout also carries the roofline of the
+dominant kernel, the end-to-end figure with host buffers, the CPU oracle timed on
+a bounded sample, the 7B decode chain and block tokens/s.  It stays short, for
+readers that keep only the end of the output; a JSON line on stderr holds what is
+longer: the roofline of every rated kernel and the other legs, one per remaining
+benchmark configuration (the 3B decode chain, the 700M-shape prefill, the
+M = 1..16384 sweep of the isolated BitLinear, ...).
 
     python bench.py [--gpus N] [--steps K] [--warmup W] [--impl ours|reference] [--legs a,b,...]
 
@@ -235,6 +237,17 @@ def run_reference(args):
         "e2e": {"value": tops, "unit": "TOPS", "h2d_bytes_per_step": 0, "d2h_bytes_per_step": 0},
     }
     print(json.dumps(line))
+
+
+LONG_KEYS = ("rooflines", "decode_3b", "prefill_700m", "sweep", "attention", "ffn_gate_first", "formats")
+
+
+def print_line(line):
+    """The result as one JSON line on stdout, its long parts (LONG_KEYS) as another on stderr ahead of it."""
+    rest = {k: line[k] for k in LONG_KEYS if line.get(k) is not None}
+    if rest:
+        print(json.dumps({"metric": line["metric"], "legs": rest}), file=sys.stderr, flush=True)
+    print(json.dumps({k: v for k, v in line.items() if k not in LONG_KEYS}), flush=True)
 
 
 # --------------------------------------------------------------------------- replicas (N > 1)
@@ -521,7 +534,7 @@ def run_ours(args):
             "cpu_baseline": cpu_baseline, "decode": decode, "decode_3b": decode3b, "prefill_700m": prefill700m,
             "sweep": sweep, "block": block, "attention": attention, "ffn_gate_first": gate_first, "formats": formats,
         }
-        print(json.dumps(line))
+        print_line(line)
     reps.close()
 
 
