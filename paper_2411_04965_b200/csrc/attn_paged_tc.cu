@@ -862,8 +862,11 @@ __global__ void __launch_bounds__(THREADS, 1) attn_paged_tc_kernel(const __grid_
 #pragma unroll
                                 for (int i = 0; i < 16; ++i) {
                                     uint32_t& w = acc[0][i >> 3][i & 7];
-                                    const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&w), __float2half2_rn(corr[(i >> 3) * 2 + ((i >> 1) & 1)]));
-                                    w = *reinterpret_cast<const uint32_t*>(&x);
+                                    // (in fp32: the factor may be below fp16's numbers where a weight of up to 2^15 times it is not)
+                                    const float by = corr[(i >> 3) * 2 + ((i >> 1) & 1)];
+                                    const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&w));
+                                    const __half2 y = __floats2half2_rn(x.x * by, x.y * by);
+                                    w = *reinterpret_cast<const uint32_t*>(&y);
                                 }
                                 tmem_st_16x16(s_at + 16 * c, acc[0][0]);
                                 tmem_st_16x16(s_at + (16u << 16) + 16 * c, acc[0][1]);

@@ -986,3 +986,30 @@ def test_beside_the_attention_of_a_contiguous_cache(a48, cuda_dev, bits, hd, hea
     # the other call: 4e-8 |score| relative to the row's largest output, and a rounding of the read value
     other = (4e-8 * top[..., None] + 4 * HALF_F32) * np.abs(out).max(-1, keepdims=True) + 2 * HALF_F32 * (1 + 2 * top[..., None]) * mag
     assert (np.abs(got - want) <= attention_bound(out, mag, top, hd, vmax) + weight_tail(n, vmax) + other).all()
+
+
+@pytest.mark.parametrize("bits", [8, 4, 3])
+@pytest.mark.parametrize("step", [20.0, 24.6, 30.0])
+def test_weights_ahead_of_a_far_larger_score(a48, cuda_dev, bits, step):
+    """Scores in octaves: 9.5 in the first tile of 128 positions, 14.9 in the first half of the second (their weights do not move
+    the reference), 9.5 + `step` behind them.  The last one's value has one entry only, so that the others show in the rest of the
+    row: they weigh 2^-9 to 2^-19 of it, which fp16 holds next to it."""
+    hd, q_len, n = 64, 128, 384
+    s = Setup(a48, cuda_dev, bits, 1, hd, 32, [q_len], [n], seed=30)
+    direction = np.where(np.arange(hd) % 2, 1.0, -1.0)
+    size, v = np.zeros(n), np.zeros((n, hd))
+    size[40], size[128:192], size[200] = 9.5, 14.9, 9.5 + step
+    v[40, 0], v[128:192, 1:], v[200, 0] = 1.0, 1.0, 1.0  # (the value scales' unit stays that of the first tile)
+    kt, vt = (torch.tensor(x, dtype=torch.float32) for x in (size[:, None] * direction, v))
+    a48.paged_write(s.cache, s.view(np.array([0, n], np.int32), [n], n), kt.to(cuda_dev), vt.to(cuda_dev),
+                    rope_base=0.0)
+    s.oracle.write([0, n], [n], s.table, kt.double().numpy(), vt.double().numpy(), 0.0, EPS32)
+    q = torch.tensor(np.tile(direction, (q_len, 2)), dtype=torch.float32).to(torch.bfloat16)
+    scale = float(np.float32(np.log(2.0) / hd))
+    got = a48.attention_paged(s.cache, s.batch, q.to(cuda_dev), scale=scale).double().cpu().numpy().reshape(q_len, 2, hd)
+    out, mag, top = s.oracle.attend(s.q_start, s.kv_len, s.table, q.double().numpy(), 2, scale)
+    vmax = np.abs(s.oracle.scales[1]).max() * 2 ** (bits - 1)  # (codes of these bits)
+    bound = attention_bound(out, mag, top, hd, vmax) + weight_tail(n, vmax)
+    if step < 30:
+        assert (np.abs(out[..., 1:]) > 4 * bound[..., 1:]).all()  # (they would be missed)
+    assert (np.abs(got - out) <= bound).all()
