@@ -1013,3 +1013,23 @@ def test_weights_ahead_of_a_far_larger_score(a48, cuda_dev, bits, step):
     if step < 30:
         assert (np.abs(out[..., 1:]) > 4 * bound[..., 1:]).all()  # (they would be missed)
     assert (np.abs(got - out) <= bound).all()
+
+
+@pytest.mark.parametrize("q_len", [1, 3, 260])
+def test_a_nan_in_one_of_many_parts(a48, cuda_dev, q_len):
+    """One sequence whose positions are split into more parts than a cluster joins: a value or key that is no number in one part
+    reaches the rows that see it through the join."""
+    rng = np.random.default_rng(43)
+    hd, kvh, heads, n = 64, 1, 2, 6000
+    s = Setup(a48, cuda_dev, 4, kvh, hd, 64, [q_len], [n], seed=31)
+    assert a48.attention_paged_workspace_bytes(s.cache, s.batch, heads) > 0
+    k, v = (torch.tensor(rng.standard_normal((n, hd)), dtype=torch.float32) for _ in range(2))
+    every = s.view(np.array([0, n], np.int32), [n], n)
+    q = torch.tensor(rng.standard_normal((q_len, heads * hd)), dtype=torch.float32).to(torch.bfloat16).to(cuda_dev)
+    for which, pos in ((0, 2), (1, 3000), (0, n - 1), (1, n - 1)):
+        x = [k.clone(), v.clone()]
+        x[which][pos, 7] = float("nan")
+        a48.paged_write(s.cache, every, x[0].to(cuda_dev), x[1].to(cuda_dev))
+        got = torch.isnan(a48.attention_paged(s.cache, s.batch, q))
+        first = max(0, pos - (n - q_len))  # the first new token that sees the position
+        assert not got[:first].any() and got[first:].all()
