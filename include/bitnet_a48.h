@@ -414,6 +414,58 @@ bitnet_a48_status bitnet_a48_ffn_dense(const bitnet_a48_weight* gate, const bitn
 size_t bitnet_a48_ffn_gate_first_workspace_bytes(const bitnet_a48_weight* gate, const bitnet_a48_weight* up,
                                                  const bitnet_a48_weight* down, int M);
 
+/* ---------------------------------------------------------------------------
+ * The output head in 8 bits, and what is read off its logits.  The paper keeps the head out of the ternary layers; here its
+ * matrix (or any other that stays in higher precision) is e4m3 with a scale for each block.
+ *
+ * Codes are e4m3, one byte each; an entry stands for scale * code.  With a = max|v| over a block of numbers v,
+ *   code = the e4m3 number nearest to 448 v / a (ties to even, in exact arithmetic),   scale = a / 448.
+ * A block of a token row [M, K] is 128 channels of one token; scales fp32 [ceil(K/128)][M]: those of all tokens for one block of
+ * channels side by side.  A block of a weight [N, K] is 128 x 128 entries; scales fp32 [ceil(N/128)][ceil(K/128)].  The last
+ * blocks may be smaller.  A block of zeros has scale 0; one with an entry that is no finite number has codes 0 and NaN for a scale.
+ *
+ * K: a multiple of 16, at most 2^20; N and V at most 2^20.  Codes, scales, gains and the inputs of the quantisers are
+ * 16-byte aligned, and a quantiser's input rows a multiple of 16 bytes apart; logits and outputs have the alignment of their
+ * elements.  Strides are elements from one row to the next and do not count where there is one row.  All calls are
+ * asynchronous on `stream`, allocate nothing and can be captured; calls that may overlap must not share a workspace.
+ */
+
+/* Token rows X_dev [M, K] (fp32, or bf16 with x_bf16 != 0) to codes_dev [M, K] and scale_dev.  gain_dev: NULL, or fp32 [K]:
+ * the rows go through RMSNorm first, v = x * gain, and the scales are a / 448 / sqrt(mean(x^2) + norm_eps).  (Products
+ * x * gain past the range of fp32 count as infinite.) */
+bitnet_a48_status bitnet_a48_quant_fp8(const void* X_dev, long long x_stride, int x_bf16, int M, int K, const float* gain_dev,
+                                       float norm_eps, uint8_t* codes_dev, float* scale_dev, void* stream);
+/* A weight W_dev [N, K] to codes_dev [N, K] and scale_dev. */
+bitnet_a48_status bitnet_a48_quant_fp8_weight(const void* W_dev, long long w_stride, int w_bf16, int N, int K, uint8_t* codes_dev,
+                                              float* scale_dev, void* stream);
+
+/* Y[m, n] = sum over blocks b of scale[b][m] * w_scale[n/128][b] * (sum over k in b of codes[m, k] * w_codes[n, k]), sums
+ * in fp32; Y_dev fp32, or bf16 (round to nearest even) with y_bf16 != 0. */
+bitnet_a48_status bitnet_a48_linear_fp8(const uint8_t* codes_dev, const float* scale_dev, int M, const uint8_t* w_codes_dev,
+                                        const float* w_scale_dev, int N, int K, void* Y_dev, long long y_stride, int y_bf16,
+                                        void* stream);
+
+/* For each of M rows of V logits x (fp32, or bf16 with x_bf16 != 0), with p = softmax(x / temperature):
+ *   logprob[m]   ln p of token t = tokens[m]                        entropy[m]  - sum p ln p
+ *   rank[m]      tokens before t in the order by (logit, lower index first); 0 for the most likely one
+ *   top_ids, top_logprobs [M][top]   the first `top` (at most 64 and V) tokens of that order and their ln p
+ * Each output but the last two may be NULL; top_ids and top_logprobs are not used when top is 0.  tokens_dev: int32, or int64
+ * with tokens_i64 != 0; NULL where neither logprob nor rank is asked for.  A token outside 0 .. V-1 (padding) has logprob 0
+ * and rank -1.  A logit of -inf is a token that cannot be.  A row without a distribution (a NaN, +inf, or nothing but -inf)
+ * gets NaN for logprob, entropy and top_logprobs and -1 for rank and top_ids.  Statistics are fp32; temperature from 1e-30 to 1e30. */
+bitnet_a48_status bitnet_a48_logprobs(const void* logits_dev, long long stride, int x_bf16, int M, int V, float temperature,
+                                      const void* tokens_dev, int tokens_i64, float* logprob_dev, float* entropy_dev,
+                                      int32_t* rank_dev, int top, int32_t* top_ids_dev, float* top_logprobs_dev, void* stream);
+
+/* From hidden states X_dev [M, K] to logprob and entropy as bitnet_a48_logprobs gives them for the logits that
+ * bitnet_a48_quant_fp8 (with this gain) and bitnet_a48_linear_fp8 give, which are never stored: perplexity, likelihoods of
+ * endings.  workspace_dev: bitnet_a48_score_workspace_bytes bytes (0 for sizes that are not supported), no need to clear it. */
+size_t bitnet_a48_score_workspace_bytes(int M, int N, int K);
+bitnet_a48_status bitnet_a48_score(const void* X_dev, long long x_stride, int x_bf16, int M, const float* gain_dev, float norm_eps,
+                                   const uint8_t* w_codes_dev, const float* w_scale_dev, int N, int K, float temperature,
+                                   const void* tokens_dev, int tokens_i64, float* logprob_dev, float* entropy_dev,
+                                   void* workspace_dev, size_t workspace_bytes, void* stream);
+
 /* Reads the device-side status words that kernels with bounded waits set when
  * a wait gives up (0 = no kernel has reported anything) and clears them.
  * Synchronises the device.  words_host receives 4 values: [0] error code,

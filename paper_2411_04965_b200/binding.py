@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 from ctypes import POINTER, byref, c_float, c_int, c_size_t, c_uint, c_void_p
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -39,6 +40,8 @@ EXPORTS = [
     "bitnet_a48_attention_prefill", "bitnet_a48_attention_prefill_workspace_bytes",
     "bitnet_a48_paged_cache_bytes", "bitnet_a48_paged_write", "bitnet_a48_paged_read",
     "bitnet_a48_attention_paged", "bitnet_a48_attention_paged_workspace_bytes",
+    "bitnet_a48_quant_fp8", "bitnet_a48_quant_fp8_weight", "bitnet_a48_linear_fp8", "bitnet_a48_logprobs",
+    "bitnet_a48_score", "bitnet_a48_score_workspace_bytes",
 ]
 
 
@@ -140,6 +143,16 @@ def lib() -> ctypes.CDLL:
         L.bitnet_a48_attention_paged_workspace_bytes.argtypes = [cache_p, batch_p, c_int, c_int, c_int]
         L.bitnet_a48_attention_paged.argtypes = [cache_p, c_void_p, batch_p, c_int, c_void_p, c_ll, c_float, c_int, c_int,
                                                  c_void_p, c_ll, c_void_p, c_size_t, c_void_p]
+        L.bitnet_a48_quant_fp8.argtypes = [c_void_p, c_ll, c_int, c_int, c_int, c_void_p, c_float, c_void_p, c_void_p, c_void_p]
+        L.bitnet_a48_quant_fp8_weight.argtypes = [c_void_p, c_ll, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p]
+        L.bitnet_a48_linear_fp8.argtypes = [c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_int, c_int, c_void_p, c_ll, c_int,
+                                            c_void_p]
+        L.bitnet_a48_logprobs.argtypes = [c_void_p, c_ll, c_int, c_int, c_int, c_float, c_void_p, c_int, c_void_p, c_void_p, c_void_p,
+                                          c_int, c_void_p, c_void_p, c_void_p]
+        L.bitnet_a48_score_workspace_bytes.restype = c_size_t
+        L.bitnet_a48_score_workspace_bytes.argtypes = [c_int, c_int, c_int]
+        L.bitnet_a48_score.argtypes = [c_void_p, c_ll, c_int, c_int, c_void_p, c_float, c_void_p, c_void_p, c_int, c_int, c_float,
+                                       c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
         _lib = L
     return _lib
 
@@ -597,6 +610,149 @@ def attention_paged(cache: PagedCache, batch: PagedBatch, q: torch.Tensor, scale
     _check(_lib.bitnet_a48_attention_paged(cache.cfg_ref, cache.pool_ptr, batch.view_ref, heads, q.data_ptr(), qs, scale, window, sinks,
                                            out.data_ptr(), os_, wp, given, st), "attention_paged")
     return out
+
+
+def _float_rows(t: torch.Tensor):
+    """(stride of the rows of a matrix with contiguous columns, whether it is bf16 and not fp32)."""
+    bf16 = t.dtype == torch.bfloat16
+    assert (bf16 or t.dtype == torch.float32) and t.dim() == 2
+    stride, one = t.stride()
+    assert one == 1 or t.shape[1] == 1
+    return stride, bf16
+
+
+def _fp8(codes: torch.Tensor, scale: torch.Tensor, device: int):
+    """Pointers of e4m3 codes [rows, K] and their scales."""
+    assert codes.dtype == torch.float8_e4m3fn and scale.dtype == torch.float32 and codes.dim() == 2
+    assert codes.is_contiguous() and scale.is_contiguous() and codes.get_device() == device and scale.get_device() == device
+    return codes.data_ptr(), scale.data_ptr()
+
+
+def _gain(gain, K: int, device: int):
+    if gain is None:
+        return None
+    assert gain.dtype == torch.float32 and gain.shape == (K,) and gain.is_contiguous() and gain.get_device() == device
+    return gain.data_ptr()
+
+
+def _tokens(tokens: torch.Tensor, M: int, device: int):
+    """(pointer, whether they are int64 and not int32) of one token for each row."""
+    i64 = tokens.dtype == torch.int64
+    assert (i64 or tokens.dtype == torch.int32) and tokens.shape == (M,) and tokens.is_contiguous() and tokens.get_device() == device
+    return tokens.data_ptr(), i64
+
+
+def quant_fp8(X: torch.Tensor, gain=None, norm_eps: float = 1e-5, codes=None, scale=None, stream=None):
+    """e4m3 codes [M, K] and scales fp32 [ceil(K/128), M] of token rows (fp32 or bf16, rows may be strided), which go through
+    RMSNorm first where a gain (fp32 [K]) is given."""
+    st = _on_stream(X, stream)
+    if st is None:
+        with _made_current(X, stream):
+            return quant_fp8(X, gain, norm_eps, codes, scale)
+    (M, K), (stride, bf16), dev = X.shape, _float_rows(X), X.get_device()
+    if codes is None:
+        codes = torch.empty(M, K, dtype=torch.float8_e4m3fn, device=X.device)
+    if scale is None:
+        scale = torch.empty((K + 127) // 128, M, dtype=torch.float32, device=X.device)
+    assert codes.shape == (M, K) and scale.shape == ((K + 127) // 128, M)
+    cp, sp = _fp8(codes, scale, dev)
+    _check(lib().bitnet_a48_quant_fp8(X.data_ptr(), stride, bf16, M, K, _gain(gain, K, dev), norm_eps, cp, sp, st), "quant_fp8")
+    return codes, scale
+
+
+def quant_fp8_weight(W: torch.Tensor, codes=None, scale=None, stream=None):
+    """e4m3 codes [N, K] and scales fp32 [ceil(N/128), ceil(K/128)] of a weight (fp32 or bf16, rows may be strided)."""
+    st = _on_stream(W, stream)
+    if st is None:
+        with _made_current(W, stream):
+            return quant_fp8_weight(W, codes, scale)
+    (N, K), (stride, bf16) = W.shape, _float_rows(W)
+    blocks = ((N + 127) // 128, (K + 127) // 128)
+    if codes is None:
+        codes = torch.empty(N, K, dtype=torch.float8_e4m3fn, device=W.device)
+    if scale is None:
+        scale = torch.empty(blocks, dtype=torch.float32, device=W.device)
+    assert codes.shape == (N, K) and scale.shape == blocks
+    cp, sp = _fp8(codes, scale, W.get_device())
+    _check(lib().bitnet_a48_quant_fp8_weight(W.data_ptr(), stride, bf16, N, K, cp, sp, st), "quant_fp8_weight")
+    return codes, scale
+
+
+def linear_fp8(codes: torch.Tensor, scale: torch.Tensor, w_codes: torch.Tensor, w_scale: torch.Tensor, dtype=torch.float32, Y=None, stream=None):
+    """Product of token rows and a weight, both as the quantisers give them.  Y [M, N] fp32 or bf16; given, its rows may be strided."""
+    st = _on_stream(codes, stream)
+    if st is None:
+        with _made_current(codes, stream):
+            return linear_fp8(codes, scale, w_codes, w_scale, dtype, Y)
+    dev = codes.get_device()
+    (xp, sp), (wp, wsp) = _fp8(codes, scale, dev), _fp8(w_codes, w_scale, dev)
+    (M, K), N = codes.shape, w_codes.shape[0]
+    assert w_codes.shape[1] == K and scale.shape == ((K + 127) // 128, M) and w_scale.shape == ((N + 127) // 128, (K + 127) // 128)
+    if Y is None:
+        Y = torch.empty(M, N, dtype=dtype, device=codes.device)
+    assert Y.shape == (M, N) and Y.get_device() == dev
+    stride, bf16 = _float_rows(Y)
+    _check(lib().bitnet_a48_linear_fp8(xp, sp, M, wp, wsp, N, K, Y.data_ptr(), stride, bf16, st), "linear_fp8")
+    return Y
+
+
+class Logprobs(NamedTuple):
+    """What ``logprobs`` gives; None for what was not asked for."""
+
+    logprob: Optional[torch.Tensor]       # fp32 [M]
+    entropy: torch.Tensor                 # fp32 [M]
+    rank: Optional[torch.Tensor]          # int32 [M]
+    top_ids: Optional[torch.Tensor]       # int32 [M, top]
+    top_logprobs: Optional[torch.Tensor]  # fp32 [M, top]
+
+
+def logprobs(logits: torch.Tensor, tokens=None, top: int = 0, temperature: float = 1.0, stream=None) -> Logprobs:
+    """Log probability and rank of the given tokens (int32 or int64 [M]; -1: none), entropy, and the ``top`` most likely tokens of
+    each row of logits [M, V] (fp32 or bf16, rows may be strided)."""
+    st = _on_stream(logits, stream)
+    if st is None:
+        with _made_current(logits, stream):
+            return logprobs(logits, tokens, top, temperature)
+    (M, V), (stride, bf16), device = logits.shape, _float_rows(logits), logits.device
+    entropy = torch.empty(M, dtype=torch.float32, device=device)
+    logprob = rank = ids = best = lp = rp = ip = bp = tp = None
+    i64 = False
+    if tokens is not None:
+        tp, i64 = _tokens(tokens, M, logits.get_device())
+        logprob, rank = torch.empty(M, dtype=torch.float32, device=device), torch.empty(M, dtype=torch.int32, device=device)
+        lp, rp = logprob.data_ptr(), rank.data_ptr()
+    if top > 0:
+        ids, best = torch.empty(M, top, dtype=torch.int32, device=device), torch.empty(M, top, dtype=torch.float32, device=device)
+        ip, bp = ids.data_ptr(), best.data_ptr()
+    _check(lib().bitnet_a48_logprobs(logits.data_ptr(), stride, bf16, M, V, temperature, tp, i64, lp, entropy.data_ptr(), rp, top, ip, bp, st),
+           "logprobs")
+    return Logprobs(logprob, entropy, rank, ids, best)
+
+
+def score_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(lib().bitnet_a48_score_workspace_bytes(M, N, K))
+
+
+def score(X: torch.Tensor, gain, w_codes: torch.Tensor, w_scale: torch.Tensor, tokens: torch.Tensor, norm_eps: float = 1e-5,
+          temperature: float = 1.0, workspace=None, stream=None):
+    """(log probability of the given tokens, entropy), fp32 [M] each, of the logits that hidden states X [M, K] have after RMSNorm (or
+    none: gain None) and the 8-bit head; no logits are stored."""
+    st = _on_stream(X, stream)
+    if st is None:
+        with _made_current(X, stream):
+            return score(X, gain, w_codes, w_scale, tokens, norm_eps, temperature, workspace)
+    (M, K), (stride, bf16), dev, N = X.shape, _float_rows(X), X.get_device(), w_codes.shape[0]
+    wp, sp = _fp8(w_codes, w_scale, dev)
+    assert w_codes.shape[1] == K and w_scale.shape == ((N + 127) // 128, (K + 127) // 128)
+    tp, i64 = _tokens(tokens, M, dev)
+    if workspace is None:
+        workspace = torch.empty(max(16, lib().bitnet_a48_score_workspace_bytes(M, N, K)), dtype=torch.uint8, device=X.device)
+    assert workspace.get_device() == dev and workspace.is_contiguous()
+    logprob, entropy = (torch.empty(M, dtype=torch.float32, device=X.device) for _ in range(2))
+    _check(lib().bitnet_a48_score(X.data_ptr(), stride, bf16, M, _gain(gain, K, dev), norm_eps, wp, sp, N, K, temperature, tp, i64,
+                                  logprob.data_ptr(), entropy.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(), st),
+           "score")
+    return logprob, entropy
 
 
 def kernel_status():

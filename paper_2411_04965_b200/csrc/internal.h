@@ -202,6 +202,9 @@ bitnet_a48_status a48_read_attn_status(unsigned int words_host[4]);
 // ---- attn_paged_tc.cu
 bitnet_a48_status a48_read_attn_paged_status(unsigned int words_host[4]);
 
+// ---- gemm_fp8.cu
+bitnet_a48_status a48_read_gemm_fp8_status(unsigned int words_host[4]);
+
 // ---- block.cu
 size_t a48_block_workspace_bytes(const bitnet_a48_block* blk, int B, int T);
 bitnet_a48_status a48_block_forward(const bitnet_a48_block* blk, const float* X, int B, int T, int pos0,

@@ -1,0 +1,429 @@
+// What is read off rows of logits x: with d = (x - max) / T, the log probability d_t - ln sum e^d of a given token t, its
+// place in the order of all tokens, the entropy ln sum e^d - sum e^d d / sum e^d, and the k most likely tokens.
+//
+// One pass.  A thread's sums are taken against a reference of its own (the largest logit it saw at first, moved where a
+// later one is far above it) and joined at the end, in base 2: 2^((x - r) c), c = log2 e / T.
+//
+// The largest k.  The first segments that a block of threads visits are kept in registers; the k-th largest of the threads'
+// maxima over them bounds the row's k-th largest logit from below, and everything at or above that bound, in these segments
+// and in the rest of the row, is noted in a list (about 4 k entries of a row of 32000).  The list is then ranked by (logit,
+// lower index first).  Segments are visited in an order that leaps over the row, so that a row that rises or falls with the
+// index does not fool the bound.  Where many logits equal the bound (masked tokens, coarse types) only what lies above it is
+// noted and equal ones are taken from the front of the row; where the list still overflows, the k-th largest is found digit
+// by digit over the whole row.  All of this costs time only: the answer is exact in every case.
+#include "fp8.cuh"
+#include "softmax_sums.cuh"
+
+namespace {
+
+using a48f8::Sums;
+
+constexpr int THREADS = 256, WARPS = THREADS / 32;
+constexpr int SAMPLE = 8;   // segments (16 bytes to a thread) kept in registers
+constexpr int CAP = 2048;   // entries of the list
+using a48f8::LN2;
+
+struct Args {
+    const void* x;
+    const void* tokens;
+    float* logprob;
+    float* entropy;
+    int32_t* rank;
+    int32_t* top_ids;
+    float* top_logprobs;
+    long long stride;
+    int V, top, tokens64;
+    int segments, leap, leap_fewer;  // most segments of a row; how far apart those visited one after the other are, for so many and one fewer
+    float c;  // log2 e / temperature
+};
+
+// Unsigned numbers in the order of the floats; -0 counts as 0.
+__device__ __forceinline__ uint32_t order_of(float x) {
+    const uint32_t b = __float_as_uint(x + 0.f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float of_order(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
+__device__ __forceinline__ unsigned long long entry_of(float x, int id) { return (unsigned long long)order_of(x) << 32 | (uint32_t)~id; }
+
+template <bool BF16>
+struct Row {
+    static constexpr int E = BF16 ? 8 : 4;  // logits in 16 bytes
+    const void* p;
+    __device__ __forceinline__ float at(int i) const {
+        return BF16 ? __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(p) + i) << 16) : __ldg(reinterpret_cast<const float*>(p) + i);
+    }
+    __device__ __forceinline__ uint4 load(int head, int vec) const {
+        return __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) + (size_t)head * (BF16 ? 2 : 4)) + vec);
+    }
+    static __device__ __forceinline__ void widen(const uint4& u, float (&v)[E]) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        if (BF16) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[(2 * i + 1) % E] = __uint_as_float(w[i] & 0xffff0000u);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
+        }
+    }
+};
+
+template <bool BF16>
+struct Walk {
+    Row<BF16> row;
+    Sums sums;
+    float c, own, least;  // least: logits at or above it go to the list
+    int token, ahead;     // ahead: logits that come before the token's in the order
+    unsigned long long* list;
+    uint32_t* count;
+
+    __device__ __forceinline__ void note(float x, int id) {
+        const uint32_t at = atomicAdd(count, 1u);
+        if (at < (uint32_t)CAP) list[at] = entry_of(x, id);
+    }
+    template <int N>
+    __device__ __forceinline__ void rank(const float (&v)[N], int id) {
+        if (id <= token && token < id + N) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) ahead += id + j < token ? v[j] >= own : v[j] > own;
+        } else if (id < token) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) ahead += v[j] >= own;
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) ahead += v[j] > own;
+        }
+    }
+    template <int N>
+    __device__ __forceinline__ void take(const float (&v)[N], int id, bool top) {
+        float m = v[0];
+#pragma unroll
+        for (int j = 1; j < N; ++j) m = fmaxf(m, v[j]);
+        if ((m - sums.r) * c > 60.f) sums.move(m, c);
+#pragma unroll
+        for (int j = 0; j < N; ++j) sums.add(v[j], c);
+        rank(v, id);
+        if (top && m >= least) {
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+                if (v[j] >= least) note(v[j], id + j);
+        }
+    }
+};
+
+// Where all threads of the block agree: inclusive sums over the block of a 0/1 flag.
+__device__ __forceinline__ int flags_before(bool flag, uint32_t* warp_counts, int& total) {
+    const uint32_t votes = __ballot_sync(0xffffffffu, flag);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (lane == 0) warp_counts[warp] = __popc(votes);
+    __syncthreads();
+    int before = 0;
+    total = 0;
+    for (int w = 0; w < WARPS; ++w) {
+        before += w < warp ? warp_counts[w] : 0;
+        total += warp_counts[w];
+    }
+    __syncthreads();
+    return before + __popc(votes & ((1u << lane) - 1));
+}
+
+template <bool BF16>
+__global__ void __launch_bounds__(THREADS) logprobs_kernel(const Args a) {
+    constexpr int E = Row<BF16>::E;
+    __shared__ unsigned long long list[CAP];
+    __shared__ float best[THREADS];
+    __shared__ float4 part[WARPS];
+    __shared__ uint32_t hist[256], counts[WARPS];
+    __shared__ uint32_t count, found[2];
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    const long long r = blockIdx.x;
+    Walk<BF16> w;
+    w.row.p = reinterpret_cast<const char*>(a.x) + (size_t)(r * a.stride) * (BF16 ? 2 : 4);
+    w.c = a.c;
+    w.list = list;
+    w.count = &count;
+    w.ahead = 0;
+    w.token = -1;
+    w.own = __uint_as_float(0x7fc00000u);  // nothing is above no number
+    if (a.tokens) {
+        const long long token = a.tokens64 ? __ldg(reinterpret_cast<const long long*>(a.tokens) + r) : __ldg(reinterpret_cast<const int*>(a.tokens) + r);
+        if (token >= 0 && token < a.V) {
+            w.token = (int)token;
+            w.own = w.row.at(w.token);
+        }
+    }
+    const bool top = a.top > 0;
+    // whole 16 bytes between the first and last few logits, which threads 0 .. E - 1 and E .. 2 E - 1 take one by one
+    const int skew = (int)(reinterpret_cast<uintptr_t>(w.row.p) & 15u) / (BF16 ? 2 : 4), head = min(a.V, skew ? E - skew : 0);
+    const int vecs = (a.V - head) / E, tail = head + vecs * E;
+    const int segments = (vecs + THREADS - 1) / THREADS;
+    const int leap = segments == a.segments ? a.leap : a.leap_fewer;
+    const int edge = t < E ? (t < head ? t : -1) : t < 2 * E && tail + t - E < a.V ? tail + t - E : -1;
+    float edge_x[1] = {-INFINITY};
+    if (edge >= 0) edge_x[0] = w.row.at(edge);
+
+    if (t == 0) count = 0;
+    uint4 kept[SAMPLE];
+    float m = edge_x[0];
+    int at = 0;  // segment
+#pragma unroll
+    for (int i = 0; i < SAMPLE; ++i) {
+        const int vec = at * THREADS + t;
+        kept[i] = i < segments && vec < vecs ? w.row.load(head, vec) : BF16 ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u) : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
+        at += leap;
+        at -= at >= segments ? segments : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < SAMPLE; ++i) {
+        float v[E];
+        Row<BF16>::widen(kept[i], v);
+#pragma unroll
+        for (int j = 0; j < E; ++j) m = fmaxf(m, v[j]);
+    }
+    w.sums.start(m);
+    bool strict = false;
+    float bound = -INFINITY;
+    if (top) {
+        best[t] = m;
+        __syncthreads();
+        // the bound, in every warp alike: halving the range of orders that holds the k-th largest of the threads' maxima
+        uint32_t key[WARPS];
+        uint32_t hi = 0;
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) {
+            key[i] = order_of(best[i * 32 + lane]);
+            hi = max(hi, key[i]);
+        }
+        hi = __reduce_max_sync(0xffffffffu, hi);
+        uint32_t lo = order_of(-INFINITY);
+        int reach = THREADS;  // maxima at or above lo, k or more
+        while (lo < hi && reach > a.top + a.top / 4 + 2) {
+            const uint32_t mid = lo + (hi - lo + 1) / 2;
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < WARPS; ++i) n += __popc(__ballot_sync(0xffffffffu, key[i] >= mid));
+            if (n >= a.top) {
+                lo = mid;
+                reach = n;
+            } else {
+                hi = mid - 1;
+            }
+        }
+        bound = of_order(lo);
+        int same = 0;
+#pragma unroll
+        for (int i = 0; i < WARPS; ++i) same += __popc(__ballot_sync(0xffffffffu, key[i] == lo));
+        strict = lo == order_of(-INFINITY) || same > 32;
+        w.least = strict ? of_order(order_of(bound) + 1) : bound;
+    }
+    int seg = 0;
+#pragma unroll
+    for (int i = 0; i < SAMPLE; ++i) {
+        float v[E];
+        Row<BF16>::widen(kept[i], v);
+        const int vec = seg * THREADS + t;
+        if (i < segments && vec < vecs) w.take(v, head + vec * E, top);
+        seg += leap;
+        seg -= seg >= segments ? segments : 0;
+    }
+    if (edge >= 0) w.take(edge_x, edge, top);
+    if (segments > SAMPLE) {
+        for (int i = SAMPLE; i < segments; i += 4) {
+            uint4 u[4];
+            int id[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int vec = at * THREADS + t;
+                id[q] = i + q < segments && vec < vecs ? vec : -1;
+                if (id[q] >= 0) u[q] = w.row.load(head, vec);
+                at += leap;
+                at -= at >= segments ? segments : 0;
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (id[q] < 0) continue;
+                float v[E];
+                Row<BF16>::widen(u[q], v);
+                w.take(v, head + id[q] * E, top);
+            }
+        }
+    }
+    // ---- joined
+    float ref = w.sums.r;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, o));
+    w.sums.move(ref, a.c);
+    float s = w.sums.s, d = w.sums.d;
+    int ahead = w.ahead;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+        s += __shfl_xor_sync(0xffffffffu, s, o);
+        d += __shfl_xor_sync(0xffffffffu, d, o);
+        ahead += __shfl_xor_sync(0xffffffffu, ahead, o);
+    }
+    if (lane == 0) part[warp] = make_float4(ref, s, d, __int_as_float(ahead));
+    __syncthreads();
+    Sums all = {part[0].x, part[0].y, part[0].z};
+    ahead = __float_as_int(part[0].w);
+    for (int i = 1; i < WARPS; ++i) {
+        Sums more = {part[i].x, part[i].y, part[i].z};
+        all.join(more, a.c);
+        ahead += __float_as_int(part[i].w);
+    }
+    const bool valid = all.valid();
+    const float log_s = log2f(all.s), nan = __uint_as_float(0x7fc00000u);
+    if (t == 0) {
+        if (a.logprob) a.logprob[r] = !valid ? nan : w.token < 0 ? 0.f : LN2 * ((w.own - all.r) * a.c - log_s);
+        if (a.entropy) a.entropy[r] = valid ? LN2 * (log_s - all.d / all.s) : nan;
+        if (a.rank) a.rank[r] = valid && w.token >= 0 ? ahead : -1;
+    }
+    if (!top) return;
+    int32_t* ids = a.top_ids + r * a.top;
+    float* logps = a.top_logprobs + r * a.top;
+    if (!valid) {
+        if (t < a.top) {
+            ids[t] = -1;
+            logps[t] = nan;
+        }
+        return;
+    }
+    int n = (int)count;
+    if (n > CAP) {  // the k-th largest of the row, eight bits at a time
+        uint32_t prefix = 0;
+        int need = a.top;
+        for (int shift = 24; shift >= 0; shift -= 8) {
+            hist[t] = 0;
+            __syncthreads();
+            for (int i = t; i < a.V; i += THREADS) {
+                const uint32_t o = order_of(w.row.at(i));
+                if (shift == 24 || o >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&hist[o >> shift & 255u], 1u);
+            }
+            __syncthreads();
+            if (t == 0) {
+                int left = need, bin = 255;
+                while ((int)hist[bin] < left) left -= (int)hist[bin--];
+                found[0] = (uint32_t)bin;
+                found[1] = (uint32_t)left;
+            }
+            __syncthreads();
+            prefix |= found[0] << shift;
+            need = (int)found[1];
+            __syncthreads();
+        }
+        bound = of_order(prefix);
+        strict = true;
+        if (t == 0) count = 0;
+        __syncthreads();
+        for (int i = t; i < a.V; i += THREADS)
+            if (w.row.at(i) > bound) w.note(w.row.at(i), i);
+        __syncthreads();
+        n = (int)count;
+    }
+    if (strict && n < a.top) {  // those that equal the bound, from the front of the row
+        int have = n;
+        for (int i0 = 0; have < a.top && i0 < a.V; i0 += THREADS) {
+            const int i = i0 + t;
+            const bool is = i < a.V && order_of(w.row.at(i)) == order_of(bound);
+            int total;
+            const int before = flags_before(is, counts, total);
+            if (is && have + before < a.top) list[have + before] = entry_of(bound, i);
+            have += total;
+        }
+        n = min(have, a.top);
+        __syncthreads();
+    }
+    for (int i = t; i < n; i += THREADS) {
+        const unsigned long long mine = list[i];
+        int place = 0;
+        for (int j = 0; j < n; ++j) place += list[j] > mine;
+        if (place < a.top) {
+            ids[place] = (int)~(uint32_t)mine;
+            logps[place] = LN2 * ((of_order((uint32_t)(mine >> 32)) - all.r) * a.c - log_s);
+        }
+    }
+}
+
+// A step near 0.618 n that shares no divisor with n, so that n steps visit all of 0 .. n - 1.
+int leap_over(int n) {
+    if (n < 3) return 1;
+    int d = (int)(0.6180339887 * n);
+    for (;; ++d) {
+        int a = n, b = d;
+        while (b) {
+            const int c = a % b;
+            a = b;
+            b = c;
+        }
+        if (a == 1) return d;  // n - 1 at the latest
+    }
+}
+
+// Joins the sums of the parts of a row's logits: eight rows to a block, 32 threads to a row.
+__global__ void __launch_bounds__(256) score_join_kernel(const float4* __restrict__ stats, int parts, int M, int V, const void* tokens,
+                                                         int tokens64, float c, const float* __restrict__ owns, float* __restrict__ logprob,
+                                                         float* __restrict__ entropy) {
+    __shared__ Sums sums[32][8];
+    const int t = threadIdx.x, row = t & 7, lane = t >> 3, m = blockIdx.x * 8 + row;
+    Sums all;
+    all.start(-INFINITY);
+    if (m < M) {
+#pragma unroll 4
+        for (int i = lane; i < parts; i += 32) {
+            const float4 f = __ldg(stats + (size_t)i * M + m);
+            all.join({f.x, f.y, f.z}, c);
+        }
+    }
+    sums[lane][row] = all;
+    __syncthreads();
+    for (int half = 16; half; half >>= 1) {
+        if (lane < half) {
+            all.join(sums[lane + half][row], c);
+            sums[lane][row] = all;
+        }
+        __syncthreads();
+    }
+    if (lane || m >= M) return;
+    const long long token = tokens64 ? reinterpret_cast<const long long*>(tokens)[m] : reinterpret_cast<const int*>(tokens)[m];
+    const float log_s = log2f(all.s), nan = __uint_as_float(0x7fc00000u);
+    const bool taken = token >= 0 && token < V;
+    logprob[m] = !all.valid() ? nan : taken ? LN2 * ((owns[m] - all.r) * c - log_s) : 0.f;
+    entropy[m] = all.valid() ? LN2 * (log_s - all.d / all.s) : nan;
+}
+
+}  // namespace
+
+namespace a48f8 {
+
+bitnet_a48_status launch_score_join(const ScoreArgs& s, const ScoreParts& w, int M, int V, cudaStream_t st) {
+    score_join_kernel<<<(M + 7) / 8, 256, 0, st>>>(w.stats, w.parts, M, V, s.tokens, s.tokens64, s.c, w.owns, s.logprob, s.entropy);
+    A48_CUDA_TRY(cudaGetLastError());
+    return BITNET_A48_OK;
+}
+
+bitnet_a48_status launch_logprobs(const LogprobArgs& g, cudaStream_t st) {
+    Args a = {};
+    a.x = g.x;
+    a.tokens = g.tokens;
+    a.logprob = g.logprob;
+    a.entropy = g.entropy;
+    a.rank = g.rank;
+    a.top_ids = g.top_ids;
+    a.top_logprobs = g.top_logprobs;
+    a.stride = g.stride;
+    a.V = g.V;
+    a.top = g.top;
+    a.tokens64 = g.tokens64;
+    a.c = (float)(1.4426950408889634 / (double)g.temperature);
+    const int vecs = g.V / (g.x_bf16 ? 8 : 4);
+    a.segments = (vecs + THREADS - 1) / THREADS;
+    a.leap = leap_over(a.segments);
+    a.leap_fewer = leap_over(a.segments - 1);
+    if (g.x_bf16) logprobs_kernel<true><<<g.M, THREADS, 0, st>>>(a);
+    else logprobs_kernel<false><<<g.M, THREADS, 0, st>>>(a);
+    A48_CUDA_TRY(cudaGetLastError());
+    return BITNET_A48_OK;
+}
+
+}  // namespace a48f8
