@@ -23,25 +23,35 @@ using a48f8::BLOCK;
 using a48f8::LinearArgs;
 
 constexpr int TMEM_COLS = 512;
+constexpr int CONTROL_WARPS = 4;  // copies, MMAs, and two that only make up a warpgroup
 
 // AR: rows of the token tile that a stage has room for (the MMA reads 128; what lies behind belongs to tokens that do not
-// exist); BN: features of a tile; PAIR: two CTAs share a tile of 256 tokens, each holds half of the weight rows.
-template <int AR_, int BN_, bool PAIR_>
+// exist).  SUBS x SUBN: features of a tile, as so many accumulators of SUBN columns, each with a warpgroup of its own that takes it
+// out of tensor memory.  PAIR: two CTAs share a tile of 256 tokens; each holds half of the weight rows of an accumulator.
+template <int AR_, int SUBS_, int SUBN_, bool PAIR_>
 struct Cfg {
-    static constexpr int AR = AR_, BN = BN_;
+    static constexpr int AR = AR_, SUBS = SUBS_, SUBN = SUBN_, BN = SUBS * SUBN;
     static constexpr bool PAIR = PAIR_;
     static constexpr int CTAS = PAIR ? 2 : 1, TM = 128 * CTAS;
-    static constexpr int BROWS = BN / CTAS;
-    static constexpr int A_BYTES = AR * BLOCK, B_BYTES = BROWS * BLOCK, STAGE_BYTES = A_BYTES + B_BYTES;
+    static constexpr int SUB_ROWS = SUBN / CTAS;  // weight rows of an accumulator that a CTA holds
+    static constexpr int A_BYTES = AR * BLOCK, SUB_BYTES = SUB_ROWS * BLOCK, STAGE_BYTES = A_BYTES + SUBS * SUB_BYTES;
     static constexpr int SLACK = AR < 128 ? (128 - AR) * BLOCK : 0;
-    static constexpr int MAX_STAGES = (220 * 1024 - SLACK) / STAGE_BYTES;
+    static constexpr int OUT_BYTES = 4096, OUT_BUFS = 2;  // 32 rows of 128 bytes on their way out, two to a warp
+    static constexpr int EPI_WARPS = 4 * SUBS, NUM_THREADS = 32 * (CONTROL_WARPS + EPI_WARPS);
+    static constexpr int OUT_ALL = EPI_WARPS * OUT_BUFS * OUT_BYTES;
+    static constexpr int MAX_STAGES = (225 * 1024 - SLACK - OUT_ALL) / STAGE_BYTES;
     static constexpr int STAGES = MAX_STAGES < 16 ? MAX_STAGES : 16;
-    static constexpr int ACC_BUFS = TMEM_COLS / BN < 8 ? TMEM_COLS / BN : 8;
-    static constexpr int EPI_SPLIT = BN >= 64 ? 2 : 1;
-    static constexpr int COLS = BN / EPI_SPLIT;  // of one thread
-    static constexpr int NUM_THREADS = 32 * (2 + 4 * EPI_SPLIT);
-    static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + SLACK + 1024 /*alignment*/ + 512 /*barriers*/;
-    static_assert(COLS % 32 == 0 && COLS <= BLOCK, "a thread's columns share a weight scale");
+    // Blocks of channels that change hands at once between the MMAs and the epilogue, each in columns of its own: what the
+    // hand-over costs (about 300 clocks) is spread over 128 columns whatever the tile.
+    static constexpr int GROUP = BLOCK / SUBN, ACC_COLS = GROUP * SUBN;
+    static constexpr int ACC_BUFS = TMEM_COLS / ACC_COLS;
+    static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + SLACK + OUT_ALL + 1024 /*alignment*/ + 512 /*barriers*/;
+    // With eight epilogue warps 168 registers a thread at launch are all an SM has; the control warps hand theirs over.
+    static constexpr bool MOVE_REGISTERS = SUBS == 2;
+    static constexpr int CONTROL_REGISTERS = 40, EPI_REGISTERS = 232;
+    static_assert(!MOVE_REGISTERS || 128 * CONTROL_REGISTERS + 256 * EPI_REGISTERS <= 384 * 168, "registers of the launch");
+    static_assert(SUBN % 32 == 0 && SUBN <= BLOCK, "the columns of an accumulator share a weight scale");
+    static_assert(ACC_BUFS % SUBS == 0 && STAGE_BYTES % 1024 == 0 && SLACK % 1024 == 0, "layout");
     static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
     static_assert(8 * (2 * STAGES + 2 * ACC_BUFS) <= 480, "barriers");
 };
@@ -51,7 +61,8 @@ struct Params {
     const float* ws;
     void* y;
     long long y_stride;
-    int M, N, kb, m_tiles, tiles, x_rows, y_bf16, y_vec;
+    int M, N, kb, m_tiles, tiles, x_rows, y_bf16;
+    int y_map;           // y is stored by tensor copies
     const void* tokens;  // the rest: products that keep sums of their logits
     int tokens64;
     float c;
@@ -59,14 +70,119 @@ struct Params {
     float* owns;
 };
 
+// Sums of the softmax over a thread's columns (the last ones may not exist), and the logit of its row's token.
+template <int COLS>
+__device__ __forceinline__ Sums sums_of(const f32x2 (&sum)[COLS / 2], int cols, float c2, long long token_at, float* own) {
+    Sums s;
+    float top = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < COLS; c += 2) {
+        float lo, hi;
+        unpack2(sum[c / 2], lo, hi);
+        if (c < cols) top = fmaxf(top, lo);
+        if (c + 1 < cols) top = fmaxf(top, hi);
+    }
+    s.start(top);
+#pragma unroll
+    for (int c = 0; c < COLS; c += 2) {
+        float lo, hi;
+        unpack2(sum[c / 2], lo, hi);
+        if (c < cols) s.add(lo, c2);
+        if (c + 1 < cols) s.add(hi, c2);
+    }
+    if (token_at >= 0 && token_at < cols) {
+#pragma unroll
+        for (int c = 0; c < COLS; c += 2) {
+            float lo, hi;
+            unpack2(sum[c / 2], lo, hi);
+            if (token_at == c) *own = lo;
+            if (token_at == c + 1) *own = hi;
+        }
+    }
+    return s;
+}
+
+// 32 rows x COLS columns of a warp to y: through shared memory, 128 bytes of every row at a time (16-byte pieces of row r
+// exchanged by r % 8, so that neither side has bank conflicts), and from there by tensor stores, or, where y's rows are not
+// 16-byte aligned, a row to an instruction.
+template <int COLS, bool BF16>
+__device__ __forceinline__ void store_rows(const f32x2 (&sum)[COLS / 2], const Params& p, const CUtensorMap* tm_y, uint8_t* out, int m0, int n0, int lane,
+                                           uint32_t& stores) {
+    constexpr int W = BF16 ? 64 : 32;  // columns in 128 bytes
+#pragma unroll
+    for (int c0 = 0; c0 < COLS; c0 += W) {
+        if (n0 + c0 >= p.N) break;
+        uint8_t* buf = out + (stores++ & 1u) * 4096;
+        if (p.y_map) {
+            if (lane == 0) tma_store_wait_read<1>();
+        }
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            uint32_t v[4];
+            if (BF16) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float lo, hi;
+                    unpack2(c0 + 8 * q + 2 * j < COLS ? sum[(c0 + 8 * q + 2 * j) / 2 % (COLS / 2)] : 0ull, lo, hi);
+                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v[j]) : "f"(hi), "f"(lo));
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    float lo, hi;
+                    unpack2(sum[(c0 + 4 * q + 2 * j) / 2], lo, hi);
+                    v[2 * j] = __float_as_uint(lo);
+                    v[2 * j + 1] = __float_as_uint(hi);
+                }
+            }
+            *reinterpret_cast<uint4*>(buf + lane * 128 + ((q ^ (lane & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
+        }
+        if (p.y_map) {
+            fence_async_shared();
+            __syncwarp();
+            if (lane == 0) tma_store_2d(tm_y, n0 + c0, m0, smem_u32(buf));
+        } else {
+            __syncwarp();
+            const int rows = min(32, p.M - m0);
+            for (int r = 0; r < rows; ++r) {
+                if (BF16) {
+                    const __nv_bfloat16* line = reinterpret_cast<const __nv_bfloat16*>(buf + r * 128);
+                    __nv_bfloat16* y = reinterpret_cast<__nv_bfloat16*>(p.y) + (size_t)(m0 + r) * p.y_stride + n0 + c0;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int i = h * 32 + lane;
+                        if (i < COLS - c0 && n0 + c0 + i < p.N) y[i] = line[((i >> 3) ^ (r & 7)) * 8 + (i & 7)];
+                    }
+                } else {
+                    const float* line = reinterpret_cast<const float*>(buf + r * 128);
+                    if (n0 + c0 + lane < p.N)
+                        reinterpret_cast<float*>(p.y)[(size_t)(m0 + r) * p.y_stride + n0 + c0 + lane] = line[((lane >> 2) ^ (r & 7)) * 4 + (lane & 3)];
+                }
+            }
+            __syncwarp();
+        }
+    }
+}
+
+// sum += scale * (lo, hi).  (The packed form of the multiply-add took longer, 797 us for 611 in the 7B head's prompt: what
+// comes from tensor memory is not in the register pairs that it wants.)
+__device__ __forceinline__ void scale_add(f32x2& sum, uint32_t lo, uint32_t hi, float scale) {
+    float a, b;
+    unpack2(sum, a, b);
+    sum = pack2(fmaf(__uint_as_float(lo), scale, a), fmaf(__uint_as_float(hi), scale, b));
+}
+
 template <class C, bool SCORE>
 __global__ void __launch_bounds__(C::NUM_THREADS, 1)
-    gemm_fp8_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const Params p) {
-    constexpr int STAGES = C::STAGES, ACC_BUFS = C::ACC_BUFS, BN = C::BN, COLS = C::COLS;
+    gemm_fp8_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_y,
+                    const Params p) {
+    constexpr int STAGES = C::STAGES, ACC_BUFS = C::ACC_BUFS, SUBS = C::SUBS, SUBN = C::SUBN;
     constexpr bool PAIR = C::PAIR;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint8_t* ctrl = smem + STAGES * C::STAGE_BYTES + C::SLACK;
+    uint8_t* out_all = smem + STAGES * C::STAGE_BYTES + C::SLACK;
+    uint8_t* ctrl = out_all + C::OUT_ALL;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl + 480);
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(ctrl + 484);
     const uint32_t bar_full = smem_u32(ctrl), bar_empty = bar_full + 8 * STAGES;
@@ -85,7 +201,7 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
         }
         for (int b = 0; b < ACC_BUFS; ++b) {
             mbar_init(bar_acc_full + 8 * b, 1);
-            mbar_init(bar_acc_empty + 8 * b, C::CTAS * 4 * C::EPI_SPLIT);  // one arrival per epilogue warp
+            mbar_init(bar_acc_empty + 8 * b, C::CTAS * 4);  // one arrival to a warp of the accumulator's warpgroup
         }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -97,206 +213,168 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
 
-    if (warp == 0) {
-        // ------------------------------------------------------------- tensor copies
-        uint32_t it = 0, s = 0, ph = 0;
-        bool ok = true;
-        const uint32_t full0 = PAIR ? map_to_rank(bar_full, 0) : bar_full;  // the pair's copies all report to rank 0
-        for (int tile = unit; tile < p.tiles && ok; tile += units) {
-            const int nt = tile / p.m_tiles, mt = tile - nt * p.m_tiles;
-            const int m0 = mt * C::TM + rank * 128, n0 = nt * BN + rank * C::BROWS;
-            for (int b = 0; b < p.kb; ++b, ++it) {
-                ok = __all_sync(0xffffffffu, mbar_wait(bar_empty + 8 * s, ph ^ 1, abort_flag, 1, it));
-                if (!ok) break;
-                if (lane == 0) {
-                    const uint32_t dst = smem_base + s * C::STAGE_BYTES;
-                    if (rank == 0) mbar_expect_tx(bar_full + 8 * s, (uint32_t)(C::CTAS * (p.x_rows * BLOCK + C::B_BYTES)));
-                    if (PAIR) {
-                        tma_load_2d_pair(dst, &tm_x, b * BLOCK, m0, full0 + 8 * s);
-                        tma_load_2d_pair(dst + C::A_BYTES, &tm_w, b * BLOCK, n0, full0 + 8 * s);
-                    } else {
-                        tma_load_2d(dst + C::A_BYTES, &tm_w, b * BLOCK, n0, full0 + 8 * s);
-                        tma_load_2d(dst, &tm_x, b * BLOCK, m0, full0 + 8 * s);
+    if (warp < CONTROL_WARPS) {
+        if (C::MOVE_REGISTERS) registers_down<C::CONTROL_REGISTERS>();
+        // One thread each for the copies and the MMAs: a wait of a whole warp costs them a vote, and the pipe a gap.
+        if (warp == 0 && elect_one()) {
+            // --------------------------------------------------------- tensor copies
+            uint32_t it = 0, s = 0, ph = 0;
+            bool ok = true;
+            const uint32_t full0 = PAIR ? map_to_rank(bar_full, 0) : bar_full;  // the pair's copies all report to rank 0
+            for (int tile = unit; tile < p.tiles && ok; tile += units) {
+                const int nt = tile / p.m_tiles, mt = tile - nt * p.m_tiles;
+                const int m0 = mt * C::TM + rank * 128, n0 = nt * C::BN + rank * C::SUB_ROWS;
+                for (int b = 0; b < p.kb; ++b, ++it) {
+                    ok = mbar_wait(bar_empty + 8 * s, ph ^ 1, abort_flag, 1, it);
+                    if (!ok) break;
+                    const uint32_t dst = smem_base + s * C::STAGE_BYTES, bar = full0 + 8 * s;
+                    if (rank == 0) mbar_expect_tx(bar_full + 8 * s, (uint32_t)(C::CTAS * (p.x_rows * BLOCK + SUBS * C::SUB_BYTES)));
+#pragma unroll
+                    for (int i = 0; i < SUBS; ++i) {
+                        if (PAIR) tma_load_2d_pair(dst + C::A_BYTES + i * C::SUB_BYTES, &tm_w, b * BLOCK, n0 + i * SUBN, bar);
+                        else tma_load_2d(dst + C::A_BYTES + i * C::SUB_BYTES, &tm_w, b * BLOCK, n0 + i * SUBN, bar);
                     }
-                }
-                __syncwarp();
-                if (++s == (uint32_t)STAGES) { s = 0; ph ^= 1; }
-            }
-        }
-        if (!ok && lane == 0) {  // let the copies already issued land before the CTA exits
-            const unsigned long long t0 = clock64();
-            if (rank == 0) {
-                for (uint32_t back = 1; back <= (uint32_t)STAGES && back <= it; ++back) {
-                    const uint32_t j = it - back, sj = j % STAGES, pj = (j / STAGES) & 1;
-                    while (!mbar_try(bar_full + 8 * sj, pj) && clock64() - t0 < kWaitClocks) {
-                    }
-                }
-            } else {
-                while (clock64() - t0 < 4000000ull) {
+                    if (PAIR) tma_load_2d_pair(dst, &tm_x, b * BLOCK, m0, bar);
+                    else tma_load_2d(dst, &tm_x, b * BLOCK, m0, bar);
+                    if (++s == (uint32_t)STAGES) { s = 0; ph ^= 1; }
                 }
             }
-        }
-    } else if (warp == 1) {
-        // ------------------------------------------------------------- MMAs (of a pair: rank 0 for both)
-        if (rank == 0) {
-            constexpr uint32_t idesc = idesc_e4m3(C::TM, BN);
-            const bool leader = elect_one();
+            if (!ok) {  // let the copies already issued land before the CTA exits
+                const unsigned long long t0 = clock64();
+                if (rank == 0) {
+                    for (uint32_t back = 1; back <= (uint32_t)STAGES && back <= it; ++back) {
+                        const uint32_t j = it - back, sj = j % STAGES, pj = (j / STAGES) & 1;
+                        while (!mbar_try(bar_full + 8 * sj, pj) && clock64() - t0 < kWaitClocks) {
+                        }
+                    }
+                } else {
+                    while (clock64() - t0 < 4000000ull) {
+                    }
+                }
+            }
+        } else if (warp == 1 && rank == 0 && elect_one()) {
+            // --------------------------------------------------------- MMAs (of a pair: rank 0 for both)
+            constexpr uint32_t idesc = idesc_e4m3(C::TM, SUBN);
             uint32_t it = 0, s = 0, ph = 0, a = 0, pa = 0;
             bool ok = true;
             for (int tile = unit; tile < p.tiles && ok; tile += units) {
-                for (int b = 0; b < p.kb; ++b, ++it) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(bar_acc_empty + 8 * a, pa ^ 1, abort_flag, 2, it));
+                for (int b = 0; b < p.kb && ok; ++b, ++it) {
+                    const int g = b % C::GROUP;
+                    const bool last = g == C::GROUP - 1 || b == p.kb - 1;
+                    ok = mbar_wait(bar_full + 8 * s, ph, abort_flag, 3, it);
                     if (!ok) break;
-                    ok = __all_sync(0xffffffffu, mbar_wait(bar_full + 8 * s, ph, abort_flag, 3, it));
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (leader) {
-                        const uint64_t a_desc = smem_desc_sw128(smem_base + s * C::STAGE_BYTES);
-                        const uint64_t b_desc = smem_desc_sw128(smem_base + s * C::STAGE_BYTES + C::A_BYTES);
+                    const uint64_t a_desc = smem_desc_sw128(smem_base + s * C::STAGE_BYTES);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) mma_f8<PAIR>(tmem_base + a * BN, a_desc + 2 * j, b_desc + 2 * j, idesc, j > 0);
-                        tc_commit<PAIR>(bar_empty + 8 * s);
-                        tc_commit<PAIR>(bar_acc_full + 8 * a);
+                    for (int i = 0; i < SUBS; ++i) {
+                        if (g == 0) ok = mbar_wait(bar_acc_empty + 8 * (a + i), pa ^ 1, abort_flag, 2, it);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint64_t b_desc = a_desc + ((C::A_BYTES + i * C::SUB_BYTES) >> 4);
+                        const uint32_t to = tmem_base + (a + i) * C::ACC_COLS + g * SUBN;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) mma_f8<PAIR>(to, a_desc + 2 * j, b_desc + 2 * j, idesc, j > 0);
+                        if (last) tc_commit<PAIR>(bar_acc_full + 8 * (a + i));
+                        if (i == SUBS - 1) tc_commit<PAIR>(bar_empty + 8 * s);
                     }
-                    __syncwarp();
                     if (++s == (uint32_t)STAGES) { s = 0; ph ^= 1; }
-                    if (++a == (uint32_t)ACC_BUFS) { a = 0; pa ^= 1; }
+                    if (last && (a += SUBS) == (uint32_t)ACC_BUFS) { a = 0; pa ^= 1; }
                 }
             }
         }
+        __syncwarp();
     } else {
         // ------------------------------------------------------------- scales, sums, stores
-        const int quad = warp & 3, col0 = ((warp - 2) >> 2) * COLS;
-        const uint32_t t_lanes = tmem_base + ((uint32_t)(quad * 32) << 16) + col0;
+        if (C::MOVE_REGISTERS) registers_up<C::EPI_REGISTERS>();
+        const int quad = warp & 3, sub = (warp - CONTROL_WARPS) >> 2;
+        const uint32_t t_lanes = tmem_base + ((uint32_t)(quad * 32) << 16);
         const uint32_t acc_empty0 = PAIR ? map_to_rank(bar_acc_empty, 0) : bar_acc_empty;
-        uint32_t it = 0, a = 0, pa = 0;
+        uint8_t* out = out_all + (warp - CONTROL_WARPS) * C::OUT_BUFS * C::OUT_BYTES;
+        uint32_t it = 0, a = sub, pa = 0, stores = 0;
         bool ok = true;
-        Sums run;  // SCORE with one tile of tokens: over all tiles of this CTA
+        Sums run;  // SCORE, a single CTA with one tile of tokens: over all tiles of this CTA
         run.start(-INFINITY);
         for (int tile = unit; tile < p.tiles && ok; tile += units) {
             const int nt = tile / p.m_tiles, mt = tile - nt * p.m_tiles;
-            const int m0 = mt * C::TM + rank * 128 + quad * 32, m = m0 + lane, n0 = nt * BN + col0;
+            const int m0 = mt * C::TM + rank * 128 + quad * 32, m = m0 + lane, n0 = nt * C::BN + sub * SUBN;
             const bool live = m0 < p.M && n0 < p.N;  // the same for the whole warp
             const float* xs = p.xs + min(m, p.M - 1);
             const float* ws = p.ws + (size_t)(min(n0, p.N - 1) / BLOCK) * p.kb;
-            float scale = __ldg(xs) * __ldg(ws);
-            f32x2 sum[COLS / 2];
+            f32x2 sum[SUBN / 2];
 #pragma unroll
-            for (int c = 0; c < COLS / 2; ++c) sum[c] = 0;
-            for (int b = 0; b < p.kb; ++b, ++it) {
-                const int next = min(b + 1, p.kb - 1);
-                const float scale_next = __ldg(xs + (size_t)next * p.M) * __ldg(ws + next);
-                ok = __all_sync(0xffffffffu, mbar_wait(bar_acc_full + 8 * a, pa, abort_flag, 4, it));
-                if (!ok) break;
-                tc_fence_after();
-                const f32x2 s2 = pack2(scale, scale);
-                if (live) {
+            for (int c = 0; c < SUBN / 2; ++c) sum[c] = 0;
+            // Scales are under way two groups ahead, 32 columns while the 32 before them are multiplied, and whether the next
+            // group's products are there is asked before this group's last columns are.
+            constexpr int GROUP = C::GROUP, CHUNKS = C::ACC_COLS / 32;
+            float x_scale[2][GROUP], w_scale[2][GROUP];
 #pragma unroll
-                    for (int c = 0; c < COLS; c += 32) {
-                        uint32_t r[32];
-                        tmem_ld32(t_lanes + a * BN + c, r);
-                        tc_wait_ld();
+            for (int u = 0; u < 2 * GROUP; ++u) {
+                x_scale[u / GROUP][u % GROUP] = __ldg(xs + (size_t)min(u, p.kb - 1) * p.M);
+                w_scale[u / GROUP][u % GROUP] = __ldg(ws + min(u, p.kb - 1));
+            }
+            bool there = mbar_test(bar_acc_full + 8 * a, pa);
+            for (int b0 = 0; b0 < p.kb && ok; b0 += 2 * GROUP) {
 #pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            sum[c / 2 + j] = fma2(pack2(__uint_as_float(r[2 * j]), __uint_as_float(r[2 * j + 1])), s2, sum[c / 2 + j]);
+                for (int u = 0; u < 2; ++u) {
+                    const int b = b0 + u * GROUP;
+                    if (b >= p.kb) break;
+                    if (!__all_sync(0xffffffffu, there)) {
+                        ok = __all_sync(0xffffffffu, there || mbar_wait_slow(bar_acc_full + 8 * a, pa, abort_flag, 4, it));
+                        if (!ok) break;
+                    }
+                    tc_fence_after();
+                    float scale[GROUP];
+#pragma unroll
+                    for (int g = 0; g < GROUP; ++g) {
+                        scale[g] = x_scale[u][g] * w_scale[u][g];
+                        const int ahead = min(b + 2 * GROUP + g, p.kb - 1);
+                        x_scale[u][g] = __ldg(xs + (size_t)ahead * p.M);
+                        w_scale[u][g] = __ldg(ws + ahead);
+                    }
+                    uint32_t r[2][32];
+                    const uint32_t from = t_lanes + a * C::ACC_COLS, done = acc_empty0 + 8 * a;
+                    ++it;
+                    if ((a += SUBS) >= (uint32_t)ACC_BUFS) { a = sub; pa ^= 1; }
+                    tmem_ld32(from, r[0]);
+#pragma unroll
+                    for (int c = 0; c < CHUNKS; ++c) {
+                        constexpr int OF_BLOCK = SUBN / 32;
+                        uint32_t(&now)[32] = r[c & 1];
+                        tmem_wait32(now);
+                        if (c + 1 < CHUNKS) tmem_ld32(from + (c + 1) * 32, r[(c + 1) & 1]);
+                        if (c + 1 == CHUNKS) {
+                            tc_fence_before();
+                            mbar_arrive_if<PAIR>(done, lane == 0);
+                            there = b + GROUP < p.kb && mbar_test(bar_acc_full + 8 * a, pa);
+                        }
+                        if (GROUP == 1 || b + c / OF_BLOCK < p.kb) {  // (columns of blocks past the last hold those of an earlier group)
+#pragma unroll
+                            for (int j = 0; j < 16; ++j)
+                                scale_add(sum[c % OF_BLOCK * 16 + j], now[2 * j], now[2 * j + 1], scale[c / OF_BLOCK]);
+                        }
                     }
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) {
-                    if (PAIR) mbar_arrive_cluster(acc_empty0 + 8 * a);
-                    else mbar_arrive(acc_empty0 + 8 * a);
-                }
-                scale = scale_next;
-                if (++a == (uint32_t)ACC_BUFS) { a = 0; pa ^= 1; }
             }
-            if (!ok || m >= p.M) continue;
-            const int cols = min(COLS, p.N - n0);
+            if (!ok) break;
             if (SCORE) {
+                if (m >= p.M) continue;
                 Sums mine;
                 mine.start(-INFINITY);
                 if (live) {
-                    float top = -INFINITY;
-#pragma unroll
-                    for (int c = 0; c < COLS; c += 2) {
-                        float lo, hi;
-                        unpack2(sum[c / 2], lo, hi);
-                        if (c < cols) top = fmaxf(top, lo);
-                        if (c + 1 < cols) top = fmaxf(top, hi);
-                    }
-                    mine.start(top);
                     const long long token = p.tokens64 ? __ldg(reinterpret_cast<const long long*>(p.tokens) + m) : __ldg(reinterpret_cast<const int*>(p.tokens) + m);
-                    const long long at = token - n0;
-#pragma unroll
-                    for (int c = 0; c < COLS; c += 2) {
-                        float lo, hi;
-                        unpack2(sum[c / 2], lo, hi);
-                        if (c < cols) mine.add(lo, p.c);
-                        if (c + 1 < cols) mine.add(hi, p.c);
-                    }
-                    if (at >= 0 && at < cols) {
-#pragma unroll
-                        for (int c = 0; c < COLS; c += 2) {
-                            float lo, hi;
-                            unpack2(sum[c / 2], lo, hi);
-                            if (at == c) p.owns[m] = lo;
-                            if (at == c + 1) p.owns[m] = hi;
-                        }
-                    }
+                    mine = sums_of<SUBN>(sum, min(SUBN, p.N - n0), p.c, token - n0, p.owns + m);
                 }
-                if (p.m_tiles > 1) {
-                    p.stats[(size_t)(nt * C::EPI_SPLIT + col0 / COLS) * p.M + m] = make_float4(mine.r, mine.s, mine.d, 0.f);
+                if (PAIR || p.m_tiles > 1) {
+                    p.stats[(size_t)(nt * SUBS + sub) * p.M + m] = make_float4(mine.r, mine.s, mine.d, 0.f);
                 } else {
                     run.join(mine, p.c);
-                    if (tile + units >= p.tiles) p.stats[(size_t)(unit * C::EPI_SPLIT + col0 / COLS) * p.M + m] = make_float4(run.r, run.s, run.d, 0.f);
+                    if (tile + units >= p.tiles) p.stats[(size_t)(unit * SUBS + sub) * p.M + m] = make_float4(run.r, run.s, run.d, 0.f);
                 }
-                continue;
-            }
-            if (!live) continue;
-            if (p.y_bf16) {
-                __nv_bfloat16* y = reinterpret_cast<__nv_bfloat16*>(p.y) + (size_t)m * p.y_stride + n0;
-                if (p.y_vec && cols == COLS) {
-#pragma unroll
-                    for (int c = 0; c < COLS; c += 8) {
-                        uint32_t v[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            float lo, hi;
-                            unpack2(sum[c / 2 + j], lo, hi);
-                            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v[j]) : "f"(hi), "f"(lo));
-                        }
-                        *reinterpret_cast<uint4*>(y + c) = make_uint4(v[0], v[1], v[2], v[3]);
-                    }
-                } else {
-#pragma unroll
-                    for (int c = 0; c < COLS; c += 2) {
-                        float lo, hi;
-                        unpack2(sum[c / 2], lo, hi);
-                        if (c < cols) y[c] = __float2bfloat16_rn(lo);
-                        if (c + 1 < cols) y[c + 1] = __float2bfloat16_rn(hi);
-                    }
-                }
-            } else {
-                float* y = reinterpret_cast<float*>(p.y) + (size_t)m * p.y_stride + n0;
-                if (p.y_vec && cols == COLS) {
-#pragma unroll
-                    for (int c = 0; c < COLS; c += 4) {
-                        float4 v;
-                        unpack2(sum[c / 2], v.x, v.y);
-                        unpack2(sum[c / 2 + 1], v.z, v.w);
-                        *reinterpret_cast<float4*>(y + c) = v;
-                    }
-                } else {
-#pragma unroll
-                    for (int c = 0; c < COLS; c += 2) {
-                        float lo, hi;
-                        unpack2(sum[c / 2], lo, hi);
-                        if (c < cols) y[c] = lo;
-                        if (c + 1 < cols) y[c + 1] = hi;
-                    }
-                }
+            } else if (live) {
+                if (p.y_bf16) store_rows<SUBN, true>(sum, p, &tm_y, out, m0, n0, lane, stores);
+                else store_rows<SUBN, false>(sum, p, &tm_y, out, m0, n0, lane, stores);
             }
         }
+        if (!SCORE && lane == 0) tma_store_wait_all();
     }
     tc_fence_before();
     __syncthreads();
@@ -323,12 +401,28 @@ template <class C, bool SCORE>
 bitnet_a48_status launch(const LinearArgs& a, const ScoreArgs* score, ScoreParts* parts, cudaStream_t st) {
     static std::atomic<bool> ready[64];
     A48_CUDA_TRY(a48_allow_smem(gemm_fp8_kernel<C, SCORE>, C::SMEM_BYTES, ready));
-    CUtensorMap tm_x, tm_w;
+    if (C::MOVE_REGISTERS) {  // warps that ask for more registers than the launch has would wait for ever
+        static std::atomic<int> registers;
+        int n = registers.load(std::memory_order_relaxed);
+        if (n == 0) {
+            cudaFuncAttributes attr;
+            A48_CUDA_TRY(cudaFuncGetAttributes(&attr, gemm_fp8_kernel<C, SCORE>));
+            registers.store(n = attr.numRegs, std::memory_order_relaxed);
+        }
+        if (n * C::NUM_THREADS < 128 * C::CONTROL_REGISTERS + 32 * C::EPI_WARPS * C::EPI_REGISTERS) return BITNET_A48_ERR_UNSUPPORTED;
+    }
+    CUtensorMap tm_x, tm_w, tm_y;
     const int x_rows = std::min((a.M + 7) / 8 * 8, C::AR);
-    if (!make_byte_map(&tm_x, a.x, (uint64_t)a.M, (uint64_t)a.K, (uint64_t)a.K, (uint32_t)x_rows) ||
-        !make_byte_map(&tm_w, a.w, (uint64_t)a.N, (uint64_t)a.K, (uint64_t)a.K, (uint32_t)C::BROWS))
+    if (!make_map(&tm_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.x, (uint64_t)a.M, (uint64_t)a.K, (uint64_t)a.K, (uint32_t)x_rows) ||
+        !make_map(&tm_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.w, (uint64_t)a.N, (uint64_t)a.K, (uint64_t)a.K, (uint32_t)C::SUB_ROWS))
         return BITNET_A48_ERR_CUDA;
     Params p = {};
+    const int size = a.y_bf16 ? 2 : 4;
+    p.y_map = !SCORE && a48_aligned16(a.y) && a.y_stride * size % 16 == 0 && (unsigned long long)a.y_stride * size < (1ull << 40);
+    tm_y = tm_x;  // not used without y_map
+    if (p.y_map && !make_map(&tm_y, a.y_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, (uint32_t)size, a.y, (uint64_t)a.M,
+                             (uint64_t)a.N, (uint64_t)a.y_stride * size, 32))
+        return BITNET_A48_ERR_CUDA;
     p.xs = a.xs;
     p.ws = a.ws;
     p.y = a.y;
@@ -342,7 +436,6 @@ bitnet_a48_status launch(const LinearArgs& a, const ScoreArgs* score, ScoreParts
     p.tiles = (int)tiles;
     p.x_rows = x_rows;
     p.y_bf16 = a.y_bf16;
-    p.y_vec = a48_aligned16(a.y) && a.y_stride % (a.y_bf16 ? 8 : 4) == 0;
     const int slots = sm_count() / C::CTAS;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(std::min(p.tiles, slots) * C::CTAS));
@@ -363,9 +456,9 @@ bitnet_a48_status launch(const LinearArgs& a, const ScoreArgs* score, ScoreParts
         p.c = score->c;
         p.stats = parts->stats;
         p.owns = parts->owns;
-        parts->parts = C::EPI_SPLIT * (p.m_tiles > 1 ? (a.N + C::BN - 1) / C::BN : (int)cfg.gridDim.x / C::CTAS);
+        parts->parts = C::SUBS * (C::PAIR || p.m_tiles > 1 ? (a.N + C::BN - 1) / C::BN : (int)cfg.gridDim.x / C::CTAS);
     }
-    A48_CUDA_TRY(cudaLaunchKernelEx(&cfg, gemm_fp8_kernel<C, SCORE>, tm_x, tm_w, p));
+    A48_CUDA_TRY(cudaLaunchKernelEx(&cfg, gemm_fp8_kernel<C, SCORE>, tm_x, tm_w, tm_y, p));
     return BITNET_A48_OK;
 }
 
@@ -379,10 +472,10 @@ bitnet_a48_status launch(const LinearArgs& a, const ScoreArgs* score, ScoreParts
 namespace a48f8 {
 
 bitnet_a48_status launch_gemm(const LinearArgs& a, const ScoreArgs* score, ScoreParts* parts, cudaStream_t st) {
-    if (a.M <= 32) return launch<Cfg<32, 32, false>>(a, score, parts, st);
-    if (a.M <= 64) return launch<Cfg<64, 64, false>>(a, score, parts, st);
-    if (a.M <= 128) return launch<Cfg<128, 128, false>>(a, score, parts, st);
-    return launch<Cfg<128, 256, true>>(a, score, parts, st);
+    if (a.M <= 32) return launch<Cfg<32, 1, 32, false>>(a, score, parts, st);
+    if (a.M <= 64) return launch<Cfg<64, 1, 64, false>>(a, score, parts, st);
+    if (a.M <= 128) return launch<Cfg<128, 1, 128, false>>(a, score, parts, st);
+    return launch<Cfg<128, 2, 128, true>>(a, score, parts, st);
 }
 
 size_t score_stats(int M, int N) {

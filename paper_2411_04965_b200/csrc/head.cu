@@ -69,7 +69,7 @@ bitnet_a48_status bitnet_a48_linear_fp8(const uint8_t* codes_dev, const float* s
         (reinterpret_cast<uintptr_t>(Y_dev) & (y_bf16 ? 1u : 3u)))
         return BITNET_A48_ERR_ALIGNMENT;
     if (!a48_have_device()) return BITNET_A48_ERR_CUDA;
-    const a48f8::LinearArgs a = {codes_dev, scale_dev, w_codes_dev, w_scale_dev, M, N, K, Y_dev, M > 1 ? y_stride : (N + 7) / 8 * 8, y_bf16};
+    const a48f8::LinearArgs a = {codes_dev, scale_dev, w_codes_dev, w_scale_dev, M, N, K, Y_dev, M > 1 ? y_stride : (N + 7) / 8 * 8ll, y_bf16};
     return a48f8::launch_gemm(a, nullptr, nullptr, (cudaStream_t)stream);
 }
 
