@@ -47,7 +47,7 @@ struct ScoreParts {
     float* owns;    // [M]
     int parts;      // set by launch_gemm
 };
-size_t score_stats(int M, int N);  // most float4 that stats may take
+size_t score_stats(int M, int N);  // most float4 that stats may take, whatever the device
 
 // ---- quant_fp8.cu
 bitnet_a48_status launch_quant_rows(const void* X, int bf16, long long stride, const float* gain, float eps, int M, int K, uint8_t* codes, float* scale,
@@ -58,7 +58,12 @@ bitnet_a48_status launch_quant_weight(const void* W, int bf16, long long stride,
 bitnet_a48_status launch_logprobs(const LogprobArgs& a, cudaStream_t st);
 bitnet_a48_status launch_score_join(const ScoreArgs& s, const ScoreParts& w, int M, int V, cudaStream_t st);
 
+// ---- rows_fp8.cu
+bool few_supported(int M, int K);
+bitnet_a48_status launch_few(const LinearArgs& a, cudaStream_t st);
+
 // ---- gemm_fp8.cu
+int sm_count();  // of the current device
 // score, parts: NULL, or the product keeps these and stores no y.
 bitnet_a48_status launch_gemm(const LinearArgs& a, const ScoreArgs* score, ScoreParts* parts, cudaStream_t st);
 

@@ -25,33 +25,31 @@ using a48f8::LinearArgs;
 constexpr int TMEM_COLS = 512;
 constexpr int CONTROL_WARPS = 4;  // copies, MMAs, and two that only make up a warpgroup
 
-// AR: rows of the token tile that a stage has room for (the MMA reads 128; what lies behind belongs to tokens that do not
-// exist).  SUBS x SUBN: features of a tile, as so many accumulators of SUBN columns, each with a warpgroup of its own that takes it
+// SUBS x SUBN: features of a tile, as so many accumulators of SUBN columns, each with a warpgroup of its own that takes it
 // out of tensor memory.  PAIR: two CTAs share a tile of 256 tokens; each holds half of the weight rows of an accumulator.
-template <int AR_, int SUBS_, int SUBN_, bool PAIR_>
+template <int SUBS_, int SUBN_, bool PAIR_>
 struct Cfg {
-    static constexpr int AR = AR_, SUBS = SUBS_, SUBN = SUBN_, BN = SUBS * SUBN;
+    static constexpr int SUBS = SUBS_, SUBN = SUBN_, BN = SUBS * SUBN;
     static constexpr bool PAIR = PAIR_;
     static constexpr int CTAS = PAIR ? 2 : 1, TM = 128 * CTAS;
     static constexpr int SUB_ROWS = SUBN / CTAS;  // weight rows of an accumulator that a CTA holds
-    static constexpr int A_BYTES = AR * BLOCK, SUB_BYTES = SUB_ROWS * BLOCK, STAGE_BYTES = A_BYTES + SUBS * SUB_BYTES;
-    static constexpr int SLACK = AR < 128 ? (128 - AR) * BLOCK : 0;
+    static constexpr int A_BYTES = 128 * BLOCK, SUB_BYTES = SUB_ROWS * BLOCK, STAGE_BYTES = A_BYTES + SUBS * SUB_BYTES;
     static constexpr int OUT_BYTES = 4096, OUT_BUFS = 2;  // 32 rows of 128 bytes on their way out, two to a warp
     static constexpr int EPI_WARPS = 4 * SUBS, NUM_THREADS = 32 * (CONTROL_WARPS + EPI_WARPS);
     static constexpr int OUT_ALL = EPI_WARPS * OUT_BUFS * OUT_BYTES;
-    static constexpr int MAX_STAGES = (225 * 1024 - SLACK - OUT_ALL) / STAGE_BYTES;
+    static constexpr int MAX_STAGES = (225 * 1024 - OUT_ALL) / STAGE_BYTES;
     static constexpr int STAGES = MAX_STAGES < 16 ? MAX_STAGES : 16;
     // Blocks of channels that change hands at once between the MMAs and the epilogue, each in columns of its own: what the
     // hand-over costs (about 300 clocks) is spread over 128 columns whatever the tile.
     static constexpr int GROUP = BLOCK / SUBN, ACC_COLS = GROUP * SUBN;
     static constexpr int ACC_BUFS = TMEM_COLS / ACC_COLS;
-    static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + SLACK + OUT_ALL + 1024 /*alignment*/ + 512 /*barriers*/;
+    static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + OUT_ALL + 1024 /*alignment*/ + 512 /*barriers*/;
     // With eight epilogue warps 168 registers a thread at launch are all an SM has; the control warps hand theirs over.
     static constexpr bool MOVE_REGISTERS = SUBS == 2;
     static constexpr int CONTROL_REGISTERS = 40, EPI_REGISTERS = 232;
     static_assert(!MOVE_REGISTERS || 128 * CONTROL_REGISTERS + 256 * EPI_REGISTERS <= 384 * 168, "registers of the launch");
     static_assert(SUBN % 32 == 0 && SUBN <= BLOCK, "the columns of an accumulator share a weight scale");
-    static_assert(ACC_BUFS % SUBS == 0 && STAGE_BYTES % 1024 == 0 && SLACK % 1024 == 0, "layout");
+    static_assert(ACC_BUFS % SUBS == 0 && STAGE_BYTES % 1024 == 0, "layout");
     static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
     static_assert(8 * (2 * STAGES + 2 * ACC_BUFS) <= 480, "barriers");
 };
@@ -181,7 +179,7 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
     constexpr bool PAIR = C::PAIR;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint8_t* out_all = smem + STAGES * C::STAGE_BYTES + C::SLACK;
+    uint8_t* out_all = smem + STAGES * C::STAGE_BYTES;
     uint8_t* ctrl = out_all + C::OUT_ALL;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl + 480);
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(ctrl + 484);
@@ -385,18 +383,6 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
     }
 }
 
-int sm_count() {
-    static std::atomic<int> n[64];
-    int dev = 0;
-    cudaGetDevice(&dev);
-    int c = n[dev & 63].load(std::memory_order_relaxed);
-    if (!c) {
-        cudaDeviceGetAttribute(&c, cudaDevAttrMultiProcessorCount, dev);
-        n[dev & 63].store(c, std::memory_order_relaxed);
-    }
-    return c;
-}
-
 template <class C, bool SCORE>
 bitnet_a48_status launch(const LinearArgs& a, const ScoreArgs* score, ScoreParts* parts, cudaStream_t st) {
     static std::atomic<bool> ready[64];
@@ -412,7 +398,7 @@ bitnet_a48_status launch(const LinearArgs& a, const ScoreArgs* score, ScoreParts
         if (n * C::NUM_THREADS < 128 * C::CONTROL_REGISTERS + 32 * C::EPI_WARPS * C::EPI_REGISTERS) return BITNET_A48_ERR_UNSUPPORTED;
     }
     CUtensorMap tm_x, tm_w, tm_y;
-    const int x_rows = std::min((a.M + 7) / 8 * 8, C::AR);
+    const int x_rows = std::min((a.M + 7) / 8 * 8, 128);
     if (!make_map(&tm_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.x, (uint64_t)a.M, (uint64_t)a.K, (uint64_t)a.K, (uint32_t)x_rows) ||
         !make_map(&tm_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, a.w, (uint64_t)a.N, (uint64_t)a.K, (uint64_t)a.K, (uint32_t)C::SUB_ROWS))
         return BITNET_A48_ERR_CUDA;
@@ -436,7 +422,7 @@ bitnet_a48_status launch(const LinearArgs& a, const ScoreArgs* score, ScoreParts
     p.tiles = (int)tiles;
     p.x_rows = x_rows;
     p.y_bf16 = a.y_bf16;
-    const int slots = sm_count() / C::CTAS;
+    const int slots = a48f8::sm_count() / C::CTAS;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(std::min(p.tiles, slots) * C::CTAS));
     cfg.blockDim = dim3(C::NUM_THREADS);
@@ -471,19 +457,42 @@ bitnet_a48_status launch(const LinearArgs& a, const ScoreArgs* score, ScoreParts
 
 namespace a48f8 {
 
-bitnet_a48_status launch_gemm(const LinearArgs& a, const ScoreArgs* score, ScoreParts* parts, cudaStream_t st) {
-    if (a.M <= 32) return launch<Cfg<32, 1, 32, false>>(a, score, parts, st);
-    if (a.M <= 64) return launch<Cfg<64, 1, 64, false>>(a, score, parts, st);
-    if (a.M <= 128) return launch<Cfg<128, 1, 128, false>>(a, score, parts, st);
-    return launch<Cfg<128, 2, 128, true>>(a, score, parts, st);
+int sm_count() {
+    static std::atomic<int> n[64];
+    int dev = 0;
+    cudaGetDevice(&dev);
+    int c = n[dev & 63].load(std::memory_order_relaxed);
+    if (!c) {
+        cudaDeviceGetAttribute(&c, cudaDevAttrMultiProcessorCount, dev);
+        n[dev & 63].store(c, std::memory_order_relaxed);
+    }
+    return c;
 }
 
-size_t score_stats(int M, int N) {
-    // one tile of tokens: a part to each half of the columns of a CTA, of which there are no more than 512 and no more than
-    // tiles of 32; more: one to each 128 columns
-    const size_t parts = M <= 128 ? std::min<size_t>(1024, 2 * ((N + 31) / 32)) : 2 * (size_t)((N + 255) / 256);
-    return parts * M;
+// Tiles: 128 tokens x 64 or 128 features of one CTA, or 256 x 256 of a pair.  A call takes as long as its rounds of tiles over
+// the SMs times what a block of 128 channels costs a tile: 0.39, 0.50 and 0.62 us (measured from 40 x 4096 x 1536 to 2048 x
+// 11008 x 4096; the model picked the fastest of the three in 15 of 16 of them, e.g. 64 tokens x 32000 x 3200: 37, 29, 35 us,
+// 64 x 4096 x 4096: 16, 19, 23 us, 512 x 32000 x 3200: 132, 91, 76 us).
+enum Form { NARROW, WIDE, PAIRED };
+constexpr int kMostSingle = 1024;  // tokens; beyond, the pairs' tiles fill the GPU
+
+Form form_of(int M, int N) {
+    const long long sms = sm_count(), m1 = (M + 127) / 128, m2 = (M + 255) / 256;
+    const long long narrow = (m1 * ((N + 63) / 64) + sms - 1) / sms * 39, wide = (m1 * ((N + 127) / 128) + sms - 1) / sms * 50;
+    const long long pair = (m2 * ((N + 255) / 256) + sms / 2 - 1) / (sms / 2) * 62;
+    if (M > kMostSingle || (pair <= wide && pair <= narrow)) return PAIRED;
+    return wide <= narrow ? WIDE : NARROW;
 }
+
+bitnet_a48_status launch_gemm(const LinearArgs& a, const ScoreArgs* score, ScoreParts* parts, cudaStream_t st) {
+    switch (form_of(a.M, a.N)) {
+        case NARROW: return launch<Cfg<1, 64, false>>(a, score, parts, st);
+        case WIDE: return launch<Cfg<1, 128, false>>(a, score, parts, st);
+        default: return launch<Cfg<2, 128, true>>(a, score, parts, st);
+    }
+}
+
+size_t score_stats(int M, int N) { return (size_t)M * (M <= kMostSingle ? (N + 63) / 64 : 2 * ((N + 255) / 256)); }
 
 }  // namespace a48f8
 

@@ -17,16 +17,19 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
 bool temperature_ok(float t) { return t >= 1e-30f && t <= 1e30f; }
 
-// Parts of the workspace of bitnet_a48_score.
+// Parts of the workspace of bitnet_a48_score.  The logits of few tokens are stored after all: they stay in L2, and the kernel that
+// streams the weight for few tokens is worth more than what they cost.
 struct ScoreSpace {
     size_t codes, scale, stats, owns, end;
     ScoreSpace(int M, int N, int K) {
+        const bool few = a48f8::few_supported(M, K);
         codes = 0;
         scale = codes + up256((size_t)M * K);
         stats = scale + up256((size_t)a48f8::blocks(K) * M * 4);
-        owns = stats + up256(a48f8::score_stats(M, N) * sizeof(float4));
-        end = owns + up256((size_t)M * 4);
+        owns = stats + up256(few ? (size_t)M * logits_stride(N) * 4 : a48f8::score_stats(M, N) * sizeof(float4));
+        end = owns + up256(few ? 0 : (size_t)M * 4);
     }
+    static long long logits_stride(int N) { return (N + 3) / 4 * 4ll; }
 };
 
 bitnet_a48_status check_quant(const void* X, int rows, int K, long long stride, int bf16, const void* codes, const void* scale) {
@@ -70,7 +73,7 @@ bitnet_a48_status bitnet_a48_linear_fp8(const uint8_t* codes_dev, const float* s
         return BITNET_A48_ERR_ALIGNMENT;
     if (!a48_have_device()) return BITNET_A48_ERR_CUDA;
     const a48f8::LinearArgs a = {codes_dev, scale_dev, w_codes_dev, w_scale_dev, M, N, K, Y_dev, M > 1 ? y_stride : (N + 7) / 8 * 8ll, y_bf16};
-    return a48f8::launch_gemm(a, nullptr, nullptr, (cudaStream_t)stream);
+    return a48f8::few_supported(M, K) ? a48f8::launch_few(a, (cudaStream_t)stream) : a48f8::launch_gemm(a, nullptr, nullptr, (cudaStream_t)stream);
 }
 
 bitnet_a48_status bitnet_a48_logprobs(const void* logits_dev, long long stride, int x_bf16, int M, int V, float temperature, const void* tokens_dev,
@@ -117,7 +120,15 @@ bitnet_a48_status bitnet_a48_score(const void* X_dev, long long x_stride, int x_
     float* scale = reinterpret_cast<float*>(ws + at.scale);
     s = a48f8::launch_quant_rows(X_dev, x_bf16, M > 1 ? x_stride : K, gain_dev, norm_eps, M, K, ws + at.codes, scale, (cudaStream_t)stream);
     if (s != BITNET_A48_OK) return s;
-    const a48f8::LinearArgs a = {ws + at.codes, scale, w_codes_dev, w_scale_dev, M, N, K, nullptr, 0, 0};
+    a48f8::LinearArgs a = {ws + at.codes, scale, w_codes_dev, w_scale_dev, M, N, K, nullptr, 0, 0};
+    if (a48f8::few_supported(M, K)) {
+        a.y = ws + at.stats;
+        a.y_stride = ScoreSpace::logits_stride(N);
+        s = a48f8::launch_few(a, (cudaStream_t)stream);
+        if (s != BITNET_A48_OK) return s;
+        const a48f8::LogprobArgs l = {a.y, tokens_dev, logprob_dev, entropy_dev, nullptr, nullptr, nullptr, a.y_stride, M, N, 0, 0, tokens_i64, temperature};
+        return a48f8::launch_logprobs(l, (cudaStream_t)stream);
+    }
     const a48f8::ScoreArgs score = {tokens_dev, tokens_i64, (float)(1.4426950408889634 / (double)temperature), logprob_dev, entropy_dev};
     a48f8::ScoreParts parts = {reinterpret_cast<float4*>(ws + at.stats), reinterpret_cast<float*>(ws + at.owns), 0};
     s = a48f8::launch_gemm(a, &score, &parts, (cudaStream_t)stream);
