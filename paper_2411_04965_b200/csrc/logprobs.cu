@@ -18,9 +18,9 @@ namespace {
 
 using a48f8::Sums;
 
-constexpr int THREADS = 256, WARPS = THREADS / 32;
-constexpr int SAMPLE = 8;   // segments (16 bytes to a thread) kept in registers
-constexpr int CAP = 2048;   // entries of the list
+constexpr int CAP = 2048;  // entries of the list
+// Threads to a row: many blocks of 256 to an SM, or 1024 where there are fewer rows than SMs.
+constexpr int MANY = 256, FEW = 1024;
 using a48f8::LN2;
 
 struct Args {
@@ -74,38 +74,37 @@ template <bool BF16>
 struct Walk {
     Row<BF16> row;
     Sums sums;
-    float c, own, least;  // least: logits at or above it go to the list
-    int token, ahead;     // ahead: logits that come before the token's in the order
+    float c, far;          // far: logits above it move the reference
+    float own, at_or_above;  // a logit counts as ahead of the token's from there on: `own` before the token, the next number behind it
+    float least;           // logits at or above it go to the list
+    int token, ahead;      // ahead: logits that come before the token's in the order
     unsigned long long* list;
     uint32_t* count;
 
+    __device__ __forceinline__ void start(float largest) {
+        sums.start(largest);
+        far = fmaf(60.f, 1.f / c, sums.r);
+    }
     __device__ __forceinline__ void note(float x, int id) {
         const uint32_t at = atomicAdd(count, 1u);
         if (at < (uint32_t)CAP) list[at] = entry_of(x, id);
     }
     template <int N>
-    __device__ __forceinline__ void rank(const float (&v)[N], int id) {
-        if (id <= token && token < id + N) {
-#pragma unroll
-            for (int j = 0; j < N; ++j) ahead += id + j < token ? v[j] >= own : v[j] > own;
-        } else if (id < token) {
-#pragma unroll
-            for (int j = 0; j < N; ++j) ahead += v[j] >= own;
-        } else {
-#pragma unroll
-            for (int j = 0; j < N; ++j) ahead += v[j] > own;
-        }
-    }
-    template <int N>
-    __device__ __forceinline__ void take(const float (&v)[N], int id, bool top) {
+    __device__ __forceinline__ void take(const float (&v)[N], int id) {
         float m = v[0];
 #pragma unroll
         for (int j = 1; j < N; ++j) m = fmaxf(m, v[j]);
-        if ((m - sums.r) * c > 60.f) sums.move(m, c);
+        if (m > far) {
+            sums.move(m, c);
+            far = fmaf(60.f, 1.f / c, sums.r);
+        }
+        const float mark = id < token ? own : at_or_above;
 #pragma unroll
-        for (int j = 0; j < N; ++j) sums.add(v[j], c);
-        rank(v, id);
-        if (top && m >= least) {
+        for (int j = 0; j < N; ++j) {
+            sums.add(v[j], c);
+            ahead += v[j] >= mark;
+        }
+        if (m >= least) {
 #pragma unroll
             for (int j = 0; j < N; ++j)
                 if (v[j] >= least) note(v[j], id + j);
@@ -113,7 +112,8 @@ struct Walk {
     }
 };
 
-// Where all threads of the block agree: inclusive sums over the block of a 0/1 flag.
+// For all threads of the block together: how many of them before this one, and in all, have the flag.
+template <int WARPS>
 __device__ __forceinline__ int flags_before(bool flag, uint32_t* warp_counts, int& total) {
     const uint32_t votes = __ballot_sync(0xffffffffu, flag);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -129,9 +129,10 @@ __device__ __forceinline__ int flags_before(bool flag, uint32_t* warp_counts, in
     return before + __popc(votes & ((1u << lane) - 1));
 }
 
-template <bool BF16>
-__global__ void __launch_bounds__(THREADS) logprobs_kernel(const Args a) {
-    constexpr int E = Row<BF16>::E;
+template <bool BF16, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_kernel(const Args a) {
+    constexpr int E = Row<BF16>::E, WARPS = THREADS / 32;
+    constexpr int SAMPLE = (THREADS == MANY ? 32 : 16) / E;  // segments (16 bytes to a thread) kept in registers
     __shared__ unsigned long long list[CAP];
     __shared__ float best[THREADS];
     __shared__ float4 part[WARPS];
@@ -146,35 +147,37 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(const Args a) {
     w.count = &count;
     w.ahead = 0;
     w.token = -1;
-    w.own = __uint_as_float(0x7fc00000u);  // nothing is above no number
-    if (a.tokens) {
-        const long long token = a.tokens64 ? __ldg(reinterpret_cast<const long long*>(a.tokens) + r) : __ldg(reinterpret_cast<const int*>(a.tokens) + r);
-        if (token >= 0 && token < a.V) {
-            w.token = (int)token;
-            w.own = w.row.at(w.token);
-        }
-    }
-    const bool top = a.top > 0;
+    w.own = w.at_or_above = w.least = __uint_as_float(0x7fc00000u);  // nothing is above no number
     // whole 16 bytes between the first and last few logits, which threads 0 .. E - 1 and E .. 2 E - 1 take one by one
     const int skew = (int)(reinterpret_cast<uintptr_t>(w.row.p) & 15u) / (BF16 ? 2 : 4), head = min(a.V, skew ? E - skew : 0);
     const int vecs = (a.V - head) / E, tail = head + vecs * E;
     const int segments = (vecs + THREADS - 1) / THREADS;
     const int leap = segments == a.segments ? a.leap : a.leap_fewer;
+    uint4 kept[SAMPLE];
+    int at = 0;  // segment
+#pragma unroll
+    for (int i = 0; i < SAMPLE; ++i) {
+        const int vec = at * THREADS + t;
+        const uint32_t none = BF16 ? 0xff80ff80u : 0xff800000u;  // -inf
+        kept[i] = i < segments && vec < vecs ? w.row.load(head, vec) : make_uint4(none, none, none, none);
+        at += leap;
+        at -= at >= segments ? segments : 0;
+    }
+    if (a.tokens) {
+        const long long token = a.tokens64 ? __ldg(reinterpret_cast<const long long*>(a.tokens) + r) : __ldg(reinterpret_cast<const int*>(a.tokens) + r);
+        if (token >= 0 && token < a.V) {
+            w.token = (int)token;
+            w.own = w.row.at(w.token);
+            w.at_or_above = of_order(order_of(w.own) + 1);
+        }
+    }
+    const bool top = a.top > 0;
     const int edge = t < E ? (t < head ? t : -1) : t < 2 * E && tail + t - E < a.V ? tail + t - E : -1;
     float edge_x[1] = {-INFINITY};
     if (edge >= 0) edge_x[0] = w.row.at(edge);
 
     if (t == 0) count = 0;
-    uint4 kept[SAMPLE];
     float m = edge_x[0];
-    int at = 0;  // segment
-#pragma unroll
-    for (int i = 0; i < SAMPLE; ++i) {
-        const int vec = at * THREADS + t;
-        kept[i] = i < segments && vec < vecs ? w.row.load(head, vec) : BF16 ? make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u) : make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u);
-        at += leap;
-        at -= at >= segments ? segments : 0;
-    }
 #pragma unroll
     for (int i = 0; i < SAMPLE; ++i) {
         float v[E];
@@ -182,41 +185,48 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(const Args a) {
 #pragma unroll
         for (int j = 0; j < E; ++j) m = fmaxf(m, v[j]);
     }
-    w.sums.start(m);
+    w.start(m);
     bool strict = false;
     float bound = -INFINITY;
     if (top) {
         best[t] = m;
         __syncthreads();
-        // the bound, in every warp alike: halving the range of orders that holds the k-th largest of the threads' maxima
-        uint32_t key[WARPS];
-        uint32_t hi = 0;
+        if (warp == 0) {  // the bound: halving the range of orders that holds the k-th largest of the threads' maxima
+            uint32_t key[WARPS], hi = 0;
 #pragma unroll
-        for (int i = 0; i < WARPS; ++i) {
-            key[i] = order_of(best[i * 32 + lane]);
-            hi = max(hi, key[i]);
-        }
-        hi = __reduce_max_sync(0xffffffffu, hi);
-        uint32_t lo = order_of(-INFINITY);
-        int reach = THREADS;  // maxima at or above lo, k or more
-        while (lo < hi && reach > a.top + a.top / 4 + 2) {
-            const uint32_t mid = lo + (hi - lo + 1) / 2;
-            int n = 0;
+            for (int i = 0; i < WARPS; ++i) {
+                key[i] = order_of(best[i * 32 + lane]);
+                hi = max(hi, key[i]);
+            }
+            hi = __reduce_max_sync(0xffffffffu, hi);
+            uint32_t lo = order_of(-INFINITY);
+            int reach = THREADS;  // maxima at or above lo, k or more
+            while (lo < hi && reach > a.top + a.top / 4 + 2) {
+                const uint32_t mid = lo + (hi - lo + 1) / 2;
+                int n = 0;
 #pragma unroll
-            for (int i = 0; i < WARPS; ++i) n += __popc(__ballot_sync(0xffffffffu, key[i] >= mid));
-            if (n >= a.top) {
-                lo = mid;
-                reach = n;
-            } else {
-                hi = mid - 1;
+                for (int i = 0; i < WARPS; ++i) n += key[i] >= mid;
+                n = __reduce_add_sync(0xffffffffu, n);
+                if (n >= a.top) {
+                    lo = mid;
+                    reach = n;
+                } else {
+                    hi = mid - 1;
+                }
+            }
+            int same = 0;
+#pragma unroll
+            for (int i = 0; i < WARPS; ++i) same += key[i] == lo;
+            same = __reduce_add_sync(0xffffffffu, same);
+            if (lane == 0) {
+                found[0] = lo;
+                found[1] = lo == order_of(-INFINITY) || same > 32;
             }
         }
-        bound = of_order(lo);
-        int same = 0;
-#pragma unroll
-        for (int i = 0; i < WARPS; ++i) same += __popc(__ballot_sync(0xffffffffu, key[i] == lo));
-        strict = lo == order_of(-INFINITY) || same > 32;
-        w.least = strict ? of_order(order_of(bound) + 1) : bound;
+        __syncthreads();
+        bound = of_order(found[0]);
+        strict = found[1] != 0;
+        w.least = strict ? of_order(found[0] + 1) : bound;
     }
     int seg = 0;
 #pragma unroll
@@ -224,54 +234,60 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(const Args a) {
         float v[E];
         Row<BF16>::widen(kept[i], v);
         const int vec = seg * THREADS + t;
-        if (i < segments && vec < vecs) w.take(v, head + vec * E, top);
+        if (i < segments && vec < vecs) w.take(v, head + vec * E);
         seg += leap;
         seg -= seg >= segments ? segments : 0;
     }
-    if (edge >= 0) w.take(edge_x, edge, top);
-    if (segments > SAMPLE) {
-        for (int i = SAMPLE; i < segments; i += 4) {
-            uint4 u[4];
-            int id[4];
+    if (edge >= 0) w.take(edge_x, edge);
+    for (int i = SAMPLE; i < segments; i += 4) {
+        uint4 u[4];
+        int id[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int vec = at * THREADS + t;
-                id[q] = i + q < segments && vec < vecs ? vec : -1;
-                if (id[q] >= 0) u[q] = w.row.load(head, vec);
-                at += leap;
-                at -= at >= segments ? segments : 0;
-            }
+        for (int q = 0; q < 4; ++q) {
+            const int vec = at * THREADS + t;
+            id[q] = i + q < segments && vec < vecs ? vec : -1;
+            if (id[q] >= 0) u[q] = w.row.load(head, vec);
+            at += leap;
+            at -= at >= segments ? segments : 0;
+        }
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (id[q] < 0) continue;
-                float v[E];
-                Row<BF16>::widen(u[q], v);
-                w.take(v, head + id[q] * E, top);
-            }
+        for (int q = 0; q < 4; ++q) {
+            if (id[q] < 0) continue;
+            float v[E];
+            Row<BF16>::widen(u[q], v);
+            w.take(v, head + id[q] * E);
         }
     }
+    if (t == 0 && w.token >= head && w.token < tail && (w.token - head) % E != 0)  // in the token's own 16 bytes, equal ones from it on do not count
+        for (int i = w.token; i < min(tail, head + (w.token - head) / E * E + E); ++i) w.ahead -= w.row.at(i) == w.own;
     // ---- joined
     float ref = w.sums.r;
 #pragma unroll
     for (int o = 16; o; o >>= 1) ref = fmaxf(ref, __shfl_xor_sync(0xffffffffu, ref, o));
     w.sums.move(ref, a.c);
     float s = w.sums.s, d = w.sums.d;
-    int ahead = w.ahead;
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         s += __shfl_xor_sync(0xffffffffu, s, o);
         d += __shfl_xor_sync(0xffffffffu, d, o);
-        ahead += __shfl_xor_sync(0xffffffffu, ahead, o);
     }
+    int ahead = __reduce_add_sync(0xffffffffu, w.ahead);
     if (lane == 0) part[warp] = make_float4(ref, s, d, __int_as_float(ahead));
     __syncthreads();
-    Sums all = {part[0].x, part[0].y, part[0].z};
-    ahead = __float_as_int(part[0].w);
-    for (int i = 1; i < WARPS; ++i) {
-        Sums more = {part[i].x, part[i].y, part[i].z};
-        all.join(more, a.c);
-        ahead += __float_as_int(part[i].w);
+    Sums all;
+    all.start(-INFINITY);
+    ahead = 0;
+    if (lane < WARPS) {
+        all = {part[lane % WARPS].x, part[lane % WARPS].y, part[lane % WARPS].z};
+        ahead = __float_as_int(part[lane % WARPS].w);
     }
+    ahead = __reduce_add_sync(0xffffffffu, ahead);
+#pragma unroll
+    for (int o = WARPS / 2; o; o >>= 1) {
+        const Sums more = {__shfl_xor_sync(0xffffffffu, all.r, o), __shfl_xor_sync(0xffffffffu, all.s, o), __shfl_xor_sync(0xffffffffu, all.d, o)};
+        all.join(more, a.c);
+    }
+    all = {__shfl_sync(0xffffffffu, all.r, 0), __shfl_sync(0xffffffffu, all.s, 0), __shfl_sync(0xffffffffu, all.d, 0)};
     const bool valid = all.valid();
     const float log_s = log2f(all.s), nan = __uint_as_float(0x7fc00000u);
     if (t == 0) {
@@ -294,7 +310,7 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(const Args a) {
         uint32_t prefix = 0;
         int need = a.top;
         for (int shift = 24; shift >= 0; shift -= 8) {
-            hist[t] = 0;
+            if (t < 256) hist[t] = 0;
             __syncthreads();
             for (int i = t; i < a.V; i += THREADS) {
                 const uint32_t o = order_of(w.row.at(i));
@@ -327,7 +343,7 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(const Args a) {
             const int i = i0 + t;
             const bool is = i < a.V && order_of(w.row.at(i)) == order_of(bound);
             int total;
-            const int before = flags_before(is, counts, total);
+            const int before = flags_before<WARPS>(is, counts, total);
             if (is && have + before < a.top) list[have + before] = entry_of(bound, i);
             have += total;
         }
@@ -416,12 +432,18 @@ bitnet_a48_status launch_logprobs(const LogprobArgs& g, cudaStream_t st) {
     a.top = g.top;
     a.tokens64 = g.tokens64;
     a.c = (float)(1.4426950408889634 / (double)g.temperature);
-    const int vecs = g.V / (g.x_bf16 ? 8 : 4);
-    a.segments = (vecs + THREADS - 1) / THREADS;
+    // fewer rows than SMs: more threads to a row (8 rows of 32000: 5.6 us for 9.6)
+    const int threads = g.M <= sm_count() && g.V >= 8192 ? FEW : MANY, vecs = g.V / (g.x_bf16 ? 8 : 4);
+    a.segments = (vecs + threads - 1) / threads;
     a.leap = leap_over(a.segments);
     a.leap_fewer = leap_over(a.segments - 1);
-    if (g.x_bf16) logprobs_kernel<true><<<g.M, THREADS, 0, st>>>(a);
-    else logprobs_kernel<false><<<g.M, THREADS, 0, st>>>(a);
+    if (threads == FEW) {
+        if (g.x_bf16) logprobs_kernel<true, FEW><<<g.M, FEW, 0, st>>>(a);
+        else logprobs_kernel<false, FEW><<<g.M, FEW, 0, st>>>(a);
+    } else {
+        if (g.x_bf16) logprobs_kernel<true, MANY><<<g.M, MANY, 0, st>>>(a);
+        else logprobs_kernel<false, MANY><<<g.M, MANY, 0, st>>>(a);
+    }
     A48_CUDA_TRY(cudaGetLastError());
     return BITNET_A48_OK;
 }

@@ -3,12 +3,16 @@
 //   code = the e4m3 number nearest to 448 v / a, ties to even;   scale = a / 448 (times 1 / rms of the row).
 // The row's size is a factor of the scale alone, so a code does not depend on the rounding of a norm.
 //
-// Codes are those of exact arithmetic.  t = v * (448 / a) in fp32 is off by less than 2^-21 of itself (2^-22 for the
-// quotient, 2^-24 each for the product with the gain, for a and for t); where t (1 - 2^-20) and t (1 + 2^-20) round to the
-// same code, so does the exact number.  The others, about one in 2^15, are redone in 64 bits, in which the product and
-// 448 v are exact and the quotient has one rounding.
+// Codes are those of exact arithmetic.  v * (448 / a) in fp32 is off by at most 2^-21 of itself (2^-22 for the quotient, 2^-24 each
+// for the product with the gain, for a, for the factor and for the product); where it rounds to the same code with a factor 5 * 2^-23
+// smaller and 5 * 2^-23 larger, so does the exact number.  For the others, about one in 10^5, 448 v is compared with a times the
+// border between the two codes, as sums of two fp32 numbers each (without a gain both are exact in that form, and with one where
+// the products fit into 47 bits).  In 64 bits this took registers from the rest: 95 us for 16384 rows of 4096 with a gain, even
+// out of line.  Blocks outside fp32's middle range are brought there by a power of two first.
 //
 // HBM bound: every input is read once, eight entries to a thread, and stays in registers.
+#include <cuda_fp16.h>
+
 #include "fp8.cuh"
 
 namespace {
@@ -23,196 +27,335 @@ __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// A 64-bit number as fp32 such that rounding that to fewer bits gives what rounding the number itself would: towards zero,
-// and the last bit set where anything was cut off.
-__device__ __forceinline__ float odd_float(double t) {
-    const float f = __double2float_rz(t);
-    return (double)f == t ? f : __uint_as_float(__float_as_uint(f) | 1u);
-}
-
+// Eight entries as they are in memory.
 template <bool BF16>
-__device__ __forceinline__ void load8(const void* X, size_t at, float (&v)[8]) {
-    if (BF16) {
-        const uint4 u = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(X) + at));
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+struct Raw {
+    uint4 u[BF16 ? 1 : 2];
+    __device__ __forceinline__ void load(const void* X, size_t at) {
+        const uint4* p = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(X) + at * (BF16 ? 2 : 4));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(w[i] << 16);
-            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-    } else {
-        const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(X) + at);
-        const float4 a = __ldg(p), b = __ldg(p + 1);
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        for (int i = 0; i < (BF16 ? 1 : 2); ++i) u[i] = __ldg(p + i);
     }
-}
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < (BF16 ? 1 : 2); ++i) u[i] = make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void widen(float (&v)[8]) const {
+        if (BF16) {
+            const uint32_t w[4] = {u[0].x, u[0].y, u[0].z, u[0].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            }
+        } else {
+            const uint4 a = u[0], b = u[BF16 ? 0 : 1];
+            const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+        }
+    }
+};
 
-// Largest |v| as bits: a NaN is above infinity, infinity above every number.
-__device__ __forceinline__ uint32_t abs_bits(const float (&v)[8]) {
-    uint32_t a = 0;
+__device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either is
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+__device__ __forceinline__ float abs_max(const float (&v)[8], float a) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(v[i]) & 0x7fffffffu);
+    for (int i = 0; i < 8; ++i) a = max_nan(a, fabsf(v[i]));
     return a;
 }
-__device__ __forceinline__ double abs_exact(const float (&x)[8], const float (&g)[8]) {
-    double a = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) a = fmax(a, fabs((double)x[i] * (double)g[i]));
-    return a;
+// Values of two codes.
+__device__ __forceinline__ float2 of_e4m3x2(uint32_t c) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((unsigned short)c));
+    return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
-// Codes from fp32 alone; false where an entry lies so near a border that 64 bits have to decide.
-__device__ __forceinline__ bool fast_codes(const float (&v)[8], float a, uint2& codes) {
-    const float r = __fdividef(TOP, a);  // off by 2 units in the last place
-    uint32_t lo[4], hi[4];
+__device__ __forceinline__ bool middle_range(float a) { return a >= TINY && a <= HUGE_; }
+// The power of two that brings a into the middle range (what is lost of entries far below a huge a is no part of their code).
+__device__ __forceinline__ float to_middle(float a) { return a < TINY ? 0x1p100f : a > HUGE_ ? 0x1p-64f : 1.f; }
+
+// Codes of bf16 numbers v and their largest a, in fp32: 448 v has 11 bits, and a quotient so near a border (5 bits) that it is not
+// on it would need 448 v and a times the border, 13 bits at most, to differ by less than they can.  So only quotients on a border
+// have to come out exactly, and one step of refinement, q + (448 v - q a) / a, does that.  (They are frequent: 448 = 7 * 64, and
+// one border in eight is a multiple of 7 * 3.)
+__device__ __forceinline__ void bf16_codes(const float (&v)[8], float a, uint32_t (&c)[4]) {
+    const float s = to_middle(a), n448 = TOP * s, b = a * s, r = __fdividef(1.f, b);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float t0 = v[2 * i] * r, t1 = v[2 * i + 1] * r;
-        constexpr float E = 0x1p-20f;
-        lo[i] = e4m3x2(fmaf(t0, -E, t0), fmaf(t1, -E, t1));
-        hi[i] = e4m3x2(fmaf(t0, E, t0), fmaf(t1, E, t1));
-    }
-    codes = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
-    return lo[0] == hi[0] && lo[1] == hi[1] && lo[2] == hi[2] && lo[3] == hi[3];
-}
-__device__ __forceinline__ uint2 exact_codes(const float (&x)[8], const float (&g)[8], double a) {
-    uint32_t w[4] = {0, 0, 0, 0};
-    if (a > 0) {
+        float q[2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            w[i] = e4m3x2(odd_float((double)x[2 * i] * (double)g[2 * i] * 448.0 / a), odd_float((double)x[2 * i + 1] * (double)g[2 * i + 1] * 448.0 / a));
+        for (int j = 0; j < 2; ++j) {
+            const float n = v[2 * i + j] * n448, first = n * r;
+            q[j] = fmaf(fmaf(-first, b, n), r, first);
+        }
+        c[i] = e4m3x2(q[0], q[1]);
     }
-    return make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
 }
 
-// One token row to a block of threads; thread t has entries 8 t .. 8 t + 7, and those blockDim * 8 further on.  Sixteen
-// neighbouring threads share a block of channels.  NV: how often eight entries to a thread cover the row (0: more than
-// registers are kept for; the row is then read a second time).
+// Codes from fp32 alone, a in the middle range, with the smaller and the larger factor; false where they differ.
+__device__ __forceinline__ bool fast_codes(const float (&v)[8], float a, uint32_t (&lo)[4], uint32_t (&hi)[4]) {
+    const float r = __fdividef(TOP, a), less = r * (1.f - 5 * 0x1p-23f), more = r * (1.f + 5 * 0x1p-23f);
+    uint32_t differ = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        lo[i] = e4m3x2(v[2 * i] * less, v[2 * i + 1] * less);
+        hi[i] = e4m3x2(v[2 * i] * more, v[2 * i + 1] * more);
+        differ |= lo[i] ^ hi[i];
+    }
+    return differ == 0;
+}
+// Which of two codes: |v + rest| * 448 against the border between them times (a + a_rest).
+__device__ __forceinline__ uint32_t decide(uint32_t lo, uint32_t hi, float lo_value, float hi_value, float v, float rest, float a, float a_rest) {
+    const float border = 0.5f * (fabsf(lo_value) + fabsf(hi_value)), t = fabsf(v);
+    rest = v < 0.f ? -rest : rest;
+    const float n = t * TOP, m = border * a;
+    const float low = (fmaf(t, TOP, -n) - fmaf(border, a, -m)) + fmaf(rest, TOP, -border * a_rest);
+    const float over = (n - m) + low;
+    return over > 0.f || (over == 0.f && !(hi & 1u)) ? hi : lo;
+}
+
+// One token row at a time to a block of threads; thread t has entries 8 t .. 8 t + 7, and those blockDim * 8 further on.  Sixteen
+// neighbouring threads share a block of channels.  NV: how often eight entries to a thread cover the row, whose next row is then
+// under way while one is worked on (0: more often than registers are kept for).  The codes do not wait for the row's sum of
+// squares: only the scales need it, at the end (waiting for it first: 94 us for 16384 rows of 4096 with a gain).
 template <bool BF16, bool NORM, int NV>
-__global__ void __launch_bounds__(512) quant_rows_kernel(const void* __restrict__ X, long long stride, const float* __restrict__ gain, float eps, int M,
-                                                         int K, uint8_t* __restrict__ codes, float* __restrict__ scale) {
-    __shared__ double part[16];
-    const int row = blockIdx.x, t = threadIdx.x, span = blockDim.x * 8;
-    const size_t base = (size_t)row * stride;
+__global__ void __launch_bounds__(512, 2) quant_rows_kernel(const void* __restrict__ X, long long stride, const float* __restrict__ gain, float eps, int M,
+                                                         int K, float inv_k, uint8_t* __restrict__ codes, float* __restrict__ scale) {
+    __shared__ double wide_part[16];
+    __shared__ float part[2][16];
+    constexpr int N = NV ? NV : 1;
+    constexpr bool KEEP = NV == 1;
+    const int t = threadIdx.x, lane = t & 31, span = blockDim.x * 8, warps = blockDim.x >> 5;
     const int steps = NV ? NV : (K + span - 1) / span;
-    float x[NV ? NV : 1][8];
-    double size = 1.0;
-    if (NORM) {
-        float sum = 0.f;
+    const long long row_bytes = stride * (BF16 ? 2 : 4);
+    const uint32_t mask = 0xffffu << (t & 16);
+    const char* at = reinterpret_cast<const char*>(X) + blockIdx.x * row_bytes;
+    Raw<BF16> next[N];
+    auto fetch = [&](const char* from, bool on) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            next[i].clear();
+            if (on && i * span + t * 8 < K) next[i].load(from, i * span + t * 8);
+        }
+    };
+    if (NV) fetch(at, true);
+    float gains[KEEP ? N : 1][8];  // of this thread's channels, where they fit
+    if (NORM && KEEP) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            Raw<false> raw;
+            raw.clear();
+            if (i * span + t * 8 < K) raw.load(gain, i * span + t * 8);
+            raw.widen(gains[KEEP ? i : 0]);
+        }
+    }
+    int flip = 0;
+    for (int row = blockIdx.x; row < M; row += gridDim.x, flip ^= 1) {
+        const char* here = at;
+        at += gridDim.x * row_bytes;
+        float sum = 0.f, unit[N];
 #pragma unroll
         for (int i = 0; i < steps; ++i) {
-            float(&v)[8] = x[NV ? i : 0];
             const int k = i * span + t * 8;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = 0.f;
-            if (k < K) load8<BF16>(X, base + k, v);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum = fmaf(v[j], v[j], sum);
-        }
-        double total = sum;
-#pragma unroll
-        for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-        if ((t & 31) == 0) part[t >> 5] = total;
-        __syncthreads();
-        total = 0;
-        for (int i = 0; i < (int)blockDim.x >> 5; ++i) total += part[i];
-        if (!(total > 1e-30 && total < 3e38)) {  // squares outside fp32's range: once more in 64 bits
-            double wide = 0;
-            for (int k = t * 8; k < K; k += span) {
-                float v[8];
-                load8<BF16>(X, base + k, v);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) wide += (double)v[j] * (double)v[j];
+            if (k - t % 16 * 8 >= K) break;  // the same for the sixteen threads of a block of channels
+            float v[8], g[8], p[8];
+            if (NV) {
+                next[NV ? i : 0].widen(v);
+                next[NV ? i : 0].clear();
+                if (row + (int)gridDim.x < M && k < K) next[NV ? i : 0].load(at, k);
+            } else {
+                next[0].clear();
+                if (k < K) next[0].load(here, k);
+                next[0].widen(v);
             }
 #pragma unroll
-            for (int o = 16; o; o >>= 1) wide += __shfl_xor_sync(0xffffffffu, wide, o);
+            for (int j = 0; j < 8; ++j) g[j] = 1.f;
+            if (NORM) {
+                if (KEEP) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) g[j] = gains[KEEP ? i : 0][j];
+                } else if (k < K) {
+                    Raw<false> raw;
+                    raw.load(gain, k);
+                    raw.widen(g);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum = fmaf(v[j], v[j], sum);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) p[j] = NORM ? v[j] * g[j] : v[j];
+            auto largest = [&]() {
+                float a = abs_max(p, 0.f);
+#pragma unroll
+                for (int o = 8; o; o >>= 1) a = max_nan(a, __shfl_xor_sync(mask, a, o));
+                return a;
+            };
+            float a = largest(), up = 1.f;
+            const bool bad = !(a < INFINITY);
+            uint32_t c[4];
+            if (BF16 && !NORM) {
+                bf16_codes(p, a, c);
+            } else {
+                if (!bad && !middle_range(a)) {  // the same for the sixteen threads
+                    up = to_middle(a);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) p[j] = v[j] * up * g[j];
+                    a = largest();
+                }
+                uint32_t hi[4];
+                const bool fine = fast_codes(p, a, c, hi) || !(a > 0.f) || bad;
+                if (NORM ? __any_sync(mask, !fine) : !fine) {
+                    float a_rest = 0.f;
+                    if (NORM) {  // what fp32 leaves of the largest |x g|
+                        a_rest = -INFINITY;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j)
+                            if (fabsf(p[j]) == a) a_rest = fmaxf(a_rest, copysignf(1.f, p[j]) * fmaf(v[j] * up, g[j], -p[j]));
+#pragma unroll
+                        for (int o = 8; o; o >>= 1) a_rest = fmaxf(a_rest, __shfl_xor_sync(mask, a_rest, o));
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (fine || c[q] == hi[q]) continue;
+                        const float2 l = of_e4m3x2(c[q]), h = of_e4m3x2(hi[q]);
+                        const float r0 = NORM ? fmaf(v[2 * q] * up, g[2 * q], -p[2 * q]) : 0.f, r1 = NORM ? fmaf(v[2 * q + 1] * up, g[2 * q + 1], -p[2 * q + 1]) : 0.f;
+                        c[q] = decide(c[q] & 255u, hi[q] & 255u, l.x, h.x, p[2 * q], r0, a, a_rest) |
+                               decide(c[q] >> 8, hi[q] >> 8, l.y, h.y, p[2 * q + 1], r1, a, a_rest) << 8;
+                    }
+                }
+            }
+            if (k < K)
+                *reinterpret_cast<uint2*>(codes + (size_t)row * K + k) =
+                    a > 0.f && !bad ? make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410)) : make_uint2(0, 0);
+            const float u = bad ? __uint_as_float(0x7fc00000u) : up == 1.f ? __fdiv_rn(a, TOP) : a / TOP / up;
+            if (NORM && NV) unit[NV ? i : 0] = u;
+            else if ((t & 15) == 0) scale[(size_t)(k / BLOCK) * M + row] = u;
+        }
+        if (NORM) {
+#pragma unroll
+            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            if (lane == 0) part[flip][t >> 5] = sum;
             __syncthreads();
-            if ((t & 31) == 0) part[t >> 5] = wide;
-            __syncthreads();
-            total = 0;
-            for (int i = 0; i < (int)blockDim.x >> 5; ++i) total += part[i];
+            sum = lane < warps ? part[flip][lane & 15] : 0.f;
+#pragma unroll
+            for (int o = 8; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            sum = __shfl_sync(0xffffffffu, sum, 0);
+            float size = rsqrtf(fmaf(sum, inv_k, eps));
+            if (!(sum > 1e-30f && sum < 3e38f)) {  // squares outside fp32's range: once more in 64 bits (the same for all threads)
+                double wide = 0;
+                for (int k = t * 8; k < K; k += span) {
+                    Raw<BF16> again;
+                    float v[8];
+                    again.load(here, k);
+                    again.widen(v);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) wide += (double)v[j] * (double)v[j];
+                }
+#pragma unroll
+                for (int o = 16; o; o >>= 1) wide += __shfl_xor_sync(0xffffffffu, wide, o);
+                if (lane == 0) wide_part[t >> 5] = wide;
+                __syncthreads();
+                wide = 0;
+                for (int i = 0; i < warps; ++i) wide += wide_part[i];
+                size = (float)rsqrt(wide / K + (double)eps);
+                __syncthreads();
+            }
+            if ((t & 15) == 0) {
+#pragma unroll
+                for (int i = 0; i < steps; ++i) {
+                    const int k = i * span + t * 8;
+                    if (k >= K) break;
+                    float* to = scale + (size_t)(k / BLOCK) * M + row;
+                    *to = (NV ? unit[NV ? i : 0] : *to) * size;
+                }
+            }
         }
-        size = rsqrt(total / K + (double)eps);
-    }
-#pragma unroll
-    for (int i = 0; i < steps; ++i) {
-        float(&v)[8] = x[NV ? i : 0];
-        const int k = i * span + t * 8;
-        if (k - t % 16 * 8 >= K) break;  // the same for the sixteen threads of a block of channels
-        float g[8], p[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) g[j] = 1.f;
-        if (!NORM || !NV) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = 0.f;
-            if (k < K) load8<BF16>(X, base + k, v);
-        }
-        if (NORM && k < K) load8<false>(gain, k, g);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = NORM ? v[j] * g[j] : v[j];
-        const uint32_t mask = 0xffffu << (t & 16);
-        uint32_t bits = abs_bits(p);
-#pragma unroll
-        for (int o = 8; o; o >>= 1) bits = max(bits, __shfl_xor_sync(mask, bits, o));
-        const float a = __uint_as_float(bits);
-        const bool bad = bits >= 0x7f800000u;
-        uint2 c = make_uint2(0, 0);
-        const bool fine = bad || (a >= TINY && a <= HUGE_ && fast_codes(p, a, c));
-        if (__any_sync(mask, !fine)) {
-            double wide = abs_exact(v, g);
-#pragma unroll
-            for (int o = 8; o; o >>= 1) wide = fmax(wide, __shfl_xor_sync(mask, wide, o));
-            if (!fine) c = exact_codes(v, g, wide);
-        }
-        if (bad) c = make_uint2(0, 0);
-        if (k < K) *reinterpret_cast<uint2*>(codes + (size_t)row * K + k) = c;
-        if ((t & 15) == 0)
-            scale[(size_t)(k / BLOCK) * M + row] = bad ? __uint_as_float(0x7fc00000u) : NORM ? (float)((double)a / 448.0 * size) : __fdiv_rn(a, TOP);
     }
 }
 
-// A block of 128 x 128 weights to 256 threads; a thread has eight rows' eight entries.
+// A block of 128 x 128 weights to 512 threads; a thread has eight entries of four rows.
 template <bool BF16>
-__global__ void __launch_bounds__(256) quant_weight_kernel(const void* __restrict__ W, long long stride, int N, int K, int kb, uint8_t* __restrict__ codes,
-                                                           float* __restrict__ scale) {
-    __shared__ uint32_t part[8];
-    const int nb = blockIdx.x / kb, b = blockIdx.x - nb * kb, t = threadIdx.x;
-    const int k = b * BLOCK + t % 16 * 8, n0 = nb * BLOCK + t / 16;
-    float v[8][8];
-    uint32_t bits = 0;
+__global__ void __launch_bounds__(512, 3) quant_weight_kernel(const void* __restrict__ W, long long stride, int N, int K,
+                                                                         uint8_t* __restrict__ codes, float* __restrict__ scale) {
+    __shared__ float part[16];
+    const int t = threadIdx.x, k = blockIdx.x * BLOCK + t % 16 * 8, n0 = blockIdx.y * BLOCK + t / 16;
+    const int rows = k < K ? (N - n0 + 31) / 32 : 0;  // of this thread, if there were no end to the block
+    const char* at = reinterpret_cast<const char*>(W) + ((size_t)n0 * stride + k) * (BF16 ? 2 : 4);
+    const size_t step = (size_t)stride * 32 * (BF16 ? 2 : 4);
+    Raw<BF16> raw[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
+        raw[i].clear();
+        if (i < rows) raw[i].load(at + i * step, 0);
+    }
+    float a = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-        if (k < K && n0 + 16 * i < N) load8<BF16>(W, (size_t)(n0 + 16 * i) * stride + k, v[i]);
+    for (int i = 0; i < 4; ++i) {
+        float v[8];
+        raw[i].widen(v);
+        a = abs_max(v, a);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) bits = max(bits, abs_bits(v[i]));
-    bits = __reduce_max_sync(0xffffffffu, bits);
-    if ((t & 31) == 0) part[t >> 5] = bits;
+    for (int o = 16; o; o >>= 1) a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, o));
+    if ((t & 31) == 0) part[t >> 5] = a;
     __syncthreads();
+    a = part[t & 15];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) bits = max(bits, part[i]);
-    const float a = __uint_as_float(bits);
-    const bool bad = bits >= 0x7f800000u;
-    const float ones[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+    for (int o = 8; o; o >>= 1) a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, o));
+    const bool bad = !(a < INFINITY);
+    uint8_t* to = codes + (size_t)n0 * K + k;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        uint2 c = make_uint2(0, 0);
-        if (!bad && !(a >= TINY && a <= HUGE_ && fast_codes(v[i], a, c))) c = exact_codes(v[i], ones, (double)a);
-        if (k < K && n0 + 16 * i < N) *reinterpret_cast<uint2*>(codes + (size_t)(n0 + 16 * i) * K + k) = c;
+    for (int i = 0; i < 4; ++i) {
+        float v[8];
+        raw[i].widen(v);
+        uint32_t c[4];
+        if (BF16) {
+            bf16_codes(v, a, c);
+        } else {
+            const float up = to_middle(a), b = a * up;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= up;
+            uint32_t hi[4];
+            if (!fast_codes(v, b, c, hi)) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if (c[q] == hi[q]) continue;
+                    const float2 l = of_e4m3x2(c[q]), h = of_e4m3x2(hi[q]);
+                    c[q] = decide(c[q] & 255u, hi[q] & 255u, l.x, h.x, v[2 * q], 0.f, b, 0.f) | decide(c[q] >> 8, hi[q] >> 8, l.y, h.y, v[2 * q + 1], 0.f, b, 0.f) << 8;
+                }
+            }
+        }
+        if (i < rows)
+            *reinterpret_cast<uint2*>(to + (size_t)i * 32 * K) =
+                a > 0.f && !bad ? make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410)) : make_uint2(0, 0);
     }
-    if (t == 0) scale[blockIdx.x] = bad ? __uint_as_float(0x7fc00000u) : __fdiv_rn(a, TOP);
+    if (t == 0) scale[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = bad ? __uint_as_float(0x7fc00000u) : __fdiv_rn(a, TOP);
+}
+
+template <bool BF16, bool NORM, int NV>
+cudaError_t launch_rows(int threads, const void* X, long long stride, const float* gain, float eps, int M, int K, uint8_t* codes, float* scale, cudaStream_t st) {
+    static std::atomic<int> resident[17];  // blocks of 32 .. 512 threads that fit on an SM
+    int n = resident[threads / 32].load(std::memory_order_relaxed);
+    if (n == 0) {
+        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, quant_rows_kernel<BF16, NORM, NV>, threads, 0);
+        if (e != cudaSuccess) return e;
+        resident[threads / 32].store(n, std::memory_order_relaxed);
+    }
+    const long long most = (long long)a48f8::sm_count() * n;
+    quant_rows_kernel<BF16, NORM, NV><<<(unsigned)(M < most ? M : most), threads, 0, st>>>(X, stride, gain, eps, M, K, 1.f / (float)K, codes, scale);
+    return cudaGetLastError();
 }
 
 template <bool BF16, bool NORM>
 cudaError_t launch_rows(const void* X, long long stride, const float* gain, float eps, int M, int K, uint8_t* codes, float* scale, cudaStream_t st) {
-    // threads for eight entries each, at most 256 of them twice or four times: more rows to an SM, more loads under way
-    const int eights = (K + 7) / 8, threads = eights <= 256 ? a48_round_up(eights, 32) : 256, nv = (eights + threads - 1) / threads;
-    if (nv == 1) quant_rows_kernel<BF16, NORM, 1><<<M, threads, 0, st>>>(X, stride, gain, eps, M, K, codes, scale);
-    else if (nv == 2) quant_rows_kernel<BF16, NORM, 2><<<M, threads, 0, st>>>(X, stride, gain, eps, M, K, codes, scale);
-    else if (nv <= 4) quant_rows_kernel<BF16, NORM, 4><<<M, threads, 0, st>>>(X, stride, gain, eps, M, K, codes, scale);
-    else quant_rows_kernel<BF16, NORM, 0><<<M, threads, 0, st>>>(X, stride, gain, eps, M, K, codes, scale);
-    return cudaGetLastError();
+    const int eights = (K + 7) / 8, threads = eights <= 512 ? a48_round_up(eights, 32) : 512, nv = (eights + threads - 1) / threads;
+    if (nv == 1) return launch_rows<BF16, NORM, 1>(threads, X, stride, gain, eps, M, K, codes, scale, st);
+    if (nv == 2) return launch_rows<BF16, NORM, 2>(threads, X, stride, gain, eps, M, K, codes, scale, st);
+    if (nv <= 4) return launch_rows<BF16, NORM, 4>(threads, X, stride, gain, eps, M, K, codes, scale, st);
+    return launch_rows<BF16, NORM, 0>(threads, X, stride, gain, eps, M, K, codes, scale, st);
 }
 
 }  // namespace
@@ -227,10 +370,9 @@ bitnet_a48_status launch_quant_rows(const void* X, int bf16, long long stride, c
 }
 
 bitnet_a48_status launch_quant_weight(const void* W, int bf16, long long stride, int N, int K, uint8_t* codes, float* scale, cudaStream_t st) {
-    const int kb = blocks(K);
-    const unsigned grid = (unsigned)(blocks(N) * kb);
-    if (bf16) quant_weight_kernel<true><<<grid, 256, 0, st>>>(W, stride, N, K, kb, codes, scale);
-    else quant_weight_kernel<false><<<grid, 256, 0, st>>>(W, stride, N, K, kb, codes, scale);
+    const dim3 grid((unsigned)blocks(K), (unsigned)blocks(N));
+    if (bf16) quant_weight_kernel<true><<<grid, 512, 0, st>>>(W, stride, N, K, codes, scale);
+    else quant_weight_kernel<false><<<grid, 512, 0, st>>>(W, stride, N, K, codes, scale);
     A48_CUDA_TRY(cudaGetLastError());
     return BITNET_A48_OK;
 }
