@@ -649,13 +649,14 @@ def quant_fp8(X: torch.Tensor, gain=None, norm_eps: float = 1e-5, codes=None, sc
     if st is None:
         with _made_current(X, stream):
             return quant_fp8(X, gain, norm_eps, codes, scale)
-    (M, K), (stride, bf16), dev = X.shape, _float_rows(X), X.get_device()
+    (M, K), (stride, bf16), dev, device = X.shape, _float_rows(X), X.get_device(), X.device
+    blocks, made = (K + 127) // 128, codes is None and scale is None
     if codes is None:
-        codes = torch.empty(M, K, dtype=torch.float8_e4m3fn, device=X.device)
+        codes = torch.empty(M, K, dtype=torch.float8_e4m3fn, device=device)
     if scale is None:
-        scale = torch.empty((K + 127) // 128, M, dtype=torch.float32, device=X.device)
-    assert codes.shape == (M, K) and scale.shape == ((K + 127) // 128, M)
-    cp, sp = _fp8(codes, scale, dev)
+        scale = torch.empty(blocks, M, dtype=torch.float32, device=device)
+    assert made or (codes.shape == (M, K) and scale.shape == (blocks, M))
+    cp, sp = (codes.data_ptr(), scale.data_ptr()) if made else _fp8(codes, scale, dev)
     _check(lib().bitnet_a48_quant_fp8(X.data_ptr(), stride, bf16, M, K, _gain(gain, K, dev), norm_eps, cp, sp, st), "quant_fp8")
     return codes, scale
 
@@ -689,9 +690,11 @@ def linear_fp8(codes: torch.Tensor, scale: torch.Tensor, w_codes: torch.Tensor, 
     (M, K), N = codes.shape, w_codes.shape[0]
     assert w_codes.shape[1] == K and scale.shape == ((K + 127) // 128, M) and w_scale.shape == ((N + 127) // 128, (K + 127) // 128)
     if Y is None:
-        Y = torch.empty(M, N, dtype=dtype, device=codes.device)
-    assert Y.shape == (M, N) and Y.get_device() == dev
-    stride, bf16 = _float_rows(Y)
+        assert dtype in (torch.float32, torch.bfloat16)
+        Y, stride, bf16 = torch.empty(M, N, dtype=dtype, device=codes.device), N, dtype == torch.bfloat16
+    else:
+        assert Y.shape == (M, N) and Y.get_device() == dev
+        stride, bf16 = _float_rows(Y)
     _check(lib().bitnet_a48_linear_fp8(xp, sp, M, wp, wsp, N, K, Y.data_ptr(), stride, bf16, st), "linear_fp8")
     return Y
 

@@ -38,7 +38,7 @@ struct LogprobArgs {
 struct ScoreArgs {
     const void* tokens;  // int32 or int64 [M]
     int tokens64;
-    float c;  // log2 e / temperature
+    float c, inv_t;  // log2 e / temperature, 1 / temperature
     float* logprob;
     float* entropy;
 };

@@ -129,7 +129,7 @@ bitnet_a48_status bitnet_a48_score(const void* X_dev, long long x_stride, int x_
         const a48f8::LogprobArgs l = {a.y, tokens_dev, logprob_dev, entropy_dev, nullptr, nullptr, nullptr, a.y_stride, M, N, 0, 0, tokens_i64, temperature};
         return a48f8::launch_logprobs(l, (cudaStream_t)stream);
     }
-    const a48f8::ScoreArgs score = {tokens_dev, tokens_i64, (float)(1.4426950408889634 / (double)temperature), logprob_dev, entropy_dev};
+    const a48f8::ScoreArgs score = {tokens_dev, tokens_i64, (float)(1.4426950408889634 / (double)temperature), 1.f / temperature, logprob_dev, entropy_dev};
     a48f8::ScoreParts parts = {reinterpret_cast<float4*>(ws + at.stats), reinterpret_cast<float*>(ws + at.owns), 0};
     s = a48f8::launch_gemm(a, &score, &parts, (cudaStream_t)stream);
     if (s != BITNET_A48_OK) return s;

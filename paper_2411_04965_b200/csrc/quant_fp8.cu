@@ -79,7 +79,7 @@ __device__ __forceinline__ float to_middle(float a) { return a < TINY ? 0x1p100f
 
 // Codes of bf16 numbers v and their largest a, in fp32: 448 v has 11 bits, and a quotient so near a border (5 bits) that it is not
 // on it would need 448 v and a times the border, 13 bits at most, to differ by less than they can.  So only quotients on a border
-// have to come out exactly, and one step of refinement, q + (448 v - q a) / a, does that.  (They are frequent: 448 = 7 * 64, and
+// have to come out exactly, and one step of refinement, q - (q a - 448 v) / a, does that.  (They are frequent: 448 = 7 * 64, and
 // one border in eight is a multiple of 7 * 3.)
 __device__ __forceinline__ void bf16_codes(const float (&v)[8], float a, uint32_t (&c)[4]) {
     const float s = to_middle(a), n448 = TOP * s, b = a * s, r = __fdividef(1.f, b);
@@ -89,7 +89,7 @@ __device__ __forceinline__ void bf16_codes(const float (&v)[8], float a, uint32_
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const float n = v[2 * i + j] * n448, first = n * r;
-            q[j] = fmaf(fmaf(-first, b, n), r, first);
+            q[j] = fmaf(-fmaf(first, b, -n), r, first);  // in this form -0 stays -0
         }
         c[i] = e4m3x2(q[0], q[1]);
     }
@@ -230,9 +230,15 @@ __global__ void __launch_bounds__(512, 2) quant_rows_kernel(const void* __restri
             if (k < K)
                 *reinterpret_cast<uint2*>(codes + (size_t)row * K + k) =
                     a > 0.f && !bad ? make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410)) : make_uint2(0, 0);
-            const float u = bad ? __uint_as_float(0x7fc00000u) : up == 1.f ? __fdiv_rn(a, TOP) : a / TOP / up;
-            if (NORM && NV) unit[NV ? i : 0] = u;
-            else if ((t & 15) == 0) scale[(size_t)(k / BLOCK) * M + row] = u;
+            if (NORM) {
+                // times the row's size at the end; a block that was brought up by 2^100 waits for it as it is, with a minus sign,
+                // for its scale may be a normal number although a / 448 is none
+                const float u = bad ? __uint_as_float(0x7fc00000u) : up > 1.f ? -a / TOP : up < 1.f ? a / TOP / up : a * (1.f / TOP);
+                if (NV) unit[NV ? i : 0] = u;
+                else if ((t & 15) == 0 && k < K) scale[(size_t)(k / BLOCK) * M + row] = u;
+            } else if ((t & 15) == 0) {
+                scale[(size_t)(k / BLOCK) * M + row] = bad ? __uint_as_float(0x7fc00000u) : up == 1.f ? __fdiv_rn(a, TOP) : a / TOP / up;
+            }
         }
         if (NORM) {
 #pragma unroll
@@ -269,7 +275,8 @@ __global__ void __launch_bounds__(512, 2) quant_rows_kernel(const void* __restri
                     const int k = i * span + t * 8;
                     if (k >= K) break;
                     float* to = scale + (size_t)(k / BLOCK) * M + row;
-                    *to = (NV ? unit[NV ? i : 0] : *to) * size;
+                    const float u = NV ? unit[NV ? i : 0] : *to;
+                    *to = fabsf(u) * size * (u < 0.f ? 0x1p-100f : 1.f);
                 }
             }
         }
