@@ -424,7 +424,8 @@ size_t bitnet_a48_ffn_gate_first_workspace_bytes(const bitnet_a48_weight* gate, 
  * channels side by side.  A block of a weight [N, K] is 128 x 128 entries; scales fp32 [ceil(N/128)][ceil(K/128)].  The last
  * blocks may be smaller.  A block of zeros has scale 0; one with an entry that is no finite number has codes 0 and NaN for a scale.
  *
- * K: a multiple of 16, at most 2^20; N and V at most 2^20.  Codes, scales, gains and the inputs of the quantisers are
+ * K: a multiple of 16, at most 2^20; N and V at most 2^20; at least one row and at most 2^30 (BITNET_A48_ERR_SHAPE and _LIMIT
+ * otherwise).  Codes, scales, gains and the inputs of the quantisers are
  * 16-byte aligned, and a quantiser's input rows a multiple of 16 bytes apart; logits and outputs have the alignment of their
  * elements.  Strides are elements from one row to the next and do not count where there is one row.  All calls are
  * asynchronous on `stream`, allocate nothing and can be captured; calls that may overlap must not share a workspace.

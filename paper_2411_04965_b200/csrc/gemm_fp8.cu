@@ -492,7 +492,10 @@ bitnet_a48_status launch_gemm(const LinearArgs& a, const ScoreArgs* score, Score
     }
 }
 
-size_t score_stats(int M, int N) { return (size_t)M * (M <= kMostSingle ? (N + 63) / 64 : 2 * ((N + 255) / 256)); }
+size_t score_stats(int M, int N) {
+    const size_t single = (size_t)(N + 63) / 64, pair = 2 * ((size_t)(N + 255) / 256);
+    return (size_t)M * (M <= kMostSingle ? std::max(single, pair) : pair);
+}
 
 }  // namespace a48f8
 

@@ -7,6 +7,7 @@ namespace {
 
 constexpr int kMaxFeatures = 1 << 20;
 constexpr int kMaxTop = 64;
+constexpr int kMaxRows = 1 << 30;
 
 // Channels of an e4m3 matrix: tensor copies want rows of a multiple of 16 bytes.
 bool channels_ok(int K) { return K > 0 && K <= kMaxFeatures && K % 16 == 0; }
@@ -35,6 +36,7 @@ struct ScoreSpace {
 bitnet_a48_status check_quant(const void* X, int rows, int K, long long stride, int bf16, const void* codes, const void* scale) {
     if (!X || !codes || !scale) return BITNET_A48_ERR_INVALID_ARG;
     if (rows <= 0 || !channels_ok(K)) return BITNET_A48_ERR_SHAPE;
+    if (rows > kMaxRows) return BITNET_A48_ERR_LIMIT;
     if (rows > 1 && stride < K) return BITNET_A48_ERR_SHAPE;
     if (!rows_ok(X, rows > 1 ? stride : K, bf16) || !a48_aligned16(codes) || !a48_aligned16(scale)) return BITNET_A48_ERR_ALIGNMENT;
     return BITNET_A48_OK;
@@ -67,6 +69,7 @@ bitnet_a48_status bitnet_a48_linear_fp8(const uint8_t* codes_dev, const float* s
                                         int N, int K, void* Y_dev, long long y_stride, int y_bf16, void* stream) {
     if (!codes_dev || !scale_dev || !w_codes_dev || !w_scale_dev || !Y_dev) return BITNET_A48_ERR_INVALID_ARG;
     if (M <= 0 || !features_ok(N) || !channels_ok(K)) return BITNET_A48_ERR_SHAPE;
+    if (M > kMaxRows) return BITNET_A48_ERR_LIMIT;
     if (M > 1 && y_stride < N) return BITNET_A48_ERR_SHAPE;
     if (!a48_aligned16(codes_dev) || !a48_aligned16(scale_dev) || !a48_aligned16(w_codes_dev) || !a48_aligned16(w_scale_dev) ||
         (reinterpret_cast<uintptr_t>(Y_dev) & (y_bf16 ? 1u : 3u)))
@@ -84,7 +87,7 @@ bitnet_a48_status bitnet_a48_logprobs(const void* logits_dev, long long stride, 
     if (top > 0 && (!top_ids_dev || !top_logprobs_dev)) return BITNET_A48_ERR_INVALID_ARG;
     if (!logprob_dev && !entropy_dev && !rank_dev && top == 0) return BITNET_A48_ERR_INVALID_ARG;
     if (M <= 0 || V <= 0 || (M > 1 && stride < V) || top > V) return BITNET_A48_ERR_SHAPE;
-    if (V > kMaxFeatures || top > kMaxTop) return BITNET_A48_ERR_LIMIT;
+    if (V > kMaxFeatures || top > kMaxTop || M > kMaxRows) return BITNET_A48_ERR_LIMIT;
     if ((reinterpret_cast<uintptr_t>(logits_dev) & (x_bf16 ? 1u : 3u)) || (reinterpret_cast<uintptr_t>(tokens_dev) & (tokens_i64 ? 7u : 3u)) ||
         (reinterpret_cast<uintptr_t>(logprob_dev) & 3u) || (reinterpret_cast<uintptr_t>(entropy_dev) & 3u) || (reinterpret_cast<uintptr_t>(rank_dev) & 3u) ||
         (reinterpret_cast<uintptr_t>(top_ids_dev) & 3u) || (reinterpret_cast<uintptr_t>(top_logprobs_dev) & 3u))
@@ -96,7 +99,7 @@ bitnet_a48_status bitnet_a48_logprobs(const void* logits_dev, long long stride, 
 }
 
 size_t bitnet_a48_score_workspace_bytes(int M, int N, int K) {
-    if (M <= 0 || !features_ok(N) || !channels_ok(K)) return 0;
+    if (M <= 0 || M > kMaxRows || !features_ok(N) || !channels_ok(K)) return 0;
     return ScoreSpace(M, N, K).end;
 }
 

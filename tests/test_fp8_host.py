@@ -78,7 +78,7 @@ def lib(a48):
 
 
 QUANT = dict(X=p, stride=256, bf16=0, M=4, K=256, gain=p, eps=1e-5, codes=p, scale=p, st=null)
-QUANT_BAD = [(dict(X=null), INVALID), (dict(codes=null), INVALID), (dict(scale=null), INVALID), (dict(M=0), SHAPE), (dict(M=-3), SHAPE),
+QUANT_BAD = [(dict(X=null), INVALID), (dict(codes=null), INVALID), (dict(scale=null), INVALID), (dict(M=0), SHAPE), (dict(M=-3), SHAPE), (dict(M=(1 << 30) + 1), LIMIT),
              (dict(K=0), SHAPE), (dict(K=24), SHAPE), (dict(K=1 << 21), SHAPE), (dict(stride=255), SHAPE), (dict(stride=258), ALIGN),
              (dict(stride=260, bf16=1), ALIGN), (dict(X=odd), ALIGN), (dict(gain=odd), ALIGN), (dict(codes=odd), ALIGN), (dict(scale=odd), ALIGN),
              (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID)]
@@ -102,7 +102,7 @@ LINEAR = dict(x=p, xs=p, M=4, w=p, ws=p, N=100, K=256, Y=p, stride=100, bf16=0, 
 
 
 @pytest.mark.parametrize("change,status", [(dict(x=null), INVALID), (dict(xs=null), INVALID), (dict(w=null), INVALID), (dict(ws=null), INVALID),
-                                           (dict(Y=null), INVALID), (dict(M=0), SHAPE), (dict(N=0), SHAPE), (dict(K=8), SHAPE), (dict(K=130), SHAPE),
+                                           (dict(Y=null), INVALID), (dict(M=0), SHAPE), (dict(M=(1 << 30) + 1), LIMIT), (dict(N=0), SHAPE), (dict(K=8), SHAPE), (dict(K=130), SHAPE),
                                            (dict(N=(1 << 20) + 1), SHAPE), (dict(stride=99), SHAPE), (dict(x=odd), ALIGN), (dict(w=odd), ALIGN),
                                            (dict(Y=P(4098)), ALIGN), (dict(Y=P(4097), bf16=1), ALIGN)])
 def test_linear_refuses(lib, change, status):
@@ -114,7 +114,7 @@ LOGPROBS = dict(x=p, stride=100, bf16=0, M=4, V=100, temperature=1.0, tokens=p, 
 
 @pytest.mark.parametrize("change,status", [(dict(x=null), INVALID), (dict(tokens=null), INVALID), (dict(tokens=null, rank=null), INVALID),
                                            (dict(ids=null), INVALID), (dict(best=null), INVALID), (dict(top=-1), INVALID), (dict(top=101), SHAPE),
-                                           (dict(top=65), LIMIT), (dict(M=0), SHAPE), (dict(V=0, top=0), SHAPE), (dict(stride=99), SHAPE),
+                                           (dict(top=65), LIMIT), (dict(M=0), SHAPE), (dict(M=(1 << 30) + 1), LIMIT), (dict(V=0, top=0), SHAPE), (dict(stride=99), SHAPE),
                                            (dict(V=(1 << 20) + 1, stride=1 << 21), LIMIT), (dict(temperature=0.0), INVALID), (dict(temperature=-1.0), INVALID),
                                            (dict(temperature=float("nan")), INVALID), (dict(temperature=float("inf")), INVALID),
                                            (dict(logprob=null, entropy=null, rank=null, top=0), INVALID), (dict(x=P(4097), bf16=1), ALIGN),
@@ -152,3 +152,6 @@ def test_workspace_sizes(a48):
     M, N, K = 4096, 32000, 4096
     assert M * K < size(M, N, K) < M * K + M * 32 * 4 + M * (250 * 16 + 4) + 4096  # sums of 128 columns instead of logits
     assert size(1 << 20, 32000, 4096) > 1 << 32  # no overflow
+    assert size((1 << 30) + 1, 100, 256) == 0
+    for N in (1, 64, 65, 128, 300):  # whichever tiles the product takes
+        assert size(700, N, 256) >= 700 * (256 + 8 + 4) + 700 * 16 * max(2 * ((N + 255) // 256), (N + 63) // 64)
