@@ -48,10 +48,11 @@ struct Cfg {
     static constexpr bool MOVE_REGISTERS = SUBS == 2;
     static constexpr int CONTROL_REGISTERS = 40, EPI_REGISTERS = 232;
     static_assert(!MOVE_REGISTERS || 128 * CONTROL_REGISTERS + 256 * EPI_REGISTERS <= 384 * 168, "registers of the launch");
+    static_assert(STAGES >= ACC_BUFS / SUBS * GROUP, "a stage comes round no sooner than its products have been read");
     static_assert(SUBN % 32 == 0 && SUBN <= BLOCK, "the columns of an accumulator share a weight scale");
     static_assert(ACC_BUFS % SUBS == 0 && STAGE_BYTES % 1024 == 0, "layout");
     static_assert(SMEM_BYTES <= 227 * 1024, "shared memory");
-    static_assert(8 * (2 * STAGES + 2 * ACC_BUFS) <= 480, "barriers");
+    static_assert(8 * ((1 + SUBS) * STAGES + ACC_BUFS) <= 480, "barriers");
 };
 
 struct Params {
@@ -183,8 +184,11 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
     uint8_t* ctrl = out_all + C::OUT_ALL;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(ctrl + 480);
     volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(ctrl + 484);
-    const uint32_t bar_full = smem_u32(ctrl), bar_empty = bar_full + 8 * STAGES;
-    const uint32_t bar_acc_full = bar_empty + 8 * STAGES, bar_acc_empty = bar_acc_full + 8 * ACC_BUFS;
+    // full: a stage's bytes have landed.  done: the MMAs that read it have completed, and with them a block's products (of the last
+    // accumulator; the one before has a barrier of its own, so that its warps can start): what both the copies and the epilogue
+    // wait for, since a commit costs the thread that issues the MMAs some 300 clocks (with commits of their own for both, a block
+    // took a single CTA 0.39 and 0.50 us instead of 0.28 and 0.43).  acc_empty: an accumulator has been read.
+    const uint32_t bar_full = smem_u32(ctrl), bar_done = bar_full + 8 * STAGES, bar_acc_empty = bar_done + 8 * SUBS * STAGES;
     const uint32_t smem_base = smem_u32(smem);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = PAIR ? (int)(blockIdx.x & 1u) : 0;
@@ -195,12 +199,9 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm_w)) : "memory");
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(bar_full + 8 * s, 1);
-            mbar_init(bar_empty + 8 * s, 1);
+            for (int i = 0; i < SUBS; ++i) mbar_init(bar_done + 8 * (i * STAGES + s), 1);
         }
-        for (int b = 0; b < ACC_BUFS; ++b) {
-            mbar_init(bar_acc_full + 8 * b, 1);
-            mbar_init(bar_acc_empty + 8 * b, C::CTAS * 4);  // one arrival to a warp of the accumulator's warpgroup
-        }
+        for (int b = 0; b < ACC_BUFS; ++b) mbar_init(bar_acc_empty + 8 * b, C::CTAS * 4);  // one arrival to a warp of the accumulator's warpgroup
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -223,7 +224,7 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
                 const int nt = tile / p.m_tiles, mt = tile - nt * p.m_tiles;
                 const int m0 = mt * C::TM + rank * 128, n0 = nt * C::BN + rank * C::SUB_ROWS;
                 for (int b = 0; b < p.kb; ++b, ++it) {
-                    ok = mbar_wait(bar_empty + 8 * s, ph ^ 1, abort_flag, 1, it);
+                    ok = mbar_wait(bar_done + 8 * ((SUBS - 1) * STAGES + s), ph ^ 1, abort_flag, 1, it);
                     if (!ok) break;
                     const uint32_t dst = smem_base + s * C::STAGE_BYTES, bar = full0 + 8 * s;
                     if (rank == 0) mbar_expect_tx(bar_full + 8 * s, (uint32_t)(C::CTAS * (p.x_rows * BLOCK + SUBS * C::SUB_BYTES)));
@@ -271,9 +272,9 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
                         const uint32_t to = tmem_base + (a + i) * C::ACC_COLS + g * SUBN;
 #pragma unroll
                         for (int j = 0; j < 4; ++j) mma_f8<PAIR>(to, a_desc + 2 * j, b_desc + 2 * j, idesc, j > 0);
-                        if (last) tc_commit<PAIR>(bar_acc_full + 8 * (a + i));
-                        if (i == SUBS - 1) tc_commit<PAIR>(bar_empty + 8 * s);
+                        tc_commit<PAIR>(bar_done + 8 * (i * STAGES + s));
                     }
+                    if (!ok) break;
                     if (++s == (uint32_t)STAGES) { s = 0; ph ^= 1; }
                     if (last && (a += SUBS) == (uint32_t)ACC_BUFS) { a = 0; pa ^= 1; }
                 }
@@ -285,9 +286,11 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
         if (C::MOVE_REGISTERS) registers_up<C::EPI_REGISTERS>();
         const int quad = warp & 3, sub = (warp - CONTROL_WARPS) >> 2;
         const uint32_t t_lanes = tmem_base + ((uint32_t)(quad * 32) << 16);
+        const uint32_t bar_mine = bar_done + 8 * sub * STAGES;
         const uint32_t acc_empty0 = PAIR ? map_to_rank(bar_acc_empty, 0) : bar_acc_empty;
         uint8_t* out = out_all + (warp - CONTROL_WARPS) * C::OUT_BUFS * C::OUT_BYTES;
-        uint32_t it = 0, a = sub, pa = 0, stores = 0;
+        uint32_t it = 0, a = sub, stores = 0;
+        uint32_t s = 0, ph = 0;  // stage and phase of the next group's first block
         bool ok = true;
         Sums run;  // SCORE, a single CTA with one tile of tokens: over all tiles of this CTA
         run.start(-INFINITY);
@@ -300,23 +303,30 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
             f32x2 sum[SUBN / 2];
 #pragma unroll
             for (int c = 0; c < SUBN / 2; ++c) sum[c] = 0;
-            // Scales are under way two groups ahead, 32 columns while the 32 before them are multiplied, and whether the next
-            // group's products are there is asked before this group's last columns are.
-            constexpr int GROUP = C::GROUP, CHUNKS = C::ACC_COLS / 32;
+            // Scales are under way two groups ahead, 16 columns while the 16 before them are multiplied, and whether the next
+            // group's products are there is asked before this group's last columns are.  (32 at a time are no faster and leave the
+            // pairs' form too few registers: what the compiler then spills costs 40%.)
+            constexpr int GROUP = C::GROUP, CHUNKS = C::ACC_COLS / 16;
             float x_scale[2][GROUP], w_scale[2][GROUP];
 #pragma unroll
             for (int u = 0; u < 2 * GROUP; ++u) {
                 x_scale[u / GROUP][u % GROUP] = __ldg(xs + (size_t)min(u, p.kb - 1) * p.M);
                 w_scale[u / GROUP][u % GROUP] = __ldg(ws + min(u, p.kb - 1));
             }
-            bool there = mbar_test(bar_acc_full + 8 * a, pa);
+            // the group's last block: its stage, by which both the products are announced and the next group is found
+            auto move_on = [&](int blocks) {
+                s += blocks;
+                if (s >= (uint32_t)STAGES) { s -= STAGES; ph ^= 1; }
+            };
+            move_on(min(GROUP, p.kb) - 1);
+            bool there = mbar_test(bar_mine + 8 * s, ph);
             for (int b0 = 0; b0 < p.kb && ok; b0 += 2 * GROUP) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const int b = b0 + u * GROUP;
                     if (b >= p.kb) break;
                     if (!__all_sync(0xffffffffu, there)) {
-                        ok = __all_sync(0xffffffffu, there || mbar_wait_slow(bar_acc_full + 8 * a, pa, abort_flag, 4, it));
+                        ok = __all_sync(0xffffffffu, there || mbar_wait_slow(bar_mine + 8 * s, ph, abort_flag, 4, it));
                         if (!ok) break;
                     }
                     tc_fence_after();
@@ -328,26 +338,27 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
                         x_scale[u][g] = __ldg(xs + (size_t)ahead * p.M);
                         w_scale[u][g] = __ldg(ws + ahead);
                     }
-                    uint32_t r[2][32];
+                    uint32_t r[2][16];
                     const uint32_t from = t_lanes + a * C::ACC_COLS, done = acc_empty0 + 8 * a;
                     ++it;
-                    if ((a += SUBS) >= (uint32_t)ACC_BUFS) { a = sub; pa ^= 1; }
-                    tmem_ld32(from, r[0]);
+                    if ((a += SUBS) >= (uint32_t)ACC_BUFS) a = sub;
+                    move_on(b + GROUP < p.kb ? min(GROUP, p.kb - b - GROUP) : 1);
+                    tmem_ld16(from, r[0]);
 #pragma unroll
                     for (int c = 0; c < CHUNKS; ++c) {
-                        constexpr int OF_BLOCK = SUBN / 32;
-                        uint32_t(&now)[32] = r[c & 1];
-                        tmem_wait32(now);
-                        if (c + 1 < CHUNKS) tmem_ld32(from + (c + 1) * 32, r[(c + 1) & 1]);
+                        constexpr int OF_BLOCK = SUBN / 16;
+                        uint32_t(&now)[16] = r[c & 1];
+                        tmem_wait16(now);
+                        if (c + 1 < CHUNKS) tmem_ld16(from + (c + 1) * 16, r[(c + 1) & 1]);
                         if (c + 1 == CHUNKS) {
                             tc_fence_before();
                             mbar_arrive_if<PAIR>(done, lane == 0);
-                            there = b + GROUP < p.kb && mbar_test(bar_acc_full + 8 * a, pa);
+                            there = b + GROUP < p.kb && mbar_test(bar_mine + 8 * s, ph);
                         }
                         if (GROUP == 1 || b + c / OF_BLOCK < p.kb) {  // (columns of blocks past the last hold those of an earlier group)
 #pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                scale_add(sum[c % OF_BLOCK * 16 + j], now[2 * j], now[2 * j + 1], scale[c / OF_BLOCK]);
+                            for (int j = 0; j < 8; ++j)
+                                scale_add(sum[c % OF_BLOCK * 8 + j], now[2 * j], now[2 * j + 1], scale[c / OF_BLOCK]);
                         }
                     }
                 }
@@ -470,15 +481,15 @@ int sm_count() {
 }
 
 // Tiles: 128 tokens x 64 or 128 features of one CTA, or 256 x 256 of a pair.  A call takes as long as its rounds of tiles over
-// the SMs times what a block of 128 channels costs a tile: 0.39, 0.50 and 0.62 us (measured from 40 x 4096 x 1536 to 2048 x
-// 11008 x 4096; the model picked the fastest of the three in 15 of 16 of them, e.g. 64 tokens x 32000 x 3200: 37, 29, 35 us,
-// 64 x 4096 x 4096: 16, 19, 23 us, 512 x 32000 x 3200: 132, 91, 76 us).
+// the SMs times what a block of 128 channels costs a tile: 0.28, 0.43 and 0.62 us (measured from 40 x 4096 x 1536 to 1024 x
+// 4096 x 4096; the model picked the fastest of the three in 13 of 14 of them, e.g. 64 tokens x 32000 x 3200: 29, 26, 35 us,
+// 64 x 4096 x 4096: 12, 16, 24 us, 512 x 32000 x 3200: 103, 83, 80 us).
 enum Form { NARROW, WIDE, PAIRED };
 constexpr int kMostSingle = 1024;  // tokens; beyond, the pairs' tiles fill the GPU
 
 Form form_of(int M, int N) {
     const long long sms = sm_count(), m1 = (M + 127) / 128, m2 = (M + 255) / 256;
-    const long long narrow = (m1 * ((N + 63) / 64) + sms - 1) / sms * 39, wide = (m1 * ((N + 127) / 128) + sms - 1) / sms * 50;
+    const long long narrow = (m1 * ((N + 63) / 64) + sms - 1) / sms * 28, wide = (m1 * ((N + 127) / 128) + sms - 1) / sms * 43;
     const long long pair = (m2 * ((N + 255) / 256) + sms / 2 - 1) / (sms / 2) * 62;
     if (M > kMostSingle || (pair <= wide && pair <= narrow)) return PAIRED;
     return wide <= narrow ? WIDE : NARROW;

@@ -18,9 +18,12 @@ namespace {
 
 using a48f8::Sums;
 
-constexpr int CAP = 2048;  // entries of the list
+constexpr int MAX_TOP = 64, SPARE = 32;
 // Threads to a row: many blocks of 256 to an SM, or 1024 where there are fewer rows than SMs.
 constexpr int MANY = 256, FEW = 1024;
+// Entries that a thread may note, and that all of them may.
+__host__ __device__ constexpr int noted_most(int threads) { return threads == MANY ? 12 : 4; }
+__host__ __device__ constexpr int list_most(int threads) { return threads == MANY ? 2048 : 1024; }
 using a48f8::LN2;
 
 struct Args {
@@ -70,7 +73,7 @@ struct Row {
     }
 };
 
-template <bool BF16>
+template <bool BF16, int THREADS>
 struct Walk {
     Row<BF16> row;
     Sums sums;
@@ -78,16 +81,12 @@ struct Walk {
     float own, at_or_above;  // a logit counts as ahead of the token's from there on: `own` before the token, the next number behind it
     float least;           // logits at or above it go to the list
     int token, ahead;      // ahead: logits that come before the token's in the order
-    unsigned long long* list;
-    uint32_t* count;
+    uint2* notes;  // this thread's, THREADS apart: the logit's bits and index
+    int noted;
 
     __device__ __forceinline__ void start(float largest) {
         sums.start(largest);
         far = fmaf(60.f, 1.f / c, sums.r);
-    }
-    __device__ __forceinline__ void note(float x, int id) {
-        const uint32_t at = atomicAdd(count, 1u);
-        if (at < (uint32_t)CAP) list[at] = entry_of(x, id);
     }
     template <int N>
     __device__ __forceinline__ void take(const float (&v)[N], int id) {
@@ -98,16 +97,20 @@ struct Walk {
             sums.move(m, c);
             far = fmaf(60.f, 1.f / c, sums.r);
         }
-        const float mark = id < token ? own : at_or_above;
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            sums.add(v[j], c);
-            ahead += v[j] >= mark;
+        for (int j = 0; j < N; ++j) sums.add(v[j], c);
+        const float mark = id < token ? own : at_or_above;
+        if (m >= mark) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) ahead += v[j] >= mark;
         }
         if (m >= least) {
 #pragma unroll
             for (int j = 0; j < N; ++j)
-                if (v[j] >= least) note(v[j], id + j);
+                if (v[j] >= least) {  // (a list for all threads, with an atomic for each entry, took 158 us for 4096 x 32000, 20 to a row)
+                    if (noted < noted_most(THREADS)) notes[noted * THREADS] = make_uint2(__float_as_uint(v[j]), id + j);
+                    ++noted;
+                }
         }
     }
 };
@@ -133,18 +136,20 @@ template <bool BF16, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_kernel(const Args a) {
     constexpr int E = Row<BF16>::E, WARPS = THREADS / 32;
     constexpr int SAMPLE = (THREADS == MANY ? 32 : 16) / E;  // segments (16 bytes to a thread) kept in registers
+    constexpr int CAP = list_most(THREADS);
     __shared__ unsigned long long list[CAP];
+    __shared__ uint2 notes[noted_most(THREADS) * THREADS];
     __shared__ float best[THREADS];
     __shared__ float4 part[WARPS];
     __shared__ uint32_t hist[256], counts[WARPS];
-    __shared__ uint32_t count, found[2];
+    __shared__ uint32_t count, taken, found[2];
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     const long long r = blockIdx.x;
-    Walk<BF16> w;
+    Walk<BF16, THREADS> w;
     w.row.p = reinterpret_cast<const char*>(a.x) + (size_t)(r * a.stride) * (BF16 ? 2 : 4);
     w.c = a.c;
-    w.list = list;
-    w.count = &count;
+    w.notes = notes + t;
+    w.noted = 0;
     w.ahead = 0;
     w.token = -1;
     w.own = w.at_or_above = w.least = __uint_as_float(0x7fc00000u);  // nothing is above no number
@@ -176,7 +181,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
     float edge_x[1] = {-INFINITY};
     if (edge >= 0) edge_x[0] = w.row.at(edge);
 
-    if (t == 0) count = 0;
+    if (t == 0) count = taken = 0;
     float m = edge_x[0];
 #pragma unroll
     for (int i = 0; i < SAMPLE; ++i) {
@@ -192,15 +197,20 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
         best[t] = m;
         __syncthreads();
         if (warp == 0) {  // the bound: halving the range of orders that holds the k-th largest of the threads' maxima
-            uint32_t key[WARPS], hi = 0;
+            uint32_t key[WARPS], hi = 0, lo = ~0u;
+            int reach = 0;  // maxima at or above lo, k or more
 #pragma unroll
             for (int i = 0; i < WARPS; ++i) {
                 key[i] = order_of(best[i * 32 + lane]);
+                const bool none = key[i] == order_of(-INFINITY);
                 hi = max(hi, key[i]);
+                lo = min(lo, none ? ~0u : key[i]);
+                reach += !none;
             }
             hi = __reduce_max_sync(0xffffffffu, hi);
-            uint32_t lo = order_of(-INFINITY);
-            int reach = THREADS;  // maxima at or above lo, k or more
+            lo = __reduce_min_sync(0xffffffffu, lo);
+            reach = __reduce_add_sync(0xffffffffu, reach);
+            if (reach < a.top) lo = hi = order_of(-INFINITY);
             while (lo < hi && reach > a.top + a.top / 4 + 2) {
                 const uint32_t mid = lo + (hi - lo + 1) / 2;
                 int n = 0;
@@ -260,6 +270,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
     }
     if (t == 0 && w.token >= head && w.token < tail && (w.token - head) % E != 0)  // in the token's own 16 bytes, equal ones from it on do not count
         for (int i = w.token; i < min(tail, head + (w.token - head) / E * E + E); ++i) w.ahead -= w.row.at(i) == w.own;
+    if (w.noted > 0) {  // into one list; more than fit are counted all the same
+        const uint32_t to = atomicAdd(&count, w.noted > noted_most(THREADS) ? CAP + 1 : w.noted);
+        for (int i = 0; i < min(w.noted, noted_most(THREADS)); ++i) {
+            const uint2 e = w.notes[i * THREADS];
+            if (to + i < CAP) list[to + i] = entry_of(__uint_as_float(e.x), (int)e.y);
+        }
+    }
     // ---- joined
     float ref = w.sums.r;
 #pragma unroll
@@ -333,7 +350,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
         if (t == 0) count = 0;
         __syncthreads();
         for (int i = t; i < a.V; i += THREADS)
-            if (w.row.at(i) > bound) w.note(w.row.at(i), i);
+            if (w.row.at(i) > bound) list[atomicAdd(&count, 1u)] = entry_of(w.row.at(i), i);  // fewer than asked for
         __syncthreads();
         n = (int)count;
     }
@@ -350,10 +367,49 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
         n = min(have, a.top);
         __syncthreads();
     }
+    // at most 32 entries beyond those asked for (halving again the range that holds the k-th largest), then their order
+    __shared__ unsigned long long shortlist[MAX_TOP + SPARE];
+    const unsigned long long* from = list;
+    if (n > a.top + SPARE) {
+        if (warp == 0) {
+            uint32_t lo = ~0u, hi = 0;
+            for (int i = lane; i < n; i += 32) {
+                lo = min(lo, (uint32_t)(list[i] >> 32));
+                hi = max(hi, (uint32_t)(list[i] >> 32));
+            }
+            lo = __reduce_min_sync(0xffffffffu, lo);
+            hi = __reduce_max_sync(0xffffffffu, hi);
+            int reach = n;
+            while (lo < hi && reach > a.top + SPARE) {
+                const uint32_t mid = lo + (hi - lo + 1) / 2;
+                int above = 0;
+                for (int i = lane; i < n; i += 32) above += (uint32_t)(list[i] >> 32) >= mid;
+                above = __reduce_add_sync(0xffffffffu, above);
+                if (above >= a.top) {
+                    lo = mid;
+                    reach = above;
+                } else {
+                    hi = mid - 1;
+                }
+            }
+            if (lane == 0) {
+                found[0] = lo;
+                found[1] = (uint32_t)reach;
+            }
+        }
+        __syncthreads();
+        if ((int)found[1] <= a.top + SPARE) {  // (more only where that many logits are equal)
+            for (int i = t; i < n; i += THREADS)
+                if ((uint32_t)(list[i] >> 32) >= found[0]) shortlist[atomicAdd(&taken, 1u)] = list[i];
+            n = (int)found[1];
+            from = shortlist;
+            __syncthreads();
+        }
+    }
     for (int i = t; i < n; i += THREADS) {
-        const unsigned long long mine = list[i];
+        const unsigned long long mine = from[i];
         int place = 0;
-        for (int j = 0; j < n; ++j) place += list[j] > mine;
+        for (int j = 0; j < n; ++j) place += from[j] > mine;
         if (place < a.top) {
             ids[place] = (int)~(uint32_t)mine;
             logps[place] = fmaf(of_order((uint32_t)(mine >> 32)) - all.r, a.inv_t, -LN2 * log_s);
