@@ -21,9 +21,7 @@ using a48f8::Sums;
 constexpr int MAX_TOP = 64, SPARE = 32;
 // Threads to a row: many blocks of 256 to an SM, or 1024 where there are fewer rows than SMs.
 constexpr int MANY = 256, FEW = 1024;
-// Entries that a thread may note, and that all of them may.
-__host__ __device__ constexpr int noted_most(int threads) { return threads == MANY ? 12 : 4; }
-__host__ __device__ constexpr int list_most(int threads) { return threads == MANY ? 2048 : 1024; }
+constexpr int SAMPLED = 32;  // logits of a thread that the bound is made of, of MANY threads; of FEW, half as many
 using a48f8::LN2;
 
 struct Args {
@@ -36,6 +34,7 @@ struct Args {
     float* top_logprobs;
     long long stride;
     int V, top, tokens64;
+    int noted_most, list_most;     // entries that a thread may note, and that all of them may
     int segments, leap, leap_fewer;  // most segments of a row; how far apart those visited one after the other are, for so many and one fewer
     float c, inv_t;  // log2 e / temperature, 1 / temperature
 };
@@ -82,7 +81,7 @@ struct Walk {
     float least;           // logits at or above it go to the list
     int token, ahead;      // ahead: logits that come before the token's in the order
     uint2* notes;  // this thread's, THREADS apart: the logit's bits and index
-    int noted;
+    int noted, noted_most;
 
     __device__ __forceinline__ void start(float largest) {
         sums.start(largest);
@@ -108,7 +107,7 @@ struct Walk {
 #pragma unroll
             for (int j = 0; j < N; ++j)
                 if (v[j] >= least) {  // (a list for all threads, with an atomic for each entry, took 158 us for 4096 x 32000, 20 to a row)
-                    if (noted < noted_most(THREADS)) notes[noted * THREADS] = make_uint2(__float_as_uint(v[j]), id + j);
+                    if (noted < noted_most) notes[noted * THREADS] = make_uint2(__float_as_uint(v[j]), id + j);
                     ++noted;
                 }
         }
@@ -135,10 +134,9 @@ __device__ __forceinline__ int flags_before(bool flag, uint32_t* warp_counts, in
 template <bool BF16, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_kernel(const Args a) {
     constexpr int E = Row<BF16>::E, WARPS = THREADS / 32;
-    constexpr int SAMPLE = (THREADS == MANY ? 32 : 16) / E;  // segments (16 bytes to a thread) kept in registers
-    constexpr int CAP = list_most(THREADS);
-    __shared__ unsigned long long list[CAP];
-    __shared__ uint2 notes[noted_most(THREADS) * THREADS];
+    constexpr int SAMPLE = (THREADS == MANY ? SAMPLED : SAMPLED / 2) / E;  // segments (16 bytes to a thread) kept in registers
+    extern __shared__ unsigned long long list[];  // [list_most], and the threads' notes; not there where nothing is listed
+    uint2* notes = reinterpret_cast<uint2*>(list + a.list_most);
     __shared__ float best[THREADS];
     __shared__ float4 part[WARPS];
     __shared__ uint32_t hist[256], counts[WARPS];
@@ -150,6 +148,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
     w.c = a.c;
     w.notes = notes + t;
     w.noted = 0;
+    w.noted_most = a.noted_most;
     w.ahead = 0;
     w.token = -1;
     w.own = w.at_or_above = w.least = __uint_as_float(0x7fc00000u);  // nothing is above no number
@@ -271,10 +270,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
     if (t == 0 && w.token >= head && w.token < tail && (w.token - head) % E != 0)  // in the token's own 16 bytes, equal ones from it on do not count
         for (int i = w.token; i < min(tail, head + (w.token - head) / E * E + E); ++i) w.ahead -= w.row.at(i) == w.own;
     if (w.noted > 0) {  // into one list; more than fit are counted all the same
-        const uint32_t to = atomicAdd(&count, w.noted > noted_most(THREADS) ? CAP + 1 : w.noted);
-        for (int i = 0; i < min(w.noted, noted_most(THREADS)); ++i) {
+        const uint32_t to = atomicAdd(&count, w.noted > a.noted_most ? a.list_most + 1 : w.noted);
+        for (int i = 0; i < min(w.noted, a.noted_most); ++i) {
             const uint2 e = w.notes[i * THREADS];
-            if (to + i < CAP) list[to + i] = entry_of(__uint_as_float(e.x), (int)e.y);
+            if (to + i < (uint32_t)a.list_most) list[to + i] = entry_of(__uint_as_float(e.x), (int)e.y);
         }
     }
     // ---- joined
@@ -323,7 +322,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
         return;
     }
     int n = (int)count;
-    if (n > CAP) {  // the k-th largest of the row, eight bits at a time
+    if (n > a.list_most) {  // the k-th largest of the row, eight bits at a time
         uint32_t prefix = 0;
         int need = a.top;
         for (int shift = 24; shift >= 0; shift -= 8) {
@@ -417,6 +416,18 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
     }
 }
 
+constexpr int NOTED_MOST = 16, LIST_MOST = 4096;
+
+template <bool BF16, int THREADS>
+bitnet_a48_status launch(const Args& a, int M, cudaStream_t st) {
+    static std::atomic<bool> ready[64];
+    A48_CUDA_TRY(a48_allow_smem(logprobs_kernel<BF16, THREADS>, (LIST_MOST + (size_t)NOTED_MOST * THREADS) * 8, ready));
+    const size_t smem = a.top ? (a.list_most + (size_t)a.noted_most * THREADS) * 8 : 0;
+    logprobs_kernel<BF16, THREADS><<<M, THREADS, smem, st>>>(a);
+    A48_CUDA_TRY(cudaGetLastError());
+    return BITNET_A48_OK;
+}
+
 // A step near 0.618 n that shares no divisor with n, so that n steps visit all of 0 .. n - 1.
 int leap_over(int n) {
     if (n < 3) return 1;
@@ -489,20 +500,18 @@ bitnet_a48_status launch_logprobs(const LogprobArgs& g, cudaStream_t st) {
     a.tokens64 = g.tokens64;
     a.c = (float)(1.4426950408889634 / (double)g.temperature);
     a.inv_t = 1.f / g.temperature;
-    // fewer rows than SMs: more threads to a row (8 rows of 32000: 5.6 us for 9.6)
+    // fewer rows than SMs: more threads to a row (8 rows of 32000: 6.7 us for 8.9, of 128000: 14.6 us for 27.7)
     const int threads = g.M <= sm_count() && g.V >= 8192 ? FEW : MANY, vecs = g.V / (g.x_bf16 ? 8 : 4);
     a.segments = (vecs + threads - 1) / threads;
     a.leap = leap_over(a.segments);
     a.leap_fewer = leap_over(a.segments - 1);
-    if (threads == FEW) {
-        if (g.x_bf16) logprobs_kernel<true, FEW><<<g.M, FEW, 0, st>>>(a);
-        else logprobs_kernel<false, FEW><<<g.M, FEW, 0, st>>>(a);
-    } else {
-        if (g.x_bf16) logprobs_kernel<true, MANY><<<g.M, MANY, 0, st>>>(a);
-        else logprobs_kernel<false, MANY><<<g.M, MANY, 0, st>>>(a);
-    }
-    A48_CUDA_TRY(cudaGetLastError());
-    return BITNET_A48_OK;
+    // Room for what is noted, which is top times row / sample: twice that, and for a thread 6 + 4 times its share (a row with a thread
+    // that has more, or one far beyond these sizes, is only slower).  As little as that, since shared memory is what L1 has not.
+    const double listed = (double)g.top * (1.0 + (double)g.V / (threads == MANY ? SAMPLED * MANY : SAMPLED / 2 * FEW));
+    a.list_most = (int)(listed > (LIST_MOST - 256) / 2 ? LIST_MOST : 256 + 2 * listed);
+    a.noted_most = (int)(4 * listed / threads > NOTED_MOST - 6 ? NOTED_MOST : 6 + 4 * listed / threads);
+    if (threads == FEW) return g.x_bf16 ? launch<true, FEW>(a, g.M, st) : launch<false, FEW>(a, g.M, st);
+    return g.x_bf16 ? launch<true, MANY>(a, g.M, st) : launch<false, MANY>(a, g.M, st);
 }
 
 }  // namespace a48f8
