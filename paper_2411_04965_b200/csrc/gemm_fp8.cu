@@ -5,7 +5,7 @@
 // fresh accumulation (four MMAs of 32 channels) into one of the buffers in tensor memory, and the epilogue warps multiply it by its
 // scale and add it to sums in registers.  Tokens are the rows of the tile (a thread of the epilogue has one token) and
 // output features its columns: a column block of 128 shares ws, so a thread's factor for a block is one number, and a
-// block costs it one packed multiply-add per two features.
+// block costs it one multiply-add per feature.
 #include <algorithm>
 
 #include "fp8.cuh"
@@ -71,32 +71,20 @@ struct Params {
 
 // Sums of the softmax over a thread's columns (the last ones may not exist), and the logit of its row's token.
 template <int COLS>
-__device__ __forceinline__ Sums sums_of(const f32x2 (&sum)[COLS / 2], int cols, float c2, long long token_at, float* own) {
+__device__ __forceinline__ Sums sums_of(const float (&sum)[COLS], int cols, float c2, long long token_at, float* own) {
     Sums s;
     float top = -INFINITY;
 #pragma unroll
-    for (int c = 0; c < COLS; c += 2) {
-        float lo, hi;
-        unpack2(sum[c / 2], lo, hi);
-        if (c < cols) top = fmaxf(top, lo);
-        if (c + 1 < cols) top = fmaxf(top, hi);
-    }
+    for (int c = 0; c < COLS; ++c)
+        if (c < cols) top = fmaxf(top, sum[c]);
     s.start(top);
 #pragma unroll
-    for (int c = 0; c < COLS; c += 2) {
-        float lo, hi;
-        unpack2(sum[c / 2], lo, hi);
-        if (c < cols) s.add(lo, c2);
-        if (c + 1 < cols) s.add(hi, c2);
-    }
+    for (int c = 0; c < COLS; ++c)
+        if (c < cols) s.add(sum[c], c2);
     if (token_at >= 0 && token_at < cols) {
 #pragma unroll
-        for (int c = 0; c < COLS; c += 2) {
-            float lo, hi;
-            unpack2(sum[c / 2], lo, hi);
-            if (token_at == c) *own = lo;
-            if (token_at == c + 1) *own = hi;
-        }
+        for (int c = 0; c < COLS; ++c)
+            if (token_at == c) *own = sum[c];
     }
     return s;
 }
@@ -105,7 +93,7 @@ __device__ __forceinline__ Sums sums_of(const f32x2 (&sum)[COLS / 2], int cols, 
 // exchanged by r % 8, so that neither side has bank conflicts), and from there by tensor stores, or, where y's rows are not
 // 16-byte aligned, a row to an instruction.
 template <int COLS, bool BF16>
-__device__ __forceinline__ void store_rows(const f32x2 (&sum)[COLS / 2], const Params& p, const CUtensorMap* tm_y, uint8_t* out, int m0, int n0, int lane,
+__device__ __forceinline__ void store_rows(const float (&sum)[COLS], const Params& p, const CUtensorMap* tm_y, uint8_t* out, int m0, int n0, int lane,
                                            uint32_t& stores) {
     constexpr int W = BF16 ? 64 : 32;  // columns in 128 bytes
 #pragma unroll
@@ -119,20 +107,13 @@ __device__ __forceinline__ void store_rows(const f32x2 (&sum)[COLS / 2], const P
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
             uint32_t v[4];
-            if (BF16) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float lo, hi;
-                    unpack2(c0 + 8 * q + 2 * j < COLS ? sum[(c0 + 8 * q + 2 * j) / 2 % (COLS / 2)] : 0ull, lo, hi);
-                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v[j]) : "f"(hi), "f"(lo));
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    float lo, hi;
-                    unpack2(sum[(c0 + 4 * q + 2 * j) / 2], lo, hi);
-                    v[2 * j] = __float_as_uint(lo);
-                    v[2 * j + 1] = __float_as_uint(hi);
+            for (int j = 0; j < 4; ++j) {
+                if (BF16) {
+                    const int c = c0 + 8 * q + 2 * j;
+                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v[j]) : "f"(c + 1 < COLS ? sum[(c + 1) % COLS] : 0.f), "f"(c < COLS ? sum[c % COLS] : 0.f));
+                } else {
+                    v[j] = __float_as_uint(sum[(c0 + 4 * q + j) % COLS]);
                 }
             }
             *reinterpret_cast<uint4*>(buf + lane * 128 + ((q ^ (lane & 7)) << 4)) = make_uint4(v[0], v[1], v[2], v[3]);
@@ -162,14 +143,6 @@ __device__ __forceinline__ void store_rows(const f32x2 (&sum)[COLS / 2], const P
             __syncwarp();
         }
     }
-}
-
-// sum += scale * (lo, hi).  (The packed form of the multiply-add took longer, 797 us for 611 in the 7B head's prompt: what
-// comes from tensor memory is not in the register pairs that it wants.)
-__device__ __forceinline__ void scale_add(f32x2& sum, uint32_t lo, uint32_t hi, float scale) {
-    float a, b;
-    unpack2(sum, a, b);
-    sum = pack2(fmaf(__uint_as_float(lo), scale, a), fmaf(__uint_as_float(hi), scale, b));
 }
 
 template <class C, bool SCORE>
@@ -300,9 +273,9 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
             const bool live = m0 < p.M && n0 < p.N;  // the same for the whole warp
             const float* xs = p.xs + min(m, p.M - 1);
             const float* ws = p.ws + (size_t)(min(n0, p.N - 1) / BLOCK) * p.kb;
-            f32x2 sum[SUBN / 2];
+            float sum[SUBN];
 #pragma unroll
-            for (int c = 0; c < SUBN / 2; ++c) sum[c] = 0;
+            for (int c = 0; c < SUBN; ++c) sum[c] = 0.f;
             // Scales are under way two groups ahead, 16 columns while the 16 before them are multiplied, and whether the next
             // group's products are there is asked before this group's last columns are.  (32 at a time are no faster and leave the
             // pairs' form too few registers: what the compiler then spills costs 40%.)
@@ -357,8 +330,10 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
                         }
                         if (GROUP == 1 || b + c / OF_BLOCK < p.kb) {  // (columns of blocks past the last hold those of an earlier group)
 #pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                scale_add(sum[c % OF_BLOCK * 8 + j], now[2 * j], now[2 * j + 1], scale[c / OF_BLOCK]);
+                            for (int j = 0; j < 16; ++j) {  // (two at a time, fma.rn.f32x2, took longer: the pairs of registers have to be made)
+                                float& to = sum[c % OF_BLOCK * 16 + j];
+                                to = fmaf(__uint_as_float(now[j]), scale[c / OF_BLOCK], to);
+                            }
                         }
                     }
                 }

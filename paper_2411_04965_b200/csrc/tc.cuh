@@ -211,20 +211,6 @@ __device__ __forceinline__ void cluster_sync_all() {
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Two fp32 numbers in one register pair.
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 pack2(float a, float b) {
-    f32x2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void unpack2(f32x2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
-    f32x2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-
 // Host: 2-d map of a row-major matrix [rows, cols], boxes of 128 bytes x box_rows with the 128-byte swizzle; what lies past the
 // matrix reads as zero and is not stored.  pitch: bytes from row to row.
 static inline bool make_map(CUtensorMap* map, CUtensorMapDataType type, uint32_t size, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch,

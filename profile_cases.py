@@ -8,6 +8,9 @@
     python profile_cases.py paged_write  --B 4 --T 2048 --kv-heads 8 --bits 4          # prompts of bf16 q, k, v
     python profile_cases.py paged_read   --B 16 --T 2048 --kv-heads 8 --bits 4         # every position, as bf16
     python profile_cases.py paged_attend --B 64 --T 1 --ctx 4095 --kv-heads 8 --bits 4 # T new tokens behind ctx positions
+    python profile_cases.py fp8_quant  --M 8192 --K 4096      # rows through RMSNorm to e4m3 (fp8_weight: N x K weights)
+    python profile_cases.py fp8_linear --M 4096 --N 8192 --K 4096   # product of e4m3 matrices, fp32 (fp8_score: its log probabilities)
+    python profile_cases.py logprobs   --M 2048 --N 32000 --top 20  # log probability, rank, entropy, alternatives of N logits
 
 Each case builds seeded synthetic inputs (the same recipes the benchmark uses),
 runs the kernel `reps` times after one warm-up call and prints the mean time
@@ -92,9 +95,40 @@ def _paged(args, dev, stream):
             "page": args.page, "ms": ms, "bytes": moved, "gbs": moved / ms / 1e6}
 
 
+def _fp8(args, dev, stream):
+    M, N, K = args.M, args.N, args.K
+    gen = torch.Generator(device=dev).manual_seed(31)
+    out = {"case": args.case, "M": M, "N": N, "K": K}
+    if args.case == "logprobs":
+        x = 2 * torch.randn(M, N, generator=gen, device=dev)
+        tokens = torch.randint(0, N, (M,), generator=gen, device=dev)
+        ms = _time(lambda: a48.logprobs(x, tokens, top=args.top), args.reps, stream)
+        return dict(out, top=args.top, ms=ms, gbs=4.0 * M * N / ms / 1e6)
+    if args.case == "fp8_weight":
+        w = (0.02 * torch.randn(N, K, generator=gen, device=dev)).bfloat16()
+        codes, scale = a48.quant_fp8_weight(w)
+        ms = _time(lambda: a48.quant_fp8_weight(w, codes, scale), args.reps, stream)
+        return dict(out, ms=ms, gbs=3.0 * N * K / ms / 1e6)
+    x, gain = synth.gaussian_outlier_activations(M, K, seed=11, device=dev), synth.norm_gains(K, 60, device=dev)
+    codes, scale = a48.quant_fp8(x, gain)
+    if args.case == "fp8_quant":
+        ms = _time(lambda: a48.quant_fp8(x, gain, codes=codes, scale=scale), args.reps, stream)
+        return dict(out, ms=ms, gbs=5.0 * M * K / ms / 1e6)
+    w, w_scale = a48.quant_fp8_weight(0.02 * torch.randn(N, K, generator=gen, device=dev))
+    if args.case == "fp8_linear":
+        y = torch.empty(M, N, device=dev)
+        ms = _time(lambda: a48.linear_fp8(codes, scale, w, w_scale, Y=y), args.reps, stream)
+    else:
+        tokens = torch.randint(0, N, (M,), generator=gen, device=dev)
+        space = torch.empty(a48.score_workspace_bytes(M, N, K), dtype=torch.uint8, device=dev)
+        ms = _time(lambda: a48.score(x, gain, w, w_scale, tokens, workspace=space), args.reps, stream)
+    return dict(out, ms=ms, tflops=2.0 * M * N * K / ms / 1e9, weight_gbs=N * K / ms / 1e6)
+
+
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("case", choices=["gemm", "quant", "decode", "block", "paged_write", "paged_read", "paged_attend"])
+    ap.add_argument("case", choices=["gemm", "quant", "decode", "block", "paged_write", "paged_read", "paged_attend",
+                                     "fp8_quant", "fp8_weight", "fp8_linear", "fp8_score", "logprobs"])
     ap.add_argument("--M", type=int, default=8192)
     ap.add_argument("--N", type=int, default=11008)
     ap.add_argument("--K", type=int, default=4096)
@@ -114,6 +148,7 @@ def main():
     ap.add_argument("--page", type=int, default=64)
     ap.add_argument("--window", type=int, default=0)
     ap.add_argument("--sinks", type=int, default=0)
+    ap.add_argument("--top", type=int, default=1)
     args = ap.parse_args()
     a48_build.build()
     dev = torch.device("cuda:0")
@@ -142,6 +177,8 @@ def main():
                "tokens_per_s": B * T / (ms * 1e-3), "attention_gflop": 4.0 * B * args.heads * (T * T / 2.0) * hd / 1e9}
     elif args.case.startswith("paged"):
         out = _paged(args, dev, stream)
+    elif args.case.startswith("fp8") or args.case == "logprobs":
+        out = _fp8(args, dev, stream)
     elif args.case == "quant":
         x = (synth.student_t3 if args.kind == "topk" else synth.gaussian_outlier_activations)(M, K, 11, device=dev)
         codes = torch.empty(M, K, dtype=torch.int8, device=dev)
