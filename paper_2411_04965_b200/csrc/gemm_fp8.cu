@@ -321,7 +321,8 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
                     for (int c = 0; c < CHUNKS; ++c) {
                         constexpr int OF_BLOCK = SUBN / 16;
                         uint32_t(&now)[16] = r[c & 1];
-                        tmem_wait16(now);
+                        float factor = scale[c / OF_BLOCK];
+                        tmem_wait(factor);
                         if (c + 1 < CHUNKS) tmem_ld16(from + (c + 1) * 16, r[(c + 1) & 1]);
                         if (c + 1 == CHUNKS) {
                             tc_fence_before();
@@ -332,7 +333,7 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
 #pragma unroll
                             for (int j = 0; j < 16; ++j) {  // (two at a time, fma.rn.f32x2, took longer: the pairs of registers have to be made)
                                 float& to = sum[c % OF_BLOCK * 16 + j];
-                                to = fmaf(__uint_as_float(now[j]), scale[c / OF_BLOCK], to);
+                                to = fmaf(__uint_as_float(now[j]), factor, to);
                             }
                         }
                     }

@@ -182,14 +182,9 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
         : "memory");
 }
 
-// Waits for this thread's loads from tensor memory; r is what one of them gives, so that nothing that reads r comes before.
-__device__ __forceinline__ void tmem_wait16(uint32_t (&r)[16]) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
-                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
-                 :
-                 : "memory");
-}
+// Waits for this thread's loads from tensor memory.  What is computed with `factor` afterwards, and so with what was loaded, cannot
+// come before.  (Tying the loaded registers themselves cost a move for each.)
+__device__ __forceinline__ void tmem_wait(float& factor) { asm volatile("tcgen05.wait::ld.sync.aligned;" : "+f"(factor) : : "memory"); }
 
 // Tensor store from shared memory; one thread issues, commits and waits for its own.
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int x, int y, uint32_t src) {
