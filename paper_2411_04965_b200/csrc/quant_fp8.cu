@@ -3,9 +3,9 @@
 //   code = the e4m3 number nearest to 448 v / a, ties to even;   scale = a / 448 (times 1 / rms of the row).
 // The row's size is a factor of the scale alone, so a code does not depend on the rounding of a norm.
 //
-// Codes are those of exact arithmetic.  v * (448 / a) in fp32 is off by at most 2^-21 of itself (2^-22 for the quotient, 2^-24 each
-// for the product with the gain, for a, for the factor and for the product); where it rounds to the same code with a factor 5 * 2^-23
-// smaller and 5 * 2^-23 larger, so does the exact number.  For the others, about one in 10^5, 448 v is compared with a times the
+// Codes are those of exact arithmetic.  v * (448 / a) in fp32 is off by at most 5 * 2^-24 of itself (the product with the gain, a,
+// the quotient, the factor and the product, a rounding each); where it rounds to the same code with a factor 3 * 2^-23 smaller and
+// 3 * 2^-23 larger, so does the exact number.  For the others, about one in 10^5, 448 v is compared with a times the
 // border between the two codes, as sums of two fp32 numbers each (without a gain both are exact in that form, and with one where
 // the products fit into 47 bits).  In 64 bits this took registers from the rest: 95 us for 16384 rows of 4096 with a gain, even
 // out of line.  Blocks outside fp32's middle range are brought there by a power of two first.
@@ -97,7 +97,8 @@ __device__ __forceinline__ void bf16_codes(const float (&v)[8], float a, uint32_
 
 // Codes from fp32 alone, a in the middle range, with the smaller and the larger factor; false where they differ.
 __device__ __forceinline__ bool fast_codes(const float (&v)[8], float a, uint32_t (&lo)[4], uint32_t (&hi)[4]) {
-    const float r = __fdividef(TOP, a), less = r * (1.f - 5 * 0x1p-23f), more = r * (1.f + 5 * 0x1p-23f);
+    const float i = __fdividef(1.f, a), first = TOP * i, r = fmaf(fmaf(-first, a, TOP), i, first);  // a step of refinement: 2^-24
+    const float less = r * (1.f - 3 * 0x1p-23f), more = r * (1.f + 3 * 0x1p-23f);
     uint32_t differ = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -120,28 +121,30 @@ __device__ __forceinline__ uint32_t decide(uint32_t lo, uint32_t hi, float lo_va
 // One token row at a time to a block of threads; thread t has entries 8 t .. 8 t + 7, and those blockDim * 8 further on.  Sixteen
 // neighbouring threads share a block of channels.  NV: how often eight entries to a thread cover the row, whose next row is then
 // under way while one is worked on (0: more often than registers are kept for).  The codes do not wait for the row's sum of
-// squares: only the scales need it, at the end (waiting for it first: 94 us for 16384 rows of 4096 with a gain).
+// squares: only the scales need it, at the end, and those of `batch` rows together, so that warps wait for one another once for
+// several rows.  16384 rows of 4096 fp32 with a gain: first the sum, then the codes 94 us, row by row 88, four rows 82 (bf16: 82
+// and 76).
+constexpr int BATCH_MOST = 4;
+
 template <bool BF16, bool NORM, int NV>
 __global__ void __launch_bounds__(512, 2) quant_rows_kernel(const void* __restrict__ X, long long stride, const float* __restrict__ gain, float eps, int M,
-                                                         int K, float inv_k, uint8_t* __restrict__ codes, float* __restrict__ scale) {
-    __shared__ double wide_part[16];
-    __shared__ float part[2][16];
+                                                         int K, int batch, float inv_k, uint8_t* __restrict__ codes, float* __restrict__ scale) {
+    __shared__ float part[2][BATCH_MOST][16], units[2][BATCH_MOST][32 * (NV ? NV : 1)];
     constexpr int N = NV ? NV : 1;
     constexpr bool KEEP = NV == 1;
     const int t = threadIdx.x, lane = t & 31, span = blockDim.x * 8, warps = blockDim.x >> 5;
     const int steps = NV ? NV : (K + span - 1) / span;
     const long long row_bytes = stride * (BF16 ? 2 : 4);
     const uint32_t mask = 0xffffu << (t & 16);
-    const char* at = reinterpret_cast<const char*>(X) + blockIdx.x * row_bytes;
+    const char* at = reinterpret_cast<const char*>(X) + (long long)blockIdx.x * batch * row_bytes;
     Raw<BF16> next[N];
-    auto fetch = [&](const char* from, bool on) {
+    if (NV) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             next[i].clear();
-            if (on && i * span + t * 8 < K) next[i].load(from, i * span + t * 8);
+            if (i * span + t * 8 < K) next[i].load(at, i * span + t * 8);
         }
-    };
-    if (NV) fetch(at, true);
+    }
     float gains[KEEP ? N : 1][8];  // of this thread's channels, where they fit
     if (NORM && KEEP) {
 #pragma unroll
@@ -153,132 +156,126 @@ __global__ void __launch_bounds__(512, 2) quant_rows_kernel(const void* __restri
         }
     }
     int flip = 0;
-    for (int row = blockIdx.x; row < M; row += gridDim.x, flip ^= 1) {
-        const char* here = at;
-        at += gridDim.x * row_bytes;
-        float sum = 0.f, unit[N];
+    for (int row0 = blockIdx.x * batch; row0 < M; row0 += batch * (int)gridDim.x, flip ^= 1) {
+#pragma unroll 1
+        for (int row = row0; row < min(M, row0 + batch); ++row) {
+            const char* here = at;
+            const bool ends = row + 1 == row0 + batch, more = (ends ? row0 + batch * (int)gridDim.x : row + 1) < M;
+            at += (ends ? (long long)batch * ((int)gridDim.x - 1) + 1 : 1) * row_bytes;
+            float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < steps; ++i) {
-            const int k = i * span + t * 8;
-            if (k - t % 16 * 8 >= K) break;  // the same for the sixteen threads of a block of channels
-            float v[8], g[8], p[8];
-            if (NV) {
-                next[NV ? i : 0].widen(v);
-                next[NV ? i : 0].clear();
-                if (row + (int)gridDim.x < M && k < K) next[NV ? i : 0].load(at, k);
-            } else {
-                next[0].clear();
-                if (k < K) next[0].load(here, k);
-                next[0].widen(v);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) g[j] = 1.f;
-            if (NORM) {
-                if (KEEP) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) g[j] = gains[KEEP ? i : 0][j];
-                } else if (k < K) {
-                    Raw<false> raw;
-                    raw.load(gain, k);
-                    raw.widen(g);
+            for (int i = 0; i < steps; ++i) {
+                const int k = i * span + t * 8;
+                if (k - t % 16 * 8 >= K) break;  // the same for the sixteen threads of a block of channels
+                float v[8], g[8], p[8];
+                if (NV) {
+                    next[NV ? i : 0].widen(v);
+                    next[NV ? i : 0].clear();
+                    if (more && k < K) next[NV ? i : 0].load(at, k);
+                } else {
+                    next[0].clear();
+                    if (k < K) next[0].load(here, k);
+                    next[0].widen(v);
                 }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sum = fmaf(v[j], v[j], sum);
-            }
+                for (int j = 0; j < 8; ++j) g[j] = 1.f;
+                if (NORM) {
+                    if (KEEP) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] = NORM ? v[j] * g[j] : v[j];
-            auto largest = [&]() {
-                float a = abs_max(p, 0.f);
-#pragma unroll
-                for (int o = 8; o; o >>= 1) a = max_nan(a, __shfl_xor_sync(mask, a, o));
-                return a;
-            };
-            float a = largest(), up = 1.f;
-            const bool bad = !(a < INFINITY);
-            uint32_t c[4];
-            if (BF16 && !NORM) {
-                bf16_codes(p, a, c);
-            } else {
-                if (!bad && !middle_range(a)) {  // the same for the sixteen threads
-                    up = to_middle(a);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) p[j] = v[j] * up * g[j];
-                    a = largest();
-                }
-                uint32_t hi[4];
-                const bool fine = fast_codes(p, a, c, hi) || !(a > 0.f) || bad;
-                if (NORM ? __any_sync(mask, !fine) : !fine) {
-                    float a_rest = 0.f;
-                    if (NORM) {  // what fp32 leaves of the largest |x g|
-                        a_rest = -INFINITY;
-#pragma unroll
-                        for (int j = 0; j < 8; ++j)
-                            if (fabsf(p[j]) == a) a_rest = fmaxf(a_rest, copysignf(1.f, p[j]) * fmaf(v[j] * up, g[j], -p[j]));
-#pragma unroll
-                        for (int o = 8; o; o >>= 1) a_rest = fmaxf(a_rest, __shfl_xor_sync(mask, a_rest, o));
+                        for (int j = 0; j < 8; ++j) g[j] = gains[KEEP ? i : 0][j];
+                    } else if (k < K) {
+                        Raw<false> raw;
+                        raw.load(gain, k);
+                        raw.widen(g);
                     }
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        if (fine || c[q] == hi[q]) continue;
-                        const float2 l = of_e4m3x2(c[q]), h = of_e4m3x2(hi[q]);
-                        const float r0 = NORM ? fmaf(v[2 * q] * up, g[2 * q], -p[2 * q]) : 0.f, r1 = NORM ? fmaf(v[2 * q + 1] * up, g[2 * q + 1], -p[2 * q + 1]) : 0.f;
-                        c[q] = decide(c[q] & 255u, hi[q] & 255u, l.x, h.x, p[2 * q], r0, a, a_rest) |
-                               decide(c[q] >> 8, hi[q] >> 8, l.y, h.y, p[2 * q + 1], r1, a, a_rest) << 8;
+                    for (int j = 0; j < 8; ++j) sum = fmaf(v[j], v[j], sum);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) p[j] = NORM ? v[j] * g[j] : v[j];
+                auto largest = [&]() {
+                    float a = abs_max(p, 0.f);
+#pragma unroll
+                    for (int o = 8; o; o >>= 1) a = max_nan(a, __shfl_xor_sync(mask, a, o));
+                    return a;
+                };
+                float a = largest(), up = 1.f;
+                const bool bad = !(a < INFINITY);
+                uint32_t c[4];
+                if (BF16 && !NORM) {
+                    bf16_codes(p, a, c);
+                } else {
+                    if (!bad && !middle_range(a)) {  // the same for the sixteen threads
+                        up = to_middle(a);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) p[j] = v[j] * up * g[j];
+                        a = largest();
+                    }
+                    uint32_t hi[4];
+                    const bool fine = fast_codes(p, a, c, hi) || !(a > 0.f) || bad;
+                    if (NORM ? __any_sync(mask, !fine) : !fine) {
+                        float a_rest = 0.f;
+                        if (NORM) {  // what fp32 leaves of the largest |x g|
+                            a_rest = -INFINITY;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                if (fabsf(p[j]) == a) a_rest = fmaxf(a_rest, copysignf(1.f, p[j]) * fmaf(v[j] * up, g[j], -p[j]));
+#pragma unroll
+                            for (int o = 8; o; o >>= 1) a_rest = fmaxf(a_rest, __shfl_xor_sync(mask, a_rest, o));
+                        }
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            if (fine || c[q] == hi[q]) continue;
+                            const float2 l = of_e4m3x2(c[q]), h = of_e4m3x2(hi[q]);
+                            const float r0 = NORM ? fmaf(v[2 * q] * up, g[2 * q], -p[2 * q]) : 0.f, r1 = NORM ? fmaf(v[2 * q + 1] * up, g[2 * q + 1], -p[2 * q + 1]) : 0.f;
+                            c[q] = decide(c[q] & 255u, hi[q] & 255u, l.x, h.x, p[2 * q], r0, a, a_rest) |
+                                   decide(c[q] >> 8, hi[q] >> 8, l.y, h.y, p[2 * q + 1], r1, a, a_rest) << 8;
+                        }
                     }
                 }
+                if (k < K)
+                    *reinterpret_cast<uint2*>(codes + (size_t)row * K + k) =
+                        a > 0.f && !bad ? make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410)) : make_uint2(0, 0);
+                if (NORM) {
+                    // times the row's size at the end; a block that was brought up by 2^100 waits for it as it is, with a minus sign,
+                    // for its scale may be a normal number although a / 448 is none
+                    const float u = bad ? __uint_as_float(0x7fc00000u) : up > 1.f ? -a / TOP : up < 1.f ? a / TOP / up : a * (1.f / TOP);
+                    if (NV && (t & 15) == 0) units[flip][row - row0][k / BLOCK] = u;
+                    else if ((t & 15) == 0 && k < K) scale[(size_t)(k / BLOCK) * M + row] = u;
+                } else if ((t & 15) == 0) {
+                    scale[(size_t)(k / BLOCK) * M + row] = bad ? __uint_as_float(0x7fc00000u) : up == 1.f ? __fdiv_rn(a, TOP) : a / TOP / up;
+                }
             }
-            if (k < K)
-                *reinterpret_cast<uint2*>(codes + (size_t)row * K + k) =
-                    a > 0.f && !bad ? make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410)) : make_uint2(0, 0);
             if (NORM) {
-                // times the row's size at the end; a block that was brought up by 2^100 waits for it as it is, with a minus sign,
-                // for its scale may be a normal number although a / 448 is none
-                const float u = bad ? __uint_as_float(0x7fc00000u) : up > 1.f ? -a / TOP : up < 1.f ? a / TOP / up : a * (1.f / TOP);
-                if (NV) unit[NV ? i : 0] = u;
-                else if ((t & 15) == 0 && k < K) scale[(size_t)(k / BLOCK) * M + row] = u;
-            } else if ((t & 15) == 0) {
-                scale[(size_t)(k / BLOCK) * M + row] = bad ? __uint_as_float(0x7fc00000u) : up == 1.f ? __fdiv_rn(a, TOP) : a / TOP / up;
+#pragma unroll
+                for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                if (lane == 0) part[flip][row - row0][t >> 5] = sum;
             }
         }
-        if (NORM) {
-#pragma unroll
-            for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            if (lane == 0) part[flip][t >> 5] = sum;
-            __syncthreads();
-            sum = lane < warps ? part[flip][lane & 15] : 0.f;
-#pragma unroll
-            for (int o = 8; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            sum = __shfl_sync(0xffffffffu, sum, 0);
+        if (!NORM) continue;
+        __syncthreads();
+        const int blocks = (K + BLOCK - 1) / BLOCK;
+        for (int j = t; j < batch * blocks; j += blockDim.x) {
+            const int b = j / batch, q = j - b * batch, row = row0 + q;
+            if (row >= M) continue;
+            float sum = 0.f;
+            for (int i = 0; i < warps; ++i) sum += part[flip][q][i];
             float size = rsqrtf(fmaf(sum, inv_k, eps));
-            if (!(sum > 1e-30f && sum < 3e38f)) {  // squares outside fp32's range: once more in 64 bits (the same for all threads)
+            if (!(sum > 1e-30f && sum < 3e38f)) {  // squares outside fp32's range: once more in 64 bits
                 double wide = 0;
-                for (int k = t * 8; k < K; k += span) {
+                for (int k = 0; k < K; k += 8) {
                     Raw<BF16> again;
                     float v[8];
-                    again.load(here, k);
+                    again.load(reinterpret_cast<const char*>(X) + row * row_bytes, k);
                     again.widen(v);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) wide += (double)v[j] * (double)v[j];
+                    for (int i = 0; i < 8; ++i) wide += (double)v[i] * (double)v[i];
                 }
-#pragma unroll
-                for (int o = 16; o; o >>= 1) wide += __shfl_xor_sync(0xffffffffu, wide, o);
-                if (lane == 0) wide_part[t >> 5] = wide;
-                __syncthreads();
-                wide = 0;
-                for (int i = 0; i < warps; ++i) wide += wide_part[i];
                 size = (float)rsqrt(wide / K + (double)eps);
-                __syncthreads();
             }
-            if ((t & 15) == 0) {
-#pragma unroll
-                for (int i = 0; i < steps; ++i) {
-                    const int k = i * span + t * 8;
-                    if (k >= K) break;
-                    float* to = scale + (size_t)(k / BLOCK) * M + row;
-                    const float u = NV ? unit[NV ? i : 0] : *to;
-                    *to = fabsf(u) * size * (u < 0.f ? 0x1p-100f : 1.f);
-                }
-            }
+            float* to = scale + (size_t)b * M + row;
+            const float u = NV ? units[flip][q][NV ? b : 0] : *to;
+            *to = fabsf(u) * size * (u < 0.f ? 0x1p-100f : 1.f);
         }
     }
 }
@@ -351,8 +348,10 @@ cudaError_t launch_rows(int threads, const void* X, long long stride, const floa
         if (e != cudaSuccess) return e;
         resident[threads / 32].store(n, std::memory_order_relaxed);
     }
-    const long long most = (long long)a48f8::sm_count() * n;
-    quant_rows_kernel<BF16, NORM, NV><<<(unsigned)(M < most ? M : most), threads, 0, st>>>(X, stride, gain, eps, M, K, 1.f / (float)K, codes, scale);
+    // four rows at a time only where that leaves none of the blocks idle: fewer rows end sooner one by one
+    const int most = a48f8::sm_count() * n, batch = NORM && NV && M >= BATCH_MOST * most ? BATCH_MOST : 1;
+    const int batches = (M - 1) / batch + 1;
+    quant_rows_kernel<BF16, NORM, NV><<<batches < most ? batches : most, threads, 0, st>>>(X, stride, gain, eps, M, K, batch, 1.f / (float)K, codes, scale);
     return cudaGetLastError();
 }
 

@@ -46,6 +46,23 @@ def test_quant_rows(a48, cuda_dev, M, K, norm, x):
 
 
 @pytest.mark.parametrize("x", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,K", [(19003, 256), (19001, 272), (4802, 2048), (2403, 4096), (2401, 8208), (2402, 11008)])
+def test_quant_many_rows_are_what_few_are(a48, cuda_dev, M, K, x):
+    torch.manual_seed(M)
+    h = torch.randn(M, K, device=cuda_dev) * torch.logspace(-12, 12, M, device=cuda_dev)[torch.randperm(M, device=cuda_dev), None]
+    h = h.bfloat16() if x == "bf16" else h
+    h[M // 2] = 0
+    h[-1] = 1e-25  # its squares are none in fp32
+    h[-2, K // 2] = float("nan")
+    gain = torch.rand(K, device=cuda_dev) + 0.5
+    codes, scale = a48.quant_fp8(h, gain)
+    for first in range(0, M, 113):
+        rows = slice(first, min(M, first + 113))
+        c, s = a48.quant_fp8(h[rows], gain)
+        assert torch.equal(c.view(torch.uint8), codes[rows].view(torch.uint8)) and torch.equal(s.view(torch.int32), scale[:, rows].contiguous().view(torch.int32))
+
+
+@pytest.mark.parametrize("x", ["fp32", "bf16"])
 @pytest.mark.parametrize("norm", [False, True])
 def test_quant_ties_go_to_the_even_code(a48, cuda_dev, x, norm):
     """The largest entry is 448, 1.75 and 21 / 16 times powers of two, so that entries halfway between two codes are exact."""
