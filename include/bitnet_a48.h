@@ -425,15 +425,14 @@ size_t bitnet_a48_ffn_gate_first_workspace_bytes(const bitnet_a48_weight* gate, 
  * blocks may be smaller.  A block of zeros has scale 0; one with an entry that is no finite number has codes 0 and NaN for a scale.
  *
  * K: a multiple of 16, at most 2^20; N and V at most 2^20; at least one row and at most 2^30 (BITNET_A48_ERR_SHAPE and _LIMIT
- * otherwise).  Codes, scales, gains and the inputs of the quantisers are
- * 16-byte aligned, and a quantiser's input rows a multiple of 16 bytes apart; logits and outputs have the alignment of their
- * elements.  Strides are elements from one row to the next and do not count where there is one row.  All calls are
+ * otherwise).  Codes, scales, gains and the inputs of the quantisers are 16-byte aligned, and a quantiser's input rows a multiple
+ * of 16 bytes apart; logits and outputs have the alignment of their elements.  Strides are elements from one row to the next and do not count where there is one row.  All calls are
  * asynchronous on `stream`, allocate nothing and can be captured; calls that may overlap must not share a workspace.
  */
 
 /* Token rows X_dev [M, K] (fp32, or bf16 with x_bf16 != 0) to codes_dev [M, K] and scale_dev.  gain_dev: NULL, or fp32 [K]:
- * the rows go through RMSNorm first, v = x * gain, and the scales are a / 448 / sqrt(mean(x^2) + norm_eps).  (Products
- * x * gain past the range of fp32 count as infinite.) */
+ * the rows go through RMSNorm first, v = x * gain, and the scales are a / 448 / sqrt(mean(x^2) + norm_eps): 0 for a row of
+ * zeros with any norm_eps >= 0, NaN for all of a row with a NaN.  (Products x * gain past the range of fp32 count as infinite.) */
 bitnet_a48_status bitnet_a48_quant_fp8(const void* X_dev, long long x_stride, int x_bf16, int M, int K, const float* gain_dev,
                                        float norm_eps, uint8_t* codes_dev, float* scale_dev, void* stream);
 /* A weight W_dev [N, K] to codes_dev [N, K] and scale_dev. */

@@ -14,13 +14,15 @@
 #include <cuda_fp16.h>
 
 #include "fp8.cuh"
+#include "softmax_sums.cuh"
 
 namespace {
 
 using a48f8::BLOCK;
+using a48f8::max_nan;
 
 constexpr float TOP = 448.f;
-constexpr float TINY = 1e-30f, HUGE_ = 1e37f;  // a block outside, where fp32 products or quotients may leave the normal range, is done in 64 bits
+constexpr float TINY = 1e-30f, HUGE_ = 1e37f;  // outside, fp32 products or quotients may leave the normal range
 
 __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
     unsigned short r;
@@ -57,11 +59,6 @@ struct Raw {
     }
 };
 
-__device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either is
-    float y;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-    return y;
-}
 __device__ __forceinline__ float abs_max(const float (&v)[8], float a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) a = max_nan(a, fabsf(v[i]));
@@ -260,8 +257,13 @@ __global__ void __launch_bounds__(512, 2) quant_rows_kernel(const void* __restri
             if (row >= M) continue;
             float sum = 0.f;
             for (int i = 0; i < warps; ++i) sum += part[flip][q][i];
-            float size = rsqrtf(fmaf(sum, inv_k, eps));
-            if (!(sum > 1e-30f && sum < 3e38f)) {  // squares outside fp32's range: once more in 64 bits
+            float* to = scale + (size_t)b * M + row;
+            const float mean = fmaf(sum, inv_k, eps), u = NV ? units[flip][q][NV ? b : 0] : *to;
+            if (u == 0.f && sum == 0.f) {  // whatever eps is
+                *to = 0.f;
+            } else if (mean > 1e-30f && sum < 3e38f) {  // (what squares below fp32's range lose of it is 2^-149)
+                *to = fabsf(u) * rsqrtf(mean) * (u < 0.f ? 0x1p-100f : 1.f);
+            } else {  // squares outside the range: once more in 64 bits
                 double wide = 0;
                 for (int k = 0; k < K; k += 8) {
                     Raw<BF16> again;
@@ -271,11 +273,8 @@ __global__ void __launch_bounds__(512, 2) quant_rows_kernel(const void* __restri
 #pragma unroll
                     for (int i = 0; i < 8; ++i) wide += (double)v[i] * (double)v[i];
                 }
-                size = (float)rsqrt(wide / K + (double)eps);
+                *to = (float)(fabs((double)u) * (u < 0.f ? 0x1p-100 : 1.0) * rsqrt(wide / K + (double)eps));
             }
-            float* to = scale + (size_t)b * M + row;
-            const float u = NV ? units[flip][q][NV ? b : 0] : *to;
-            *to = fabsf(u) * size * (u < 0.f ? 0x1p-100f : 1.f);
         }
     }
 }

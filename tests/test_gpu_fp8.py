@@ -129,6 +129,40 @@ def test_quant_extremes(a48, cuda_dev, x, norm):
     assert np.all(np.abs(scale - want_scale)[fine] <= (norm_tol(384) * np.abs(want_scale) + 2.0 ** -148)[fine])
 
 
+@pytest.mark.parametrize("x", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,K", [(6, 384), (3, 20000)])
+def test_quant_with_nothing_added_to_the_mean(a48, cuda_dev, M, K, x):
+    v = np.random.default_rng(K).standard_normal((M, K)).astype(np.float32)
+    v[0] = 0
+    v[1] *= np.float32(1e-25)
+    v[2] = np.where(np.arange(K) % 3, 2.0 ** -133, 0)
+    t, gain = torch.tensor(v).to(DT[x]), torch.linspace(0.5, 2.0, K)
+    codes, scale = a48.quant_fp8(t.to(cuda_dev), gain.to(cuda_dev), 0.0)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        want, want_scale = fp8.quant_rows(t.double().numpy(), gain.double().numpy(), 0.0)
+    want_scale[:, 0] = 0
+    assert np.array_equal(bits(codes), want)
+    check_scale(scale, want_scale, norm_tol(K))
+
+
+def test_rows_past_two_to_the_31_entries(a48, cuda_dev):
+    M, N, few = 70001, 32000, 2000
+    torch.manual_seed(1)
+    wc, ws = a48.quant_fp8_weight(torch.randn(N, 16, device=cuda_dev))
+    h = torch.randn(M, 16, device=cuda_dev)
+    end = slice(M - few, M)
+    for dtype in (torch.float32, torch.bfloat16):
+        y = a48.linear_fp8(*a48.quant_fp8(h), wc, ws, dtype=dtype)
+        assert torch.equal(y[end], a48.linear_fp8(*a48.quant_fp8(h[end]), wc, ws, dtype=dtype))
+        tokens = torch.randint(N, (M,), device=cuda_dev)
+        for all_of, of_end in zip(a48.logprobs(y, tokens, top=2), a48.logprobs(y[end], tokens[end], top=2)):
+            assert torch.equal(all_of[end], of_end)
+        codes, scale = a48.quant_fp8(y, torch.ones(N, device=cuda_dev))
+        c, s = a48.quant_fp8(y[end], torch.ones(N, device=cuda_dev))
+        assert torch.equal(codes[end].view(torch.uint8), c.view(torch.uint8)) and torch.equal(scale[:, end].contiguous(), s)
+        del y, codes
+
+
 def test_quant_rows_may_be_strided_and_outputs_given(a48, cuda_dev):
     wide = torch.randn(40, 512, device=cuda_dev).bfloat16()
     part = wide[:, 128:384]
@@ -302,7 +336,7 @@ KINDS = ["random", "peaked", "equal", "rising", "falling", "masked", "lowest", "
 
 @pytest.mark.parametrize("x", ["fp32", "bf16"])
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("M,V,top", [(3, 32000, 20), (160, 8201, 64), (4, 50021, 5)])
+@pytest.mark.parametrize("M,V,top", [(3, 32000, 20), (160, 8201, 64), (4, 50021, 5), (3, 1 << 20, 64)])
 def test_logprobs(a48, cuda_dev, M, V, top, kind, x):
     rng = np.random.default_rng(V + KINDS.index(kind))
     v = torch.tensor(rows_of(kind, M, V, rng), dtype=torch.float32).to(DT[x])
