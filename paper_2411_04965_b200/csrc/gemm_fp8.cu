@@ -178,6 +178,7 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    a48_pdl_prologue();  // before tensor memory is taken, which the kernel ahead may still need
     if (warp == 1) tc_alloc<PAIR>(smem_u32(tmem_slot), TMEM_COLS);
     tc_fence_before();
     __syncthreads();
@@ -415,14 +416,14 @@ bitnet_a48_status launch(const LinearArgs& a, const ScoreArgs* score, ScoreParts
     cfg.blockDim = dim3(C::NUM_THREADS);
     cfg.dynamicSmemBytes = C::SMEM_BYTES;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    if (C::PAIR) {
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = 2;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-    }
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = C::PAIR ? 2 : 1;
     if (SCORE) {
         p.tokens = score->tokens;
         p.tokens64 = score->tokens64;

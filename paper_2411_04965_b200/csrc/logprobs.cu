@@ -145,6 +145,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
     const long long r = blockIdx.x;
     Walk<BF16, THREADS> w;
     w.row.p = reinterpret_cast<const char*>(a.x) + (size_t)(r * a.stride) * (BF16 ? 2 : 4);
+    a48_pdl_prologue();
     w.c = a.c;
     w.notes = notes + t;
     w.noted = 0;
@@ -423,8 +424,7 @@ bitnet_a48_status launch(const Args& a, int M, cudaStream_t st) {
     static std::atomic<bool> ready[64];
     A48_CUDA_TRY(a48_allow_smem(logprobs_kernel<BF16, THREADS>, (LIST_MOST + (size_t)NOTED_MOST * THREADS) * 8, ready));
     const size_t smem = a.top ? (a.list_most + (size_t)a.noted_most * THREADS) * 8 : 0;
-    logprobs_kernel<BF16, THREADS><<<M, THREADS, smem, st>>>(a);
-    A48_CUDA_TRY(cudaGetLastError());
+    A48_CUDA_TRY(a48_launch_pdl(logprobs_kernel<BF16, THREADS>, dim3(M), dim3(THREADS), smem, st, a));
     return BITNET_A48_OK;
 }
 
@@ -451,6 +451,7 @@ __global__ void __launch_bounds__(256) score_join_kernel(const float4* __restric
     const int t = threadIdx.x, row = t & 7, lane = t >> 3, m = blockIdx.x * 8 + row;
     Sums all;
     all.start(-INFINITY);
+    a48_pdl_prologue();
     if (m < M) {
 #pragma unroll 4
         for (int i = lane; i < parts; i += 32) {
@@ -480,8 +481,7 @@ __global__ void __launch_bounds__(256) score_join_kernel(const float4* __restric
 namespace a48f8 {
 
 bitnet_a48_status launch_score_join(const ScoreArgs& s, const ScoreParts& w, int M, int V, cudaStream_t st) {
-    score_join_kernel<<<(M + 7) / 8, 256, 0, st>>>(w.stats, w.parts, M, V, s.tokens, s.tokens64, s.c, s.inv_t, w.owns, s.logprob, s.entropy);
-    A48_CUDA_TRY(cudaGetLastError());
+    A48_CUDA_TRY(a48_launch_pdl(score_join_kernel, dim3((M + 7) / 8), dim3(256), 0, st, w.stats, w.parts, M, V, s.tokens, s.tokens64, s.c, s.inv_t, w.owns, s.logprob, s.entropy));
     return BITNET_A48_OK;
 }
 

@@ -134,6 +134,7 @@ __global__ void __launch_bounds__(512, 2) quant_rows_kernel(const void* __restri
     const long long row_bytes = stride * (BF16 ? 2 : 4);
     const uint32_t mask = 0xffffu << (t & 16);
     const char* at = reinterpret_cast<const char*>(X) + (long long)blockIdx.x * batch * row_bytes;
+    a48_pdl_prologue();
     Raw<BF16> next[N];
     if (NV) {
 #pragma unroll
@@ -288,6 +289,7 @@ __global__ void __launch_bounds__(512, 3) quant_weight_kernel(const void* __rest
     const int rows = k < K ? (N - n0 + 31) / 32 : 0;  // of this thread, if there were no end to the block
     const char* at = reinterpret_cast<const char*>(W) + ((size_t)n0 * stride + k) * (BF16 ? 2 : 4);
     const size_t step = (size_t)stride * 32 * (BF16 ? 2 : 4);
+    a48_pdl_prologue();
     Raw<BF16> raw[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -350,8 +352,8 @@ cudaError_t launch_rows(int threads, const void* X, long long stride, const floa
     // four rows at a time only where that leaves none of the blocks idle: fewer rows end sooner one by one
     const int most = a48f8::sm_count() * n, batch = NORM && NV && M >= BATCH_MOST * most ? BATCH_MOST : 1;
     const int batches = (M - 1) / batch + 1;
-    quant_rows_kernel<BF16, NORM, NV><<<batches < most ? batches : most, threads, 0, st>>>(X, stride, gain, eps, M, K, batch, 1.f / (float)K, codes, scale);
-    return cudaGetLastError();
+    return a48_launch_pdl(quant_rows_kernel<BF16, NORM, NV>, dim3(batches < most ? batches : most), dim3(threads), 0, st, X, stride, gain, eps, M, K, batch, 1.f / (float)K,
+                          codes, scale);
 }
 
 template <bool BF16, bool NORM>
@@ -376,9 +378,7 @@ bitnet_a48_status launch_quant_rows(const void* X, int bf16, long long stride, c
 
 bitnet_a48_status launch_quant_weight(const void* W, int bf16, long long stride, int N, int K, uint8_t* codes, float* scale, cudaStream_t st) {
     const dim3 grid((unsigned)blocks(K), (unsigned)blocks(N));
-    if (bf16) quant_weight_kernel<true><<<grid, 512, 0, st>>>(W, stride, N, K, codes, scale);
-    else quant_weight_kernel<false><<<grid, 512, 0, st>>>(W, stride, N, K, codes, scale);
-    A48_CUDA_TRY(cudaGetLastError());
+    A48_CUDA_TRY(a48_launch_pdl(bf16 ? quant_weight_kernel<true> : quant_weight_kernel<false>, grid, dim3(512), 0, st, W, stride, N, K, codes, scale));
     return BITNET_A48_OK;
 }
 

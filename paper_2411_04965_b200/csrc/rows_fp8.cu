@@ -76,6 +76,7 @@ __global__ void __launch_bounds__(32 * warps_of(NT), 1) rows_fp8_kernel(const Pa
             ++next_round;
         }
     };
+    a48_pdl_prologue();
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) load(ring[u]);
 
@@ -189,8 +190,7 @@ bitnet_a48_status launch(const LinearArgs& a, cudaStream_t st) {
         }
     }
     Params p = {a.x, a.xs, a.w, a.ws, a.y, a.y_stride, a.M, a.N, a.K, kb, a.y_bf16, split, rounds, kb * BLOCK + 64};
-    rows_fp8_kernel<NT><<<std::min(groups, sms), 32 * WARPS, smem_bytes(NT, a.K, split), st>>>(p);
-    A48_CUDA_TRY(cudaGetLastError());
+    A48_CUDA_TRY(a48_launch_pdl(rows_fp8_kernel<NT>, dim3(std::min(groups, sms)), dim3(32 * WARPS), smem_bytes(NT, a.K, split), st, p));
     return BITNET_A48_OK;
 }
 
