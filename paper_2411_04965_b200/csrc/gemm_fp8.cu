@@ -7,6 +7,7 @@
 // output features its columns: a column block of 128 shares ws, so a thread's factor for a block is one number, and a
 // block costs it one multiply-add per feature.
 #include <algorithm>
+#include <type_traits>
 
 #include "fp8.cuh"
 #include "softmax_sums.cuh"
@@ -124,21 +125,27 @@ __device__ __forceinline__ void store_rows(const float (&sum)[COLS], const Param
             if (lane == 0) tma_store_2d(tm_y, n0 + c0, m0, smem_u32(buf));
         } else {
             __syncwarp();
+            // eight rows' reads before their stores (4096 tokens, 32001 x 4096: 580 us, row by row 654)
             const int rows = min(32, p.M - m0);
-            for (int r = 0; r < rows; ++r) {
-                if (BF16) {
-                    const __nv_bfloat16* line = reinterpret_cast<const __nv_bfloat16*>(buf + r * 128);
-                    __nv_bfloat16* y = reinterpret_cast<__nv_bfloat16*>(p.y) + (size_t)(m0 + r) * p.y_stride + n0 + c0;
+            using T = typename std::conditional<BF16, __nv_bfloat16, float>::type;
+            T* y = reinterpret_cast<T*>(p.y) + (size_t)m0 * p.y_stride + n0 + c0 + lane;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
+            for (int r0 = 0; r0 < 32; r0 += 8) {
+                if (r0 >= rows) break;
+                T v[8][W / 32];
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+#pragma unroll
+                    for (int h = 0; h < W / 32; ++h) {
+                        constexpr int PIECE = 16 / sizeof(T);
                         const int i = h * 32 + lane;
-                        if (i < COLS - c0 && n0 + c0 + i < p.N) y[i] = line[((i >> 3) ^ (r & 7)) * 8 + (i & 7)];
+                        v[r][h] = reinterpret_cast<const T*>(buf + (r0 + r) * 128)[((i / PIECE) ^ r) * PIECE + i % PIECE];
                     }
-                } else {
-                    const float* line = reinterpret_cast<const float*>(buf + r * 128);
-                    if (n0 + c0 + lane < p.N)
-                        reinterpret_cast<float*>(p.y)[(size_t)(m0 + r) * p.y_stride + n0 + c0 + lane] = line[((lane >> 2) ^ (r & 7)) * 4 + (lane & 3)];
-                }
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+#pragma unroll
+                    for (int h = 0; h < W / 32; ++h)
+                        if (r0 + r < rows && h * 32 < COLS - c0 && n0 + c0 + h * 32 + lane < p.N) y[(size_t)(r0 + r) * p.y_stride + h * 32] = v[r][h];
             }
             __syncwarp();
         }
