@@ -115,12 +115,84 @@ __device__ __forceinline__ uint32_t decide(uint32_t lo, uint32_t hi, float lo_va
     return over > 0.f || (over == 0.f && !(hi & 1u)) ? hi : lo;
 }
 
+// The codes of a block of a row, eight entries v (and gains g) to each of the sixteen threads of `mask`, and its scale.  With a gain
+// that is still to be multiplied by the row's size; a block that was brought up by 2^100 waits for that as it is, with a minus
+// sign, for its scale may be a normal number although a / 448 is none.
+template <bool BF16, bool NORM>
+__device__ __forceinline__ uint2 block_codes(const float (&v)[8], const float (&g)[8], uint32_t mask, float& unit) {
+    float p[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] = NORM ? v[j] * g[j] : v[j];
+    auto largest = [&]() {
+        float a = abs_max(p, 0.f);
+#pragma unroll
+        for (int o = 8; o; o >>= 1) a = max_nan(a, __shfl_xor_sync(mask, a, o));
+        return a;
+    };
+    float a = largest(), up = 1.f;
+    const bool bad = !(a < INFINITY);
+    uint32_t c[4];
+    if (BF16 && !NORM) {
+        bf16_codes(p, a, c);
+    } else {
+        if (!bad && !middle_range(a)) {  // the same for the sixteen threads
+            up = to_middle(a);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) p[j] = v[j] * up * g[j];
+            a = largest();
+        }
+        uint32_t hi[4];
+        const bool fine = fast_codes(p, a, c, hi) || !(a > 0.f) || bad;
+        if (NORM ? __any_sync(mask, !fine) : !fine) {
+            float a_rest = 0.f;
+            if (NORM) {  // what fp32 leaves of the largest |x g|
+                a_rest = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (fabsf(p[j]) == a) a_rest = fmaxf(a_rest, copysignf(1.f, p[j]) * fmaf(v[j] * up, g[j], -p[j]));
+#pragma unroll
+                for (int o = 8; o; o >>= 1) a_rest = fmaxf(a_rest, __shfl_xor_sync(mask, a_rest, o));
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (fine || c[q] == hi[q]) continue;
+                const float2 l = of_e4m3x2(c[q]), h = of_e4m3x2(hi[q]);
+                const float r0 = NORM ? fmaf(v[2 * q] * up, g[2 * q], -p[2 * q]) : 0.f, r1 = NORM ? fmaf(v[2 * q + 1] * up, g[2 * q + 1], -p[2 * q + 1]) : 0.f;
+                c[q] = decide(c[q] & 255u, hi[q] & 255u, l.x, h.x, p[2 * q], r0, a, a_rest) |
+                       decide(c[q] >> 8, hi[q] >> 8, l.y, h.y, p[2 * q + 1], r1, a, a_rest) << 8;
+            }
+        }
+    }
+    if (bad) unit = __uint_as_float(0x7fc00000u);
+    else if (NORM) unit = up > 1.f ? -a / TOP : up < 1.f ? a / TOP / up : a * (1.f / TOP);
+    else unit = up == 1.f ? __fdiv_rn(a, TOP) : a / TOP / up;
+    return a > 0.f && !bad ? make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410)) : make_uint2(0, 0);
+}
+
+// A block's scale from `unit` and the sum of the row's squares.
+template <bool BF16>
+__device__ __forceinline__ float row_scale(float unit, float sum, const char* row, int K, float inv_k, float eps) {
+    if (unit == 0.f && sum == 0.f) return 0.f;  // whatever eps is
+    const float mean = fmaf(sum, inv_k, eps);
+    if (mean > 1e-30f && sum < 3e38f) return fabsf(unit) * rsqrtf(mean) * (unit < 0.f ? 0x1p-100f : 1.f);  // (what squares below fp32's range lose of it is 2^-149)
+    double wide = 0;  // squares outside the range: once more in 64 bits
+    for (int k = 0; k < K; k += 8) {
+        Raw<BF16> again;
+        float v[8];
+        again.load(row, k);
+        again.widen(v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) wide += (double)v[i] * (double)v[i];
+    }
+    return (float)(fabs((double)unit) * (unit < 0.f ? 0x1p-100 : 1.0) * rsqrt(wide / K + (double)eps));
+}
+
 // One token row at a time to a block of threads; thread t has entries 8 t .. 8 t + 7, and those blockDim * 8 further on.  Sixteen
 // neighbouring threads share a block of channels.  NV: how often eight entries to a thread cover the row, whose next row is then
 // under way while one is worked on (0: more often than registers are kept for).  The codes do not wait for the row's sum of
 // squares: only the scales need it, at the end, and those of `batch` rows together, so that warps wait for one another once for
-// several rows.  16384 rows of 4096 fp32 with a gain: first the sum, then the codes 94 us, row by row 88, four rows 82 (bf16: 82
-// and 76).
+// several rows.  16384 rows of 4096 fp32 with a gain: first the sum, then the codes 94 us, row by row 88, four rows 77 to 82 (bf16:
+// 82 and 75).
 constexpr int BATCH_MOST = 4;
 
 template <bool BF16, bool NORM, int NV>
@@ -165,7 +237,7 @@ __global__ void __launch_bounds__(512, 2) quant_rows_kernel(const void* __restri
             for (int i = 0; i < steps; ++i) {
                 const int k = i * span + t * 8;
                 if (k - t % 16 * 8 >= K) break;  // the same for the sixteen threads of a block of channels
-                float v[8], g[8], p[8];
+                float v[8], g[8];
                 if (NV) {
                     next[NV ? i : 0].widen(v);
                     next[NV ? i : 0].clear();
@@ -189,59 +261,12 @@ __global__ void __launch_bounds__(512, 2) quant_rows_kernel(const void* __restri
 #pragma unroll
                     for (int j = 0; j < 8; ++j) sum = fmaf(v[j], v[j], sum);
                 }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) p[j] = NORM ? v[j] * g[j] : v[j];
-                auto largest = [&]() {
-                    float a = abs_max(p, 0.f);
-#pragma unroll
-                    for (int o = 8; o; o >>= 1) a = max_nan(a, __shfl_xor_sync(mask, a, o));
-                    return a;
-                };
-                float a = largest(), up = 1.f;
-                const bool bad = !(a < INFINITY);
-                uint32_t c[4];
-                if (BF16 && !NORM) {
-                    bf16_codes(p, a, c);
-                } else {
-                    if (!bad && !middle_range(a)) {  // the same for the sixteen threads
-                        up = to_middle(a);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) p[j] = v[j] * up * g[j];
-                        a = largest();
-                    }
-                    uint32_t hi[4];
-                    const bool fine = fast_codes(p, a, c, hi) || !(a > 0.f) || bad;
-                    if (NORM ? __any_sync(mask, !fine) : !fine) {
-                        float a_rest = 0.f;
-                        if (NORM) {  // what fp32 leaves of the largest |x g|
-                            a_rest = -INFINITY;
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                if (fabsf(p[j]) == a) a_rest = fmaxf(a_rest, copysignf(1.f, p[j]) * fmaf(v[j] * up, g[j], -p[j]));
-#pragma unroll
-                            for (int o = 8; o; o >>= 1) a_rest = fmaxf(a_rest, __shfl_xor_sync(mask, a_rest, o));
-                        }
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            if (fine || c[q] == hi[q]) continue;
-                            const float2 l = of_e4m3x2(c[q]), h = of_e4m3x2(hi[q]);
-                            const float r0 = NORM ? fmaf(v[2 * q] * up, g[2 * q], -p[2 * q]) : 0.f, r1 = NORM ? fmaf(v[2 * q + 1] * up, g[2 * q + 1], -p[2 * q + 1]) : 0.f;
-                            c[q] = decide(c[q] & 255u, hi[q] & 255u, l.x, h.x, p[2 * q], r0, a, a_rest) |
-                                   decide(c[q] >> 8, hi[q] >> 8, l.y, h.y, p[2 * q + 1], r1, a, a_rest) << 8;
-                        }
-                    }
-                }
-                if (k < K)
-                    *reinterpret_cast<uint2*>(codes + (size_t)row * K + k) =
-                        a > 0.f && !bad ? make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410)) : make_uint2(0, 0);
-                if (NORM) {
-                    // times the row's size at the end; a block that was brought up by 2^100 waits for it as it is, with a minus sign,
-                    // for its scale may be a normal number although a / 448 is none
-                    const float u = bad ? __uint_as_float(0x7fc00000u) : up > 1.f ? -a / TOP : up < 1.f ? a / TOP / up : a * (1.f / TOP);
-                    if (NV && (t & 15) == 0) units[flip][row - row0][k / BLOCK] = u;
-                    else if ((t & 15) == 0 && k < K) scale[(size_t)(k / BLOCK) * M + row] = u;
-                } else if ((t & 15) == 0) {
-                    scale[(size_t)(k / BLOCK) * M + row] = bad ? __uint_as_float(0x7fc00000u) : up == 1.f ? __fdiv_rn(a, TOP) : a / TOP / up;
+                float unit;
+                const uint2 c = block_codes<BF16, NORM>(v, g, mask, unit);
+                if (k < K) *reinterpret_cast<uint2*>(codes + (size_t)row * K + k) = c;
+                if ((t & 15) == 0) {
+                    if (NORM && NV) units[flip][row - row0][k / BLOCK] = unit;
+                    else scale[(size_t)(k / BLOCK) * M + row] = unit;
                 }
             }
             if (NORM) {
@@ -258,24 +283,8 @@ __global__ void __launch_bounds__(512, 2) quant_rows_kernel(const void* __restri
             if (row >= M) continue;
             float sum = 0.f;
             for (int i = 0; i < warps; ++i) sum += part[flip][q][i];
-            float* to = scale + (size_t)b * M + row;
-            const float mean = fmaf(sum, inv_k, eps), u = NV ? units[flip][q][NV ? b : 0] : *to;
-            if (u == 0.f && sum == 0.f) {  // whatever eps is
-                *to = 0.f;
-            } else if (mean > 1e-30f && sum < 3e38f) {  // (what squares below fp32's range lose of it is 2^-149)
-                *to = fabsf(u) * rsqrtf(mean) * (u < 0.f ? 0x1p-100f : 1.f);
-            } else {  // squares outside the range: once more in 64 bits
-                double wide = 0;
-                for (int k = 0; k < K; k += 8) {
-                    Raw<BF16> again;
-                    float v[8];
-                    again.load(reinterpret_cast<const char*>(X) + row * row_bytes, k);
-                    again.widen(v);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) wide += (double)v[i] * (double)v[i];
-                }
-                *to = (float)(fabs((double)u) * (u < 0.f ? 0x1p-100 : 1.0) * rsqrt(wide / K + (double)eps));
-            }
+            const float u = NV ? units[flip][q][NV ? b : 0] : scale[(size_t)b * M + row];
+            scale[(size_t)b * M + row] = row_scale<BF16>(u, sum, reinterpret_cast<const char*>(X) + row * row_bytes, K, inv_k, eps);
         }
     }
 }
@@ -358,10 +367,13 @@ cudaError_t launch_rows(int threads, const void* X, long long stride, const floa
 
 template <bool BF16, bool NORM>
 cudaError_t launch_rows(const void* X, long long stride, const float* gain, float eps, int M, int K, uint8_t* codes, float* scale, cudaStream_t st) {
-    const int eights = (K + 7) / 8, threads = eights <= 512 ? a48_round_up(eights, 32) : 512, nv = (eights + threads - 1) / threads;
+    // (512 threads for all of more than 4096 channels left many of them without the last of their entries: 8192 x 5120 fp32 with a gain
+    // took 91 us for 72, 8192 x 8640 127 for 118)
+    const int eights = (K + 7) / 8, nv = (eights + 511) / 512, threads = nv <= 4 ? a48_round_up((eights + nv - 1) / nv, 32) : 512;
     if (nv == 1) return launch_rows<BF16, NORM, 1>(threads, X, stride, gain, eps, M, K, codes, scale, st);
     if (nv == 2) return launch_rows<BF16, NORM, 2>(threads, X, stride, gain, eps, M, K, codes, scale, st);
-    if (nv <= 4) return launch_rows<BF16, NORM, 4>(threads, X, stride, gain, eps, M, K, codes, scale, st);
+    if (nv == 3) return launch_rows<BF16, NORM, 3>(threads, X, stride, gain, eps, M, K, codes, scale, st);
+    if (nv == 4) return launch_rows<BF16, NORM, 4>(threads, X, stride, gain, eps, M, K, codes, scale, st);
     return launch_rows<BF16, NORM, 0>(threads, X, stride, gain, eps, M, K, codes, scale, st);
 }
 

@@ -46,7 +46,7 @@ def test_quant_rows(a48, cuda_dev, M, K, norm, x):
 
 
 @pytest.mark.parametrize("x", ["fp32", "bf16"])
-@pytest.mark.parametrize("M,K", [(19003, 256), (19001, 272), (4802, 2048), (2403, 4096), (2401, 8208), (2402, 11008)])
+@pytest.mark.parametrize("M,K", [(19003, 256), (19001, 272), (4802, 2048), (2403, 4096), (2401, 8208), (2402, 11008), (4001, 4112), (3701, 8208), (3601, 16384), (3601, 16400)])
 def test_quant_many_rows_are_what_few_are(a48, cuda_dev, M, K, x):
     torch.manual_seed(M)
     h = torch.randn(M, K, device=cuda_dev) * torch.logspace(-12, 12, M, device=cuda_dev)[torch.randperm(M, device=cuda_dev), None]
