@@ -115,18 +115,19 @@ __device__ __forceinline__ uint32_t decide(uint32_t lo, uint32_t hi, float lo_va
     return over > 0.f || (over == 0.f && !(hi & 1u)) ? hi : lo;
 }
 
-// The codes of a block of a row, eight entries v (and gains g) to each of the sixteen threads of `mask`, and its scale.  With a gain
+// The codes of a block of a row, eight entries v (and gains g) to each of sixteen threads, and its scale.  With a gain
 // that is still to be multiplied by the row's size; a block that was brought up by 2^100 waits for that as it is, with a minus
-// sign, for its scale may be a normal number although a / 448 is none.
+// sign, for its scale may be a normal number although a / 448 is none.  For whole warps: with masks of sixteen threads every
+// exchange costs an instruction more.
 template <bool BF16, bool NORM>
-__device__ __forceinline__ uint2 block_codes(const float (&v)[8], const float (&g)[8], uint32_t mask, float& unit) {
+__device__ __forceinline__ uint2 block_codes(const float (&v)[8], const float (&g)[8], float& unit) {
     float p[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) p[j] = NORM ? v[j] * g[j] : v[j];
     auto largest = [&]() {
         float a = abs_max(p, 0.f);
 #pragma unroll
-        for (int o = 8; o; o >>= 1) a = max_nan(a, __shfl_xor_sync(mask, a, o));
+        for (int o = 8; o; o >>= 1) a = max_nan(a, __shfl_xor_sync(0xffffffffu, a, o));
         return a;
     };
     float a = largest(), up = 1.f;
@@ -135,15 +136,16 @@ __device__ __forceinline__ uint2 block_codes(const float (&v)[8], const float (&
     if (BF16 && !NORM) {
         bf16_codes(p, a, c);
     } else {
-        if (!bad && !middle_range(a)) {  // the same for the sixteen threads
-            up = to_middle(a);
+        const bool outside = !bad && a > 0.f && !middle_range(a);  // the same for the sixteen threads
+        if (__any_sync(0xffffffffu, outside)) {
+            up = outside ? to_middle(a) : 1.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) p[j] = v[j] * up * g[j];
             a = largest();
         }
         uint32_t hi[4];
         const bool fine = fast_codes(p, a, c, hi) || !(a > 0.f) || bad;
-        if (NORM ? __any_sync(mask, !fine) : !fine) {
+        if (NORM ? __any_sync(0xffffffffu, !fine) : !fine) {
             float a_rest = 0.f;
             if (NORM) {  // what fp32 leaves of the largest |x g|
                 a_rest = -INFINITY;
@@ -151,7 +153,7 @@ __device__ __forceinline__ uint2 block_codes(const float (&v)[8], const float (&
                 for (int j = 0; j < 8; ++j)
                     if (fabsf(p[j]) == a) a_rest = fmaxf(a_rest, copysignf(1.f, p[j]) * fmaf(v[j] * up, g[j], -p[j]));
 #pragma unroll
-                for (int o = 8; o; o >>= 1) a_rest = fmaxf(a_rest, __shfl_xor_sync(mask, a_rest, o));
+                for (int o = 8; o; o >>= 1) a_rest = fmaxf(a_rest, __shfl_xor_sync(0xffffffffu, a_rest, o));
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -191,8 +193,8 @@ __device__ __forceinline__ float row_scale(float unit, float sum, const char* ro
 // neighbouring threads share a block of channels.  NV: how often eight entries to a thread cover the row, whose next row is then
 // under way while one is worked on (0: more often than registers are kept for).  The codes do not wait for the row's sum of
 // squares: only the scales need it, at the end, and those of `batch` rows together, so that warps wait for one another once for
-// several rows.  16384 rows of 4096 fp32 with a gain: first the sum, then the codes 94 us, row by row 88, four rows 77 to 82 (bf16:
-// 82 and 75).
+// several rows.  16384 rows of 4096 fp32 with a gain take 76 us, bf16 69 (first the sum, then the codes: 94 us for 88 at the time;
+// row by row: 88 for 82).
 constexpr int BATCH_MOST = 4;
 
 template <bool BF16, bool NORM, int NV>
@@ -204,7 +206,6 @@ __global__ void __launch_bounds__(512, 2) quant_rows_kernel(const void* __restri
     const int t = threadIdx.x, lane = t & 31, span = blockDim.x * 8, warps = blockDim.x >> 5;
     const int steps = NV ? NV : (K + span - 1) / span;
     const long long row_bytes = stride * (BF16 ? 2 : 4);
-    const uint32_t mask = 0xffffu << (t & 16);
     const char* at = reinterpret_cast<const char*>(X) + (long long)blockIdx.x * batch * row_bytes;
     a48_pdl_prologue();
     Raw<BF16> next[N];
@@ -236,7 +237,7 @@ __global__ void __launch_bounds__(512, 2) quant_rows_kernel(const void* __restri
 #pragma unroll
             for (int i = 0; i < steps; ++i) {
                 const int k = i * span + t * 8;
-                if (k - t % 16 * 8 >= K) break;  // the same for the sixteen threads of a block of channels
+                if (k - lane * 8 >= K) break;  // the same for a warp
                 float v[8], g[8];
                 if (NV) {
                     next[NV ? i : 0].widen(v);
@@ -262,9 +263,9 @@ __global__ void __launch_bounds__(512, 2) quant_rows_kernel(const void* __restri
                     for (int j = 0; j < 8; ++j) sum = fmaf(v[j], v[j], sum);
                 }
                 float unit;
-                const uint2 c = block_codes<BF16, NORM>(v, g, mask, unit);
+                const uint2 c = block_codes<BF16, NORM>(v, g, unit);
                 if (k < K) *reinterpret_cast<uint2*>(codes + (size_t)row * K + k) = c;
-                if ((t & 15) == 0) {
+                if ((t & 15) == 0 && k < K) {
                     if (NORM && NV) units[flip][row - row0][k / BLOCK] = unit;
                     else scale[(size_t)(k / BLOCK) * M + row] = unit;
                 }
