@@ -22,7 +22,7 @@ using a48f8::BLOCK;
 using a48f8::max_nan;
 
 constexpr float TOP = 448.f;
-constexpr float TINY = 1e-30f, HUGE_ = 1e37f;  // outside, fp32 products or quotients may leave the normal range
+constexpr float TINY = 1e-30f, HUGE_ = 5e35f;  // outside, fp32 products (448 times an entry among them) or quotients may leave the normal range
 
 __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
     unsigned short r;

@@ -202,6 +202,44 @@ def test_quant_weight_blocks_do_not_touch_one_another(a48, cuda_dev):
         assert np.all(np.abs(s - want_scale)[fine] <= 2 * U * want_scale[fine] + 2.0 ** -149)
 
 
+def borders(peak):
+    """253 entries: the numbers halfway between two codes, and the codes' own, of a block whose largest entry is `peak`."""
+    row = np.concatenate([(fp8.GRID[1:] + fp8.GRID[:-1]) / 2, fp8.GRID]) * (peak / 448.0)
+    row[::2] *= -1
+    return row
+
+
+PEAKS = [m * 2.0 ** e for e in range(-126, 128) for m in (1.75, 1.3359375)]
+
+
+@pytest.mark.parametrize("x", ["fp32", "bf16"])
+@pytest.mark.parametrize("norm", [False, True])
+def test_quant_blocks_of_every_size(a48, cuda_dev, norm, x):
+    """Codes stay exact up to the largest and down to the smallest numbers; so do those of entries halfway between two codes."""
+    v = np.zeros((len(PEAKS), 256), np.float64)
+    for row, peak in zip(v, PEAKS):
+        row[:253] = borders(peak)
+        row[127] = row[255] = peak
+    t = torch.tensor(v, dtype=torch.float32).to(DT[x])
+    codes, scale = a48.quant_fp8(t.to(cuda_dev), torch.ones(256, device=cuda_dev) if norm else None)
+    want, want_scale = fp8.quant_rows(t.double().numpy(), np.ones(256) if norm else None, float(np.float32(1e-5)))
+    assert np.array_equal(bits(codes), want)
+    check_scale(scale, want_scale, norm_tol(256) if norm else 2 * U)
+
+
+@pytest.mark.parametrize("x", ["fp32", "bf16"])
+def test_quant_weight_blocks_of_every_size(a48, cuda_dev, x):
+    peaks = PEAKS[::7]
+    w = np.zeros((128 * len(peaks), 128))
+    for i, peak in enumerate(peaks):
+        w[128 * i + 3:128 * i + 5] = np.append(borders(peak), [peak, 0, 0]).reshape(2, 128)
+    t = torch.tensor(w, dtype=torch.float32).to(DT[x])
+    codes, scale = a48.quant_fp8_weight(t.to(cuda_dev))
+    want, want_scale = fp8.quant_weight(t.double().numpy())
+    assert np.array_equal(bits(codes), want)
+    check_scale(scale, want_scale, 2 * U)
+
+
 # ------------------------------------------------------------------------------------------------ product
 def operands(M, N, K, seed=0):
     g = torch.Generator().manual_seed(seed + M * 7 + N * 3 + K)
