@@ -432,7 +432,8 @@ size_t bitnet_a48_ffn_gate_first_workspace_bytes(const bitnet_a48_weight* gate, 
 
 /* Token rows X_dev [M, K] (fp32, or bf16 with x_bf16 != 0) to codes_dev [M, K] and scale_dev.  gain_dev: NULL, or fp32 [K]:
  * the rows go through RMSNorm first, v = x * gain, and the scales are a / 448 / sqrt(mean(x^2) + norm_eps): 0 for a row of
- * zeros with any norm_eps >= 0, NaN for all of a row with a NaN.  (Products x * gain past the range of fp32 count as infinite.) */
+ * zeros with any norm_eps >= 0, NaN for all of a row with a NaN.  (Products x * gain past the range of fp32 count as infinite, and
+ * a block whose products all round to 0 in fp32 as one of zeros.) */
 bitnet_a48_status bitnet_a48_quant_fp8(const void* X_dev, long long x_stride, int x_bf16, int M, int K, const float* gain_dev,
                                        float norm_eps, uint8_t* codes_dev, float* scale_dev, void* stream);
 /* A weight W_dev [N, K] to codes_dev [N, K] and scale_dev. */

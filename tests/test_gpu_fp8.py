@@ -240,6 +240,43 @@ def test_quant_weight_blocks_of_every_size(a48, cuda_dev, x):
     check_scale(scale, want_scale, 2 * U)
 
 
+@pytest.mark.parametrize("x", ["fp32", "bf16"])
+def test_quant_gains_of_every_size(a48, cuda_dev, x):
+    """Blocks whose products are tiny or huge though an entry or its gain is neither, zeros among the gains, and gains that bring
+    all of a block's products below fp32's range (a block of zeros then)."""
+    rng = np.random.default_rng(11)
+    g = rng.uniform(0.5, 2.0, (9, 128)) * np.where(rng.random((9, 128)) < 0.3, -1, 1)
+    v = rng.standard_normal((5, 9, 128))
+    v[:, 0] *= 1e10
+    g[0] *= 1e-42          # products 1e-32
+    v[:, 1] *= 1e-33
+    v[:, 1, 5::16], g[1, 5::16] = 1e36, 0.0   # nothing but the channels without a gain are large
+    v[:, 2] *= 1e-38
+    g[2] *= 1e38
+    v[:, 3] *= 1e-38
+    g[3] *= 1e4
+    v[:, 4] *= 1e30
+    g[4] *= 5e6            # up to 3e37
+    g[5] = 0.0
+    v[:, 6] *= 1e-30
+    g[6] *= 1e-25          # products of 0 in fp32
+    g[7] = np.where(np.arange(128) % 3, 0.0, 1.0)
+    v[:, 8] *= 1e-4
+    v[:, 8, 7] = 3e8
+    g[8] *= 1e-35          # 3e8 * 2^100 would be infinite
+    t, gain = torch.tensor(v.reshape(5, -1), dtype=torch.float32).to(DT[x]), torch.tensor(g.reshape(-1), dtype=torch.float32)
+    codes, scale = a48.quant_fp8(t.to(cuda_dev), gain.to(cuda_dev), 1e-5)
+    d = t.double().numpy()
+    d[:, 6 * 128:7 * 128] = 0
+    want, want_scale = fp8.quant_rows(d, gain.double().numpy(), float(np.float32(1e-5)))
+    assert np.array_equal(bits(codes), want)
+    check_scale(scale, want_scale, norm_tol(9 * 128))
+    codes, scale = a48.quant_fp8(t[:, 128 * 8:].contiguous().to(cuda_dev), gain[128 * 8:].contiguous().to(cuda_dev), 0.0)
+    want, want_scale = fp8.quant_rows(d[:, 128 * 8:], gain[128 * 8:].double().numpy(), 0.0)
+    assert np.array_equal(bits(codes), want)
+    check_scale(scale, want_scale, norm_tol(128))
+
+
 # ------------------------------------------------------------------------------------------------ product
 def operands(M, N, K, seed=0):
     g = torch.Generator().manual_seed(seed + M * 7 + N * 3 + K)
