@@ -1,8 +1,11 @@
 // What is read off rows of logits x: with d = (x - max) / T, the log probability d_t - ln sum e^d of a given token t, its
 // place in the order of all tokens, the entropy ln sum e^d - sum e^d d / sum e^d, and the k most likely tokens.
 //
-// One pass.  A thread's sums are taken against a reference of its own (the largest logit it saw at first, moved where a
-// later one is far above it) and joined at the end, in base 2: 2^((x - r) c), c = log2 e / T.
+// One pass.  A thread's sums are taken against a reference of its own and joined at the end, in base 2: 2^((x - r) c), c = log2 e / T.
+// The reference is the largest logit so far, of the thread and of what its warp saw at first (a later one is above that once or twice
+// in a row, so moving costs nothing that can be measured).  So the row's largest logit counts as 1 exactly, and where it is all but
+// certain its log probability and the entropy keep what little the others leave of them, and their signs.  (A reference that only moved
+// for logits far above it gave 4e-6 for -4e-8.)
 //
 // The largest k.  The first segments that a block of threads visits are kept in registers; the k-th largest of the threads'
 // maxima over them bounds the row's k-th largest logit from below, and everything at or above that bound, in these segments
@@ -76,26 +79,19 @@ template <bool BF16, int THREADS>
 struct Walk {
     Row<BF16> row;
     Sums sums;
-    float c, far;          // far: logits above it move the reference
+    float c;
     float own, at_or_above;  // a logit counts as ahead of the token's from there on: `own` before the token, the next number behind it
     float least;           // logits at or above it go to the list
     int token, ahead;      // ahead: logits that come before the token's in the order
     uint2* notes;  // this thread's, THREADS apart: the logit's bits and index
     int noted, noted_most;
 
-    __device__ __forceinline__ void start(float largest) {
-        sums.start(largest);
-        far = fmaf(60.f, 1.f / c, sums.r);
-    }
     template <int N>
     __device__ __forceinline__ void take(const float (&v)[N], int id) {
         float m = v[0];
 #pragma unroll
         for (int j = 1; j < N; ++j) m = fmaxf(m, v[j]);
-        if (m > far) {
-            sums.move(m, c);
-            far = fmaf(60.f, 1.f / c, sums.r);
-        }
+        if (m > sums.r) sums.move(m, c);
 #pragma unroll
         for (int j = 0; j < N; ++j) sums.add(v[j], c);
         const float mark = id < token ? own : at_or_above;
@@ -190,7 +186,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
 #pragma unroll
         for (int j = 0; j < E; ++j) m = fmaxf(m, v[j]);
     }
-    w.start(m);
+    float first = m;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) first = fmaxf(first, __shfl_xor_sync(0xffffffffu, first, o));
+    w.sums.start(first);
     bool strict = false;
     float bound = -INFINITY;
     if (top) {

@@ -491,6 +491,30 @@ def test_logprobs_temperature(a48, cuda_dev, temperature):
     check_logprobs(a48, cuda_dev, x, torch.arange(5), 7, temperature)
 
 
+@pytest.mark.parametrize("x", ["fp32", "bf16"])
+@pytest.mark.parametrize("M,V", [(200, 32000), (100, 32000), (160, 128001)])
+def test_logprobs_of_a_token_that_is_nearly_certain(a48, cuda_dev, M, V, x):
+    """A peak anywhere in the row, 15 to 40 above the rest: no log probability above 0, no entropy below it, and errors that are small
+    beside the tail.  What is added to the peak's own 1 rounds to a unit at most for a term of that size and to the term itself below
+    (V / 256 of them in a thread, a dozen sums that are joined, a logarithm and two products); the terms' own relative errors are those of
+    `logprob_bound` and act on the tail."""
+    rng = np.random.default_rng(V + M)
+    v = rng.standard_normal((M, V))
+    at, height = rng.integers(0, V, M), rng.uniform(15, 40, M)
+    v[np.arange(M), at] = v.max(1) + height
+    v = torch.tensor(v, dtype=torch.float32).to(DT[x])
+    got = a48.logprobs(v.to(cuda_dev), torch.tensor(at).to(cuda_dev), top=2)
+    o = fp8.logprobs(v.double().numpy(), at, 2)
+    lp, ent, best = (t.double().cpu().numpy() for t in (got.logprob, got.entropy, got.top_logprobs))
+    assert np.all(lp <= 0) and np.all(ent >= 0) and np.array_equal(best[:, 0], lp)
+    tail, second = -np.expm1(o["logprob"]), np.exp(o["top_logprobs"][:, 1])
+    tol = U * 24 + V / 256 * np.minimum(U, second) + tail * U * (8 * o["spread"] + 64)
+    assert np.all(np.abs(lp - o["logprob"]) <= tol), float((np.abs(lp - o["logprob"]) / tol).max())
+    tol_ent = 2 * tol + tail * o["spread"] * U * (8 * o["spread"] + V / 256 + 64)  # the products' sum is at most tail * spread
+    assert np.all(np.abs(ent - o["entropy"]) <= tol_ent), float((np.abs(ent - o["entropy"]) / tol_ent).max())
+    assert np.array_equal(got.rank.cpu().numpy(), np.zeros(M)) and np.array_equal(got.top_ids.cpu().numpy(), o["top_ids"])
+
+
 # ------------------------------------------------------------------------------------------------ scores
 @pytest.mark.parametrize("M,N,K,x,norm,temperature", [
     (1, 32000, 256, "bf16", True, 1.0), (5, 1003, 208, "fp32", True, 0.8), (32, 500, 1040, "bf16", False, 1.0), (33, 2003, 528, "bf16", True, 1.0),
