@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
     const bool valid = all.valid();
     const float log_s = log2f(all.s), nan = __uint_as_float(0x7fc00000u);
     if (t == 0) {
-        if (a.logprob) a.logprob[r] = !valid ? nan : w.token < 0 ? 0.f : fmaf(w.own - all.r, a.inv_t, -LN2 * log_s);
+        if (a.logprob) a.logprob[r] = !valid ? nan : w.token < 0 ? 0.f : all.log_share(w.own, a.inv_t, log_s);
         if (a.entropy) a.entropy[r] = valid ? LN2 * (log_s - all.d / all.s) : nan;
         if (a.rank) a.rank[r] = valid && w.token >= 0 ? ahead : -1;
     }
@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
         for (int j = 0; j < n; ++j) place += from[j] > mine;
         if (place < a.top) {
             ids[place] = (int)~(uint32_t)mine;
-            logps[place] = fmaf(of_order((uint32_t)(mine >> 32)) - all.r, a.inv_t, -LN2 * log_s);
+            logps[place] = all.log_share(of_order((uint32_t)(mine >> 32)), a.inv_t, log_s);
         }
     }
 }
@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(256) score_join_kernel(const float4* __restric
     const long long token = tokens64 ? reinterpret_cast<const long long*>(tokens)[m] : reinterpret_cast<const int*>(tokens)[m];
     const float log_s = log2f(all.s), nan = __uint_as_float(0x7fc00000u);
     const bool taken = token >= 0 && token < V;
-    logprob[m] = !all.valid() ? nan : taken ? fmaf(owns[m] - all.r, inv_t, -LN2 * log_s) : 0.f;
+    logprob[m] = !all.valid() ? nan : taken ? all.log_share(owns[m], inv_t, log_s) : 0.f;
     entropy[m] = all.valid() ? LN2 * (log_s - all.d / all.s) : nan;
 }
 

@@ -49,6 +49,9 @@ struct Sums {
         d += o.d;
     }
     __device__ __forceinline__ bool valid() const { return s > 0.f && s < INFINITY; }
+    // ln of x's share, log_s = log2 s; halves, since numbers at both ends of the range are further apart than the largest one, which
+    // a high temperature makes a number again.
+    __device__ __forceinline__ float log_share(float x, float inv_t, float log_s) const { return fmaf(0.5f * x - 0.5f * r, 2.f * inv_t, -LN2 * log_s); }
 };
 
 }  // namespace a48f8

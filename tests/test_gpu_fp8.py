@@ -515,6 +515,26 @@ def test_logprobs_of_a_token_that_is_nearly_certain(a48, cuda_dev, M, V, x):
     assert np.array_equal(got.rank.cpu().numpy(), np.zeros(M)) and np.array_equal(got.top_ids.cpu().numpy(), o["top_ids"])
 
 
+@pytest.mark.parametrize("x", ["fp32", "bf16"])
+def test_logprobs_of_logits_further_apart_than_the_largest_number(a48, cuda_dev, x):
+    """At a temperature that makes such a difference a number again, a logit of the lowest value is still a token that can be."""
+    most = float(torch.finfo(DT[x]).max)
+    for M, V in ((3, 9000), (200, 500)):
+        v = torch.full((M, V), -most)
+        v[:, 100] = most
+        tokens = torch.arange(M) % 90
+        check_logprobs(a48, cuda_dev, v.to(DT[x]), tokens, 5, 1e30)
+    h = torch.full((40, 128), 1.0, device=cuda_dev)
+    w = torch.full((256, 128), -1.0, device=cuda_dev)
+    w[7] = 1.0
+    wc, ws = a48.quant_fp8_weight(w * 2.6e36)  # logits of 3.3e38 either way
+    for M in (5, 40):
+        lp, ent = a48.score(h[:M], None, wc, ws, torch.arange(M, device=cuda_dev), temperature=1e30)
+        logits = a48.linear_fp8(*a48.quant_fp8(h[:M]), wc, ws).double().cpu().numpy()
+        o = fp8.logprobs(logits, np.arange(M), 0, float(np.float32(1e30)))
+        assert np.all(np.abs(lp.double().cpu().numpy() - o["logprob"]) <= 8 * U * np.abs(o["logprob"])) and torch.all(ent == 0)
+
+
 # ------------------------------------------------------------------------------------------------ scores
 @pytest.mark.parametrize("M,N,K,x,norm,temperature", [
     (1, 32000, 256, "bf16", True, 1.0), (5, 1003, 208, "fp32", True, 0.8), (32, 500, 1040, "bf16", False, 1.0), (33, 2003, 528, "bf16", True, 1.0),
