@@ -6,9 +6,8 @@
 // Codes are those of exact arithmetic.  v * (448 / a) in fp32 is off by at most 5 * 2^-24 of itself (the product with the gain, a,
 // the quotient, the factor and the product, a rounding each); where it rounds to the same code with a factor 3 * 2^-23 smaller and
 // 3 * 2^-23 larger, so does the exact number.  For the others, about one in 10^5, 448 v is compared with a times the
-// border between the two codes, as sums of two fp32 numbers each (without a gain both are exact in that form, and with one where
-// the products fit into 47 bits).  In 64 bits this took registers from the rest: 95 us for 16384 rows of 4096 with a gain, even
-// out of line.  Blocks outside fp32's middle range are brought there by a power of two first.
+// border between the two codes, as sums of a few fp32 numbers each, exactly.  In 64 bits this took registers from the rest: 95 us
+// for 16384 rows of 4096 with a gain.  Blocks outside fp32's middle range are brought there by a power of two first.
 //
 // HBM bound: every input is read once, eight entries to a thread, and stays in registers.
 #include <cuda_fp16.h>
@@ -22,7 +21,8 @@ using a48f8::BLOCK;
 using a48f8::max_nan;
 
 constexpr float TOP = 448.f;
-constexpr float TINY = 1e-30f, HUGE_ = 5e35f;  // outside, fp32 products (448 times an entry among them) or quotients may leave the normal range
+// Outside, fp32 products (448 times an entry among them), quotients, or what is left of products may leave fp32's range.
+constexpr float TINY = 1e-24f, HUGE_ = 5e35f;
 
 __device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
     unsigned short r;
@@ -117,14 +117,29 @@ __device__ __forceinline__ bool fast_codes(const float (&v)[8], float a, uint32_
     }
     return differ == 0;
 }
-// Which of two codes: |v + rest| * 448 against the border between them times (a + a_rest).
+// Which of two codes: |v + rest| * 448 against the border between them times (a + a_rest), of v and a that are so near it that the
+// difference of the products' leading parts takes few bits.  It is exact, and so are the smaller products as sums of two numbers; what
+// adding them loses is kept too (Knuth's two-sum), and comes to few bits again.  So the sign is that of exact arithmetic: every
+// number here is a multiple of a * 2^-66, which TINY keeps above the smallest.
+template <bool RESTS>
 __device__ __noinline__ uint32_t decide(uint32_t lo, uint32_t hi, float v, float rest, float a, float a_rest) {
     const float2 values = of_e4m3x2(lo | hi << 8);
     const float border = 0.5f * (fabsf(values.x) + fabsf(values.y)), t = fabsf(v);
-    rest = v < 0.f ? -rest : rest;
     const float n = t * TOP, m = border * a;
-    const float low = (fmaf(t, TOP, -n) - fmaf(border, a, -m)) + fmaf(rest, TOP, -border * a_rest);
-    const float over = (n - m) + low;
+    float over = (n - m) + (fmaf(t, TOP, -n) - fmaf(border, a, -m));
+    if (RESTS) {
+        rest = v < 0.f ? -rest : rest;
+        float low = 0.f;
+        auto add = [&](float x) {
+            const float sum = over + x, of_x = sum - over;
+            low += (over - (sum - of_x)) + (x - of_x);
+            over = sum;
+        };
+        const float x = rest * TOP, y = border * a_rest;
+        add(x);
+        add(-y);
+        over += low + (fmaf(rest, TOP, -x) - fmaf(border, a_rest, -y));
+    }
     return over > 0.f || (over == 0.f && !(hi & 1u)) ? hi : lo;
 }
 
@@ -176,8 +191,8 @@ __device__ __forceinline__ uint2 block_codes(const float (&v)[8], const float (&
             for (int q = 0; q < 4; ++q) {
                 if (fine || c[q] == hi[q]) continue;
                 const float r0 = NORM ? rest(2 * q) : 0.f, r1 = NORM ? rest(2 * q + 1) : 0.f;
-                c[q] = decide(c[q] & 255u, hi[q] & 255u, p[2 * q], r0, a, a_rest) |
-                       decide(c[q] >> 8, hi[q] >> 8, p[2 * q + 1], r1, a, a_rest) << 8;
+                c[q] = decide<NORM>(c[q] & 255u, hi[q] & 255u, p[2 * q], r0, a, a_rest) |
+                       decide<NORM>(c[q] >> 8, hi[q] >> 8, p[2 * q + 1], r1, a, a_rest) << 8;
             }
         }
     }
@@ -354,7 +369,7 @@ __global__ void __launch_bounds__(512, 3) quant_weight_kernel(const void* __rest
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     if (c[q] == hi[q]) continue;
-                    c[q] = decide(c[q] & 255u, hi[q] & 255u, v[2 * q], 0.f, b, 0.f) | decide(c[q] >> 8, hi[q] >> 8, v[2 * q + 1], 0.f, b, 0.f) << 8;
+                    c[q] = decide<false>(c[q] & 255u, hi[q] & 255u, v[2 * q], 0.f, b, 0.f) | decide<false>(c[q] >> 8, hi[q] >> 8, v[2 * q + 1], 0.f, b, 0.f) << 8;
                 }
             }
         }

@@ -277,6 +277,33 @@ def test_quant_gains_of_every_size(a48, cuda_dev, x):
     check_scale(scale, want_scale, norm_tol(128))
 
 
+# Factors of a block's largest product, and x 2^e and g of one next to the border between two codes: nearer than 2^-47 of it.
+NEAR_BORDERS = [(15524161, 13731829, 15155671, -14, 11553968), (12255099, 16753811, 15555131, -1, 14613708), (16166145, 11826467, 11563907, -1, 15942728),
+                (11866993, 10753029, 14909512, -5, 12838058), (16547609, 11469091, 12663397, -10, 16592724), (12604235, 12582685, 15283787, -12, 10747286),
+                (10712629, 9457341, 12678437, -7, 13128019), (15317239, 15067483, 16015965, -11, 14924784), (14480513, 14705649, 15924659, -6, 14804770),
+                (9987623, 16761003, 16324057, -3, 13917448), (8957797, 9663743, 13162533, -6, 15971952), (12181003, 12295769, 11348118, -4, 16026393)]
+
+
+@pytest.mark.parametrize("of_x,of_gain", [(0, 0), (-64, -60), (-70, -74), (-100, -40), (-20, -149), (40, 26), (38, 38)])
+def test_quant_products_next_to_a_border(a48, cuda_dev, of_x, of_gain):
+    """Products of an entry and its gain have 48 bits, all of which may count."""
+    from fractions import Fraction
+    x, gain, want = np.zeros((len(NEAR_BORDERS), 128)), np.ones((len(NEAR_BORDERS), 128)), np.zeros((len(NEAR_BORDERS), 128), np.uint8)
+    for i, (xa, ga, xb, e, gb) in enumerate(NEAR_BORDERS):
+        x[i, [5, 6, 100]], gain[i, [5, 6, 100]] = (xa, xb * 2.0 ** e, -xb * 2.0 ** e), (ga, gb, gb)
+        t = Fraction(448 * xb * gb, xa * ga) * Fraction(2) ** e
+        off = [abs(Fraction(float(v)) - t) for v in fp8.GRID]
+        code = min(range(127), key=lambda c: (off[c], c % 2))
+        other = sorted(off)[1]
+        assert 0 < other - off[code] < other * Fraction(1, 2 ** 40)
+        want[i, [5, 6, 100]] = 126, code, code | 128
+    x, gain = x.reshape(1, -1) * 2.0 ** of_x, gain.reshape(-1) * 2.0 ** of_gain
+    t, g = torch.tensor(x, dtype=torch.float32), torch.tensor(gain, dtype=torch.float32)
+    assert np.array_equal(t.double().numpy(), x) and np.array_equal(g.double().numpy(), gain)
+    codes, _ = a48.quant_fp8(t.to(cuda_dev), g.to(cuda_dev))
+    assert np.array_equal(bits(codes).reshape(want.shape), want)
+
+
 # ------------------------------------------------------------------------------------------------ product
 def operands(M, N, K, seed=0):
     g = torch.Generator().manual_seed(seed + M * 7 + N * 3 + K)
