@@ -276,6 +276,7 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
         Sums run;  // SCORE, a single CTA with one tile of tokens: over all tiles of this CTA
         run.start(-INFINITY);
         for (int tile = unit; tile < p.tiles && ok; tile += units) {
+            __syncwarp();  // loads from tensor memory want the warp together, wherever the lanes' stores and waits went apart
             const int nt = tile / p.m_tiles, mt = tile - nt * p.m_tiles;
             const int m0 = mt * C::TM + rank * 128 + quad * 32, m = m0 + lane, n0 = nt * C::BN + sub * SUBN;
             const bool live = m0 < p.M && n0 < p.N;  // the same for the whole warp
@@ -309,6 +310,7 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
                     if (!__all_sync(0xffffffffu, there)) {
                         ok = __all_sync(0xffffffffu, there || mbar_wait_slow(bar_mine + 8 * s, ph, abort_flag, 4, it));
                         if (!ok) break;
+                        __syncwarp();
                     }
                     tc_fence_after();
                     float scale[GROUP];
@@ -349,18 +351,19 @@ __global__ void __launch_bounds__(C::NUM_THREADS, 1)
             }
             if (!ok) break;
             if (SCORE) {
-                if (m >= p.M) continue;
+                const bool row = m < p.M;
                 Sums mine;
                 mine.start(-INFINITY);
                 if (live) {
-                    const long long token = p.tokens64 ? __ldg(reinterpret_cast<const long long*>(p.tokens) + m) : __ldg(reinterpret_cast<const int*>(p.tokens) + m);
-                    mine = sums_of<SUBN>(sum, min(SUBN, p.N - n0), p.c, token - n0, p.owns + m);
+                    long long token = -1;
+                    if (row) token = p.tokens64 ? __ldg(reinterpret_cast<const long long*>(p.tokens) + m) : __ldg(reinterpret_cast<const int*>(p.tokens) + m);
+                    mine = sums_of<SUBN>(sum, min(SUBN, p.N - n0), p.c, token < 0 ? -1 : token - n0, p.owns + m);
                 }
                 if (PAIR || p.m_tiles > 1) {
-                    p.stats[(size_t)(nt * SUBS + sub) * p.M + m] = make_float4(mine.r, mine.s, mine.d, 0.f);
+                    if (row) p.stats[(size_t)(nt * SUBS + sub) * p.M + m] = make_float4(mine.r, mine.s, mine.d, 0.f);
                 } else {
                     run.join(mine, p.c);
-                    if (tile + units >= p.tiles) p.stats[(size_t)(unit * SUBS + sub) * p.M + m] = make_float4(run.r, run.s, run.d, 0.f);
+                    if (row && tile + units >= p.tiles) p.stats[(size_t)(unit * SUBS + sub) * p.M + m] = make_float4(run.r, run.s, run.d, 0.f);
                 }
             } else if (live) {
                 if (p.y_bf16) store_rows<SUBN, true>(sum, p, &tm_y, out, m0, n0, lane, stores);

@@ -613,6 +613,21 @@ def test_score_with_tokens_that_are_no_numbers(a48, cuda_dev, M):
     assert torch.equal(lp[others], clean[0][others]) and torch.equal(ent[others], clean[1][others])
 
 
+@pytest.mark.parametrize("M", [33, 97, 129, 260, 1030, 1281])
+def test_score_of_a_last_warp_that_is_not_full(a48, cuda_dev, M):
+    """Rows are scored alike whichever rows share a tile with them, over many tiles of features, the tokens in any of them."""
+    N, K = 20001, 272
+    torch.manual_seed(M)
+    h, gain = torch.randn(M, K, device=cuda_dev), torch.rand(K, device=cuda_dev) + 0.5
+    wc, ws = a48.quant_fp8_weight(torch.randn(N, K, device=cuda_dev))
+    tokens = torch.randint(N, (M,), device=cuda_dev)
+    tokens[::5] = torch.arange(N - 1, -1, -1, device=cuda_dev)[: tokens[::5].numel()]
+    lp, ent = a48.score(h, gain, wc, ws, tokens)
+    r = a48.logprobs(a48.linear_fp8(*a48.quant_fp8(h, gain), wc, ws), tokens)
+    assert a48.kernel_status()[0] == 0
+    assert torch.allclose(lp, r.logprob, rtol=0, atol=1e-4) and torch.allclose(ent, r.entropy, rtol=0, atol=1e-4)
+
+
 # ------------------------------------------------------------------------------------------------ together, streams, graphs
 def test_a_blocks_output_through_the_head(a48, cuda_dev):
     """One transformer block, then scores of a prompt and the logits of its last token: the head on what the framework computes."""
