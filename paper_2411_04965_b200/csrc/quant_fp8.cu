@@ -79,9 +79,8 @@ struct Factors {
     float v, g;
 };
 __device__ __forceinline__ Factors scaled(float v, float g, float up) { return fabsf(v) >= 1.f ? Factors{v, g * up} : Factors{v * up, g}; }
-// What fp32 leaves of that product, p.  (Rare, like `decide`, and a function out of line as that is: in line their registers cost the
-// rest, 8192 x 8640 fp32 with a gain 126 us for 101, a weight of 32000 x 4096 fp32 144 for 104.)
-__device__ __noinline__ float rest_of(float v, float g, float p, float up) {
+// What fp32 leaves of that product, p.
+__device__ __forceinline__ float rest_of(float v, float g, float p, float up) {
     const Factors f = scaled(v, g, up);
     return fmaf(f.v, f.g, -p);
 }
@@ -121,6 +120,8 @@ __device__ __forceinline__ bool fast_codes(const float (&v)[8], float a, uint32_
 // difference of the products' leading parts takes few bits.  It is exact, and so are the smaller products as sums of two numbers; what
 // adding them loses is kept too (Knuth's two-sum), and comes to few bits again.  So the sign is that of exact arithmetic: every
 // number here is a multiple of a * 2^-66, which TINY keeps above the smallest.
+// Rare, and out of line: in line its registers cost the rest (4096 x 11008 fp32 with a gain 79 us for 70, a weight of 32000 x 4096
+// fp32 144 for 104).
 template <bool RESTS>
 __device__ __noinline__ uint32_t decide(uint32_t lo, uint32_t hi, float v, float rest, float a, float a_rest) {
     const float2 values = of_e4m3x2(lo | hi << 8);
