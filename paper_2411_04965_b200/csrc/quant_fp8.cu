@@ -203,22 +203,46 @@ __device__ __forceinline__ uint2 block_codes(const float (&v)[8], const float (&
     return a > 0.f && !bad ? make_uint2(__byte_perm(c[0], c[1], 0x5410), __byte_perm(c[2], c[3], 0x5410)) : make_uint2(0, 0);
 }
 
-// A block's scale from `unit` and the sum of the row's squares.
-template <bool BF16>
-__device__ __forceinline__ float row_scale(float unit, float sum, const char* row, int K, float inv_k, float eps) {
-    if (unit == 0.f && sum == 0.f) return 0.f;  // whatever eps is
+// A block's scale from `unit` and the sum of its row's squares; false where squares lie outside of fp32's range.
+__device__ __forceinline__ bool row_scale(float unit, float sum, float inv_k, float eps, float& scale) {
     const float mean = fmaf(sum, inv_k, eps);
-    if (mean > 1e-30f && sum < 3e38f) return fabsf(unit) * rsqrtf(mean) * (unit < 0.f ? 0x1p-100f : 1.f);  // (what squares below fp32's range lose of it is 2^-149)
-    double wide = 0;  // squares outside the range: once more in 64 bits
-    for (int k = 0; k < K; k += 8) {
-        Raw<BF16> again;
-        float v[8];
-        again.load(row, k);
-        again.widen(v);
+    const bool zeros = unit == 0.f && sum == 0.f;  // whatever eps is
+    scale = zeros ? 0.f : fabsf(unit) * rsqrtf(mean) * (unit < 0.f ? 0x1p-100f : 1.f);  // (what squares below fp32's range lose of it is 2^-149)
+    return zeros || !(mean <= 1e-30f || sum >= 3e38f);  // (a sum that is no number stays none)
+}
+// The scales of a warp's blocks for which that was false, with the squares in 64 bits: once for each of the rows among them, by all of
+// the warp's threads.  64 rows of 16384 fp32 with one such row take 15 us, without 10; 147 where each block's thread added them alone.
+template <bool BF16>
+__device__ __noinline__ void wide_scales(const char* X, long long row_bytes, int row0, int batch, int M, int K, float inv_k, float eps, const float (*part)[16],
+                                         const float* units, int units_row, int warps, float* scale) {
+    const int lane = threadIdx.x & 31, most = batch * ((K + BLOCK - 1) / BLOCK);
+    for (int j0 = threadIdx.x - lane; j0 < most; j0 += blockDim.x) {
+        const int j = j0 + lane, b = j / batch, q = j - b * batch, row = row0 + q;
+        float unit = 0.f, sum = 0.f, s;
+        if (j < most && row < M) {
+            for (int i = 0; i < warps; ++i) sum += part[q][i];
+            unit = units ? units[q * units_row + b] : scale[(size_t)b * M + row];
+        }
+        bool odd = !row_scale(unit, sum, inv_k, eps, s) && j < most && row < M;
+        for (uint32_t left; (left = __ballot_sync(0xffffffffu, odd));) {
+            const int of = __shfl_sync(0xffffffffu, row, __ffs(left) - 1);
+            double wide = 0;
+            for (int k = lane * 8; k < K; k += 256) {
+                Raw<BF16> again;
+                float v[8];
+                again.load(X + of * row_bytes, k);
+                again.widen(v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) wide += (double)v[i] * (double)v[i];
+                for (int i = 0; i < 8; ++i) wide += (double)v[i] * (double)v[i];
+            }
+#pragma unroll
+            for (int o = 16; o; o >>= 1) wide += __shfl_xor_sync(0xffffffffu, wide, o);
+            if (odd && row == of) {
+                scale[(size_t)b * M + row] = (float)(fabs((double)unit) * (unit < 0.f ? 0x1p-100 : 1.0) * rsqrt(wide / K + (double)eps));
+                odd = false;
+            }
+        }
     }
-    return (float)(fabs((double)unit) * (unit < 0.f ? 0x1p-100 : 1.0) * rsqrt(wide / K + (double)eps));
 }
 
 // One token row at a time to a block of threads; thread t has entries 8 t .. 8 t + 7, and those blockDim * 8 further on.  Sixteen
@@ -311,14 +335,19 @@ __global__ void __launch_bounds__(512, 2) quant_rows_kernel(const void* __restri
         if (!NORM) continue;
         __syncthreads();
         const int blocks = (K + BLOCK - 1) / BLOCK;
+        bool odd = false;
         for (int j = t; j < batch * blocks; j += blockDim.x) {
             const int b = j / batch, q = j - b * batch, row = row0 + q;
             if (row >= M) continue;
-            float sum = 0.f;
+            float sum = 0.f, s;
             for (int i = 0; i < warps; ++i) sum += part[flip][q][i];
             const float u = NV ? units[flip][q][NV ? b : 0] : scale[(size_t)b * M + row];
-            scale[(size_t)b * M + row] = row_scale<BF16>(u, sum, reinterpret_cast<const char*>(X) + row * row_bytes, K, inv_k, eps);
+            if (row_scale(u, sum, inv_k, eps, s)) scale[(size_t)b * M + row] = s;
+            else odd = true;
         }
+        if (__any_sync(0xffffffffu, odd))
+            wide_scales<BF16>(reinterpret_cast<const char*>(X), row_bytes, row0, batch, M, K, inv_k, eps, part[flip], NV ? units[flip][0] : nullptr,
+                              (int)(sizeof units[0][0] / sizeof(float)), warps, scale);
     }
 }
 

@@ -304,6 +304,42 @@ def test_quant_products_next_to_a_border(a48, cuda_dev, of_x, of_gain):
     assert np.array_equal(bits(codes).reshape(want.shape), want)
 
 
+def least_time(call, n=12):
+    """Least of n times in us, the call replayed from a graph."""
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    times = []
+    for _ in range(n):
+        begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        torch.cuda.synchronize()
+        begin.record()
+        graph.replay()
+        end.record()
+        torch.cuda.synchronize()
+        times.append(begin.elapsed_time(end) * 1e3)
+    return min(times)
+
+
+@pytest.mark.parametrize("x", ["fp32", "bf16"])
+@pytest.mark.parametrize("K", [4096, 16384, 20000])
+def test_quant_rows_whose_squares_are_out_of_range_hold_nobody_up(a48, cuda_dev, K, x):
+    """The squares of such a row are added once more in 64 bits, by many threads at once (by one for each block of channels the
+    call took tens of times as long); those of a row with a NaN are not."""
+    h, gain = torch.randn(64, K, device=cuda_dev).to(DT[x]), torch.ones(K, device=cuda_dev)
+    codes, scale = torch.empty(64, K, dtype=torch.float8_e4m3fn, device=cuda_dev), torch.empty((K + 127) // 128, 64, device=cuda_dev)
+    usual = least_time(lambda: a48.quant_fp8(h, gain, codes=codes, scale=scale))
+    for odd, most in ((float("nan"), 1.5), (1e25, 4.0), (float("inf"), 4.0)):
+        h[9, 100] = odd
+        assert least_time(lambda: a48.quant_fp8(h, gain, codes=codes, scale=scale)) <= most * usual + 2.0, odd
+        want, want_scale = fp8.quant_rows(h.double().cpu().numpy(), np.ones(K), float(np.float32(1e-5)))
+        if odd == float("inf"):
+            want_scale[1:, 9] = 0
+        assert np.array_equal(bits(codes), want)
+        check_scale(scale, want_scale if odd == odd else np.where(np.arange(64) == 9, np.nan, want_scale), norm_tol(K))
+
+
 # ------------------------------------------------------------------------------------------------ product
 def operands(M, N, K, seed=0):
     g = torch.Generator().manual_seed(seed + M * 7 + N * 3 + K)
