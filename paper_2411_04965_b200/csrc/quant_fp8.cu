@@ -116,19 +116,18 @@ __device__ __forceinline__ bool fast_codes(const float (&v)[8], float a, uint32_
     }
     return differ == 0;
 }
-// Which of two codes: |v + rest| * 448 against the border between them times (a + a_rest), of v and a that are so near it that the
-// difference of the products' leading parts takes few bits.  It is exact, and so are the smaller products as sums of two numbers; what
-// adding them loses is kept too (Knuth's two-sum), and comes to few bits again.  So the sign is that of exact arithmetic: every
-// number here is a multiple of a * 2^-66, which TINY keeps above the smallest.
-// Rare, and out of line: in line its registers cost the rest (4096 x 11008 fp32 with a gain 79 us for 70, a weight of 32000 x 4096
-// fp32 144 for 104).
+// Whether 448 |v + rest| lies beyond the border between a code and the next, times (a + a_rest): the next one's code then, or on the
+// border the even one's.  For v and a that are so near it, the difference of the products' leading parts is exact in few bits, and so are
+// what fp32 leaves of them and the sum.  The smaller products are exact as sums of two numbers each; what adding them loses is kept too
+// (Knuth's two-sum), and comes to few bits again.  So the sign is that of exact arithmetic: every number here is a multiple of
+// a * 2^-66, which TINY keeps above the smallest.
 template <bool RESTS>
-__device__ __noinline__ uint32_t decide(uint32_t lo, uint32_t hi, float v, float rest, float a, float a_rest) {
-    const float2 values = of_e4m3x2(lo | hi << 8);
+__device__ __forceinline__ uint32_t decide(uint32_t code, float v, float rest, float a, float a_rest) {
+    const float2 values = of_e4m3x2(code | (code + 1) << 8);
     const float border = 0.5f * (fabsf(values.x) + fabsf(values.y)), t = fabsf(v);
     const float n = t * TOP, m = border * a;
     float over = (n - m) + (fmaf(t, TOP, -n) - fmaf(border, a, -m));
-    if (RESTS) {
+    if (RESTS && (rest != 0.f || a_rest != 0.f)) {
         rest = v < 0.f ? -rest : rest;
         float low = 0.f;
         auto add = [&](float x) {
@@ -141,7 +140,34 @@ __device__ __noinline__ uint32_t decide(uint32_t lo, uint32_t hi, float v, float
         add(-y);
         over += low + (fmaf(rest, TOP, -x) - fmaf(border, a_rest, -y));
     }
-    return over > 0.f || (over == 0.f && !(hi & 1u)) ? hi : lo;
+    return code + (over > 0.f || (over == 0.f && (code & 1u)));
+}
+__device__ __forceinline__ float pick(const float (&x)[8], int e) {
+    float r = x[0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) r = e == j ? x[j] : r;
+    return r;
+}
+// Decides where the codes with the smaller and the larger factor, neighbours then, differ: one entry of a thread at a time, which is
+// little code (in line for all eight it overflowed the instruction cache where entries on a border are frequent).  rest(e, v): what
+// fp32 leaves of entry e, v.
+template <bool RESTS, class Rest>
+__device__ __forceinline__ void settle(uint32_t (&c)[4], const uint32_t (&hi)[4], const float (&p)[8], float a, float a_rest, Rest rest) {
+    uint32_t todo = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t d = c[q] ^ hi[q];
+        todo |= ((d & 255u) ? 1u << 2 * q : 0u) | ((d >> 8) ? 2u << 2 * q : 0u);
+    }
+#pragma unroll 1
+    for (; todo; todo &= todo - 1) {
+        const int e = __ffs(todo) - 1, shift = e & 1 ? 8 : 0;
+        const uint32_t pair = e < 4 ? (e < 2 ? c[0] : c[1]) : (e < 6 ? c[2] : c[3]), code = pair >> shift & 255u;
+        const float v = pick(p, e);
+        const uint32_t up = (decide<RESTS>(code, v, RESTS ? rest(e, v) : 0.f, a, a_rest) - code) << shift;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) c[q] += e >> 1 == q ? up : 0u;
+    }
 }
 
 // The codes of a block of a row, eight entries v (and gains g) to each of sixteen threads, and its scale.  With a gain
@@ -178,23 +204,22 @@ __device__ __forceinline__ uint2 block_codes(const float (&v)[8], const float (&
         uint32_t hi[4];
         const bool fine = fast_codes(p, a, c, hi) || !(a > 0.f) || bad;
         if (NORM ? __any_sync(0xffffffffu, !fine) : !fine) {
-            auto rest = [&](int j) { return rest_of(v[j], g[j], p[j], up); };
             float a_rest = 0.f;
-            if (NORM) {  // of the largest |x g|
-                a_rest = -INFINITY;
+            bool rests = false;  // none with gains of 1 or of eight bits, where entries on a border are frequent
+            if (NORM) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) rests |= fmaf(v[j], g[j], -p[j]) != 0.f;  // (not 0 either where p is scaled)
+                rests = __any_sync(0xffffffffu, rests);
+            }
+            if (rests) {
+                a_rest = -INFINITY;  // of the largest |x g|
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
-                    if (fabsf(p[j]) == a) a_rest = fmaxf(a_rest, copysignf(1.f, p[j]) * rest(j));
+                    if (fabsf(p[j]) == a) a_rest = fmaxf(a_rest, copysignf(1.f, p[j]) * rest_of(v[j], g[j], p[j], up));
 #pragma unroll
                 for (int o = 8; o; o >>= 1) a_rest = fmaxf(a_rest, __shfl_xor_sync(0xffffffffu, a_rest, o));
             }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (fine || c[q] == hi[q]) continue;
-                const float r0 = NORM ? rest(2 * q) : 0.f, r1 = NORM ? rest(2 * q + 1) : 0.f;
-                c[q] = decide<NORM>(c[q] & 255u, hi[q] & 255u, p[2 * q], r0, a, a_rest) |
-                       decide<NORM>(c[q] >> 8, hi[q] >> 8, p[2 * q + 1], r1, a, a_rest) << 8;
-            }
+            if (!fine) settle<NORM>(c, hi, p, a, a_rest, [&](int e, float x) { return rests ? rest_of(pick(v, e), pick(g, e), x, up) : 0.f; });
         }
     }
     if (bad) unit = __uint_as_float(0x7fc00000u);
@@ -395,13 +420,7 @@ __global__ void __launch_bounds__(512, 3) quant_weight_kernel(const void* __rest
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] *= up;
             uint32_t hi[4];
-            if (!fast_codes(v, b, c, hi)) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    if (c[q] == hi[q]) continue;
-                    c[q] = decide<false>(c[q] & 255u, hi[q] & 255u, v[2 * q], 0.f, b, 0.f) | decide<false>(c[q] >> 8, hi[q] >> 8, v[2 * q + 1], 0.f, b, 0.f) << 8;
-                }
-            }
+            if (!fast_codes(v, b, c, hi)) settle<false>(c, hi, v, b, 0.f, [](int, float) { return 0.f; });
         }
         if (i < rows)
             *reinterpret_cast<uint2*>(to + (size_t)i * 32 * K) =
