@@ -459,8 +459,9 @@ bitnet_a48_status bitnet_a48_logprobs(const void* logits_dev, long long stride, 
                                       int32_t* rank_dev, int top, int32_t* top_ids_dev, float* top_logprobs_dev, void* stream);
 
 /* From hidden states X_dev [M, K] to logprob and entropy as bitnet_a48_logprobs gives them for the logits that
- * bitnet_a48_quant_fp8 (with this gain) and bitnet_a48_linear_fp8 give, which are never stored: perplexity, likelihoods of
- * endings.  workspace_dev: bitnet_a48_score_workspace_bytes bytes (0 for sizes that are not supported), no need to clear it. */
+ * bitnet_a48_quant_fp8 (with this gain) and bitnet_a48_linear_fp8 give: perplexity, likelihoods of endings.  The logits of few
+ * rows (at most 32) pass through the workspace; those of more are never stored.  workspace_dev: bitnet_a48_score_workspace_bytes
+ * bytes (0 for sizes that are not supported), no need to clear it. */
 size_t bitnet_a48_score_workspace_bytes(int M, int N, int K);
 bitnet_a48_status bitnet_a48_score(const void* X_dev, long long x_stride, int x_bf16, int M, const float* gain_dev, float norm_eps,
                                    const uint8_t* w_codes_dev, const float* w_scale_dev, int N, int K, float temperature,

@@ -739,7 +739,7 @@ def score_workspace_bytes(M: int, N: int, K: int) -> int:
 def score(X: torch.Tensor, gain, w_codes: torch.Tensor, w_scale: torch.Tensor, tokens: torch.Tensor, norm_eps: float = 1e-5,
           temperature: float = 1.0, workspace=None, stream=None):
     """(log probability of the given tokens, entropy), fp32 [M] each, of the logits that hidden states X [M, K] have after RMSNorm (or
-    none: gain None) and the 8-bit head; no logits are stored."""
+    none: gain None) and the 8-bit head; logits are stored, in the workspace, of few rows (at most 32) only."""
     st = _on_stream(X, stream)
     if st is None:
         with _made_current(X, stream):

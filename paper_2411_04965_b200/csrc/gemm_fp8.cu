@@ -472,7 +472,10 @@ int sm_count() {
 // 4096 x 4096; the model picked the fastest of the three in 13 of 14 of them, e.g. 64 tokens x 32000 x 3200: 29, 26, 35 us,
 // 64 x 4096 x 4096: 12, 16, 24 us, 512 x 32000 x 3200: 103, 83, 80 us).
 enum Form { NARROW, WIDE, PAIRED };
-constexpr int kMostSingle = 1024;  // tokens; beyond, the pairs' tiles fill the GPU
+// Tokens beyond which only pairs are taken, which bounds the workspace of a score; score_stats counts on it.  Their tiles fill the GPU
+// then, but not where features are few: 4096 x 128 x 4096 takes 19 us so (10 by the model), 4096 x 512 20 (13.6), 2048 x 1024 20 (13.4);
+// from 2000 features on the two are the same.
+constexpr int kMostSingle = 1024;
 
 Form form_of(int M, int N) {
     const long long sms = sm_count(), m1 = (M + 127) / 128, m2 = (M + 255) / 256;

@@ -9,7 +9,8 @@
 // border between the two codes, as sums of a few fp32 numbers each, exactly.  In 64 bits this took registers from the rest: 95 us
 // for 16384 rows of 4096 with a gain.  Blocks outside fp32's middle range are brought there by a power of two first.
 //
-// HBM bound: every input is read once, eight entries to a thread, and stays in registers.
+// Every input is read once, eight entries to a thread, and stays in registers.  With a gain instructions bound it (28 an entry, 62% of
+// the issue slots with DRAM at 44%), without one memory does nearly (16384 x 4096 fp32 55 us, the bytes alone 51).
 #include <cuda_fp16.h>
 
 #include "fp8.cuh"
@@ -274,7 +275,7 @@ __device__ __noinline__ void wide_scales(const char* X, long long row_bytes, int
 // neighbouring threads share a block of channels.  NV: how often eight entries to a thread cover the row, whose next row is then
 // under way while one is worked on (0: more often than registers are kept for).  The codes do not wait for the row's sum of
 // squares: only the scales need it, at the end, and those of `batch` rows together, so that warps wait for one another once for
-// several rows.  16384 rows of 4096 fp32 with a gain take 76 us, bf16 69 (first the sum, then the codes: 94 us for 88 at the time;
+// several rows.  16384 rows of 4096 fp32 with a gain take 74 us, bf16 70 (first the sum, then the codes: 94 us for 88 at the time;
 // row by row: 88 for 82).
 constexpr int BATCH_MOST = 4;
 
@@ -448,7 +449,7 @@ cudaError_t launch_rows(int threads, const void* X, long long stride, const floa
 template <bool BF16, bool NORM>
 cudaError_t launch_rows(const void* X, long long stride, const float* gain, float eps, int M, int K, uint8_t* codes, float* scale, cudaStream_t st) {
     // (512 threads for all of more than 4096 channels left many of them without the last of their entries: 8192 x 5120 fp32 with a gain
-    // took 91 us for 72, 8192 x 8640 127 for 118)
+    // took 91 us for 72, 8192 x 8640 127 for 118, now 110)
     const int eights = (K + 7) / 8, nv = (eights + 511) / 512, threads = nv <= 4 ? a48_round_up((eights + nv - 1) / nv, 32) : 512;
     if (nv == 1) return launch_rows<BF16, NORM, 1>(threads, X, stride, gain, eps, M, K, codes, scale, st);
     if (nv == 2) return launch_rows<BF16, NORM, 2>(threads, X, stride, gain, eps, M, K, codes, scale, st);

@@ -1,4 +1,4 @@
-// PTX forms shared by the kernels of the 8-bit head: mbarriers with bounded waits, tensor copies, tcgen05.
+// PTX forms of the 8-bit product: mbarriers with bounded waits, tensor copies, tcgen05.
 #pragma once
 
 #include <cuda.h>
@@ -15,9 +15,6 @@ __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)_
 
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 // Address, in the cluster's shared window, of this CTA's shared-memory address `addr` in the CTA of rank `rank`.
 __device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank) {
