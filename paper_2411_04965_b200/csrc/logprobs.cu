@@ -79,6 +79,7 @@ template <bool BF16, int THREADS>
 struct Walk {
     Row<BF16> row;
     Sums sums;
+    float fresh;  // terms that are not in sums.s yet: beside a 1 there they would be lost one by one, and together are not
     float c;
     float own, at_or_above;  // a logit counts as ahead of the token's from there on: `own` before the token, the next number behind it
     float least;           // logits at or above it go to the list
@@ -86,14 +87,21 @@ struct Walk {
     uint2* notes;  // this thread's, THREADS apart: the logit's bits and index
     int noted, noted_most;
 
+    __device__ __forceinline__ void fold() {
+        sums.s += fresh;
+        fresh = 0.f;
+    }
     template <int N>
     __device__ __forceinline__ void take(const float (&v)[N], int id) {
         float m = v[0];
 #pragma unroll
         for (int j = 1; j < N; ++j) m = fmaxf(m, v[j]);
-        if (m > sums.r) sums.move(m, c);
+        if (m > sums.r) {
+            fold();
+            sums.move(m, c);
+        }
 #pragma unroll
-        for (int j = 0; j < N; ++j) sums.add(v[j], c);
+        for (int j = 0; j < N; ++j) sums.add(v[j], c, fresh);
         const float mark = id < token ? own : at_or_above;
         if (m >= mark) {
 #pragma unroll
@@ -190,6 +198,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
 #pragma unroll
     for (int o = 16; o; o >>= 1) first = fmaxf(first, __shfl_xor_sync(0xffffffffu, first, o));
     w.sums.start(first);
+    w.fresh = 0.f;
     bool strict = false;
     float bound = -INFINITY;
     if (top) {
@@ -248,6 +257,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
         seg -= seg >= segments ? segments : 0;
     }
     if (edge >= 0) w.take(edge_x, edge);
+    w.fold();
     for (int i = SAMPLE; i < segments; i += 4) {
         uint4 u[4];
         int id[4];
@@ -266,6 +276,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == MANY ? 4 : 1) logprobs_ker
             Row<BF16>::widen(u[q], v);
             w.take(v, head + id[q] * E);
         }
+        w.fold();
     }
     if (t == 0 && w.token >= head && w.token < tail && (w.token - head) % E != 0)  // in the token's own 16 bytes, equal ones from it on do not count
         for (int i = w.token; i < min(tail, head + (w.token - head) / E * E + E); ++i) w.ahead -= w.row.at(i) == w.own;

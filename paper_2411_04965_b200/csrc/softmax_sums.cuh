@@ -29,10 +29,12 @@ struct Sums {
         r = fminf(fmaxf(largest, -FLT_MAX), FLT_MAX);
         s = d = 0.f;
     }
-    __device__ __forceinline__ void add(float x, float c) {
+    __device__ __forceinline__ void add(float x, float c) { add(x, c, s); }
+    // The same with the term of s to a sum that is added to s later.
+    __device__ __forceinline__ void add(float x, float c, float& to) {
         const float t = max_nan((x - r) * c, -150.f);  // 2^t is 0 from there on, and 0 times -inf would be no number
         const float e = exp2_approx(t);
-        s += e;
+        to += e;
         d = fmaf(e, t, d);
     }
     __device__ __forceinline__ void move(float to, float c) {  // to another reference

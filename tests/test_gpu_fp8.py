@@ -579,6 +579,21 @@ def test_logprobs_of_a_token_that_is_nearly_certain(a48, cuda_dev, M, V, x):
 
 
 @pytest.mark.parametrize("x", ["fp32", "bf16"])
+def test_logprobs_keeps_a_tail_of_terms_that_are_nothing_beside_the_peak(a48, cuda_dev, x):
+    """Each of a million equal logits 17.5 below the peak is less than half a unit beside its 1.  Sixteen terms or more of a thread are
+    added together: V / 4096 roundings of half a unit (U) at most, and a few dozen of sums that are joined."""
+    M, V, below = 160, 1 << 20, 17.5
+    v = torch.zeros(M, V, dtype=DT[x], device=cuda_dev)
+    at = torch.arange(M, device=cuda_dev) * 6001
+    v[torch.arange(M, device=cuda_dev), at] = below
+    got = a48.logprobs(v, at)
+    tail = (V - 1) * np.exp(-below)
+    assert np.all(np.abs(got.logprob.double().cpu().numpy() + np.log1p(tail)) <= U * (V / 4096 + 64 + tail * 8 * below))
+    entropy = np.log1p(tail) + tail * below / (1 + tail)  # the sum of its products has V / 256 roundings in a thread
+    assert np.all(np.abs(got.entropy.double().cpu().numpy() - entropy) <= U * (V / 4096 + 64 + tail * below * (8 * below + V / 256 + 64)))
+
+
+@pytest.mark.parametrize("x", ["fp32", "bf16"])
 def test_logprobs_of_logits_further_apart_than_the_largest_number(a48, cuda_dev, x):
     """At a temperature that makes such a difference a number again, a logit of the lowest value is still a token that can be."""
     most = float(torch.finfo(DT[x]).max)
