@@ -79,9 +79,15 @@ __device__ __forceinline__ Sums sums_of(const float (&sum)[COLS], int cols, floa
     for (int c = 0; c < COLS; ++c)
         if (c < cols) top = fmaxf(top, sum[c]);
     s.start(top);
+    float sixteen = 0.f;  // together, since one by one small terms are lost beside the largest one's 1
 #pragma unroll
-    for (int c = 0; c < COLS; ++c)
-        if (c < cols) s.add(sum[c], c2);
+    for (int c = 0; c < COLS; ++c) {
+        if (c < cols) s.add(sum[c], c2, sixteen);
+        if (c % 16 == 15) {
+            s.s += sixteen;
+            sixteen = 0.f;
+        }
+    }
     if (token_at >= 0 && token_at < cols) {
 #pragma unroll
         for (int c = 0; c < COLS; ++c)

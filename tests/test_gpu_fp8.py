@@ -679,6 +679,20 @@ def test_score_of_a_last_warp_that_is_not_full(a48, cuda_dev, M):
     assert torch.allclose(lp, r.logprob, rtol=0, atol=1e-4) and torch.allclose(ent, r.entropy, rtol=0, atol=1e-4)
 
 
+@pytest.mark.parametrize("M", [20, 100, 300, 1300])
+def test_score_keeps_a_tail_of_terms_that_are_nothing_beside_the_peak(a48, cuda_dev, M):
+    """One logit of 17.5, ahead of the others in its tile, among zeros.  At most 15 terms of less than half a unit (U) are lost beside its 1, and what is joined with it is
+    rounded some 25 times."""
+    N, K, below = 32000, 128, 17.5
+    w = torch.zeros(N, K, device=cuda_dev)
+    w[12288] = below / K
+    lp, ent = a48.score(torch.ones(M, K, device=cuda_dev), None, *a48.quant_fp8_weight(w), torch.full((M,), 12288, device=cuda_dev))
+    tail = (N - 1) * np.exp(-below)
+    assert np.all(np.abs(lp.double().cpu().numpy() + np.log1p(tail)) <= U * (40 + tail * 16 * below))
+    entropy = np.log1p(tail) + tail * below / (1 + tail)
+    assert np.all(np.abs(ent.double().cpu().numpy() - entropy) <= U * (40 + tail * below * (16 * below + 256)))
+
+
 # ------------------------------------------------------------------------------------------------ together, streams, graphs
 def test_a_blocks_output_through_the_head(a48, cuda_dev):
     """One transformer block, then scores of a prompt and the logits of its last token: the head on what the framework computes."""
