@@ -9,8 +9,8 @@
 // border between the two codes, as sums of a few fp32 numbers each, exactly.  In 64 bits this took registers from the rest: 95 us
 // for 16384 rows of 4096 with a gain.  Blocks outside fp32's middle range are brought there by a power of two first.
 //
-// Every input is read once, eight entries to a thread, and stays in registers.  With a gain instructions bound it (28 an entry, 62% of
-// the issue slots with DRAM at 44%), without one memory does nearly (16384 x 4096 fp32 55 us, the bytes alone 51).
+// Every input is read once, eight entries to a thread, and stays in registers.  With a gain instructions bound it (29 an entry, 65% of
+// the issue slots with DRAM at 45%), without one memory does nearly (16384 x 4096 fp32 55 us, the bytes alone 51).
 #include <cuda_fp16.h>
 
 #include "fp8.cuh"
