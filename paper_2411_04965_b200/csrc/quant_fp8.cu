@@ -150,8 +150,8 @@ __device__ __forceinline__ float pick(const float (&x)[8], int e) {
     return r;
 }
 // Decides where the codes with the smaller and the larger factor, neighbours then, differ: one entry of a thread at a time, which is
-// little code (in line for all eight it overflowed the instruction cache where entries on a border are frequent).  rest(e, v): what
-// fp32 leaves of entry e, v.
+// little code: 8192 x 8640 bf16 with a gain of ones, where entries on a border are frequent, take 102 us (in line for all eight 195, a
+// function for each 140).  rest(e, v): what fp32 leaves of entry e, v.
 template <bool RESTS, class Rest>
 __device__ __forceinline__ void settle(uint32_t (&c)[4], const uint32_t (&hi)[4], const float (&p)[8], float a, float a_rest, Rest rest) {
     uint32_t todo = 0;
